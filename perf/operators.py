@@ -284,7 +284,7 @@ def run(s):
                        positions=s["new_positions"], tree=s["tree"], softcap=s["softcap"], slopes=s["slopes"], lse=s["lse"],
                        accumulate=kind == "decode")
         if kind in ("weigh", "step"):
-            ctx.weigh(cache, s["q"], s["scale"], s["lse"], s["accepted"], ws, tree=s["tree"], softcap=s["softcap"],
+            ctx.weigh(cache, s["q"], s["scale"], s["lse"], s["accepted"], tree=s["tree"], softcap=s["softcap"],
                       slopes=s["slopes"])
         if kind == "evict":
             ctx.append(cache, s["k_new"], s["v_new"], s["new_positions"])
