@@ -472,6 +472,122 @@ structkv_status structkv_mass_recovery(structkv_ctx* ctx, const float* scores, l
                                        void* stream);
 
 /*
+ * Decoding over a compacted cache.  The paper stops where the cache is compacted; these calls go on from there: attention of the
+ * tokens that come next (one a sequence, a few, or a tree of drafted ones), the attention weight that cached tokens gather, and
+ * eviction by it.  n_q_heads, n_kv_heads, head_dim and dtype are the context's (its window and max_seq do not matter here);
+ * G = H / H_kv query heads read a KV head.
+ *
+ * A cache holds, for every (sequence b, KV head g), lengths[b, g] tokens in slots 0 .. lengths[b, g] - 1, in any order; every
+ * token has the position it has in its prompt.  A caller that keeps all layers in one allocation may count a layer as more
+ * sequences (append, commit and evict then serve all layers in one launch).
+ *   k, v        device, element (b, g, slot, c) at k + b*stride_batch + g*stride_head + slot*stride_token + c (elements; d
+ *               contiguous; bases 16-byte aligned, strides multiples of 16 bytes; sequences, heads and slots do not overlap).
+ *   positions   device, [batch, H_kv, capacity] int32, not negative.
+ *   weights     device, [batch, H_kv, capacity] fp32, or NULL where nothing is accumulated or evicted.
+ *   lengths     device, [batch, H_kv] int32.  The calls read it on the device: one that is negative or leaves no room for the new
+ *               tokens records STRUCTKV_ERR_INVALID_ARG in the device status word, and nothing of that KV head is read or written.
+ * Calls on one cache are ordered by the caller (one stream).  All of them can be captured into graphs.  The context's device has
+ * to be current.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  long long stride_batch, stride_head, stride_token;
+  int* positions;
+  float* weights;
+  int* lengths;
+  int batch, capacity;
+} structkv_cache;
+
+#define STRUCTKV_MAX_NEW 64 /* new tokens of a sequence in one call */
+
+/* Rows of new tokens: element (b, i, g, c) at k + b*stride_batch + i*stride_token + g*stride_head + c (16-byte aligned, strides
+ * multiples of 16 bytes, any order, 0 for a dimension that is broadcast); positions device, [batch, n_new] int32 contiguous. */
+typedef struct {
+  const void* k;
+  const void* v;
+  long long stride_batch, stride_token, stride_head;
+  const int* positions;
+} structkv_new_rows;
+
+/*
+ * Writes the rows of n_new (1 .. 64) new tokens a sequence to slots lengths .. lengths + n_new - 1, their positions, and weight
+ * 0.  `lengths` stays: the tokens count once they are committed.  Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
+ */
+structkv_status structkv_append(structkv_ctx* ctx, const structkv_cache* cache, const structkv_new_rows* rows, int n_new,
+                                void* stream);
+
+/*
+ * Attention of n_new new tokens a sequence over its cache and over themselves.  With n = lengths[b, g], new token i (slot n + i)
+ * and query head h of KV head g:
+ *     x[j] = scale q.k[j], then softcap tanh(x / softcap) if softcap > 0, then - slopes[h] (position[n + i] - position[j])
+ *     lse = log sum_j exp(x[j]),  out = sum_j exp(x[j] - lse) v[j]
+ * over the slots j < n and those new tokens n + u that tree[b, i] names (bit u); without a tree u <= i.  A tree's bits from
+ * n_new on are ignored; a token usually names its ancestors and itself.  A token that sees nothing gets out 0 and lse minus infinity.
+ *   q           device, element (b, i, h, c) at q + b*q_stride_batch + i*q_stride_token + h*q_stride_head + c, dtype of the config,
+ *               positional encoding already applied; 16-byte aligned, strides multiples of 16 bytes.
+ *   slopes      device, [H] fp32 or NULL.       tree    device, [batch, n_new] 64-bit words or NULL.
+ *   rows        host, the new tokens' rows, which are appended first; NULL: they are in the cache already.
+ *   out         device, [batch, n_new, H, d] contiguous, dtype of the config, 16-byte aligned.
+ *   lse         device, [batch, n_new, H] fp32 or NULL.
+ *   accumulate  not 0: weights[j] = decay weights[j] + the sum over the G heads of exp(x[j] - lse), for all lengths + 1 slots;
+ *               for n_new = 1 only (a tree's tokens count once they are accepted: structkv_weigh).
+ *   workspace   device, 256-byte aligned, at least structkv_attend_workspace_bytes() bytes (0 for arguments that are not valid),
+ *               caller-owned; calls that share it are ordered by the caller.
+ * Values are accumulated in fp32; for bf16 storage the probabilities are rounded to bf16 for their product with V.  New tokens
+ * that a row does not see do not reach it, whatever they hold.  Errors: INVALID_ARG, UNSUPPORTED (accumulate with several tokens),
+ * WORKSPACE, CUDA.  Asynchronous on `stream`.
+ */
+typedef struct {
+  const void* q;
+  long long q_stride_batch, q_stride_token, q_stride_head;
+  int n_new;
+  float scale, softcap;
+  const float* slopes;
+  const unsigned long long* tree;
+  const structkv_new_rows* rows;
+  void* out;
+  float* lse;
+  int accumulate;
+  float decay;
+  void* workspace;
+  size_t workspace_bytes;
+} structkv_attend_args;
+size_t structkv_attend_workspace_bytes(const structkv_config* cfg, int batch, int n_new, int capacity);
+structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* args, void* stream);
+
+/*
+ * Adds the attention weight that accepted new tokens gave: weights[j] = decay weights[j] + the sum of exp(x - lse) over the new
+ * tokens i whose bit is set in accepted[b] and the G heads, for all lengths + n_new slots.  Called between structkv_attend and
+ * structkv_commit, with the q, scale, softcap, slopes, tree and n_new of the former and the lse that it wrote (rows, out,
+ * accumulate and workspace are not looked at).
+ *   accepted    device, [batch] 64-bit words; bits from n_new on are ignored.
+ * Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
+ */
+structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* args,
+                               const unsigned long long* accepted, void* stream);
+
+/*
+ * New tokens become cached ones: of the n_new tokens in the slots behind lengths, sequence b keeps path[b, 0 .. counts[b] - 1]
+ * (ascending numbers of new tokens), moved together behind the old ones with their positions and weights, and its lengths grow by
+ * counts[b].  Without a path it keeps the first counts[b], without counts all n_new.
+ *   counts      device, [batch] int32 or NULL.     path    device, [batch, n_new] int32 or NULL (then with counts).
+ * A count outside 0 .. n_new or a path that does not ascend within it records STRUCTKV_ERR_INVALID_ARG in the device status
+ * word and leaves that sequence as it is.  Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
+ */
+structkv_status structkv_commit(structkv_ctx* ctx, const structkv_cache* cache, int n_new, const int* counts, const int* path,
+                                void* stream);
+
+/*
+ * Eviction by accumulated attention weight: every KV head of more than `budget` (at least 1) tokens keeps `budget` of them: first
+ * those whose position is above its newest one less `recent` (recent >= 0; of more than `budget` such ones the lower slots), then
+ * by weight, larger first (a NaN counts as larger than any number), ties to the lower slot.  Kept tokens in slots from `budget` on move, in order, into the slots below it whose tokens
+ * go, the lowest first; other slots stay as they are, so that slots are not in the order of positions.  lengths becomes `budget`.
+ * Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
+ */
+structkv_status structkv_evict(structkv_ctx* ctx, const structkv_cache* cache, int budget, int recent, void* stream);
+
+/*
  * Self-test of the error path every device-side wait shares (the paper has no counterpart; the
  * conventions at the top of this header define it): launches one thread that waits, with the
  * scorer's bounded-wait helper and a bound of `limit_cycles` SM clock cycles (1 .. 4e9), on a

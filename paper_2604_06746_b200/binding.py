@@ -132,6 +132,17 @@ def fill_prefill(args: PrefillArgs, layers, hidden, positions, s_hist, head_cols
 
 lib.structkv_prefill.restype = _i
 lib.structkv_prefill.argtypes = [_vp, ctypes.POINTER(PrefillArgs), ctypes.POINTER(_i), ctypes.POINTER(_f), _vp]
+
+
+class CacheStruct(ctypes.Structure):
+    """structkv_cache."""
+    _fields_ = [("k", _vp), ("v", _vp), ("stride_batch", _ll), ("stride_head", _ll), ("stride_token", _ll),
+                ("positions", _vp), ("weights", _vp), ("lengths", _vp), ("batch", _i), ("capacity", _i)]
+
+
+MAX_NEW = 64
+lib.structkv_attend_workspace_bytes.restype = ctypes.c_size_t
+lib.structkv_attend_workspace_bytes.argtypes = [ctypes.POINTER(Config), _i, _i, _i]
 lib.structkv_selftest_wait_expiry.restype = _i
 lib.structkv_selftest_wait_expiry.argtypes = [_vp, ctypes.c_ulonglong, _vp]
 lib.structkv_selftest_ctas.restype = _i
@@ -210,6 +221,33 @@ class LayerSources:
         self.row_stride_bytes = s0.stride(1) * self.elem_size
         self.row_bytes = row_elems * self.elem_size
         self.n_slabs, self.n_rows = s0.shape[0], s0.shape[1]
+
+
+class Cache:
+    """structkv_cache over tensors of the caller, which it keeps: ``k``, ``v [batch, H_kv, capacity, d]`` (same strides, ``d``
+    contiguous), ``positions`` int32 and ``weights`` float32 ``[batch, H_kv, capacity]`` (``weights`` may be None where nothing is
+    accumulated or evicted), ``lengths`` int32 ``[batch, H_kv]``: slots ``0 .. lengths - 1`` hold tokens."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, weights: Optional[torch.Tensor],
+                 lengths: torch.Tensor):
+        assert k.dim() == 4 and k.dtype in _CODES and v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride()
+        assert k.stride(3) == 1
+        batch, n_kv, capacity, d = k.shape
+        assert positions.shape == (batch, n_kv, capacity) and positions.dtype == torch.int32 and positions.is_contiguous()
+        assert weights is None or (weights.shape == positions.shape and weights.dtype == torch.float32 and weights.is_contiguous())
+        assert lengths.shape == (batch, n_kv) and lengths.dtype == torch.int32 and lengths.is_contiguous()
+        assert k.is_cuda and all(t is None or t.device == k.device for t in (v, positions, weights, lengths))
+        self._tensors = (k, v, positions, weights, lengths)
+        self._struct = CacheStruct(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), positions.data_ptr(),
+                                   _ptr(weights), lengths.data_ptr(), batch, capacity)
+        self.native = (ctypes.addressof(self._struct), _CODES[k.dtype], k.device.index, batch, n_kv, d, capacity)
+        self.batch, self.n_kv_heads, self.capacity, self.head_dim, self.dtype, self.device = batch, n_kv, capacity, d, k.dtype, k.device
+
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    positions = property(lambda self: self._tensors[2])
+    weights = property(lambda self: self._tensors[3])
+    lengths = property(lambda self: self._tensors[4])
 
 
 class Context:
@@ -412,6 +450,55 @@ class Context:
                       stream: Optional[torch.cuda.Stream] = None) -> None:
         """structkv_mass_recovery: share of each row of ``scores [batch, n]`` that lies at ``idx``."""
         _check(_native.mass_recovery(self._h.value, scores, idx, out, stream), "structkv_mass_recovery")
+
+    # ---- decoding over a compacted cache ----------------------------------------------------
+    def _of(self, cache: Cache) -> tuple:
+        c = self.cfg
+        assert cache.n_kv_heads == c.n_kv_heads and cache.head_dim == c.head_dim and cache.dtype == self.dtype, \
+            "the cache has another shape or dtype than the context"
+        return cache.native
+
+    def attend_workspace(self, cache: Cache, n_new: int) -> torch.Tensor:
+        """A workspace for ``attend`` with ``n_new`` new tokens a sequence over ``cache``."""
+        self._of(cache)
+        n = lib.structkv_attend_workspace_bytes(ctypes.byref(self.cfg), cache.batch, n_new, cache.capacity)
+        if n == 0:
+            raise StructKVError(ERR_INVALID_ARG, "structkv_attend_workspace_bytes")
+        return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+    def append(self, cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, positions: torch.Tensor,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+        """structkv_append: rows ``[batch, n_new, H_kv, d]`` and ``positions [batch, n_new]`` int32 of new tokens."""
+        _check(_native.append(self._h.value, self.cfg.n_q_heads, self._of(cache), k_new, v_new, positions, stream),
+               "structkv_append")
+
+    def attend(self, cache: Cache, q: torch.Tensor, scale: float, out: torch.Tensor, workspace: torch.Tensor,
+               k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+               positions: Optional[torch.Tensor] = None, tree: Optional[torch.Tensor] = None, softcap: float = 0.0,
+               slopes: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, accumulate: bool = False,
+               decay: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """structkv_attend: ``q``, ``out [batch, n_new, H, d]``, ``lse [batch, n_new, H]`` float32; the new tokens' rows are
+        appended first where they are given.  ``tree [batch, n_new]`` int64: bit u of word i says that token i sees token u."""
+        _check(_native.attend(self._h.value, self.cfg.n_q_heads, self._of(cache), q, scale, out, workspace, k_new, v_new,
+                              positions, tree, softcap, slopes, lse, accumulate, decay, stream), "structkv_attend")
+
+    def weigh(self, cache: Cache, q: torch.Tensor, scale: float, lse: torch.Tensor, accepted: torch.Tensor,
+              tree: Optional[torch.Tensor] = None, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+              decay: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """structkv_weigh: ``accepted [batch]`` int64, a bit for every new token; the other arguments are those of the call of
+        ``attend`` that wrote ``lse``."""
+        _check(_native.weigh(self._h.value, self.cfg.n_q_heads, self._of(cache), q, scale, lse, accepted, tree, softcap,
+                             slopes, decay, stream), "structkv_weigh")
+
+    def commit(self, cache: Cache, n_new: int, counts: Optional[torch.Tensor] = None, path: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+        """structkv_commit: of ``n_new`` new tokens the ``counts[b]`` (int32 ``[batch]``; None: all) that ``path[b]`` (int32
+        ``[batch, n_new]``; None: the first) names become cached ones."""
+        _check(_native.commit(self._h.value, self.cfg.n_q_heads, self._of(cache), n_new, counts, path, stream), "structkv_commit")
+
+    def evict(self, cache: Cache, budget: int, recent: int, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """structkv_evict: every KV head keeps its ``recent`` newest tokens and the heaviest others, ``budget`` in all."""
+        _check(_native.evict(self._h.value, self.cfg.n_q_heads, self._of(cache), budget, recent, stream), "structkv_evict")
 
     def selftest_wait_expiry(self, limit_cycles: int, stream: Optional[torch.cuda.Stream] = None) -> None:
         """structkv_selftest_wait_expiry: lets one bounded device wait run out (records TIMEOUT)."""

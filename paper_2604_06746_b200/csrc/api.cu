@@ -12,10 +12,6 @@
 #include "common.cuh"
 #include "host_slots.h"
 
-struct structkv_ctx {
-  skv::Ctx c;
-};
-
 namespace skv {
 
 static bool config_ok(const structkv_config& cfg) {

@@ -1,0 +1,166 @@
+// C ABI of decoding over a compacted cache: argument validation and dispatch.
+#include <algorithm>
+#include <cmath>
+
+#include "attend.cuh"
+
+using namespace skv;
+
+namespace skv {
+namespace {
+
+AttendPlan attend_plan(const structkv_config& cfg, int n_new, int sms) {
+  const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
+  if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms};
+  return {rows <= 16 ? 16 : rows <= 32 ? 32 : 64, 64, rows <= 16 ? 2 * sms : sms};
+}
+
+struct AttendWs { int* unit_start; float2* part_stat; float *part_out, *row_lse, *logits; size_t bytes; };
+AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch, int n_new, int capacity, void* base) {
+  AttendWs w{};
+  char* at = (char*)base;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    void* r = at ? (void*)(at + off) : nullptr;
+    off += align_up(bytes, 256);
+    return r;
+  };
+  const size_t units = (size_t)batch * cfg.n_kv_heads, group = cfg.n_q_heads / cfg.n_kv_heads;
+  w.unit_start = (int*)take((units + 1) * sizeof(int));
+  w.part_stat = (float2*)take((size_t)2 * p.ctas * p.rb * sizeof(float2));
+  w.part_out = (float*)take((size_t)2 * p.ctas * p.rb * cfg.head_dim * sizeof(float));
+  if (n_new == 1) {
+    w.row_lse = (float*)take(units * group * sizeof(float));
+    w.logits = (float*)take(units * group * capacity * sizeof(float));
+  }
+  w.bytes = off;
+  return w;
+}
+
+// (tiles of all units are counted in 31 bits)
+bool sizes_ok(const structkv_config& cfg, int batch, int n_new, int capacity) {
+  if (batch < 1 || capacity < 1 || capacity > 1 << 30 || n_new < 0 || n_new > kMaxNew || n_new > capacity) return false;
+  const long long heads = (long long)batch * cfg.n_q_heads * std::max(1, n_new);
+  return heads <= 0x3fffffffll && heads * (capacity / 64 + 1) <= 0x7fffffffll * 8;
+}
+bool strides_ok(int elem, long long a, long long b, long long c) { return (a * elem) % 16 == 0 && (b * elem) % 16 == 0 && (c * elem) % 16 == 0; }
+
+// False: not a cache of this context's shape.
+bool view_of(const structkv_ctx* ctx, const structkv_cache* cache, int n_new, CacheView* v) {
+  if (!ctx || !cache || !cache->k || !cache->v || !cache->positions || !cache->lengths) return false;
+  const structkv_config& cfg = ctx->c.cfg;
+  const int elem = cfg.dtype == STRUCTKV_BF16 ? 2 : 4;
+  if (!sizes_ok(cfg, cache->batch, n_new, cache->capacity)) return false;
+  if (((uintptr_t)cache->k | (uintptr_t)cache->v) % 16 || ((uintptr_t)cache->positions | (uintptr_t)cache->weights | (uintptr_t)cache->lengths) % 4)
+    return false;
+  if (!strides_ok(elem, cache->stride_batch, cache->stride_head, cache->stride_token)) return false;
+  if ((cache->capacity > 1 && cache->stride_token < cfg.head_dim) || (cfg.n_kv_heads > 1 && cache->stride_head < cfg.head_dim) ||
+      (cache->batch > 1 && cache->stride_batch < cfg.head_dim))
+    return false;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev != ctx->c.device) return false;
+  *v = CacheView{(char*)cache->k, (char*)cache->v, cache->stride_batch * elem, cache->stride_head * elem, cache->stride_token * elem,
+                 cache->positions, cache->weights, cache->lengths, cache->batch * cfg.n_kv_heads, cfg.n_kv_heads, cache->capacity,
+                 cfg.head_dim * elem, ctx->c.ws.status};
+  return true;
+}
+bool rows_of(const structkv_ctx* ctx, const structkv_new_rows* r, NewRows* out) {
+  const int elem = ctx->c.cfg.dtype == STRUCTKV_BF16 ? 2 : 4;
+  if (!r || !r->k || !r->v || !r->positions || ((uintptr_t)r->k | (uintptr_t)r->v) % 16 || (uintptr_t)r->positions % 4) return false;
+  if (!strides_ok(elem, r->stride_batch, r->stride_token, r->stride_head)) return false;
+  *out = NewRows{(const char*)r->k, (const char*)r->v, r->stride_batch * elem, r->stride_token * elem, r->stride_head * elem, r->positions};
+  return true;
+}
+// What attend and weigh have in common.
+bool args_of(const structkv_ctx* ctx, const structkv_attend_args* x, AttendArgs* a) {
+  const structkv_config& cfg = ctx->c.cfg;
+  const int elem = cfg.dtype == STRUCTKV_BF16 ? 2 : 4;
+  if (!x->q || (uintptr_t)x->q % 16 || !strides_ok(elem, x->q_stride_batch, x->q_stride_token, x->q_stride_head)) return false;
+  if (!std::isfinite(x->scale) || !std::isfinite(x->softcap) || x->softcap < 0.f || !std::isfinite(x->decay)) return false;
+  if ((uintptr_t)x->slopes % 4 || (uintptr_t)x->tree % 8 || (uintptr_t)x->lse % 4) return false;
+  const float inv = x->softcap > 0.f ? x->scale / x->softcap : 0.f, cap2 = x->softcap * kLog2e;
+  if (!std::isfinite(inv) || !std::isfinite(cap2) || !std::isfinite(x->scale * kLog2e)) return false;
+  a->q = (const char*)x->q;
+  a->q_batch = x->q_stride_batch * elem;
+  a->q_token = x->q_stride_token * elem;
+  a->q_head = x->q_stride_head * elem;
+  a->n_new = x->n_new;
+  a->group = cfg.n_q_heads / cfg.n_kv_heads;
+  a->rows = a->group * x->n_new;
+  a->scale2 = x->scale * kLog2e;
+  a->cap2 = cap2;
+  a->inv_cap = inv;
+  a->slopes = x->slopes;
+  a->tree = x->tree;
+  a->decay = x->decay;
+  a->lse = x->lse;
+  return true;
+}
+structkv_status told(cudaError_t e) { return e == cudaSuccess ? STRUCTKV_OK : STRUCTKV_ERR_CUDA; }
+
+}  // namespace
+}  // namespace skv
+
+extern "C" {
+
+structkv_status structkv_append(structkv_ctx* ctx, const structkv_cache* cache, const structkv_new_rows* rows, int n_new, void* stream) {
+  CacheView v;
+  NewRows r;
+  if (n_new < 1 || !view_of(ctx, cache, n_new, &v) || !rows_of(ctx, rows, &r)) return STRUCTKV_ERR_INVALID_ARG;
+  return told(launch_append(v, r, n_new, (cudaStream_t)stream));
+}
+
+size_t structkv_attend_workspace_bytes(const structkv_config* cfg, int batch, int n_new, int capacity) {
+  if (structkv_workspace_bytes(cfg) == 0 || n_new < 1 || !sizes_ok(*cfg, batch, n_new, capacity)) return 0;
+  return carve_attend(*cfg, attend_plan(*cfg, n_new, kMaxSms), batch, n_new, capacity, nullptr).bytes;
+}
+
+structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* args, void* stream) {
+  AttendArgs a{};
+  NewRows r;
+  if (!args || args->n_new < 1 || !view_of(ctx, cache, args->n_new, &a.c) || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
+  if (!args->out || (uintptr_t)args->out % 16 || (args->rows && !rows_of(ctx, args->rows, &r))) return STRUCTKV_ERR_INVALID_ARG;
+  if (args->accumulate && !cache->weights) return STRUCTKV_ERR_INVALID_ARG;
+  if (args->accumulate && args->n_new > 1) return STRUCTKV_ERR_UNSUPPORTED;
+  const Ctx& c = ctx->c;
+  const AttendPlan plan = attend_plan(c.cfg, args->n_new, std::min(c.sm_count, kMaxSms));
+  const AttendWs w = carve_attend(c.cfg, plan, cache->batch, args->n_new, cache->capacity, args->workspace);
+  if (!args->workspace || args->workspace_bytes < w.bytes || (uintptr_t)args->workspace % 256) return STRUCTKV_ERR_WORKSPACE;
+  a.out = (char*)args->out;
+  a.accumulate = args->accumulate != 0;
+  a.unit_start = w.unit_start;
+  a.part_stat = w.part_stat;
+  a.part_out = w.part_out;
+  a.row_lse = w.row_lse;
+  a.logits = w.logits;
+  a.ctas = plan.ctas;
+  cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e = args->rows ? launch_append(a.c, r, args->n_new, st) : cudaSuccess;
+  if (e == cudaSuccess) e = c.cfg.dtype == STRUCTKV_BF16 ? launch_attend_mma(c, a, plan, st) : launch_attend_simt(c, a, plan, st);
+  if (e == cudaSuccess) e = launch_attend_finish(c, a, plan, st);
+  return told(e);
+}
+
+structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* args,
+                               const unsigned long long* accepted, void* stream) {
+  AttendArgs a{};
+  if (!args || args->n_new < 1 || !accepted || (uintptr_t)accepted % 8 || !args->lse) return STRUCTKV_ERR_INVALID_ARG;
+  if (!view_of(ctx, cache, args->n_new, &a.c) || !cache->weights || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
+  return told((ctx->c.cfg.dtype == STRUCTKV_BF16 ? launch_weigh_bf16 : launch_weigh_fp32)(ctx->c, a, accepted, (cudaStream_t)stream));
+}
+
+structkv_status structkv_commit(structkv_ctx* ctx, const structkv_cache* cache, int n_new, const int* counts, const int* path,
+                                void* stream) {
+  CacheView v;
+  if (n_new < 1 || (path && !counts) || ((uintptr_t)path | (uintptr_t)counts) % 4 || !view_of(ctx, cache, n_new, &v))
+    return STRUCTKV_ERR_INVALID_ARG;
+  return told(launch_commit(v, n_new, counts, path, (cudaStream_t)stream));
+}
+
+structkv_status structkv_evict(structkv_ctx* ctx, const structkv_cache* cache, int budget, int recent, void* stream) {
+  CacheView v;
+  if (budget < 1 || recent < 0 || !view_of(ctx, cache, 0, &v) || !cache->weights) return STRUCTKV_ERR_INVALID_ARG;
+  return told(launch_evict(v, budget, recent, (cudaStream_t)stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,261 @@
+// Rows that come into a compacted cache, are moved in it, and go: append, commit, evict.
+#include "attend.cuh"
+#include "radix.cuh"
+
+namespace skv {
+namespace {
+
+__device__ __forceinline__ const char* new_row(const char* base, const NewRows& r, int u, int n_kv, int i) {
+  return base + (size_t)(u / n_kv) * r.s_batch + (size_t)i * r.s_token + (size_t)(u % n_kv) * r.s_head;
+}
+
+// A block per unit: rows of the new tokens to slots lengths[u] and up, with their positions and weight 0.
+__global__ void __launch_bounds__(256) append(const __grid_constant__ CacheView c, const __grid_constant__ NewRows r, int n_new) {
+  pdl_trigger();
+  pdl_wait();
+  const int u = blockIdx.x, n = unit_keys(c, u, n_new) - n_new;
+  if (n < 0) return;
+  const size_t off = unit_offset(c, u);
+  const int per_row = c.row_bytes / 16, total = n_new * per_row;
+  for (int i = threadIdx.x; i < 2 * total; i += blockDim.x) {
+    const bool is_v = i >= total;
+    const int e = is_v ? i - total : i, tok = e / per_row, ch = e % per_row;
+    const uint4 x = *(const uint4*)(new_row(is_v ? r.v : r.k, r, u, c.n_kv, tok) + ch * 16);
+    *(uint4*)((is_v ? c.v : c.k) + off + (size_t)(n + tok) * c.s_token + ch * 16) = x;
+  }
+  const size_t w = (size_t)u * c.capacity + n;
+  for (int i = threadIdx.x; i < n_new; i += blockDim.x) {
+    c.positions[w + i] = r.positions[(size_t)(u / c.n_kv) * n_new + i];
+    if (c.weights) c.weights[w + i] = 0.f;
+  }
+}
+
+// A block per unit: the accepted new tokens, path[0] < path[1] < ..., move to the first slots behind the old ones.  A thread has
+// one 16-byte column of K or V (or the words) and goes through the rows in order, several at a time: path[i] >= i, so that a row
+// that is still to be read is never written before.
+__global__ void __launch_bounds__(256) commit(const __grid_constant__ CacheView c, int n_new, const int* __restrict__ counts,
+                                              const int* __restrict__ path) {
+  __shared__ int from[kMaxNew];
+  __shared__ int bad;
+  const int u = blockIdx.x, b = u / c.n_kv, tid = threadIdx.x;
+  if (tid == 0) bad = 0;
+  pdl_trigger();
+  pdl_wait();
+  const int n = unit_keys(c, u, n_new) - n_new, m = counts ? counts[b] : n_new;
+  __syncthreads();
+  if (path && tid < n_new && tid < m) {
+    const int p = path[(size_t)b * n_new + tid];
+    if (p < 0 || p >= n_new || (tid > 0 && p <= path[(size_t)b * n_new + tid - 1])) bad = 1;
+    from[tid] = p;
+  }
+  if (tid == 0 && (m < 0 || m > n_new)) bad = 1;
+  __syncthreads();
+  if (n < 0) return;
+  if (bad) {
+    if (tid == 0) atomicCAS(c.status, 0, (int)STRUCTKV_ERR_INVALID_ARG);
+    return;
+  }
+  if (path) {
+    const size_t off = unit_offset(c, u) + (size_t)n * c.s_token, w = (size_t)u * c.capacity + n;
+    const int per_row = c.row_bytes / 16;
+    constexpr int kGo = 8;
+    for (int i = tid; i < 2 * per_row; i += blockDim.x) {
+      char* const col = (i < per_row ? c.k : c.v) + off + (size_t)(i % per_row) * 16;
+      for (int r0 = 0; r0 < m; r0 += kGo) {
+        uint4 x[kGo];
+#pragma unroll
+        for (int e = 0; e < kGo; ++e)
+          if (r0 + e < m) x[e] = *(const uint4*)(col + (size_t)from[r0 + e] * c.s_token);
+#pragma unroll
+        for (int e = 0; e < kGo; ++e)
+          if (r0 + e < m && from[r0 + e] != r0 + e) *(uint4*)(col + (size_t)(r0 + e) * c.s_token) = x[e];
+      }
+    }
+    if (tid >= 192) {                                              // two warps: positions, weights; read before written
+      int* const words = tid < 224 ? c.positions + w : (int*)c.weights + w;
+      if (tid < 224 || c.weights) {
+        const int lane = tid & 31;
+        int x[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (lane + 32 * e < m) x[e] = words[from[lane + 32 * e]];
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (lane + 32 * e < m) words[lane + 32 * e] = x[e];
+      }
+    }
+  }
+  if (tid == 0) c.lengths[u] = n + m;
+}
+
+// A block per unit with more than `budget` tokens.  Kept are the budget first by (recent or not, weight, lower slot), recent:
+// position above the newest less `recent`.  The kept tokens in slots from budget on move, in order, into the slots below it
+// whose tokens go.  The two sets are disjoint, so that nothing is read after it was written, and a step that brought E tokens
+// moves at most E rows, where a compaction in order would move up to `budget`.
+//
+// The threshold is found as in select.cu (radix.cuh); lists of both sets are taken kList entries at a time.
+constexpr int kItems = 8, kList = 4096;
+struct EvictShared {
+  RadixShared<1> radix;
+  unsigned counts[3][32];
+  int newest[32];
+};
+
+__global__ void __launch_bounds__(kRxThreads, 2) evict(const __grid_constant__ CacheView c, int budget, int recent) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  EvictShared& s = *reinterpret_cast<EvictShared*>(smem);
+  int* const lists = reinterpret_cast<int*>(&s.radix);                // [2][kList], once the threshold is known
+  static_assert(sizeof(RadixShared<1>) >= 2 * kList * sizeof(int), "the lists take the histograms' place");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, u = blockIdx.x;
+  pdl_trigger();
+  radix_clear(s.radix);
+  pdl_wait();
+  const int n = unit_keys(c, u, 0);
+  if (n <= budget) return;
+  const int* const pos = c.positions + (size_t)u * c.capacity;
+  const float* const wt = c.weights + (size_t)u * c.capacity;
+  constexpr int kChunk = kRxThreads * kItems;
+  const int chunks = (n + kChunk - 1) / kChunk;                       // more than one: the unit does not fit the registers
+  int newest = -1;
+#pragma unroll 8
+  for (int j = tid; j < n; j += kRxThreads) newest = max(newest, pos[j]);
+  newest = __reduce_max_sync(0xffffffffu, newest);
+  if (lane == 0) s.newest[warp] = newest;
+  __syncthreads();
+  newest = __reduce_max_sync(0xffffffffu, s.newest[lane]);
+  const long long line = (long long)newest - recent;
+
+  unsigned key[kItems];
+  int mine = 0;
+  // a warp's tokens are consecutive; item e of this thread: first + 32 e
+  auto first_of = [&](int ch) { return ch * kChunk + warp * (32 * kItems) + lane; };
+  auto load = [&](int ch) {
+    const int first = first_of(ch);
+    mine = min(kItems, (n - first + 31) >> 5);
+    float v[kItems];
+    int p[kItems];
+#pragma unroll
+    for (int e = 0; e < kItems; ++e) {
+      v[e] = e < mine ? wt[first + 32 * e] : 0.f;
+      p[e] = e < mine ? pos[first + 32 * e] : 0;
+    }
+    // (a NaN weight, all bits set, comes below the recent ones)
+#pragma unroll
+    for (int e = 0; e < kItems; ++e) key[e] = p[e] > line ? 0xffffffffu : min(order_key(v[e]), 0xfffffffeu);
+  };
+  if (chunks == 1) load(0);
+  unsigned thr = 0, remaining = (unsigned)budget, above = 0, need_eq = 0;
+  int level = 0;
+#pragma unroll 1
+  for (; level < kRxLevels; ++level) {
+    const unsigned mask = level == 0 ? 0u : 0xffffffffu << radix_shift(level - 1);
+    for (int ch = 0; ch < chunks; ++ch) {
+      if (chunks > 1) load(ch);
+#pragma unroll
+      for (int e = 0; e < kItems; ++e)
+        radix_count(s.radix, level, radix_digit(key[e], level), e < mine && (key[e] & mask) == thr);
+    }
+    unsigned digit, in;
+    radix_pick(s.radix, level, remaining, digit, in);
+    thr |= digit << radix_shift(level);
+    if (in == remaining) break;
+  }
+  above = level < kRxLevels ? thr - 1 : thr;
+  need_eq = level < kRxLevels ? 0 : remaining;
+  const unsigned below = (1u << lane) - 1u;
+
+  // Entries [lo, lo + kList) of both lists, then their tokens.  Where the lists are longer, the last entries come first: the
+  // tokens moved then lie above all that is still to be listed, and the copies that moved count as kept, equal ones before
+  // the kept ones that remain, as many as were kept behind them.
+  const size_t off = unit_offset(c, u);
+  const int per_row = c.row_bytes / 16;
+  bool sized = false;
+  for (int lo = 0; lo >= 0;) {
+    __syncthreads();
+    unsigned run_eq = 0, run_free = 0, run_move = 0;
+    for (int ch = 0; ch < chunks; ++ch) {
+      if (chunks > 1) load(ch);
+      // this warp's tokens equal to the threshold, which decide by rank
+      unsigned eq = 0;
+      if (need_eq) {
+#pragma unroll
+        for (int e = 0; e < kItems; ++e) eq += __popc(__ballot_sync(0xffffffffu, e < mine && key[e] == thr));
+        if (lane == 0) s.counts[0][warp] = eq;
+        __syncthreads();
+        const unsigned incl = warp_scan(s.counts[0][lane], lane);
+        eq = run_eq + __shfl_sync(0xffffffffu, incl - s.counts[0][lane], warp);
+        run_eq += __shfl_sync(0xffffffffu, incl, 31);
+      }
+      const int first = first_of(ch);
+      unsigned is_free = 0, is_move = 0, n_free = 0, n_move = 0;      // bits: item e
+#pragma unroll
+      for (int e = 0; e < kItems; ++e) {
+        const bool there = e < mine, equal = there && need_eq && key[e] == thr;
+        const unsigned be = __ballot_sync(0xffffffffu, equal);
+        const bool kept = there && (key[e] > above || (equal && eq + __popc(be & below) < need_eq));
+        eq += __popc(be);
+        const int j = first + 32 * e;
+        const bool fr = there && !kept && j < budget, mv = kept && j >= budget;
+        is_free |= (unsigned)fr << e;
+        is_move |= (unsigned)mv << e;
+        n_free += __popc(__ballot_sync(0xffffffffu, fr));
+        n_move += __popc(__ballot_sync(0xffffffffu, mv));
+      }
+      if (lane == 0) { s.counts[1][warp] = n_free; s.counts[2][warp] = n_move; }
+      __syncthreads();
+      const unsigned fi = warp_scan(s.counts[1][lane], lane), mi = warp_scan(s.counts[2][lane], lane);
+      unsigned f_at = run_free + __shfl_sync(0xffffffffu, fi - s.counts[1][lane], warp);
+      unsigned m_at = run_move + __shfl_sync(0xffffffffu, mi - s.counts[2][lane], warp);
+      run_free += __shfl_sync(0xffffffffu, fi, 31);
+      run_move += __shfl_sync(0xffffffffu, mi, 31);
+#pragma unroll
+      for (int e = 0; e < kItems; ++e) {
+        const bool fr = is_free >> e & 1, mv = is_move >> e & 1;
+        const unsigned bf = __ballot_sync(0xffffffffu, fr), bm = __ballot_sync(0xffffffffu, mv);
+        const unsigned fa = f_at + __popc(bf & below) - lo, ma = m_at + __popc(bm & below) - lo;
+        if (fr && fa < (unsigned)kList) lists[fa] = first + 32 * e;
+        if (mv && ma < (unsigned)kList) lists[kList + ma] = first + 32 * e;
+        f_at += __popc(bf);
+        m_at += __popc(bm);
+      }
+      __syncthreads();                                                // the counts have been read
+    }
+    const int moves = (int)run_move;                                  // as many free slots as tokens to move
+    if (!sized && moves > kList) {
+      sized = true;
+      lo = (moves - 1) / kList * kList;
+      continue;
+    }
+    sized = true;
+    const int here = min(kList, moves - lo);
+    for (int i = tid; i < here * 2 * per_row; i += kRxThreads) {
+      const int row = i / (2 * per_row), ch = i % (2 * per_row);
+      char* const col = (ch < per_row ? c.k : c.v) + off + (size_t)(ch < per_row ? ch : ch - per_row) * 16;
+      *(uint4*)(col + (size_t)lists[row] * c.s_token) = *(const uint4*)(col + (size_t)lists[kList + row] * c.s_token);
+    }
+    int* const p = c.positions + (size_t)u * c.capacity;
+    float* const w = c.weights + (size_t)u * c.capacity;
+    for (int i = tid; i < here; i += kRxThreads) {
+      p[lists[i]] = p[lists[kList + i]];
+      w[lists[i]] = w[lists[kList + i]];
+    }
+    lo -= kList;
+  }
+  if (tid == 0) c.lengths[u] = budget;
+}
+
+}  // namespace
+
+cudaError_t launch_append(const CacheView& c, const NewRows& r, int n_new, cudaStream_t st) {
+  return launch_pdl(append, dim3(c.units), dim3(256), 0, st, c, r, n_new);
+}
+cudaError_t launch_commit(const CacheView& c, int n_new, const int* counts, const int* path, cudaStream_t st) {
+  return launch_pdl(commit, dim3(c.units), dim3(256), 0, st, c, n_new, counts, path);
+}
+cudaError_t launch_evict(const CacheView& c, int budget, int recent, cudaStream_t st) {
+  const cudaError_t e = allow_smem<evict>((int)sizeof(EvictShared));
+  return e != cudaSuccess ? e : launch_pdl(evict, dim3(c.units), dim3(kRxThreads), sizeof(EvictShared), st, c, budget, recent);
+}
+
+}  // namespace skv

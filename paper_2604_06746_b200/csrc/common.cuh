@@ -286,3 +286,7 @@ __device__ __forceinline__ void merge_partials(float& M, float& W, float& X, con
   }
 }
 }  // namespace skv
+
+struct structkv_ctx {
+  skv::Ctx c;
+};

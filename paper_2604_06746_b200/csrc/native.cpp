@@ -4,6 +4,7 @@
 // the interpreter lock is released while the library runs.
 #include <Python.h>
 
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -363,10 +364,159 @@ PyObject* prefill(PyObject* const* a) {
   return Py_BuildValue("iiN", (int)s, pivot, list);
 }
 
+// ---- decoding over a compacted cache: a cache is (address of a structkv_cache, dtype, device, batch, KV heads, head dim, capacity), a
+// tuple that binding.Cache keeps with its tensors --------------------------------------------------------------------------
+struct CacheOf {
+  const structkv_cache* c;
+  at::ScalarType dtype;
+  int device;
+  int64_t batch, heads, kv, d, capacity;
+};
+CacheOf cache_of(PyObject* o, PyObject* heads) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 7) fail(PyExc_TypeError, "a cache is expected");
+  auto size = [&](int i) { return integer(PyTuple_GET_ITEM(o, i)); };
+  return {(const structkv_cache*)size(0), dtype_of(PyTuple_GET_ITEM(o, 1)), (int)size(2), size(3), integer(heads), size(4), size(5), size(6)};
+}
+void there(const CacheOf& c, const at::Tensor& t, const char* what) { require(t.is_cuda() && t.get_device() == c.device, what); }
+// [batch, n_new, heads, d] with contiguous vectors
+void vectors(const CacheOf& c, const at::Tensor& t, int64_t n_new, int64_t heads, const char* what) {
+  require(t.dim() == 4 && t.size(0) == c.batch && t.size(1) == n_new && t.size(2) == heads && t.size(3) == c.d && t.stride(3) == 1 &&
+              t.scalar_type() == c.dtype, what);
+}
+const int* words(const CacheOf& c, PyObject* o, at::IntArrayRef shape, const char* what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  require(fits(t, shape, at::kInt), what);
+  there(c, t, what);
+  return (const int*)t.data_ptr();
+}
+structkv_new_rows rows_of(const CacheOf& c, PyObject* ko, PyObject* vo, PyObject* po, int64_t n_new) {
+  const at::Tensor &k = tensor(ko), &v = tensor(vo);
+  vectors(c, k, n_new, c.kv, "k_new: [batch, n_new, H_kv, d] of the context's dtype, contiguous vectors");
+  vectors(c, v, n_new, c.kv, "v_new: as k_new");
+  require(k.strides() == v.strides(), "k_new and v_new: the same strides");
+  const int* const p = words(c, po, {c.batch, n_new}, "positions: contiguous int32 [batch, n_new], on the cache's device");
+  require(p, "positions come with the rows");
+  there(c, k, "k_new: on the cache's device");
+  there(c, v, "v_new: on the cache's device");
+  return {k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), p};
+}
+// The stream of a call on the cache's device (None: its current one).
+void* stream_on(const CacheOf& c, PyObject* o) { return o == Py_None ? c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)c.device).stream() : stream_of(o); }
+template <typename F>
+PyObject* call_on(const CacheOf& c, F f) {
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)c.device);
+  return call(f);
+}
+// ctx, heads, cache, k_new, v_new, positions, stream
+PyObject* append(PyObject* const* a) {
+  structkv_ctx* const x = context(a[0]);
+  const CacheOf c = cache_of(a[2], a[1]);
+  const int64_t n = dim_of(tensor(a[3]), 1);
+  const structkv_new_rows r = rows_of(c, a[3], a[4], a[5], n);
+  require(n <= STRUCTKV_MAX_NEW, "k_new: 1 to 64 new tokens");
+  void* const st = stream_on(c, a[6]);
+  return call_on(c, [&] { return structkv_append(x, c.c, &r, (int)n, st); });
+}
+// What attend and weigh have in common: q, scale, tree, softcap, slopes.
+structkv_attend_args attend_args(const CacheOf& c, PyObject* qo, PyObject* scale, PyObject* tree, PyObject* softcap, PyObject* slopes) {
+  structkv_attend_args p{};
+  const at::Tensor& q = tensor(qo);
+  const int64_t n = dim_of(q, 1);
+  vectors(c, q, n, c.heads, "q: [batch, n_new, H, d] of the context's dtype, contiguous vectors");
+  require(n >= 1 && n <= STRUCTKV_MAX_NEW, "q: 1 to 64 new tokens");
+  p.scale = real(scale);
+  p.softcap = real(softcap);
+  if (tree != Py_None) {
+    const at::Tensor& t = tensor(tree);
+    require(fits(t, {c.batch, n}, at::kLong), "tree: contiguous int64 [batch, n_new]");
+    there(c, t, "tree: on the cache's device");
+    p.tree = (const unsigned long long*)t.data_ptr();
+  }
+  if (slopes != Py_None) {
+    const at::Tensor& t = tensor(slopes);
+    require(fits(t, {c.heads}, at::kFloat), "slopes: contiguous float32 [H]");
+    there(c, t, "slopes: on the cache's device");
+    p.slopes = (const float*)t.data_ptr();
+  }
+  there(c, q, "q: on the cache's device");
+  p.q = q.data_ptr();
+  p.q_stride_batch = q.stride(0);
+  p.q_stride_token = q.stride(1);
+  p.q_stride_head = q.stride(2);
+  p.n_new = (int)n;
+  return p;
+}
+// ctx, heads, cache, q, scale, out, workspace, k_new, v_new, positions, tree, softcap, slopes, lse, accumulate, decay, stream
+PyObject* attend(PyObject* const* a) {
+  structkv_ctx* const x = context(a[0]);
+  const CacheOf c = cache_of(a[2], a[1]);
+  const at::Tensor &out = tensor(a[5]), &ws = tensor(a[6]);
+  const int64_t n = dim_of(tensor(a[3]), 1);
+  require(fits(out, {c.batch, n, c.heads, c.d}, c.dtype), "out: contiguous [batch, n_new, H, d] of the context's dtype");
+  structkv_new_rows r;
+  const bool rows = a[7] != Py_None;
+  require(rows || (a[8] == Py_None && a[9] == Py_None), "k_new, v_new and positions come together");
+  if (rows) r = rows_of(c, a[7], a[8], a[9], n);
+  structkv_attend_args p = attend_args(c, a[3], a[4], a[10], a[11], a[12]);
+  if (rows) p.rows = &r;
+  there(c, out, "out: on the cache's device");
+  there(c, ws, "workspace: on the cache's device");
+  p.out = out.data_ptr();
+  if (a[13] != Py_None) {
+    const at::Tensor& lse = tensor(a[13]);
+    require(fits(lse, {c.batch, n, c.heads}, at::kFloat), "lse: contiguous float32 [batch, n_new, H]");
+    there(c, lse, "lse: on the cache's device");
+    p.lse = (float*)lse.data_ptr();
+  }
+  p.accumulate = PyObject_IsTrue(a[14]);
+  if (p.accumulate < 0) throw PyError{};
+  p.decay = real(a[15]);
+  p.workspace = ws.data_ptr();
+  p.workspace_bytes = (size_t)(ws.is_contiguous() ? ws.numel() * ws.element_size() : 0);
+  void* const st = stream_on(c, a[16]);
+  return call_on(c, [&] { return structkv_attend(x, c.c, &p, st); });
+}
+// ctx, heads, cache, q, scale, lse, accepted, tree, softcap, slopes, decay, stream
+PyObject* weigh(PyObject* const* a) {
+  structkv_ctx* const x = context(a[0]);
+  const CacheOf c = cache_of(a[2], a[1]);
+  structkv_attend_args p = attend_args(c, a[3], a[4], a[7], a[8], a[9]);
+  const at::Tensor &lse = tensor(a[5]), &acc = tensor(a[6]);
+  require(fits(lse, {c.batch, p.n_new, c.heads}, at::kFloat), "lse: contiguous float32 [batch, n_new, H]");
+  require(fits(acc, {c.batch}, at::kLong), "accepted: contiguous int64 [batch]");
+  there(c, lse, "lse: on the cache's device");
+  there(c, acc, "accepted: on the cache's device");
+  p.lse = (float*)lse.data_ptr();
+  p.decay = real(a[10]);
+  const unsigned long long* const ap = (const unsigned long long*)acc.data_ptr();
+  void* const st = stream_on(c, a[11]);
+  return call_on(c, [&] { return structkv_weigh(x, c.c, &p, ap, st); });
+}
+// ctx, heads, cache, n_new, counts, path, stream
+PyObject* commit(PyObject* const* a) {
+  structkv_ctx* const x = context(a[0]);
+  const CacheOf c = cache_of(a[2], a[1]);
+  const int n = int_of(a[3]);
+  const int* const counts = words(c, a[4], {c.batch}, "counts: contiguous int32 [batch], on the cache's device");
+  const int* const path = words(c, a[5], {c.batch, (int64_t)n}, "path: contiguous int32 [batch, n_new], on the cache's device");
+  void* const st = stream_on(c, a[6]);
+  return call_on(c, [&] { return structkv_commit(x, c.c, n, counts, path, st); });
+}
+// ctx, heads, cache, budget, recent, stream
+PyObject* evict(PyObject* const* a) {
+  structkv_ctx* const x = context(a[0]);
+  const CacheOf c = cache_of(a[2], a[1]);
+  const int budget = int_of(a[3]), recent = int_of(a[4]);
+  void* const st = stream_on(c, a[5]);
+  return call_on(c, [&] { return structkv_evict(x, c.c, budget, recent, st); });
+}
+
 #define ENTRY(f, n) {#f, (PyCFunction)(void (*)())entry<f, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(score_layer, 12), ENTRY(select, 6), ENTRY(compact, 5), ENTRY(compact_per_slab, 5),
                          ENTRY(group_saliency, 6), ENTRY(block_scores, 5), ENTRY(mass_recovery, 5), ENTRY(accumulate, 6),
-                         ENTRY(fill_prefill, 19), ENTRY(prefill, 3), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(fill_prefill, 19), ENTRY(prefill, 3), ENTRY(append, 7), ENTRY(attend, 17),
+                         ENTRY(weigh, 12), ENTRY(commit, 7), ENTRY(evict, 6), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
