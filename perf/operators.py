@@ -270,7 +270,7 @@ def _handle(s):
         if key not in _contexts:
             _contexts[key] = binding.Context(*key[:3], 8, 8, key[3], DEV)
         s["cache"] = binding.Cache(s["k"], s["v"], s["positions"], s["weights"], s["lengths"])
-        s["workspace"] = _contexts[key].attend_workspace(s["cache"], s["new"])
+        s["workspace"] = _contexts[key].attend_workspace(s["cache"], s["new"]) if s["kind"] in ("decode", "tree", "step") else None
         s["context"] = _contexts[key]
     return s["context"], s["cache"], s["workspace"]
 
