@@ -499,7 +499,7 @@ typedef struct {
   int batch, capacity;
 } structkv_cache;
 
-#define STRUCTKV_MAX_NEW 64 /* new tokens of a sequence in one call */
+#define STRUCTKV_MAX_NEW 64 /* new tokens of a sequence that attend in one call */
 
 /* Rows of new tokens: element (b, i, g, c) at k + b*stride_batch + i*stride_token + g*stride_head + c (16-byte aligned, strides
  * multiples of 16 bytes, any order, 0 for a dimension that is broadcast); positions device, [batch, n_new] int32 contiguous. */
@@ -511,14 +511,14 @@ typedef struct {
 } structkv_new_rows;
 
 /*
- * Writes the rows of n_new (1 .. 64) new tokens a sequence to slots lengths .. lengths + n_new - 1, their positions, and weight
+ * Writes the rows of n_new (1 .. capacity) new tokens a sequence to slots lengths .. lengths + n_new - 1, their positions, and weight
  * 0.  `lengths` stays: the tokens count once they are committed.  Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
  */
 structkv_status structkv_append(structkv_ctx* ctx, const structkv_cache* cache, const structkv_new_rows* rows, int n_new,
                                 void* stream);
 
 /*
- * Attention of n_new new tokens a sequence over its cache and over themselves.  With n = lengths[b, g], new token i (slot n + i)
+ * Attention of n_new (1 .. 64) new tokens a sequence over its cache and over themselves.  With n = lengths[b, g], new token i (slot n + i)
  * and query head h of KV head g:
  *     x[j] = scale q.k[j], then softcap tanh(x / softcap) if softcap > 0, then - slopes[h] (position[n + i] - position[j])
  *     lse = log sum_j exp(x[j]),  out = sum_j exp(x[j] - lse) v[j]
@@ -570,7 +570,7 @@ structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, c
 /*
  * New tokens become cached ones: of the n_new tokens in the slots behind lengths, sequence b keeps path[b, 0 .. counts[b] - 1]
  * (ascending numbers of new tokens), moved together behind the old ones with their positions and weights, and its lengths grow by
- * counts[b].  Without a path it keeps the first counts[b], without counts all n_new.
+ * counts[b].  Without a path it keeps the first counts[b], without counts all n_new (1 .. capacity; with a path 1 .. 64).
  *   counts      device, [batch] int32 or NULL.     path    device, [batch, n_new] int32 or NULL (then with counts).
  * A count outside 0 .. n_new or a path that does not ascend within it records STRUCTKV_ERR_INVALID_ARG in the device status
  * word and leaves that sequence as it is.  Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.

@@ -39,7 +39,7 @@ AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch
 
 // (tiles of all units are counted in 31 bits)
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, int capacity) {
-  if (batch < 1 || capacity < 1 || capacity > 1 << 30 || n_new < 0 || n_new > kMaxNew || n_new > capacity) return false;
+  if (batch < 1 || capacity < 1 || capacity > 1 << 30 || n_new < 0 || n_new > capacity) return false;
   const long long heads = (long long)batch * cfg.n_q_heads * std::max(1, n_new);
   return heads <= 0x3fffffffll && heads * (capacity / 64 + 1) <= 0x7fffffffll * 8;
 }
@@ -75,7 +75,7 @@ bool rows_of(const structkv_ctx* ctx, const structkv_new_rows* r, NewRows* out) 
 bool args_of(const structkv_ctx* ctx, const structkv_attend_args* x, AttendArgs* a) {
   const structkv_config& cfg = ctx->c.cfg;
   const int elem = cfg.dtype == STRUCTKV_BF16 ? 2 : 4;
-  if (!x->q || (uintptr_t)x->q % 16 || !strides_ok(elem, x->q_stride_batch, x->q_stride_token, x->q_stride_head)) return false;
+  if (x->n_new < 1 || x->n_new > kMaxNew || !x->q || (uintptr_t)x->q % 16 || !strides_ok(elem, x->q_stride_batch, x->q_stride_token, x->q_stride_head)) return false;
   if (!std::isfinite(x->scale) || !std::isfinite(x->softcap) || x->softcap < 0.f || !std::isfinite(x->decay)) return false;
   if ((uintptr_t)x->slopes % 4 || (uintptr_t)x->tree % 8 || (uintptr_t)x->lse % 4) return false;
   const float inv = x->softcap > 0.f ? x->scale / x->softcap : 0.f, cap2 = x->softcap * kLog2e;
@@ -111,14 +111,14 @@ structkv_status structkv_append(structkv_ctx* ctx, const structkv_cache* cache, 
 }
 
 size_t structkv_attend_workspace_bytes(const structkv_config* cfg, int batch, int n_new, int capacity) {
-  if (structkv_workspace_bytes(cfg) == 0 || n_new < 1 || !sizes_ok(*cfg, batch, n_new, capacity)) return 0;
+  if (structkv_workspace_bytes(cfg) == 0 || n_new < 1 || n_new > kMaxNew || !sizes_ok(*cfg, batch, n_new, capacity)) return 0;
   return carve_attend(*cfg, attend_plan(*cfg, n_new, kMaxSms), batch, n_new, capacity, nullptr).bytes;
 }
 
 structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* args, void* stream) {
   AttendArgs a{};
   NewRows r;
-  if (!args || args->n_new < 1 || !view_of(ctx, cache, args->n_new, &a.c) || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
+  if (!args || !view_of(ctx, cache, args->n_new, &a.c) || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
   if (!args->out || (uintptr_t)args->out % 16 || (args->rows && !rows_of(ctx, args->rows, &r))) return STRUCTKV_ERR_INVALID_ARG;
   if (args->accumulate && !cache->weights) return STRUCTKV_ERR_INVALID_ARG;
   if (args->accumulate && args->n_new > 1) return STRUCTKV_ERR_UNSUPPORTED;
@@ -144,7 +144,7 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
 structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* args,
                                const unsigned long long* accepted, void* stream) {
   AttendArgs a{};
-  if (!args || args->n_new < 1 || !accepted || (uintptr_t)accepted % 8 || !args->lse) return STRUCTKV_ERR_INVALID_ARG;
+  if (!args || !accepted || (uintptr_t)accepted % 8 || !args->lse) return STRUCTKV_ERR_INVALID_ARG;
   if (!view_of(ctx, cache, args->n_new, &a.c) || !cache->weights || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
   return told((ctx->c.cfg.dtype == STRUCTKV_BF16 ? launch_weigh_bf16 : launch_weigh_fp32)(ctx->c, a, accepted, (cudaStream_t)stream));
 }
@@ -152,7 +152,7 @@ structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, c
 structkv_status structkv_commit(structkv_ctx* ctx, const structkv_cache* cache, int n_new, const int* counts, const int* path,
                                 void* stream) {
   CacheView v;
-  if (n_new < 1 || (path && !counts) || ((uintptr_t)path | (uintptr_t)counts) % 4 || !view_of(ctx, cache, n_new, &v))
+  if (n_new < 1 || (path && (!counts || n_new > kMaxNew)) || ((uintptr_t)path | (uintptr_t)counts) % 4 || !view_of(ctx, cache, n_new, &v))
     return STRUCTKV_ERR_INVALID_ARG;
   return told(launch_commit(v, n_new, counts, path, (cudaStream_t)stream));
 }

@@ -414,7 +414,7 @@ PyObject* append(PyObject* const* a) {
   const CacheOf c = cache_of(a[2], a[1]);
   const int64_t n = dim_of(tensor(a[3]), 1);
   const structkv_new_rows r = rows_of(c, a[3], a[4], a[5], n);
-  require(n <= STRUCTKV_MAX_NEW, "k_new: 1 to 64 new tokens");
+  require(n <= c.capacity, "k_new: more tokens than the cache has slots");
   void* const st = stream_on(c, a[6]);
   return call_on(c, [&] { return structkv_append(x, c.c, &r, (int)n, st); });
 }

@@ -236,7 +236,7 @@ def test_refusals(cuda_device):
     with pytest.raises(binding.StructKVError, match="invalid"):
         ctx.evict(bare, 10, 1)
     for f in (lambda: ctx.evict(cache, 0, 1), lambda: ctx.evict(cache, 10, -1), lambda: ctx.commit(cache, 0),
-              lambda: ctx.commit(cache, 65), lambda: ctx.commit(cache, 3, path=torch.zeros((1, 3), dtype=torch.int32, device=cuda_device))):
+              lambda: ctx.commit(cache, p.cap + 1), lambda: ctx.commit(cache, 3, path=torch.zeros((1, 3), dtype=torch.int32, device=cuda_device))):
         with pytest.raises(binding.StructKVError, match="invalid"):
             f()
     odd = torch.zeros((1, 8, 60, 132), dtype=BF, device=cuda_device)[..., :128]   # rows of 264 bytes

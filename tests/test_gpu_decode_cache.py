@@ -152,3 +152,24 @@ def test_append_of_strided_rows(cuda_device):
             s.k[b, g, n:n + 4], s.v[b, g, n:n + 4] = rows[b, :, g], rows[b, :, 3 + g]
             s.pos[b, g, n:n + 4], s.w[b, g, n:n + 4] = pos[b], 0
     s.check()
+
+
+def test_a_long_piece_comes_in(cuda_device):
+    """More tokens at once than attend in one call."""
+    from paper_2604_06746_b200 import binding
+    s = Store(cuda_device, [[3, 0], [40, 7]], 400, 64, seed=10)
+    rows = np.random.default_rng(1).integers(-2 ** 14, 2 ** 14, size=(2, 2, 350, 2, 64)).astype(np.int16)
+    dev = torch.from_numpy(rows).to(cuda_device).view(torch.bfloat16)
+    pos = np.random.default_rng(2).integers(0, 9999, size=(2, 350)).astype(np.int32)
+    s.ctx.append(s.cache, dev[0], dev[1], torch.from_numpy(pos).to(cuda_device))
+    s.ctx.commit(s.cache, 350, counts=torch.tensor([350, 129], dtype=torch.int32, device=cuda_device))
+    for b in range(2):
+        for g in range(2):
+            n = int(s.n[b, g])
+            s.k[b, g, n:n + 350], s.v[b, g, n:n + 350] = rows[0, b, :, g], rows[1, b, :, g]
+            s.pos[b, g, n:n + 350], s.w[b, g, n:n + 350] = pos[b], 0
+            s.n[b, g] += (350, 129)[b]
+    s.check()
+    with pytest.raises(binding.StructKVError, match="invalid"):
+        s.ctx.commit(s.cache, 65, counts=torch.zeros(2, dtype=torch.int32, device=cuda_device),
+                     path=torch.zeros((2, 65), dtype=torch.int32, device=cuda_device))
