@@ -12,7 +12,7 @@ namespace {
 AttendPlan attend_plan(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
   if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms};
-  return {rows <= 16 ? 16 : rows <= 32 ? 32 : 64, 64, rows <= 16 ? 2 * sms : sms};
+  return {rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64, 64, sms};
 }
 
 struct AttendWs { int* unit_start; float2* part_stat; float *part_out, *row_lse, *logits; size_t bytes; };
@@ -40,8 +40,8 @@ AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch
 // (tiles of all units are counted in 31 bits)
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, int capacity) {
   if (batch < 1 || capacity < 1 || capacity > 1 << 30 || n_new < 0 || n_new > capacity) return false;
-  const long long heads = (long long)batch * cfg.n_q_heads * std::max(1, n_new);
-  return heads <= 0x3fffffffll && heads * (capacity / 64 + 1) <= 0x7fffffffll * 8;
+  const long long units = (long long)batch * cfg.n_kv_heads, rows = (long long)cfg.n_q_heads / cfg.n_kv_heads * std::max(1, n_new);
+  return units * rows <= 0x3fffffffll && units * ((rows + 3) / 4) <= 0x7fffffffll / (capacity / 64 + 1);
 }
 bool strides_ok(int elem, long long a, long long b, long long c) { return (a * elem) % 16 == 0 && (b * elem) % 16 == 0 && (c * elem) % 16 == 0; }
 
@@ -54,6 +54,7 @@ bool view_of(const structkv_ctx* ctx, const structkv_cache* cache, int n_new, Ca
   if (((uintptr_t)cache->k | (uintptr_t)cache->v) % 16 || ((uintptr_t)cache->positions | (uintptr_t)cache->weights | (uintptr_t)cache->lengths) % 4)
     return false;
   if (!strides_ok(elem, cache->stride_batch, cache->stride_head, cache->stride_token)) return false;
+  if (std::max({cache->stride_batch, cache->stride_head, cache->stride_token}) >= 1ll << 37) return false;   // (a tensor map's limit: 2^40 bytes)
   if ((cache->capacity > 1 && cache->stride_token < cfg.head_dim) || (cfg.n_kv_heads > 1 && cache->stride_head < cfg.head_dim) ||
       (cache->batch > 1 && cache->stride_batch < cfg.head_dim))
     return false;

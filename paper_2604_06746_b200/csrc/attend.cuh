@@ -50,7 +50,7 @@ struct AttendArgs {
   float2* part_stat;                   // [2 ctas][RB] maximum and sum
   float* part_out;                     // [2 ctas][RB][d]
   float* row_lse;                      // [units][rows] in bits (accumulate)
-  float* logits;                       // [units][group][capacity] in bits (accumulate)
+  float* logits;                       // [units][capacity][group] in bits (accumulate)
   int ctas;
 };
 
@@ -168,12 +168,17 @@ __device__ __forceinline__ float capped(float s, float cap2, float inv_cap) {
   return copysignf(cap2 * (1.f - __fdividef(2.f, e + 1.f)), y);
 }
 
+// The new tokens that row r of a unit sees, as bits.
+__device__ __forceinline__ unsigned long long row_seen(const AttendArgs& a, int u, int r) {
+  const int i = r / a.group;
+  return a.tree ? a.tree[(size_t)(u / a.c.n_kv) * a.n_new + i] : (i == 63 ? ~0ull : (1ull << (i + 1)) - 1);
+}
 // A row's option values.
 struct RowOptions { unsigned long long seen; float slope2; int position; };
 __device__ __forceinline__ RowOptions row_options(const AttendArgs& a, int u, int r) {
   RowOptions o;
-  const int b = u / a.c.n_kv, g = u % a.c.n_kv, i = r / a.group, h = r % a.group;
-  o.seen = a.tree ? a.tree[(size_t)b * a.n_new + i] : (i == 63 ? ~0ull : (1ull << (i + 1)) - 1);
+  const int g = u % a.c.n_kv, i = r / a.group, h = r % a.group;
+  o.seen = row_seen(a, u, r);
   o.slope2 = a.slopes ? a.slopes[g * a.group + h] * kLog2e : 0.f;
   o.position = a.slopes ? a.c.positions[(size_t)u * a.c.capacity + a.c.lengths[u] + i] : 0;
   return o;

@@ -12,22 +12,22 @@ namespace {
 constexpr int kThreads = 256;
 
 // CTAs that took an item, and the slot of CTA c.
-struct Cover { int first, last; long long start; };
+struct Cover { int first, last; };
 __device__ __forceinline__ Cover cover_of(long long start, int tiles, long long W, int C) {
-  return {cta_of(start, W, C), cta_of(start + tiles - 1, W, C), start};
+  return {cta_of(start, W, C), cta_of(start + tiles - 1, W, C)};
 }
-__device__ __forceinline__ int slot_of(const Cover& v, int c, long long W, int C) { return 2 * c + (v.start >= cut(c, W, C)); }
+__device__ __forceinline__ int slot_of(const Cover& v, int c) { return 2 * c + (c == v.first); }   // it begins there, or goes on
 
 // Maximum and sum of a row over its CTAs, by a warp (the same in every lane).
-__device__ __forceinline__ float2 merged_stat(const AttendArgs& a, const Cover& v, long long W, int C, int rb_rows, int row, int lane) {
+__device__ __forceinline__ float2 merged_stat(const AttendArgs& a, const Cover& v, int rb_rows, int row, int lane) {
   float M = -INFINITY;
-  for (int c = v.first + lane; c <= v.last; c += 32) M = fmaxf(M, a.part_stat[(size_t)slot_of(v, c, W, C) * rb_rows + row].x);
+  for (int c = v.first + lane; c <= v.last; c += 32) M = fmaxf(M, a.part_stat[(size_t)slot_of(v, c) * rb_rows + row].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   if (M == -INFINITY) return make_float2(M, 0.f);
   float L = 0.f;
   for (int c = v.first + lane; c <= v.last; c += 32) {
-    const float2 p = a.part_stat[(size_t)slot_of(v, c, W, C) * rb_rows + row];
+    const float2 p = a.part_stat[(size_t)slot_of(v, c) * rb_rows + row];
     L += p.y * fast_exp2(p.x - M);
   }
 #pragma unroll
@@ -55,12 +55,12 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
     if (tiles == 0) continue;
     const Cover v = cover_of((long long)start + (long long)rb * tiles, tiles, W, C);
     if (v.first == v.last) continue;                              // finished there
-    const float2 st = merged_stat(a, v, W, C, rb_rows, row, lane);
+    const float2 st = merged_stat(a, v, rb_rows, row, lane);
     float acc[DL] = {};
     if (st.x != -INFINITY) {
 #pragma unroll 4
       for (int c = v.first; c <= v.last; ++c) {
-        const size_t at = (size_t)slot_of(v, c, W, C) * rb_rows + row;
+        const size_t at = (size_t)slot_of(v, c) * rb_rows + row;
         const float f = fast_exp2(a.part_stat[at].x - st.x);
 #pragma unroll
         for (int e = 0; e < DL; ++e) acc[e] = fmaf(f, a.part_out[at * D + e * 32 + lane], acc[e]);
@@ -99,15 +99,22 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
       for (int h = warp; h < heads; h += kThreads / 32) {
         const int r = h0 + h, rb = r / rb_rows;
         const Cover v = cover_of((long long)start + (long long)rb * tiles, tiles, W, C);
-        const float x = v.first == v.last ? a.row_lse[(size_t)u * a.rows + r] : bits_of(merged_stat(a, v, W, C, rb_rows, r % rb_rows, lane));
+        const float x = v.first == v.last ? a.row_lse[(size_t)u * a.rows + r] : bits_of(merged_stat(a, v, rb_rows, r % rb_rows, lane));
         if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
       }
       __syncthreads();
+      const bool fours = a.group % 4 == 0;
       for (int j = t0 * tile + tid; j < min(keys, t1 * tile); j += kThreads) {
-        const float* const x = a.logits + ((size_t)u * a.group + h0) * a.c.capacity + j;
+        const float* const x = a.logits + ((size_t)u * a.c.capacity + j) * a.group + h0;
         float sum = 0.f;
-#pragma unroll 4
-        for (int h = 0; h < heads; ++h) sum += fast_exp2(x[(size_t)h * a.c.capacity] - lse[h]);
+        if (fours) {
+          for (int h = 0; h < heads; h += 4) {
+            const float4 v = *(const float4*)(x + h);
+            sum += (fast_exp2(v.x - lse[h]) + fast_exp2(v.y - lse[h + 1])) + (fast_exp2(v.z - lse[h + 2]) + fast_exp2(v.w - lse[h + 3]));
+          }
+        } else {
+          for (int h = 0; h < heads; ++h) sum += fast_exp2(x[h] - lse[h]);
+        }
         w[j] = (h0 == 0 ? a.decay * w[j] : w[j]) + sum;
       }
     }

@@ -1,9 +1,12 @@
 // Attention of new tokens over a bf16 cache, up to 64 rows of a KV head at a time, and the weight of accepted tokens.
 //
-// Flash form: per row a running maximum m, sum l and unscaled output O over the keys seen so far; a key tile of 64 gives
-// S = Q K^T, p = 2^(x - m), l += sum p, O += p V.  WK warps share a tile's keys (16 or 32 each), WR warps the rows (16 each);
-// every warp has statistics of its own, so that nothing but the ring of tiles is waited for, and a segment's end merges
-// them.  Products are m16n8k16: rows are few, and reading K and V is the bound.
+// Flash form: per row a reference m, sum l and unscaled output O over the keys seen so far; a tile of 64 keys gives
+// S = K Q^T, p = 2^(x - m), l += sum p, O^T += V^T p.  Rows are few and reading K and V is the bound, so keys are the long side of
+// the m16n8k16 products (16 keys x 8 rows, then 16 columns of V x 8 rows): four rows of a single token fill half a product, in
+// the other orientation a quarter.  A warp takes 16 keys of a tile and up to 32 rows; tiles come by TMA (128-byte swizzle)
+// through a ring that one warp fills; NG groups of warps take tiles in turn, each warp with statistics of its own, so that
+// nothing but the ring is waited for, and a segment's end merges the warps.  The reference follows a row's maximum only where
+// that outgrows it by 2^kSlack: p then stays below 2^kSlack, far from overflow, and most tiles need neither shuffles nor scaling.
 #include <algorithm>
 
 #include "attend.cuh"
@@ -13,6 +16,7 @@ namespace skv {
 namespace {
 
 constexpr int kTileKeys = 64;
+constexpr float kSlack = 8.f;
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -20,9 +24,14 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) 
 __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// Arrives once this thread's cp.async copies so far are there (one of the barrier's expected arrivals).
+__device__ __forceinline__ void cp_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%3, %4, %5, %6}], [%2], %7;"
+      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "l"(policy) : "memory");
+}
 __device__ __forceinline__ void ldsm(uint32_t at, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -30,6 +39,12 @@ __device__ __forceinline__ void ldsm(uint32_t at, uint32_t (&r)[4]) {
 __device__ __forceinline__ void ldsm_t(uint32_t at, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+// Transposes an 8 x 8 matrix of 16-bit values that a warp holds.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
   uint32_t r;
@@ -42,19 +57,17 @@ __device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) ==
 // in different banks.
 template <int D>
 __device__ __forceinline__ uint32_t chunk_at(int row, int chunk) { return row * (D * 2) + ((chunk ^ (row & 7)) << 4); }
+// The same within a tile that TMA wrote: 64 columns after 64 columns, rows of 128 bytes.
+__device__ __forceinline__ uint32_t tile_at(int row, int chunk) {
+  return (chunk >> 3) * (kTileKeys * 128) + row * 128 + (((chunk ^ row) & 7) << 4);
+}
 
 // Where a CTA is in its run of tiles.
-struct Cursor {
-  int u, rb, t, tiles, keys;
-  const char *k, *v;
-};
+struct Cursor { int u, rb, t, tiles, keys; };
 __device__ __forceinline__ void enter(Cursor& c, const CacheView& cache, int n_new, int tile) {
   c.keys = c.u < cache.units ? unit_keys(cache, c.u, n_new) : 0;
   while (c.keys == 0 && c.u < cache.units - 1) c.keys = unit_keys(cache, ++c.u, n_new);
   c.tiles = (c.keys + tile - 1) / tile;
-  const size_t off = unit_offset(cache, min(c.u, cache.units - 1));
-  c.k = cache.k + off;
-  c.v = cache.v + off;
 }
 __device__ __forceinline__ void advance(Cursor& c, const CacheView& cache, int n_new, int tile, int blocks) {
   if (++c.t < c.tiles) return;
@@ -65,34 +78,54 @@ __device__ __forceinline__ void advance(Cursor& c, const CacheView& cache, int n
   enter(c, cache, n_new, tile);
 }
 
-template <int D, int WR, int WK>
+struct CacheMaps { CUtensorMap k, v; };
+
+// NR blocks of 8 rows a warp, WR such warps beside each other, four along a tile's keys, NG groups of these.
+template <int D, int NR, int WR, int NG>
 struct AttendShape {
-  static constexpr int RB = 16 * WR, THREADS = WR * WK * 32, KW = kTileKeys / WK;
-  static constexpr int kTileBytes = kTileKeys * D * 2, kQBytes = RB * D * 2;
-  static constexpr int kStage = 2 * kTileBytes + kQBytes + kTileKeys * 4;
-  static constexpr int kStages = WR == 1 ? 3 : WR == 2 ? 4 : 3;
-  static constexpr int kMergeRow = D + 4;
-  static constexpr int kSmem = kStages * kStage + RB * kMergeRow * 4 + 2 * WK * RB * 4 + 128;
+  static constexpr int RB = 8 * NR * WR, kGroupWarps = 4 * WR, kWarps = kGroupWarps * NG, THREADS = 32 + kWarps * 32, kSets = 4 * NG;
+  static constexpr int kTileBytes = kTileKeys * D * 2;
+  static constexpr int kPosOff = 2 * kTileBytes, kQOff = kPosOff + 1024;
+  static constexpr int kStage = kQOff + (RB * D * 2 + 1023) / 1024 * 1024;
+  static constexpr int kRegs = NR * D / 4;                       // output registers of a thread
+  static constexpr int kMerge = kSets / 2 * WR * kRegs * 32 * 4;
+  static constexpr int kFixed = kMerge + 2 * kSets * RB * 4 + 256 + 1024;
+  static constexpr int kStages = std::min(6, (226 * 1024 - kFixed) / kStage);
+  static constexpr int kSmem = kStages * kStage + kFixed;
+  static_assert(kStages >= 2, "a ring");
 };
 
-template <int D, int WR, int WK, bool OPT>
-__global__ void __launch_bounds__(WR * WK * 32, WR == 1 ? 2 : 1) attend_mma(const __grid_constant__ AttendArgs a) {
-  using S = AttendShape<D, WR, WK>;
-  constexpr int RB = S::RB, KW = S::KW, NT = S::THREADS, CH = D / 8, NB = KW / 8;
+template <int D, int NR, int WR, int NG, bool OPT>
+__global__ void __launch_bounds__(32 + 128 * WR * NG, 1) attend_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps) {
+  using S = AttendShape<D, NR, WR, NG>;
+  constexpr int RB = S::RB, NT = S::THREADS, CH = D / 8, ST = S::kStages, KK = D / 16;
   extern __shared__ unsigned char smem_raw[];
-  const uint32_t base = (smem_u32(smem_raw) + 127u) & ~127u;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
-  float* const merge = (float*)(sm + S::kStages * S::kStage);
-  float* const stat = merge + RB * S::kMergeRow;                // [2][WK][RB]
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wr = warp / WK, wk = warp % WK;
+  float* const merge = (float*)(sm + ST * S::kStage);           // [sets / 2][WR][register][lane]
+  float* const stat = merge + S::kMerge / 4;                    // [2][sets][RB]
+  const uint32_t bars = smem_u32(stat + 2 * S::kSets * RB);     // full [ST], empty [ST]
+  volatile int* const abort_flag = (volatile int*)(stat + 2 * S::kSets * RB) + 4 * ST;
+  auto full = [&](int st) { return bars + 8 * st; };
+  auto empty = [&](int st) { return bars + 8 * (ST + st); };
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cta = blockIdx.x, blocks = (a.rows + RB - 1) / RB;
   pdl_trigger();
+  if (tid == 0) {
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(full(i), 33);                                   // the copies by TMA, and 32 lanes' own
+      mbar_init(empty(i), S::kGroupWarps);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   pdl_wait();
   const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, blocks, [&](long long W) { return cut(cta, W, sharers(W, gridDim.x)); },
                                      cta == 0 ? a.unit_start : nullptr);
   const int C = sharers(ws.total, gridDim.x);
   const long long lo = cut(cta, ws.total, C), hi = cut(cta + 1, ws.total, C);
   if (lo >= hi) return;
+  const int run = (int)(hi - lo);
   Cursor cur;
   cur.u = ws.unit;
   enter(cur, a.c, a.n_new, kTileKeys);
@@ -101,434 +134,571 @@ __global__ void __launch_bounds__(WR * WK * 32, WR == 1 ? 2 : 1) attend_mma(cons
     cur.rb = rest / cur.tiles;
     cur.t = rest - cur.rb * cur.tiles;
   }
-  Cursor ld = cur;
-  long long at = lo, ld_at = lo;
 
-  auto load = [&]() {
-    const int stage = (int)((ld_at - lo) % S::kStages);
-    const uint32_t to = base + stage * S::kStage;
-    const int j0 = ld.t * kTileKeys;
-#pragma unroll 4
-    for (int i = tid; i < kTileKeys * CH; i += NT) {
-      const int row = i / CH, ch = i % CH, j = j0 + row;
-      const bool there = j < ld.keys;
-      const size_t off = there ? (size_t)j * a.c.s_token + ch * 16 : 0;
-      cp16(to + chunk_at<D>(row, ch), ld.k + off, there);
-      cp16(to + S::kTileBytes + chunk_at<D>(row, ch), ld.v + off, there);
-    }
-    if (OPT && a.slopes)
-      for (int i = tid; i < kTileKeys; i += NT) {
-        const bool there = j0 + i < ld.keys;
-        cp4(to + 2 * S::kTileBytes + S::kQBytes + i * 4, a.c.positions + (size_t)ld.u * a.c.capacity + (there ? j0 + i : 0), there);
+  if (warp == 0) {
+    // the ring's producer
+    const uint64_t policy = l2_policy_evict_first();
+    int since = 0;                                              // tiles since the segment began
+    int n = 0;
+    for (; n < run; ++n) {
+      const int st = n % ST, b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv;
+      const uint32_t to = base + st * S::kStage;
+      if (cur.t == 0) since = 0;
+      if (n >= ST && !mbar_wait_producer(empty(st), (n / ST - 1) & 1, abort_flag, kWaitCycles)) break;
+      if (lane == 0) {
+        mbar_expect_tx(full(st), 2 * S::kTileBytes);
+        const uint64_t hint = blocks == 1 ? policy : l2_policy_evict_normal();
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          tma_load_4d(to + c * kTileKeys * 128, &maps.k, full(st), c * 64, cur.t * kTileKeys, g, b, hint);
+          tma_load_4d(to + S::kTileBytes + c * kTileKeys * 128, &maps.v, full(st), c * 64, cur.t * kTileKeys, g, b, hint);
+        }
       }
-    if (ld.t == 0 || ld_at == lo) {                             // a segment begins: its rows come along
-      const int b = ld.u / a.c.n_kv, g = ld.u % a.c.n_kv;
-      for (int i = tid; i < RB * CH; i += NT) {
-        const int row = i / CH, ch = i % CH, r = ld.rb * RB + row;
-        const bool there = r < a.rows;
-        const int tok = there ? r / a.group : 0, h = there ? r - tok * a.group : 0;
-        cp16(to + 2 * S::kTileBytes + chunk_at<D>(row, ch),
-             a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head + ch * 16, there);
+      if (OPT && a.slopes) {
+        const int* const pos = a.c.positions + (size_t)cur.u * a.c.capacity;
+#pragma unroll
+        for (int i = lane; i < kTileKeys; i += 32) {
+          const int j = cur.t * kTileKeys + i;
+          cp4(to + S::kPosOff + i * 4, pos + (j < cur.keys ? j : 0), j < cur.keys);
+        }
       }
+      if (since < NG) {                                         // a segment begins: every group's first tile brings the rows
+        for (int i = lane; i < RB * CH; i += 32) {
+          const int row = i / CH, ch = i % CH, r = cur.rb * RB + row;
+          const bool is = r < a.rows;
+          const int tok = is ? r / a.group : 0, h = is ? r - tok * a.group : 0;
+          cp16(to + S::kQOff + chunk_at<D>(row, ch),
+               a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head + ch * 16, is);
+        }
+      }
+      cp_arrive(full(st));
+      ++since;
+      if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
     }
-    ++ld_at;
-    if (ld_at < hi) advance(ld, a.c, a.n_new, kTileKeys, blocks);
-  };
-#pragma unroll 1
-  for (int s = 0; s < S::kStages - 1; ++s) {
-    if (ld_at < hi) load();
-    cp_commit();
+    if (*abort_flag) {
+      // copies in flight end before the block does
+      for (int i = max(0, n - ST); i < n; ++i) mbar_drain(full(i % ST), (i / ST) & 1, abort_flag);
+      if (lane == 0) atomicCAS(a.c.status, 0, (int)STRUCTKV_ERR_TIMEOUT);
+    }
+    return;
   }
 
-  uint32_t qf[D / 16][4];
-  float o[D / 8][4];
-  float m[2], l[2];
-  RowOptions ro[2];
+  const int cw = warp - 1, grp = cw / S::kGroupWarps, wr = cw % S::kGroupWarps / 4, kw = cw % 4;
+  const int g8 = lane >> 2, t4 = lane & 3;
+  auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(S::kWarps * 32) : "memory"); };
+  uint32_t qf[NR][KK][2];
+  float o[NR][KK][4];                                           // column g8 (+ 8) of 16, rows 2 t4 and + 1 of the block
+  float m[NR][2], l[NR][2];
+  float slope2[NR][2];
+  int place[NR][2];
+  bool fresh = true;                                            // nothing of this segment yet
   int seg_first = 0;                                            // 1: the segment begins the item
-  const int rowa = wr * 16 + (lane >> 2);                       // this thread's rows of the block: rowa, rowa + 8
-#pragma unroll 1
-  for (; at < hi; ++at) {
-    const int stage = (int)((at - lo) % S::kStages);
-    const uint32_t from = base + stage * S::kStage;
-    unsigned char* const here = sm + stage * S::kStage;
-    cp_wait<S::kStages - 2>();
-    __syncthreads();
-    if (ld_at < hi) load();
-    cp_commit();
-    if (cur.t == 0 || at == lo) {
-      seg_first = cur.t == 0;
+  auto clear = [&]() {
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk)
-        ldsm(from + 2 * S::kTileBytes + chunk_at<D>(wr * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), kk * 2 + (lane >> 4)), qf[kk]);
+    for (int i = 0; i < NR; ++i) {
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-      m[0] = m[1] = -INFINITY;
-      l[0] = l[1] = 0.f;
+      for (int x = 0; x < 2; ++x) { m[i][x] = -INFINITY; l[i][x] = 0.f; }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) ro[x] = row_options(a, cur.u, min(cur.rb * RB + rowa + 8 * x, a.rows - 1));
+      for (int k = 0; k < KK; ++k) o[i][k][0] = o[i][k][1] = o[i][k][2] = o[i][k][3] = 0.f;
     }
-    const int n_old = cur.keys - a.n_new, j0 = cur.t * kTileKeys + wk * KW;
-    // products
-    float s[NB][4];
+    fresh = true;
+  };
+  clear();
+  int seg = 0;                                                  // first tile of the segment in the run
+  seg_first = cur.t == 0;
+#pragma unroll 1
+  for (int n = 0; n < run; ++n) {
+    const int first_row = cur.rb * RB + wr * 8 * NR + 2 * t4;   // row of (block i, x): first_row + 8 i + x
+    if (n % NG == grp) {
+      const int st = n % ST;
+      const uint32_t from = base + st * S::kStage;
+      const unsigned char* const here = sm + st * S::kStage;
+      mbar_wait(full(st), (n / ST) & 1, abort_flag);            // (on expiry the numbers are void, the control flow goes on)
+      if (fresh) {
+        fresh = false;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
+        for (int i = 0; i < NR; ++i)
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk)
+          for (int kk = 0; kk < KK; kk += 2) {
+            uint32_t x[4];
+            ldsm(from + S::kQOff + chunk_at<D>((wr * NR + i) * 8 + (lane & 7), kk * 2 + (lane >> 3)), x);
+            qf[i][kk][0] = x[0]; qf[i][kk][1] = x[1]; qf[i][kk + 1][0] = x[2]; qf[i][kk + 1][1] = x[3];
+          }
+        if (OPT && a.slopes)
 #pragma unroll
-      for (int nb = 0; nb < NB; nb += 2) {
+          for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const RowOptions ro = row_options(a, cur.u, min(first_row + 8 * i + x, a.rows - 1));
+              slope2[i][x] = ro.slope2;
+              place[i][x] = ro.position;
+            }
+      }
+      // products: two chains where a warp has one block of rows
+      constexpr int CHAINS = NR == 1 ? 2 : 1;
+      float acc[CHAINS][NR][4];
+#pragma unroll
+      for (int c = 0; c < CHAINS; ++c)
+#pragma unroll
+        for (int i = 0; i < NR; ++i) acc[c][i][0] = acc[c][i][1] = acc[c][i][2] = acc[c][i][3] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
         uint32_t kf[4];
-        ldsm(from + chunk_at<D>(wk * KW + nb * 8 + (lane >> 4) * 8 + (lane & 7), kk * 2 + ((lane >> 3) & 1)), kf);
-        mma_16x8x16(s[nb], qf[kk][0], qf[kk][1], qf[kk][2], qf[kk][3], kf[0], kf[1]);
-        mma_16x8x16(s[nb + 1], qf[kk][0], qf[kk][1], qf[kk][2], qf[kk][3], kf[2], kf[3]);
+        ldsm(from + tile_at(kw * 16 + (lane & 15), kk * 2 + (lane >> 4)), kf);
+#pragma unroll
+        for (int i = 0; i < NR; ++i) mma_16x8x16(acc[kk % CHAINS][i], kf[0], kf[1], kf[2], kf[3], qf[i][kk][0], qf[i][kk][1]);
       }
-    // x in bits
-    const int* const kp = (const int*)(here + 2 * S::kTileBytes + S::kQBytes) + wk * KW;
-    const bool tail = j0 + KW > n_old;
+      float s[NR][4];                                           // element 2 y + x: key g8 + 8 y, row x
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+      for (int i = 0; i < NR; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int jj = nb * 8 + (lane & 3) * 2 + (e & 1);
-        float x = OPT ? biased(a, s[nb][e], ro[e >> 1], a.slopes ? kp[jj] : 0) : s[nb][e] * a.scale2;
-        if (tail && (j0 + jj >= cur.keys || !sees(ro[e >> 1].seen, j0 + jj, n_old))) x = -INFINITY;
-        s[nb][e] = x;
+        for (int e = 0; e < 4; ++e) s[i][e] = CHAINS == 2 ? acc[0][i][e] + acc[CHAINS - 1][i][e] : acc[0][i][e];
+      // x in bits
+      const int n_old = cur.keys - a.n_new, j0 = cur.t * kTileKeys + kw * 16;
+      const bool tail = j0 + 16 > n_old;
+      if (OPT) {
+        int kp[2] = {0, 0};
+        if (a.slopes) { kp[0] = ((const int*)(here + S::kPosOff))[kw * 16 + g8]; kp[1] = ((const int*)(here + S::kPosOff))[kw * 16 + g8 + 8]; }
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = a.cap2 != 0.f ? capped(s[i][e], a.cap2, a.inv_cap) : s[i][e] * a.scale2;
+            if (a.slopes) x = fmaf(-slope2[i][e & 1], (float)(place[i][e & 1] - kp[e >> 1]), x);
+            s[i][e] = x;
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[i][e] *= a.scale2;
       }
-    if (a.accumulate) {
+      if (tail) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int j = j0 + nb * 8 + (lane & 3) * 2 + (e & 1), r = cur.rb * RB + rowa + 8 * (e >> 1);
-          if (j < cur.keys && r < a.rows) a.logits[((size_t)cur.u * a.group + r) * a.c.capacity + j] = s[nb][e];
-        }
-    }
-    // running maximum
-    bool grown = false;
-    float ref[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      float t = -INFINITY;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) t = fmaxf(t, fmaxf(s[nb][2 * x], s[nb][2 * x + 1]));
-      t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
-      t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-      ref[x] = fmaxf(t, m[x]);
-      grown |= ref[x] > m[x];
-    }
-    if (__any_sync(0xffffffffu, grown)) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float f = m[x] == -INFINITY ? 0.f : fast_exp2(m[x] - ref[x]);
-        l[x] *= f;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) { o[i][2 * x] *= f; o[i][2 * x + 1] *= f; }
-        m[x] = ref[x];
-      }
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) ref[x] = m[x] == -INFINITY ? 0.f : m[x];
-    uint32_t pf[NB][2];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      float p[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = fast_exp2(s[nb][e] - ref[e >> 1]);
-      l[0] += p[0] + p[1];
-      l[1] += p[2] + p[3];
-      // p keeps 8 bits for the product, as V does; the sum l is of the unrounded values
-      pf[nb][0] = bf16x2(p[0], p[1]);
-      pf[nb][1] = bf16x2(p[2], p[3]);
-    }
-    // Where a new token's V is not finite, rows that do not see it must not meet it: 0 x infinity.
-    bool plain = true;
-    if (tail) {
-      bool bad = false;
-#pragma unroll 2
-      for (int i = lane; i < KW * CH; i += 32) {
-        const uint4 w = *(const uint4*)(here + S::kTileBytes + (wk * KW + i / CH) * (D * 2) + (i % CH) * 16);
-        bad |= not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
-      }
-      plain = !__any_sync(0xffffffffu, bad);
-    }
-    if (plain) {
-#pragma unroll
-      for (int nb = 0; nb < NB; nb += 2)
-#pragma unroll
-        for (int dn = 0; dn < D / 16; ++dn) {
-          uint32_t vf[4];
-          ldsm_t(from + S::kTileBytes + chunk_at<D>(wk * KW + nb * 8 + ((lane >> 3) & 1) * 8 + (lane & 7), dn * 2 + (lane >> 4)), vf);
-          mma_16x8x16(o[2 * dn], pf[nb][0], pf[nb][1], pf[nb + 1][0], pf[nb + 1][1], vf[0], vf[1]);
-          mma_16x8x16(o[2 * dn + 1], pf[nb][0], pf[nb][1], pf[nb + 1][0], pf[nb + 1][1], vf[2], vf[3]);
-        }
-    } else {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll 1
-        for (int kk = 0; kk < 8; ++kk) {
-          const int key = wk * KW + nb * 8 + kk;
-          float p[2];
+        for (int i = 0; i < NR; ++i)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const uint32_t w = __shfl_sync(0xffffffffu, pf[nb][x], (lane & ~3) | (kk >> 1));
-            p[x] = __uint_as_float(kk & 1 ? w & 0xffff0000u : w << 16);
+            const unsigned long long seen = row_seen(a, cur.u, min(first_row + 8 * i + x, a.rows - 1));
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const int j = j0 + g8 + 8 * y;
+              if (j >= cur.keys || !sees(seen, j, n_old)) s[i][2 * y + x] = -INFINITY;
+            }
           }
+      }
+      if (a.accumulate) {
+        float* const to = a.logits + ((size_t)cur.u * a.c.capacity + j0 + g8) * a.group;
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            const uint32_t w = *(const uint32_t*)(here + S::kTileBytes + chunk_at<D>(key, i) + (lane & 3) * 4);
+        for (int i = 0; i < NR; ++i)
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-              if (p[x] != 0.f) {
-                o[i][2 * x] = fmaf(p[x], __uint_as_float(w << 16), o[i][2 * x]);
-                o[i][2 * x + 1] = fmaf(p[x], __uint_as_float(w & 0xffff0000u), o[i][2 * x + 1]);
+          for (int e = 0; e < 4; ++e) {
+            const int r = first_row + 8 * i + (e & 1);
+            if (r < a.rows && j0 + g8 + 8 * (e >> 1) < cur.keys) to[(size_t)8 * (e >> 1) * a.group + r] = s[i][e];
+          }
+      }
+      // references
+      bool grown = false;
+#pragma unroll
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) grown |= fmaxf(s[i][x], s[i][2 + x]) > m[i][x] + kSlack;
+      if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float t = fmaxf(s[i][x], s[i][2 + x]);
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            t = fmaxf(t, m[i][x]);
+            const float f = m[i][x] == -INFINITY ? 0.f : fast_exp2(m[i][x] - t);
+            m[i][x] = t;
+            l[i][x] *= f;
+#pragma unroll
+            for (int k = 0; k < KK; ++k) { o[i][k][x] *= f; o[i][k][2 + x] *= f; }
+          }
+      }
+      uint32_t pf[NR][2];                                       // keys 2 t4 and + 1 (+ 8), row g8
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = fast_exp2(s[i][e] - (m[i][e & 1] == -INFINITY ? 0.f : m[i][e & 1]));
+        l[i][0] += p[0] + p[2];
+        l[i][1] += p[1] + p[3];
+        // p keeps 8 bits for the product, as V does; the sum l is of the unrounded values
+        pf[i][0] = transposed(bf16x2(p[0], p[1]));
+        pf[i][1] = transposed(bf16x2(p[2], p[3]));
+      }
+      // Where V of a new token, or of a slot behind them, is not finite, rows that do not see it must not meet it: 0 x infinity.
+      bool plain = true;
+      if (tail) {
+        bool bad = false;
+#pragma unroll 2
+        for (int i = lane; i < 16 * CH; i += 32) {
+          const uint4 w = *(const uint4*)(here + S::kTileBytes + tile_at(kw * 16 + i / CH, i % CH));
+          bad |= not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
+        }
+        plain = !__any_sync(0xffffffffu, bad);
+      }
+      if (plain) {
+#pragma unroll
+        for (int k = 0; k < KK; ++k) {
+          uint32_t vf[4];
+          ldsm_t(from + S::kTileBytes + tile_at(kw * 16 + (lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1)), vf);
+#pragma unroll
+          for (int i = 0; i < NR; ++i) mma_16x8x16(o[i][k], vf[0], vf[1], vf[2], vf[3], pf[i][0], pf[i][1]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll 1
+          for (int j = 0; j < 16; ++j) {
+            float p[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {                       // key j of row 2 t4 + x: lane (row, j / 2 mod 4)
+              const uint32_t w0 = __shfl_sync(0xffffffffu, pf[i][0], (2 * t4 + x) * 4 + ((j & 7) >> 1));
+              const uint32_t w1 = __shfl_sync(0xffffffffu, pf[i][1], (2 * t4 + x) * 4 + ((j & 7) >> 1));
+              const uint32_t w = j < 8 ? w0 : w1;
+              p[x] = __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+            }
+#pragma unroll
+            for (int k = 0; k < KK; ++k)
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const unsigned short h = *(const unsigned short*)(here + S::kTileBytes + tile_at(kw * 16 + j, k * 2 + y) + g8 * 2);
+                const float v = __uint_as_float((uint32_t)h << 16);
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                  if (p[x] != 0.f) o[i][k][2 * y + x] = fmaf(p[x], v, o[i][k][2 * y + x]);
               }
           }
-        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(st));
     }
 
     const bool item_ends = cur.t + 1 == cur.tiles;
-    if (item_ends || at + 1 == hi) {
-      // the warps that share the keys: common maximum, then their outputs one after the other
+    if (item_ends || n + 1 == run) {
+      // the warps that shared the keys: common reference, then their outputs, halving
+      const int sets = min(S::kSets, (n + 1 - seg) * 4);        // (groups without a tile have nothing)
+      const int used = sets > 8 ? 16 : sets > 4 ? 8 : 4, my = ((grp + NG - seg % NG) % NG) * 4 + kw;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
-        l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
-        if ((lane & 3) == 0) {
-          stat[wk * RB + rowa + 8 * x] = m[x];
-          stat[(WK + wk) * RB + rowa + 8 * x] = l[x];
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) l[i][x] += __shfl_xor_sync(0xffffffffu, l[i][x], d);
+          if (g8 == 0) {
+            const int row = wr * 8 * NR + 8 * i + 2 * t4 + x;
+            stat[my * RB + row] = m[i][x];
+            stat[(S::kSets + my) * RB + row] = l[i][x];
+          }
         }
-      }
-      __syncthreads();
-      float f[2];
+      sync();
+      float M[NR][2], L[NR][2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        float M = -INFINITY;
+      for (int i = 0; i < NR; ++i)
 #pragma unroll
-        for (int w = 0; w < WK; ++w) M = fmaxf(M, stat[w * RB + rowa + 8 * x]);
-        f[x] = m[x] == -INFINITY ? 0.f : fast_exp2(m[x] - M);
-      }
+        for (int x = 0; x < 2; ++x) {
+          const float* const sp = stat + wr * 8 * NR + 8 * i + 2 * t4 + x;
+          float top = -INFINITY, sum = 0.f;
+          for (int w = 0; w < used; ++w) top = fmaxf(top, sp[w * RB]);
+          if (top != -INFINITY)
+            for (int w = 0; w < used; ++w) sum += sp[(S::kSets + w) * RB] * fast_exp2(sp[w * RB] - top);
+          const float f = m[i][x] == -INFINITY ? 0.f : fast_exp2(m[i][x] - top);
+#pragma unroll
+          for (int k = 0; k < KK; ++k) { o[i][k][x] *= f; o[i][k][2 + x] *= f; }
+          M[i][x] = top;
+          L[i][x] = sum;
+        }
 #pragma unroll 1
-      for (int w = 0; w < WK; ++w) {
-        if (wk == w) {
+      for (int half = used / 2; half >= 1; half /= 2) {
+        float* const buf = merge + ((size_t)((my % half) * WR + wr) * S::kRegs) * 32 + lane;
+        if (my >= half && my < 2 * half)
 #pragma unroll
-          for (int i = 0; i < D / 8; ++i)
+          for (int i = 0; i < NR; ++i)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              float2* const to = (float2*)(merge + (rowa + 8 * x) * S::kMergeRow + i * 8 + (lane & 3) * 2);
-              float2 v = make_float2(o[i][2 * x] * f[x], o[i][2 * x + 1] * f[x]);
-              if (w > 0) { const float2 e = *to; v.x += e.x; v.y += e.y; }
-              *to = v;
+            for (int k = 0; k < KK; ++k)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) buf[((i * KK + k) * 4 + e) * 32] = o[i][k][e];
+        sync();
+        if (my < half)
+#pragma unroll
+          for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int k = 0; k < KK; ++k)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][k][e] += buf[((i * KK + k) * 4 + e) * 32];
+        sync();
+      }
+      if (my == 0) {
+        const bool whole = seg_first && item_ends;
+        const int slot = 2 * cta + seg_first, b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv;
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int row = wr * 8 * NR + 8 * i + 2 * t4 + x, r = cur.rb * RB + row;
+            if (r >= a.rows) continue;
+            if (!whole) {
+              float* const to = a.part_out + ((size_t)slot * RB + row) * D + g8;
+#pragma unroll
+              for (int k = 0; k < KK; ++k) { to[k * 16] = o[i][k][x]; to[k * 16 + 8] = o[i][k][2 + x]; }
+              if (g8 == 0) a.part_stat[(size_t)slot * RB + row] = make_float2(M[i][x], L[i][x]);
+              continue;
             }
-        }
-        __syncthreads();
-      }
-      const bool whole = seg_first && item_ends;
-      const int slot = 2 * cta + seg_first;
-      const int b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv;
-      for (int i = tid; i < RB * (D / 4); i += NT) {
-        const int row = i / (D / 4), c4 = i % (D / 4), r = cur.rb * RB + row;
-        if (r >= a.rows) break;
-        float M = -INFINITY, L = 0.f;
+            const int tok = r / a.group, h = r - tok * a.group;
+            const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
+            const float inv = M[i][x] == -INFINITY ? 0.f : 1.f / L[i][x];      // (a NaN row stays one)
+            __nv_bfloat16* const to = (__nv_bfloat16*)a.out + q * D + g8;
 #pragma unroll
-        for (int w = 0; w < WK; ++w) M = fmaxf(M, stat[w * RB + row]);
-        if (M != -INFINITY)
-#pragma unroll
-          for (int w = 0; w < WK; ++w) L += stat[(WK + w) * RB + row] * fast_exp2(stat[w * RB + row] - M);
-        const float4 v = *(const float4*)(merge + row * S::kMergeRow + c4 * 4);
-        if (!whole) {
-          *(float4*)(a.part_out + ((size_t)slot * RB + row) * D + c4 * 4) = v;
-          if (c4 == 0) a.part_stat[(size_t)slot * RB + row] = make_float2(M, L);
-          continue;
-        }
-        const int tok = r / a.group, h = r - tok * a.group;
-        const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
-        const float inv = M == -INFINITY ? 0.f : 1.f / L;          // (a NaN row stays one)
-        *(uint2*)(a.out + (q * D + c4 * 4) * 2) = make_uint2(bf16x2(v.x * inv, v.y * inv), bf16x2(v.z * inv, v.w * inv));
-        if (c4 == 0) {
-          const float bits = M == -INFINITY ? M : M + log2f(L);
-          if (a.lse) a.lse[q] = bits * kLn2;
-          if (a.accumulate) a.row_lse[(size_t)cur.u * a.rows + r] = bits;
-        }
+            for (int k = 0; k < KK; ++k) {
+              to[k * 16] = __float2bfloat16(o[i][k][x] * inv);
+              to[k * 16 + 8] = __float2bfloat16(o[i][k][2 + x] * inv);
+            }
+            if (g8 == 0) {
+              const float bits = M[i][x] == -INFINITY ? M[i][x] : M[i][x] + log2f(L[i][x]);
+              if (a.lse) a.lse[q] = bits * kLn2;
+              if (a.accumulate) a.row_lse[(size_t)cur.u * a.rows + r] = bits;
+            }
+          }
       }
-      __syncthreads();
+      clear();
+      seg = n + 1;
+      seg_first = 1;
     }
-    advance(cur, a.c, a.n_new, kTileKeys, blocks);
+    if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
   }
 }
 
 // ---- weights of accepted tokens ------------------------------------------------------------------
-// weights[j] = decay weights[j] + sum over accepted rows of 2^(x - lse): the accepted tokens' rows are the operand that stays
-// (kWeighRows at a time), K tiles stream past them; a key belongs to one warp, which adds up its rows.
-constexpr int kWeighRows = 64, kWeighStages = 4, kWeighWarps = 4;
+// weights[j] = decay weights[j] + sum over accepted rows of 2^(x - lse): K tiles stream past the accepted tokens' rows
+// (kWeighRows at a time in shared memory); a warp has 16 keys of a tile in registers and adds up their rows.
+constexpr int kWeighRows = 64, kWeighStages = 8, kWeighGroups = 2, kWeighWarps = 4 * kWeighGroups;
 
 template <int D>
-constexpr int weigh_smem() { return kWeighStages * (kTileKeys * D * 2 + kTileKeys * 4) + kWeighRows * (D * 2 + 4 + sizeof(RowOptions)) + 128; }
+constexpr int weigh_smem() {
+  return kWeighStages * (kTileKeys * D * 2 + 1024) + kWeighRows * (D * 2 + 4 + sizeof(RowOptions)) + 256 + 1024;
+}
 
 template <int D, bool OPT>
-__global__ void __launch_bounds__(kWeighWarps * 32, 2) weigh_mma(const __grid_constant__ AttendArgs a, const unsigned long long* __restrict__ accepted) {
-  constexpr int NT = kWeighWarps * 32, CH = D / 8, kStage = kTileKeys * D * 2 + kTileKeys * 4;
+__global__ void __launch_bounds__(32 + kWeighWarps * 32, 1)
+weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps, const unsigned long long* __restrict__ accepted) {
+  constexpr int NT = 32 + kWeighWarps * 32, CH = D / 8, KK = D / 16, ST = kWeighStages, kTileBytes = kTileKeys * D * 2, kStage = kTileBytes + 1024;
   extern __shared__ unsigned char smem_raw[];
-  const uint32_t base = (smem_u32(smem_raw) + 127u) & ~127u;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
-  constexpr uint32_t kQ = kWeighStages * kStage;
-  float* const lse = (float*)(sm + kQ + kWeighRows * D * 2);      // in bits, +inf: no row
-  RowOptions* const opts = (RowOptions*)(lse + kWeighRows);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int cta = blockIdx.x;
+  constexpr uint32_t kQ = ST * kStage;
+  RowOptions* const opts = (RowOptions*)(sm + kQ + kWeighRows * D * 2);
+  float* const lse = (float*)(opts + kWeighRows);                 // in bits, +inf: no row
+  const uint32_t bars = smem_u32(lse + kWeighRows);
+  volatile int* const abort_flag = (volatile int*)(lse + kWeighRows) + 4 * ST;
+  auto full = [&](int st) { return bars + 8 * st; };
+  auto empty = [&](int st) { return bars + 8 * (ST + st); };
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
   pdl_trigger();
+  if (tid == 0) {
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(full(i), 33);
+      mbar_init(empty(i), 4);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   pdl_wait();
   const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, 1, [&](long long W) { return cut(cta, W, sharers(W, gridDim.x)); }, nullptr);
   const int C = sharers(ws.total, gridDim.x);
   const long long lo = cut(cta, ws.total, C), hi = cut(cta + 1, ws.total, C);
   if (lo >= hi) return;
-  long long at = lo;
+  const int run = (int)(hi - lo);
   Cursor cur;
   cur.u = ws.unit;
   enter(cur, a.c, a.n_new, kTileKeys);
   cur.rb = 0;
   cur.t = (int)(lo - ws.before);
+  // rows of the accepted tokens of a unit, and how often its tiles are gone through
+  auto taken_of = [&](int u) { return accepted[u / a.c.n_kv] & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1); };
+  auto rounds_of = [&](int rows) { return rows <= kWeighRows ? 1 : (rows + kWeighRows - 1) / kWeighRows; };
+
+  if (warp == 0) {
+    const uint64_t policy = l2_policy_evict_first(), again = l2_policy_evict_normal();
+    int n = 0;
+    bool ok = true;
 #pragma unroll 1
-  while (at < hi) {                                               // a unit's tiles of this CTA
-    const int t0 = cur.t, t1 = (int)min((long long)cur.tiles, cur.t + (hi - at));
+    for (int left = run; left > 0 && ok;) {
+      const int t0 = cur.t, t1 = min(cur.tiles, t0 + left), b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv;
+      const int rounds = rounds_of(__popcll(taken_of(cur.u)) * a.group);
+      for (int i = 0; i < rounds * (t1 - t0); ++i, ++n) {
+        const int st = n % ST, t = t0 + i % (t1 - t0);
+        const uint32_t to = base + st * kStage;
+        if (n >= ST && !(ok = mbar_wait_producer(empty(st), (n / ST - 1) & 1, abort_flag, kWaitCycles))) break;
+        if (lane == 0) {
+          mbar_expect_tx(full(st), kTileBytes);
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c)
+            tma_load_4d(to + c * kTileKeys * 128, &maps.k, full(st), c * 64, t * kTileKeys, g, b, rounds == 1 ? policy : again);
+        }
+        if (OPT && a.slopes) {
+          const int* const pos = a.c.positions + (size_t)cur.u * a.c.capacity;
+#pragma unroll
+          for (int e = lane; e < kTileKeys; e += 32) {
+            const int j = t * kTileKeys + e;
+            cp4(to + kTileBytes + e * 4, pos + (j < cur.keys ? j : 0), j < cur.keys);
+          }
+        }
+        cp_arrive(full(st));
+      }
+      left -= t1 - t0;
+      cur.t = t1 - 1;
+      if (left > 0) advance(cur, a.c, a.n_new, kTileKeys, 1);
+    }
+    if (*abort_flag) {
+      for (int i = max(0, n - ST); i < n; ++i) mbar_drain(full(i % ST), (i / ST) & 1, abort_flag);
+      if (lane == 0) atomicCAS(a.c.status, 0, (int)STRUCTKV_ERR_TIMEOUT);
+    }
+    return;
+  }
+
+  const int cw = warp - 1, grp = cw / 4, kw = cw % 4, g8 = lane >> 2, t4 = lane & 3;
+  auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kWeighWarps * 32) : "memory"); };
+  int n = 0;
+#pragma unroll 1
+  for (int left = run; left > 0;) {                               // a unit's tiles of this CTA
+    const int t0 = cur.t, t1 = min(cur.tiles, t0 + left);
     const int b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv, n_old = cur.keys - a.n_new;
-    const unsigned long long taken = accepted[b] & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1);
-    const int rows = __popcll(taken) * a.group;
+    const unsigned long long taken = taken_of(cur.u);
+    const int rows = __popcll(taken) * a.group, rounds = rounds_of(rows);
     float* const w = a.c.weights + (size_t)cur.u * a.c.capacity;
 #pragma unroll 1
-    for (int r0 = 0; r0 == 0 || r0 < rows; r0 += kWeighRows) {
-      const int n_rows = min(kWeighRows, rows - r0), n_blocks = (n_rows + 15) / 16;
-      __syncthreads();
-      for (int i = tid; i < kWeighRows; i += NT) {
-        float x = INFINITY;
-        if (i < n_rows) {
-          unsigned long long rest = taken;                        // token of row r0 + i: the bit of that rank
-          for (int skip = (r0 + i) / a.group; skip > 0; --skip) rest &= rest - 1;
-          const int tok = __ffsll((long long)rest) - 1, h = (r0 + i) % a.group;
-          x = a.lse[((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h] * kLog2e;
-          if (x == -INFINITY) x = INFINITY;                       // a row that saw nothing gave nothing
-          opts[i] = row_options(a, cur.u, tok * a.group + h);
-          const char* const src = a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head;
-#pragma unroll 4
-          for (int ch = 0; ch < CH; ++ch) *(uint4*)(sm + kQ + chunk_at<D>(i, ch)) = *(const uint4*)(src + ch * 16);
-        } else {
-          for (int ch = 0; ch < CH; ++ch) *(uint4*)(sm + kQ + chunk_at<D>(i, ch)) = make_uint4(0, 0, 0, 0);
-          opts[i] = RowOptions{0, 0.f, 0};
-        }
-        lse[i] = x;
-      }
-      auto load = [&](int t) {
-        const uint32_t to = base + (t - t0) % kWeighStages * kStage;
-        for (int i = tid; i < kTileKeys * CH; i += NT) {
-          const int row = i / CH, ch = i % CH, j = t * kTileKeys + row;
-          cp16(to + chunk_at<D>(row, ch), cur.k + (j < cur.keys ? (size_t)j * a.c.s_token + ch * 16 : 0), j < cur.keys);
-        }
-        if (OPT && a.slopes)
-          for (int i = tid; i < kTileKeys; i += NT) {
-            const int j = t * kTileKeys + i;
-            cp4(to + kTileKeys * D * 2 + i * 4, a.c.positions + (size_t)cur.u * a.c.capacity + (j < cur.keys ? j : 0), j < cur.keys);
+    for (int round = 0; round < rounds; ++round) {
+      const int r0 = round * kWeighRows, n_rows = min(kWeighRows, rows - r0), n_blocks = (n_rows + 7) / 8;
+      sync();
+      for (int i = tid - 32; i < n_blocks * 8 * CH; i += kWeighWarps * 32) {
+        const int row = i / CH, ch = i % CH;
+        uint4 x = make_uint4(0, 0, 0, 0);
+        float ref = INFINITY;
+        RowOptions ro{0, 0.f, 0};
+        if (row < n_rows) {
+          unsigned long long rest = taken;                        // token of row r0 + row: the bit of that rank
+          for (int skip = (r0 + row) / a.group; skip > 0; --skip) rest &= rest - 1;
+          const int tok = __ffsll((long long)rest) - 1, h = (r0 + row) % a.group;
+          x = *(const uint4*)(a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head + ch * 16);
+          if (ch == 0) {
+            ref = a.lse[((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h] * kLog2e;
+            if (ref == -INFINITY) ref = INFINITY;                 // a row that saw nothing gave nothing
+            ro = row_options(a, cur.u, tok * a.group + h);
           }
-      };
-#pragma unroll 1
-      for (int s = 0; s < kWeighStages - 1; ++s) {
-        if (t0 + s < t1) load(t0 + s);
-        cp_commit();
+        }
+        *(uint4*)(sm + kQ + chunk_at<D>(row, ch)) = x;
+        if (ch == 0) { lse[row] = ref; opts[row] = ro; }
       }
+      sync();
 #pragma unroll 1
-      for (int t = t0; t < t1; ++t) {
-        cp_wait<kWeighStages - 2>();
-        __syncthreads();
-        if (t + kWeighStages - 1 < t1) load(t + kWeighStages - 1);
-        cp_commit();
-        const int stage = (t - t0) % kWeighStages;
-        const uint32_t from = base + stage * kStage;
-        const int* const kp = (const int*)(sm + stage * kStage + kTileKeys * D * 2) + warp * 16;
-        const int j0 = t * kTileKeys + warp * 16;
+      for (int t = t0; t < t1; ++t, ++n) {
+        if (n % kWeighGroups != grp) continue;
+        const int st = n % ST;
+        const uint32_t from = base + st * kStage;
+        mbar_wait(full(st), (n / ST) & 1, abort_flag);
+        const int* const kp = (const int*)(sm + st * kStage + kTileBytes) + kw * 16;
+        int pos[2] = {0, 0};
+        if (OPT && a.slopes) { pos[0] = kp[g8]; pos[1] = kp[g8 + 8]; }
+        uint32_t kf[KK][4];
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) ldsm(from + tile_at(kw * 16 + (lane & 15), kk * 2 + (lane >> 4)), kf[kk]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty(st));
+        const int j0 = t * kTileKeys + kw * 16;
         const bool tail = j0 + 16 > n_old;
-        float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};               // of keys 8 nb + 2 (lane % 4) + e
+        float sum[2] = {0.f, 0.f};                                // of keys g8 and g8 + 8, this thread's rows
 #pragma unroll 1
         for (int rb = 0; rb < n_blocks; ++rb) {
           float s[2][4] = {};
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            uint32_t qf[4], kf[4];
-            ldsm(base + kQ + chunk_at<D>(rb * 16 + ((lane >> 3) & 1) * 8 + (lane & 7), kk * 2 + (lane >> 4)), qf);
-            ldsm(from + chunk_at<D>(warp * 16 + (lane >> 4) * 8 + (lane & 7), kk * 2 + ((lane >> 3) & 1)), kf);
-            mma_16x8x16(s[0], qf[0], qf[1], qf[2], qf[3], kf[0], kf[1]);
-            mma_16x8x16(s[1], qf[0], qf[1], qf[2], qf[3], kf[2], kf[3]);
+          for (int kk = 0; kk < KK; kk += 2) {
+            uint32_t qf[4];
+            ldsm(base + kQ + chunk_at<D>(rb * 8 + (lane & 7), kk * 2 + (lane >> 3)), qf);
+            mma_16x8x16(s[0], kf[kk][0], kf[kk][1], kf[kk][2], kf[kk][3], qf[0], qf[1]);
+            mma_16x8x16(s[1], kf[kk + 1][0], kf[kk + 1][1], kf[kk + 1][2], kf[kk + 1][3], qf[2], qf[3]);
           }
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const int row = rb * 16 + (lane >> 2) + 8 * x;
+            const int row = rb * 8 + 2 * t4 + x;
             const float ref = lse[row];
             RowOptions ro{};
             if (OPT || tail) ro = opts[row];
 #pragma unroll
-            for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int jj = nb * 8 + (lane & 3) * 2 + e;
-                float v = OPT ? biased(a, s[nb][2 * x + e], ro, a.slopes ? kp[jj] : 0) : s[nb][2 * x + e] * a.scale2;
-                if (tail && (j0 + jj >= cur.keys || !sees(ro.seen, j0 + jj, n_old))) v = -INFINITY;
-                sum[nb][e] += ref == INFINITY ? 0.f : fast_exp2(v - ref);
-              }
+            for (int y = 0; y < 2; ++y) {
+              const int j = j0 + g8 + 8 * y;
+              const float dot = s[0][2 * y + x] + s[1][2 * y + x];
+              float v = OPT ? biased(a, dot, ro, pos[y]) : dot * a.scale2;
+              if (tail && (j >= cur.keys || !sees(ro.seen, j, n_old))) v = -INFINITY;
+              sum[y] += ref == INFINITY ? 0.f : fast_exp2(v - ref);
+            }
           }
         }
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-#pragma unroll
-            for (int d = 4; d < 32; d *= 2) sum[nb][e] += __shfl_xor_sync(0xffffffffu, sum[nb][e], d);
-          }
-        // lane l < 16 has key l: nb = l / 8, l % 8 = 2 (source lane) + e
-        float mine = 0.f;
-#pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float v = __shfl_sync(0xffffffffu, sum[nb][e], (lane & 7) >> 1);
-            if ((lane >> 3 & 1) == nb && (lane & 1) == e) mine = v;
-          }
-        if (lane < 16 && j0 + lane < cur.keys) {
-          const float old = w[j0 + lane];
-          w[j0 + lane] = (r0 == 0 ? a.decay * old : old) + mine;
+        for (int y = 0; y < 2; ++y) {
+          sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 1);
+          sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
+        }
+        if (t4 < 2) {                                             // lane t4 = y of the four has key g8 + 8 y
+          const int j = j0 + g8 + 8 * t4;
+          if (j < cur.keys) w[j] = (round == 0 ? a.decay * w[j] : w[j]) + (t4 ? sum[1] : sum[0]);
         }
       }
+      if (rounds > 1) __threadfence_block();                      // (another warp may have the key in the next round)
     }
-    at += t1 - t0;
+    left -= t1 - t0;
     cur.t = t1 - 1;
-    if (at < hi) advance(cur, a.c, a.n_new, kTileKeys, 1);
+    if (left > 0) advance(cur, a.c, a.n_new, kTileKeys, 1);
   }
 }
 
-template <int D, int WR, int WK, bool OPT>
-cudaError_t launch_one(const AttendArgs& a, cudaStream_t st) {
-  using S = AttendShape<D, WR, WK>;
-  const cudaError_t e = allow_smem<attend_mma<D, WR, WK, OPT>>(S::kSmem);
-  return e != cudaSuccess ? e : launch_pdl(attend_mma<D, WR, WK, OPT>, dim3(a.ctas), dim3(S::THREADS), S::kSmem, st, a);
-}
-template <int D, bool OPT>
-cudaError_t launch_rows(const AttendArgs& a, const AttendPlan& p, cudaStream_t st) {
-  return p.rb == 16 ? launch_one<D, 1, 4, OPT>(a, st) : p.rb == 32 ? launch_one<D, 2, 4, OPT>(a, st) : launch_one<D, 4, 2, OPT>(a, st);
-}
 bool options(const AttendArgs& a) { return a.cap2 != 0.f || a.slopes; }
+bool encode(const Ctx& ctx, const AttendArgs& a, CacheMaps* m) {
+  const CacheView& c = a.c;
+  const int batch = c.units / c.n_kv;
+  return tc_encode_cache(ctx, &m->k, c.k, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTileKeys) &&
+         tc_encode_cache(ctx, &m->v, c.v, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTileKeys);
+}
 
+template <int D, int NR, int WR, int NG, bool OPT>
+cudaError_t launch_one(const AttendArgs& a, const CacheMaps& m, cudaStream_t st) {
+  using S = AttendShape<D, NR, WR, NG>;
+  const cudaError_t e = allow_smem<attend_mma<D, NR, WR, NG, OPT>>(S::kSmem);
+  return e != cudaSuccess ? e : launch_pdl(attend_mma<D, NR, WR, NG, OPT>, dim3(a.ctas), dim3(S::THREADS), S::kSmem, st, a, m);
+}
 template <int D, bool OPT>
-cudaError_t launch_weigh(const AttendArgs& a, const unsigned long long* accepted, int ctas, cudaStream_t st) {
+cudaError_t launch_rows(const AttendArgs& a, const AttendPlan& p, const CacheMaps& m, cudaStream_t st) {
+  switch (p.rb) {
+    case 8: return launch_one<D, 1, 1, 4, OPT>(a, m, st);
+    case 16: return launch_one<D, 2, 1, 2, OPT>(a, m, st);
+    case 32: return launch_one<D, 2, 2, 1, OPT>(a, m, st);
+    default: return launch_one<D, 4, 2, 1, OPT>(a, m, st);
+  }
+}
+template <int D, bool OPT>
+cudaError_t launch_weigh(const AttendArgs& a, const CacheMaps& m, const unsigned long long* accepted, int ctas, cudaStream_t st) {
   const cudaError_t e = allow_smem<weigh_mma<D, OPT>>(weigh_smem<D>());
-  return e != cudaSuccess ? e : launch_pdl(weigh_mma<D, OPT>, dim3(ctas), dim3(kWeighWarps * 32), weigh_smem<D>(), st, a, accepted);
+  return e != cudaSuccess ? e : launch_pdl(weigh_mma<D, OPT>, dim3(ctas), dim3(32 + kWeighWarps * 32), weigh_smem<D>(), st, a, m, accepted);
 }
 
 }  // namespace
 
 cudaError_t launch_attend_mma(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st) {
-  if (ctx.cfg.head_dim == 128) return options(a) ? launch_rows<128, true>(a, p, st) : launch_rows<128, false>(a, p, st);
-  return options(a) ? launch_rows<64, true>(a, p, st) : launch_rows<64, false>(a, p, st);
+  CacheMaps m;
+  if (!encode(ctx, a, &m)) return cudaErrorInvalidValue;
+  if (ctx.cfg.head_dim == 128) return options(a) ? launch_rows<128, true>(a, p, m, st) : launch_rows<128, false>(a, p, m, st);
+  return options(a) ? launch_rows<64, true>(a, p, m, st) : launch_rows<64, false>(a, p, m, st);
 }
 
 cudaError_t launch_weigh_bf16(const Ctx& ctx, const AttendArgs& a, const unsigned long long* accepted, cudaStream_t st) {
-  const int ctas = 2 * ctx.sm_count;
-  if (ctx.cfg.head_dim == 128) return options(a) ? launch_weigh<128, true>(a, accepted, ctas, st) : launch_weigh<128, false>(a, accepted, ctas, st);
-  return options(a) ? launch_weigh<64, true>(a, accepted, ctas, st) : launch_weigh<64, false>(a, accepted, ctas, st);
+  CacheMaps m;
+  if (!encode(ctx, a, &m)) return cudaErrorInvalidValue;
+  const int ctas = ctx.sm_count;
+  if (ctx.cfg.head_dim == 128) return options(a) ? launch_weigh<128, true>(a, m, accepted, ctas, st) : launch_weigh<128, false>(a, m, accepted, ctas, st);
+  return options(a) ? launch_weigh<64, true>(a, m, accepted, ctas, st) : launch_weigh<64, false>(a, m, accepted, ctas, st);
 }
 
 }  // namespace skv

@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
         float x = biased(a, s[r], ro[r], kp);
         if (j >= keys || !sees(ro[r].seen, j, n_old)) x = -INFINITY;
         if (a.accumulate && (lane & 3) == 0 && j < keys && rb * R + r < a.rows)
-          a.logits[((size_t)u * a.group + rb * R + r) * a.c.capacity + j] = x;
+          a.logits[((size_t)u * a.c.capacity + j) * a.group + rb * R + r] = x;
         float top = x;
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
