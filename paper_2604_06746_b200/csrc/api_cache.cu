@@ -12,10 +12,10 @@ namespace {
 AttendPlan attend_plan(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
   if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms};
-  return {rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64, 64, sms};
+  return {rows <= 8 ? 8 : 16, 64, sms};
 }
 
-struct AttendWs { int* unit_start; float2* part_stat; float *part_out, *row_lse, *logits; size_t bytes; };
+struct AttendWs { int* unit_start; float2* part_stat; float *part_out, *logits; size_t bytes; };
 AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch, int n_new, int capacity, void* base) {
   AttendWs w{};
   char* at = (char*)base;
@@ -27,12 +27,10 @@ AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch
   };
   const size_t units = (size_t)batch * cfg.n_kv_heads, group = cfg.n_q_heads / cfg.n_kv_heads;
   w.unit_start = (int*)take((units + 1) * sizeof(int));
-  w.part_stat = (float2*)take((size_t)2 * p.ctas * p.rb * sizeof(float2));
-  w.part_out = (float*)take((size_t)2 * p.ctas * p.rb * cfg.head_dim * sizeof(float));
-  if (n_new == 1) {
-    w.row_lse = (float*)take(units * group * sizeof(float));
-    w.logits = (float*)take(units * group * capacity * sizeof(float));
-  }
+  const size_t slots = units * ((group * n_new + p.rb - 1) / p.rb) + p.ctas;
+  w.part_stat = (float2*)take(slots * p.rb * sizeof(float2));
+  w.part_out = (float*)take(slots * p.rb * cfg.head_dim * sizeof(float));
+  if (n_new == 1) w.logits = (float*)take(units * group * capacity * sizeof(float));
   w.bytes = off;
   return w;
 }
@@ -88,6 +86,9 @@ bool args_of(const structkv_ctx* ctx, const structkv_attend_args* x, AttendArgs*
   a->n_new = x->n_new;
   a->group = cfg.n_q_heads / cfg.n_kv_heads;
   a->rows = a->group * x->n_new;
+  a->by_kv = div_by(cfg.n_kv_heads);
+  a->by_group = div_by(a->group);
+  a->by_rows = div_by(a->rows);
   a->scale2 = x->scale * kLog2e;
   a->cap2 = cap2;
   a->inv_cap = inv;
@@ -132,11 +133,13 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
   a.unit_start = w.unit_start;
   a.part_stat = w.part_stat;
   a.part_out = w.part_out;
-  a.row_lse = w.row_lse;
   a.logits = w.logits;
   a.ctas = plan.ctas;
   cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e = args->rows ? launch_append(a.c, r, args->n_new, st) : cudaSuccess;
+  // A few rows are appended by the kernel itself; a warp that copies more of them holds its tiles up.
+  cudaError_t e = cudaSuccess;
+  if (args->rows && c.cfg.dtype == STRUCTKV_BF16 && args->n_new <= 8) a.fresh = r;
+  else if (args->rows) e = launch_append(a.c, r, args->n_new, st);
   if (e == cudaSuccess) e = c.cfg.dtype == STRUCTKV_BF16 ? launch_attend_mma(c, a, plan, st) : launch_attend_simt(c, a, plan, st);
   if (e == cudaSuccess) e = launch_attend_finish(c, a, plan, st);
   return told(e);

@@ -2,10 +2,10 @@
 //
 // A unit is (sequence, KV head) u = b H_kv + g, with lengths[u] + n_new keys (the new tokens are the last ones) and rows
 // r = i G + h, new token i and head h of the group.  An item is a unit's block of up to RB rows over all of its keys; items
-// follow one another unit after unit, and their key tiles form one sequence of W tiles.  CTA c of C takes tiles
-// [c W / C, (c + 1) W / C): every CTA reads equally much whatever the lengths, which only the device knows.  An item that
-// lies in one CTA is finished there; of the others each CTA leaves a partial (row maximum, sum, unscaled output), which
-// attend_finish() merges in the order of the CTAs: results do not depend on timing.
+// follow one another unit after unit, and their key tiles form one sequence of W tiles.  C CTAs take runs of it whose lengths
+// differ by one tile at most: every CTA reads equally much whatever the lengths, which only the device knows.  What a CTA has of
+// an item it leaves as a partial (row references, sums, unscaled output) in slot item + CTA, which no other pair has, so that an
+// item's partials lie side by side; attend_finish() merges them in that order: results do not depend on timing.
 #pragma once
 
 #include <atomic>
@@ -32,8 +32,17 @@ inline __host__ __device__ size_t unit_offset(const CacheView& c, int u) {
 
 struct NewRows { const char *k, *v; long long s_batch, s_token, s_head; const int* positions; };
 
+// Division by a number that the launch knows, of n < 2^31.
+struct Div { unsigned mul, shift; };
+inline Div div_by(unsigned d) {
+  unsigned s = 0;
+  while (1ull << s < d) ++s;
+  return {(unsigned)((((1ull << s) - d) << 32) / d + 1), s};
+}
+
 struct AttendArgs {
   CacheView c;
+  Div by_kv, by_group, by_rows;        // H_kv, group, rows
   const char* q;                       // element strides in bytes
   long long q_batch, q_token, q_head;
   int n_new, group, rows;              // rows = n_new * group
@@ -45,11 +54,11 @@ struct AttendArgs {
   char* out;                           // [batch, n_new, H, d]
   float* lse;                          // [batch, n_new, H] or NULL
   bool accumulate;                     // (n_new = 1)
+  NewRows fresh;                       // the new tokens' rows, where the kernel appends them; k NULL: they are in the cache
   // workspace
-  int* unit_start;                     // [units + 1] tiles before a unit
-  float2* part_stat;                   // [2 ctas][RB] maximum and sum
-  float* part_out;                     // [2 ctas][RB][d]
-  float* row_lse;                      // [units][rows] in bits (accumulate)
+  int* unit_start;                     // [units + 1] tiles before a unit, of one block of rows
+  float2* part_stat;                   // [slot][RB] reference (bits) and sum
+  float* part_out;                     // [slot][RB][d]
   float* logits;                       // [units][capacity][group] in bits (accumulate)
   int ctas;
 };
@@ -94,32 +103,58 @@ __device__ __forceinline__ int unit_keys(const CacheView& c, int u, int n_new) {
   return n + n_new;
 }
 
-// First tile of CTA c of C, and the CTA that has tile x.  C is at most W, so that no CTA in between is without a tile; those from
-// C on have none.
-__device__ __forceinline__ int sharers(long long W, int ctas) { return (int)min(W, (long long)ctas); }
-__device__ __forceinline__ long long cut(int c, long long W, int C) { return c >= C ? W : c * W / C; }
-__device__ __forceinline__ int cta_of(long long x, long long W, int C) { return (int)(((x + 1) * C - 1) / W); }
+// Rows, positions and weight 0 of a unit's new tokens, by a warp: to slots n and up.
+__device__ __forceinline__ void append_rows(const CacheView& c, const NewRows& r, int n_new, int u, int b, int g, int n, int lane) {
+  const size_t off = unit_offset(c, u);
+  const int per_row = c.row_bytes / 16;
+  for (int tok = 0; tok < n_new; ++tok) {
+    const size_t from = (size_t)b * r.s_batch + (size_t)tok * r.s_token + (size_t)g * r.s_head, to = off + (size_t)(n + tok) * c.s_token;
+    for (int i = lane; i < 2 * per_row; i += 32) {
+      const int ch = i < per_row ? i : i - per_row;
+      *(uint4*)((i < per_row ? c.k : c.v) + to + ch * 16) = *(const uint4*)((i < per_row ? r.k : r.v) + from + ch * 16);
+    }
+  }
+  const size_t w = (size_t)u * c.capacity + n;
+  for (int i = lane; i < n_new; i += 32) {
+    c.positions[w + i] = r.positions[(size_t)b * n_new + i];
+    if (c.weights) c.weights[w + i] = 0.f;
+  }
+}
 
-struct WorkStart { int unit, before; long long total; };   // unit that holds a tile, tiles before the unit, tiles of all units
+__device__ __forceinline__ int quotient(int n, Div d) { return (int)((__umulhi((unsigned)n, d.mul) + (unsigned)n) >> d.shift); }
 
-// By the whole block: tiles of all units, and the unit that holds tile number want(total).  Units are scanned THREADS at a time.
-// save: unit_start.
-template <int THREADS, typename Want>
-__device__ __forceinline__ WorkStart find_work(const CacheView& c, int n_new, int tile, int blocks, Want want, int* save) {
+// How W tiles are shared out: CTA c has tiles [first(c), first(c + 1)); no more CTAs than tiles, so that each has one.
+struct Shares { int W, C, each, more; };
+__device__ __forceinline__ Shares shares_of(int W, int ctas) {
+  const int C = max(1, min(W, ctas)), each = W / C;
+  return {W, C, each, W - each * C};
+}
+__device__ __forceinline__ int first_of(const Shares& s, int c) { return c >= s.C ? s.W : c * s.each + min(c, s.more); }
+__device__ __forceinline__ int cta_of(const Shares& s, int x) {
+  const int line = s.more * (s.each + 1);
+  return x < line ? x / (s.each + 1) : s.more + (x - line) / s.each;
+}
+
+// A CTA's run of tiles, and the unit that its first tile is in: keys, tiles of one block of rows before it.
+struct WorkStart { int lo, hi, unit, before, keys; };
+
+// By the whole block.  Units are scanned THREADS at a time.  save: unit_start.
+template <int THREADS>
+__device__ __forceinline__ WorkStart find_work(const CacheView& c, int n_new, int tile, int blocks, int ctas, int* save) {
   constexpr int WARPS = THREADS / 32;
-  __shared__ int warp_tiles[WARPS], hit[2];
-  __shared__ long long sum;
+  __shared__ int warp_tiles[WARPS], hit[3];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // (one round where the units fit the block; total is known only after all rounds, so a second sweep looks for the tile)
-  long long total = 0;
-  int mine = 0, incl = 0;
+  // (one round where the units fit the block; the sum of all is known only after all of them, so that a second sweep follows)
+  int total = 0, mine = 0, incl = 0, keys = 0, lo = 0, hi = 0;
+#pragma unroll 1
   for (int round = 0; round < 2; ++round) {
-    long long before = 0;
-    const long long at = round ? want(total) : 0;
+    int before = 0;
+#pragma unroll 1
     for (int u0 = 0; u0 < c.units; u0 += THREADS) {
       if (round == 0 || c.units > THREADS) {
         const int u = u0 + tid;
-        mine = u < c.units ? (unit_keys(c, u, n_new) + tile - 1) / tile * blocks : 0;
+        keys = u < c.units ? unit_keys(c, u, n_new) : 0;
+        mine = (keys + tile - 1) / tile;
         incl = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -129,28 +164,27 @@ __device__ __forceinline__ WorkStart find_work(const CacheView& c, int n_new, in
         __syncthreads();
         if (lane == 31) warp_tiles[warp] = incl;
         __syncthreads();
-        int earlier = 0, all = 0;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-          earlier += w < warp ? warp_tiles[w] : 0;
-          all += warp_tiles[w];
-        }
-        incl += earlier;
-        if (round == 0 && save && u < c.units) save[u] = (int)(before + incl - mine);
-        if (tid == 0) sum = all;
+        const int w = lane < WARPS ? warp_tiles[lane] : 0;
+        incl += before + (int)__reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
+        before += (int)__reduce_add_sync(0xffffffffu, w);
+        if (round == 0 && save && u < c.units) save[u] = incl - mine;
       }
-      if (round == 1 && before + incl - mine <= at && at < before + incl) {
+      if (round == 1 && (incl - mine) * blocks <= lo && lo < incl * blocks) {
         hit[0] = u0 + tid;
-        hit[1] = (int)(before + incl - mine);
+        hit[1] = incl - mine;
+        hit[2] = keys;
       }
-      __syncthreads();
-      before += sum;
     }
-    total = before;
+    if (round == 0) {
+      total = before;
+      const Shares s = shares_of(total * blocks, ctas);
+      lo = first_of(s, blockIdx.x);
+      hi = first_of(s, blockIdx.x + 1);
+    }
   }
-  if (save && tid == 0) save[c.units] = (int)total;
+  if (save && tid == 0) save[c.units] = total;
   __syncthreads();
-  return {hit[0], hit[1], total};
+  return {lo, hi, hit[0], hit[1], hit[2]};
 }
 
 // cap tanh(scale s / cap) in bits: for small arguments the odd series, else 1 - 2 / (e^2y + 1), both to fp32's last bits.
@@ -170,17 +204,21 @@ __device__ __forceinline__ float capped(float s, float cap2, float inv_cap) {
 
 // The new tokens that row r of a unit sees, as bits.
 __device__ __forceinline__ unsigned long long row_seen(const AttendArgs& a, int u, int r) {
-  const int i = r / a.group;
-  return a.tree ? a.tree[(size_t)(u / a.c.n_kv) * a.n_new + i] : (i == 63 ? ~0ull : (1ull << (i + 1)) - 1);
+  const int i = quotient(r, a.by_group);
+  return a.tree ? a.tree[(size_t)quotient(u, a.by_kv) * a.n_new + i] : (i == 63 ? ~0ull : (1ull << (i + 1)) - 1);
 }
 // A row's option values.
 struct RowOptions { unsigned long long seen; float slope2; int position; };
 __device__ __forceinline__ RowOptions row_options(const AttendArgs& a, int u, int r) {
   RowOptions o;
-  const int g = u % a.c.n_kv, i = r / a.group, h = r % a.group;
   o.seen = row_seen(a, u, r);
-  o.slope2 = a.slopes ? a.slopes[g * a.group + h] * kLog2e : 0.f;
-  o.position = a.slopes ? a.c.positions[(size_t)u * a.c.capacity + a.c.lengths[u] + i] : 0;
+  o.slope2 = 0.f;
+  o.position = 0;
+  if (a.slopes) {
+    const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, i = quotient(r, a.by_group), h = r - i * a.group;
+    o.slope2 = a.slopes[g * a.group + h] * kLog2e;
+    o.position = a.fresh.k ? a.fresh.positions[(size_t)b * a.n_new + i] : a.c.positions[(size_t)u * a.c.capacity + a.c.lengths[u] + i];
+  }
   return o;
 }
 // Whether key j of a unit whose first n tokens are old is seen.

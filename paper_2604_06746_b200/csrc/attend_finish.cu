@@ -1,9 +1,11 @@
-// What follows the attention kernels: items that several CTAs took are merged, and for single tokens every key's attention
-// weight is added to what it has gathered.
+// What follows the attention kernels: an item's partials are merged, and for single tokens every key's attention weight is
+// added to what it has gathered.
 //
-// Merging: a warp per row; with the CTAs' maxima m_c and sums l_c, M = max m_c, out = sum 2^(m_c - M) O_c / sum 2^(m_c - M) l_c,
-// c ascending.  Weights: the attention kernel left every logit (4 bytes a head and key beside the 4 d bytes of K and V that it
-// read; the second reading of K that would spare them is 2 d); block c takes the keys of run c of C of all tiles.
+// Merging: a warp per row; with the partials' references m_c and sums l_c, M = max m_c, out = sum 2^(m_c - M) O_c / sum 2^(m_c - M)
+// l_c, c ascending.  Weights: the attention kernel left every logit (4 bytes a head and key beside the 4 d bytes of K and V that
+// it read; the second reading of K that would spare them is 2 d); block c takes the keys of run c of all tiles.
+// Bound by the chain of loads: where the partials lie follows from unit_start, their weights from their references.  With
+// 64-bit divisions for the former the code alone (51 KB, fetched once a launch) took 10 us.
 #include "attend.cuh"
 
 namespace skv {
@@ -11,108 +13,118 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// CTAs that took an item, and the slot of CTA c.
-struct Cover { int first, last; };
-__device__ __forceinline__ Cover cover_of(long long start, int tiles, long long W, int C) {
-  return {cta_of(start, W, C), cta_of(start + tiles - 1, W, C)};
+// First partial of an item and how many it has.
+struct Parts { int first, count; };
+__device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, int tiles) {
+  const int c0 = cta_of(s, start), c1 = tiles == 1 ? c0 : cta_of(s, start + tiles - 1);
+  return {item + c0, c1 - c0 + 1};
 }
-__device__ __forceinline__ int slot_of(const Cover& v, int c) { return 2 * c + (c == v.first); }   // it begins there, or goes on
-
-// Maximum and sum of a row over its CTAs, by a warp (the same in every lane).
-__device__ __forceinline__ float2 merged_stat(const AttendArgs& a, const Cover& v, int rb_rows, int row, int lane) {
-  float M = -INFINITY;
-  for (int c = v.first + lane; c <= v.last; c += 32) M = fmaxf(M, a.part_stat[(size_t)slot_of(v, c) * rb_rows + row].x);
+// Reference and sum of a row over its partials, by a warp (the same in every lane).
+__device__ __forceinline__ float2 merged(const float2* __restrict__ stat, Parts p, int rb_rows, int row, int lane) {
+  float M = -INFINITY, L = 0.f;
+  float2 mine = make_float2(-INFINITY, 0.f);
+#pragma unroll 1
+  for (int c = lane; c < p.count; c += 32) {                      // (more than 32: their sums as they come)
+    const float2 x = stat[(size_t)(p.first + c) * rb_rows + row];
+    const float top = fmaxf(mine.x, x.x), ref = top == -INFINITY ? 0.f : top;
+    mine = make_float2(top, mine.y * fast_exp2(mine.x - ref) + x.y * fast_exp2(x.x - ref));
+  }
+  M = mine.x;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  if (M == -INFINITY) return make_float2(M, 0.f);
-  float L = 0.f;
-  for (int c = v.first + lane; c <= v.last; c += 32) {
-    const float2 p = a.part_stat[(size_t)slot_of(v, c) * rb_rows + row];
-    L += p.y * fast_exp2(p.x - M);
-  }
+  L = mine.y * fast_exp2(mine.x - (M == -INFINITY ? 0.f : M));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
   return make_float2(M, L);
 }
-__device__ __forceinline__ float bits_of(float2 st) { return st.x == -INFINITY ? st.x : st.x + log2f(st.y); }
+// (a row that saw nothing has reference minus infinity and sum 0, one that saw only NaN has its sum)
+__device__ __forceinline__ float bits_of(float2 st) { return st.x == -INFINITY && st.y == 0.f ? st.x : st.x == -INFINITY ? st.y : st.x + log2f(st.y); }
+
+template <int DL>
+struct Cols { float v[DL]; };
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant__ AttendArgs a, int rb_rows, int tile) {
+__global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant__ AttendArgs a, int rb_shift, int tile_shift) {
   constexpr int DL = D / 32;
   __shared__ int hit;
   __shared__ float lse[kThreads];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int blocks = (a.rows + rb_rows - 1) / rb_rows;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rb_rows = 1 << rb_shift;
+  const int blocks = (a.rows + rb_rows - 1) >> rb_shift;
   pdl_trigger();
   pdl_wait();
-  const long long W = a.unit_start[a.c.units];
-  if (W == 0) return;
-  const int C = sharers(W, a.ctas);
+  const int W1 = a.unit_start[a.c.units];                         // tiles of one block of rows each
+  if (W1 == 0) return;
+  const Shares sh = shares_of(W1 * blocks, a.ctas);
   const int all_rows = a.c.units * a.rows;
+#pragma unroll 1
   for (int i = blockIdx.x * (kThreads / 32) + warp; i < all_rows; i += gridDim.x * (kThreads / 32)) {
-    const int u = i / a.rows, r = i % a.rows, rb = r / rb_rows, row = r % rb_rows;
-    const int start = a.unit_start[u], tiles = (a.unit_start[u + 1] - start) / blocks;
+    const int u = quotient(i, a.by_rows), r = i - u * a.rows, rb = r >> rb_shift, row = r & (rb_rows - 1);
+    const int start = a.unit_start[u], tiles = a.unit_start[u + 1] - start;
     if (tiles == 0) continue;
-    const Cover v = cover_of((long long)start + (long long)rb * tiles, tiles, W, C);
-    if (v.first == v.last) continue;                              // finished there
-    const float2 st = merged_stat(a, v, rb_rows, row, lane);
-    float acc[DL] = {};
-    if (st.x != -INFINITY) {
+    const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles);
+    const float2 st = merged(a.part_stat, p, rb_rows, row, lane);
+    const float ref = st.x == -INFINITY ? 0.f : st.x;
+    Cols<DL> acc{};
 #pragma unroll 4
-      for (int c = v.first; c <= v.last; ++c) {
-        const size_t at = (size_t)slot_of(v, c) * rb_rows + row;
-        const float f = fast_exp2(a.part_stat[at].x - st.x);
+    for (int c = 0; c < p.count; ++c) {
+      const size_t at = (size_t)(p.first + c) * rb_rows + row;
+      const float f = fast_exp2(a.part_stat[at].x - ref);
+      const Cols<DL> x = *(const Cols<DL>*)(a.part_out + at * D + lane * DL);
 #pragma unroll
-        for (int e = 0; e < DL; ++e) acc[e] = fmaf(f, a.part_out[at * D + e * 32 + lane], acc[e]);
-      }
+      for (int e = 0; e < DL; ++e) acc.v[e] = fmaf(f, x.v[e], acc.v[e]);
     }
-    const float inv = st.x == -INFINITY ? 0.f : 1.f / st.y;
-    const int b = u / a.c.n_kv, g = u % a.c.n_kv, tok = r / a.group, h = r % a.group;
+    const float inv = st.x == -INFINITY ? 0.f : 1.f / st.y;       // (a NaN row stays one)
+    const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, tok = quotient(r, a.by_group), h = r - tok * a.group;
     const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
 #pragma unroll
     for (int e = 0; e < DL; ++e) {
-      if (BF16) ((__nv_bfloat16*)a.out)[q * D + e * 32 + lane] = __float2bfloat16(acc[e] * inv);
-      else ((float*)a.out)[q * D + e * 32 + lane] = acc[e] * inv;
+      if (BF16) ((__nv_bfloat16*)a.out)[q * D + lane * DL + e] = __float2bfloat16(acc.v[e] * inv);
+      else ((float*)a.out)[q * D + lane * DL + e] = acc.v[e] * inv;
     }
     if (lane == 0 && a.lse) a.lse[q] = bits_of(st) * kLn2;
   }
   if (!a.accumulate) return;
 
-  // tiles of all units, one block of rows each
-  const long long W1 = W / blocks, lo = cut(blockIdx.x, W1, sharers(W1, gridDim.x)), hi = cut(blockIdx.x + 1, W1, sharers(W1, gridDim.x));
+  const Shares runs = shares_of(W1, gridDim.x);
+  const int lo = first_of(runs, blockIdx.x), hi = first_of(runs, blockIdx.x + 1);
   if (lo >= hi) return;
+#pragma unroll 1
   for (int u = tid; u < a.c.units; u += kThreads)
-    if (a.unit_start[u] / blocks <= lo && lo < a.unit_start[u + 1] / blocks) hit = u;
+    if (a.unit_start[u] <= lo && lo < a.unit_start[u + 1]) hit = u;
   __syncthreads();
   int u = hit;
 #pragma unroll 1
-  for (long long at = lo; at < hi; ++u) {
-    const int start = a.unit_start[u], tiles = (a.unit_start[u + 1] - start) / blocks;
+  for (int at = lo; at < hi; ++u) {
+    const int start = a.unit_start[u], tiles = a.unit_start[u + 1] - start;
     if (tiles == 0) continue;
-    const int t0 = (int)(at - start / blocks), t1 = (int)min((long long)tiles, t0 + (hi - at));
-    const int keys = unit_keys(a.c, u, a.n_new);
+    const int t0 = at - start, t1 = min(tiles, t0 + (hi - at));
+    const int keys = a.c.lengths[u] + a.n_new;
     float* const w = a.c.weights + (size_t)u * a.c.capacity;
 #pragma unroll 1
     for (int h0 = 0; h0 < a.group; h0 += kThreads) {              // (one round, but for groups of more than 256 heads)
       const int heads = min(kThreads, a.group - h0);
       __syncthreads();
+#pragma unroll 1
       for (int h = warp; h < heads; h += kThreads / 32) {
-        const int r = h0 + h, rb = r / rb_rows;
-        const Cover v = cover_of((long long)start + (long long)rb * tiles, tiles, W, C);
-        const float x = v.first == v.last ? a.row_lse[(size_t)u * a.rows + r] : bits_of(merged_stat(a, v, rb_rows, r % rb_rows, lane));
+        const int r = h0 + h, rb = r >> rb_shift;
+        const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles);
+        const float x = bits_of(merged(a.part_stat, p, rb_rows, r & (rb_rows - 1), lane));
         if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
       }
       __syncthreads();
       const bool fours = a.group % 4 == 0;
-      for (int j = t0 * tile + tid; j < min(keys, t1 * tile); j += kThreads) {
+#pragma unroll 2
+      for (int j = (t0 << tile_shift) + tid; j < min(keys, t1 << tile_shift); j += kThreads) {
         const float* const x = a.logits + ((size_t)u * a.c.capacity + j) * a.group + h0;
         float sum = 0.f;
         if (fours) {
+#pragma unroll 1
           for (int h = 0; h < heads; h += 4) {
             const float4 v = *(const float4*)(x + h);
             sum += (fast_exp2(v.x - lse[h]) + fast_exp2(v.y - lse[h + 1])) + (fast_exp2(v.z - lse[h + 2]) + fast_exp2(v.w - lse[h + 3]));
           }
         } else {
+#pragma unroll 1
           for (int h = 0; h < heads; ++h) sum += fast_exp2(x[h] - lse[h]);
         }
         w[j] = (h0 == 0 ? a.decay * w[j] : w[j]) + sum;
@@ -122,9 +134,14 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
   }
 }
 
+int log2_of(int x) {
+  int s = 0;
+  while (1 << s < x) ++s;
+  return s;
+}
 template <int D, bool BF16>
 cudaError_t launch(const AttendArgs& a, const AttendPlan& p, int ctas, cudaStream_t st) {
-  return launch_pdl(attend_finish<D, BF16>, dim3(ctas), dim3(kThreads), 0, st, a, p.rb, p.tile);
+  return launch_pdl(attend_finish<D, BF16>, dim3(ctas), dim3(kThreads), 0, st, a, log2_of(p.rb), log2_of(p.tile));
 }
 
 }  // namespace

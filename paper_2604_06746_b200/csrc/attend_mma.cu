@@ -1,9 +1,9 @@
-// Attention of new tokens over a bf16 cache, up to 64 rows of a KV head at a time, and the weight of accepted tokens.
+// Attention of new tokens over a bf16 cache, up to 16 rows of a KV head at a time, and the weight of accepted tokens.
 //
 // Flash form: per row a reference m, sum l and unscaled output O over the keys seen so far; a tile of 64 keys gives
 // S = K Q^T, p = 2^(x - m), l += sum p, O^T += V^T p.  Rows are few and reading K and V is the bound, so keys are the long side of
 // the m16n8k16 products (16 keys x 8 rows, then 16 columns of V x 8 rows): four rows of a single token fill half a product, in
-// the other orientation a quarter.  A warp takes 16 keys of a tile and up to 32 rows; tiles come by TMA (128-byte swizzle)
+// the other orientation a quarter.  A warp takes 16 keys of a tile and all rows; tiles come by TMA (128-byte swizzle)
 // through a ring that one warp fills; NG groups of warps take tiles in turn, each warp with statistics of its own, so that
 // nothing but the ring is waited for, and a segment's end merges the warps.  The reference follows a row's maximum only where
 // that outgrows it by 2^kSlack: p then stays below 2^kSlack, far from overflow, and most tiles need neither shuffles nor scaling.
@@ -80,74 +80,74 @@ __device__ __forceinline__ void advance(Cursor& c, const CacheView& cache, int n
 
 struct CacheMaps { CUtensorMap k, v; };
 
-// NR blocks of 8 rows a warp, WR such warps beside each other, four along a tile's keys, NG groups of these.
-template <int D, int NR, int WR, int NG>
+// NR blocks of 8 rows; four warps along a tile's keys, NG groups of these.
+template <int D, int NR, int NG>
 struct AttendShape {
-  static constexpr int RB = 8 * NR * WR, kGroupWarps = 4 * WR, kWarps = kGroupWarps * NG, THREADS = 32 + kWarps * 32, kSets = 4 * NG;
+  static constexpr int RB = 8 * NR, kWarps = 4 * NG, THREADS = 32 + kWarps * 32, kSets = 4 * NG;
   static constexpr int kTileBytes = kTileKeys * D * 2;
-  static constexpr int kPosOff = 2 * kTileBytes, kQOff = kPosOff + 1024;
-  static constexpr int kStage = kQOff + (RB * D * 2 + 1023) / 1024 * 1024;
-  static constexpr int kRegs = NR * D / 4;                       // output registers of a thread
-  static constexpr int kMerge = kSets / 2 * WR * kRegs * 32 * 4;
-  static constexpr int kFixed = kMerge + 2 * kSets * RB * 4 + 256 + 1024;
-  static constexpr int kStages = std::min(6, (226 * 1024 - kFixed) / kStage);
+  static constexpr int kPosOff = 2 * kTileBytes, kQOff = kPosOff + 1024, kStage = kQOff + RB * D * 2;
+  static constexpr int kRow = D + 4;                             // of a set's output: rows two apart are eight banks apart
+  static constexpr int kFixed = kSets * RB * (kRow + 2) * 4 + 256 + 1024;
+  static constexpr int kStages = std::min(8, (226 * 1024 - kFixed) / kStage);
   static constexpr int kSmem = kStages * kStage + kFixed;
-  static_assert(kStages >= 2, "a ring");
+  static_assert(kStages >= 3 && kStage % 1024 == 0, "a ring");
 };
 
-template <int D, int NR, int WR, int NG, bool OPT>
-__global__ void __launch_bounds__(32 + 128 * WR * NG, 1) attend_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps) {
-  using S = AttendShape<D, NR, WR, NG>;
+template <int D, int NR, int NG, bool OPT>
+__global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps) {
+  using S = AttendShape<D, NR, NG>;
   constexpr int RB = S::RB, NT = S::THREADS, CH = D / 8, ST = S::kStages, KK = D / 16;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
-  float* const merge = (float*)(sm + ST * S::kStage);           // [sets / 2][WR][register][lane]
-  float* const stat = merge + S::kMerge / 4;                    // [2][sets][RB]
+  float* const outs = (float*)(sm + ST * S::kStage);            // [set][RB][kRow]
+  float* const stat = outs + S::kSets * RB * S::kRow;           // [2][set][RB]
   const uint32_t bars = smem_u32(stat + 2 * S::kSets * RB);     // full [ST], empty [ST]
   volatile int* const abort_flag = (volatile int*)(stat + 2 * S::kSets * RB) + 4 * ST;
   auto full = [&](int st) { return bars + 8 * st; };
   auto empty = [&](int st) { return bars + 8 * (ST + st); };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int cta = blockIdx.x, blocks = (a.rows + RB - 1) / RB;
+  const int blocks = (a.rows + RB - 1) / RB;
   pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < ST; ++i) {
       mbar_init(full(i), 33);                                   // the copies by TMA, and 32 lanes' own
-      mbar_init(empty(i), S::kGroupWarps);
+      mbar_init(empty(i), 4);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.v) : "memory");
   }
   pdl_wait();
-  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, blocks, [&](long long W) { return cut(cta, W, sharers(W, gridDim.x)); },
-                                     cta == 0 ? a.unit_start : nullptr);
-  const int C = sharers(ws.total, gridDim.x);
-  const long long lo = cut(cta, ws.total, C), hi = cut(cta + 1, ws.total, C);
-  if (lo >= hi) return;
-  const int run = (int)(hi - lo);
-  Cursor cur;
-  cur.u = ws.unit;
-  enter(cur, a.c, a.n_new, kTileKeys);
-  {
-    const int rest = (int)(lo - ws.before);
-    cur.rb = rest / cur.tiles;
-    cur.t = rest - cur.rb * cur.tiles;
+  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, blocks, a.ctas, blockIdx.x == 0 ? a.unit_start : nullptr);
+  if (ws.lo >= ws.hi) return;
+  const int run = ws.hi - ws.lo;
+  Cursor cur{ws.unit, 0, 0, (ws.keys + kTileKeys - 1) / kTileKeys, ws.keys};
+  cur.t = ws.lo - ws.before * blocks;
+  if (blocks > 1) {
+    cur.rb = cur.t / cur.tiles;
+    cur.t -= cur.rb * cur.tiles;
   }
 
   if (warp == 0) {
     // the ring's producer
-    const uint64_t policy = l2_policy_evict_first();
-    int since = 0;                                              // tiles since the segment began
+    const uint64_t hint = blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
+    int since = 0, st = 0;                                      // tiles since the segment began
     int n = 0;
+#pragma unroll 1
     for (; n < run; ++n) {
-      const int st = n % ST, b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv;
+      const int b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv;
       const uint32_t to = base + st * S::kStage;
       if (cur.t == 0) since = 0;
+      if (a.fresh.k && (cur.t + 1) * kTileKeys > cur.keys - a.n_new) {
+        append_rows(a.c, a.fresh, a.n_new, cur.u, b, g, cur.keys - a.n_new, lane);
+        asm volatile("fence.proxy.async;" ::: "memory");        // they are read by TMA
+        __syncwarp();
+      }
       if (n >= ST && !mbar_wait_producer(empty(st), (n / ST - 1) & 1, abort_flag, kWaitCycles)) break;
       if (lane == 0) {
         mbar_expect_tx(full(st), 2 * S::kTileBytes);
-        const uint64_t hint = blocks == 1 ? policy : l2_policy_evict_normal();
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
           tma_load_4d(to + c * kTileKeys * 128, &maps.k, full(st), c * 64, cur.t * kTileKeys, g, b, hint);
@@ -163,16 +163,18 @@ __global__ void __launch_bounds__(32 + 128 * WR * NG, 1) attend_mma(const __grid
         }
       }
       if (since < NG) {                                         // a segment begins: every group's first tile brings the rows
+#pragma unroll 1
         for (int i = lane; i < RB * CH; i += 32) {
           const int row = i / CH, ch = i % CH, r = cur.rb * RB + row;
           const bool is = r < a.rows;
-          const int tok = is ? r / a.group : 0, h = is ? r - tok * a.group : 0;
+          const int tok = is ? quotient(r, a.by_group) : 0, h = is ? r - tok * a.group : 0;
           cp16(to + S::kQOff + chunk_at<D>(row, ch),
                a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head + ch * 16, is);
         }
       }
       cp_arrive(full(st));
       ++since;
+      if (++st == ST) st = 0;
       if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
     }
     if (*abort_flag) {
@@ -183,8 +185,7 @@ __global__ void __launch_bounds__(32 + 128 * WR * NG, 1) attend_mma(const __grid
     return;
   }
 
-  const int cw = warp - 1, grp = cw / S::kGroupWarps, wr = cw % S::kGroupWarps / 4, kw = cw % 4;
-  const int g8 = lane >> 2, t4 = lane & 3;
+  const int cw = warp - 1, grp = cw / 4, kw = cw % 4, g8 = lane >> 2, t4 = lane & 3;
   auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(S::kWarps * 32) : "memory"); };
   uint32_t qf[NR][KK][2];
   float o[NR][KK][4];                                           // column g8 (+ 8) of 16, rows 2 t4 and + 1 of the block
@@ -192,38 +193,29 @@ __global__ void __launch_bounds__(32 + 128 * WR * NG, 1) attend_mma(const __grid
   float slope2[NR][2];
   int place[NR][2];
   bool fresh = true;                                            // nothing of this segment yet
-  int seg_first = 0;                                            // 1: the segment begins the item
-  auto clear = [&]() {
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x) { m[i][x] = -INFINITY; l[i][x] = 0.f; }
-#pragma unroll
-      for (int k = 0; k < KK; ++k) o[i][k][0] = o[i][k][1] = o[i][k][2] = o[i][k][3] = 0.f;
-    }
-    fresh = true;
-  };
-  clear();
   int seg = 0;                                                  // first tile of the segment in the run
-  seg_first = cur.t == 0;
 #pragma unroll 1
-  for (int n = 0; n < run; ++n) {
-    const int first_row = cur.rb * RB + wr * 8 * NR + 2 * t4;   // row of (block i, x): first_row + 8 i + x
+  for (int n = 0, st = 0; n < run; ++n, st = st + 1 == ST ? 0 : st + 1) {
+    const int first_row = cur.rb * RB + 2 * t4;                 // row of (block i, x): first_row + 8 i + x
     if (n % NG == grp) {
-      const int st = n % ST;
       const uint32_t from = base + st * S::kStage;
       const unsigned char* const here = sm + st * S::kStage;
       mbar_wait(full(st), (n / ST) & 1, abort_flag);            // (on expiry the numbers are void, the control flow goes on)
       if (fresh) {
         fresh = false;
 #pragma unroll
-        for (int i = 0; i < NR; ++i)
+        for (int i = 0; i < NR; ++i) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) { m[i][x] = -INFINITY; l[i][x] = 0.f; }
+#pragma unroll
+          for (int k = 0; k < KK; ++k) o[i][k][0] = o[i][k][1] = o[i][k][2] = o[i][k][3] = 0.f;
 #pragma unroll
           for (int kk = 0; kk < KK; kk += 2) {
             uint32_t x[4];
-            ldsm(from + S::kQOff + chunk_at<D>((wr * NR + i) * 8 + (lane & 7), kk * 2 + (lane >> 3)), x);
+            ldsm(from + S::kQOff + chunk_at<D>(i * 8 + (lane & 7), kk * 2 + (lane >> 3)), x);
             qf[i][kk][0] = x[0]; qf[i][kk][1] = x[1]; qf[i][kk + 1][0] = x[2]; qf[i][kk + 1][1] = x[3];
           }
+        }
         if (OPT && a.slopes)
 #pragma unroll
           for (int i = 0; i < NR; ++i)
@@ -293,7 +285,7 @@ __global__ void __launch_bounds__(32 + 128 * WR * NG, 1) attend_mma(const __grid
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = first_row + 8 * i + (e & 1);
-            if (r < a.rows && j0 + g8 + 8 * (e >> 1) < cur.keys) to[(size_t)8 * (e >> 1) * a.group + r] = s[i][e];
+            if (r < a.rows && j0 + g8 + 8 * (e >> 1) < cur.keys) to[8 * (e >> 1) * a.group + r] = s[i][e];
           }
       }
       // references
@@ -378,95 +370,50 @@ __global__ void __launch_bounds__(32 + 128 * WR * NG, 1) attend_mma(const __grid
       if (lane == 0) mbar_arrive(empty(st));
     }
 
-    const bool item_ends = cur.t + 1 == cur.tiles;
-    if (item_ends || n + 1 == run) {
-      // the warps that shared the keys: common reference, then their outputs, halving
-      const int sets = min(S::kSets, (n + 1 - seg) * 4);        // (groups without a tile have nothing)
-      const int used = sets > 8 ? 16 : sets > 4 ? 8 : 4, my = ((grp + NG - seg % NG) % NG) * 4 + kw;
-#pragma unroll
-      for (int i = 0; i < NR; ++i)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-#pragma unroll
-          for (int d = 4; d < 32; d *= 2) l[i][x] += __shfl_xor_sync(0xffffffffu, l[i][x], d);
-          if (g8 == 0) {
-            const int row = wr * 8 * NR + 8 * i + 2 * t4 + x;
-            stat[my * RB + row] = m[i][x];
-            stat[(S::kSets + my) * RB + row] = l[i][x];
-          }
-        }
-      sync();
-      float M[NR][2], L[NR][2];
-#pragma unroll
-      for (int i = 0; i < NR; ++i)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float* const sp = stat + wr * 8 * NR + 8 * i + 2 * t4 + x;
-          float top = -INFINITY, sum = 0.f;
-          for (int w = 0; w < used; ++w) top = fmaxf(top, sp[w * RB]);
-          if (top != -INFINITY)
-            for (int w = 0; w < used; ++w) sum += sp[(S::kSets + w) * RB] * fast_exp2(sp[w * RB] - top);
-          const float f = m[i][x] == -INFINITY ? 0.f : fast_exp2(m[i][x] - top);
-#pragma unroll
-          for (int k = 0; k < KK; ++k) { o[i][k][x] *= f; o[i][k][2 + x] *= f; }
-          M[i][x] = top;
-          L[i][x] = sum;
-        }
-#pragma unroll 1
-      for (int half = used / 2; half >= 1; half /= 2) {
-        float* const buf = merge + ((size_t)((my % half) * WR + wr) * S::kRegs) * 32 + lane;
-        if (my >= half && my < 2 * half)
-#pragma unroll
-          for (int i = 0; i < NR; ++i)
-#pragma unroll
-            for (int k = 0; k < KK; ++k)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) buf[((i * KK + k) * 4 + e) * 32] = o[i][k][e];
-        sync();
-        if (my < half)
-#pragma unroll
-          for (int i = 0; i < NR; ++i)
-#pragma unroll
-            for (int k = 0; k < KK; ++k)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[i][k][e] += buf[((i * KK + k) * 4 + e) * 32];
-        sync();
-      }
-      if (my == 0) {
-        const bool whole = seg_first && item_ends;
-        const int slot = 2 * cta + seg_first, b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv;
+    if (cur.t + 1 == cur.tiles || n + 1 == run) {
+      // the segment ends: its warps' outputs, each against its own reference, then their sum against a common one.  Sets (a group's
+      // quarter of the keys) are counted from the group that took the segment's first tile.
+      const int sets = min(S::kSets, (n + 1 - seg) * 4), my = ((grp + NG - seg % NG) % NG) * 4 + kw;
+      if (my < sets) {
 #pragma unroll
         for (int i = 0; i < NR; ++i)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const int row = wr * 8 * NR + 8 * i + 2 * t4 + x, r = cur.rb * RB + row;
-            if (r >= a.rows) continue;
-            if (!whole) {
-              float* const to = a.part_out + ((size_t)slot * RB + row) * D + g8;
 #pragma unroll
-              for (int k = 0; k < KK; ++k) { to[k * 16] = o[i][k][x]; to[k * 16 + 8] = o[i][k][2 + x]; }
-              if (g8 == 0) a.part_stat[(size_t)slot * RB + row] = make_float2(M[i][x], L[i][x]);
-              continue;
-            }
-            const int tok = r / a.group, h = r - tok * a.group;
-            const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
-            const float inv = M[i][x] == -INFINITY ? 0.f : 1.f / L[i][x];      // (a NaN row stays one)
-            __nv_bfloat16* const to = (__nv_bfloat16*)a.out + q * D + g8;
-#pragma unroll
-            for (int k = 0; k < KK; ++k) {
-              to[k * 16] = __float2bfloat16(o[i][k][x] * inv);
-              to[k * 16 + 8] = __float2bfloat16(o[i][k][2 + x] * inv);
-            }
+            for (int d = 4; d < 32; d *= 2) l[i][x] += __shfl_xor_sync(0xffffffffu, l[i][x], d);
+            const int row = 8 * i + 2 * t4 + x;
             if (g8 == 0) {
-              const float bits = M[i][x] == -INFINITY ? M[i][x] : M[i][x] + log2f(L[i][x]);
-              if (a.lse) a.lse[q] = bits * kLn2;
-              if (a.accumulate) a.row_lse[(size_t)cur.u * a.rows + r] = bits;
+              stat[my * RB + row] = m[i][x];
+              stat[(S::kSets + my) * RB + row] = l[i][x];
             }
+            float* const to = outs + (my * RB + row) * S::kRow + g8;
+#pragma unroll
+            for (int k = 0; k < KK; ++k) { to[k * 16] = o[i][k][x]; to[k * 16 + 8] = o[i][k][2 + x]; }
           }
       }
-      clear();
+      sync();
+      const int slot = cur.u * blocks + cur.rb + blockIdx.x, rows = min(RB, a.rows - cur.rb * RB);
+#pragma unroll 1
+      for (int i = tid - 32; i < rows * (D / 4); i += S::kWarps * 32) {
+        const int row = i / (D / 4), c4 = i % (D / 4);
+        float top = -INFINITY, sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int w = 0; w < sets; ++w) top = fmaxf(top, stat[w * RB + row]);
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+        for (int w = 0; w < sets; ++w) {
+          const float f = fast_exp2(stat[w * RB + row] - ref);
+          const float4 x = *(const float4*)(outs + (w * RB + row) * S::kRow + c4 * 4);
+          sum = fmaf(f, stat[(S::kSets + w) * RB + row], sum);
+          v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+        }
+        *(float4*)(a.part_out + ((size_t)slot * RB + row) * D + c4 * 4) = v;
+        if (c4 == 0) a.part_stat[(size_t)slot * RB + row] = make_float2(top, sum);
+      }
+      if (n + 1 < run) sync();
+      fresh = true;
       seg = n + 1;
-      seg_first = 1;
     }
     if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
   }
@@ -496,7 +443,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
   volatile int* const abort_flag = (volatile int*)(lse + kWeighRows) + 4 * ST;
   auto full = [&](int st) { return bars + 8 * st; };
   auto empty = [&](int st) { return bars + 8 * (ST + st); };
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < ST; ++i) {
@@ -507,18 +454,12 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   pdl_wait();
-  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, 1, [&](long long W) { return cut(cta, W, sharers(W, gridDim.x)); }, nullptr);
-  const int C = sharers(ws.total, gridDim.x);
-  const long long lo = cut(cta, ws.total, C), hi = cut(cta + 1, ws.total, C);
-  if (lo >= hi) return;
-  const int run = (int)(hi - lo);
-  Cursor cur;
-  cur.u = ws.unit;
-  enter(cur, a.c, a.n_new, kTileKeys);
-  cur.rb = 0;
-  cur.t = (int)(lo - ws.before);
+  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, 1, gridDim.x, nullptr);
+  if (ws.lo >= ws.hi) return;
+  const int run = ws.hi - ws.lo;
+  Cursor cur{ws.unit, 0, ws.lo - ws.before, (ws.keys + kTileKeys - 1) / kTileKeys, ws.keys};
   // rows of the accepted tokens of a unit, and how often its tiles are gone through
-  auto taken_of = [&](int u) { return accepted[u / a.c.n_kv] & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1); };
+  auto taken_of = [&](int u) { return accepted[quotient(u, a.by_kv)] & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1); };
   auto rounds_of = [&](int rows) { return rows <= kWeighRows ? 1 : (rows + kWeighRows - 1) / kWeighRows; };
 
   if (warp == 0) {
@@ -527,7 +468,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
     bool ok = true;
 #pragma unroll 1
     for (int left = run; left > 0 && ok;) {
-      const int t0 = cur.t, t1 = min(cur.tiles, t0 + left), b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv;
+      const int t0 = cur.t, t1 = min(cur.tiles, t0 + left), b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv;
       const int rounds = rounds_of(__popcll(taken_of(cur.u)) * a.group);
       for (int i = 0; i < rounds * (t1 - t0); ++i, ++n) {
         const int st = n % ST, t = t0 + i % (t1 - t0);
@@ -566,7 +507,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
 #pragma unroll 1
   for (int left = run; left > 0;) {                               // a unit's tiles of this CTA
     const int t0 = cur.t, t1 = min(cur.tiles, t0 + left);
-    const int b = cur.u / a.c.n_kv, g = cur.u % a.c.n_kv, n_old = cur.keys - a.n_new;
+    const int b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv, n_old = cur.keys - a.n_new;
     const unsigned long long taken = taken_of(cur.u);
     const int rows = __popcll(taken) * a.group, rounds = rounds_of(rows);
     float* const w = a.c.weights + (size_t)cur.u * a.c.capacity;
@@ -581,8 +522,9 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
         RowOptions ro{0, 0.f, 0};
         if (row < n_rows) {
           unsigned long long rest = taken;                        // token of row r0 + row: the bit of that rank
-          for (int skip = (r0 + row) / a.group; skip > 0; --skip) rest &= rest - 1;
-          const int tok = __ffsll((long long)rest) - 1, h = (r0 + row) % a.group;
+          const int rank = quotient(r0 + row, a.by_group), h = r0 + row - rank * a.group;
+          for (int skip = rank; skip > 0; --skip) rest &= rest - 1;
+          const int tok = __ffsll((long long)rest) - 1;
           x = *(const uint4*)(a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head + ch * 16);
           if (ch == 0) {
             ref = a.lse[((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h] * kLog2e;
@@ -663,20 +605,15 @@ bool encode(const Ctx& ctx, const AttendArgs& a, CacheMaps* m) {
          tc_encode_cache(ctx, &m->v, c.v, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTileKeys);
 }
 
-template <int D, int NR, int WR, int NG, bool OPT>
+template <int D, int NR, int NG, bool OPT>
 cudaError_t launch_one(const AttendArgs& a, const CacheMaps& m, cudaStream_t st) {
-  using S = AttendShape<D, NR, WR, NG>;
-  const cudaError_t e = allow_smem<attend_mma<D, NR, WR, NG, OPT>>(S::kSmem);
-  return e != cudaSuccess ? e : launch_pdl(attend_mma<D, NR, WR, NG, OPT>, dim3(a.ctas), dim3(S::THREADS), S::kSmem, st, a, m);
+  using S = AttendShape<D, NR, NG>;
+  const cudaError_t e = allow_smem<attend_mma<D, NR, NG, OPT>>(S::kSmem);
+  return e != cudaSuccess ? e : launch_pdl(attend_mma<D, NR, NG, OPT>, dim3(a.ctas), dim3(S::THREADS), S::kSmem, st, a, m);
 }
 template <int D, bool OPT>
 cudaError_t launch_rows(const AttendArgs& a, const AttendPlan& p, const CacheMaps& m, cudaStream_t st) {
-  switch (p.rb) {
-    case 8: return launch_one<D, 1, 1, 4, OPT>(a, m, st);
-    case 16: return launch_one<D, 2, 1, 2, OPT>(a, m, st);
-    case 32: return launch_one<D, 2, 2, 1, OPT>(a, m, st);
-    default: return launch_one<D, 4, 2, 1, OPT>(a, m, st);
-  }
+  return p.rb == 8 ? launch_one<D, 1, 4, OPT>(a, m, st) : launch_one<D, 2, 2, OPT>(a, m, st);
 }
 template <int D, bool OPT>
 cudaError_t launch_weigh(const AttendArgs& a, const CacheMaps& m, const unsigned long long* accepted, int ctas, cudaStream_t st) {

@@ -68,22 +68,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
   float* const qs = sm + S::kStages * S::kStage;
   float* const part = qs + R * D;                                     // [warp][R][D], then [warp][R] maxima and sums
   float* const stat = part + kWarps * R * D;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, blocks = (a.rows + R - 1) / R;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, blocks = (a.rows + R - 1) / R;
   pdl_trigger();
   pdl_wait();
-  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, blocks, [&](long long W) { return cut(cta, W, sharers(W, gridDim.x)); },
-                                           cta == 0 ? a.unit_start : nullptr);
-  const int C = sharers(ws.total, gridDim.x);
-  const long long lo = cut(cta, ws.total, C), hi = cut(cta + 1, ws.total, C);
-  int u = ws.unit;
-  long long at = lo, unit_at = ws.before;
+  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, blocks, a.ctas, blockIdx.x == 0 ? a.unit_start : nullptr);
+  const int hi = ws.hi;
+  int u = ws.unit, at = ws.lo, unit_at = ws.before * blocks;
 #pragma unroll 1
   while (at < hi) {                                                   // the tiles of an item in this CTA
     int keys = unit_keys(a.c, u, a.n_new);
     while (keys == 0 && u < a.c.units - 1) keys = unit_keys(a.c, ++u, a.n_new);
-    const int tiles = (keys + kTileKeys - 1) / kTileKeys, rb = (int)((at - unit_at) / tiles);
-    const int t0 = (int)((at - unit_at) % tiles), t1 = (int)min((long long)tiles, t0 + (hi - at));
-    const int b = u / a.c.n_kv, g = u % a.c.n_kv, n_old = keys - a.n_new;
+    const int tiles = (keys + kTileKeys - 1) / kTileKeys, rb = blocks > 1 ? (at - unit_at) / tiles : 0;
+    const int t0 = at - unit_at - rb * tiles, t1 = min(tiles, t0 + (hi - at));
+    const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, n_old = keys - a.n_new;
     const char *const k = a.c.k + unit_offset(a.c, u), *const v = a.c.v + unit_offset(a.c, u);
     __syncthreads();
 #pragma unroll 1
@@ -163,37 +160,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
       for (int c = 0; c < DL; ++c) part[(warp * R + r) * D + c * 32 + lane] = o[r][c];
     }
     __syncthreads();
-    const bool first = t0 == 0, whole = first && t1 == tiles;
-    const int slot = 2 * cta + first;
+    const int slot = u * blocks + rb + blockIdx.x;
     for (int i = tid; i < R * D; i += kThreads) {
-      const int row = i / D, col = i % D, r = rb * R + row;
-      if (r >= a.rows) break;
+      const int row = i / D, col = i % D;
+      if (rb * R + row >= a.rows) break;
       float M = -INFINITY, L = 0.f, acc = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) M = fmaxf(M, stat[w * R + row]);
-      if (M != -INFINITY)
+      const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float f = fast_exp2(stat[w * R + row] - M);
-          L += stat[(kWarps + w) * R + row] * f;
-          acc += part[(w * R + row) * D + col] * f;
-        }
-      if (!whole) {
-        a.part_out[((size_t)slot * R + row) * D + col] = acc;
-        if (col == 0) a.part_stat[(size_t)slot * R + row] = make_float2(M, L);
-        continue;
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = fast_exp2(stat[w * R + row] - ref);
+        L = fmaf(stat[(kWarps + w) * R + row], f, L);
+        acc = fmaf(part[(w * R + row) * D + col], f, acc);
       }
-      const size_t q = ((size_t)b * a.n_new + r / a.group) * (a.group * a.c.n_kv) + g * a.group + r % a.group;
-      ((float*)a.out)[q * D + col] = M == -INFINITY ? 0.f : acc / L;
-      if (col == 0) {
-        const float bits = M == -INFINITY ? M : M + log2f(L);
-        if (a.lse) a.lse[q] = bits * kLn2;
-        if (a.accumulate) a.row_lse[(size_t)u * a.rows + r] = bits;
-      }
+      a.part_out[((size_t)slot * R + row) * D + col] = acc;
+      if (col == 0) a.part_stat[(size_t)slot * R + row] = make_float2(M, L);
     }
     at += t1 - t0;
     if (t1 == tiles && rb + 1 == blocks) {
-      unit_at += (long long)tiles * blocks;
+      unit_at += tiles * blocks;
       ++u;
     }
   }
@@ -208,20 +194,18 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant_
   float* const qs = sm + kTileKeys * S::kRow;
   __shared__ float lse[R];
   __shared__ int row_of[R];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_trigger();
   pdl_wait();
-  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, 1, [&](long long W) { return cut(cta, W, sharers(W, gridDim.x)); }, nullptr);
-  const int C = sharers(ws.total, gridDim.x);
-  const long long lo = cut(cta, ws.total, C), hi = cut(cta + 1, ws.total, C);
-  int u = ws.unit;
-  long long at = lo, unit_at = ws.before;
+  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, 1, gridDim.x, nullptr);
+  const int hi = ws.hi;
+  int u = ws.unit, at = ws.lo, unit_at = ws.before;
 #pragma unroll 1
   while (at < hi) {
     int keys = unit_keys(a.c, u, a.n_new);
     while (keys == 0 && u < a.c.units - 1) keys = unit_keys(a.c, ++u, a.n_new);
-    const int tiles = (keys + kTileKeys - 1) / kTileKeys, t0 = (int)(at - unit_at), t1 = (int)min((long long)tiles, t0 + (hi - at));
-    const int b = u / a.c.n_kv, g = u % a.c.n_kv, n_old = keys - a.n_new;
+    const int tiles = (keys + kTileKeys - 1) / kTileKeys, t0 = at - unit_at, t1 = min(tiles, t0 + (hi - at));
+    const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, n_old = keys - a.n_new;
     const unsigned long long taken = accepted[b] & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1);
     const int rows = __popcll(taken) * a.group;
     float* const w = a.c.weights + (size_t)u * a.c.capacity;
@@ -233,8 +217,9 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant_
         float x = INFINITY;                                           // no row
         if (r0 + tid < rows) {
           unsigned long long rest = taken;
-          for (int skip = (r0 + tid) / a.group; skip > 0; --skip) rest &= rest - 1;
-          const int tok = __ffsll((long long)rest) - 1, h = (r0 + tid) % a.group;
+          const int rank = quotient(r0 + tid, a.by_group), h = r0 + tid - rank * a.group;
+          for (int skip = rank; skip > 0; --skip) rest &= rest - 1;
+          const int tok = __ffsll((long long)rest) - 1;
           r = tok * a.group + h;
           x = a.lse[((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h] * kLog2e;
           if (x == -INFINITY) x = INFINITY;                           // a row that saw nothing gave nothing

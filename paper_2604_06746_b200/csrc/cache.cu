@@ -5,27 +5,23 @@
 namespace skv {
 namespace {
 
-__device__ __forceinline__ const char* new_row(const char* base, const NewRows& r, int u, int n_kv, int i) {
-  return base + (size_t)(u / n_kv) * r.s_batch + (size_t)i * r.s_token + (size_t)(u % n_kv) * r.s_head;
-}
-
 // A block per unit: rows of the new tokens to slots lengths[u] and up, with their positions and weight 0.
 __global__ void __launch_bounds__(256) append(const __grid_constant__ CacheView c, const __grid_constant__ NewRows r, int n_new) {
   pdl_trigger();
   pdl_wait();
-  const int u = blockIdx.x, n = unit_keys(c, u, n_new) - n_new;
+  const int u = blockIdx.x, n = unit_keys(c, u, n_new) - n_new, b = u / c.n_kv, g = u - b * c.n_kv;
   if (n < 0) return;
-  const size_t off = unit_offset(c, u);
-  const int per_row = c.row_bytes / 16, total = n_new * per_row;
-  for (int i = threadIdx.x; i < 2 * total; i += blockDim.x) {
-    const bool is_v = i >= total;
-    const int e = is_v ? i - total : i, tok = e / per_row, ch = e % per_row;
-    const uint4 x = *(const uint4*)(new_row(is_v ? r.v : r.k, r, u, c.n_kv, tok) + ch * 16);
-    *(uint4*)((is_v ? c.v : c.k) + off + (size_t)(n + tok) * c.s_token + ch * 16) = x;
+  const int per_row = c.row_bytes / 16, shift = per_row == 8 ? 3 : per_row == 16 ? 4 : 5;      // (64 or 128 elements of 2 or 4 bytes)
+  const size_t off = unit_offset(c, u) + (size_t)n * c.s_token, from = (size_t)b * r.s_batch + (size_t)g * r.s_head;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n_new << (shift + 1); i += blockDim.x) {
+    const int tok = i >> (shift + 1), ch = i & (per_row - 1);
+    const bool is_v = i >> shift & 1;
+    *(uint4*)((is_v ? c.v : c.k) + off + (size_t)tok * c.s_token + ch * 16) = *(const uint4*)((is_v ? r.v : r.k) + from + (size_t)tok * r.s_token + ch * 16);
   }
   const size_t w = (size_t)u * c.capacity + n;
   for (int i = threadIdx.x; i < n_new; i += blockDim.x) {
-    c.positions[w + i] = r.positions[(size_t)(u / c.n_kv) * n_new + i];
+    c.positions[w + i] = r.positions[(size_t)b * n_new + i];
     if (c.weights) c.weights[w + i] = 0.f;
   }
 }
@@ -129,9 +125,9 @@ __global__ void __launch_bounds__(kRxThreads, 2) evict(const __grid_constant__ C
   unsigned key[kItems];
   int mine = 0;
   // a warp's tokens are consecutive; item e of this thread: first + 32 e
-  auto first_of = [&](int ch) { return ch * kChunk + warp * (32 * kItems) + lane; };
+  auto token_of = [&](int ch) { return ch * kChunk + warp * (32 * kItems) + lane; };
   auto load = [&](int ch) {
-    const int first = first_of(ch);
+    const int first = token_of(ch);
     mine = min(kItems, (n - first + 31) >> 5);
     float v[kItems];
     int p[kItems];
@@ -187,7 +183,7 @@ __global__ void __launch_bounds__(kRxThreads, 2) evict(const __grid_constant__ C
         eq = run_eq + __shfl_sync(0xffffffffu, incl - s.counts[0][lane], warp);
         run_eq += __shfl_sync(0xffffffffu, incl, 31);
       }
-      const int first = first_of(ch);
+      const int first = token_of(ch);
       unsigned is_free = 0, is_move = 0, n_free = 0, n_move = 0;      // bits: item e
 #pragma unroll
       for (int e = 0; e < kItems; ++e) {
