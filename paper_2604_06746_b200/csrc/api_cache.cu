@@ -9,10 +9,16 @@ using namespace skv;
 namespace skv {
 namespace {
 
+// A tile of the tensor cores has 128 rows: from 17 on they take them (single tokens of 17 heads and more stay, 16 at a time, with
+// the kernel that leaves the logits).
+bool by_tensor_cores(const structkv_config& cfg, int n_new) {
+  return cfg.dtype == STRUCTKV_BF16 && n_new > 1 && cfg.n_q_heads / cfg.n_kv_heads * n_new > 16;
+}
 AttendPlan attend_plan(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms};
-  return {rows <= 8 ? 8 : 16, 64, sms};
+  if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms, 1};
+  if (by_tensor_cores(cfg, n_new)) return rows <= 128 ? AttendPlan{128, 128, sms, 2} : AttendPlan{256, 128, sms, 1};
+  return {rows <= 8 ? 8 : 16, 64, sms, 1};
 }
 
 struct AttendWs { int* unit_start; float2* part_stat; float *part_out, *logits; size_t bytes; };
@@ -27,7 +33,7 @@ AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch
   };
   const size_t units = (size_t)batch * cfg.n_kv_heads, group = cfg.n_q_heads / cfg.n_kv_heads;
   w.unit_start = (int*)take((units + 1) * sizeof(int));
-  const size_t slots = units * ((group * n_new + p.rb - 1) / p.rb) + p.ctas;
+  const size_t slots = (units * ((group * n_new + p.rb - 1) / p.rb) + p.ctas) * p.parts;
   w.part_stat = (float2*)take(slots * p.rb * sizeof(float2));
   w.part_out = (float*)take(slots * p.rb * cfg.head_dim * sizeof(float));
   if (n_new == 1) w.logits = (float*)take(units * group * capacity * sizeof(float));
@@ -138,9 +144,11 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
   cudaStream_t st = (cudaStream_t)stream;
   // A few rows are appended by the kernel itself; a warp that copies more of them holds its tiles up.
   cudaError_t e = cudaSuccess;
-  if (args->rows && c.cfg.dtype == STRUCTKV_BF16 && args->n_new <= 8) a.fresh = r;
+  const bool tc = by_tensor_cores(c.cfg, args->n_new);
+  if (args->rows && c.cfg.dtype == STRUCTKV_BF16 && !tc && args->n_new <= 8) a.fresh = r;
   else if (args->rows) e = launch_append(a.c, r, args->n_new, st);
-  if (e == cudaSuccess) e = c.cfg.dtype == STRUCTKV_BF16 ? launch_attend_mma(c, a, plan, st) : launch_attend_simt(c, a, plan, st);
+  if (e == cudaSuccess)
+    e = (c.cfg.dtype != STRUCTKV_BF16 ? launch_attend_simt : tc ? launch_attend_tc : launch_attend_mma)(c, a, plan, st);
   if (e == cudaSuccess) e = launch_attend_finish(c, a, plan, st);
   return told(e);
 }

@@ -63,8 +63,8 @@ struct AttendArgs {
   int ctas;
 };
 
-// Rows of a block, keys of a tile, CTAs that run at once.
-struct AttendPlan { int rb, tile, ctas; };
+// Rows of a block, keys of a tile, CTAs that run at once, partials a CTA leaves of an item.
+struct AttendPlan { int rb, tile, ctas, parts; };
 
 cudaError_t launch_append(const CacheView& c, const NewRows& r, int n_new, cudaStream_t st);
 cudaError_t launch_commit(const CacheView& c, int n_new, const int* counts, const int* path, cudaStream_t st);
@@ -72,6 +72,7 @@ cudaError_t launch_evict(const CacheView& c, int budget, int recent, cudaStream_
 // The kernels: fp32 storage on the CUDA cores; bf16 storage.
 cudaError_t launch_attend_simt(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st);
 cudaError_t launch_attend_mma(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st);
+cudaError_t launch_attend_tc(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st);
 cudaError_t launch_attend_finish(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st);
 // weights[j] = decay weights[j] + the sum of exp(x - lse) over the rows of the accepted new tokens.
 cudaError_t launch_weigh_fp32(const Ctx& ctx, const AttendArgs& a, const unsigned long long* accepted, cudaStream_t st);

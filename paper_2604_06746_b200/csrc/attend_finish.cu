@@ -15,9 +15,9 @@ constexpr int kThreads = 256;
 
 // First partial of an item and how many it has.
 struct Parts { int first, count; };
-__device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, int tiles) {
+__device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, int tiles, int each) {
   const int c0 = cta_of(s, start), c1 = tiles == 1 ? c0 : cta_of(s, start + tiles - 1);
-  return {item + c0, c1 - c0 + 1};
+  return {(item + c0) * each, (c1 - c0 + 1) * each};
 }
 // Reference and sum of a row over its partials, by a warp (the same in every lane).
 __device__ __forceinline__ float2 merged(const float2* __restrict__ stat, Parts p, int rb_rows, int row, int lane) {
@@ -44,7 +44,7 @@ template <int DL>
 struct Cols { float v[DL]; };
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant__ AttendArgs a, int rb_shift, int tile_shift) {
+__global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant__ AttendArgs a, int rb_shift, int tile_shift, int each) {
   constexpr int DL = D / 32;
   __shared__ int hit;
   __shared__ float lse[kThreads];
@@ -61,14 +61,16 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
     const int u = quotient(i, a.by_rows), r = i - u * a.rows, rb = r >> rb_shift, row = r & (rb_rows - 1);
     const int start = a.unit_start[u], tiles = a.unit_start[u + 1] - start;
     if (tiles == 0) continue;
-    const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles);
+    const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles, each);
     const float2 st = merged(a.part_stat, p, rb_rows, row, lane);
     const float ref = st.x == -INFINITY ? 0.f : st.x;
     Cols<DL> acc{};
 #pragma unroll 4
     for (int c = 0; c < p.count; ++c) {
       const size_t at = (size_t)(p.first + c) * rb_rows + row;
-      const float f = fast_exp2(a.part_stat[at].x - ref);
+      const float2 ps = a.part_stat[at];
+      if (ps.x == -INFINITY && ps.y == 0.f) continue;             // nothing there
+      const float f = fast_exp2(ps.x - ref);
       const Cols<DL> x = *(const Cols<DL>*)(a.part_out + at * D + lane * DL);
 #pragma unroll
       for (int e = 0; e < DL; ++e) acc.v[e] = fmaf(f, x.v[e], acc.v[e]);
@@ -107,7 +109,7 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
 #pragma unroll 1
       for (int h = warp; h < heads; h += kThreads / 32) {
         const int r = h0 + h, rb = r >> rb_shift;
-        const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles);
+        const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles, each);
         const float x = bits_of(merged(a.part_stat, p, rb_rows, r & (rb_rows - 1), lane));
         if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
       }
@@ -141,7 +143,7 @@ int log2_of(int x) {
 }
 template <int D, bool BF16>
 cudaError_t launch(const AttendArgs& a, const AttendPlan& p, int ctas, cudaStream_t st) {
-  return launch_pdl(attend_finish<D, BF16>, dim3(ctas), dim3(kThreads), 0, st, a, log2_of(p.rb), log2_of(p.tile));
+  return launch_pdl(attend_finish<D, BF16>, dim3(ctas), dim3(kThreads), 0, st, a, log2_of(p.rb), log2_of(p.tile), p.parts);
 }
 
 }  // namespace

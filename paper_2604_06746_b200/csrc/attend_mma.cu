@@ -88,9 +88,10 @@ struct AttendShape {
   static constexpr int kPosOff = 2 * kTileBytes, kQOff = kPosOff + 1024, kStage = kQOff + RB * D * 2;
   static constexpr int kRow = D + 4;                             // of a set's output: rows two apart are eight banks apart
   static constexpr int kFixed = kSets * RB * (kRow + 2) * 4 + 256 + 1024;
-  static constexpr int kStages = std::min(8, (226 * 1024 - kFixed) / kStage);
+  // (a place of the ring always serves the same group: a wait by parity holds only for who follows a barrier from phase to phase)
+  static constexpr int kStages = std::min(8, (226 * 1024 - kFixed) / kStage) / NG * NG;
   static constexpr int kSmem = kStages * kStage + kFixed;
-  static_assert(kStages >= 3 && kStage % 1024 == 0, "a ring");
+  static_assert(kStages >= 4 && kStage % 1024 == 0, "a ring");
 };
 
 template <int D, int NR, int NG, bool OPT>
@@ -423,6 +424,7 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
 // weights[j] = decay weights[j] + sum over accepted rows of 2^(x - lse): K tiles stream past the accepted tokens' rows
 // (kWeighRows at a time in shared memory); a warp has 16 keys of a tile in registers and adds up their rows.
 constexpr int kWeighRows = 64, kWeighStages = 8, kWeighGroups = 2, kWeighWarps = 4 * kWeighGroups;
+static_assert(kWeighStages % kWeighGroups == 0, "a place of the ring serves one group");
 
 template <int D>
 constexpr int weigh_smem() {

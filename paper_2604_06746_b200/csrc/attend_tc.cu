@@ -1,0 +1,483 @@
+// Attention of new tokens over a bf16 cache where a KV head has more than 16 rows: drafted trees, pieces of a prompt.
+//
+// S = Q K^T and O += P V on the tensor cores (tcgen05): a tile of 128 rows x 128 keys, lane = row, so that a row's maximum and sum
+// stay inside one thread; P goes back to tensor memory, over S, as the A operand of the second product; V, whose rows are
+// keys, is its B operand as it lies (N-major).  Two streams of such tiles alternate, so that one's products run beside the other's
+// exponentials: the two halves of up to 256 rows over the same keys, or, with up to 128 rows, the even and the odd key tiles (the
+// streams then leave a partial each).  Work is cut as everywhere (attend.cuh).
+//
+// Warps: 0 fills the ring of K and V tiles by TMA, 1 issues the products, 2 and 3 bring a segment's rows and look through V tiles that
+// hold new tokens (what is not finite there is taken out and added, at the end, to the rows that see it: 0 x infinity), 4-7 and
+// 8-11 are the streams' softmax.  The reference of a row follows its maximum only where that outgrows it by 2^kSlack.
+// Bound by reading K and V up to about 128 rows, beyond by products and exponentials together.
+#include <algorithm>
+
+#include "attend.cuh"
+#include "score_tc.cuh"
+
+namespace skv {
+namespace {
+
+constexpr int kTile = 128, kThreads = 384;
+constexpr float kSlack = 8.f;
+
+struct CacheMaps { CUtensorMap k, v; };
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%3, %4, %5, %6}], [%2], %7;"
+      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "l"(policy) : "memory");
+}
+// An N-major operand of 64-element blocks of 128-byte rows (128-byte swizzle): blocks kTile rows apart, 8-row groups 1024 bytes.
+__device__ __forceinline__ uint64_t smem_desc_n(uint32_t addr) {
+  return smem_desc(addr) & ~(0x3fffull << 16) | (uint64_t)((kTile * 128) >> 4) << 16;
+}
+constexpr uint32_t kTransposeB = 1u << 16;
+// d += a b with a in tensor memory.
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+                 "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&f)[32]) {
+  uint32_t lo[16], hi[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) { lo[i] = __float_as_uint(f[i]); hi[i] = __float_as_uint(f[16 + i]); }
+  tmem_st16(taddr, lo);
+  tmem_st16(taddr + 16, hi);
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+// 16-byte chunk of a row in a tile of 128-byte rows, 64 columns after 64 columns, 128-byte swizzle.
+__device__ __forceinline__ uint32_t tile_at(int row, int chunk) { return (chunk >> 3) * (kTile * 128) + row * 128 + (((chunk ^ row) & 7) << 4); }
+
+// A CTA's run, item by item: segments [t0, t1) of an item's tiles.
+struct Segments {
+  int u, rb, t0, t1, keys, tiles, left;
+};
+__device__ __forceinline__ Segments first_segment(const WorkStart& ws, int blocks) {
+  Segments s;
+  s.u = ws.unit;
+  s.keys = ws.keys;
+  s.tiles = (ws.keys + kTile - 1) / kTile;
+  s.t0 = ws.lo - ws.before * blocks;
+  s.rb = blocks > 1 ? s.t0 / s.tiles : 0;
+  s.t0 -= s.rb * s.tiles;
+  s.left = ws.hi - ws.lo;
+  s.t1 = min(s.tiles, s.t0 + s.left);
+  return s;
+}
+__device__ __forceinline__ bool next_segment(Segments& s, const AttendArgs& a, int blocks) {
+  s.left -= s.t1 - s.t0;
+  if (s.left <= 0) return false;
+  if (++s.rb == blocks) {
+    s.rb = 0;
+    do ++s.u;
+    while ((s.keys = unit_keys(a.c, s.u, a.n_new)) == 0 && s.u < a.c.units - 1);
+    s.tiles = (s.keys + kTile - 1) / kTile;
+  }
+  s.t0 = 0;
+  s.t1 = min(s.tiles, s.left);
+  return true;
+}
+
+// MT: halves of 128 rows in a block.
+template <int D, int MT, bool OPT>
+struct TcAttend {
+  static constexpr int RB = 128 * MT, kUnit = kTile * D * 2, kQ = RB * D * 2, kPos = OPT ? kTile * 4 : 0;
+  static constexpr int kFixed = kQ + 1024 + 512;
+  static constexpr int kUnits = std::min(8, (227 * 1024 - 512 - kFixed) / (kUnit + kPos));   // (512: static shared memory)
+  static constexpr int kSmem = kUnits * (kUnit + kPos) + kFixed;
+  static_assert(kUnits >= 4, "a ring");
+};
+
+template <int D, int MT, bool OPT>
+__global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps) {
+  using S = TcAttend<D, MT, OPT>;
+  constexpr int RB = S::RB, NU = S::kUnits, CH = D / 8;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
+  constexpr uint32_t kRing = S::kQ, kPosAt = kRing + NU * S::kUnit, kBars = kPosAt + NU * S::kPos;
+  const uint32_t bars = base + kBars, more = bars + 16 * NU;
+  auto full = [&](int u) { return bars + 8 * u; };
+  auto empty = [&](int u) { return bars + 8 * (NU + u); };
+  const uint32_t q_full = more, q_empty = more + 8, v_look = more + 16, v_ready = more + 24;
+  auto s_full = [&](int s) { return more + 32 + 8 * s; };
+  auto p_ready = [&](int s) { return more + 48 + 8 * s; };
+  auto o_done = [&](int s) { return more + 64 + 8 * s; };
+  auto o_free = [&](int s) { return more + 80 + 8 * s; };
+  const uint32_t drained = more + 96;
+  volatile int* const words = (volatile int*)(sm + kBars + 16 * NU + 104);
+  volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v: some new token's V was not finite
+  volatile uint32_t* const tmem_at = (volatile uint32_t*)words + 1;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int blocks = (a.rows + RB - 1) / RB;
+  pdl_trigger();
+  if (tid == 0) {
+    for (int i = 0; i < NU; ++i) { mbar_init(full(i), S::kPos ? 33 : 1); mbar_init(empty(i), 1); }
+    mbar_init(q_full, 64);
+    mbar_init(q_empty, 1);
+    mbar_init(v_look, 1);
+    mbar_init(v_ready, 64);
+    mbar_init(drained, 1);
+    for (int s = 0; s < 2; ++s) { mbar_init(s_full(s), 1); mbar_init(p_ready(s), 4); mbar_init(o_done(s), 1); mbar_init(o_free(s), 4); }
+    *abort_flag = 0;
+    *odd_v = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.v) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_at)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    tc_fence_before();
+  }
+  pdl_wait();
+  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTile, blocks, a.ctas, blockIdx.x == 0 ? a.unit_start : nullptr);   // (barriers inside)
+  tc_fence_after();
+  const uint32_t tmem = *tmem_at;
+  const bool work = ws.lo < ws.hi;
+  // (one answer for the warp: what follows is for all of its lanes)
+  auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
+  bool clean = true;                                             // every MMA of this CTA has retired
+
+  if (work && warp == 0) {
+    const uint64_t hint = blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
+    Segments sg = first_segment(ws, blocks);
+    int n = 0;                                                   // units: K and V of a tile after one another
+    bool ok = true;
+    do {
+      const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv;
+#pragma unroll 1
+      for (int t = sg.t0; t < sg.t1 && ok; ++t)
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv, ++n) {
+          const int st = n % NU;
+          if (n >= NU && !(ok = mbar_wait_producer(empty(st), (n / NU - 1) & 1, abort_flag, kWaitCycles))) break;
+          if (lane == 0) {
+            mbar_expect_tx(full(st), S::kUnit);
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c)
+              tma_load_4d(base + kRing + st * S::kUnit + c * kTile * 128, kv ? &maps.v : &maps.k, full(st), c * 64, t * kTile, g, b, hint);
+          }
+          if (S::kPos) {
+            // positions go with V: its place is held until the softmax has read them
+            if (a.slopes && kv == 1)
+#pragma unroll
+              for (int i = lane; i < kTile; i += 32) {
+                const int j = t * kTile + i;
+                ((int*)(sm + kPosAt + st * S::kPos))[i] = j < sg.keys ? a.c.positions[(size_t)sg.u * a.c.capacity + j] : 0;
+              }
+            mbar_arrive(full(st));
+          }
+        }
+    } while (ok && next_segment(sg, a, blocks));
+    // copies in flight end before the block does
+    if (!ok)
+      for (int i = max(0, n - NU); i < n; ++i) mbar_drain(full(i % NU), (i / NU) & 1, abort_flag);
+  } else if (work && warp == 1) {
+    // Products, by one lane.  Job j of a segment: tile j / MT by stream j % 2; scores run two jobs ahead of outputs.
+    const uint32_t idesc_s = instr_desc(128, kTile) | (a.scale2 < 0.f || a.inv_cap < 0.f ? 1u << 13 : 0u);
+    constexpr uint32_t idesc_o = instr_desc(128, D) | kTransposeB;
+    const uint64_t q_desc = smem_desc(base), k_desc0 = smem_desc(base + kRing), v_desc0 = smem_desc_n(base + kRing);
+    Segments sg = first_segment(ws, blocks);
+    int n = 0, seg = 0, tails = 0;                               // tiles before the segment; segments; tiles that were looked through
+    int done[2] = {0, 0}, used[2] = {0, 0};                      // jobs of a stream so far; segments it had jobs in
+    bool ok = true;
+    do {
+      const int tiles = sg.t1 - sg.t0, jobs = tiles * MT, n_old = sg.keys - a.n_new;
+      ok = wait(q_full, seg & 1);
+      auto scores = [&](int j) {
+        const int s = j & 1, unit = 2 * (n + j / MT), st = unit % NU;
+        if (!ok || !(ok = wait(full(st), (unit / NU) & 1))) return;
+        tc_fence_after();
+        if (lane == 0) {
+          const uint64_t qd = q_desc + (uint64_t)(MT == 2 ? (s * 128 * 128) >> 4 : 0), kd = k_desc0 + (uint64_t)((st * S::kUnit) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            tc_mma_bf16(tmem + s * 128, qd + (uint64_t)(((kk / 4) * RB * 128 + (kk % 4) * 32) >> 4),
+                        kd + (uint64_t)(((kk / 4) * kTile * 128 + (kk % 4) * 32) >> 4), idesc_s, kk > 0);
+          tc_commit(s_full(s));
+          if (j % MT == MT - 1) tc_commit(empty(st));
+          if (j == jobs - 1) tc_commit(q_empty);
+        }
+        __syncwarp();
+      };
+      scores(0);
+      if (jobs > 1) scores(1);
+#pragma unroll 1
+      for (int j = 0; j < jobs && ok; ++j) {
+        const int s = j & 1, t = j / MT, unit = 2 * (n + t) + 1, st = unit % NU;
+        if (!(ok = wait(full(st), (unit / NU) & 1))) break;
+        // A tile with new tokens is handed to the warps that look through it, and taken back: by barriers of their own, as a wait
+        // by parity holds only for who follows a barrier from phase to phase.
+        const bool tail = (sg.t0 + t + 1) * kTile > n_old && j % MT == 0;
+        if (tail && lane == 0) mbar_arrive(v_look);
+        if (j < 2 && used[s] > 0 && !(ok = wait(o_free(s), (used[s] - 1) & 1))) break;
+        if (j < 2) ++used[s];
+        if (!(ok = wait(p_ready(s), done[s] & 1))) break;
+        if (tail && !(ok = wait(v_ready, tails++ & 1))) break;
+        tc_fence_after();
+        if (lane == 0) {
+          const uint64_t vd = v_desc0 + (uint64_t)((st * S::kUnit) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < kTile / 16; ++kk)
+            tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + kk * 8, vd + (uint64_t)((kk * 16 * 128) >> 4), idesc_o, j >= 2 || kk > 0);
+          tc_commit(o_done(s));
+          if (j % MT == MT - 1) tc_commit(empty(st));
+        }
+        __syncwarp();
+        ++done[s];
+        if (j + 2 < jobs) scores(j + 2);
+      }
+      n += tiles;
+      ++seg;
+    } while (ok && next_segment(sg, a, blocks));
+    if (lane == 0) tc_commit(drained);
+    __syncwarp();
+    clean = mbar_drain(drained, 0, abort_flag);
+  } else if (work && warp < 4) {
+    // rows of a segment, then V tiles with new tokens
+    const int hl = tid - 64;
+    Segments sg = first_segment(ws, blocks);
+    int n = 0, seg = 0, tails = 0;
+    bool ok = true;
+    do {
+      if (seg > 0 && !(ok = mbar_wait_producer(q_empty, (seg - 1) & 1, abort_flag, kWaitCycles))) break;
+      const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv, n_old = sg.keys - a.n_new;
+      const char* const q0 = a.q + (size_t)b * a.q_batch + (size_t)(g * a.group) * a.q_head;
+#pragma unroll 4
+      for (int i = hl; i < RB * CH; i += 64) {
+        const int row = i / CH, ch = i % CH, r = sg.rb * RB + row;
+        const bool is = r < a.rows;
+        const int tok = is ? quotient(r, a.by_group) : 0, h = is ? r - tok * a.group : 0;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                     ::"r"(base + (ch >> 3) * (RB * 128) + row * 128 + (((ch ^ row) & 7) << 4)),
+                       "l"(q0 + (size_t)tok * a.q_token + (size_t)h * a.q_head + ch * 16), "r"(is ? 16 : 0) : "memory");
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive(q_full);
+      for (int t = max(sg.t0, n_old / kTile); t < sg.t1 && ok; ++t) {
+        const int unit = 2 * (n + t - sg.t0) + 1, st = unit % NU;
+        if (!(ok = mbar_wait_producer(v_look, tails++ & 1, abort_flag, kWaitCycles))) break;
+        const int row0 = max(0, n_old - t * kTile);
+#pragma unroll 4
+        for (int i = row0 * CH + hl; i < kTile * CH; i += 64) {
+          uint4* const p = (uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH));
+          uint32_t w[4] = {p->x, p->y, p->z, p->w};
+          bool bad = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bad |= not_finite(w[e]);
+          if (bad) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
+              if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu;
+            }
+            *p = make_uint4(w[0], w[1], w[2], w[3]);
+            if (t * kTile + i / CH < sg.keys) *odd_v = 1;
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(v_ready);
+      }
+      n += sg.t1 - sg.t0;
+      ++seg;
+    } while (ok && next_segment(sg, a, blocks));
+  } else if (work) {
+    const int s = (warp - 4) / 4, quarter = warp % 4;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
+    const float scale2 = fabsf(a.scale2), inv_cap = fabsf(a.inv_cap);   // (a negative scale negates the product)
+    Segments sg = first_segment(ws, blocks);
+    int n = 0, done = 0;
+    bool ok = true;
+    do {
+      const int tiles = sg.t1 - sg.t0, jobs = MT == 2 ? tiles : (tiles + 1 - s) / 2, n_old = sg.keys - a.n_new;
+      const int row = (MT == 2 ? s * 128 : 0) + quarter * 32 + lane, r = sg.rb * RB + row;
+      const bool idle = r - lane >= a.rows;                      // no row of this warp: it only keeps step
+      const RowOptions ro = row_options(a, sg.u, min(r, a.rows - 1));
+      float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+      for (int k = 0; k < jobs; ++k, ++done) {
+        const int t = MT == 2 ? k : 2 * k + s, j0 = (sg.t0 + t) * kTile;
+        if (!(ok = wait(s_full(s), done & 1))) break;
+        const int* kp = nullptr;
+        if (OPT && a.slopes) {
+          // (these scores were made after the outputs of the tile before, so that the place's previous tile has come and gone)
+          const int unit = 2 * (n + t) + 1, st = unit % NU;
+          if (!(ok = wait(full(st), (unit / NU) & 1))) break;
+          kp = (const int*)(sm + kPosAt + st * S::kPos);
+        }
+        tc_fence_after();
+        if (!idle) {
+          const bool tail = j0 + kTile > n_old;
+          float top = -INFINITY, mul = scale2;
+          float v[32];
+          if (OPT || tail) {
+            // x in bits, back to its place
+            mul = 1.f;
+#pragma unroll 1
+            for (int c = 0; c < kTile; c += 32) {
+              tmem_ld(s_at + c, v);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                float x = v[e] * scale2;
+                if (OPT) {
+                  if (a.cap2 != 0.f) x = capped(v[e], a.cap2, inv_cap);
+                  if (a.slopes) x = fmaf(-ro.slope2, (float)(ro.position - kp[c + e]), x);
+                }
+                const int j = j0 + c + e;
+                if (tail && (j >= sg.keys || !sees(ro.seen, j, n_old))) x = -INFINITY;
+                v[e] = x;
+                top = fmaxf(top, x);
+              }
+              tmem_st32(s_at + c, v);
+            }
+            tmem_st_wait();
+          } else {
+#pragma unroll
+            for (int c = 0; c < kTile; c += 32) {
+              tmem_ld(s_at + c, v);
+              float t0 = fmaxf(v[0], v[1]), t1 = fmaxf(v[2], v[3]);
+#pragma unroll
+              for (int e = 4; e < 32; e += 4) {
+                t0 = fmaxf(t0, fmaxf(v[e], v[e + 1]));
+                t1 = fmaxf(t1, fmaxf(v[e + 2], v[e + 3]));
+              }
+              top = fmaxf(top, fmaxf(t0, t1));
+            }
+            top *= scale2;
+          }
+          const bool grown = top > m + kSlack;
+          if (__any_sync(0xffffffffu, grown)) {
+            const float to = grown ? top : m, f = m == -INFINITY ? 0.f : fast_exp2(m - to);
+            m = to;
+            l *= f;
+            if (k > 0) {
+              if (!(ok = wait(o_done(s), (done - 1) & 1))) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < D; c += 32) {
+                tmem_ld(o_at + c, v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] *= f;
+                tmem_st32(o_at + c, v);
+              }
+              tmem_st_wait();
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 1
+          for (int c = 0; c < kTile; c += 32) {
+            tmem_ld(s_at + c, v);
+            uint32_t p[16];
+            float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              const float p0 = fast_exp2(fmaf(v[e], mul, -ref)), p1 = fast_exp2(fmaf(v[e + 1], mul, -ref));
+              sum0 += p0;
+              sum1 += p1;
+              // p keeps 8 bits for the product, as V does; the sum l is of the unrounded values
+              p[e / 2] = bf16x2(p0, p1);
+            }
+            l += sum0 + sum1;
+            tmem_st16(s_at + c / 2, p);                          // (over columns that have been read)
+          }
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_ready(s));
+      }
+      if (!ok) break;
+      const int slot = sg.u * blocks + sg.rb + blockIdx.x;
+      const size_t at = MT == 2 ? (size_t)slot * RB + row : ((size_t)slot * 2 + s) * RB + row;
+      if (r < a.rows) a.part_stat[at] = make_float2(m, l);
+      if (jobs > 0) {
+        if (!(ok = wait(o_done(s), (done - 1) & 1))) break;
+        tc_fence_after();
+        if (!idle) {
+          const bool odd = *odd_v && sg.t1 * kTile > n_old && (MT == 2 || s == 0);
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            float v[32];
+            tmem_ld(o_at + c, v);
+            if (odd) {
+              // V of new tokens that is not finite was left out of the product: it makes what sees it so
+              unsigned long long rest = ro.seen & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1);
+#pragma unroll 1
+              for (; rest; rest &= rest - 1) {
+                const int i = __ffsll((long long)rest) - 1;
+                const uint32_t* const from = (const uint32_t*)(a.c.v + unit_offset(a.c, sg.u) + (size_t)(n_old + i) * a.c.s_token + c * 2);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const uint32_t w = from[e];
+                  if ((w & 0x7f80u) == 0x7f80u) v[2 * e] += __uint_as_float(w << 16);
+                  if ((w & 0x7f800000u) == 0x7f800000u) v[2 * e + 1] += __uint_as_float(w & 0xffff0000u);
+                }
+              }
+            }
+            if (r < a.rows) {
+              float4* const to = (float4*)(a.part_out + at * D + c);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) to[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(o_free(s));
+      }
+      n += tiles;
+    } while (next_segment(sg, a, blocks));
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    if (clean) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+  if (tid == 0 && *abort_flag) atomicCAS(a.c.status, 0, (int)STRUCTKV_ERR_TIMEOUT);
+}
+
+template <int D, int MT, bool OPT>
+cudaError_t launch_one(const AttendArgs& a, const CacheMaps& m, cudaStream_t st) {
+  using S = TcAttend<D, MT, OPT>;
+  const cudaError_t e = allow_smem<attend_tc<D, MT, OPT>>(S::kSmem);
+  return e != cudaSuccess ? e : launch_pdl(attend_tc<D, MT, OPT>, dim3(a.ctas), dim3(kThreads), S::kSmem, st, a, m);
+}
+template <int D>
+cudaError_t launch_d(const AttendArgs& a, const AttendPlan& p, const CacheMaps& m, cudaStream_t st) {
+  const bool opt = a.cap2 != 0.f || a.slopes;
+  if (p.rb == 256) return opt ? launch_one<D, 2, true>(a, m, st) : launch_one<D, 2, false>(a, m, st);
+  return opt ? launch_one<D, 1, true>(a, m, st) : launch_one<D, 1, false>(a, m, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tc(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st) {
+  const CacheView& c = a.c;
+  CacheMaps m;
+  const int batch = c.units / c.n_kv;
+  if (!tc_encode_cache(ctx, &m.k, c.k, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTile) ||
+      !tc_encode_cache(ctx, &m.v, c.v, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTile))
+    return cudaErrorInvalidValue;
+  return ctx.cfg.head_dim == 128 ? launch_d<128>(a, p, m, st) : launch_d<64>(a, p, m, st);
+}
+
+}  // namespace skv

@@ -32,6 +32,14 @@ CASES = [
     ("qwen", [17, 1], 64, F32, {}),
     ("llama", [900], 1, BF, dict(spread=12.0)),           # sharp rows: the running maximum grows late
     ("llama", [900], 17, BF, dict(spread=12.0, tree="random")),
+    # several tiles and several short KV heads to a CTA
+    ("qwen", [4096, 1001, 2500, 333, 4095, 64, 3777, 2049], 16, BF, dict(tree="random", softcap=30.0)),
+    ("llama", [5000, 30, 128, 4097, 127, 200, 1, 6000], 9, BF, dict(tree="random", distance=True)),
+    ("llama", [9000, 40, 70, 2000], 64, BF, dict(tree="random")),
+    ("small", [100, 20000, 64, 65] * 8, 40, BF, dict(tree="random", softcap=9.0, distance=True)),
+    ("single", [50] * 70 + [5000], 30, BF, dict(tree="empty rows")),
+    ("llama", [3000, 50, 64, 10] * 6, 1, BF, {}),
+    ("qwen", [20000, 9, 100], 2, BF, dict(tree="random")),
 ]
 
 
@@ -111,17 +119,19 @@ def test_accepted_tokens_weigh(cuda_device, shape, lengths, t, dtype, accepted, 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("value", [float("nan"), float("inf")])
-def test_a_draft_that_is_not_finite_reaches_only_those_that_see_it(cuda_device, dtype, value):
-    p = Problem(cuda_device, "llama", [70, 0, 640], 6, dtype, seed=3, tree="random")
-    for b in range(p.b):                                  # token 4 is nobody's ancestor
-        p.tree_words[b] = [m & ~(1 << 4) if i != 4 else m for i, m in enumerate(p.tree_words[b])]
+@pytest.mark.parametrize("t", [2, 6, 50])
+def test_a_draft_that_is_not_finite_reaches_only_those_that_see_it(cuda_device, dtype, value, t):
+    p = Problem(cuda_device, "llama", [70, 0, 640], t, dtype, seed=3, tree="random")
+    bad = min(4, t - 1)
+    for b in range(p.b):                                  # that token is nobody's ancestor
+        p.tree_words[b] = [m & ~(1 << bad) if i != bad else m for i, m in enumerate(p.tree_words[b])]
     p.dtree = torch.tensor([[signed(m) for m in row] for row in p.tree_words], dtype=torch.int64, device=cuda_device)
-    p.k_new[:, 4] = value
-    p.v_new[:, 4] = value
+    p.k_new[:, bad] = value
+    p.v_new[:, bad] = value
     p.dk_new, p.dv_new = p.k_new.to(cuda_device), p.v_new.to(cuda_device)
     run(p)
-    p.check_attention(rows=[0, 1, 2, 3, 5])
-    assert not torch.isfinite(p.out[:, 4].float()).all()
+    p.check_attention(rows=[i for i in range(t) if i != bad])
+    assert not torch.isfinite(p.out[:, bad].float()).any()
 
 
 def test_results_do_not_depend_on_the_run(cuda_device):
