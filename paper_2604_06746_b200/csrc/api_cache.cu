@@ -16,9 +16,9 @@ bool by_tensor_cores(const structkv_config& cfg, int n_new) {
 }
 AttendPlan attend_plan(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms, 1};
-  if (by_tensor_cores(cfg, n_new)) return rows <= 128 ? AttendPlan{128, 128, sms, 2} : AttendPlan{256, 128, sms, 1};
-  return {rows <= 8 ? 8 : 16, 64, sms, 1};
+  if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms, 1, 2};
+  if (by_tensor_cores(cfg, n_new)) return rows <= 128 ? AttendPlan{128, 128, sms, 2, 2} : AttendPlan{256, 128, sms, 1, 1};
+  return {rows <= 8 ? 8 : 16, 64, sms, 1, rows <= 8 ? 4 : 2};
 }
 
 struct AttendWs { int* unit_start; float2* part_stat; float *part_out, *logits; size_t bytes; };
@@ -141,6 +141,7 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
   a.part_out = w.part_out;
   a.logits = w.logits;
   a.ctas = plan.ctas;
+  a.least = plan.least;
   cudaStream_t st = (cudaStream_t)stream;
   // A few rows are appended by the kernel itself; a warp that copies more of them holds its tiles up.
   cudaError_t e = cudaSuccess;

@@ -60,11 +60,11 @@ struct AttendArgs {
   float2* part_stat;                   // [slot][RB] reference (bits) and sum
   float* part_out;                     // [slot][RB][d]
   float* logits;                       // [units][capacity][group] in bits (accumulate)
-  int ctas;
+  int ctas, least;                     // CTAs, tiles one of them has at least
 };
 
-// Rows of a block, keys of a tile, CTAs that run at once, partials a CTA leaves of an item.
-struct AttendPlan { int rb, tile, ctas, parts; };
+// Rows of a block, keys of a tile, CTAs that run at once, partials a CTA leaves of an item, tiles it takes at least.
+struct AttendPlan { int rb, tile, ctas, parts, least; };
 
 cudaError_t launch_append(const CacheView& c, const NewRows& r, int n_new, cudaStream_t st);
 cudaError_t launch_commit(const CacheView& c, int n_new, const int* counts, const int* path, cudaStream_t st);
@@ -124,10 +124,10 @@ __device__ __forceinline__ void append_rows(const CacheView& c, const NewRows& r
 
 __device__ __forceinline__ int quotient(int n, Div d) { return (int)((__umulhi((unsigned)n, d.mul) + (unsigned)n) >> d.shift); }
 
-// How W tiles are shared out: CTA c has tiles [first(c), first(c + 1)); no more CTAs than tiles, so that each has one.
+// How W tiles are shared out: CTA c has tiles [first(c), first(c + 1)), at least `least` of them if there are as many.
 struct Shares { int W, C, each, more; };
-__device__ __forceinline__ Shares shares_of(int W, int ctas) {
-  const int C = max(1, min(W, ctas)), each = W / C;
+__device__ __forceinline__ Shares shares_of(int W, int ctas, int least) {
+  const int C = max(1, min(W / least, ctas)), each = W / C;
   return {W, C, each, W - each * C};
 }
 __device__ __forceinline__ int first_of(const Shares& s, int c) { return c >= s.C ? s.W : c * s.each + min(c, s.more); }
@@ -141,7 +141,7 @@ struct WorkStart { int lo, hi, unit, before, keys; };
 
 // By the whole block.  Units are scanned THREADS at a time.  save: unit_start.
 template <int THREADS>
-__device__ __forceinline__ WorkStart find_work(const CacheView& c, int n_new, int tile, int blocks, int ctas, int* save) {
+__device__ __forceinline__ WorkStart find_work(const CacheView& c, int n_new, int tile, int blocks, int ctas, int least, int* save) {
   constexpr int WARPS = THREADS / 32;
   __shared__ int warp_tiles[WARPS], hit[3];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -178,7 +178,7 @@ __device__ __forceinline__ WorkStart find_work(const CacheView& c, int n_new, in
     }
     if (round == 0) {
       total = before;
-      const Shares s = shares_of(total * blocks, ctas);
+      const Shares s = shares_of(total * blocks, ctas, least);
       lo = first_of(s, blockIdx.x);
       hi = first_of(s, blockIdx.x + 1);
     }

@@ -11,7 +11,7 @@
 namespace skv {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 
 // First partial of an item and how many it has.
 struct Parts { int first, count; };
@@ -19,79 +19,105 @@ __device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, 
   const int c0 = cta_of(s, start), c1 = tiles == 1 ? c0 : cta_of(s, start + tiles - 1);
   return {(item + c0) * each, (c1 - c0 + 1) * each};
 }
-// Reference and sum of a row over its partials, by a warp (the same in every lane).
-__device__ __forceinline__ float2 merged(const float2* __restrict__ stat, Parts p, int rb_rows, int row, int lane) {
-  float M = -INFINITY, L = 0.f;
-  float2 mine = make_float2(-INFINITY, 0.f);
+// Reference and sum of a row over its partials, by a warp (the same in every lane).  mine: the lane's own partial, of the first 32.
+__device__ __forceinline__ float2 merged(const float2* __restrict__ stat, Parts p, int rb_rows, int row, int lane, float2& mine) {
+  mine = lane < p.count ? stat[(size_t)(p.first + lane) * rb_rows + row] : make_float2(-INFINITY, 0.f);
+  float2 all = mine;
 #pragma unroll 1
-  for (int c = lane; c < p.count; c += 32) {                      // (more than 32: their sums as they come)
+  for (int c = lane + 32; c < p.count; c += 32) {
     const float2 x = stat[(size_t)(p.first + c) * rb_rows + row];
-    const float top = fmaxf(mine.x, x.x), ref = top == -INFINITY ? 0.f : top;
-    mine = make_float2(top, mine.y * fast_exp2(mine.x - ref) + x.y * fast_exp2(x.x - ref));
+    const float top = fmaxf(all.x, x.x), ref = top == -INFINITY ? 0.f : top;
+    all = make_float2(top, all.y * fast_exp2(all.x - ref) + x.y * fast_exp2(x.x - ref));
   }
-  M = mine.x;
+  float M = all.x;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  L = mine.y * fast_exp2(mine.x - (M == -INFINITY ? 0.f : M));
+  float L = all.y * fast_exp2(all.x - (M == -INFINITY ? 0.f : M));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
   return make_float2(M, L);
 }
-// (a row that saw nothing has reference minus infinity and sum 0, one that saw only NaN has its sum)
 __device__ __forceinline__ float bits_of(float2 st) { return st.x == -INFINITY && st.y == 0.f ? st.x : st.x == -INFINITY ? st.y : st.x + log2f(st.y); }
 
 template <int DL>
-struct Cols { float v[DL]; };
+struct alignas(4 * DL) Cols { float v[DL]; };
 
+// Blocks of 128 threads, which find room beside an attention CTA and so are there when it ends.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant__ AttendArgs a, int rb_shift, int tile_shift, int each) {
-  constexpr int DL = D / 32;
+  constexpr int DL = D / 32, kAhead = 8;
   __shared__ int hit;
   __shared__ float lse[kThreads];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rb_rows = 1 << rb_shift;
-  const int blocks = (a.rows + rb_rows - 1) >> rb_shift;
+  const int blocks = (a.rows + rb_rows - 1) >> rb_shift, all_rows = a.c.units * a.rows;
   pdl_trigger();
   pdl_wait();
+  // (loads that depend on nothing go together: the total, the item's unit, the units among which this block's run begins)
   const int W1 = a.unit_start[a.c.units];                         // tiles of one block of rows each
+  int i = blockIdx.x * (kThreads / 32) + warp;
+  const int u0 = min(tid, a.c.units - 1), start0 = a.unit_start[u0], end0 = a.unit_start[u0 + 1];
   if (W1 == 0) return;
-  const Shares sh = shares_of(W1 * blocks, a.ctas);
-  const int all_rows = a.c.units * a.rows;
+  const Shares sh = shares_of(W1 * blocks, a.ctas, a.least);
 #pragma unroll 1
-  for (int i = blockIdx.x * (kThreads / 32) + warp; i < all_rows; i += gridDim.x * (kThreads / 32)) {
+  for (; i < all_rows; i += gridDim.x * (kThreads / 32)) {
     const int u = quotient(i, a.by_rows), r = i - u * a.rows, rb = r >> rb_shift, row = r & (rb_rows - 1);
     const int start = a.unit_start[u], tiles = a.unit_start[u + 1] - start;
     if (tiles == 0) continue;
     const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles, each);
-    const float2 st = merged(a.part_stat, p, rb_rows, row, lane);
+    const float* from = a.part_out + ((size_t)p.first * rb_rows + row) * D + lane * DL;
+    Cols<DL> x[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) x[e] = e < p.count ? *(const Cols<DL>*)(from + (size_t)e * rb_rows * D) : Cols<DL>{};
+    float2 mine;
+    const float2 st = merged(a.part_stat, p, rb_rows, row, lane, mine);
     const float ref = st.x == -INFINITY ? 0.f : st.x;
     Cols<DL> acc{};
-#pragma unroll 4
-    for (int c = 0; c < p.count; ++c) {
-      const size_t at = (size_t)(p.first + c) * rb_rows + row;
-      const float2 ps = a.part_stat[at];
-      if (ps.x == -INFINITY && ps.y == 0.f) continue;             // nothing there
-      const float f = fast_exp2(ps.x - ref);
-      const Cols<DL> x = *(const Cols<DL>*)(a.part_out + at * D + lane * DL);
+#pragma unroll 1
+    for (int c0 = 0; c0 < p.count; c0 += 32) {
+      if (c0 > 0) mine = c0 + lane < p.count ? a.part_stat[(size_t)(p.first + c0 + lane) * rb_rows + row] : make_float2(-INFINITY, 0.f);
+      // (a partial that has nothing was not written)
+      const float f = mine.x == -INFINITY && mine.y == 0.f ? -1.f : fast_exp2(mine.x - ref);
+      const int n = min(32, p.count - c0);
+#pragma unroll 1
+      for (int c = 0; c < n; c += kAhead) {
+        Cols<DL> y[kAhead];
+        from += (size_t)kAhead * rb_rows * D;
 #pragma unroll
-      for (int e = 0; e < DL; ++e) acc.v[e] = fmaf(f, x.v[e], acc.v[e]);
+        for (int e = 0; e < kAhead; ++e) y[e] = c0 + c + kAhead + e < p.count ? *(const Cols<DL>*)(from + (size_t)e * rb_rows * D) : Cols<DL>{};
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const float w = __shfl_sync(0xffffffffu, f, (c + e) & 31);
+          if (c + e < n && w != -1.f)
+#pragma unroll
+            for (int d = 0; d < DL; ++d) acc.v[d] = fmaf(w, x[e].v[d], acc.v[d]);
+          x[e] = y[e];
+        }
+      }
     }
     const float inv = st.x == -INFINITY ? 0.f : 1.f / st.y;       // (a NaN row stays one)
     const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, tok = quotient(r, a.by_group), h = r - tok * a.group;
     const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
+    if (BF16) {
+      __nv_bfloat162 y[DL / 2];
 #pragma unroll
-    for (int e = 0; e < DL; ++e) {
-      if (BF16) ((__nv_bfloat16*)a.out)[q * D + lane * DL + e] = __float2bfloat16(acc.v[e] * inv);
-      else ((float*)a.out)[q * D + lane * DL + e] = acc.v[e] * inv;
+      for (int e = 0; e < DL / 2; ++e) y[e] = __floats2bfloat162_rn(acc.v[2 * e] * inv, acc.v[2 * e + 1] * inv);
+      if constexpr (DL == 4) *(uint2*)(a.out + (q * D + lane * DL) * 2) = *(uint2*)y;
+      else *(__nv_bfloat162*)(a.out + (q * D + lane * DL) * 2) = y[0];
+    } else {
+#pragma unroll
+      for (int e = 0; e < DL; ++e) acc.v[e] *= inv;
+      *(Cols<DL>*)(a.out + (q * D + lane * DL) * 4) = acc;
     }
     if (lane == 0 && a.lse) a.lse[q] = bits_of(st) * kLn2;
   }
   if (!a.accumulate) return;
 
-  const Shares runs = shares_of(W1, gridDim.x);
+  const Shares runs = shares_of(W1, gridDim.x, 1);
   const int lo = first_of(runs, blockIdx.x), hi = first_of(runs, blockIdx.x + 1);
   if (lo >= hi) return;
+  if (start0 <= lo && lo < end0) hit = u0;
 #pragma unroll 1
-  for (int u = tid; u < a.c.units; u += kThreads)
+  for (int u = tid + kThreads; u < a.c.units; u += kThreads)
     if (a.unit_start[u] <= lo && lo < a.unit_start[u + 1]) hit = u;
   __syncthreads();
   int u = hit;
@@ -100,36 +126,50 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
     const int start = a.unit_start[u], tiles = a.unit_start[u + 1] - start;
     if (tiles == 0) continue;
     const int t0 = at - start, t1 = min(tiles, t0 + (hi - at));
-    const int keys = a.c.lengths[u] + a.n_new;
+    const int end = min(a.c.lengths[u] + a.n_new, t1 << tile_shift);
     float* const w = a.c.weights + (size_t)u * a.c.capacity;
 #pragma unroll 1
-    for (int h0 = 0; h0 < a.group; h0 += kThreads) {              // (one round, but for groups of more than 256 heads)
+    for (int h0 = 0; h0 < a.group; h0 += kThreads) {              // (one round, but for groups of more than 128 heads)
       const int heads = min(kThreads, a.group - h0);
       __syncthreads();
 #pragma unroll 1
       for (int h = warp; h < heads; h += kThreads / 32) {
         const int r = h0 + h, rb = r >> rb_shift;
         const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles, each);
-        const float x = bits_of(merged(a.part_stat, p, rb_rows, r & (rb_rows - 1), lane));
+        float2 mine;
+        const float x = bits_of(merged(a.part_stat, p, rb_rows, r & (rb_rows - 1), lane, mine));
         if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
       }
       __syncthreads();
-      const bool fours = a.group % 4 == 0;
-#pragma unroll 2
-      for (int j = (t0 << tile_shift) + tid; j < min(keys, t1 << tile_shift); j += kThreads) {
-        const float* const x = a.logits + ((size_t)u * a.c.capacity + j) * a.group + h0;
-        float sum = 0.f;
-        if (fours) {
+      int j = (t0 << tile_shift) + tid;
+      if (heads == 4) {
+        // the commonest group: four keys' loads in flight
 #pragma unroll 1
-          for (int h = 0; h < heads; h += 4) {
-            const float4 v = *(const float4*)(x + h);
-            sum += (fast_exp2(v.x - lse[h]) + fast_exp2(v.y - lse[h + 1])) + (fast_exp2(v.z - lse[h + 2]) + fast_exp2(v.w - lse[h + 3]));
+        for (; j < end; j += 4 * kThreads) {
+          float4 x[4];
+          float old[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int k = j + e * kThreads;
+            x[e] = k < end ? *(const float4*)(a.logits + ((size_t)u * a.c.capacity + k) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+            old[e] = k < end ? w[k] : 0.f;
           }
-        } else {
-#pragma unroll 1
-          for (int h = 0; h < heads; ++h) sum += fast_exp2(x[h] - lse[h]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int k = j + e * kThreads;
+            const float sum = (fast_exp2(x[e].x - lse[0]) + fast_exp2(x[e].y - lse[1])) + (fast_exp2(x[e].z - lse[2]) + fast_exp2(x[e].w - lse[3]));
+            if (k < end) w[k] = fmaf(a.decay, old[e], sum);
+          }
         }
-        w[j] = (h0 == 0 ? a.decay * w[j] : w[j]) + sum;
+      } else {
+#pragma unroll 1
+        for (; j < end; j += kThreads) {
+          const float* const x = a.logits + ((size_t)u * a.c.capacity + j) * a.group + h0;
+          float sum = 0.f;
+#pragma unroll 4
+          for (int h = 0; h < heads; ++h) sum += fast_exp2(x[h] - lse[h]);
+          w[j] = (h0 == 0 ? a.decay * w[j] : w[j]) + sum;
+        }
       }
     }
     at += t1 - t0;
@@ -149,7 +189,7 @@ cudaError_t launch(const AttendArgs& a, const AttendPlan& p, int ctas, cudaStrea
 }  // namespace
 
 cudaError_t launch_attend_finish(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st) {
-  const int ctas = 2 * ctx.sm_count;
+  const int ctas = 4 * ctx.sm_count;
   if (ctx.cfg.dtype == STRUCTKV_BF16)
     return ctx.cfg.head_dim == 128 ? launch<128, true>(a, p, ctas, st) : launch<64, true>(a, p, ctas, st);
   return ctx.cfg.head_dim == 128 ? launch<128, false>(a, p, ctas, st) : launch<64, false>(a, p, ctas, st);

@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.v) : "memory");
   }
   pdl_wait();
-  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, blocks, a.ctas, blockIdx.x == 0 ? a.unit_start : nullptr);
+  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, blocks, a.ctas, a.least, blockIdx.x == 0 ? a.unit_start : nullptr);
   if (ws.lo >= ws.hi) return;
   const int run = ws.hi - ws.lo;
   Cursor cur{ws.unit, 0, 0, (ws.keys + kTileKeys - 1) / kTileKeys, ws.keys};
@@ -456,7 +456,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   pdl_wait();
-  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, 1, gridDim.x, nullptr);
+  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, 1, gridDim.x, 1, nullptr);
   if (ws.lo >= ws.hi) return;
   const int run = ws.hi - ws.lo;
   Cursor cur{ws.unit, 0, ws.lo - ws.before, (ws.keys + kTileKeys - 1) / kTileKeys, ws.keys};

@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, blocks = (a.rows + R - 1) / R;
   pdl_trigger();
   pdl_wait();
-  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, blocks, a.ctas, blockIdx.x == 0 ? a.unit_start : nullptr);
+  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, blocks, a.ctas, a.least, blockIdx.x == 0 ? a.unit_start : nullptr);
   const int hi = ws.hi;
   int u = ws.unit, at = ws.lo, unit_at = ws.before * blocks;
 #pragma unroll 1
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant_
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_trigger();
   pdl_wait();
-  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, 1, gridDim.x, nullptr);
+  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, 1, gridDim.x, 1, nullptr);
   const int hi = ws.hi;
   int u = ws.unit, at = ws.lo, unit_at = ws.before;
 #pragma unroll 1

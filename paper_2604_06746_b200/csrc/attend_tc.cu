@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     tc_fence_before();
   }
   pdl_wait();
-  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTile, blocks, a.ctas, blockIdx.x == 0 ? a.unit_start : nullptr);   // (barriers inside)
+  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTile, blocks, a.ctas, a.least, blockIdx.x == 0 ? a.unit_start : nullptr);   // (barriers inside)
   tc_fence_after();
   const uint32_t tmem = *tmem_at;
   const bool work = ws.lo < ws.hi;
