@@ -44,24 +44,30 @@ struct alignas(4 * DL) Cols { float v[DL]; };
 
 // Blocks of 128 threads, which find room beside an attention CTA and so are there when it ends.
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant__ AttendArgs a, int rb_shift, int tile_shift, int each) {
+__global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_constant__ AttendArgs a, int rb_shift, int tile_shift, int each) {
   constexpr int DL = D / 32, kAhead = 8;
-  __shared__ int hit;
+  __shared__ int hit[4];
   __shared__ float lse[kThreads];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rb_rows = 1 << rb_shift;
   const int blocks = (a.rows + rb_rows - 1) >> rb_shift, all_rows = a.c.units * a.rows;
+  int i = blockIdx.x * (kThreads / 32) + warp;
+  const int u_row = quotient(min(i, all_rows - 1), a.by_rows), u_mine = min(tid, a.c.units - 1);
   pdl_trigger();
   pdl_wait();
-  // (loads that depend on nothing go together: the total, the item's unit, the units among which this block's run begins)
+  // (loads that depend on nothing go together: the total, the first row's unit, the units among which this block's run begins)
   const int W1 = a.unit_start[a.c.units];                         // tiles of one block of rows each
-  int i = blockIdx.x * (kThreads / 32) + warp;
-  const int u0 = min(tid, a.c.units - 1), start0 = a.unit_start[u0], end0 = a.unit_start[u0 + 1];
+  int start = a.unit_start[u_row], tiles = a.unit_start[u_row + 1];
+  const int start0 = a.unit_start[u_mine], end0 = a.unit_start[u_mine + 1], keys0 = a.c.lengths[u_mine] + a.n_new;
+  tiles -= start;
   if (W1 == 0) return;
   const Shares sh = shares_of(W1 * blocks, a.ctas, a.least);
 #pragma unroll 1
-  for (; i < all_rows; i += gridDim.x * (kThreads / 32)) {
+  for (int at = i; i < all_rows; i += gridDim.x * (kThreads / 32)) {
     const int u = quotient(i, a.by_rows), r = i - u * a.rows, rb = r >> rb_shift, row = r & (rb_rows - 1);
-    const int start = a.unit_start[u], tiles = a.unit_start[u + 1] - start;
+    if (i != at) {
+      start = a.unit_start[u];
+      tiles = a.unit_start[u + 1] - start;
+    }
     if (tiles == 0) continue;
     const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles, each);
     const float* from = a.part_out + ((size_t)p.first * rb_rows + row) * D + lane * DL;
@@ -80,17 +86,16 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
       const int n = min(32, p.count - c0);
 #pragma unroll 1
       for (int c = 0; c < n; c += kAhead) {
-        Cols<DL> y[kAhead];
-        from += (size_t)kAhead * rb_rows * D;
+        if (c0 + c > 0)
 #pragma unroll
-        for (int e = 0; e < kAhead; ++e) y[e] = c0 + c + kAhead + e < p.count ? *(const Cols<DL>*)(from + (size_t)e * rb_rows * D) : Cols<DL>{};
+          for (int e = 0; e < kAhead; ++e) x[e] = c + e < n ? *(const Cols<DL>*)(from + (size_t)e * rb_rows * D) : Cols<DL>{};
+        from += (size_t)kAhead * rb_rows * D;
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
           const float w = __shfl_sync(0xffffffffu, f, (c + e) & 31);
           if (c + e < n && w != -1.f)
 #pragma unroll
             for (int d = 0; d < DL; ++d) acc.v[d] = fmaf(w, x[e].v[d], acc.v[d]);
-          x[e] = y[e];
         }
       }
     }
@@ -115,22 +120,36 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
   const Shares runs = shares_of(W1, gridDim.x, 1);
   const int lo = first_of(runs, blockIdx.x), hi = first_of(runs, blockIdx.x + 1);
   if (lo >= hi) return;
-  if (start0 <= lo && lo < end0) hit = u0;
+  auto found = [&](int u, int start, int end, int keys) {
+    if (start <= lo && lo < end) { hit[0] = u; hit[1] = start; hit[2] = end - start; hit[3] = keys; }
+  };
+  found(u_mine, start0, end0, keys0);
 #pragma unroll 1
-  for (int u = tid + kThreads; u < a.c.units; u += kThreads)
-    if (a.unit_start[u] <= lo && lo < a.unit_start[u + 1]) hit = u;
+  for (int u = tid + kThreads; u < a.c.units; u += kThreads) found(u, a.unit_start[u], a.unit_start[u + 1], a.c.lengths[u] + a.n_new);
   __syncthreads();
-  int u = hit;
+  int u = hit[0], keys = hit[3];
+  start = hit[1];
+  tiles = hit[2];
 #pragma unroll 1
-  for (int at = lo; at < hi; ++u) {
-    const int start = a.unit_start[u], tiles = a.unit_start[u + 1] - start;
-    if (tiles == 0) continue;
-    const int t0 = at - start, t1 = min(tiles, t0 + (hi - at));
-    const int end = min(a.c.lengths[u] + a.n_new, t1 << tile_shift);
+  for (int at = lo; at < hi;) {
+    const int t0 = at - start, t1 = min(tiles, t0 + (hi - at)), end = min(keys, t1 << tile_shift);
     float* const w = a.c.weights + (size_t)u * a.c.capacity;
 #pragma unroll 1
     for (int h0 = 0; h0 < a.group; h0 += kThreads) {              // (one round, but for groups of more than 128 heads)
       const int heads = min(kThreads, a.group - h0);
+      // the commonest group: four keys' loads in flight, the first ones while the references are on their way
+      float4 x[4];
+      float old[4];
+      int j = (t0 << tile_shift) + tid;
+      auto load = [&]() {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int k = j + e * kThreads;
+          x[e] = k < end ? *(const float4*)(a.logits + ((size_t)u * a.c.capacity + k) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+          old[e] = k < end ? w[k] : 0.f;
+        }
+      };
+      if (heads == 4) load();
       __syncthreads();
 #pragma unroll 1
       for (int h = warp; h < heads; h += kThreads / 32) {
@@ -141,25 +160,17 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
         if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
       }
       __syncthreads();
-      int j = (t0 << tile_shift) + tid;
       if (heads == 4) {
-        // the commonest group: four keys' loads in flight
 #pragma unroll 1
-        for (; j < end; j += 4 * kThreads) {
-          float4 x[4];
-          float old[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int k = j + e * kThreads;
-            x[e] = k < end ? *(const float4*)(a.logits + ((size_t)u * a.c.capacity + k) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-            old[e] = k < end ? w[k] : 0.f;
-          }
+        while (j < end) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int k = j + e * kThreads;
             const float sum = (fast_exp2(x[e].x - lse[0]) + fast_exp2(x[e].y - lse[1])) + (fast_exp2(x[e].z - lse[2]) + fast_exp2(x[e].w - lse[3]));
             if (k < end) w[k] = fmaf(a.decay, old[e], sum);
           }
+          j += 4 * kThreads;
+          load();
         }
       } else {
 #pragma unroll 1
@@ -173,6 +184,14 @@ __global__ void __launch_bounds__(kThreads) attend_finish(const __grid_constant_
       }
     }
     at += t1 - t0;
+    if (at < hi) {
+      do {
+        ++u;
+        start = a.unit_start[u];
+        tiles = a.unit_start[u + 1] - start;
+      } while (tiles == 0);
+      keys = a.c.lengths[u] + a.n_new;
+    }
   }
 }
 

@@ -80,12 +80,21 @@ __device__ __forceinline__ void advance(Cursor& c, const CacheView& cache, int n
 
 struct CacheMaps { CUtensorMap k, v; };
 
+// Bounded wait of a warp for a count in shared memory to grow above n.
+__device__ __forceinline__ bool wait_above(const volatile int* count, int n, volatile int* abort_flag) {
+  bool ok = *count > n;
+  for (const long long t0 = clock64(); !ok && !*abort_flag; ok = *count > n)
+    if ((unsigned long long)(clock64() - t0) > kWaitCycles) *abort_flag = 1;
+  __threadfence_block();
+  return __all_sync(0xffffffffu, ok);
+}
+
 // NR blocks of 8 rows; four warps along a tile's keys, NG groups of these.
 template <int D, int NR, int NG>
 struct AttendShape {
-  static constexpr int RB = 8 * NR, kWarps = 4 * NG, THREADS = 32 + kWarps * 32, kSets = 4 * NG;
+  static constexpr int RB = 8 * NR, kWarps = 4 * NG, THREADS = 64 + kWarps * 32, kSets = 4 * NG;
   static constexpr int kTileBytes = kTileKeys * D * 2;
-  static constexpr int kPosOff = 2 * kTileBytes, kQOff = kPosOff + 1024, kStage = kQOff + RB * D * 2;
+  static constexpr int kPosOff = 2 * kTileBytes, kStage = kPosOff + 1024;
   static constexpr int kRow = D + 4;                             // of a set's output: rows two apart are eight banks apart
   static constexpr int kFixed = kSets * RB * (kRow + 2) * 4 + 256 + 1024;
   // (a place of the ring always serves the same group: a wait by parity holds only for who follows a barrier from phase to phase)
@@ -95,7 +104,7 @@ struct AttendShape {
 };
 
 template <int D, int NR, int NG, bool OPT>
-__global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps) {
+__global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps) {
   using S = AttendShape<D, NR, NG>;
   constexpr int RB = S::RB, NT = S::THREADS, CH = D / 8, ST = S::kStages, KK = D / 16;
   extern __shared__ unsigned char smem_raw[];
@@ -105,6 +114,7 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
   float* const stat = outs + S::kSets * RB * S::kRow;           // [2][set][RB]
   const uint32_t bars = smem_u32(stat + 2 * S::kSets * RB);     // full [ST], empty [ST]
   volatile int* const abort_flag = (volatile int*)(stat + 2 * S::kSets * RB) + 4 * ST;
+  volatile int* const appended = abort_flag + 1;                // tiles of the run up to which new rows are in the cache
   auto full = [&](int st) { return bars + 8 * st; };
   auto empty = [&](int st) { return bars + 8 * (ST + st); };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -112,10 +122,11 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
   pdl_trigger();
   if (tid == 0) {
     for (int i = 0; i < ST; ++i) {
-      mbar_init(full(i), 33);                                   // the copies by TMA, and 32 lanes' own
+      mbar_init(full(i), OPT ? 33 : 1);                         // the copies by TMA, and 32 lanes' own
       mbar_init(empty(i), 4);
     }
     *abort_flag = 0;
+    *appended = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.v) : "memory");
@@ -134,19 +145,13 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
   if (warp == 0) {
     // the ring's producer
     const uint64_t hint = blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
-    int since = 0, st = 0;                                      // tiles since the segment began
-    int n = 0;
+    int st = 0, n = 0;
 #pragma unroll 1
     for (; n < run; ++n) {
       const int b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv;
       const uint32_t to = base + st * S::kStage;
-      if (cur.t == 0) since = 0;
-      if (a.fresh.k && (cur.t + 1) * kTileKeys > cur.keys - a.n_new) {
-        append_rows(a.c, a.fresh, a.n_new, cur.u, b, g, cur.keys - a.n_new, lane);
-        asm volatile("fence.proxy.async;" ::: "memory");        // they are read by TMA
-        __syncwarp();
-      }
       if (n >= ST && !mbar_wait_producer(empty(st), (n / ST - 1) & 1, abort_flag, kWaitCycles)) break;
+      if (a.fresh.k && (cur.t + 1) * kTileKeys > cur.keys - a.n_new && !wait_above(appended, n, abort_flag)) break;
       if (lane == 0) {
         mbar_expect_tx(full(st), 2 * S::kTileBytes);
 #pragma unroll
@@ -155,26 +160,17 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
           tma_load_4d(to + S::kTileBytes + c * kTileKeys * 128, &maps.v, full(st), c * 64, cur.t * kTileKeys, g, b, hint);
         }
       }
-      if (OPT && a.slopes) {
-        const int* const pos = a.c.positions + (size_t)cur.u * a.c.capacity;
+      if (OPT) {
+        if (a.slopes) {
+          const int* const pos = a.c.positions + (size_t)cur.u * a.c.capacity;
 #pragma unroll
-        for (int i = lane; i < kTileKeys; i += 32) {
-          const int j = cur.t * kTileKeys + i;
-          cp4(to + S::kPosOff + i * 4, pos + (j < cur.keys ? j : 0), j < cur.keys);
+          for (int i = lane; i < kTileKeys; i += 32) {
+            const int j = cur.t * kTileKeys + i;
+            cp4(to + S::kPosOff + i * 4, pos + (j < cur.keys ? j : 0), j < cur.keys);
+          }
         }
+        cp_arrive(full(st));
       }
-      if (since < NG) {                                         // a segment begins: every group's first tile brings the rows
-#pragma unroll 1
-        for (int i = lane; i < RB * CH; i += 32) {
-          const int row = i / CH, ch = i % CH, r = cur.rb * RB + row;
-          const bool is = r < a.rows;
-          const int tok = is ? quotient(r, a.by_group) : 0, h = is ? r - tok * a.group : 0;
-          cp16(to + S::kQOff + chunk_at<D>(row, ch),
-               a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head + ch * 16, is);
-        }
-      }
-      cp_arrive(full(st));
-      ++since;
       if (++st == ST) st = 0;
       if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
     }
@@ -185,8 +181,26 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
     }
     return;
   }
+  if (warp == 1) {
+    // New rows go into the cache ahead of the tiles that have them, which TMA reads.  (Row blocks of a unit in other CTAs write the
+    // same bytes.)
+    if (!a.fresh.k) return;
+#pragma unroll 1
+    for (int n = 0; n < run; ++n) {
+      if ((cur.t + 1) * kTileKeys > cur.keys - a.n_new) {
+        const int b = quotient(cur.u, a.by_kv);
+        append_rows(a.c, a.fresh, a.n_new, cur.u, b, cur.u - b * a.c.n_kv, cur.keys - a.n_new, lane);
+        asm volatile("fence.proxy.async;" ::: "memory");
+        __syncwarp();
+        __threadfence_block();
+        if (lane == 0) *appended = n + 1;
+      }
+      if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
+    }
+    return;
+  }
 
-  const int cw = warp - 1, grp = cw / 4, kw = cw % 4, g8 = lane >> 2, t4 = lane & 3;
+  const int cw = warp - 2, grp = cw / 4, kw = cw % 4, g8 = lane >> 2, t4 = lane & 3;
   auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(S::kWarps * 32) : "memory"); };
   uint32_t qf[NR][KK][2];
   float o[NR][KK][4];                                           // column g8 (+ 8) of 16, rows 2 t4 and + 1 of the block
@@ -201,21 +215,24 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
     if (n % NG == grp) {
       const uint32_t from = base + st * S::kStage;
       const unsigned char* const here = sm + st * S::kStage;
-      mbar_wait(full(st), (n / ST) & 1, abort_flag);            // (on expiry the numbers are void, the control flow goes on)
       if (fresh) {
+        // a segment begins: its rows, while the tile is on its way
         fresh = false;
+        const int b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) { m[i][x] = -INFINITY; l[i][x] = 0.f; }
 #pragma unroll
           for (int k = 0; k < KK; ++k) o[i][k][0] = o[i][k][1] = o[i][k][2] = o[i][k][3] = 0.f;
+          const int r = cur.rb * RB + 8 * i + g8;
+          const bool is = r < a.rows;
+          const int tok = is ? quotient(r, a.by_group) : 0, h = is ? r - tok * a.group : 0;
+          const char* const q = a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head + t4 * 4;
 #pragma unroll
-          for (int kk = 0; kk < KK; kk += 2) {
-            uint32_t x[4];
-            ldsm(from + S::kQOff + chunk_at<D>(i * 8 + (lane & 7), kk * 2 + (lane >> 3)), x);
-            qf[i][kk][0] = x[0]; qf[i][kk][1] = x[1]; qf[i][kk + 1][0] = x[2]; qf[i][kk + 1][1] = x[3];
-          }
+          for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) qf[i][kk][y] = is ? *(const uint32_t*)(q + kk * 32 + y * 16) : 0u;
         }
         if (OPT && a.slopes)
 #pragma unroll
@@ -227,6 +244,7 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
               place[i][x] = ro.position;
             }
       }
+      mbar_wait(full(st), (n / ST) & 1, abort_flag);            // (on expiry the numbers are void, the control flow goes on)
       // products: two chains where a warp has one block of rows
       constexpr int CHAINS = NR == 1 ? 2 : 1;
       float acc[CHAINS][NR][4];
@@ -395,14 +413,14 @@ __global__ void __launch_bounds__(32 + 128 * NG, 1) attend_mma(const __grid_cons
       sync();
       const int slot = cur.u * blocks + cur.rb + blockIdx.x, rows = min(RB, a.rows - cur.rb * RB);
 #pragma unroll 1
-      for (int i = tid - 32; i < rows * (D / 4); i += S::kWarps * 32) {
+      for (int i = tid - 64; i < rows * (D / 4); i += S::kWarps * 32) {
         const int row = i / (D / 4), c4 = i % (D / 4);
         float top = -INFINITY, sum = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int w = 0; w < sets; ++w) top = fmaxf(top, stat[w * RB + row]);
+#pragma unroll
+        for (int w = 0; w < S::kSets; ++w) top = fmaxf(top, w < sets ? stat[w * RB + row] : -INFINITY);
         const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll 4
+#pragma unroll 8
         for (int w = 0; w < sets; ++w) {
           const float f = fast_exp2(stat[w * RB + row] - ref);
           const float4 x = *(const float4*)(outs + (w * RB + row) * S::kRow + c4 * 4);

@@ -46,6 +46,32 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
                ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
                  "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
+// The load of 32 columns and its wait apart: several loads travel together.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+               "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                 "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+                 "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]),
+                 "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]),
+                 "=f"(v[30]), "=f"(v[31])
+               : "r"(taddr) : "memory");
+}
+// (registers that a load in flight writes are operands of a wait, so that no use of them comes before it)
+__device__ __forceinline__ void tmem_landed(float* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                 "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
+                 "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]),
+                 "+f"(v[30]), "+f"(v[31])
+               :: "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&f)[32]) {
   uint32_t lo[16], hi[16];
 #pragma unroll
@@ -154,6 +180,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
   bool clean = true;                                             // every MMA of this CTA has retired
 
+  // 128 x 88 + 256 x 200 registers of the 384 x 168 that the block was launched with
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (work && warp == 0) {
     const uint64_t hint = blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
     Segments sg = first_segment(ws, blocks);
@@ -260,13 +289,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
       const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv, n_old = sg.keys - a.n_new;
       const char* const q0 = a.q + (size_t)b * a.q_batch + (size_t)(g * a.group) * a.q_head;
 #pragma unroll 4
-      for (int i = hl; i < RB * CH; i += 64) {
-        const int row = i / CH, ch = i % CH, r = sg.rb * RB + row;
-        const bool is = r < a.rows;
-        const int tok = is ? quotient(r, a.by_group) : 0, h = is ? r - tok * a.group : 0;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+      for (int i = hl; i < min(RB, a.rows - sg.rb * RB) * CH; i += 64) {   // (rows beyond them do not reach these)
+        const int row = i / CH, ch = i % CH, r = sg.rb * RB + row, tok = quotient(r, a.by_group), h = r - tok * a.group;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
                      ::"r"(base + (ch >> 3) * (RB * 128) + row * 128 + (((ch ^ row) & 7) << 4)),
-                       "l"(q0 + (size_t)tok * a.q_token + (size_t)h * a.q_head + ch * 16), "r"(is ? 16 : 0) : "memory");
+                       "l"(q0 + (size_t)tok * a.q_token + (size_t)h * a.q_head + ch * 16) : "memory");
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -298,7 +325,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
       n += sg.t1 - sg.t0;
       ++seg;
     } while (ok && next_segment(sg, a, blocks));
-  } else if (work) {
+  }
+  } else {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+  if (work) {
     const int s = (warp - 4) / 4, quarter = warp % 4;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
     const float scale2 = fabsf(a.scale2), inv_cap = fabsf(a.inv_cap);   // (a negative scale negates the product)
@@ -324,44 +354,49 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
         }
         tc_fence_after();
         if (!idle) {
-          const bool tail = j0 + kTile > n_old;
-          float top = -INFINITY, mul = scale2;
-          float v[32];
-          if (OPT || tail) {
-            // x in bits, back to its place
-            mul = 1.f;
+          if (OPT) {
+            // x in bits, back to its place (a loop: this code 128 times over would not stay in the instruction cache)
 #pragma unroll 1
             for (int c = 0; c < kTile; c += 32) {
-              tmem_ld(s_at + c, v);
+              float x[32];
+              tmem_ld(s_at + c, x);
 #pragma unroll
               for (int e = 0; e < 32; ++e) {
-                float x = v[e] * scale2;
-                if (OPT) {
-                  if (a.cap2 != 0.f) x = capped(v[e], a.cap2, inv_cap);
-                  if (a.slopes) x = fmaf(-ro.slope2, (float)(ro.position - kp[c + e]), x);
-                }
-                const int j = j0 + c + e;
-                if (tail && (j >= sg.keys || !sees(ro.seen, j, n_old))) x = -INFINITY;
-                v[e] = x;
-                top = fmaxf(top, x);
+                x[e] = a.cap2 != 0.f ? capped(x[e], a.cap2, inv_cap) : x[e] * scale2;
+                if (a.slopes) x[e] = fmaf(-ro.slope2, (float)(ro.position - kp[c + e]), x[e]);
               }
-              tmem_st32(s_at + c, v);
+              tmem_st32(s_at + c, x);
             }
             tmem_st_wait();
-          } else {
+          }
+          float v[kTile], top = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < kTile; c += 32) tmem_ld32(s_at + c, v + c);
+#pragma unroll
+          for (int c = 0; c < kTile; c += 32) tmem_landed(v + c);
+          if (j0 + kTile > n_old) {
+            // the tile has new tokens: bit e of a word says whether column c + e is seen
 #pragma unroll
             for (int c = 0; c < kTile; c += 32) {
-              tmem_ld(s_at + c, v);
-              float t0 = fmaxf(v[0], v[1]), t1 = fmaxf(v[2], v[3]);
+              const int first = j0 + c - n_old, keys = sg.keys - j0 - c;     // of the new tokens; keys from here on
+              uint32_t see = first >= 64 ? 0u : first >= 0 ? (uint32_t)(ro.seen >> first)
+                             : first > -32 ? (uint32_t)(ro.seen << -first) | ((1u << -first) - 1u) : 0xffffffffu;
+              see = keys >= 32 ? see : keys <= 0 ? 0u : see & ((1u << keys) - 1u);
 #pragma unroll
-              for (int e = 4; e < 32; e += 4) {
-                t0 = fmaxf(t0, fmaxf(v[e], v[e + 1]));
-                t1 = fmaxf(t1, fmaxf(v[e + 2], v[e + 3]));
-              }
-              top = fmaxf(top, fmaxf(t0, t1));
+              for (int e = 0; e < 32; ++e) v[c + e] = see >> e & 1 ? v[c + e] : -INFINITY;
             }
-            top *= scale2;
           }
+          {
+            float t0 = v[0], t1 = v[1];
+#pragma unroll
+            for (int e = 2; e + 3 < kTile; e += 4) {
+              t0 = max3(t0, v[e], v[e + 1]);
+              t1 = max3(t1, v[e + 2], v[e + 3]);
+            }
+            top = fmaxf(max3(t0, t1, v[kTile - 2]), v[kTile - 1]);
+          }
+          const float mul = OPT ? 1.f : scale2;
+          top *= mul;
           const bool grown = top > m + kSlack;
           if (__any_sync(0xffffffffu, grown)) {
             const float to = grown ? top : m, f = m == -INFINITY ? 0.f : fast_exp2(m - to);
@@ -371,32 +406,38 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
               if (!(ok = wait(o_done(s), (done - 1) & 1))) break;
               tc_fence_after();
 #pragma unroll 1
-              for (int c = 0; c < D; c += 32) {
-                tmem_ld(o_at + c, v);
+              for (int c = 0; c < D; c += 16) {
+                float x[16];
+                uint32_t y[16];
+                tmem_ld_issue<16>(o_at + c, x);
+                tmem_ld_wait(x);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] *= f;
-                tmem_st32(o_at + c, v);
+                for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(x[e] * f);
+                tmem_st16(o_at + c, y);
               }
               tmem_st_wait();
             }
           }
           const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll 1
+          const uint64_t mul2 = pack2(mul, mul), ref2 = pack2(-ref, -ref);
+          uint64_t sum = pack2(0.f, 0.f);
+#pragma unroll
           for (int c = 0; c < kTile; c += 32) {
-            tmem_ld(s_at + c, v);
             uint32_t p[16];
-            float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              const float p0 = fast_exp2(fmaf(v[e], mul, -ref)), p1 = fast_exp2(fmaf(v[e + 1], mul, -ref));
-              sum0 += p0;
-              sum1 += p1;
+              const uint64_t x = exp2_sfu2(fma2(pack2(v[c + e], v[c + e + 1]), mul2, ref2));
+              float p0, p1;
+              unpack2(x, p0, p1);
+              sum = add2(sum, x);
               // p keeps 8 bits for the product, as V does; the sum l is of the unrounded values
               p[e / 2] = bf16x2(p0, p1);
             }
-            l += sum0 + sum1;
-            tmem_st16(s_at + c / 2, p);                          // (over columns that have been read)
+            tmem_st16(s_at + c / 2, p);                          // (over scores, which are in registers)
           }
+          float s0, s1;
+          unpack2(sum, s0, s1);
+          l += s0 + s1;
           tmem_st_wait();
         }
         tc_fence_before();
@@ -416,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
           for (int c = 0; c < D; c += 32) {
             float v[32];
             tmem_ld(o_at + c, v);
-            if (odd) {
+            if (odd && r < a.rows) {
               // V of new tokens that is not finite was left out of the product: it makes what sees it so
               unsigned long long rest = ro.seen & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1);
 #pragma unroll 1
@@ -444,6 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
       }
       n += tiles;
     } while (next_segment(sg, a, blocks));
+  }
   }
 
   tc_fence_before();
