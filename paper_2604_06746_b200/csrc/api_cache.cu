@@ -16,9 +16,9 @@ bool by_tensor_cores(const structkv_config& cfg, int n_new) {
 }
 AttendPlan attend_plan(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms, 1, 2};
-  if (by_tensor_cores(cfg, n_new)) return rows <= 128 ? AttendPlan{128, 128, sms, 2, 2} : AttendPlan{256, 128, sms, 1, 1};
-  return {rows <= 8 ? 8 : 16, 64, sms, 1, rows <= 8 ? 4 : 2};
+  if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms, 1, 1};
+  if (by_tensor_cores(cfg, n_new)) return rows <= 128 ? AttendPlan{128, 128, sms, 2, 0} : AttendPlan{256, 128, sms, 1, 0};
+  return {rows <= 8 ? 8 : 16, 64, sms, 1, rows <= 8 ? 1 : 0};
 }
 
 struct AttendWs { int* unit_start; float2* part_stat; float *part_out, *logits; size_t bytes; };
@@ -134,6 +134,7 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
   const AttendPlan plan = attend_plan(c.cfg, args->n_new, std::min(c.sm_count, kMaxSms));
   const AttendWs w = carve_attend(c.cfg, plan, cache->batch, args->n_new, cache->capacity, args->workspace);
   if (!args->workspace || args->workspace_bytes < w.bytes || (uintptr_t)args->workspace % 256) return STRUCTKV_ERR_WORKSPACE;
+  const bool tc = by_tensor_cores(c.cfg, args->n_new);
   a.out = (char*)args->out;
   a.accumulate = args->accumulate != 0;
   a.unit_start = w.unit_start;
@@ -141,11 +142,11 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
   a.part_out = w.part_out;
   a.logits = w.logits;
   a.ctas = plan.ctas;
+  a.by_ctas = div_by(plan.ctas);
   a.least = plan.least;
   cudaStream_t st = (cudaStream_t)stream;
   // A few rows are appended by the kernel itself; a warp that copies more of them holds its tiles up.
   cudaError_t e = cudaSuccess;
-  const bool tc = by_tensor_cores(c.cfg, args->n_new);
   if (args->rows && c.cfg.dtype == STRUCTKV_BF16 && !tc && args->n_new <= 8) a.fresh = r;
   else if (args->rows) e = launch_append(a.c, r, args->n_new, st);
   if (e == cudaSuccess)
@@ -159,6 +160,8 @@ structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, c
   AttendArgs a{};
   if (!args || !accepted || (uintptr_t)accepted % 8 || !args->lse) return STRUCTKV_ERR_INVALID_ARG;
   if (!view_of(ctx, cache, args->n_new, &a.c) || !cache->weights || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
+  a.ctas = ctx->c.cfg.dtype == STRUCTKV_BF16 ? ctx->c.sm_count : 4 * ctx->c.sm_count;   // (CTAs that run at once)
+  a.by_ctas = div_by(a.ctas);
   return told((ctx->c.cfg.dtype == STRUCTKV_BF16 ? launch_weigh_bf16 : launch_weigh_fp32)(ctx->c, a, accepted, (cudaStream_t)stream));
 }
 

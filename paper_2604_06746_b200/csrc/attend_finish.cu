@@ -13,12 +13,6 @@ namespace {
 
 constexpr int kThreads = 128;
 
-// First partial of an item and how many it has.
-struct Parts { int first, count; };
-__device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, int tiles, int each) {
-  const int c0 = cta_of(s, start), c1 = tiles == 1 ? c0 : cta_of(s, start + tiles - 1);
-  return {(item + c0) * each, (c1 - c0 + 1) * each};
-}
 // Reference and sum of a row over its partials, by a warp (the same in every lane).  mine: the lane's own partial, of the first 32.
 __device__ __forceinline__ float2 merged(const float2* __restrict__ stat, Parts p, int rb_rows, int row, int lane, float2& mine) {
   mine = lane < p.count ? stat[(size_t)(p.first + lane) * rb_rows + row] : make_float2(-INFINITY, 0.f);
@@ -44,7 +38,7 @@ struct alignas(4 * DL) Cols { float v[DL]; };
 
 // Blocks of 128 threads, which find room beside an attention CTA and so are there when it ends.
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_constant__ AttendArgs a, int rb_shift, int tile_shift, int each) {
+__global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_constant__ AttendArgs a, int rb_shift, int tile_shift, int each, Div by_grid) {
   constexpr int DL = D / 32, kAhead = 8;
   __shared__ int hit[4];
   __shared__ float lse[kThreads];
@@ -60,7 +54,7 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
   const int start0 = a.unit_start[u_mine], end0 = a.unit_start[u_mine + 1], keys0 = a.c.lengths[u_mine] + a.n_new;
   tiles -= start;
   if (W1 == 0) return;
-  const Shares sh = shares_of(W1 * blocks, a.ctas, a.least);
+  const Shares sh = shares_of(W1 * blocks, a.ctas, a.by_ctas, a.least);
 #pragma unroll 1
   for (int at = i; i < all_rows; i += gridDim.x * (kThreads / 32)) {
     const int u = quotient(i, a.by_rows), r = i - u * a.rows, rb = r >> rb_shift, row = r & (rb_rows - 1);
@@ -117,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
   }
   if (!a.accumulate) return;
 
-  const Shares runs = shares_of(W1, gridDim.x, 1);
+  const Shares runs = shares_of(W1, gridDim.x, by_grid, 0);
   const int lo = first_of(runs, blockIdx.x), hi = first_of(runs, blockIdx.x + 1);
   if (lo >= hi) return;
   auto found = [&](int u, int start, int end, int keys) {
@@ -202,7 +196,7 @@ int log2_of(int x) {
 }
 template <int D, bool BF16>
 cudaError_t launch(const AttendArgs& a, const AttendPlan& p, int ctas, cudaStream_t st) {
-  return launch_pdl(attend_finish<D, BF16>, dim3(ctas), dim3(kThreads), 0, st, a, log2_of(p.rb), log2_of(p.tile), p.parts);
+  return launch_pdl(attend_finish<D, BF16>, dim3(ctas), dim3(kThreads), 0, st, a, log2_of(p.rb), log2_of(p.tile), p.parts, div_by(ctas));
 }
 
 }  // namespace

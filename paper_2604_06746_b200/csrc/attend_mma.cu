@@ -18,19 +18,16 @@ namespace {
 constexpr int kTileKeys = 64;
 constexpr float kSlack = 8.f;
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
 // Arrives once this thread's cp.async copies so far are there (one of the barrier's expected arrivals).
 __device__ __forceinline__ void cp_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, uint64_t policy) {
+__device__ __forceinline__ void tma_load_slots(uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot, int head, int seq, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
-      "[%0], [%1, {%3, %4, %5, %6}], [%2], %7;"
-      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "l"(policy) : "memory");
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%3, %4, %3, %5, %6}], [%2], %7;"
+      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(0), "r"(slot), "r"(head), "r"(seq), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void ldsm(uint32_t at, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -106,12 +103,12 @@ struct AttendShape {
 template <int D, int NR, int NG, bool OPT>
 __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps) {
   using S = AttendShape<D, NR, NG>;
-  constexpr int RB = S::RB, NT = S::THREADS, CH = D / 8, ST = S::kStages, KK = D / 16;
+  constexpr int RB = S::RB, CH = D / 8, ST = S::kStages, KK = D / 16;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
   float* const outs = (float*)(sm + ST * S::kStage);            // [set][RB][kRow]
-  float* const stat = outs + S::kSets * RB * S::kRow;           // [2][set][RB]
+  float* const stat = outs + S::kSets * RB * S::kRow;           // [2][RB][set]
   const uint32_t bars = smem_u32(stat + 2 * S::kSets * RB);     // full [ST], empty [ST]
   volatile int* const abort_flag = (volatile int*)(stat + 2 * S::kSets * RB) + 4 * ST;
   volatile int* const appended = abort_flag + 1;                // tiles of the run up to which new rows are in the cache
@@ -131,8 +128,9 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.v) : "memory");
   }
+  __syncthreads();
   pdl_wait();
-  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, blocks, a.ctas, a.least, blockIdx.x == 0 ? a.unit_start : nullptr);
+  const WorkStart ws = find_work(a, 6, blocks, blockIdx.x == 0 ? a.unit_start : nullptr);
   if (ws.lo >= ws.hi) return;
   const int run = ws.hi - ws.lo;
   Cursor cur{ws.unit, 0, 0, (ws.keys + kTileKeys - 1) / kTileKeys, ws.keys};
@@ -154,11 +152,8 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
       if (a.fresh.k && (cur.t + 1) * kTileKeys > cur.keys - a.n_new && !wait_above(appended, n, abort_flag)) break;
       if (lane == 0) {
         mbar_expect_tx(full(st), 2 * S::kTileBytes);
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          tma_load_4d(to + c * kTileKeys * 128, &maps.k, full(st), c * 64, cur.t * kTileKeys, g, b, hint);
-          tma_load_4d(to + S::kTileBytes + c * kTileKeys * 128, &maps.v, full(st), c * 64, cur.t * kTileKeys, g, b, hint);
-        }
+        tma_load_slots(to, &maps.k, full(st), cur.t * kTileKeys, g, b, hint);
+        tma_load_slots(to + S::kTileBytes, &maps.v, full(st), cur.t * kTileKeys, g, b, hint);
       }
       if (OPT) {
         if (a.slopes) {
@@ -402,34 +397,16 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
             for (int d = 4; d < 32; d *= 2) l[i][x] += __shfl_xor_sync(0xffffffffu, l[i][x], d);
             const int row = 8 * i + 2 * t4 + x;
             if (g8 == 0) {
-              stat[my * RB + row] = m[i][x];
-              stat[(S::kSets + my) * RB + row] = l[i][x];
+              stat[row * S::kSets + my] = m[i][x];
+              stat[(RB + row) * S::kSets + my] = l[i][x];
             }
             float* const to = outs + (my * RB + row) * S::kRow + g8;
 #pragma unroll
             for (int k = 0; k < KK; ++k) { to[k * 16] = o[i][k][x]; to[k * 16 + 8] = o[i][k][2 + x]; }
           }
       }
-      sync();
-      const int slot = cur.u * blocks + cur.rb + blockIdx.x, rows = min(RB, a.rows - cur.rb * RB);
-#pragma unroll 1
-      for (int i = tid - 64; i < rows * (D / 4); i += S::kWarps * 32) {
-        const int row = i / (D / 4), c4 = i % (D / 4);
-        float top = -INFINITY, sum = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < S::kSets; ++w) top = fmaxf(top, w < sets ? stat[w * RB + row] : -INFINITY);
-        const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll 8
-        for (int w = 0; w < sets; ++w) {
-          const float f = fast_exp2(stat[w * RB + row] - ref);
-          const float4 x = *(const float4*)(outs + (w * RB + row) * S::kRow + c4 * 4);
-          sum = fmaf(f, stat[(S::kSets + w) * RB + row], sum);
-          v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
-        }
-        *(float4*)(a.part_out + ((size_t)slot * RB + row) * D + c4 * 4) = v;
-        if (c4 == 0) a.part_stat[(size_t)slot * RB + row] = make_float2(top, sum);
-      }
+      leave_partial<D, S::kWarps * 32, RB, S::kRow, S::kSets>(a, cur.u * blocks + cur.rb + blockIdx.x, min(RB, a.rows - cur.rb * RB), outs, stat,
+                                                              stat + RB * S::kSets, sets, tid - 64, sync);
       if (n + 1 < run) sync();
       fresh = true;
       seg = n + 1;
@@ -452,7 +429,7 @@ constexpr int weigh_smem() {
 template <int D, bool OPT>
 __global__ void __launch_bounds__(32 + kWeighWarps * 32, 1)
 weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMaps maps, const unsigned long long* __restrict__ accepted) {
-  constexpr int NT = 32 + kWeighWarps * 32, CH = D / 8, KK = D / 16, ST = kWeighStages, kTileBytes = kTileKeys * D * 2, kStage = kTileBytes + 1024;
+  constexpr int CH = D / 8, KK = D / 16, ST = kWeighStages, kTileBytes = kTileKeys * D * 2, kStage = kTileBytes + 1024;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
@@ -473,8 +450,9 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  __syncthreads();
   pdl_wait();
-  const WorkStart ws = find_work<NT>(a.c, a.n_new, kTileKeys, 1, gridDim.x, 1, nullptr);
+  const WorkStart ws = find_work(a, 6, 1, nullptr);
   if (ws.lo >= ws.hi) return;
   const int run = ws.hi - ws.lo;
   Cursor cur{ws.unit, 0, ws.lo - ws.before, (ws.keys + kTileKeys - 1) / kTileKeys, ws.keys};
@@ -496,9 +474,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
         if (n >= ST && !(ok = mbar_wait_producer(empty(st), (n / ST - 1) & 1, abort_flag, kWaitCycles))) break;
         if (lane == 0) {
           mbar_expect_tx(full(st), kTileBytes);
-#pragma unroll
-          for (int c = 0; c < D / 64; ++c)
-            tma_load_4d(to + c * kTileKeys * 128, &maps.k, full(st), c * 64, t * kTileKeys, g, b, rounds == 1 ? policy : again);
+          tma_load_slots(to, &maps.k, full(st), t * kTileKeys, g, b, rounds == 1 ? policy : again);
         }
         if (OPT && a.slopes) {
           const int* const pos = a.c.positions + (size_t)cur.u * a.c.capacity;
@@ -636,9 +612,9 @@ cudaError_t launch_rows(const AttendArgs& a, const AttendPlan& p, const CacheMap
   return p.rb == 8 ? launch_one<D, 1, 4, OPT>(a, m, st) : launch_one<D, 2, 2, OPT>(a, m, st);
 }
 template <int D, bool OPT>
-cudaError_t launch_weigh(const AttendArgs& a, const CacheMaps& m, const unsigned long long* accepted, int ctas, cudaStream_t st) {
+cudaError_t launch_weigh(const AttendArgs& a, const CacheMaps& m, const unsigned long long* accepted, cudaStream_t st) {
   const cudaError_t e = allow_smem<weigh_mma<D, OPT>>(weigh_smem<D>());
-  return e != cudaSuccess ? e : launch_pdl(weigh_mma<D, OPT>, dim3(ctas), dim3(32 + kWeighWarps * 32), weigh_smem<D>(), st, a, m, accepted);
+  return e != cudaSuccess ? e : launch_pdl(weigh_mma<D, OPT>, dim3(a.ctas), dim3(32 + kWeighWarps * 32), weigh_smem<D>(), st, a, m, accepted);
 }
 
 }  // namespace
@@ -653,9 +629,8 @@ cudaError_t launch_attend_mma(const Ctx& ctx, const AttendArgs& a, const AttendP
 cudaError_t launch_weigh_bf16(const Ctx& ctx, const AttendArgs& a, const unsigned long long* accepted, cudaStream_t st) {
   CacheMaps m;
   if (!encode(ctx, a, &m)) return cudaErrorInvalidValue;
-  const int ctas = ctx.sm_count;
-  if (ctx.cfg.head_dim == 128) return options(a) ? launch_weigh<128, true>(a, m, accepted, ctas, st) : launch_weigh<128, false>(a, m, accepted, ctas, st);
-  return options(a) ? launch_weigh<64, true>(a, m, accepted, ctas, st) : launch_weigh<64, false>(a, m, accepted, ctas, st);
+  if (ctx.cfg.head_dim == 128) return options(a) ? launch_weigh<128, true>(a, m, accepted, st) : launch_weigh<128, false>(a, m, accepted, st);
+  return options(a) ? launch_weigh<64, true>(a, m, accepted, st) : launch_weigh<64, false>(a, m, accepted, st);
 }
 
 }  // namespace skv

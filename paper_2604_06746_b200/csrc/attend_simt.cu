@@ -24,7 +24,8 @@ template <int D>
 struct Shape {
   static constexpr int kRow = D + 16, kStages = D == 128 ? 2 : 4;
   static constexpr int kStage = kTileKeys * kRow + kTileKeys * D;     // floats
-  static constexpr int kSmem(int R) { return (kStages * kStage + R * D + kWarps * R * (D + 2)) * 4; }
+  template <int R>
+  static constexpr int kSmem = (kStages * kStage + R * D + kWarps * R * (D + 2)) * 4;
 };
 
 template <int D>
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, blocks = (a.rows + R - 1) / R;
   pdl_trigger();
   pdl_wait();
-  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, blocks, a.ctas, a.least, blockIdx.x == 0 ? a.unit_start : nullptr);
+  const WorkStart ws = find_work(a, 6, blocks, blockIdx.x == 0 ? a.unit_start : nullptr);
   const int hi = ws.hi;
   int u = ws.unit, at = ws.lo, unit_at = ws.before * blocks;
 #pragma unroll 1
@@ -155,28 +156,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
     for (int r = 0; r < R; ++r) {
 #pragma unroll
       for (int d = 4; d < 32; d *= 2) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
-      if (lane == 0) { stat[warp * R + r] = m[r]; stat[(kWarps + warp) * R + r] = l[r]; }
+      if (lane == 0) { stat[r * kWarps + warp] = m[r]; stat[(R + r) * kWarps + warp] = l[r]; }
 #pragma unroll
       for (int c = 0; c < DL; ++c) part[(warp * R + r) * D + c * 32 + lane] = o[r][c];
     }
-    __syncthreads();
-    const int slot = u * blocks + rb + blockIdx.x;
-    for (int i = tid; i < R * D; i += kThreads) {
-      const int row = i / D, col = i % D;
-      if (rb * R + row >= a.rows) break;
-      float M = -INFINITY, L = 0.f, acc = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, stat[w * R + row]);
-      const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = fast_exp2(stat[w * R + row] - ref);
-        L = fmaf(stat[(kWarps + w) * R + row], f, L);
-        acc = fmaf(part[(w * R + row) * D + col], f, acc);
-      }
-      a.part_out[((size_t)slot * R + row) * D + col] = acc;
-      if (col == 0) a.part_stat[(size_t)slot * R + row] = make_float2(M, L);
-    }
+    leave_partial<D, kThreads, R, D, kWarps>(a, u * blocks + rb + blockIdx.x, min(R, a.rows - rb * R), part, stat, stat + kWarps * R, kWarps,
+                                             tid, [] { __syncthreads(); });
     at += t1 - t0;
     if (t1 == tiles && rb + 1 == blocks) {
       unit_at += tiles * blocks;
@@ -197,7 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant_
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_trigger();
   pdl_wait();
-  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTileKeys, 1, gridDim.x, 1, nullptr);
+  const WorkStart ws = find_work(a, 6, 1, nullptr);
   const int hi = ws.hi;
   int u = ws.unit, at = ws.lo, unit_at = ws.before;
 #pragma unroll 1
@@ -263,14 +248,14 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant_
 
 template <int D, int R>
 cudaError_t launch_one(const AttendArgs& a, cudaStream_t st) {
-  const cudaError_t e = allow_smem<attend_simt<D, R>>(Shape<D>::kSmem(R));
-  return e != cudaSuccess ? e : launch_pdl(attend_simt<D, R>, dim3(a.ctas), dim3(kThreads), Shape<D>::kSmem(R), st, a);
+  const cudaError_t e = allow_smem<attend_simt<D, R>>(Shape<D>::template kSmem<R>);
+  return e != cudaSuccess ? e : launch_pdl(attend_simt<D, R>, dim3(a.ctas), dim3(kThreads), Shape<D>::template kSmem<R>, st, a);
 }
 template <int D>
-cudaError_t launch_weigh(const AttendArgs& a, const unsigned long long* accepted, int ctas, cudaStream_t st) {
+cudaError_t launch_weigh(const AttendArgs& a, const unsigned long long* accepted, cudaStream_t st) {
   constexpr int smem = (kTileKeys * Shape<D>::kRow + 8 * D) * 4;
   static_assert(smem <= 48 * 1024, "no limit to raise");
-  return launch_pdl(weigh_simt<D>, dim3(ctas), dim3(kThreads), smem, st, a, accepted);
+  return launch_pdl(weigh_simt<D>, dim3(a.ctas), dim3(kThreads), smem, st, a, accepted);
 }
 
 }  // namespace
@@ -280,7 +265,7 @@ cudaError_t launch_attend_simt(const Ctx& ctx, const AttendArgs& a, const Attend
   return p.rb == 4 ? launch_one<64, 4>(a, st) : launch_one<64, 8>(a, st);
 }
 cudaError_t launch_weigh_fp32(const Ctx& ctx, const AttendArgs& a, const unsigned long long* accepted, cudaStream_t st) {
-  return ctx.cfg.head_dim == 128 ? launch_weigh<128>(a, accepted, 4 * ctx.sm_count, st) : launch_weigh<64>(a, accepted, 4 * ctx.sm_count, st);
+  return ctx.cfg.head_dim == 128 ? launch_weigh<128>(a, accepted, st) : launch_weigh<64>(a, accepted, st);
 }
 
 }  // namespace skv

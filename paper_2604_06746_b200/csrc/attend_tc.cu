@@ -23,11 +23,11 @@ constexpr float kSlack = 8.f;
 
 struct CacheMaps { CUtensorMap k, v; };
 
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2, int c3, uint64_t policy) {
+__device__ __forceinline__ void tma_load_slots(uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot, int head, int seq, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
-      "[%0], [%1, {%3, %4, %5, %6}], [%2], %7;"
-      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "l"(policy) : "memory");
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%3, %4, %3, %5, %6}], [%2], %7;"
+      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(0), "r"(slot), "r"(head), "r"(seq), "l"(policy) : "memory");
 }
 // An N-major operand of 64-element blocks of 128-byte rows (128-byte swizzle): blocks kTile rows apart, 8-row groups 1024 bytes.
 __device__ __forceinline__ uint64_t smem_desc_n(uint32_t addr) {
@@ -171,8 +171,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     tc_fence_before();
   }
+  __syncthreads();
   pdl_wait();
-  const WorkStart ws = find_work<kThreads>(a.c, a.n_new, kTile, blocks, a.ctas, a.least, blockIdx.x == 0 ? a.unit_start : nullptr);   // (barriers inside)
+  const WorkStart ws = find_work(a, 7, blocks, blockIdx.x == 0 ? a.unit_start : nullptr);
   tc_fence_after();
   const uint32_t tmem = *tmem_at;
   const bool work = ws.lo < ws.hi;
@@ -198,9 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
           if (n >= NU && !(ok = mbar_wait_producer(empty(st), (n / NU - 1) & 1, abort_flag, kWaitCycles))) break;
           if (lane == 0) {
             mbar_expect_tx(full(st), S::kUnit);
-#pragma unroll
-            for (int c = 0; c < D / 64; ++c)
-              tma_load_4d(base + kRing + st * S::kUnit + c * kTile * 128, kv ? &maps.v : &maps.k, full(st), c * 64, t * kTile, g, b, hint);
+            tma_load_slots(base + kRing + st * S::kUnit, kv ? &maps.v : &maps.k, full(st), t * kTile, g, b, hint);
           }
           if (S::kPos) {
             // positions go with V: its place is held until the softmax has read them

@@ -256,11 +256,11 @@ bool tc_encode3(const Ctx& ctx, CUtensorMap* m, const void* base, cuuint64_t d1,
 bool tc_encode_cache(const Ctx& ctx, CUtensorMap* m, const void* base, int slots, int heads, int batch, long long s_token,
                      long long s_head, long long s_batch, int box_rows) {
   // (a stride that nothing steps over still has to be one)
-  const cuuint64_t dims[4] = {(cuuint64_t)ctx.cfg.head_dim, (cuuint64_t)slots, (cuuint64_t)heads, (cuuint64_t)batch};
   const cuuint64_t row = (cuuint64_t)ctx.cfg.head_dim * 2;
-  const cuuint64_t strides[3] = {slots > 1 ? (cuuint64_t)s_token : row, heads > 1 ? (cuuint64_t)s_head : row, batch > 1 ? (cuuint64_t)s_batch : row};
-  const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, estr[4] = {1, 1, 1, 1};
-  return ((TcState*)ctx.tc)->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box,
+  const cuuint64_t dims[5] = {64, (cuuint64_t)slots, (cuuint64_t)ctx.cfg.head_dim / 64, (cuuint64_t)heads, (cuuint64_t)batch};
+  const cuuint64_t strides[4] = {slots > 1 ? (cuuint64_t)s_token : row, 128, heads > 1 ? (cuuint64_t)s_head : row, batch > 1 ? (cuuint64_t)s_batch : row};
+  const cuuint32_t box[5] = {64, (cuuint32_t)box_rows, (cuuint32_t)ctx.cfg.head_dim / 64, 1, 1}, estr[5] = {1, 1, 1, 1, 1};
+  return ((TcState*)ctx.tc)->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box,
                                     estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

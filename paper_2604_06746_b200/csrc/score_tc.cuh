@@ -1352,7 +1352,8 @@ cudaError_t tc_launch(const TcParams<MAXP>& p, int grid, int device, cudaStream_
 // boxes of b1 x b2 rows.
 bool tc_encode3(const Ctx& ctx, CUtensorMap* m, const void* base, cuuint64_t d1, cuuint64_t d2, cuuint64_t s1,
                 cuuint64_t s2, cuuint32_t b1, cuuint32_t b2);
-// The same of a compacted cache's K or V: slots, heads and sequences of the strides given (bytes), boxes of box_rows slots.
+// A map of a compacted cache's K or V: slots, heads and sequences of the strides given (bytes); a box is box_rows whole slots, 64
+// columns after 64 columns (coordinates 0, slot, 0, head, sequence).
 bool tc_encode_cache(const Ctx& ctx, CUtensorMap* m, const void* base, int slots, int heads, int batch, long long s_token,
                      long long s_head, long long s_batch, int box_rows);
 
