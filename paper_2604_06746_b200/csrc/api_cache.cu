@@ -45,7 +45,7 @@ AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, int capacity) {
   if (batch < 1 || capacity < 1 || capacity > 1 << 30 || n_new < 0 || n_new > capacity) return false;
   const long long units = (long long)batch * cfg.n_kv_heads, rows = (long long)cfg.n_q_heads / cfg.n_kv_heads * std::max(1, n_new);
-  return units * rows <= 0x3fffffffll && units * ((rows + 3) / 4) <= 0x7fffffffll / (capacity / 64 + 1);
+  return units * rows <= 0x3fffffffll && units * ((rows + 3) / 4) <= 0x7fffffffll / (capacity / 64 + 1 + kOver);
 }
 bool strides_ok(int elem, long long a, long long b, long long c) { return (a * elem) % 16 == 0 && (b * elem) % 16 == 0 && (c * elem) % 16 == 0; }
 

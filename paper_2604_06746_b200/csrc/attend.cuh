@@ -2,8 +2,10 @@
 //
 // A unit is (sequence, KV head) u = b H_kv + g, with lengths[u] + n_new keys (the new tokens are the last ones) and rows
 // r = i G + h, new token i and head h of the group.  An item is a unit's block of up to RB rows over all of its keys; items
-// follow one another unit after unit, and their key tiles form one sequence of W tiles.  C CTAs take runs of it whose lengths
-// differ by one tile at most: every CTA reads equally much whatever the lengths, which only the device knows.  What a CTA has of
+// follow one another unit after unit, and their key tiles, behind kOver places for what an item costs beside them, form one sequence of
+// W places.  C CTAs take runs of it whose lengths differ by one place at most: every CTA has equally much to do whatever the lengths,
+// which only the device knows.  (Without the places for the items' own cost 16 sequences of 1 to 5003 tokens took 45 us: a CTA that
+// got eight KV heads of one token was busy for 38, the others for 20.)  What a CTA has of
 // an item it leaves as a partial (row references, sums, unscaled output) in slot item + CTA, which no other pair has, so that an
 // item's partials lie side by side; attend_finish() merges them in that order: results do not depend on timing.  (Merged by the CTA
 // that leaves an item's last partial, which spares the launch, 1 x 1024 keys took 16.8 us instead of 13.4: all of its work then stands
@@ -16,6 +18,7 @@
 
 namespace skv {
 
+constexpr int kOver = 4;
 constexpr int kMaxNew = STRUCTKV_MAX_NEW;   // new tokens of a sequence: a tree's masks are words of 64 bits
 
 // The cache as the kernels see it; strides in bytes, words [batch, H_kv, capacity], lengths [batch, H_kv].
@@ -58,7 +61,7 @@ struct AttendArgs {
   bool accumulate;                     // (n_new = 1)
   NewRows fresh;                       // the new tokens' rows, where the kernel appends them; k NULL: they are in the cache
   // workspace
-  int* unit_start;                     // [units + 1] tiles before a unit, of one block of rows
+  int* unit_start;                     // [units + 1] places before a unit, of one block of rows
   float2* part_stat;                   // [slot][RB] reference (bits) and sum
   float* part_out;                     // [slot][RB][d]
   float* logits;                       // [units][capacity][group] in bits (accumulate)
@@ -126,7 +129,7 @@ __device__ __forceinline__ void append_rows(const CacheView& c, const NewRows& r
 
 __device__ __forceinline__ int quotient(int n, Div d) { return (int)((__umulhi((unsigned)n, d.mul) + (unsigned)n) >> d.shift); }
 
-// How W tiles are shared out: CTA c has tiles [first(c), first(c + 1)), at least 2^least of them if there are as many.
+// How W places are shared out: CTA c has [first(c), first(c + 1)), at least 2^least of them if there are as many.
 struct Shares { int W, C, each, more; };
 __device__ __forceinline__ Shares shares_of(int W, int ctas, Div by_ctas, int least) {
   if (W >> least >= ctas) {
@@ -149,15 +152,18 @@ __device__ __forceinline__ int cta_of(const Shares& s, int x) {
   return (low ? 0 : s.more) + q;
 }
 
+__device__ __forceinline__ int tiles_of(int keys, int tile_shift) { return (keys + (1 << tile_shift) - 1) >> tile_shift; }
+__device__ __forceinline__ int places_of(int keys, int tile_shift) { return keys == 0 ? 0 : tiles_of(keys, tile_shift) + kOver; }
+
 // First partial of an item and how many it has; each: partials a CTA leaves of an item.
 struct Parts { int first, count; };
-__device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, int tiles, int each) {
-  const int c0 = cta_of(s, start), c1 = cta_of(s, start + tiles - 1);
+__device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, int places, int each) {
+  const int c0 = cta_of(s, start + kOver), c1 = cta_of(s, start + places - 1);
   return {(item + c0) * each, (c1 - c0 + 1) * each};
 }
 
-// A CTA's run of tiles, and the unit that its first tile is in: keys, tiles of one block of rows before it.
-struct WorkStart { int lo, hi, unit, before, keys; Shares all; };
+// A CTA's run of places, and the unit that its first one is in: keys, places of one block of rows before it.
+struct WorkStart { int lo, hi, unit, before, keys; };
 
 // By the whole block, every warp for itself; a lane has `kLaneUnits` neighbouring units of a sweep.  save: unit_start.
 constexpr int kLaneUnits = 4;
@@ -172,7 +178,7 @@ __device__ __forceinline__ WorkStart find_work(const AttendArgs& a, int tile_shi
 #pragma unroll
     for (int e = 0; e < kLaneUnits; ++e) keys[e] = u0 + lane * kLaneUnits + e < c.units ? keys_of(c, keys[e], a.n_new) : 0;
 #pragma unroll
-    for (int e = 0; e < kLaneUnits; ++e) sum += (keys[e] + (1 << tile_shift) - 1) >> tile_shift;
+    for (int e = 0; e < kLaneUnits; ++e) sum += places_of(keys[e], tile_shift);
     incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -191,16 +197,16 @@ __device__ __forceinline__ WorkStart find_work(const AttendArgs& a, int tile_shi
       for (int e = 0; e < kLaneUnits; ++e) {
         const int u = u0 + lane * kLaneUnits + e;
         if (u < c.units) save[u] = at;
-        at += (keys[e] + (1 << tile_shift) - 1) >> tile_shift;
+        at += places_of(keys[e], tile_shift);
       }
     }
     total += __shfl_sync(0xffffffffu, incl, 31);
   }
   if (save && threadIdx.x == 0) save[c.units] = total;
   WorkStart w{};
-  w.all = shares_of(total * blocks, a.ctas, a.by_ctas, a.least);
-  w.lo = first_of(w.all, blockIdx.x);
-  w.hi = first_of(w.all, blockIdx.x + 1);
+  const Shares all = shares_of(total * blocks, a.ctas, a.by_ctas, a.least);
+  w.lo = first_of(all, blockIdx.x);
+  w.hi = first_of(all, blockIdx.x + 1);
   if (w.lo >= w.hi) return w;
   int before = 0;
 #pragma unroll 1
@@ -212,7 +218,7 @@ __device__ __forceinline__ WorkStart find_work(const AttendArgs& a, int tile_shi
       int at = before + __shfl_sync(0xffffffffu, incl - sum, from);
 #pragma unroll
       for (int e = 0; e < kLaneUnits; ++e) {
-        const int k = __shfl_sync(0xffffffffu, keys[e], from), t = (k + (1 << tile_shift) - 1) >> tile_shift;
+        const int k = __shfl_sync(0xffffffffu, keys[e], from), t = places_of(k, tile_shift);
         if (at * blocks <= w.lo && w.lo < (at + t) * blocks) {
           w.unit = u0 + from * kLaneUnits + e;
           w.before = at;
@@ -225,6 +231,36 @@ __device__ __forceinline__ WorkStart find_work(const AttendArgs& a, int tile_shi
     before += __shfl_sync(0xffffffffu, incl, 31);
   }
   return w;
+}
+
+// A CTA's run, item by item: tiles [t0, t1) of an item's.  (None left: t1 = 0.)
+struct Segments {
+  int u, rb, t0, t1, keys, tiles;
+  int at, hi;                                                    // place where the item begins, where the run ends
+};
+__device__ __forceinline__ void next_segment(Segments& s, const AttendArgs& a, int tile_shift, int blocks) {
+  s.at += s.tiles + kOver;
+  s.t0 = s.t1 = 0;
+  if (s.at + kOver >= s.hi) return;
+  if (++s.rb == blocks) {
+    s.rb = 0;
+    do ++s.u;
+    while ((s.keys = unit_keys(a.c, s.u, a.n_new)) == 0 && s.u < a.c.units - 1);
+    s.tiles = tiles_of(s.keys, tile_shift);
+  }
+  s.t1 = min(s.tiles, s.hi - s.at - kOver);
+}
+__device__ __forceinline__ Segments first_segment(const AttendArgs& a, const WorkStart& w, int tile_shift, int blocks) {
+  Segments s{w.unit, 0, 0, 0, w.keys, tiles_of(w.keys, tile_shift), w.before * blocks, w.hi};
+  if (w.lo >= w.hi) return s;
+  while (w.lo >= s.at + s.tiles + kOver) {
+    s.at += s.tiles + kOver;
+    ++s.rb;
+  }
+  s.t0 = max(0, w.lo - s.at - kOver);
+  s.t1 = max(0, min(s.tiles, w.hi - s.at - kOver));
+  if (s.t1 <= s.t0) next_segment(s, a, tile_shift, blocks);
+  return s;
 }
 
 // cap tanh(scale s / cap) in bits: for small arguments the odd series, else 1 - 2 / (e^2y + 1), both to fp32's last bits.

@@ -44,15 +44,16 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
   __shared__ float lse[kThreads];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rb_rows = 1 << rb_shift;
   const int blocks = (a.rows + rb_rows - 1) >> rb_shift, all_rows = a.c.units * a.rows;
-  int i = blockIdx.x * (kThreads / 32) + warp;
+  // (rows from the last block on, weights from the first one on: where both are few they are beside one another)
+  int i = (gridDim.x - 1 - blockIdx.x) * (kThreads / 32) + warp;
   const int u_row = quotient(min(i, all_rows - 1), a.by_rows), u_mine = min(tid, a.c.units - 1);
   pdl_trigger();
   pdl_wait();
   // (loads that depend on nothing go together: the total, the first row's unit, the units among which this block's run begins)
-  const int W1 = a.unit_start[a.c.units];                         // tiles of one block of rows each
-  int start = a.unit_start[u_row], tiles = a.unit_start[u_row + 1];
+  const int W1 = a.unit_start[a.c.units];                         // places of one block of rows each
+  int start = a.unit_start[u_row], places = a.unit_start[u_row + 1];
   const int start0 = a.unit_start[u_mine], end0 = a.unit_start[u_mine + 1], keys0 = a.c.lengths[u_mine] + a.n_new;
-  tiles -= start;
+  places -= start;
   if (W1 == 0) return;
   const Shares sh = shares_of(W1 * blocks, a.ctas, a.by_ctas, a.least);
 #pragma unroll 1
@@ -60,10 +61,10 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
     const int u = quotient(i, a.by_rows), r = i - u * a.rows, rb = r >> rb_shift, row = r & (rb_rows - 1);
     if (i != at) {
       start = a.unit_start[u];
-      tiles = a.unit_start[u + 1] - start;
+      places = a.unit_start[u + 1] - start;
     }
-    if (tiles == 0) continue;
-    const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles, each);
+    if (places == 0) continue;
+    const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * places, places, each);
     const float* from = a.part_out + ((size_t)p.first * rb_rows + row) * D + lane * DL;
     Cols<DL> x[kAhead];
 #pragma unroll
@@ -123,13 +124,14 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
   __syncthreads();
   int u = hit[0], keys = hit[3];
   start = hit[1];
-  tiles = hit[2];
+  places = hit[2];
 #pragma unroll 1
   for (int at = lo; at < hi;) {
-    const int t0 = at - start, t1 = min(tiles, t0 + (hi - at)), end = min(keys, t1 << tile_shift);
+    const int next = min(hi, start + places), t0 = max(0, at - start - kOver), t1 = max(0, next - start - kOver);
+    const int end = min(keys, t1 << tile_shift);
     float* const w = a.c.weights + (size_t)u * a.c.capacity;
 #pragma unroll 1
-    for (int h0 = 0; h0 < a.group; h0 += kThreads) {              // (one round, but for groups of more than 128 heads)
+    for (int h0 = 0; t0 < t1 && h0 < a.group; h0 += kThreads) {              // (one round, but for groups of more than 128 heads)
       const int heads = min(kThreads, a.group - h0);
       // the commonest group: four keys' loads in flight, the first ones while the references are on their way
       float4 x[4];
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
 #pragma unroll 1
       for (int h = warp; h < heads; h += kThreads / 32) {
         const int r = h0 + h, rb = r >> rb_shift;
-        const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * tiles, tiles, each);
+        const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * places, places, each);
         float2 mine;
         const float x = bits_of(merged(a.part_stat, p, rb_rows, r & (rb_rows - 1), lane, mine));
         if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
@@ -177,13 +179,13 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
         }
       }
     }
-    at += t1 - t0;
+    at = next;
     if (at < hi) {
       do {
         ++u;
         start = a.unit_start[u];
-        tiles = a.unit_start[u + 1] - start;
-      } while (tiles == 0);
+        places = a.unit_start[u + 1] - start;
+      } while (places == 0);
       keys = a.c.lengths[u] + a.n_new;
     }
   }

@@ -59,32 +59,7 @@ __device__ __forceinline__ uint32_t tile_at(int row, int chunk) {
   return (chunk >> 3) * (kTileKeys * 128) + row * 128 + (((chunk ^ row) & 7) << 4);
 }
 
-// Where a CTA is in its run of tiles.
-struct Cursor { int u, rb, t, tiles, keys; };
-__device__ __forceinline__ void enter(Cursor& c, const CacheView& cache, int n_new, int tile) {
-  c.keys = c.u < cache.units ? unit_keys(cache, c.u, n_new) : 0;
-  while (c.keys == 0 && c.u < cache.units - 1) c.keys = unit_keys(cache, ++c.u, n_new);
-  c.tiles = (c.keys + tile - 1) / tile;
-}
-__device__ __forceinline__ void advance(Cursor& c, const CacheView& cache, int n_new, int tile, int blocks) {
-  if (++c.t < c.tiles) return;
-  c.t = 0;
-  if (++c.rb < blocks) return;
-  c.rb = 0;
-  ++c.u;
-  enter(c, cache, n_new, tile);
-}
-
 struct CacheMaps { CUtensorMap k, v; };
-
-// Bounded wait of a warp for a count in shared memory to grow above n.
-__device__ __forceinline__ bool wait_above(const volatile int* count, int n, volatile int* abort_flag) {
-  bool ok = *count > n;
-  for (const long long t0 = clock64(); !ok && !*abort_flag; ok = *count > n)
-    if ((unsigned long long)(clock64() - t0) > kWaitCycles) *abort_flag = 1;
-  __threadfence_block();
-  return __all_sync(0xffffffffu, ok);
-}
 
 // NR blocks of 8 rows; four warps along a tile's keys, NG groups of these.
 template <int D, int NR, int NG>
@@ -111,7 +86,6 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
   float* const stat = outs + S::kSets * RB * S::kRow;           // [2][RB][set]
   const uint32_t bars = smem_u32(stat + 2 * S::kSets * RB);     // full [ST], empty [ST]
   volatile int* const abort_flag = (volatile int*)(stat + 2 * S::kSets * RB) + 4 * ST;
-  volatile int* const appended = abort_flag + 1;                // tiles of the run up to which new rows are in the cache
   auto full = [&](int st) { return bars + 8 * st; };
   auto empty = [&](int st) { return bars + 8 * (ST + st); };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -123,7 +97,6 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
       mbar_init(empty(i), 4);
     }
     *abort_flag = 0;
-    *appended = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.v) : "memory");
@@ -131,43 +104,41 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
   __syncthreads();
   pdl_wait();
   const WorkStart ws = find_work(a, 6, blocks, blockIdx.x == 0 ? a.unit_start : nullptr);
-  if (ws.lo >= ws.hi) return;
-  const int run = ws.hi - ws.lo;
-  Cursor cur{ws.unit, 0, 0, (ws.keys + kTileKeys - 1) / kTileKeys, ws.keys};
-  cur.t = ws.lo - ws.before * blocks;
-  if (blocks > 1) {
-    cur.rb = cur.t / cur.tiles;
-    cur.t -= cur.rb * cur.tiles;
-  }
+  Segments sg = first_segment(a, ws, 6, blocks);
+  if (sg.t1 == 0) return;
 
   if (warp == 0) {
     // the ring's producer
     const uint64_t hint = blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
     int st = 0, n = 0;
+    bool ok = true;
 #pragma unroll 1
-    for (; n < run; ++n) {
-      const int b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv;
-      const uint32_t to = base + st * S::kStage;
-      if (n >= ST && !mbar_wait_producer(empty(st), (n / ST - 1) & 1, abort_flag, kWaitCycles)) break;
-      if (a.fresh.k && (cur.t + 1) * kTileKeys > cur.keys - a.n_new && !wait_above(appended, n, abort_flag)) break;
-      if (lane == 0) {
-        mbar_expect_tx(full(st), 2 * S::kTileBytes);
-        tma_load_slots(to, &maps.k, full(st), cur.t * kTileKeys, g, b, hint);
-        tma_load_slots(to + S::kTileBytes, &maps.v, full(st), cur.t * kTileKeys, g, b, hint);
-      }
-      if (OPT) {
-        if (a.slopes) {
-          const int* const pos = a.c.positions + (size_t)cur.u * a.c.capacity;
-#pragma unroll
-          for (int i = lane; i < kTileKeys; i += 32) {
-            const int j = cur.t * kTileKeys + i;
-            cp4(to + S::kPosOff + i * 4, pos + (j < cur.keys ? j : 0), j < cur.keys);
-          }
+    for (; sg.t1 && ok; next_segment(sg, a, 6, blocks)) {
+      const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv;
+#pragma unroll 1
+      for (int t = sg.t0; t < sg.t1; ++t, ++n) {
+        const uint32_t to = base + st * S::kStage;
+        if (n >= ST && !(ok = mbar_wait_producer(empty(st), (n / ST - 1) & 1, abort_flag, kWaitCycles))) break;
+        if (lane == 0) {
+          mbar_expect_tx(full(st), 2 * S::kTileBytes);
+          tma_load_slots(to, &maps.k, full(st), t * kTileKeys, g, b, hint);
+          tma_load_slots(to + S::kTileBytes, &maps.v, full(st), t * kTileKeys, g, b, hint);
         }
-        cp_arrive(full(st));
+        if (OPT) {
+          if (a.slopes) {
+            const int* const pos = a.c.positions + (size_t)sg.u * a.c.capacity;
+            const int n_old = sg.keys - a.n_new;
+#pragma unroll
+            for (int i = lane; i < kTileKeys; i += 32) {
+              const int j = t * kTileKeys + i;
+              const bool is_new = a.fresh.k && j >= n_old && j < sg.keys;      // (their places in the cache are being written)
+              cp4(to + S::kPosOff + i * 4, is_new ? a.fresh.positions + (size_t)b * a.n_new + j - n_old : pos + (j < sg.keys ? j : 0), j < sg.keys);
+            }
+          }
+          cp_arrive(full(st));
+        }
+        if (++st == ST) st = 0;
       }
-      if (++st == ST) st = 0;
-      if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
     }
     if (*abort_flag) {
       // copies in flight end before the block does
@@ -177,20 +148,13 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
     return;
   }
   if (warp == 1) {
-    // New rows go into the cache ahead of the tiles that have them, which TMA reads.  (Row blocks of a unit in other CTAs write the
-    // same bytes.)
+    // New rows go into the cache; nobody here waits for that (patch() below).  Row blocks of a unit in other CTAs write the same bytes.
     if (!a.fresh.k) return;
 #pragma unroll 1
-    for (int n = 0; n < run; ++n) {
-      if ((cur.t + 1) * kTileKeys > cur.keys - a.n_new) {
-        const int b = quotient(cur.u, a.by_kv);
-        append_rows(a.c, a.fresh, a.n_new, cur.u, b, cur.u - b * a.c.n_kv, cur.keys - a.n_new, lane);
-        asm volatile("fence.proxy.async;" ::: "memory");
-        __syncwarp();
-        __threadfence_block();
-        if (lane == 0) *appended = n + 1;
-      }
-      if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
+    for (; sg.t1; next_segment(sg, a, 6, blocks)) {
+      if (sg.t1 * kTileKeys <= sg.keys - a.n_new) continue;
+      const int b = quotient(sg.u, a.by_kv);
+      append_rows(a.c, a.fresh, a.n_new, sg.u, b, sg.u - b * a.c.n_kv, sg.keys - a.n_new, lane);
     }
     return;
   }
@@ -203,24 +167,26 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
   float slope2[NR][2];
   int place[NR][2];
   bool fresh = true;                                            // nothing of this segment yet
-  int seg = 0;                                                  // first tile of the segment in the run
+  int n = 0, st = 0;
 #pragma unroll 1
-  for (int n = 0, st = 0; n < run; ++n, st = st + 1 == ST ? 0 : st + 1) {
-    const int first_row = cur.rb * RB + 2 * t4;                 // row of (block i, x): first_row + 8 i + x
-    if (n % NG == grp) {
+  for (; sg.t1; next_segment(sg, a, 6, blocks)) {
+    const int first_row = sg.rb * RB + 2 * t4;                  // row of (block i, x): first_row + 8 i + x
+    const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv, n_old = sg.keys - a.n_new, seg = n;
+#pragma unroll 1
+    for (int t = sg.t0; t < sg.t1; ++t, ++n, st = st + 1 == ST ? 0 : st + 1) {
+      if (n % NG != grp) continue;
       const uint32_t from = base + st * S::kStage;
       const unsigned char* const here = sm + st * S::kStage;
       if (fresh) {
         // a segment begins: its rows, while the tile is on its way
         fresh = false;
-        const int b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) { m[i][x] = -INFINITY; l[i][x] = 0.f; }
 #pragma unroll
           for (int k = 0; k < KK; ++k) o[i][k][0] = o[i][k][1] = o[i][k][2] = o[i][k][3] = 0.f;
-          const int r = cur.rb * RB + 8 * i + g8;
+          const int r = sg.rb * RB + 8 * i + g8;
           const bool is = r < a.rows;
           const int tok = is ? quotient(r, a.by_group) : 0, h = is ? r - tok * a.group : 0;
           const char* const q = a.q + (size_t)b * a.q_batch + (size_t)tok * a.q_token + (size_t)(g * a.group + h) * a.q_head + t4 * 4;
@@ -234,12 +200,29 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
           for (int i = 0; i < NR; ++i)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              const RowOptions ro = row_options(a, cur.u, min(first_row + 8 * i + x, a.rows - 1));
+              const RowOptions ro = row_options(a, sg.u, min(first_row + 8 * i + x, a.rows - 1));
               slope2[i][x] = ro.slope2;
               place[i][x] = ro.position;
             }
       }
+      const int j0 = t * kTileKeys + kw * 16;
+      const bool tail = j0 + 16 > n_old;
       mbar_wait(full(st), (n / ST) & 1, abort_flag);            // (on expiry the numbers are void, the control flow goes on)
+      if (tail && a.fresh.k) {
+        // patch: new tokens among this warp's 16 keys, whose rows TMA did not find in the cache
+#pragma unroll 1
+        for (int i = max(0, j0 - n_old); i < min(a.n_new, j0 + 16 - n_old); ++i) {
+          const size_t from = (size_t)b * a.fresh.s_batch + (size_t)i * a.fresh.s_token + (size_t)g * a.fresh.s_head;
+          const int row = n_old + i - t * kTileKeys;
+          for (int e = lane; e < 2 * CH; e += 32) {
+            const bool is_v = e >= CH;
+            const int ch = is_v ? e - CH : e;
+            *(uint4*)(sm + st * S::kStage + (is_v ? S::kTileBytes : 0) + tile_at(row, ch)) = *(const uint4*)((is_v ? a.fresh.v : a.fresh.k) + from + ch * 16);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the place's next tile comes by TMA)
+        __syncwarp();
+      }
       // products: two chains where a warp has one block of rows
       constexpr int CHAINS = NR == 1 ? 2 : 1;
       float acc[CHAINS][NR][4];
@@ -260,8 +243,6 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[i][e] = CHAINS == 2 ? acc[0][i][e] + acc[CHAINS - 1][i][e] : acc[0][i][e];
       // x in bits
-      const int n_old = cur.keys - a.n_new, j0 = cur.t * kTileKeys + kw * 16;
-      const bool tail = j0 + 16 > n_old;
       if (OPT) {
         int kp[2] = {0, 0};
         if (a.slopes) { kp[0] = ((const int*)(here + S::kPosOff))[kw * 16 + g8]; kp[1] = ((const int*)(here + S::kPosOff))[kw * 16 + g8 + 8]; }
@@ -284,22 +265,22 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
         for (int i = 0; i < NR; ++i)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const unsigned long long seen = row_seen(a, cur.u, min(first_row + 8 * i + x, a.rows - 1));
+            const unsigned long long seen = row_seen(a, sg.u, min(first_row + 8 * i + x, a.rows - 1));
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
               const int j = j0 + g8 + 8 * y;
-              if (j >= cur.keys || !sees(seen, j, n_old)) s[i][2 * y + x] = -INFINITY;
+              if (j >= sg.keys || !sees(seen, j, n_old)) s[i][2 * y + x] = -INFINITY;
             }
           }
       }
       if (a.accumulate) {
-        float* const to = a.logits + ((size_t)cur.u * a.c.capacity + j0 + g8) * a.group;
+        float* const to = a.logits + ((size_t)sg.u * a.c.capacity + j0 + g8) * a.group;
 #pragma unroll
         for (int i = 0; i < NR; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = first_row + 8 * i + (e & 1);
-            if (r < a.rows && j0 + g8 + 8 * (e >> 1) < cur.keys) to[8 * (e >> 1) * a.group + r] = s[i][e];
+            if (r < a.rows && j0 + g8 + 8 * (e >> 1) < sg.keys) to[8 * (e >> 1) * a.group + r] = s[i][e];
           }
       }
       // references
@@ -384,10 +365,10 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
       if (lane == 0) mbar_arrive(empty(st));
     }
 
-    if (cur.t + 1 == cur.tiles || n + 1 == run) {
+    {
       // the segment ends: its warps' outputs, each against its own reference, then their sum against a common one.  Sets (a group's
       // quarter of the keys) are counted from the group that took the segment's first tile.
-      const int sets = min(S::kSets, (n + 1 - seg) * 4), my = ((grp + NG - seg % NG) % NG) * 4 + kw;
+      const int sets = min(S::kSets, (n - seg) * 4), my = ((grp + NG - seg % NG) % NG) * 4 + kw;
       if (my < sets) {
 #pragma unroll
         for (int i = 0; i < NR; ++i)
@@ -405,13 +386,11 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
             for (int k = 0; k < KK; ++k) { to[k * 16] = o[i][k][x]; to[k * 16 + 8] = o[i][k][2 + x]; }
           }
       }
-      leave_partial<D, S::kWarps * 32, RB, S::kRow, S::kSets>(a, cur.u * blocks + cur.rb + blockIdx.x, min(RB, a.rows - cur.rb * RB), outs, stat,
+      leave_partial<D, S::kWarps * 32, RB, S::kRow, S::kSets>(a, sg.u * blocks + sg.rb + blockIdx.x, min(RB, a.rows - sg.rb * RB), outs, stat,
                                                               stat + RB * S::kSets, sets, tid - 64, sync);
-      if (n + 1 < run) sync();
+      sync();
       fresh = true;
-      seg = n + 1;
     }
-    if (n + 1 < run) advance(cur, a.c, a.n_new, kTileKeys, blocks);
   }
 }
 
@@ -453,9 +432,8 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
   __syncthreads();
   pdl_wait();
   const WorkStart ws = find_work(a, 6, 1, nullptr);
-  if (ws.lo >= ws.hi) return;
-  const int run = ws.hi - ws.lo;
-  Cursor cur{ws.unit, 0, ws.lo - ws.before, (ws.keys + kTileKeys - 1) / kTileKeys, ws.keys};
+  Segments sg = first_segment(a, ws, 6, 1);
+  if (sg.t1 == 0) return;
   // rows of the accepted tokens of a unit, and how often its tiles are gone through
   auto taken_of = [&](int u) { return accepted[quotient(u, a.by_kv)] & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1); };
   auto rounds_of = [&](int rows) { return rows <= kWeighRows ? 1 : (rows + kWeighRows - 1) / kWeighRows; };
@@ -465,9 +443,9 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
     int n = 0;
     bool ok = true;
 #pragma unroll 1
-    for (int left = run; left > 0 && ok;) {
-      const int t0 = cur.t, t1 = min(cur.tiles, t0 + left), b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv;
-      const int rounds = rounds_of(__popcll(taken_of(cur.u)) * a.group);
+    for (; sg.t1 && ok; next_segment(sg, a, 6, 1)) {
+      const int t0 = sg.t0, t1 = sg.t1, b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv;
+      const int rounds = rounds_of(__popcll(taken_of(sg.u)) * a.group);
       for (int i = 0; i < rounds * (t1 - t0); ++i, ++n) {
         const int st = n % ST, t = t0 + i % (t1 - t0);
         const uint32_t to = base + st * kStage;
@@ -477,18 +455,15 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
           tma_load_slots(to, &maps.k, full(st), t * kTileKeys, g, b, rounds == 1 ? policy : again);
         }
         if (OPT && a.slopes) {
-          const int* const pos = a.c.positions + (size_t)cur.u * a.c.capacity;
+          const int* const pos = a.c.positions + (size_t)sg.u * a.c.capacity;
 #pragma unroll
           for (int e = lane; e < kTileKeys; e += 32) {
             const int j = t * kTileKeys + e;
-            cp4(to + kTileBytes + e * 4, pos + (j < cur.keys ? j : 0), j < cur.keys);
+            cp4(to + kTileBytes + e * 4, pos + (j < sg.keys ? j : 0), j < sg.keys);
           }
         }
         cp_arrive(full(st));
       }
-      left -= t1 - t0;
-      cur.t = t1 - 1;
-      if (left > 0) advance(cur, a.c, a.n_new, kTileKeys, 1);
     }
     if (*abort_flag) {
       for (int i = max(0, n - ST); i < n; ++i) mbar_drain(full(i % ST), (i / ST) & 1, abort_flag);
@@ -501,12 +476,12 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
   auto sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kWeighWarps * 32) : "memory"); };
   int n = 0;
 #pragma unroll 1
-  for (int left = run; left > 0;) {                               // a unit's tiles of this CTA
-    const int t0 = cur.t, t1 = min(cur.tiles, t0 + left);
-    const int b = quotient(cur.u, a.by_kv), g = cur.u - b * a.c.n_kv, n_old = cur.keys - a.n_new;
-    const unsigned long long taken = taken_of(cur.u);
+  for (; sg.t1; next_segment(sg, a, 6, 1)) {                      // a unit's tiles of this CTA
+    const int t0 = sg.t0, t1 = sg.t1;
+    const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv, n_old = sg.keys - a.n_new;
+    const unsigned long long taken = taken_of(sg.u);
     const int rows = __popcll(taken) * a.group, rounds = rounds_of(rows);
-    float* const w = a.c.weights + (size_t)cur.u * a.c.capacity;
+    float* const w = a.c.weights + (size_t)sg.u * a.c.capacity;
 #pragma unroll 1
     for (int round = 0; round < rounds; ++round) {
       const int r0 = round * kWeighRows, n_rows = min(kWeighRows, rows - r0), n_blocks = (n_rows + 7) / 8;
@@ -525,7 +500,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
           if (ch == 0) {
             ref = a.lse[((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h] * kLog2e;
             if (ref == -INFINITY) ref = INFINITY;                 // a row that saw nothing gave nothing
-            ro = row_options(a, cur.u, tok * a.group + h);
+            ro = row_options(a, sg.u, tok * a.group + h);
           }
         }
         *(uint4*)(sm + kQ + chunk_at<D>(row, ch)) = x;
@@ -570,7 +545,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
               const int j = j0 + g8 + 8 * y;
               const float dot = s[0][2 * y + x] + s[1][2 * y + x];
               float v = OPT ? biased(a, dot, ro, pos[y]) : dot * a.scale2;
-              if (tail && (j >= cur.keys || !sees(ro.seen, j, n_old))) v = -INFINITY;
+              if (tail && (j >= sg.keys || !sees(ro.seen, j, n_old))) v = -INFINITY;
               sum[y] += ref == INFINITY ? 0.f : fast_exp2(v - ref);
             }
           }
@@ -582,14 +557,11 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
         }
         if (t4 < 2) {                                             // lane t4 = y of the four has key g8 + 8 y
           const int j = j0 + g8 + 8 * t4;
-          if (j < cur.keys) w[j] = (round == 0 ? a.decay * w[j] : w[j]) + (t4 ? sum[1] : sum[0]);
+          if (j < sg.keys) w[j] = (round == 0 ? a.decay * w[j] : w[j]) + (t4 ? sum[1] : sum[0]);
         }
       }
       if (rounds > 1) __threadfence_block();                      // (another warp may have the key in the next round)
     }
-    left -= t1 - t0;
-    cur.t = t1 - 1;
-    if (left > 0) advance(cur, a.c, a.n_new, kTileKeys, 1);
   }
 }
 

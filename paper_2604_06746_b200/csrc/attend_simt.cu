@@ -73,14 +73,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
   pdl_trigger();
   pdl_wait();
   const WorkStart ws = find_work(a, 6, blocks, blockIdx.x == 0 ? a.unit_start : nullptr);
-  const int hi = ws.hi;
-  int u = ws.unit, at = ws.lo, unit_at = ws.before * blocks;
 #pragma unroll 1
-  while (at < hi) {                                                   // the tiles of an item in this CTA
-    int keys = unit_keys(a.c, u, a.n_new);
-    while (keys == 0 && u < a.c.units - 1) keys = unit_keys(a.c, ++u, a.n_new);
-    const int tiles = (keys + kTileKeys - 1) / kTileKeys, rb = blocks > 1 ? (at - unit_at) / tiles : 0;
-    const int t0 = at - unit_at - rb * tiles, t1 = min(tiles, t0 + (hi - at));
+  for (Segments sg = first_segment(a, ws, 6, blocks); sg.t1; next_segment(sg, a, 6, blocks)) {   // the tiles of an item in this CTA
+    const int u = sg.u, rb = sg.rb, keys = sg.keys, t0 = sg.t0, t1 = sg.t1;
     const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, n_old = keys - a.n_new;
     const char *const k = a.c.k + unit_offset(a.c, u), *const v = a.c.v + unit_offset(a.c, u);
     __syncthreads();
@@ -162,11 +157,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
     }
     leave_partial<D, kThreads, R, D, kWarps>(a, u * blocks + rb + blockIdx.x, min(R, a.rows - rb * R), part, stat, stat + kWarps * R, kWarps,
                                              tid, [] { __syncthreads(); });
-    at += t1 - t0;
-    if (t1 == tiles && rb + 1 == blocks) {
-      unit_at += tiles * blocks;
-      ++u;
-    }
   }
 }
 
@@ -183,13 +173,9 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant_
   pdl_trigger();
   pdl_wait();
   const WorkStart ws = find_work(a, 6, 1, nullptr);
-  const int hi = ws.hi;
-  int u = ws.unit, at = ws.lo, unit_at = ws.before;
 #pragma unroll 1
-  while (at < hi) {
-    int keys = unit_keys(a.c, u, a.n_new);
-    while (keys == 0 && u < a.c.units - 1) keys = unit_keys(a.c, ++u, a.n_new);
-    const int tiles = (keys + kTileKeys - 1) / kTileKeys, t0 = at - unit_at, t1 = min(tiles, t0 + (hi - at));
+  for (Segments sg = first_segment(a, ws, 6, 1); sg.t1; next_segment(sg, a, 6, 1)) {
+    const int u = sg.u, keys = sg.keys, t0 = sg.t0, t1 = sg.t1;
     const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, n_old = keys - a.n_new;
     const unsigned long long taken = accepted[b] & (a.n_new == 64 ? ~0ull : (1ull << a.n_new) - 1);
     const int rows = __popcll(taken) * a.group;
@@ -237,11 +223,6 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant_
           if (lse[r] != INFINITY && sees(ro[r].seen, j, n_old)) sum += fast_exp2(biased(a, s[r], ro[r], kp) - lse[r]);
         if ((lane & 3) == 0 && j < keys) w[j] = (r0 == 0 ? a.decay * w[j] : w[j]) + sum;
       }
-    }
-    at += t1 - t0;
-    if (t1 == tiles) {
-      unit_at += tiles;
-      ++u;
     }
   }
 }

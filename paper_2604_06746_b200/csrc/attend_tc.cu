@@ -89,36 +89,6 @@ __device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) ==
 // 16-byte chunk of a row in a tile of 128-byte rows, 64 columns after 64 columns, 128-byte swizzle.
 __device__ __forceinline__ uint32_t tile_at(int row, int chunk) { return (chunk >> 3) * (kTile * 128) + row * 128 + (((chunk ^ row) & 7) << 4); }
 
-// A CTA's run, item by item: segments [t0, t1) of an item's tiles.
-struct Segments {
-  int u, rb, t0, t1, keys, tiles, left;
-};
-__device__ __forceinline__ Segments first_segment(const WorkStart& ws, int blocks) {
-  Segments s;
-  s.u = ws.unit;
-  s.keys = ws.keys;
-  s.tiles = (ws.keys + kTile - 1) / kTile;
-  s.t0 = ws.lo - ws.before * blocks;
-  s.rb = blocks > 1 ? s.t0 / s.tiles : 0;
-  s.t0 -= s.rb * s.tiles;
-  s.left = ws.hi - ws.lo;
-  s.t1 = min(s.tiles, s.t0 + s.left);
-  return s;
-}
-__device__ __forceinline__ bool next_segment(Segments& s, const AttendArgs& a, int blocks) {
-  s.left -= s.t1 - s.t0;
-  if (s.left <= 0) return false;
-  if (++s.rb == blocks) {
-    s.rb = 0;
-    do ++s.u;
-    while ((s.keys = unit_keys(a.c, s.u, a.n_new)) == 0 && s.u < a.c.units - 1);
-    s.tiles = (s.keys + kTile - 1) / kTile;
-  }
-  s.t0 = 0;
-  s.t1 = min(s.tiles, s.left);
-  return true;
-}
-
 // MT: halves of 128 rows in a block.
 template <int D, int MT, bool OPT>
 struct TcAttend {
@@ -176,7 +146,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   const WorkStart ws = find_work(a, 7, blocks, blockIdx.x == 0 ? a.unit_start : nullptr);
   tc_fence_after();
   const uint32_t tmem = *tmem_at;
-  const bool work = ws.lo < ws.hi;
+  Segments sg = first_segment(a, ws, 7, blocks);
+  const bool work = sg.t1 > 0;
   // (one answer for the warp: what follows is for all of its lanes)
   auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag)); };
   bool clean = true;                                             // every MMA of this CTA has retired
@@ -186,7 +157,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (work && warp == 0) {
     const uint64_t hint = blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
-    Segments sg = first_segment(ws, blocks);
     int n = 0;                                                   // units: K and V of a tile after one another
     bool ok = true;
     do {
@@ -212,7 +182,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
             mbar_arrive(full(st));
           }
         }
-    } while (ok && next_segment(sg, a, blocks));
+      next_segment(sg, a, 7, blocks);
+    } while (ok && sg.t1);
     // copies in flight end before the block does
     if (!ok)
       for (int i = max(0, n - NU); i < n; ++i) mbar_drain(full(i % NU), (i / NU) & 1, abort_flag);
@@ -221,7 +192,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     const uint32_t idesc_s = instr_desc(128, kTile) | (a.scale2 < 0.f || a.inv_cap < 0.f ? 1u << 13 : 0u);
     constexpr uint32_t idesc_o = instr_desc(128, D) | kTransposeB;
     const uint64_t q_desc = smem_desc(base), k_desc0 = smem_desc(base + kRing), v_desc0 = smem_desc_n(base + kRing);
-    Segments sg = first_segment(ws, blocks);
     int n = 0, seg = 0, tails = 0;                               // tiles before the segment; segments; tiles that were looked through
     int done[2] = {0, 0}, used[2] = {0, 0};                      // jobs of a stream so far; segments it had jobs in
     bool ok = true;
@@ -273,14 +243,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
       }
       n += tiles;
       ++seg;
-    } while (ok && next_segment(sg, a, blocks));
+      next_segment(sg, a, 7, blocks);
+    } while (ok && sg.t1);
     if (lane == 0) tc_commit(drained);
     __syncwarp();
     clean = mbar_drain(drained, 0, abort_flag);
   } else if (work && warp < 4) {
     // rows of a segment, then V tiles with new tokens
     const int hl = tid - 64;
-    Segments sg = first_segment(ws, blocks);
     int n = 0, seg = 0, tails = 0;
     bool ok = true;
     do {
@@ -323,7 +293,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
       }
       n += sg.t1 - sg.t0;
       ++seg;
-    } while (ok && next_segment(sg, a, blocks));
+      next_segment(sg, a, 7, blocks);
+    } while (ok && sg.t1);
   }
   } else {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
@@ -331,7 +302,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     const int s = (warp - 4) / 4, quarter = warp % 4;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
     const float scale2 = fabsf(a.scale2), inv_cap = fabsf(a.inv_cap);   // (a negative scale negates the product)
-    Segments sg = first_segment(ws, blocks);
     int n = 0, done = 0;
     bool ok = true;
     do {
@@ -483,7 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
         if (lane == 0) mbar_arrive(o_free(s));
       }
       n += tiles;
-    } while (next_segment(sg, a, blocks));
+      next_segment(sg, a, 7, blocks);
+    } while (sg.t1);
   }
   }
 
