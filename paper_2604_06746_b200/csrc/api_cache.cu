@@ -17,7 +17,7 @@ bool by_tensor_cores(const structkv_config& cfg, int n_new) {
 AttendPlan attend_plan(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
   if (cfg.dtype == STRUCTKV_FP32) return {rows <= 4 ? 4 : 8, 64, sms, 1, 1};
-  if (by_tensor_cores(cfg, n_new)) return rows <= 128 ? AttendPlan{128, 128, sms, 2, 0} : AttendPlan{256, 128, sms, 1, 0};
+  if (by_tensor_cores(cfg, n_new)) return rows <= 128 ? AttendPlan{128, 128, sms, 2, 1} : AttendPlan{256, 128, sms, 1, 0};
   return {rows <= 8 ? 8 : 16, 64, sms, 1, rows <= 8 ? 1 : 0};
 }
 

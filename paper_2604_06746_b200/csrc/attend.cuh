@@ -263,19 +263,11 @@ __device__ __forceinline__ Segments first_segment(const AttendArgs& a, const Wor
   return s;
 }
 
-// cap tanh(scale s / cap) in bits: for small arguments the odd series, else 1 - 2 / (e^2y + 1), both to fp32's last bits.
+// cap tanh(y) in bits, y = scale s / cap, as cap - 2 cap / (e^2y + 1): off by 2^-22 cap at most, whatever y (infinite ones too).
 __device__ __forceinline__ float capped(float s, float cap2, float inv_cap) {
-  const float y = s * inv_cap, a = fabsf(y), y2 = y * y;
-  if (a < 0.25f) {
-    // Taylor series of tanh about 0; the first term left out is below 9e-9 relative
-    float p = fmaf(y2, 62.f / 2835.f, -17.f / 315.f);
-    p = fmaf(y2, p, 2.f / 15.f);
-    p = fmaf(y2, p, -1.f / 3.f);
-    return cap2 * fmaf(y * y2, p, y);
-  }
-  if (!(a < 20.f)) return a == a ? copysignf(cap2, y) : y;        // (1 in fp32 from 10 on; a NaN stays one)
-  const float e = fast_exp2(a * (2.f * kLog2e));
-  return copysignf(cap2 * (1.f - __fdividef(2.f, e + 1.f)), y);
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fast_exp2(s * (inv_cap * (2.f * kLog2e))) + 1.f));
+  return fmaf(-2.f * cap2, r, cap2);
 }
 
 // The new tokens that row r of a unit sees, as bits.

@@ -6,9 +6,10 @@
 // exponentials: the two halves of up to 256 rows over the same keys, or, with up to 128 rows, the even and the odd key tiles (the
 // streams then leave a partial each).  Work is cut as everywhere (attend.cuh).
 //
-// Warps: 0 fills the ring of K and V tiles by TMA, 1 issues the products, 2 and 3 bring a segment's rows and look through V tiles that
-// hold new tokens (what is not finite there is taken out and added, at the end, to the rows that see it: 0 x infinity), 4-7 and
-// 8-11 are the streams' softmax.  The reference of a row follows its maximum only where that outgrows it by 2^kSlack.
+// Warps: 0 fills the ring of K and V tiles by TMA; 1 and 2 issue the streams' products (issuing eight takes 900 clocks: by one warp
+// for both a key tile of 256 rows took 5850, the softmax of it 1840); 3 looks through V tiles that hold new tokens (what is not
+// finite there is taken out and added, at the end, to the rows that see it: 0 x infinity); 4-7 and 8-11 bring a segment's rows
+// and are the streams' softmax.  The reference of a row follows its maximum only where that outgrows it by 2^kSlack.
 // Bound by reading K and V up to about 128 rows, beyond by products and exponentials together.
 #include <algorithm>
 
@@ -34,12 +35,24 @@ __device__ __forceinline__ uint64_t smem_desc_n(uint32_t addr) {
   return smem_desc(addr) & ~(0x3fffull << 16) | (uint64_t)((kTile * 128) >> 4) << 16;
 }
 constexpr uint32_t kTransposeB = 1u << 16;
-// d += a b with a in tensor memory.
-__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// Products that a whole warp comes by and one lane (lead) issues: without a branch for it the operands can stay uniform.  Descriptors
+// by their lower words; hi: the upper word, the same for all of an operand's.
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate, uint32_t lead) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+      "{\n.reg .pred p, q;\n.reg .b64 da, db;\nsetp.ne.b32 q, %6, 0;\nsetp.ne.b32 p, %5, 0;\nmov.b64 da, {%1, %3};\nmov.b64 db, {%2, %3};\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(lead) : "memory");
+}
+// a in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate, uint32_t lead) {
+  asm volatile(
+      "{\n.reg .pred p, q;\n.reg .b64 db;\nsetp.ne.b32 q, %6, 0;\nsetp.ne.b32 p, %5, 0;\nmov.b64 db, {%2, %3};\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}"
+      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void commit_by(uint32_t lead, uint32_t bar) {
+  asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}"
+               ::"r"(bar), "r"(lead) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -94,7 +107,10 @@ template <int D, int MT, bool OPT>
 struct TcAttend {
   static constexpr int RB = 128 * MT, kUnit = kTile * D * 2, kQ = RB * D * 2, kPos = OPT ? kTile * 4 : 0;
   static constexpr int kFixed = kQ + 1024 + 512;
-  static constexpr int kUnits = std::min(8, (227 * 1024 - 512 - kFixed) / (kUnit + kPos));   // (512: static shared memory)
+  // Places for tiles of K and of V; with two streams over different tiles each has a ring of its own: a wait by parity holds only for
+  // who follows a barrier from phase to phase.
+  static constexpr int kUnits = std::min(8, (227 * 1024 - 512 - kFixed) / (kUnit + kPos)) / (MT == 2 ? 1 : 2) * (MT == 2 ? 1 : 2);
+  static constexpr int kRingUnits = MT == 2 ? kUnits : kUnits / 2;
   static constexpr int kSmem = kUnits * (kUnit + kPos) + kFixed;
   static_assert(kUnits >= 4, "a ring");
 };
@@ -108,28 +124,34 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
   constexpr uint32_t kRing = S::kQ, kPosAt = kRing + NU * S::kUnit, kBars = kPosAt + NU * S::kPos;
   const uint32_t bars = base + kBars, more = bars + 16 * NU;
+  // where unit u (K and V of a tile after one another) of the ring of stream s lies, and its phase there
+  constexpr int NR = S::kRingUnits;
+  auto place_of = [](int s, int u) { return (MT == 2 ? 0 : s * NR) + u % NR; };
+  auto phase_of = [](int u) { return (u / NR) & 1; };
   auto full = [&](int u) { return bars + 8 * u; };
   auto empty = [&](int u) { return bars + 8 * (NU + u); };
-  const uint32_t q_full = more, q_empty = more + 8, v_look = more + 16, v_ready = more + 24;
-  auto s_full = [&](int s) { return more + 32 + 8 * s; };
-  auto p_ready = [&](int s) { return more + 48 + 8 * s; };
-  auto o_done = [&](int s) { return more + 64 + 8 * s; };
-  auto o_free = [&](int s) { return more + 80 + 8 * s; };
-  const uint32_t drained = more + 96;
-  volatile int* const words = (volatile int*)(sm + kBars + 16 * NU + 104);
+  auto s_full = [&](int s) { return more + 8 * s; };
+  auto p_ready = [&](int s) { return more + 16 + 8 * s; };
+  auto o_done = [&](int s) { return more + 32 + 8 * s; };
+  auto o_free = [&](int s) { return more + 48 + 8 * s; };
+  auto v_look = [&](int s) { return more + 64 + 8 * s; };
+  auto v_ready = [&](int s) { return more + 80 + 8 * s; };
+  auto drained = [&](int s) { return more + 96 + 8 * s; };
+  const uint32_t q_full = more + 112, q_empty = more + 120;
+  volatile int* const words = (volatile int*)(sm + kBars + 16 * NU + 128);
   volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v: some new token's V was not finite
   volatile uint32_t* const tmem_at = (volatile uint32_t*)words + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int blocks = (a.rows + RB - 1) / RB;
   pdl_trigger();
   if (tid == 0) {
-    for (int i = 0; i < NU; ++i) { mbar_init(full(i), S::kPos ? 33 : 1); mbar_init(empty(i), 1); }
-    mbar_init(q_full, 64);
-    mbar_init(q_empty, 1);
-    mbar_init(v_look, 1);
-    mbar_init(v_ready, 64);
-    mbar_init(drained, 1);
-    for (int s = 0; s < 2; ++s) { mbar_init(s_full(s), 1); mbar_init(p_ready(s), 4); mbar_init(o_done(s), 1); mbar_init(o_free(s), 4); }
+    for (int i = 0; i < NU; ++i) { mbar_init(full(i), S::kPos ? 33 : 1); mbar_init(empty(i), MT); }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(s_full(s), 1); mbar_init(p_ready(s), 4); mbar_init(o_done(s), 1); mbar_init(o_free(s), 4);
+      mbar_init(v_look(s), 1); mbar_init(v_ready(s), 32); mbar_init(drained(s), 1);
+    }
+    mbar_init(q_full, 256);
+    mbar_init(q_empty, 8);
     *abort_flag = 0;
     *odd_v = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -157,16 +179,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (work && warp == 0) {
     const uint64_t hint = blocks == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
-    int n = 0;                                                   // units: K and V of a tile after one another
+    int made[2] = {0, 0};                                        // units of the rings
     bool ok = true;
     do {
       const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv;
 #pragma unroll 1
       for (int t = sg.t0; t < sg.t1 && ok; ++t)
 #pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv, ++n) {
-          const int st = n % NU;
-          if (n >= NU && !(ok = mbar_wait_producer(empty(st), (n / NU - 1) & 1, abort_flag, kWaitCycles))) break;
+        for (int kv = 0; kv < 2; ++kv) {
+          const int s = MT == 2 ? 0 : (t - sg.t0) & 1, n = s ? made[1]++ : made[0]++, st = place_of(s, n);
+          if (n >= NR && !(ok = mbar_wait_producer(empty(st), phase_of(n) ^ 1, abort_flag, kWaitCycles))) {
+            --(s ? made[1] : made[0]);
+            break;
+          }
           if (lane == 0) {
             mbar_expect_tx(full(st), S::kUnit);
             tma_load_slots(base + kRing + st * S::kUnit, kv ? &maps.v : &maps.k, full(st), t * kTile, g, b, hint);
@@ -186,93 +211,75 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     } while (ok && sg.t1);
     // copies in flight end before the block does
     if (!ok)
-      for (int i = max(0, n - NU); i < n; ++i) mbar_drain(full(i % NU), (i / NU) & 1, abort_flag);
-  } else if (work && warp == 1) {
-    // Products, by one lane.  Job j of a segment: tile j / MT by stream j % 2; scores run two jobs ahead of outputs.
+      for (int s = 0; s < 2; ++s)
+        for (int n = s ? made[1] : made[0], i = max(0, n - NR); i < n; ++i) mbar_drain(full(place_of(s, i)), phase_of(i), abort_flag);
+  } else if (work && warp < 3) {
+    // Products of stream s, each job's scores made after the outputs of the job before.
+    const int s = warp - 1;
+    const uint32_t lead = lane == 0;
     const uint32_t idesc_s = instr_desc(128, kTile) | (a.scale2 < 0.f || a.inv_cap < 0.f ? 1u << 13 : 0u);
     constexpr uint32_t idesc_o = instr_desc(128, D) | kTransposeB;
-    const uint64_t q_desc = smem_desc(base), k_desc0 = smem_desc(base + kRing), v_desc0 = smem_desc_n(base + kRing);
-    int n = 0, seg = 0, tails = 0;                               // tiles before the segment; segments; tiles that were looked through
-    int done[2] = {0, 0}, used[2] = {0, 0};                      // jobs of a stream so far; segments it had jobs in
+    const uint64_t q_desc = smem_desc(base + (MT == 2 ? s * 128 * 128 : 0)), k_desc = smem_desc(base + kRing), v_desc = smem_desc_n(base + kRing);
+    const uint32_t q_lo = (uint32_t)q_desc, k_lo = (uint32_t)k_desc, v_lo = (uint32_t)v_desc, hi_k = (uint32_t)(q_desc >> 32), hi_v = (uint32_t)(v_desc >> 32);
+    const uint32_t s_at = tmem + s * 128, o_at = tmem + 256 + s * 128;
+    int n = 0, seg = 0, tails = 0, done = 0, used = 0;           // jobs before the segment; segments; tails, jobs, segments with jobs
     bool ok = true;
     do {
-      const int tiles = sg.t1 - sg.t0, jobs = tiles * MT, n_old = sg.keys - a.n_new;
-      ok = wait(q_full, seg & 1);
-      auto scores = [&](int j) {
-        const int s = j & 1, unit = 2 * (n + j / MT), st = unit % NU;
-        if (!ok || !(ok = wait(full(st), (unit / NU) & 1))) return;
+      const int tiles = sg.t1 - sg.t0, jobs = MT == 2 ? tiles : (tiles + 1 - s) / 2, n_old = sg.keys - a.n_new;
+      auto scores = [&](int k) {
+        const int unit = 2 * (n + k), st = place_of(s, unit);
+        if (!(ok = wait(full(st), phase_of(unit)))) return;
         tc_fence_after();
-        if (lane == 0) {
-          const uint64_t qd = q_desc + (uint64_t)(MT == 2 ? (s * 128 * 128) >> 4 : 0), kd = k_desc0 + (uint64_t)((st * S::kUnit) >> 4);
+        const uint32_t kd = k_lo + ((st * S::kUnit) >> 4);
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            tc_mma_bf16(tmem + s * 128, qd + (uint64_t)(((kk / 4) * RB * 128 + (kk % 4) * 32) >> 4),
-                        kd + (uint64_t)(((kk / 4) * kTile * 128 + (kk % 4) * 32) >> 4), idesc_s, kk > 0);
-          tc_commit(s_full(s));
-          if (j % MT == MT - 1) tc_commit(empty(st));
-          if (j == jobs - 1) tc_commit(q_empty);
-        }
-        __syncwarp();
+        for (int kk = 0; kk < D / 16; ++kk)
+          mma_ss(s_at, q_lo + (((kk / 4) * RB * 128 + (kk % 4) * 32) >> 4), kd + (((kk / 4) * kTile * 128 + (kk % 4) * 32) >> 4), hi_k, idesc_s, kk > 0, lead);
+        commit_by(lead, s_full(s));
+        commit_by(lead, empty(st));
       };
-      scores(0);
-      if (jobs > 1) scores(1);
+      ok = wait(q_full, seg & 1);
+      if (ok && jobs > 0) scores(0);
 #pragma unroll 1
-      for (int j = 0; j < jobs && ok; ++j) {
-        const int s = j & 1, t = j / MT, unit = 2 * (n + t) + 1, st = unit % NU;
-        if (!(ok = wait(full(st), (unit / NU) & 1))) break;
-        // A tile with new tokens is handed to the warps that look through it, and taken back: by barriers of their own, as a wait
-        // by parity holds only for who follows a barrier from phase to phase.
-        const bool tail = (sg.t0 + t + 1) * kTile > n_old && j % MT == 0;
-        if (tail && lane == 0) mbar_arrive(v_look);
-        if (j < 2 && used[s] > 0 && !(ok = wait(o_free(s), (used[s] - 1) & 1))) break;
-        if (j < 2) ++used[s];
-        if (!(ok = wait(p_ready(s), done[s] & 1))) break;
-        if (tail && !(ok = wait(v_ready, tails++ & 1))) break;
+      for (int k = 0; k < jobs && ok; ++k) {
+        const int t = MT == 2 ? k : 2 * k + s, unit = 2 * (n + k) + 1, st = place_of(s, unit);
+        if (!(ok = wait(full(st), phase_of(unit)))) break;
+        // A tile with new tokens is handed to the warp that looks through it, and taken back: by barriers of their own, as a wait by
+        // parity holds only for who follows a barrier from phase to phase.
+        const bool tail = (sg.t0 + t + 1) * kTile > n_old;
+        if (tail && lead) mbar_arrive(v_look(s));
+        if (k == 0 && used++ > 0 && !(ok = wait(o_free(s), used & 1))) break;
+        if (!(ok = wait(p_ready(s), done & 1))) break;
+        if (tail && !(ok = wait(v_ready(s), tails++ & 1))) break;
         tc_fence_after();
-        if (lane == 0) {
-          const uint64_t vd = v_desc0 + (uint64_t)((st * S::kUnit) >> 4);
+        const uint32_t vd = v_lo + ((st * S::kUnit) >> 4);
 #pragma unroll
-          for (int kk = 0; kk < kTile / 16; ++kk)
-            tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + kk * 8, vd + (uint64_t)((kk * 16 * 128) >> 4), idesc_o, j >= 2 || kk > 0);
-          tc_commit(o_done(s));
-          if (j % MT == MT - 1) tc_commit(empty(st));
-        }
-        __syncwarp();
-        ++done[s];
-        if (j + 2 < jobs) scores(j + 2);
+        for (int kk = 0; kk < kTile / 16; ++kk) mma_ts(o_at, s_at + kk * 8, vd + ((kk * 16 * 128) >> 4), hi_v, idesc_o, k > 0 || kk > 0, lead);
+        commit_by(lead, o_done(s));
+        commit_by(lead, empty(st));
+        ++done;
+        if (k + 1 < jobs) scores(k + 1);
       }
-      n += tiles;
+      n += jobs;
       ++seg;
       next_segment(sg, a, 7, blocks);
     } while (ok && sg.t1);
-    if (lane == 0) tc_commit(drained);
-    __syncwarp();
-    clean = mbar_drain(drained, 0, abort_flag);
-  } else if (work && warp < 4) {
-    // rows of a segment, then V tiles with new tokens
-    const int hl = tid - 64;
-    int n = 0, seg = 0, tails = 0;
+    commit_by(lead, drained(s));
+    clean = mbar_drain(drained(s), 0, abort_flag);
+    if (!clean) *abort_flag = 2;
+  } else if (work) {
+    // V tiles with new tokens
+    int n[2] = {0, 0}, tails[2] = {0, 0};                        // jobs of the streams before the segment
     bool ok = true;
     do {
-      if (seg > 0 && !(ok = mbar_wait_producer(q_empty, (seg - 1) & 1, abort_flag, kWaitCycles))) break;
-      const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv, n_old = sg.keys - a.n_new;
-      const char* const q0 = a.q + (size_t)b * a.q_batch + (size_t)(g * a.group) * a.q_head;
-#pragma unroll 4
-      for (int i = hl; i < min(RB, a.rows - sg.rb * RB) * CH; i += 64) {   // (rows beyond them do not reach these)
-        const int row = i / CH, ch = i % CH, r = sg.rb * RB + row, tok = quotient(r, a.by_group), h = r - tok * a.group;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                     ::"r"(base + (ch >> 3) * (RB * 128) + row * 128 + (((ch ^ row) & 7) << 4)),
-                       "l"(q0 + (size_t)tok * a.q_token + (size_t)h * a.q_head + ch * 16) : "memory");
-      }
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive(q_full);
+      const int n_old = sg.keys - a.n_new;
       for (int t = max(sg.t0, n_old / kTile); t < sg.t1 && ok; ++t) {
-        const int unit = 2 * (n + t - sg.t0) + 1, st = unit % NU;
-        if (!(ok = mbar_wait_producer(v_look, tails++ & 1, abort_flag, kWaitCycles))) break;
+        const int of = MT == 2 ? 0 : (t - sg.t0) & 1, k = MT == 2 ? t - sg.t0 : (t - sg.t0) / 2, st = place_of(of, 2 * ((of ? n[1] : n[0]) + k) + 1);
         const int row0 = max(0, n_old - t * kTile);
+        for (int s = 0; s < 2 && ok; ++s)
+          if (MT == 2 || ((t - sg.t0) & 1) == s) ok = mbar_wait_producer(v_look(s), tails[s]++ & 1, abort_flag, kWaitCycles);
+        if (!ok) break;
 #pragma unroll 4
-        for (int i = row0 * CH + hl; i < kTile * CH; i += 64) {
+        for (int i = row0 * CH + lane; i < kTile * CH; i += 32) {
           uint4* const p = (uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH));
           uint32_t w[4] = {p->x, p->y, p->z, p->w};
           bool bad = false;
@@ -289,10 +296,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(v_ready);
+        for (int s = 0; s < 2; ++s)
+          if (MT == 2 || ((t - sg.t0) & 1) == s) mbar_arrive(v_ready(s));
       }
-      n += sg.t1 - sg.t0;
-      ++seg;
+      const int tiles = sg.t1 - sg.t0;
+      n[0] += MT == 2 ? tiles : (tiles + 1) / 2;
+      n[1] += MT == 2 ? tiles : tiles / 2;
       next_segment(sg, a, 7, blocks);
     } while (ok && sg.t1);
   }
@@ -302,9 +311,26 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     const int s = (warp - 4) / 4, quarter = warp % 4;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
     const float scale2 = fabsf(a.scale2), inv_cap = fabsf(a.inv_cap);   // (a negative scale negates the product)
-    int n = 0, done = 0;
+    int done = 0, seg = 0;
     bool ok = true;
     do {
+      {
+        // the segment's rows, once the products of the segment before have read theirs  (rows beyond the last do not reach these)
+        if (seg > 0 && !(ok = wait(q_empty, (seg - 1) & 1))) break;
+        const int b = quotient(sg.u, a.by_kv), g = sg.u - b * a.c.n_kv;
+        const char* const q0 = a.q + (size_t)b * a.q_batch + (size_t)(g * a.group) * a.q_head;
+#pragma unroll 4
+        for (int i = tid - 128; i < min(RB, a.rows - sg.rb * RB) * CH; i += 256) {
+          const int row = i / CH, ch = i % CH, r = sg.rb * RB + row, tok = quotient(r, a.by_group), h = r - tok * a.group;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                       ::"r"(base + (ch >> 3) * (RB * 128) + row * 128 + (((ch ^ row) & 7) << 4)),
+                         "l"(q0 + (size_t)tok * a.q_token + (size_t)h * a.q_head + ch * 16) : "memory");
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(q_full);
+        ++seg;
+      }
       const int tiles = sg.t1 - sg.t0, jobs = MT == 2 ? tiles : (tiles + 1 - s) / 2, n_old = sg.keys - a.n_new;
       const int row = (MT == 2 ? s * 128 : 0) + quarter * 32 + lane, r = sg.rb * RB + row;
       const bool idle = r - lane >= a.rows;                      // no row of this warp: it only keeps step
@@ -317,8 +343,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
         const int* kp = nullptr;
         if (OPT && a.slopes) {
           // (these scores were made after the outputs of the tile before, so that the place's previous tile has come and gone)
-          const int unit = 2 * (n + t) + 1, st = unit % NU;
-          if (!(ok = wait(full(st), (unit / NU) & 1))) break;
+          const int unit = 2 * done + 1, st = place_of(s, unit);
+          if (!(ok = wait(full(st), phase_of(unit)))) break;
           kp = (const int*)(sm + kPosAt + st * S::kPos);
         }
         tc_fence_after();
@@ -414,6 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
         if (lane == 0) mbar_arrive(p_ready(s));
       }
       if (!ok) break;
+      if (lane == 0) mbar_arrive(q_empty);                       // (this stream's scores are all there)
       const int slot = sg.u * blocks + sg.rb + blockIdx.x;
       const size_t at = MT == 2 ? (size_t)slot * RB + row : ((size_t)slot * 2 + s) * RB + row;
       if (r < a.rows) a.part_stat[at] = make_float2(m, l);
@@ -442,9 +469,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
               }
             }
             if (r < a.rows) {
-              float4* const to = (float4*)(a.part_out + at * D + c);
+              // (column after column of four: neighbouring rows, the lanes, side by side)
+              float4* const to = (float4*)a.part_out + ((at - row) / RB * (D / 4) + c / 4) * RB + row;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) to[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+              for (int e = 0; e < 8; ++e) to[e * RB] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
             }
           }
         }
@@ -452,7 +480,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
         __syncwarp();
         if (lane == 0) mbar_arrive(o_free(s));
       }
-      n += tiles;
       next_segment(sg, a, 7, blocks);
     } while (sg.t1);
   }
@@ -462,6 +489,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
+    clean = *abort_flag != 2;
     if (clean) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
   if (tid == 0 && *abort_flag) atomicCAS(a.c.status, 0, (int)STRUCTKV_ERR_TIMEOUT);

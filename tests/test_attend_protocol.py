@@ -66,98 +66,101 @@ def segments_of(rng, tiles_of_items, run):
 @pytest.mark.parametrize("nu", [4, 5, 6, 8])
 @pytest.mark.parametrize("positions", [False, True])
 def test_tensor_core_kernel(mt, nu, positions):
-    for seed in range(60):
+    nr = nu if mt == 2 else nu // 2                       # places of a ring
+    for seed in range(100):
         rng = random.Random(seed)
         segs = segments_of(rng, [rng.choice([1, 1, 1, 2, 3, 7]) for _ in range(rng.randint(1, 8))], rng.randint(1, 16))
         n_tail = rng.randint(1, 2)                        # tiles of an item with new tokens
         m = Machine(seed)
-        full, empty = [Barrier(1) for _ in range(nu)], [Barrier(1) for _ in range(nu)]
-        q_full, q_empty, v_look, v_ready = Barrier(2), Barrier(1), Barrier(1), Barrier(2)
-        s_full, p_ready, o_done, o_free = ([Barrier(c) for _ in range(2)] for c in (1, 1, 1, 1))
-        copies = [[] for _ in range(nu)]
-        mma = []
-        m.queues = copies + [mma]
+        full, empty = [Barrier(1) for _ in range(nu)], [Barrier(mt) for _ in range(nu)]
+        q_full, q_empty = Barrier(2), Barrier(2)
+        s_full, p_ready, o_done, o_free, v_look, v_ready = ([Barrier(1) for _ in range(2)] for _ in range(6))
+        copies, mma = [[] for _ in range(nu)], [[], []]
+        m.queues = copies + mma
+
+        def place(s, unit):
+            return (0 if mt == 2 else s * nr) + unit % nr
+
+        def jobs_of(s, tiles):
+            return tiles if mt == 2 else (tiles + 1 - s) // 2
 
         def producer():
-            n = 0
+            made = [0, 0]
             for t0, t1, _ in segs:
-                for _ in range(2 * (t1 - t0)):
-                    if n >= nu:
-                        yield empty[n % nu], n // nu - 1
-                    copies[n % nu].append(full[n % nu].arrive)
-                    n += 1
+                for t in range(t1 - t0):
+                    s = 0 if mt == 2 else t & 1
+                    for _ in range(2):
+                        unit = made[s]
+                        if unit >= nr:
+                            yield empty[place(s, unit)], unit // nr - 1
+                        copies[place(s, unit)].append(full[place(s, unit)].arrive)
+                        made[s] += 1
 
-        def products():
-            n, tails, done, used = 0, 0, [0, 0], [0, 0]
+        def products(s):
+            n, tails, done, used = 0, 0, 0, 0
             for seg, (t0, t1, tiles) in enumerate(segs):
-                jobs = (t1 - t0) * mt
+                jobs = jobs_of(s, t1 - t0)
 
-                def scores(j):
-                    unit = 2 * (n + j // mt)
-                    yield full[unit % nu], unit // nu
-                    mma.append(s_full[j & 1].arrive)
-                    if j % mt == mt - 1:
-                        mma.append(empty[unit % nu].arrive)
-                    if j == jobs - 1:
-                        mma.append(q_empty.arrive)
+                def scores(k):
+                    unit = 2 * (n + k)
+                    yield full[place(s, unit)], unit // nr
+                    mma[s] += [s_full[s].arrive, empty[place(s, unit)].arrive]
 
                 yield q_full, seg
-                for j in range(min(2, jobs)):
-                    yield from scores(j)
-                for j in range(jobs):
-                    s, t = j & 1, j // mt
-                    unit = 2 * (n + t) + 1
-                    yield full[unit % nu], unit // nu
-                    tail = t0 + t >= tiles - n_tail and j % mt == 0
+                if jobs:
+                    yield from scores(0)
+                for k in range(jobs):
+                    t, unit = k if mt == 2 else 2 * k + s, 2 * (n + k) + 1
+                    yield full[place(s, unit)], unit // nr
+                    tail = t0 + t >= tiles - n_tail
                     if tail:
-                        v_look.arrive()
-                    if j < 2:
-                        if used[s]:
-                            yield o_free[s], used[s] - 1
-                        used[s] += 1
-                    yield p_ready[s], done[s]
+                        v_look[s].arrive()
+                    if k == 0:
+                        if used:
+                            yield o_free[s], used - 1
+                        used += 1
+                    yield p_ready[s], done
                     if tail:
-                        yield v_ready, tails
+                        yield v_ready[s], tails
                         tails += 1
-                    mma.append(o_done[s].arrive)
-                    if j % mt == mt - 1:
-                        mma.append(empty[unit % nu].arrive)
-                    done[s] += 1
-                    if j + 2 < jobs:
-                        yield from scores(j + 2)
-                n += t1 - t0
+                    mma[s] += [o_done[s].arrive, empty[place(s, unit)].arrive]
+                    done += 1
+                    if k + 1 < jobs:
+                        yield from scores(k + 1)
+                n += jobs
 
-        def helper():
-            tails = 0
-            for seg, (t0, t1, tiles) in enumerate(segs):
+        def looks():
+            tails = [0, 0]
+            for t0, t1, tiles in segs:
+                for t in range(max(t0, tiles - n_tail, 0), t1):
+                    mine = [0, 1] if mt == 2 else [(t - t0) & 1]
+                    for s in mine:
+                        yield v_look[s], tails[s]
+                        tails[s] += 1
+                    for s in mine:
+                        v_ready[s].arrive()
+
+        def softmax(s):
+            done = 0
+            for seg, (t0, t1, _) in enumerate(segs):
                 if seg:
                     yield q_empty, seg - 1
                 q_full.arrive()
-                for _ in range(max(t0, tiles - n_tail, 0), t1):
-                    yield v_look, tails
-                    tails += 1
-                    v_ready.arrive()
-
-        def softmax(s):
-            n, done = 0, 0
-            for t0, t1, _ in segs:
-                tiles = t1 - t0
-                jobs = tiles if mt == 2 else (tiles + 1 - s) // 2
+                jobs = jobs_of(s, t1 - t0)
                 for k in range(jobs):
                     yield s_full[s], done
                     if positions:
-                        unit = 2 * (n + (k if mt == 2 else 2 * k + s)) + 1
-                        yield full[unit % nu], unit // nu
+                        yield full[place(s, 2 * done + 1)], (2 * done + 1) // nr
                     if k and rng.random() < 0.5:
                         yield o_done[s], done - 1
                     p_ready[s].arrive()
                     done += 1
+                q_empty.arrive()
                 if jobs:
                     yield o_done[s], done - 1
                     o_free[s].arrive()
-                n += tiles
 
-        m.roles = [producer(), products(), helper(), helper(), softmax(0), softmax(1)]
+        m.roles = [producer(), products(0), products(1), looks(), softmax(0), softmax(1)]
         m.run()
 
 
