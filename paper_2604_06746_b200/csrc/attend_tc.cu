@@ -137,8 +137,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   auto v_look = [&](int s) { return more + 64 + 8 * s; };
   auto v_ready = [&](int s) { return more + 80 + 8 * s; };
   auto drained = [&](int s) { return more + 96 + 8 * s; };
-  const uint32_t q_full = more + 112, q_empty = more + 120;
-  volatile int* const words = (volatile int*)(sm + kBars + 16 * NU + 128);
+  auto turn = [&](int s) { return more + 112 + 8 * s; };
+  const uint32_t q_full = more + 128, q_empty = more + 136;
+  volatile int* const words = (volatile int*)(sm + kBars + 16 * NU + 144);
   volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v: some new token's V was not finite
   volatile uint32_t* const tmem_at = (volatile uint32_t*)words + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     for (int i = 0; i < NU; ++i) { mbar_init(full(i), S::kPos ? 33 : 1); mbar_init(empty(i), MT); }
     for (int s = 0; s < 2; ++s) {
       mbar_init(s_full(s), 1); mbar_init(p_ready(s), 4); mbar_init(o_done(s), 1); mbar_init(o_free(s), 4);
-      mbar_init(v_look(s), 1); mbar_init(v_ready(s), 32); mbar_init(drained(s), 1);
+      mbar_init(v_look(s), 1); mbar_init(v_ready(s), 32); mbar_init(drained(s), 1); mbar_init(turn(s), 4);
     }
     mbar_init(q_full, 256);
     mbar_init(q_empty, 8);
@@ -413,6 +414,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
               tmem_st_wait();
             }
           }
+          // The halves of the rows take turns with the exponentials, so that one's run beside the other's products: left alone they fall
+          // into step, and exponentials and products wait for one another (a key tile of 256 rows 5200 clocks).
+          if (MT == 2 && done >= 1 - s && !(ok = wait(turn(s), (done - 1 + s) & 1))) break;
           const float ref = m == -INFINITY ? 0.f : m;
           const uint64_t mul2 = pack2(mul, mul), ref2 = pack2(-ref, -ref);
           uint64_t sum = pack2(0.f, 0.f);
@@ -434,10 +438,15 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
           unpack2(sum, s0, s1);
           l += s0 + s1;
           tmem_st_wait();
+        } else if (MT == 2 && done >= 1 - s && !(ok = wait(turn(s), (done - 1 + s) & 1))) {
+          break;
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready(s));
+        if (lane == 0) {
+          mbar_arrive(p_ready(s));
+          if (MT == 2) mbar_arrive(turn(1 - s));
+        }
       }
       if (!ok) break;
       if (lane == 0) mbar_arrive(q_empty);                       // (this stream's scores are all there)

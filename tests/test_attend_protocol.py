@@ -75,6 +75,7 @@ def test_tensor_core_kernel(mt, nu, positions):
         full, empty = [Barrier(1) for _ in range(nu)], [Barrier(mt) for _ in range(nu)]
         q_full, q_empty = Barrier(2), Barrier(2)
         s_full, p_ready, o_done, o_free, v_look, v_ready = ([Barrier(1) for _ in range(2)] for _ in range(6))
+        turn = [Barrier(1), Barrier(1)]
         copies, mma = [[] for _ in range(nu)], [[], []]
         m.queues = copies + mma
 
@@ -153,7 +154,11 @@ def test_tensor_core_kernel(mt, nu, positions):
                         yield full[place(s, 2 * done + 1)], (2 * done + 1) // nr
                     if k and rng.random() < 0.5:
                         yield o_done[s], done - 1
+                    if mt == 2 and done >= 1 - s:
+                        yield turn[s], done - 1 + s
                     p_ready[s].arrive()
+                    if mt == 2:
+                        turn[1 - s].arrive()
                     done += 1
                 q_empty.arrive()
                 if jobs:
