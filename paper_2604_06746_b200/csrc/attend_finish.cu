@@ -6,6 +6,8 @@
 // it read; the second reading of K that would spare them is 2 d); block c takes the keys of run c of all tiles.
 // Bound by the chain of loads: where the partials lie follows from unit_start, their weights from their references.  With
 // 64-bit divisions for the former the code alone (51 KB, fetched once a launch) took 10 us.
+#include <algorithm>
+
 #include "attend.cuh"
 
 namespace skv {
@@ -191,85 +193,91 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
   }
 }
 
-// The same where rows are many (attend_tc.cu): a block takes 32 rows, a lane each, and 16 columns; its warps share an item's partials
-// out, four in flight each, and add up in order.  Partials lie column of four after column, [slot][d / 4][RB].
+// The same where rows are many (attend_tc.cu): a task is 32 rows, a lane each, and four columns, which lie side by side in a
+// partial ([slot][d / 4][RB]). 2^by of a block's warps share a task's partials, eight of them in flight for each, and the
+// first joins what they found.
+constexpr int kRowWarps = 8;
+
 template <int D>
-__global__ void __launch_bounds__(kThreads, 6) attend_finish_rows(const __grid_constant__ AttendArgs a, int rb_shift, int each) {
-  constexpr int CG = D / 16, WARPS = kThreads / 32, kAhead = 4;
-  __shared__ float2 stat[WARPS][32];
-  __shared__ float4 sums[WARPS][4][32];
+__global__ void __launch_bounds__(kRowWarps * 32, 3) attend_finish_rows(const __grid_constant__ AttendArgs a, int rb_shift, int each, int by, Div by_groups, Div by_blocks) {
+  constexpr int C4 = D / 4, kAhead = 8;
+  __shared__ float4 s_acc[kRowWarps][32];
+  __shared__ float2 s_stat[kRowWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, RB = 1 << rb_shift, blocks = (a.rows + RB - 1) >> rb_shift;
-  const int per_item = (min(a.rows, RB) + 31) / 32 * CG, all = a.c.units * blocks * per_item;
+  const int groups = (min(a.rows, RB) + 31) / 32;
+  const int i = (blockIdx.x * kRowWarps + warp) >> by, mine = warp & ((1 << by) - 1);
+  const int c4 = i % C4, rest = i / C4, item = quotient(rest, by_groups), row0 = (rest - item * groups) * 32;
+  const int u = quotient(item, by_blocks), rb = item - u * blocks, row = row0 + lane, r = rb * RB + row;
+  bool live = u < a.c.units && rb * RB + row0 < a.rows;
   pdl_trigger();
   pdl_wait();
-  const int W1 = a.unit_start[a.c.units];
-  if (W1 == 0) return;
-  const Shares sh = shares_of(W1 * blocks, a.ctas, a.by_ctas, a.least);
+  float M = -INFINITY, L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto join = [&](float2 s, float4 x, float ref) {
+    if (s.x == -INFINITY && s.y == 0.f) return;                   // (was not written)
+    const float w = fast_exp2(s.x - ref);
+    L = fmaf(w, s.y, L);
+    acc.x = fmaf(w, x.x, acc.x); acc.y = fmaf(w, x.y, acc.y); acc.z = fmaf(w, x.z, acc.z); acc.w = fmaf(w, x.w, acc.w);
+  };
+  if (live) {
+    const int W1 = a.unit_start[a.c.units], start = a.unit_start[u], places = a.unit_start[u + 1] - start;
+    live = places != 0;
+    if (live) {
+      const Shares sh = shares_of(W1 * blocks, a.ctas, a.by_ctas, a.least);
+      const Parts p = parts_of(sh, item, start * blocks + rb * places, places, each);
+      const int share = (p.count + (1 << by) - 1) >> by, begin = p.first + mine * share;
+      const int left = min(share, p.count - mine * share);
+      const float2* st = a.part_stat + ((size_t)begin << rb_shift) + row;
+      const float4* from = (const float4*)a.part_out + (((size_t)begin * C4 + c4) << rb_shift) + row;
 #pragma unroll 1
-  for (int i = blockIdx.x; i < all; i += gridDim.x) {
-    const int item = i / per_item, part = i - item * per_item, row0 = part / CG * 32, col0 = part % CG * 4;   // (columns of four)
-    const int u = blocks > 1 ? item / blocks : item, rb = item - u * blocks, row = row0 + lane, r = rb * RB + row;
-    const int start = a.unit_start[u], places = a.unit_start[u + 1] - start;
-    if (places == 0 || rb * RB + row0 >= a.rows) continue;
-    const Parts p = parts_of(sh, item, start * blocks + rb * places, places, each);
-    const float2* const st = a.part_stat + ((size_t)p.first << rb_shift) + row;
-    const float4* const from = (const float4*)a.part_out + (((size_t)p.first * (D / 4) + col0) << rb_shift) + row;
-    float M = -INFINITY, L = 0.f;
-    float4 acc[4];
+      for (int c = 0; c < left; c += kAhead) {
+        float2 s[kAhead];
+        float4 x[kAhead];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    for (int c0 = warp; c0 < p.count; c0 += WARPS * kAhead) {
-      float2 s[kAhead];
-      float4 x[kAhead][4];
+        for (int k = 0; k < kAhead; ++k)
+          if (c + k < left) {
+            s[k] = st[(size_t)k << rb_shift];
+            x[k] = from[(size_t)(k * C4) << rb_shift];
+          }
+        st += (size_t)kAhead << rb_shift;
+        from += (size_t)(kAhead * C4) << rb_shift;
+        float top = M;
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int c = min(c0 + k * WARPS, p.count - 1);
-        s[k] = st[(size_t)c << rb_shift];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[k][e] = from[((size_t)c * (D / 4) + e) << rb_shift];
-      }
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        if (r >= a.rows || c0 + k * WARPS >= p.count || (s[k].x == -INFINITY && s[k].y == 0.f)) continue;   // (the last: not written)
-        const float top = fmaxf(M, s[k].x), ref = top == -INFINITY ? 0.f : top, f = fast_exp2(M - ref), w = fast_exp2(s[k].x - ref);
-        M = top;
-        L = fmaf(L, f, s[k].y * w);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          acc[e].x = fmaf(acc[e].x, f, w * x[k][e].x); acc[e].y = fmaf(acc[e].y, f, w * x[k][e].y);
-          acc[e].z = fmaf(acc[e].z, f, w * x[k][e].z); acc[e].w = fmaf(acc[e].w, f, w * x[k][e].w);
+        for (int k = 0; k < kAhead; ++k) {
+          if (c + k >= left || r >= a.rows) s[k] = make_float2(-INFINITY, 0.f);
+          top = fmaxf(top, s[k].x);
         }
+        const float ref = top == -INFINITY ? 0.f : top, f = fast_exp2(M - ref);
+        M = top;
+        L *= f;
+        acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) join(s[k], x[k], ref);
       }
     }
-    stat[warp][lane] = make_float2(M, L);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sums[warp][e][lane] = acc[e];
-    __syncthreads();
-    // warp w: column w of the four, all lanes' rows
-    float top = -INFINITY, sum = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, stat[w][lane].x);
-    const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      const float2 s = stat[w][lane];
-      const float f = fast_exp2(s.x - ref);
-      const float4 x = sums[w][warp][lane];
-      sum = fmaf(f, s.y, sum);
-      v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
-    }
-    if (r < a.rows) {
-      const float inv = top == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;   // (a NaN row stays one)
-      const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, tok = quotient(r, a.by_group), h = r - tok * a.group;
-      const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
-      const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x * inv, v.y * inv), hi = __floats2bfloat162_rn(v.z * inv, v.w * inv);
-      *(uint2*)(a.out + (q * D + (col0 + warp) * 4) * 2) = make_uint2(*(const uint32_t*)&lo, *(const uint32_t*)&hi);
-      if (col0 == 0 && warp == 0 && a.lse) a.lse[q] = bits_of(make_float2(top, sum)) * kLn2;
-    }
-    __syncthreads();
   }
+  if (by) {
+    if (mine) {
+      s_acc[warp][lane] = acc;
+      s_stat[warp][lane] = make_float2(M, L);
+    }
+    __syncthreads();
+    if (mine) return;
+    float top = M;
+    for (int k = 1; k < 1 << by; ++k) top = fmaxf(top, s_stat[warp + k][lane].x);
+    const float ref = top == -INFINITY ? 0.f : top, f = fast_exp2(M - ref);
+    M = top;
+    L *= f;
+    acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+    for (int k = 1; k < 1 << by; ++k) join(s_stat[warp + k][lane], s_acc[warp + k][lane], ref);
+  }
+  if (!live || r >= a.rows) return;
+  const float inv = M == -INFINITY && L == 0.f ? 0.f : 1.f / L;   // (a NaN row stays one)
+  const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, tok = quotient(r, a.by_group), h = r - tok * a.group;
+  const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+  *(uint2*)(a.out + (q * D + c4 * 4) * 2) = make_uint2(*(const uint32_t*)&lo, *(const uint32_t*)&hi);
+  if (c4 == 0 && a.lse) a.lse[q] = bits_of(make_float2(M, L)) * kLn2;
 }
 
 int log2_of(int x) {
@@ -286,8 +294,14 @@ cudaError_t launch(const AttendArgs& a, const AttendPlan& p, int ctas, cudaStrea
 
 cudaError_t launch_attend_finish(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st) {
   const int ctas = 4 * ctx.sm_count;
-  if (p.rb >= 128)
-    return launch_pdl(ctx.cfg.head_dim == 128 ? attend_finish_rows<128> : attend_finish_rows<64>, dim3(ctas), dim3(kThreads), 0, st, a, log2_of(p.rb), p.parts);
+  if (p.rb >= 128) {
+    const int blocks = (a.rows + p.rb - 1) / p.rb, groups = (std::min(a.rows, p.rb) + 31) / 32;
+    const long long tasks = (long long)a.c.units * blocks * groups * (ctx.cfg.head_dim / 4);
+    int by = 0;                                                   // (as many warps as the SMs hold, up to a block a task)
+    while (by < 3 && tasks << by < 16 * ctx.sm_count) ++by;
+    return launch_pdl(ctx.cfg.head_dim == 128 ? attend_finish_rows<128> : attend_finish_rows<64>, dim3((unsigned)((((tasks << by)) + kRowWarps - 1) / kRowWarps)),
+                      dim3(kRowWarps * 32), 0, st, a, log2_of(p.rb), p.parts, by, div_by(groups), div_by(blocks));
+  }
   if (ctx.cfg.dtype == STRUCTKV_BF16)
     return ctx.cfg.head_dim == 128 ? launch<128, true>(a, p, ctas, st) : launch<64, true>(a, p, ctas, st);
   return ctx.cfg.head_dim == 128 ? launch<128, false>(a, p, ctas, st) : launch<64, false>(a, p, ctas, st);
