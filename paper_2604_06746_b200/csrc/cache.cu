@@ -1,11 +1,15 @@
 // Rows that come into a compacted cache, are moved in it, and go: append, commit, evict.
+#include <algorithm>
+
 #include "attend.cuh"
 #include "radix.cuh"
 
 namespace skv {
 namespace {
 
-// A block per unit: rows of the new tokens to slots lengths[u] and up, with their positions and weight 0.
+// Rows of the new tokens to slots lengths[u] and up, with their positions and weight 0: gridDim.y blocks a unit take kAppend
+// tokens each, in turn.  (One block a unit took 12 us for 128 units of 128 tokens.)
+constexpr int kAppend = 16;
 __global__ void __launch_bounds__(256) append(const __grid_constant__ CacheView c, const __grid_constant__ NewRows r, int n_new) {
   pdl_trigger();
   pdl_wait();
@@ -13,16 +17,19 @@ __global__ void __launch_bounds__(256) append(const __grid_constant__ CacheView 
   if (n < 0) return;
   const int per_row = c.row_bytes / 16, shift = per_row == 8 ? 3 : per_row == 16 ? 4 : 5;      // (64 or 128 elements of 2 or 4 bytes)
   const size_t off = unit_offset(c, u) + (size_t)n * c.s_token, from = (size_t)b * r.s_batch + (size_t)g * r.s_head;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n_new << (shift + 1); i += blockDim.x) {
-    const int tok = i >> (shift + 1), ch = i & (per_row - 1);
-    const bool is_v = i >> shift & 1;
-    *(uint4*)((is_v ? c.v : c.k) + off + (size_t)tok * c.s_token + ch * 16) = *(const uint4*)((is_v ? r.v : r.k) + from + (size_t)tok * r.s_token + ch * 16);
-  }
   const size_t w = (size_t)u * c.capacity + n;
-  for (int i = threadIdx.x; i < n_new; i += blockDim.x) {
-    c.positions[w + i] = r.positions[(size_t)b * n_new + i];
-    if (c.weights) c.weights[w + i] = 0.f;
+  for (int t0 = blockIdx.y * kAppend; t0 < n_new; t0 += gridDim.y * kAppend) {
+    const int count = min(kAppend, n_new - t0);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < count << (shift + 1); i += blockDim.x) {
+      const int tok = t0 + (i >> (shift + 1)), ch = i & (per_row - 1);
+      const bool is_v = i >> shift & 1;
+      *(uint4*)((is_v ? c.v : c.k) + off + (size_t)tok * c.s_token + ch * 16) = *(const uint4*)((is_v ? r.v : r.k) + from + (size_t)tok * r.s_token + ch * 16);
+    }
+    if (threadIdx.x < count) {
+      c.positions[w + t0 + threadIdx.x] = r.positions[(size_t)b * n_new + t0 + threadIdx.x];
+      if (c.weights) c.weights[w + t0 + threadIdx.x] = 0.f;
+    }
   }
 }
 
@@ -91,14 +98,20 @@ __global__ void __launch_bounds__(256) commit(const __grid_constant__ CacheView 
 // moves at most E rows, where a compaction in order would move up to `budget`.
 //
 // The threshold is found as in select.cu (radix.cuh); lists of both sets are taken kList entries at a time.
-constexpr int kItems = 8, kList = 4096;
+//
+// Where one token goes, which is what a step of decoding asks for, there is no rank to search: it is the last of the lowest.
+// A thread holds kItems tokens of a chunk: 8 where the capacity fits them or holds more than a chunk of 16, with two blocks an SM,
+// else 16 with one.  (A unit of 8320 tokens was read anew for each level with 8.)
+constexpr int kList = 4096;
 struct EvictShared {
   RadixShared<1> radix;
   unsigned counts[3][32];
   int newest[32];
+  unsigned low[2][32];
 };
 
-__global__ void __launch_bounds__(kRxThreads, 2) evict(const __grid_constant__ CacheView c, int budget, int recent) {
+template <int kItems>
+__global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const __grid_constant__ CacheView c, int budget, int recent) {
   extern __shared__ __align__(16) unsigned char smem[];
   EvictShared& s = *reinterpret_cast<EvictShared*>(smem);
   int* const lists = reinterpret_cast<int*>(&s.radix);                // [2][kList], once the threshold is known
@@ -113,34 +126,80 @@ __global__ void __launch_bounds__(kRxThreads, 2) evict(const __grid_constant__ C
   const float* const wt = c.weights + (size_t)u * c.capacity;
   constexpr int kChunk = kRxThreads * kItems;
   const int chunks = (n + kChunk - 1) / kChunk;                       // more than one: the unit does not fit the registers
+  unsigned key[kItems];
+  int mine = 0;
+  // a warp's tokens are consecutive; item e of this thread: first + 32 e
+  auto token_of = [&](int ch) { return ch * kChunk + warp * (32 * kItems) + lane; };
+  int p[kItems];
+  auto fetch = [&](int ch) {
+    const int first = token_of(ch);
+    mine = min(kItems, (n - first + 31) >> 5);
+#pragma unroll
+    for (int e = 0; e < kItems; ++e) {
+      key[e] = e < mine ? __float_as_uint(wt[first + 32 * e]) : 0u;
+      p[e] = e < mine ? pos[first + 32 * e] : -1;
+    }
+  };
   int newest = -1;
-#pragma unroll 8
-  for (int j = tid; j < n; j += kRxThreads) newest = max(newest, pos[j]);
+  for (int ch = 0; ch < chunks; ++ch) {
+    fetch(ch);
+#pragma unroll
+    for (int e = 0; e < kItems; ++e) newest = max(newest, p[e]);
+  }
   newest = __reduce_max_sync(0xffffffffu, newest);
   if (lane == 0) s.newest[warp] = newest;
   __syncthreads();
   newest = __reduce_max_sync(0xffffffffu, s.newest[lane]);
   const long long line = (long long)newest - recent;
-
-  unsigned key[kItems];
-  int mine = 0;
-  // a warp's tokens are consecutive; item e of this thread: first + 32 e
-  auto token_of = [&](int ch) { return ch * kChunk + warp * (32 * kItems) + lane; };
-  auto load = [&](int ch) {
-    const int first = token_of(ch);
-    mine = min(kItems, (n - first + 31) >> 5);
-    float v[kItems];
-    int p[kItems];
+  // (a NaN weight, all bits set, comes below the recent ones)
+  auto keys = [&] {
 #pragma unroll
-    for (int e = 0; e < kItems; ++e) {
-      v[e] = e < mine ? wt[first + 32 * e] : 0.f;
-      p[e] = e < mine ? pos[first + 32 * e] : 0;
-    }
-    // (a NaN weight, all bits set, comes below the recent ones)
-#pragma unroll
-    for (int e = 0; e < kItems; ++e) key[e] = p[e] > line ? 0xffffffffu : min(order_key(v[e]), 0xfffffffeu);
+    for (int e = 0; e < kItems; ++e) key[e] = p[e] > line ? 0xffffffffu : min(order_key(__uint_as_float(key[e])), 0xfffffffeu);
   };
-  if (chunks == 1) load(0);
+  auto load = [&](int ch) {
+    fetch(ch);
+    keys();
+  };
+  const size_t off = unit_offset(c, u);
+  const int per_row = c.row_bytes / 16, row_shift = per_row == 8 ? 3 : per_row == 16 ? 4 : 5;
+  if (chunks == 1) keys();
+  if (n - budget == 1) {
+    unsigned low = 0xffffffffu;
+    int at = -1;
+    for (int ch = 0; ch < chunks; ++ch) {
+      if (chunks > 1) load(ch);
+      const int first = token_of(ch);
+#pragma unroll
+      for (int e = 0; e < kItems; ++e)
+        if (e < mine && key[e] <= low) {
+          low = key[e];
+          at = first + 32 * e;
+        }
+    }
+    const unsigned low_warp = __reduce_min_sync(0xffffffffu, low);
+    at = __reduce_max_sync(0xffffffffu, low == low_warp ? at : -1);
+    if (lane == 0) {
+      s.low[0][warp] = low_warp;
+      s.low[1][warp] = (unsigned)at;
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    low = s.low[0][lane];
+    const unsigned lowest = __reduce_min_sync(0xffffffffu, low);
+    at = __reduce_max_sync(0xffffffffu, low == lowest ? (int)s.low[1][lane] : -1);
+    if (at != budget) {
+      for (int i = lane; i < 2 << row_shift; i += 32) {
+        char* const col = (i >> row_shift ? c.v : c.k) + off + (i & (per_row - 1)) * 16;
+        *(uint4*)(col + (size_t)at * c.s_token) = *(const uint4*)(col + (size_t)budget * c.s_token);
+      }
+      if (lane == 0) {
+        c.positions[(size_t)u * c.capacity + at] = pos[budget];
+        c.weights[(size_t)u * c.capacity + at] = wt[budget];
+      }
+    }
+    if (lane == 0) c.lengths[u] = budget;
+    return;
+  }
   unsigned thr = 0, remaining = (unsigned)budget, above = 0, need_eq = 0;
   int level = 0;
 #pragma unroll 1
@@ -164,8 +223,6 @@ __global__ void __launch_bounds__(kRxThreads, 2) evict(const __grid_constant__ C
   // Entries [lo, lo + kList) of both lists, then their tokens.  Where the lists are longer, the last entries come first: the
   // tokens moved then lie above all that is still to be listed, and the copies that moved count as kept, equal ones before
   // the kept ones that remain, as many as were kept behind them.
-  const size_t off = unit_offset(c, u);
-  const int per_row = c.row_bytes / 16;
   bool sized = false;
   for (int lo = 0; lo >= 0;) {
     __syncthreads();
@@ -225,16 +282,28 @@ __global__ void __launch_bounds__(kRxThreads, 2) evict(const __grid_constant__ C
     }
     sized = true;
     const int here = min(kList, moves - lo);
-    for (int i = tid; i < here * 2 * per_row; i += kRxThreads) {
-      const int row = i / (2 * per_row), ch = i % (2 * per_row);
-      char* const col = (ch < per_row ? c.k : c.v) + off + (size_t)(ch < per_row ? ch : ch - per_row) * 16;
-      *(uint4*)(col + (size_t)lists[row] * c.s_token) = *(const uint4*)(col + (size_t)lists[kList + row] * c.s_token);
+    constexpr int kGo = 4;
+    for (int i0 = tid; i0 < here << (row_shift + 1); i0 += kGo * kRxThreads) {
+      uint4 x[kGo];
+      char* col[kGo];
+#pragma unroll
+      for (int e = 0; e < kGo; ++e) {
+        const int i = i0 + e * kRxThreads, row = i >> (row_shift + 1);
+        if (row < here) {
+          col[e] = (i >> row_shift & 1 ? c.v : c.k) + off + (i & (per_row - 1)) * 16;
+          x[e] = *(const uint4*)(col[e] + (size_t)lists[kList + row] * c.s_token);
+          col[e] += (size_t)lists[row] * c.s_token;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < kGo; ++e)
+        if ((i0 + e * kRxThreads) >> (row_shift + 1) < here) *(uint4*)col[e] = x[e];
     }
-    int* const p = c.positions + (size_t)u * c.capacity;
-    float* const w = c.weights + (size_t)u * c.capacity;
+    int* const to_pos = c.positions + (size_t)u * c.capacity;
+    float* const to_wt = c.weights + (size_t)u * c.capacity;
     for (int i = tid; i < here; i += kRxThreads) {
-      p[lists[i]] = p[lists[kList + i]];
-      w[lists[i]] = w[lists[kList + i]];
+      to_pos[lists[i]] = pos[lists[kList + i]];
+      to_wt[lists[i]] = wt[lists[kList + i]];
     }
     lo -= kList;
   }
@@ -244,14 +313,17 @@ __global__ void __launch_bounds__(kRxThreads, 2) evict(const __grid_constant__ C
 }  // namespace
 
 cudaError_t launch_append(const CacheView& c, const NewRows& r, int n_new, cudaStream_t st) {
-  return launch_pdl(append, dim3(c.units), dim3(256), 0, st, c, r, n_new);
+  return launch_pdl(append, dim3(c.units, std::min((n_new + kAppend - 1) / kAppend, 64)), dim3(256), 0, st, c, r, n_new);
 }
 cudaError_t launch_commit(const CacheView& c, int n_new, const int* counts, const int* path, cudaStream_t st) {
   return launch_pdl(commit, dim3(c.units), dim3(256), 0, st, c, n_new, counts, path);
 }
 cudaError_t launch_evict(const CacheView& c, int budget, int recent, cudaStream_t st) {
-  const cudaError_t e = allow_smem<evict>((int)sizeof(EvictShared));
-  return e != cudaSuccess ? e : launch_pdl(evict, dim3(c.units), dim3(kRxThreads), sizeof(EvictShared), st, c, budget, recent);
+  auto go = [&](auto kernel, cudaError_t e) {
+    return e != cudaSuccess ? e : launch_pdl(kernel, dim3(c.units), dim3(kRxThreads), sizeof(EvictShared), st, c, budget, recent);
+  };
+  if (c.capacity > 8 * kRxThreads && c.capacity <= 16 * kRxThreads) return go(evict<16>, allow_smem<evict<16>>((int)sizeof(EvictShared)));
+  return go(evict<8>, allow_smem<evict<8>>((int)sizeof(EvictShared)));
 }
 
 }  // namespace skv
