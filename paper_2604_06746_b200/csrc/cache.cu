@@ -127,13 +127,16 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
   constexpr int kChunk = kRxThreads * kItems;
   const int chunks = (n + kChunk - 1) / kChunk;                       // more than one: the unit does not fit the registers
   unsigned key[kItems];
-  int mine = 0;
-  // a warp's tokens are consecutive; item e of this thread: first + 32 e
-  auto token_of = [&](int ch) { return ch * kChunk + warp * (32 * kItems) + lane; };
+  int mine = 0, items = 0;
+  // a warp's tokens are consecutive, as many for every warp; item e of this thread: first + 32 e
+  auto token_of = [&](int ch) {
+    items = min(kItems, (n - ch * kChunk + kRxThreads - 1) / kRxThreads);
+    return ch * kChunk + warp * (32 * items) + lane;
+  };
   int p[kItems];
   auto fetch = [&](int ch) {
     const int first = token_of(ch);
-    mine = min(kItems, (n - first + 31) >> 5);
+    mine = min(items, (n - first + 31) >> 5);
 #pragma unroll
     for (int e = 0; e < kItems; ++e) {
       key[e] = e < mine ? __float_as_uint(wt[first + 32 * e]) : 0u;
@@ -209,7 +212,7 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
       if (chunks > 1) load(ch);
 #pragma unroll
       for (int e = 0; e < kItems; ++e)
-        radix_count(s.radix, level, radix_digit(key[e], level), e < mine && (key[e] & mask) == thr);
+        if (e < items) radix_count(s.radix, level, radix_digit(key[e], level), e < mine && (key[e] & mask) == thr);
     }
     unsigned digit, in;
     radix_pick(s.radix, level, remaining, digit, in);
@@ -233,7 +236,8 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
       unsigned eq = 0;
       if (need_eq) {
 #pragma unroll
-        for (int e = 0; e < kItems; ++e) eq += __popc(__ballot_sync(0xffffffffu, e < mine && key[e] == thr));
+        for (int e = 0; e < kItems; ++e)
+          if (e < items) eq += __popc(__ballot_sync(0xffffffffu, e < mine && key[e] == thr));
         if (lane == 0) s.counts[0][warp] = eq;
         __syncthreads();
         const unsigned incl = warp_scan(s.counts[0][lane], lane);
@@ -244,6 +248,7 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
       unsigned is_free = 0, is_move = 0, n_free = 0, n_move = 0;      // bits: item e
 #pragma unroll
       for (int e = 0; e < kItems; ++e) {
+        if (e >= items) break;
         const bool there = e < mine, equal = there && need_eq && key[e] == thr;
         const unsigned be = __ballot_sync(0xffffffffu, equal);
         const bool kept = there && (key[e] > above || (equal && eq + __popc(be & below) < need_eq));
@@ -264,6 +269,7 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
       run_move += __shfl_sync(0xffffffffu, mi, 31);
 #pragma unroll
       for (int e = 0; e < kItems; ++e) {
+        if (e >= items) break;
         const bool fr = is_free >> e & 1, mv = is_move >> e & 1;
         const unsigned bf = __ballot_sync(0xffffffffu, fr), bm = __ballot_sync(0xffffffffu, mv);
         const unsigned fa = f_at + __popc(bf & below) - lo, ma = m_at + __popc(bm & below) - lo;
