@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
 // ---- weights of accepted tokens ------------------------------------------------------------------
 // weights[j] = decay weights[j] + sum over accepted rows of 2^(x - lse): K tiles stream past the accepted tokens' rows
 // (kWeighRows at a time in shared memory); a warp has 16 keys of a tile in registers and adds up their rows.
-constexpr int kWeighRows = 64, kWeighStages = 8, kWeighGroups = 2, kWeighWarps = 4 * kWeighGroups;
+constexpr int kWeighRows = 64, kWeighStages = 8, kWeighGroups = 4, kWeighWarps = 4 * kWeighGroups;
 static_assert(kWeighStages % kWeighGroups == 0, "a place of the ring serves one group");
 
 template <int D>
@@ -512,6 +512,8 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
         if (n % kWeighGroups != grp) continue;
         const int st = n % ST;
         const uint32_t from = base + st * kStage;
+        const int j_mine = t * kTileKeys + kw * 16 + g8 + 8 * t4;   // lane t4 = y of the four has key g8 + 8 y
+        const float before = t4 < 2 && j_mine < sg.keys ? w[j_mine] : 0.f;
         mbar_wait(full(st), (n / ST) & 1, abort_flag);
         const int* const kp = (const int*)(sm + st * kStage + kTileBytes) + kw * 16;
         int pos[2] = {0, 0};
@@ -555,10 +557,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
           sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 1);
           sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], 2);
         }
-        if (t4 < 2) {                                             // lane t4 = y of the four has key g8 + 8 y
-          const int j = j0 + g8 + 8 * t4;
-          if (j < sg.keys) w[j] = (round == 0 ? a.decay * w[j] : w[j]) + (t4 ? sum[1] : sum[0]);
-        }
+        if (t4 < 2 && j_mine < sg.keys) w[j_mine] = (round == 0 ? a.decay * before : before) + (t4 ? sum[1] : sum[0]);
       }
       if (rounds > 1) __threadfence_block();                      // (another warp may have the key in the next round)
     }
