@@ -458,13 +458,17 @@ class Context:
             "the cache has another shape or dtype than the context"
         return cache.native
 
-    def attend_workspace(self, cache: Cache, n_new: int) -> torch.Tensor:
-        """A workspace for ``attend`` with ``n_new`` new tokens a sequence over ``cache``."""
+    def attend_workspace_bytes(self, cache: Cache, n_new: int) -> int:
+        """structkv_attend_workspace_bytes for ``n_new`` new tokens a sequence over ``cache``."""
         self._of(cache)
         n = lib.structkv_attend_workspace_bytes(ctypes.byref(self.cfg), cache.batch, n_new, cache.capacity)
         if n == 0:
             raise StructKVError(ERR_INVALID_ARG, "structkv_attend_workspace_bytes")
-        return torch.empty(n, dtype=torch.uint8, device=cache.device)
+        return n
+
+    def attend_workspace(self, cache: Cache, n_new: int) -> torch.Tensor:
+        """A workspace for ``attend`` with ``n_new`` new tokens a sequence over ``cache``."""
+        return torch.empty(self.attend_workspace_bytes(cache, n_new), dtype=torch.uint8, device=cache.device)
 
     def append(self, cache: Cache, k_new: torch.Tensor, v_new: torch.Tensor, positions: torch.Tensor,
                stream: Optional[torch.cuda.Stream] = None) -> None:

@@ -512,7 +512,8 @@ cudaError_t launch_one(const AttendArgs& a, const CacheMaps& m, cudaStream_t st)
 }
 template <int D>
 cudaError_t launch_d(const AttendArgs& a, const AttendPlan& p, const CacheMaps& m, cudaStream_t st) {
-  const bool opt = a.cap2 != 0.f || a.slopes;
+  // (without options the largest product is the largest logit and a masked one minus infinity: for a positive scale)
+  const bool opt = a.cap2 != 0.f || a.slopes || !(a.scale2 > 0.f);
   if (p.rb == 256) return opt ? launch_one<D, 2, true>(a, m, st) : launch_one<D, 2, false>(a, m, st);
   return opt ? launch_one<D, 1, true>(a, m, st) : launch_one<D, 1, false>(a, m, st);
 }

@@ -205,3 +205,100 @@ class Prefill:
             self._layers_ws = self.ctx.layers_workspace(L)
             a.layers_workspace, a.layers_workspace_bytes = self._layers_ws.data_ptr(), self._layers_ws.numel()
         return a
+
+
+class Decode:
+    """Decoding over what a Prefill kept (the paper stops at the compacted cache).  A token's step is ``step`` for every layer, then
+    ``advance``; drafted tokens, a tree of them or a chain, are looked at by ``verify`` for every layer, then ``accept`` keeps
+    some.  Cached tokens gather the attention weight that new ones give them; with a ``budget`` every KV head keeps its
+    ``recent`` newest tokens and the heaviest others.  All layers of all sequences are in one cache (sequence ``layer * batch +
+    b``), so that commit and eviction are one launch each; every call can be captured into a graph."""
+
+    def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, capacity: int, dtype: torch.dtype,
+                 batch: int = 1, budget: int = 0, recent: int = 0, max_new: int = 1, softcap: float = 0.0,
+                 slopes: Optional[torch.Tensor] = None, decay: float = 1.0, device: str = "cuda:0"):
+        if not 1 <= max_new <= binding.MAX_NEW:
+            raise ValueError(f"max_new: 1 to {binding.MAX_NEW} new tokens")
+        if budget < 0 or recent < 0 or (budget or 1) + max_new > capacity:
+            raise ValueError("capacity: room for the budget and max_new tokens behind it")
+        self.L, self.B, self.max_new = n_layers, batch, max_new
+        self.budget, self.recent, self.softcap, self.slopes, self.decay = budget, recent, softcap, slopes, decay
+        self.ctx = binding.Context(n_q_heads, n_kv_heads, head_dim, 8, 8, dtype, device)
+        dev, f32, i32 = torch.device(device), torch.float32, torch.int32
+        rows = (n_layers * batch, n_kv_heads, capacity)
+        k, v = (torch.empty(rows + (head_dim,), dtype=dtype, device=dev) for _ in range(2))
+        positions, weights = torch.zeros(rows, dtype=i32, device=dev), torch.zeros(rows, dtype=f32, device=dev)
+        lengths = torch.zeros(rows[:2], dtype=i32, device=dev)
+        self.cache = binding.Cache(k, v, positions, weights, lengths)
+        self.layers = [binding.Cache(*(t[l * batch:(l + 1) * batch] for t in (k, v, positions, weights, lengths)))
+                       for l in range(n_layers)]
+        self.lse = torch.empty((n_layers, batch, max_new, n_q_heads), dtype=f32, device=dev)
+        self._ws = self.ctx.attend_workspace(self.layers[0], 1)
+        for t in range(2, max_new + 1):                      # (not always more for more tokens)
+            if self.ctx.attend_workspace_bytes(self.layers[0], t) > self._ws.numel():
+                self._ws = self.ctx.attend_workspace(self.layers[0], t)
+        self._seen: List[Optional[tuple]] = [None] * n_layers
+
+    def take(self, prefill: Prefill, sequence: int = 0, positions: Optional[torch.Tensor] = None) -> None:
+        """Sequence ``sequence`` begins with the prompt that ``prefill`` compacted: its K and V, its tokens' positions (``positions
+        [L, kv_budget]`` int32; None: the prompt's indices) and, as the weight that they start with, the saliency that selected
+        them."""
+        n = prefill.kv_budget
+        if not prefill.keep_kv or (prefill.L, prefill.Hkv, prefill.d, prefill.dtype) != (
+                self.L, self.cache.n_kv_heads, self.cache.head_dim, self.cache.dtype):
+            raise ValueError("take: a Prefill of these layers, heads and type that keeps K and V")
+        if n > self.cache.capacity - self.max_new:
+            raise ValueError("take: capacity for the prompt's tokens and max_new behind them")
+        if not 0 <= sequence < self.B:
+            raise ValueError("take: no such sequence")
+        at = slice(sequence, None, self.B)
+        c, start = self.cache, torch.empty((self.L, 1, n, 1), dtype=torch.float32, device=self.cache.device)
+        for lo in range(0, self.L, 128):
+            hi = min(self.L, lo + 128)
+            prefill.ctx.compact_layers([s[None, :, None] for s in prefill.s_hist[lo:hi]], prefill.i_kv[lo:hi], start[lo:hi])
+        c.k[at, :, :n], c.v[at, :, :n] = prefill.k_out, prefill.v_out
+        c.positions[at, :, :n] = (prefill.i_kv if positions is None else positions)[:, None]
+        c.weights[at, :, :n] = start[:, :, :, 0]
+        c.lengths[at] = n
+
+    def step(self, layer: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, positions: torch.Tensor,
+             scale: float, out: torch.Tensor) -> None:
+        """One token a sequence, ``q``, ``out [batch, 1, H, d]``, ``k_new``, ``v_new [batch, 1, H_kv, d]``: it is appended, attends,
+        and its attention weight is added."""
+        self.ctx.attend(self.layers[layer], q, scale, out, self._ws, k_new=k_new, v_new=v_new, positions=positions,
+                        softcap=self.softcap, slopes=self.slopes, accumulate=True, decay=self.decay)
+
+    def advance(self, n_new: int = 1) -> None:
+        """After the last layer: the new tokens stay, and every KV head goes back to its budget."""
+        self.ctx.commit(self.cache, n_new)
+        self._evict()
+
+    def verify(self, layer: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, positions: torch.Tensor,
+               scale: float, out: torch.Tensor, tree: Optional[torch.Tensor] = None) -> None:
+        """Drafted tokens, ``max_new`` of a sequence at most, see the cache and one another as ``tree`` says (None: those before
+        them).  ``q`` and ``tree`` are looked at again by ``accept``."""
+        n_new = q.shape[1]
+        if n_new > self.max_new:
+            raise ValueError("verify: more tokens than max_new")
+        lse = self.lse[layer].view(-1)[:self.B * n_new * q.shape[2]].view(self.B, n_new, q.shape[2])
+        self.ctx.attend(self.layers[layer], q, scale, out, self._ws, k_new=k_new, v_new=v_new, positions=positions, tree=tree,
+                        softcap=self.softcap, slopes=self.slopes, lse=lse)
+        self._seen[layer] = (q, scale, lse, tree)
+
+    def accept(self, counts: torch.Tensor, path: torch.Tensor) -> None:
+        """After ``verify`` of every layer: sequence b keeps the ``counts[b]`` drafted tokens that ``path[b]`` names, ascending
+        (int32 ``[batch]`` and ``[batch, n_new]``); they give their attention weight, the others leave nothing."""
+        n_new = path.shape[1]
+        if any(s is None or s[0].shape[1] != n_new for s in self._seen):
+            raise ValueError("accept: verify of every layer comes first, of as many tokens")
+        among = torch.arange(n_new, device=path.device)[None] < counts[:, None]
+        words = torch.where(among, torch.ones_like(path, dtype=torch.int64) << path.clamp(0, n_new - 1).long(), 0).sum(1)
+        for cache, (q, scale, lse, tree) in zip(self.layers, self._seen):
+            self.ctx.weigh(cache, q, scale, lse, words, tree=tree, softcap=self.softcap, slopes=self.slopes, decay=self.decay)
+        self.ctx.commit(self.cache, n_new, counts=counts.repeat(self.L), path=path.repeat(self.L, 1))
+        self._seen = [None] * self.L
+        self._evict()
+
+    def _evict(self) -> None:
+        if self.budget:
+            self.ctx.evict(self.cache, self.budget, self.recent)
