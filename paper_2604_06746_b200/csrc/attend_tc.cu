@@ -275,25 +275,38 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
       const int n_old = sg.keys - a.n_new;
       for (int t = max(sg.t0, n_old / kTile); t < sg.t1 && ok; ++t) {
         const int of = MT == 2 ? 0 : (t - sg.t0) & 1, k = MT == 2 ? t - sg.t0 : (t - sg.t0) / 2, st = place_of(of, 2 * ((of ? n[1] : n[0]) + k) + 1);
-        const int row0 = max(0, n_old - t * kTile);
+        const int row0 = max(0, n_old - t * kTile), row1 = min(kTile, sg.keys - t * kTile);
         for (int s = 0; s < 2 && ok; ++s)
           if (MT == 2 || ((t - sg.t0) & 1) == s) ok = mbar_wait_producer(v_look(s), tails[s]++ & 1, abort_flag, kWaitCycles);
         if (!ok) break;
-#pragma unroll 4
-        for (int i = row0 * CH + lane; i < kTile * CH; i += 32) {
-          uint4* const p = (uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH));
-          uint32_t w[4] = {p->x, p->y, p->z, p->w};
+        // (rows behind the last key hold what the cache held there)
+#pragma unroll 8
+        for (int i = row1 * CH + lane; i < kTile * CH; i += 32) *(uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH)) = make_uint4(0, 0, 0, 0);
+        constexpr int kGo = 8;
+#pragma unroll 1
+        for (int i0 = row0 * CH + lane; i0 < row1 * CH; i0 += 32 * kGo) {
+          uint4 x[kGo];
+#pragma unroll
+          for (int e = 0; e < kGo; ++e) {
+            const int i = min(i0 + 32 * e, row1 * CH - 1);
+            x[e] = *(const uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH));
+          }
           bool bad = false;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) bad |= not_finite(w[e]);
+          for (int e = 0; e < kGo; ++e) bad |= not_finite(x[e].x) || not_finite(x[e].y) || not_finite(x[e].z) || not_finite(x[e].w);
           if (bad) {
+            *odd_v = 1;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
-              if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu;
+            for (int e = 0; e < kGo; ++e) {
+              const int i = min(i0 + 32 * e, row1 * CH - 1);
+              uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+#pragma unroll
+              for (int f = 0; f < 4; ++f) {
+                if ((w[f] & 0x7f80u) == 0x7f80u) w[f] &= 0xffff0000u;
+                if ((w[f] & 0x7f800000u) == 0x7f800000u) w[f] &= 0xffffu;
+              }
+              *(uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH)) = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            *p = make_uint4(w[0], w[1], w[2], w[3]);
-            if (t * kTile + i / CH < sg.keys) *odd_v = 1;
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -512,8 +525,8 @@ cudaError_t launch_one(const AttendArgs& a, const CacheMaps& m, cudaStream_t st)
 }
 template <int D>
 cudaError_t launch_d(const AttendArgs& a, const AttendPlan& p, const CacheMaps& m, cudaStream_t st) {
-  // (without options the largest product is the largest logit and a masked one minus infinity: for a positive scale)
-  const bool opt = a.cap2 != 0.f || a.slopes || !(a.scale2 > 0.f);
+  // (without options what is masked is minus infinity before it is scaled: not for a scale of zero)
+  const bool opt = a.cap2 != 0.f || a.slopes || a.scale2 == 0.f;
   if (p.rb == 256) return opt ? launch_one<D, 2, true>(a, m, st) : launch_one<D, 2, false>(a, m, st);
   return opt ? launch_one<D, 1, true>(a, m, st) : launch_one<D, 1, false>(a, m, st);
 }
