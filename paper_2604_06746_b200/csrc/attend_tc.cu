@@ -138,6 +138,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   auto v_ready = [&](int s) { return more + 80 + 8 * s; };
   auto drained = [&](int s) { return more + 96 + 8 * s; };
   auto turn = [&](int s) { return more + 112 + 8 * s; };
+  auto p_half = [&](int s) { return more + 160 + 8 * s; };       // (behind the words)
   const uint32_t q_full = more + 128, q_empty = more + 136;
   volatile int* const words = (volatile int*)(sm + kBars + 16 * NU + 144);
   volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v: some new token's V was not finite
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   if (tid == 0) {
     for (int i = 0; i < NU; ++i) { mbar_init(full(i), S::kPos ? 33 : 1); mbar_init(empty(i), MT); }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(s_full(s), 1); mbar_init(p_ready(s), 4); mbar_init(o_done(s), 1); mbar_init(o_free(s), 4);
+      mbar_init(s_full(s), 1); mbar_init(p_half(s), 4); mbar_init(p_ready(s), 4); mbar_init(o_done(s), 1); mbar_init(o_free(s), 4);
       mbar_init(v_look(s), 1); mbar_init(v_ready(s), 32); mbar_init(drained(s), 1); mbar_init(turn(s), 4);
     }
     mbar_init(q_full, 256);
@@ -249,12 +250,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
         const bool tail = (sg.t0 + t + 1) * kTile > n_old;
         if (tail && lead) mbar_arrive(v_look(s));
         if (k == 0 && used++ > 0 && !(ok = wait(o_free(s), used & 1))) break;
-        if (!(ok = wait(p_ready(s), done & 1))) break;
         if (tail && !(ok = wait(v_ready(s), tails++ & 1))) break;
-        tc_fence_after();
         const uint32_t vd = v_lo + ((st * S::kUnit) >> 4);
+        // the first half of the keys beside the exponentials of the second
+        if (!(ok = wait(p_half(s), done & 1))) break;
+        tc_fence_after();
 #pragma unroll
-        for (int kk = 0; kk < kTile / 16; ++kk) mma_ts(o_at, s_at + kk * 8, vd + ((kk * 16 * 128) >> 4), hi_v, idesc_o, k > 0 || kk > 0, lead);
+        for (int kk = 0; kk < kTile / 32; ++kk) mma_ts(o_at, s_at + kk * 8, vd + ((kk * 16 * 128) >> 4), hi_v, idesc_o, k > 0 || kk > 0, lead);
+        if (!(ok = wait(p_ready(s), done & 1))) break;
+        tc_fence_after();
+#pragma unroll
+        for (int kk = kTile / 32; kk < kTile / 16; ++kk) mma_ts(o_at, s_at + kk * 8, vd + ((kk * 16 * 128) >> 4), hi_v, idesc_o, 1, lead);
         commit_by(lead, o_done(s));
         commit_by(lead, empty(st));
         ++done;
@@ -446,13 +452,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
               p[e / 2] = bf16x2(p0, p1);
             }
             tmem_st16(s_at + c / 2, p);                          // (over scores, which are in registers)
+            if (c == kTile / 2 - 32) {
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(p_half(s));
+            }
           }
           float s0, s1;
           unpack2(sum, s0, s1);
           l += s0 + s1;
           tmem_st_wait();
-        } else if (MT == 2 && done >= 1 - s && !(ok = wait(turn(s), (done - 1 + s) & 1))) {
-          break;
+        } else {
+          if (MT == 2 && done >= 1 - s && !(ok = wait(turn(s), (done - 1 + s) & 1))) break;
+          if (lane == 0) mbar_arrive(p_half(s));
         }
         tc_fence_before();
         __syncwarp();

@@ -74,7 +74,7 @@ def test_tensor_core_kernel(mt, nu, positions):
         m = Machine(seed)
         full, empty = [Barrier(1) for _ in range(nu)], [Barrier(mt) for _ in range(nu)]
         q_full, q_empty = Barrier(2), Barrier(2)
-        s_full, p_ready, o_done, o_free, v_look, v_ready = ([Barrier(1) for _ in range(2)] for _ in range(6))
+        s_full, p_half, p_ready, o_done, o_free, v_look, v_ready = ([Barrier(1) for _ in range(2)] for _ in range(7))
         turn = [Barrier(1), Barrier(1)]
         copies, mma = [[] for _ in range(nu)], [[], []]
         m.queues = copies + mma
@@ -120,10 +120,11 @@ def test_tensor_core_kernel(mt, nu, positions):
                         if used:
                             yield o_free[s], used - 1
                         used += 1
-                    yield p_ready[s], done
                     if tail:
                         yield v_ready[s], tails
                         tails += 1
+                    yield p_half[s], done
+                    yield p_ready[s], done
                     mma[s] += [o_done[s].arrive, empty[place(s, unit)].arrive]
                     done += 1
                     if k + 1 < jobs:
@@ -156,6 +157,8 @@ def test_tensor_core_kernel(mt, nu, positions):
                         yield o_done[s], done - 1
                     if mt == 2 and done >= 1 - s:
                         yield turn[s], done - 1 + s
+                    p_half[s].arrive()
+                    yield None                            # (others may go on)
                     p_ready[s].arrive()
                     if mt == 2:
                         turn[1 - s].arrive()
