@@ -9,8 +9,9 @@ using namespace skv;
 namespace skv {
 namespace {
 
-// A tile of the tensor cores has 128 rows: from 17 on they take them (single tokens of 17 heads and more stay, 16 at a time, with
-// the kernel that leaves the logits).
+// tcgen05's tiles have 128 rows, attend_mma's 16 at most: from 17 rows on the former takes them (single tokens of 17 heads and more stay,
+// 16 at a time, with the kernel that leaves the logits).  us, 32 heads over 8, attend_mma / attend_tc: 16 rows over 2048 keys 13.3 / 12.6,
+// 4 x 4096 18.8 / 24.7, 8 x 8192 46.8 / 53.4; 20 rows 12.8 / 12.7, 25.2 / 24.9, 73.0 / 53.1; 32 rows 13.4 / 12.8, 27.0 / 24.3, 75.5 / 52.0.
 bool by_tensor_cores(const structkv_config& cfg, int n_new) {
   return cfg.dtype == STRUCTKV_BF16 && n_new > 1 && cfg.n_q_heads / cfg.n_kv_heads * n_new > 16;
 }
@@ -45,7 +46,7 @@ AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, int capacity) {
   if (batch < 1 || capacity < 1 || capacity > 1 << 30 || n_new < 0 || n_new > capacity) return false;
   const long long units = (long long)batch * cfg.n_kv_heads, rows = (long long)cfg.n_q_heads / cfg.n_kv_heads * std::max(1, n_new);
-  return units * rows <= 0x3fffffffll && units * ((rows + 3) / 4) <= 0x7fffffffll / (capacity / 64 + 1 + kOver);
+  return units * rows <= 0x3fffffffll && units * ((rows + 3) / 4) <= 0x7fffffffll / (capacity / 64 + 1 + kOverKeys / 64);
 }
 bool strides_ok(int elem, long long a, long long b, long long c) { return (a * elem) % 16 == 0 && (b * elem) % 16 == 0 && (c * elem) % 16 == 0; }
 
@@ -144,8 +145,10 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
   a.ctas = plan.ctas;
   a.by_ctas = div_by(plan.ctas);
   a.least = plan.least;
+  a.over = kOverKeys / plan.tile;
   cudaStream_t st = (cudaStream_t)stream;
-  // A few rows are appended by the kernel itself; a warp that copies more of them holds its tiles up.
+  // A few rows are appended by the kernel itself (a launch of its own takes 0.9 to 1.3 us more, whatever the keys); a warp that copies
+  // more of them holds its tiles up.
   cudaError_t e = cudaSuccess;
   if (args->rows && c.cfg.dtype == STRUCTKV_BF16 && !tc && args->n_new <= 8) a.fresh = r;
   else if (args->rows) e = launch_append(a.c, r, args->n_new, st);
@@ -162,6 +165,7 @@ structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, c
   if (!view_of(ctx, cache, args->n_new, &a.c) || !cache->weights || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
   a.ctas = ctx->c.cfg.dtype == STRUCTKV_BF16 ? ctx->c.sm_count : 4 * ctx->c.sm_count;   // (CTAs that run at once)
   a.by_ctas = div_by(a.ctas);
+  a.over = kWeighOverKeys / 64;
   return told((ctx->c.cfg.dtype == STRUCTKV_BF16 ? launch_weigh_bf16 : launch_weigh_fp32)(ctx->c, a, accepted, (cudaStream_t)stream));
 }
 

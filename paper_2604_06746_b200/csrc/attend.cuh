@@ -2,7 +2,7 @@
 //
 // A unit is (sequence, KV head) u = b H_kv + g, with lengths[u] + n_new keys (the new tokens are the last ones) and rows
 // r = i G + h, new token i and head h of the group.  An item is a unit's block of up to RB rows over all of its keys; items
-// follow one another unit after unit, and their key tiles, behind kOver places for what an item costs beside them, form one sequence of
+// follow one another unit after unit, and their key tiles, behind the places of 512 keys for what an item costs beside them, form one sequence of
 // W places.  C CTAs take runs of it whose lengths differ by one place at most: every CTA has equally much to do whatever the lengths,
 // which only the device knows.  (Without the places for the items' own cost 16 sequences of 1 to 5003 tokens took 45 us: a CTA that
 // got eight KV heads of one token was busy for 38, the others for 20.)  What a CTA has of
@@ -18,7 +18,11 @@
 
 namespace skv {
 
-constexpr int kOver = 4;
+// Keys whose places are an item's own cost: a launch's AttendArgs::over is that in tiles.  (us, bf16, 32 heads over 8, with 0 / 256 / 512 keys
+// in attend_mma, whose tiles have 64: 16 sequences of 1 to 5003 keys 56.0 / 32.9 / 28.6, 3 tokens over 4 x 4096 keys 20.1 / 18.0 /
+// 16.9; in attend_tc, 128, with 0 / 512 / 1024: 8 tokens over the 16 sequences 51.4 / 35.4 / 38.7, 64 over 8 x 8192 keys 94.5 / 91.2 /
+// 94.9; a speculative step over 4 x 4096 keys whose weighing has 0 / 256 / 512: 43.8 / 43.4 / 47.3.)
+constexpr int kOverKeys = 512, kWeighOverKeys = 256;
 constexpr int kMaxNew = STRUCTKV_MAX_NEW;   // new tokens of a sequence: a tree's masks are words of 64 bits
 
 // The cache as the kernels see it; strides in bytes, words [batch, H_kv, capacity], lengths [batch, H_kv].
@@ -65,7 +69,7 @@ struct AttendArgs {
   float2* part_stat;                   // [slot][RB] reference (bits) and sum
   float* part_out;                     // [slot][RB][d]
   float* logits;                       // [units][capacity][group] in bits (accumulate)
-  int ctas, least;                     // CTAs; log2 of the tiles that one of them has at least
+  int ctas, least, over;               // CTAs; log2 of the tiles that one of them has at least; places before an item's tiles
 };
 
 // Rows of a block, keys of a tile, CTAs that run at once, partials a CTA leaves of an item, log2 of the tiles it takes at least.
@@ -153,12 +157,12 @@ __device__ __forceinline__ int cta_of(const Shares& s, int x) {
 }
 
 __device__ __forceinline__ int tiles_of(int keys, int tile_shift) { return (keys + (1 << tile_shift) - 1) >> tile_shift; }
-__device__ __forceinline__ int places_of(int keys, int tile_shift) { return keys == 0 ? 0 : tiles_of(keys, tile_shift) + kOver; }
+__device__ __forceinline__ int places_of(int keys, int tile_shift, int over) { return keys == 0 ? 0 : tiles_of(keys, tile_shift) + over; }
 
 // First partial of an item and how many it has; each: partials a CTA leaves of an item.
 struct Parts { int first, count; };
-__device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, int places, int each) {
-  const int c0 = cta_of(s, start + kOver), c1 = cta_of(s, start + places - 1);
+__device__ __forceinline__ Parts parts_of(const Shares& s, int item, int start, int places, int each, int over) {
+  const int c0 = cta_of(s, start + over), c1 = cta_of(s, start + places - 1);
   return {(item + c0) * each, (c1 - c0 + 1) * each};
 }
 
@@ -178,7 +182,7 @@ __device__ __forceinline__ WorkStart find_work(const AttendArgs& a, int tile_shi
 #pragma unroll
     for (int e = 0; e < kLaneUnits; ++e) keys[e] = u0 + lane * kLaneUnits + e < c.units ? keys_of(c, keys[e], a.n_new) : 0;
 #pragma unroll
-    for (int e = 0; e < kLaneUnits; ++e) sum += places_of(keys[e], tile_shift);
+    for (int e = 0; e < kLaneUnits; ++e) sum += places_of(keys[e], tile_shift, a.over);
     incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -197,7 +201,7 @@ __device__ __forceinline__ WorkStart find_work(const AttendArgs& a, int tile_shi
       for (int e = 0; e < kLaneUnits; ++e) {
         const int u = u0 + lane * kLaneUnits + e;
         if (u < c.units) save[u] = at;
-        at += places_of(keys[e], tile_shift);
+        at += places_of(keys[e], tile_shift, a.over);
       }
     }
     total += __shfl_sync(0xffffffffu, incl, 31);
@@ -218,7 +222,7 @@ __device__ __forceinline__ WorkStart find_work(const AttendArgs& a, int tile_shi
       int at = before + __shfl_sync(0xffffffffu, incl - sum, from);
 #pragma unroll
       for (int e = 0; e < kLaneUnits; ++e) {
-        const int k = __shfl_sync(0xffffffffu, keys[e], from), t = places_of(k, tile_shift);
+        const int k = __shfl_sync(0xffffffffu, keys[e], from), t = places_of(k, tile_shift, a.over);
         if (at * blocks <= w.lo && w.lo < (at + t) * blocks) {
           w.unit = u0 + from * kLaneUnits + e;
           w.before = at;
@@ -239,26 +243,26 @@ struct Segments {
   int at, hi;                                                    // place where the item begins, where the run ends
 };
 __device__ __forceinline__ void next_segment(Segments& s, const AttendArgs& a, int tile_shift, int blocks) {
-  s.at += s.tiles + kOver;
+  s.at += s.tiles + a.over;
   s.t0 = s.t1 = 0;
-  if (s.at + kOver >= s.hi) return;
+  if (s.at + a.over >= s.hi) return;
   if (++s.rb == blocks) {
     s.rb = 0;
     do ++s.u;
     while ((s.keys = unit_keys(a.c, s.u, a.n_new)) == 0 && s.u < a.c.units - 1);
     s.tiles = tiles_of(s.keys, tile_shift);
   }
-  s.t1 = min(s.tiles, s.hi - s.at - kOver);
+  s.t1 = min(s.tiles, s.hi - s.at - a.over);
 }
 __device__ __forceinline__ Segments first_segment(const AttendArgs& a, const WorkStart& w, int tile_shift, int blocks) {
   Segments s{w.unit, 0, 0, 0, w.keys, tiles_of(w.keys, tile_shift), w.before * blocks, w.hi};
   if (w.lo >= w.hi) return s;
-  while (w.lo >= s.at + s.tiles + kOver) {
-    s.at += s.tiles + kOver;
+  while (w.lo >= s.at + s.tiles + a.over) {
+    s.at += s.tiles + a.over;
     ++s.rb;
   }
-  s.t0 = max(0, w.lo - s.at - kOver);
-  s.t1 = max(0, min(s.tiles, w.hi - s.at - kOver));
+  s.t0 = max(0, w.lo - s.at - a.over);
+  s.t1 = max(0, min(s.tiles, w.hi - s.at - a.over));
   if (s.t1 <= s.t0) next_segment(s, a, tile_shift, blocks);
   return s;
 }

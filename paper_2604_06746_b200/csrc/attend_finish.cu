@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
       places = a.unit_start[u + 1] - start;
     }
     if (places == 0) continue;
-    const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * places, places, each);
+    const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * places, places, each, a.over);
     const float* from = a.part_out + ((size_t)p.first * rb_rows + row) * D + lane * DL;
     Cols<DL> x[kAhead];
 #pragma unroll
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
   places = hit[2];
 #pragma unroll 1
   for (int at = lo; at < hi;) {
-    const int next = min(hi, start + places), t0 = max(0, at - start - kOver), t1 = max(0, next - start - kOver);
+    const int next = min(hi, start + places), t0 = max(0, at - start - a.over), t1 = max(0, next - start - a.over);
     const int end = min(keys, t1 << tile_shift);
     float* const w = a.c.weights + (size_t)u * a.c.capacity;
 #pragma unroll 1
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
 #pragma unroll 1
       for (int h = warp; h < heads; h += kThreads / 32) {
         const int r = h0 + h, rb = r >> rb_shift;
-        const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * places, places, each);
+        const Parts p = parts_of(sh, u * blocks + rb, start * blocks + rb * places, places, each, a.over);
         float2 mine;
         const float x = bits_of(merged(a.part_stat, p, rb_rows, r & (rb_rows - 1), lane, mine));
         if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 3) attend_finish_rows(const __
     live = places != 0;
     if (live) {
       const Shares sh = shares_of(W1 * blocks, a.ctas, a.by_ctas, a.least);
-      const Parts p = parts_of(sh, item, start * blocks + rb * places, places, each);
+      const Parts p = parts_of(sh, item, start * blocks + rb * places, places, each, a.over);
       const int share = (p.count + (1 << by) - 1) >> by, begin = p.first + mine * share;
       const int left = min(share, p.count - mine * share);
       const float2* st = a.part_stat + ((size_t)begin << rb_shift) + row;
