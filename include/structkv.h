@@ -581,8 +581,9 @@ structkv_status structkv_commit(structkv_ctx* ctx, const structkv_cache* cache, 
 /*
  * Eviction by accumulated attention weight: every KV head of more than `budget` (at least 1) tokens keeps `budget` of them: first
  * those whose position is above its newest one less `recent` (recent >= 0; of more than `budget` such ones the lower slots), then
- * by weight, larger first (a NaN counts as larger than any number), ties to the lower slot.  Kept tokens in slots from `budget` on move, in order, into the slots below it whose tokens
- * go, the lowest first; other slots stay as they are, so that slots are not in the order of positions.  lengths becomes `budget`.
+ * by weight, larger first (a NaN counts as larger than any number), ties to the lower slot.  Kept tokens in slots from `budget` on
+ * move, in order, into the slots below it whose tokens go, the lowest first; other slots stay as they are, so that slots are not
+ * in the order of positions.  lengths becomes `budget`.
  * Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
  */
 structkv_status structkv_evict(structkv_ctx* ctx, const structkv_cache* cache, int budget, int recent, void* stream);

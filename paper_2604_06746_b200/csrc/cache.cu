@@ -105,7 +105,8 @@ __global__ void __launch_bounds__(256) commit(const __grid_constant__ CacheView 
 constexpr int kList = 4096;
 struct EvictShared {
   RadixShared<1> radix;
-  unsigned counts[3][32];
+  unsigned counts[2][32];
+  unsigned kept[16 * kRxThreads / 32];   // bits of a chunk's tokens
   int newest[32];
   unsigned low[2][32];
 };
@@ -244,41 +245,43 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
         eq = run_eq + __shfl_sync(0xffffffffu, incl - s.counts[0][lane], warp);
         run_eq += __shfl_sync(0xffffffffu, incl, 31);
       }
-      const int first = token_of(ch);
-      unsigned is_free = 0, is_move = 0, n_free = 0, n_move = 0;      // bits: item e
+      // a word for 32 tokens, by the warp that has them; then a thread a word
+      token_of(ch);
 #pragma unroll
       for (int e = 0; e < kItems; ++e) {
         if (e >= items) break;
-        const bool there = e < mine, equal = there && need_eq && key[e] == thr;
-        const unsigned be = __ballot_sync(0xffffffffu, equal);
-        const bool kept = there && (key[e] > above || (equal && eq + __popc(be & below) < need_eq));
-        eq += __popc(be);
-        const int j = first + 32 * e;
-        const bool fr = there && !kept && j < budget, mv = kept && j >= budget;
-        is_free |= (unsigned)fr << e;
-        is_move |= (unsigned)mv << e;
-        n_free += __popc(__ballot_sync(0xffffffffu, fr));
-        n_move += __popc(__ballot_sync(0xffffffffu, mv));
+        bool kept = e < mine && key[e] > above;
+        if (need_eq) {
+          const bool equal = e < mine && key[e] == thr;
+          const unsigned be = __ballot_sync(0xffffffffu, equal);
+          kept |= equal && eq + __popc(be & below) < need_eq;
+          eq += __popc(be);
+        }
+        const unsigned bits = __ballot_sync(0xffffffffu, kept);
+        if (lane == 0) s.kept[warp * items + e] = bits;
       }
-      if (lane == 0) { s.counts[1][warp] = n_free; s.counts[2][warp] = n_move; }
       __syncthreads();
-      const unsigned fi = warp_scan(s.counts[1][lane], lane), mi = warp_scan(s.counts[2][lane], lane);
-      unsigned f_at = run_free + __shfl_sync(0xffffffffu, fi - s.counts[1][lane], warp);
-      unsigned m_at = run_move + __shfl_sync(0xffffffffu, mi - s.counts[2][lane], warp);
-      run_free += __shfl_sync(0xffffffffu, fi, 31);
-      run_move += __shfl_sync(0xffffffffu, mi, 31);
-#pragma unroll
-      for (int e = 0; e < kItems; ++e) {
-        if (e >= items) break;
-        const bool fr = is_free >> e & 1, mv = is_move >> e & 1;
-        const unsigned bf = __ballot_sync(0xffffffffu, fr), bm = __ballot_sync(0xffffffffu, mv);
-        const unsigned fa = f_at + __popc(bf & below) - lo, ma = m_at + __popc(bm & below) - lo;
-        if (fr && fa < (unsigned)kList) lists[fa] = first + 32 * e;
-        if (mv && ma < (unsigned)kList) lists[kList + ma] = first + 32 * e;
-        f_at += __popc(bf);
-        m_at += __popc(bm);
+      const int j0 = ch * kChunk + 32 * tid;
+      auto under = [&](int line) { return line <= j0 ? 0u : line - j0 >= 32 ? 0xffffffffu : (1u << (line - j0)) - 1u; };
+      unsigned fr = 0, mv = 0;
+      if (tid < 32 * items) {
+        const unsigned kept = s.kept[tid], low = under(budget);
+        fr = under(n) & ~kept & low;
+        mv = kept & ~low;
       }
-      __syncthreads();                                                // the counts have been read
+      const unsigned both = __popc(fr) | __popc(mv) << 16, incl = warp_scan(both, lane);      // (a chunk has at most 2^14)
+      if (lane == 31) s.counts[1][warp] = incl;
+      __syncthreads();
+      const unsigned of_warp = s.counts[1][lane], upto = warp_scan(of_warp, lane), all = __shfl_sync(0xffffffffu, upto, 31);
+      const unsigned at = __shfl_sync(0xffffffffu, upto - of_warp, warp) + incl - both;
+      unsigned fa = run_free + (at & 0xffffu) - lo, ma = run_move + (at >> 16) - lo;
+      run_free += all & 0xffffu;
+      run_move += all >> 16;
+      for (; fr; fr &= fr - 1, ++fa)
+        if (fa < (unsigned)kList) lists[fa] = j0 + __ffs(fr) - 1;
+      for (; mv; mv &= mv - 1, ++ma)
+        if (ma < (unsigned)kList) lists[kList + ma] = j0 + __ffs(mv) - 1;
+      __syncthreads();
     }
     const int moves = (int)run_move;                                  // as many free slots as tokens to move
     if (!sized && moves > kList) {
@@ -288,6 +291,14 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
     }
     sized = true;
     const int here = min(kList, moves - lo);
+    int* const to_pos = c.positions + (size_t)u * c.capacity;
+    float* const to_wt = c.weights + (size_t)u * c.capacity;
+    int p0 = 0;
+    float w0 = 0.f;
+    if (tid < here) {
+      p0 = pos[lists[kList + tid]];
+      w0 = wt[lists[kList + tid]];
+    }
     constexpr int kGo = 4;
     for (int i0 = tid; i0 < here << (row_shift + 1); i0 += kGo * kRxThreads) {
       uint4 x[kGo];
@@ -305,9 +316,11 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
       for (int e = 0; e < kGo; ++e)
         if ((i0 + e * kRxThreads) >> (row_shift + 1) < here) *(uint4*)col[e] = x[e];
     }
-    int* const to_pos = c.positions + (size_t)u * c.capacity;
-    float* const to_wt = c.weights + (size_t)u * c.capacity;
-    for (int i = tid; i < here; i += kRxThreads) {
+    if (tid < here) {
+      to_pos[lists[tid]] = p0;
+      to_wt[lists[tid]] = w0;
+    }
+    for (int i = tid + kRxThreads; i < here; i += kRxThreads) {
       to_pos[lists[i]] = pos[lists[kList + i]];
       to_wt[lists[i]] = wt[lists[kList + i]];
     }

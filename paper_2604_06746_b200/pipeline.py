@@ -1,8 +1,8 @@
 """Sequencing of the C-ABI calls over one prompt (the control flow of Algorithm 1
 replayed over per-layer tensors): score every layer, detect the pivot, rebuild
 the centrality at the pivot, select both budgets, compact K/V, hidden states
-and position ids.  All arithmetic happens inside the library's kernels; this
-file only owns buffers and call order.
+and position ids; and over the tokens that follow it (Decode).  All arithmetic happens
+inside the library's kernels; this file only owns buffers and call order.
 """
 from __future__ import annotations
 
@@ -212,7 +212,8 @@ class Decode:
     ``advance``; drafted tokens, a tree of them or a chain, are looked at by ``verify`` for every layer, then ``accept`` keeps
     some.  Cached tokens gather the attention weight that new ones give them; with a ``budget`` every KV head keeps its
     ``recent`` newest tokens and the heaviest others.  All layers of all sequences are in one cache (sequence ``layer * batch +
-    b``), so that commit and eviction are one launch each; every call can be captured into a graph."""
+    b``), so that commit and eviction are one launch each; every call can be captured into a graph.  Lengths live on the device:
+    a KV head that has no room for new tokens is left as it is, and ``ctx.poll_device_status`` says so."""
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, capacity: int, dtype: torch.dtype,
                  batch: int = 1, budget: int = 0, recent: int = 0, max_new: int = 1, softcap: float = 0.0,
