@@ -101,7 +101,8 @@ __global__ void __launch_bounds__(256) commit(const __grid_constant__ CacheView 
 //
 // Where one token goes, which is what a step of decoding asks for, there is no rank to search: it is the last of the lowest.
 // A thread holds kItems tokens of a chunk: 8 where the capacity fits them or holds more than a chunk of 16, with two blocks an SM,
-// else 16 with one.  (A unit of 8320 tokens was read anew for each level with 8.)
+// else 16 with one.  (A unit of 8320 tokens was read anew for each level with 8.)  The code runs once a block, so that fetching it counts:
+// the forms for one chunk and for many are compiled apart.
 constexpr int kList = 4096;
 struct EvictShared {
   RadixShared<1> radix;
@@ -111,7 +112,7 @@ struct EvictShared {
   unsigned low[2][32];
 };
 
-template <int kItems>
+template <int kItems, bool kMany>
 __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const __grid_constant__ CacheView c, int budget, int recent) {
   extern __shared__ __align__(16) unsigned char smem[];
   EvictShared& s = *reinterpret_cast<EvictShared*>(smem);
@@ -126,7 +127,7 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
   const int* const pos = c.positions + (size_t)u * c.capacity;
   const float* const wt = c.weights + (size_t)u * c.capacity;
   constexpr int kChunk = kRxThreads * kItems;
-  const int chunks = (n + kChunk - 1) / kChunk;                       // more than one: the unit does not fit the registers
+  const int chunks = kMany ? (n + kChunk - 1) / kChunk : 1;           // more than one: the unit does not fit the registers
   unsigned key[kItems];
   int mine = 0, items = 0;
   // a warp's tokens are consecutive, as many for every warp; item e of this thread: first + 32 e
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
   if (lane == 0) s.newest[warp] = newest;
   __syncthreads();
   newest = __reduce_max_sync(0xffffffffu, s.newest[lane]);
-  const long long line = (long long)newest - recent;
+  const int line = newest - recent;                                   // (newest is -1 at least)
   // (a NaN weight, all bits set, comes below the recent ones)
   auto keys = [&] {
 #pragma unroll
@@ -246,19 +247,24 @@ __global__ void __launch_bounds__(kRxThreads, kItems == 8 ? 2 : 1) evict(const _
         run_eq += __shfl_sync(0xffffffffu, incl, 31);
       }
       // a word for 32 tokens, by the warp that has them; then a thread a word
+      // (this code runs once a launch: what bounds it is that it is fetched)
       token_of(ch);
 #pragma unroll
       for (int e = 0; e < kItems; ++e) {
         if (e >= items) break;
-        bool kept = e < mine && key[e] > above;
-        if (need_eq) {
-          const bool equal = e < mine && key[e] == thr;
-          const unsigned be = __ballot_sync(0xffffffffu, equal);
-          kept |= equal && eq + __popc(be & below) < need_eq;
-          eq += __popc(be);
-        }
-        const unsigned bits = __ballot_sync(0xffffffffu, kept);
+        const unsigned bits = __ballot_sync(0xffffffffu, e < mine && key[e] > above);
         if (lane == 0) s.kept[warp * items + e] = bits;
+      }
+      if (need_eq) {
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < kItems; ++e) {
+          if (e >= items) break;
+          const bool equal = e < mine && key[e] == thr;
+          const unsigned be = __ballot_sync(0xffffffffu, equal), bits = __ballot_sync(0xffffffffu, equal && eq + __popc(be & below) < need_eq);
+          eq += __popc(be);
+          if (lane == 0) s.kept[warp * items + e] |= bits;
+        }
       }
       __syncthreads();
       const int j0 = ch * kChunk + 32 * tid;
@@ -341,8 +347,10 @@ cudaError_t launch_evict(const CacheView& c, int budget, int recent, cudaStream_
   auto go = [&](auto kernel, cudaError_t e) {
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3(c.units), dim3(kRxThreads), sizeof(EvictShared), st, c, budget, recent);
   };
-  if (c.capacity > 8 * kRxThreads && c.capacity <= 16 * kRxThreads) return go(evict<16>, allow_smem<evict<16>>((int)sizeof(EvictShared)));
-  return go(evict<8>, allow_smem<evict<8>>((int)sizeof(EvictShared)));
+  constexpr int kBytes = (int)sizeof(EvictShared);
+  if (c.capacity <= 8 * kRxThreads) return go(evict<8, false>, allow_smem<evict<8, false>>(kBytes));
+  if (c.capacity <= 16 * kRxThreads) return go(evict<16, false>, allow_smem<evict<16, false>>(kBytes));
+  return go(evict<8, true>, allow_smem<evict<8, true>>(kBytes));
 }
 
 }  // namespace skv
