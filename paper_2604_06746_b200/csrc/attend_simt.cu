@@ -160,7 +160,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
   }
 }
 
-// weights[j] = decay weights[j] + sum over accepted rows of 2^(x - lse), eight rows at a time over the same keys.
+// weights[j] = decay weights[j] + sum over accepted rows of 2^(x - lse), eight rows at a time over the same keys (a weight is
+// rounded once for every eight: its rows' sum is not kept anywhere else).
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant__ AttendArgs a, const unsigned long long* __restrict__ accepted) {
   using S = Shape<D>;
