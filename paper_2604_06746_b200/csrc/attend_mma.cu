@@ -1,6 +1,6 @@
 // Attention of new tokens over a bf16 cache, up to 16 rows of a KV head at a time, and the weight of accepted tokens.
 //
-// Flash form: per row a reference m, sum l and unscaled output O over the keys seen so far; a tile of 64 keys gives
+// One pass: per row a reference m, sum l and unscaled output O over the keys seen so far; a tile of 64 keys gives
 // S = K Q^T, p = 2^(x - m), l += sum p, O^T += V^T p.  Rows are few and reading K and V is the bound, so keys are the long side of
 // the m16n8k16 products (16 keys x 8 rows, then 16 columns of V x 8 rows): four rows of a single token fill half a product, in
 // the other orientation a quarter.  A warp takes 16 keys of a tile and all rows; tiles come by TMA (128-byte swizzle)

@@ -1,6 +1,6 @@
 // Attention of new tokens over an fp32 cache on the CUDA cores, and the weight of accepted tokens.
 //
-// The flash form of attend_mma.cu in fp32: eight warps share a tile of 64 keys, eight each, and every warp takes all of the
+// The one pass of attend_mma.cu in fp32: eight warps share a tile of 64 keys, eight each, and every warp takes all of the
 // block's R rows (4 or 8).  Products: lane = (key, quarter of the head dimension), the quarters added by two shuffles; output:
 // lane = D / 32 columns, the probabilities by shuffle.  K and V are read from shared memory once a block of rows.
 #include <algorithm>

@@ -103,6 +103,10 @@ __global__ void __launch_bounds__(256) commit(const __grid_constant__ CacheView 
 // A thread holds kItems tokens of a chunk: 8 where the capacity fits them or holds more than a chunk of 16, with two blocks an SM,
 // else 16 with one.  (A unit of 8320 tokens was read anew for each level with 8.)  The code runs once a block, so that fetching it counts:
 // the forms for one chunk and for many are compiled apart.
+//
+// A block goes through its steps once, each waiting for the one before: 128 units of 8320 tokens, 128 of which go, take 9.5 us (8.5 MB
+// read, 8.4 MB moved: 3 at the copy bandwidth): words there 1.3, keys 1.2, rank 1.7, lists 2.0, rows 1.5, their words and the
+// end 1.8; 256 units of 2049, one of which goes, 3.5.
 constexpr int kList = 4096;
 struct EvictShared {
   RadixShared<1> radix;
