@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
       mbar_init(v_look(s), 1); mbar_init(v_ready(s), 32); mbar_init(drained(s), 1); mbar_init(turn(s), 4);
     }
     mbar_init(q_full, 256);
-    mbar_init(q_empty, 8);
+    mbar_init(q_empty, 10);                                        // softmax's warps, products' warps
     *abort_flag = 0;
     *odd_v = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -246,7 +246,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
           commit_by(lead, s_full(s));
           commit_by(lead, empty(st));
         };
-        ok = wait(q_full, seg & 1);
+        // (a stream without a tile in the segment says as well that it came by: else its wait might be for a phase that is gone)
+        if ((ok = wait(q_full, seg & 1)) && lead) mbar_arrive(q_empty);
         if (ok && jobs > 0) scores(0);
 #pragma unroll 1
         for (int k = 0; k < jobs && ok; ++k) {
