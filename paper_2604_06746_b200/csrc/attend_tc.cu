@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
   auto p_half = [&](int s) { return more + 160 + 8 * s; };       // (behind the words)
   const uint32_t q_full = more + 128, q_empty = more + 136;
   volatile int* const words = (volatile int*)(sm + kBars + 16 * NU + 144);
-  volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v: some new token's V was not finite
+  volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v[s]: in a tile of stream s some new token's V was not finite
   volatile uint32_t* const tmem_at = (volatile uint32_t*)words + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int blocks = (a.rows + RB - 1) / RB;
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     mbar_init(q_full, 256);
     mbar_init(q_empty, 10);                                        // softmax's warps, products' warps
     *abort_flag = 0;
-    *odd_v = 0;
+    odd_v[0] = odd_v[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&maps.v) : "memory");
@@ -309,7 +309,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
 #pragma unroll
             for (int e = 0; e < kGo; ++e) bad |= not_finite(x[e].x) || not_finite(x[e].y) || not_finite(x[e].z) || not_finite(x[e].w);
             if (bad) {
-              *odd_v = 1;
+              if (MT == 2) odd_v[0] = odd_v[1] = 1;
+              else odd_v[of] = 1;
 #pragma unroll
               for (int e = 0; e < kGo; ++e) {
                 const int i = min(i0 + 32 * e, row1 * CH - 1);
@@ -491,7 +492,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
           if (!(ok = wait(o_done(s), (done - 1) & 1))) break;
           tc_fence_after();
           if (!idle) {
-            const bool odd = *odd_v && sg.t1 * kTile > n_old && (MT == 2 || s == 0);
+            // (this stream's own flag: o_done(s) comes behind the look through its tiles alone.  Tokens across two tiles may be added by both
+            // streams: infinity and NaN stay what they are.)
+            const bool odd = odd_v[s] && sg.t1 * kTile > n_old;
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
               float v[32];
