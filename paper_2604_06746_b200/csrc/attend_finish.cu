@@ -137,7 +137,8 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
 #pragma unroll 1
     for (int h0 = 0; t0 < t1 && h0 < a.group; h0 += kThreads) {              // (one round, but for groups of more than 128 heads)
       const int heads = min(kThreads, a.group - h0);
-      // the commonest group: four keys' loads in flight, the first ones while the references are on their way
+      // the commonest group, not the last four heads of a larger one: four keys' loads in flight, the first ones while the references
+      // are on their way
       float4 x[4];
       float old[4];
       int j = (t0 << tile_shift) + tid;
@@ -149,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
           old[e] = k < end ? w[k] : 0.f;
         }
       };
-      if (heads == 4) load();
+      if (a.group == 4) load();
       __syncthreads();
 #pragma unroll 1
       for (int h = warp; h < heads; h += kThreads / 32) {
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 6) attend_finish(const __grid_consta
         if (lane == 0) lse[h] = x == -INFINITY ? INFINITY : x;
       }
       __syncthreads();
-      if (heads == 4) {
+      if (a.group == 4) {
 #pragma unroll 1
         while (j < end) {
 #pragma unroll
