@@ -42,10 +42,13 @@ AttendWs carve_attend(const structkv_config& cfg, const AttendPlan& p, int batch
   return w;
 }
 
-// (tiles of all units are counted in 31 bits)
+// (units are counted in 31 bits)
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, int capacity) {
-  if (batch < 1 || capacity < 1 || capacity > 1 << 30 || n_new < 0 || n_new > capacity) return false;
-  const long long units = (long long)batch * cfg.n_kv_heads, rows = (long long)cfg.n_q_heads / cfg.n_kv_heads * std::max(1, n_new);
+  return batch >= 1 && capacity >= 1 && capacity <= 1 << 30 && n_new >= 0 && n_new <= capacity && (long long)batch * cfg.n_kv_heads <= 0x3fffffffll;
+}
+// What lays out tiles of new tokens' rows, attend and weigh: these and the tiles of all units are counted in 31 bits as well.
+bool tiles_ok(const structkv_config& cfg, int batch, int n_new, int capacity) {
+  const long long units = (long long)batch * cfg.n_kv_heads, rows = (long long)cfg.n_q_heads / cfg.n_kv_heads * n_new;
   return units * rows <= 0x3fffffffll && units * ((rows + 3) / 4) <= 0x7fffffffll / (capacity / 64 + 1 + kOverKeys / 64);
 }
 bool strides_ok(int elem, long long a, long long b, long long c) { return (a * elem) % 16 == 0 && (b * elem) % 16 == 0 && (c * elem) % 16 == 0; }
@@ -78,10 +81,11 @@ bool rows_of(const structkv_ctx* ctx, const structkv_new_rows* r, NewRows* out) 
   return true;
 }
 // What attend and weigh have in common.
-bool args_of(const structkv_ctx* ctx, const structkv_attend_args* x, AttendArgs* a) {
+bool args_of(const structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* x, AttendArgs* a) {
   const structkv_config& cfg = ctx->c.cfg;
   const int elem = cfg.dtype == STRUCTKV_BF16 ? 2 : 4;
-  if (x->n_new < 1 || x->n_new > kMaxNew || !x->q || (uintptr_t)x->q % 16 || !strides_ok(elem, x->q_stride_batch, x->q_stride_token, x->q_stride_head)) return false;
+  if (x->n_new < 1 || x->n_new > kMaxNew || !tiles_ok(cfg, cache->batch, x->n_new, cache->capacity)) return false;
+  if (!x->q || (uintptr_t)x->q % 16 || !strides_ok(elem, x->q_stride_batch, x->q_stride_token, x->q_stride_head)) return false;
   if (!std::isfinite(x->scale) || !std::isfinite(x->softcap) || x->softcap < 0.f || !std::isfinite(x->decay)) return false;
   if ((uintptr_t)x->slopes % 4 || (uintptr_t)x->tree % 8 || (uintptr_t)x->lse % 4) return false;
   const float inv = x->softcap > 0.f ? x->scale / x->softcap : 0.f, cap2 = x->softcap * kLog2e;
@@ -120,14 +124,16 @@ structkv_status structkv_append(structkv_ctx* ctx, const structkv_cache* cache, 
 }
 
 size_t structkv_attend_workspace_bytes(const structkv_config* cfg, int batch, int n_new, int capacity) {
-  if (structkv_workspace_bytes(cfg) == 0 || n_new < 1 || n_new > kMaxNew || !sizes_ok(*cfg, batch, n_new, capacity)) return 0;
+  if (structkv_workspace_bytes(cfg) == 0 || n_new < 1 || n_new > kMaxNew || !sizes_ok(*cfg, batch, n_new, capacity) ||
+      !tiles_ok(*cfg, batch, n_new, capacity))
+    return 0;
   return carve_attend(*cfg, attend_plan(*cfg, n_new, kMaxSms), batch, n_new, capacity, nullptr).bytes;
 }
 
 structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* args, void* stream) {
   AttendArgs a{};
   NewRows r;
-  if (!args || !view_of(ctx, cache, args->n_new, &a.c) || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
+  if (!args || !view_of(ctx, cache, args->n_new, &a.c) || !args_of(ctx, cache, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
   if (!args->out || (uintptr_t)args->out % 16 || (args->rows && !rows_of(ctx, args->rows, &r))) return STRUCTKV_ERR_INVALID_ARG;
   if (args->accumulate && !cache->weights) return STRUCTKV_ERR_INVALID_ARG;
   if (args->accumulate && args->n_new > 1) return STRUCTKV_ERR_UNSUPPORTED;
@@ -162,7 +168,7 @@ structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, c
                                const unsigned long long* accepted, void* stream) {
   AttendArgs a{};
   if (!args || !accepted || (uintptr_t)accepted % 8 || !args->lse) return STRUCTKV_ERR_INVALID_ARG;
-  if (!view_of(ctx, cache, args->n_new, &a.c) || !cache->weights || !args_of(ctx, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
+  if (!view_of(ctx, cache, args->n_new, &a.c) || !cache->weights || !args_of(ctx, cache, args, &a)) return STRUCTKV_ERR_INVALID_ARG;
   a.ctas = ctx->c.cfg.dtype == STRUCTKV_BF16 ? ctx->c.sm_count : 4 * ctx->c.sm_count;   // (CTAs that run at once)
   a.by_ctas = div_by(a.ctas);
   a.over = kWeighOverKeys / 64;
