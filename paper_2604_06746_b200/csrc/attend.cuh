@@ -15,6 +15,7 @@
 #include <atomic>
 
 #include "common.cuh"
+#include "score_tc.cuh"
 
 namespace skv {
 
@@ -267,11 +268,41 @@ __device__ __forceinline__ Segments first_segment(const AttendArgs& a, const Wor
   return s;
 }
 
-// cap tanh(y) in bits, y = scale s / cap, as cap - 2 cap / (e^2y + 1): off by 2^-22 cap at most, whatever y (infinite ones too).
-__device__ __forceinline__ float capped(float s, float cap2, float inv_cap) {
+// cap tanh(y) in bits of two scores, y = scale s / cap: tanh(y) = y P(y^2) / Q(y^2), relatively exact down to zero (cap - 2 cap / (e^2y + 1)
+// cancels there: off by 2^-22 cap whatever the score).  P and Q of degree four approximate tanh(y) / y on |y| <= 8.7, where tanh is 1 to 24
+// bits, with the least largest relative error (1.5e-8; least squares of P - Q tanh(y) / y, reweighted by the error until it is level:
+// Lawson's method); in fp32 tanh is off by 2^-21.4 at most, and by 2^-23 more for the reciprocal.  Infinite y give cap, NaN stays NaN.
+// Packed instructions: one score at a time a tree of 16 over eight ragged sequences takes 44 us, so 30, and with e^2y 31.
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float within(float y, float end) {
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(y) : "f"(end));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(y) : "f"(-end));
+  return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {
   float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fast_exp2(s * (inv_cap * (2.f * kLog2e))) + 1.f));
-  return fmaf(-2.f * cap2, r, cap2);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void capped2(float& a, float& b, uint64_t cap2, uint64_t inv_cap) {
+  const float P[5] = {1.3962095e-8f, 2.104377e-5f, 3.5219393e-3f, 1.3403216e-1f, 1.f};
+  const float Q[5] = {8.0239e-7f, 3.328758e-4f, 2.5977228e-2f, 4.673654e-1f, 1.f};
+  constexpr float kEnd = 8.7f;
+  float y0, y1, q0, q1;
+  unpack2(mul2(pack2(a, b), inv_cap), y0, y1);
+  const uint64_t y = pack2(within(y0, kEnd), within(y1, kEnd)), z = mul2(y, y);
+  uint64_t p = pack2(P[0], P[0]), q = pack2(Q[0], Q[0]);
+#pragma unroll
+  for (int i = 1; i < 5; ++i) {
+    p = fma2(p, z, pack2(P[i], P[i]));
+    q = fma2(q, z, pack2(Q[i], Q[i]));
+  }
+  unpack2(q, q0, q1);
+  unpack2(mul2(cap2, mul2(mul2(y, p), pack2(reciprocal(q0), reciprocal(q1)))), a, b);
 }
 
 // The new tokens that row r of a unit sees, as bits.
@@ -296,11 +327,16 @@ __device__ __forceinline__ RowOptions row_options(const AttendArgs& a, int u, in
 // Whether key j of a unit whose first n tokens are old is seen.
 __device__ __forceinline__ bool sees(unsigned long long mask, int j, int n) { return j < n || (mask >> ((j - n) & 63) & 1); }
 
-// x in bits from the product of a row and a key.
-__device__ __forceinline__ float biased(const AttendArgs& a, float s, const RowOptions& o, int key_position) {
-  float x = a.cap2 != 0.f ? capped(s, a.cap2, a.inv_cap) : s * a.scale2;
-  if (a.slopes) x = fmaf(-o.slope2, (float)(o.position - key_position), x);
-  return x;
+// x in bits from the products of rows and keys, two at a time, but for the bias; and with it.
+__device__ __forceinline__ void in_bits2(const AttendArgs& a, float& s0, float& s1) {
+  if (a.cap2 != 0.f) capped2(s0, s1, pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
+  else {
+    s0 *= a.scale2;
+    s1 *= a.scale2;
+  }
+}
+__device__ __forceinline__ float biased(const AttendArgs& a, float x, const RowOptions& o, int key_position) {
+  return a.slopes ? fmaf(-o.slope2, (float)(o.position - key_position), x) : x;
 }
 
 // A segment's end, by NT threads: the outputs of `sets` warps (a multiple of four) in shared memory, [set][RB][ROW] each against its own

@@ -10,7 +10,6 @@
 #include <algorithm>
 
 #include "attend.cuh"
-#include "score_tc.cuh"
 
 namespace skv {
 namespace {
@@ -249,10 +248,11 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
 #pragma unroll
         for (int i = 0; i < NR; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = a.cap2 != 0.f ? capped(s[i][e], a.cap2, a.inv_cap) : s[i][e] * a.scale2;
-            if (a.slopes) x = fmaf(-slope2[i][e & 1], (float)(place[i][e & 1] - kp[e >> 1]), x);
-            s[i][e] = x;
+          for (int e = 0; e < 4; e += 2) {
+            in_bits2(a, s[i][e], s[i][e + 1]);
+            if (a.slopes)
+#pragma unroll
+              for (int x = 0; x < 2; ++x) s[i][e + x] = fmaf(-slope2[i][x], (float)(place[i][x] - kp[e >> 1]), s[i][e + x]);
           }
       } else {
 #pragma unroll
@@ -544,11 +544,12 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
             const float ref = lse[row];
             RowOptions ro{};
             if (OPT || tail) ro = opts[row];
+            float dot[2] = {s[0][x] + s[1][x], s[0][2 + x] + s[1][2 + x]};
+            if (OPT) in_bits2(a, dot[0], dot[1]);
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
               const int j = j0 + g8 + 8 * y;
-              const float dot = s[0][2 * y + x] + s[1][2 * y + x];
-              float v = OPT ? biased(a, dot, ro, pos[y]) : dot * a.scale2;
+              float v = OPT ? biased(a, dot[y], ro, pos[y]) : dot[y] * a.scale2;
               if (tail && (j >= sg.keys || !sees(ro.seen, j, n_old))) v = -INFINITY;
               sum[y] += ref == INFINITY ? 0.f : fast_exp2(v - ref);
             }

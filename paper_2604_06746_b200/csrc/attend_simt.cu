@@ -115,6 +115,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
       const int j = t * kTileKeys + warp * 8 + (lane >> 2);
       const int kp = a.slopes && j < keys ? a.c.positions[(size_t)u * a.c.capacity + j] : 0;
 #pragma unroll
+      for (int r = 0; r < R; r += 2) in_bits2(a, s[r], s[r + 1]);
+#pragma unroll
       for (int r = 0; r < R; ++r) {
         float x = biased(a, s[r], ro[r], kp);
         if (j >= keys || !sees(ro[r].seen, j, n_old)) x = -INFINITY;
@@ -219,6 +221,8 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_simt(const __grid_constant_
         products<D, R>(qs, sm + warp * 8 * S::kRow, lane, s);
         const int j = t * kTileKeys + warp * 8 + (lane >> 2);
         const int kp = a.slopes && j < keys ? a.c.positions[(size_t)u * a.c.capacity + j] : 0;
+#pragma unroll
+        for (int r = 0; r < R; r += 2) in_bits2(a, s[r], s[r + 1]);
 #pragma unroll
         for (int r = 0; r < R; ++r)
           if (lse[r] != INFINITY && sees(ro[r].seen, j, n_old)) sum += fast_exp2(biased(a, s[r], ro[r], kp) - lse[r]);

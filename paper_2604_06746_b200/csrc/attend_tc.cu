@@ -21,7 +21,6 @@
 #include <algorithm>
 
 #include "attend.cuh"
-#include "score_tc.cuh"
 
 namespace skv {
 namespace {
@@ -339,7 +338,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
     if (work) {
       const int s = (warp - 4) / 4, quarter = warp % 4;
       const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
-      const float scale2 = fabsf(a.scale2), inv_cap = fabsf(a.inv_cap);   // (a negative scale negates the product)
+      const float scale2 = fabsf(a.scale2);                       // (a negative scale negates the product)
+      const uint64_t cap2 = pack2(a.cap2, a.cap2), inv2 = pack2(fabsf(a.inv_cap), fabsf(a.inv_cap));
       int done = 0, seg = 0;
       bool ok = true;
       do {
@@ -384,10 +384,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
               for (int c = 0; c < kTile; c += 32) {
                 float x[32];
                 tmem_ld(s_at + c, x);
+                if (a.cap2 != 0.f) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                  x[e] = a.cap2 != 0.f ? capped(x[e], a.cap2, inv_cap) : x[e] * scale2;
-                  if (a.slopes) x[e] = fmaf(-ro.slope2, (float)(ro.position - kp[c + e]), x[e]);
+                  for (int e = 0; e < 32; e += 2) capped2(x[e], x[e + 1], cap2, inv2);
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) x[e] *= scale2;
+                }
+                if (a.slopes) {
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) x[e] = fmaf(-ro.slope2, (float)(ro.position - kp[c + e]), x[e]);
                 }
                 tmem_st32(s_at + c, x);
               }
