@@ -231,8 +231,9 @@ class Decode:
         positions, weights = torch.zeros(rows, dtype=i32, device=dev), torch.zeros(rows, dtype=f32, device=dev)
         lengths = torch.zeros(rows[:2], dtype=i32, device=dev)
         self.cache = binding.Cache(k, v, positions, weights, lengths)
-        self.layers = [binding.Cache(*(t[l * batch:(l + 1) * batch] for t in (k, v, positions, weights, lengths)))
-                       for l in range(n_layers)]
+        self._weighed = torch.empty_like(lengths)              # lengths as accept() weighs by them
+        self.layers, self._weighing = ([binding.Cache(*(t[l * batch:(l + 1) * batch] for t in (k, v, positions, weights, n)))
+                                        for l in range(n_layers)] for n in (lengths, self._weighed))
         self.lse = torch.empty((n_layers, batch, max_new, n_q_heads), dtype=f32, device=dev)
         self._ws = self.ctx.attend_workspace(self.layers[0], 1)
         for t in range(2, max_new + 1):                      # (not always more for more tokens)
@@ -288,13 +289,20 @@ class Decode:
 
     def accept(self, counts: torch.Tensor, path: torch.Tensor) -> None:
         """After ``verify`` of every layer: sequence b keeps the ``counts[b]`` drafted tokens that ``path[b]`` names, ascending
-        (int32 ``[batch]`` and ``[batch, n_new]``); they give their attention weight, the others leave nothing."""
-        n_new = path.shape[1]
+        (int32 ``[batch]`` and ``[batch, n_new]``); they give their attention weight, the others leave nothing.  A sequence whose
+        count is not 0 .. n_new, or whose path does not ascend within them, is left as it is, and ``ctx.poll_device_status`` says so."""
+        n_new, dev, i32 = path.shape[1] if path.dim() == 2 else 0, self.cache.device, torch.int32
+        if counts.shape != (self.B,) or path.shape != (self.B, n_new) or any((t.dtype, t.device) != (i32, dev) for t in (counts, path)):
+            raise ValueError("accept: counts [batch] and path [batch, n_new], int32 on the cache's device")
         if any(s is None or s[0].shape[1] != n_new for s in self._seen):
             raise ValueError("accept: verify of every layer comes first, of as many tokens")
-        among = torch.arange(n_new, device=path.device)[None] < counts[:, None]
-        words = torch.where(among, torch.ones_like(path, dtype=torch.int64) << path.clamp(0, n_new - 1).long(), 0).sum(1)
-        for cache, (q, scale, lse, tree) in zip(self.layers, self._seen):
+        # What commit will refuse must not weigh either: such a sequence's lengths are no lengths for it.
+        among = torch.arange(n_new, device=dev)[None] < counts[:, None]
+        above = torch.nn.functional.pad(path[:, :-1], (1, 0), value=-1)
+        good = ((path > above) & (path < n_new) | ~among).all(1) & (counts >= 0) & (counts <= n_new)
+        words = torch.where(among & good[:, None], torch.ones_like(path, dtype=torch.int64) << path.clamp(0, n_new - 1).long(), 0).sum(1)
+        self._weighed.copy_(torch.where(good.repeat(self.L)[:, None], self.cache.lengths, -1))
+        for cache, (q, scale, lse, tree) in zip(self._weighing, self._seen):
             self.ctx.weigh(cache, q, scale, lse, words, tree=tree, softcap=self.softcap, slopes=self.slopes, decay=self.decay)
         self.ctx.commit(self.cache, n_new, counts=counts.repeat(self.L), path=path.repeat(self.L, 1))
         self._seen = [None] * self.L
