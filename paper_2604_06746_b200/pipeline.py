@@ -249,6 +249,8 @@ class Decode:
         if not prefill.keep_kv or (prefill.L, prefill.Hkv, prefill.d, prefill.dtype) != (
                 self.L, self.cache.n_kv_heads, self.cache.head_dim, self.cache.dtype):
             raise ValueError("take: a Prefill of these layers, heads and type that keeps K and V")
+        if prefill.i_kv.device != self.cache.device:
+            raise ValueError("take: a Prefill on the cache's device")
         if n > self.cache.capacity - self.max_new:
             raise ValueError("take: capacity for the prompt's tokens and max_new behind them")
         if not 0 <= sequence < self.B:
