@@ -535,7 +535,8 @@ structkv_status structkv_append(structkv_ctx* ctx, const structkv_cache* cache, 
  *   workspace   device, 256-byte aligned, at least structkv_attend_workspace_bytes() bytes (0 for arguments that are not valid),
  *               caller-owned; calls that share it are ordered by the caller.
  * Values are accumulated in fp32; for bf16 storage the probabilities are rounded to bf16 for their product with V.  New tokens
- * that a row does not see do not reach it, whatever they hold.  Tiles of 64 keys are counted in 31 bits, for every four rows of a KV
+ * that a row does not see do not reach it, whatever they hold; V that is not finite makes its column so in every row that sees the
+ * token, if the token's score is a number, however small its probability.  Tiles of 64 keys are counted in 31 bits, for every four rows of a KV
  * head (new token, head of the group) and with nine more for each; a call whose cache could hold more is refused, as structkv_weigh
  * is.  Errors: INVALID_ARG, UNSUPPORTED (accumulate with several tokens), WORKSPACE, CUDA.  Asynchronous on `stream`.
  */

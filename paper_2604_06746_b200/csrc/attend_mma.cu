@@ -317,7 +317,8 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
         pf[i][0] = transposed(bf16x2(p[0], p[1]));
         pf[i][1] = transposed(bf16x2(p[2], p[3]));
       }
-      // Where V of a new token, or of a slot behind them, is not finite, rows that do not see it must not meet it: 0 x infinity.
+      // Where V of a new token, or of a slot behind them, is not finite, rows that do not see it must not meet it: 0 x infinity.  Those that
+      // see it meet it, whatever is left of its probability.
       bool plain = true;
       if (tail) {
         bool bad = false;
@@ -338,7 +339,15 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < NR; ++i)
+        for (int i = 0; i < NR; ++i) {
+          unsigned see[2];                                      // keys of this warp's 16 that row 2 t4 + x sees
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const unsigned long long seen = row_seen(a, sg.u, min(first_row + 8 * i + x, a.rows - 1));
+            see[x] = 0;
+#pragma unroll 1
+            for (int j = 0; j < 16; ++j) see[x] |= (unsigned)(j0 + j < sg.keys && sees(seen, j0 + j, n_old)) << j;
+          }
 #pragma unroll 1
           for (int j = 0; j < 16; ++j) {
             float p[2];
@@ -357,9 +366,10 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
                 const float v = __uint_as_float((uint32_t)h << 16);
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
-                  if (p[x] != 0.f) o[i][k][2 * y + x] = fmaf(p[x], v, o[i][k][2 * y + x]);
+                  if (see[x] >> j & 1) o[i][k][2 * y + x] = fmaf(p[x], v, o[i][k][2 * y + x]);
               }
           }
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(empty(st));

@@ -134,6 +134,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_simt(const __grid_constant
         }
         s[r] = fast_exp2(x - (m[r] == -INFINITY ? 0.f : m[r]));
         l[r] += s[r];                                                 // (each key in four lanes)
+        // nothing that is seen weighs zero: V that is not finite reaches the row, however small its probability
+        float least = x == -INFINITY ? 0.f : 1e-45f;
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(s[r]) : "f"(least));
       }
 #pragma unroll
       for (int jj = 0; jj < 8; ++jj) {
