@@ -234,6 +234,11 @@ class Decode:
         self._weighed = torch.empty_like(lengths)              # lengths as accept() weighs by them
         self.layers, self._weighing = ([binding.Cache(*(t[l * batch:(l + 1) * batch] for t in (k, v, positions, weights, n)))
                                         for l in range(n_layers)] for n in (lengths, self._weighed))
+        few = (batch, n_kv_heads, max_new)                     # (accept() asks whether its counts and paths are well-formed)
+        self._asked = binding.Cache(*(torch.zeros(few + (head_dim,), dtype=dtype, device=dev) for _ in range(2)),
+                                    torch.zeros(few, dtype=i32, device=dev), None, torch.zeros(few[:2], dtype=i32, device=dev))
+        self._nth, self._one = torch.arange(max_new, dtype=i32, device=dev), torch.ones(1, dtype=torch.int64, device=dev)
+        self._none = torch.full((1,), -1, dtype=i32, device=dev)
         self.lse = torch.empty((n_layers, batch, max_new, n_q_heads), dtype=f32, device=dev)
         self._ws = self.ctx.attend_workspace(self.layers[0], 1)
         for t in range(2, max_new + 1):                      # (not always more for more tokens)
@@ -293,17 +298,17 @@ class Decode:
         """After ``verify`` of every layer: sequence b keeps the ``counts[b]`` drafted tokens that ``path[b]`` names, ascending
         (int32 ``[batch]`` and ``[batch, n_new]``); they give their attention weight, the others leave nothing.  A sequence whose
         count is not 0 .. n_new, or whose path does not ascend within them, is left as it is, and ``ctx.poll_device_status`` says so."""
-        n_new, dev, i32 = path.shape[1] if path.dim() == 2 else 0, self.cache.device, torch.int32
-        if counts.shape != (self.B,) or path.shape != (self.B, n_new) or any((t.dtype, t.device) != (i32, dev) for t in (counts, path)):
+        n_new, kind = path.shape[1] if path.dim() == 2 else 0, (torch.int32, self.cache.device)
+        if counts.shape != (self.B,) or path.shape != (self.B, n_new) or (counts.dtype, counts.device) != kind or (path.dtype, path.device) != kind:
             raise ValueError("accept: counts [batch] and path [batch, n_new], int32 on the cache's device")
         if any(s is None or s[0].shape[1] != n_new for s in self._seen):
             raise ValueError("accept: verify of every layer comes first, of as many tokens")
-        # What commit will refuse must not weigh either: such a sequence's lengths are no lengths for it.
-        among = torch.arange(n_new, device=dev)[None] < counts[:, None]
-        above = torch.nn.functional.pad(path[:, :-1], (1, 0), value=-1)
-        good = ((path > above) & (path < n_new) | ~among).all(1) & (counts >= 0) & (counts <= n_new)
-        words = torch.where(among & good[:, None], torch.ones_like(path, dtype=torch.int64) << path.clamp(0, n_new - 1).long(), 0).sum(1)
-        self._weighed.copy_(torch.where(good.repeat(self.L)[:, None], self.cache.lengths, -1))
+        # What commit refuses must not weigh either: it is asked first, over caches without tokens, and what it leaves so has no lengths.
+        self._asked.lengths.zero_()
+        self.ctx.commit(self._asked, n_new, counts=counts.contiguous(), path=path.contiguous())
+        torch.where(self._asked.lengths == counts[:, None], self.cache.lengths.view(self.L, self.B, -1), self._none,
+                    out=self._weighed.view(self.L, self.B, -1))
+        words = torch.where(self._nth[:n_new] < counts[:, None], self._one << path, 0).sum(1)
         for cache, (q, scale, lse, tree) in zip(self._weighing, self._seen):
             self.ctx.weigh(cache, q, scale, lse, words, tree=tree, softcap=self.softcap, slopes=self.slopes, decay=self.decay)
         self.ctx.commit(self.cache, n_new, counts=counts.repeat(self.L), path=path.repeat(self.L, 1))
