@@ -339,6 +339,33 @@ __device__ __forceinline__ float biased(const AttendArgs& a, float x, const RowO
   return a.slopes ? fmaf(-o.slope2, (float)(o.position - key_position), x) : x;
 }
 
+// Maps of a cache's K and V, and a copy of a tile's slots: 64 columns after 64 columns, rows of 128 bytes, 128-byte swizzle.
+struct CacheMaps { CUtensorMap k, v; };
+inline bool cache_maps(const Ctx& ctx, const AttendArgs& a, int tile, CacheMaps* m) {
+  const CacheView& c = a.c;
+  const int batch = c.units / c.n_kv;
+  return tc_encode_cache(ctx, &m->k, c.k, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, tile) &&
+         tc_encode_cache(ctx, &m->v, c.v, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, tile);
+}
+__device__ __forceinline__ void tma_load_slots(uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot, int head, int seq, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%3, %4, %3, %5, %6}], [%2], %7;"
+      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(0), "r"(slot), "r"(head), "r"(seq), "l"(policy) : "memory");
+}
+// Where 16-byte chunk `chunk` of a row lies in a tile of ROWS rows.
+template <int ROWS>
+__device__ __forceinline__ uint32_t tile_at(int row, int chunk) { return (chunk >> 3) * (ROWS * 128) + row * 128 + (((chunk ^ row) & 7) << 4); }
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// Whether one of two bf16 is infinite or NaN.
+__device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+// A row's reference follows its maximum only where that outgrows it by 2^kSlack.
+constexpr float kSlack = 8.f;
+
 // A segment's end, by NT threads: the outputs of `sets` warps (a multiple of four) in shared memory, [set][RB][ROW] each against its own
 // reference, with references and sums [RB][SETS], become a partial.  sync: a barrier of the NT threads; none at the end.
 template <int D, int NT, int RB, int ROW, int SETS, typename Sync>

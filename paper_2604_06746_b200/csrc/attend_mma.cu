@@ -15,19 +15,12 @@ namespace skv {
 namespace {
 
 constexpr int kTileKeys = 64;
-constexpr float kSlack = 8.f;
 
 __device__ __forceinline__ void cp4(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
 // Arrives once this thread's cp.async copies so far are there (one of the barrier's expected arrivals).
 __device__ __forceinline__ void cp_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ void tma_load_slots(uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot, int head, int seq, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
-      "[%0], [%1, {%3, %4, %3, %5, %6}], [%2], %7;"
-      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(0), "r"(slot), "r"(head), "r"(seq), "l"(policy) : "memory");
-}
 __device__ __forceinline__ void ldsm(uint32_t at, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -42,23 +35,10 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-// Whether one of two bf16 is infinite or NaN.
-__device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 // Rows of D bf16 in shared memory: 16-byte chunk c of row r lies at chunk c ^ (r mod 8), so that eight rows' equal chunks are
 // in different banks.
 template <int D>
 __device__ __forceinline__ uint32_t chunk_at(int row, int chunk) { return row * (D * 2) + ((chunk ^ (row & 7)) << 4); }
-// The same within a tile that TMA wrote: 64 columns after 64 columns, rows of 128 bytes.
-__device__ __forceinline__ uint32_t tile_at(int row, int chunk) {
-  return (chunk >> 3) * (kTileKeys * 128) + row * 128 + (((chunk ^ row) & 7) << 4);
-}
-
-struct CacheMaps { CUtensorMap k, v; };
 
 // NR blocks of 8 rows; four warps along a tile's keys, NG groups of these.
 template <int D, int NR, int NG>
@@ -216,7 +196,7 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
           for (int e = lane; e < 2 * CH; e += 32) {
             const bool is_v = e >= CH;
             const int ch = is_v ? e - CH : e;
-            *(uint4*)(sm + st * S::kStage + (is_v ? S::kTileBytes : 0) + tile_at(row, ch)) = *(const uint4*)((is_v ? a.fresh.v : a.fresh.k) + from + ch * 16);
+            *(uint4*)(sm + st * S::kStage + (is_v ? S::kTileBytes : 0) + tile_at<kTileKeys>(row, ch)) = *(const uint4*)((is_v ? a.fresh.v : a.fresh.k) + from + ch * 16);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the place's next tile comes by TMA)
@@ -232,7 +212,7 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
         uint32_t kf[4];
-        ldsm(from + tile_at(kw * 16 + (lane & 15), kk * 2 + (lane >> 4)), kf);
+        ldsm(from + tile_at<kTileKeys>(kw * 16 + (lane & 15), kk * 2 + (lane >> 4)), kf);
 #pragma unroll
         for (int i = 0; i < NR; ++i) mma_16x8x16(acc[kk % CHAINS][i], kf[0], kf[1], kf[2], kf[3], qf[i][kk][0], qf[i][kk][1]);
       }
@@ -324,7 +304,7 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
         bool bad = false;
 #pragma unroll 2
         for (int i = lane; i < 16 * CH; i += 32) {
-          const uint4 w = *(const uint4*)(here + S::kTileBytes + tile_at(kw * 16 + i / CH, i % CH));
+          const uint4 w = *(const uint4*)(here + S::kTileBytes + tile_at<kTileKeys>(kw * 16 + i / CH, i % CH));
           bad |= not_finite(w.x) || not_finite(w.y) || not_finite(w.z) || not_finite(w.w);
         }
         plain = !__any_sync(0xffffffffu, bad);
@@ -333,7 +313,7 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
 #pragma unroll
         for (int k = 0; k < KK; ++k) {
           uint32_t vf[4];
-          ldsm_t(from + S::kTileBytes + tile_at(kw * 16 + (lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1)), vf);
+          ldsm_t(from + S::kTileBytes + tile_at<kTileKeys>(kw * 16 + (lane & 7) + (lane >> 4) * 8, k * 2 + ((lane >> 3) & 1)), vf);
 #pragma unroll
           for (int i = 0; i < NR; ++i) mma_16x8x16(o[i][k], vf[0], vf[1], vf[2], vf[3], pf[i][0], pf[i][1]);
         }
@@ -362,7 +342,7 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
             for (int k = 0; k < KK; ++k)
 #pragma unroll
               for (int y = 0; y < 2; ++y) {
-                const unsigned short h = *(const unsigned short*)(here + S::kTileBytes + tile_at(kw * 16 + j, k * 2 + y) + g8 * 2);
+                const unsigned short h = *(const unsigned short*)(here + S::kTileBytes + tile_at<kTileKeys>(kw * 16 + j, k * 2 + y) + g8 * 2);
                 const float v = __uint_as_float((uint32_t)h << 16);
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
@@ -532,7 +512,7 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
         if (OPT && a.slopes) { pos[0] = kp[g8]; pos[1] = kp[g8 + 8]; }
         uint32_t kf[KK][4];
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) ldsm(from + tile_at(kw * 16 + (lane & 15), kk * 2 + (lane >> 4)), kf[kk]);
+        for (int kk = 0; kk < KK; ++kk) ldsm(from + tile_at<kTileKeys>(kw * 16 + (lane & 15), kk * 2 + (lane >> 4)), kf[kk]);
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(st));
         const int j0 = t * kTileKeys + kw * 16;
@@ -578,12 +558,6 @@ weigh_mma(const __grid_constant__ AttendArgs a, const __grid_constant__ CacheMap
 }
 
 bool options(const AttendArgs& a) { return a.cap2 != 0.f || a.slopes; }
-bool encode(const Ctx& ctx, const AttendArgs& a, CacheMaps* m) {
-  const CacheView& c = a.c;
-  const int batch = c.units / c.n_kv;
-  return tc_encode_cache(ctx, &m->k, c.k, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTileKeys) &&
-         tc_encode_cache(ctx, &m->v, c.v, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTileKeys);
-}
 
 template <int D, int NR, int NG, bool OPT>
 cudaError_t launch_one(const AttendArgs& a, const CacheMaps& m, cudaStream_t st) {
@@ -605,14 +579,14 @@ cudaError_t launch_weigh(const AttendArgs& a, const CacheMaps& m, const unsigned
 
 cudaError_t launch_attend_mma(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st) {
   CacheMaps m;
-  if (!encode(ctx, a, &m)) return cudaErrorInvalidValue;
+  if (!cache_maps(ctx, a, kTileKeys, &m)) return cudaErrorInvalidValue;
   if (ctx.cfg.head_dim == 128) return options(a) ? launch_rows<128, true>(a, p, m, st) : launch_rows<128, false>(a, p, m, st);
   return options(a) ? launch_rows<64, true>(a, p, m, st) : launch_rows<64, false>(a, p, m, st);
 }
 
 cudaError_t launch_weigh_bf16(const Ctx& ctx, const AttendArgs& a, const unsigned long long* accepted, cudaStream_t st) {
   CacheMaps m;
-  if (!encode(ctx, a, &m)) return cudaErrorInvalidValue;
+  if (!cache_maps(ctx, a, kTileKeys, &m)) return cudaErrorInvalidValue;
   if (ctx.cfg.head_dim == 128) return options(a) ? launch_weigh<128, true>(a, m, accepted, st) : launch_weigh<128, false>(a, m, accepted, st);
   return options(a) ? launch_weigh<64, true>(a, m, accepted, st) : launch_weigh<64, false>(a, m, accepted, st);
 }

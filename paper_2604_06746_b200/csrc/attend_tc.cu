@@ -26,16 +26,7 @@ namespace skv {
 namespace {
 
 constexpr int kTile = 128, kThreads = 384;
-constexpr float kSlack = 8.f;
 
-struct CacheMaps { CUtensorMap k, v; };
-
-__device__ __forceinline__ void tma_load_slots(uint32_t dst, const CUtensorMap* map, uint32_t bar, int slot, int head, int seq, uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
-      "[%0], [%1, {%3, %4, %3, %5, %6}], [%2], %7;"
-      ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(0), "r"(slot), "r"(head), "r"(seq), "l"(policy) : "memory");
-}
 // An N-major operand of 64-element blocks of 128-byte rows (128-byte swizzle): blocks kTile rows apart, 8-row groups 1024 bytes.
 __device__ __forceinline__ uint64_t smem_desc_n(uint32_t addr) {
   return smem_desc(addr) & ~(0x3fffull << 16) | (uint64_t)((kTile * 128) >> 4) << 16;
@@ -99,14 +90,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&f)[32]) 
   tmem_st16(taddr + 16, hi);
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
-// 16-byte chunk of a row in a tile of 128-byte rows, 64 columns after 64 columns, 128-byte swizzle.
-__device__ __forceinline__ uint32_t tile_at(int row, int chunk) { return (chunk >> 3) * (kTile * 128) + row * 128 + (((chunk ^ row) & 7) << 4); }
 
 // MT: halves of 128 rows in a block.
 template <int D, int MT, bool OPT>
@@ -294,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
           if (!ok) break;
           // (rows behind the last key hold what the cache held there)
 #pragma unroll 8
-          for (int i = row1 * CH + lane; i < kTile * CH; i += 32) *(uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH)) = make_uint4(0, 0, 0, 0);
+          for (int i = row1 * CH + lane; i < kTile * CH; i += 32) *(uint4*)(sm + kRing + st * S::kUnit + tile_at<kTile>(i / CH, i % CH)) = make_uint4(0, 0, 0, 0);
           constexpr int kGo = 8;
 #pragma unroll 1
           for (int i0 = row0 * CH + lane; i0 < row1 * CH; i0 += 32 * kGo) {
@@ -302,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
 #pragma unroll
             for (int e = 0; e < kGo; ++e) {
               const int i = min(i0 + 32 * e, row1 * CH - 1);
-              x[e] = *(const uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH));
+              x[e] = *(const uint4*)(sm + kRing + st * S::kUnit + tile_at<kTile>(i / CH, i % CH));
             }
             bool bad = false;
 #pragma unroll
@@ -319,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
                   if ((w[f] & 0x7f80u) == 0x7f80u) w[f] &= 0xffff0000u;
                   if ((w[f] & 0x7f800000u) == 0x7f800000u) w[f] &= 0xffffu;
                 }
-                *(uint4*)(sm + kRing + st * S::kUnit + tile_at(i / CH, i % CH)) = make_uint4(w[0], w[1], w[2], w[3]);
+                *(uint4*)(sm + kRing + st * S::kUnit + tile_at<kTile>(i / CH, i % CH)) = make_uint4(w[0], w[1], w[2], w[3]);
               }
             }
           }
@@ -564,12 +547,8 @@ cudaError_t launch_d(const AttendArgs& a, const AttendPlan& p, const CacheMaps& 
 }  // namespace
 
 cudaError_t launch_attend_tc(const Ctx& ctx, const AttendArgs& a, const AttendPlan& p, cudaStream_t st) {
-  const CacheView& c = a.c;
   CacheMaps m;
-  const int batch = c.units / c.n_kv;
-  if (!tc_encode_cache(ctx, &m.k, c.k, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTile) ||
-      !tc_encode_cache(ctx, &m.v, c.v, c.capacity, c.n_kv, batch, c.s_token, c.s_head, c.s_batch, kTile))
-    return cudaErrorInvalidValue;
+  if (!cache_maps(ctx, a, kTile, &m)) return cudaErrorInvalidValue;
   return ctx.cfg.head_dim == 128 ? launch_d<128>(a, p, m, st) : launch_d<64>(a, p, m, st);
 }
 
