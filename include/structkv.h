@@ -564,6 +564,8 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
  * structkv_commit, with the q, scale, softcap, slopes, tree and n_new of the former and the lse that it wrote (rows, out,
  * accumulate and workspace are not looked at).
  *   accepted    device, [batch] 64-bit words; bits from n_new on are ignored.
+ * decay is applied once a call, however many tokens were accepted: three tokens one by one decay a weight three times, three at once
+ * a single time.  A caller who wants it by the token passes its power.
  * Sums are in fp32; they are added to a weight, which rounds it, once for every 8 (fp32 storage) or 64 rows.
  * Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
  */

@@ -10,8 +10,12 @@ namespace skv {
 namespace {
 
 // tcgen05's tiles have 128 rows, attend_mma's 16 at most: from 17 rows on the former takes them (single tokens of 17 heads and more stay,
-// 16 at a time, with the kernel that leaves the logits).  us, 32 heads over 8, attend_mma / attend_tc: 16 rows over 2048 keys 13.3 / 12.6,
-// 4 x 4096 18.8 / 24.7, 8 x 8192 46.8 / 53.4; 20 rows 12.8 / 12.7, 25.2 / 24.9, 73.0 / 53.1; 32 rows 13.4 / 12.8, 27.0 / 24.3, 75.5 / 52.0.
+// 16 at a time, with the kernel that leaves the logits).  us, attend_mma / attend_tc over 1 x 2048, 4 x 4096 and 8 x 8192 keys:
+//   32 heads over 8, d 128: 16 rows 12.2 / 12.7, 17.0 / 23.3, 45.4 / 53.5; 20 rows 13.1 / 12.9, 23.7 / 23.4, 71 / 54; 32 rows 13.5 / 13.0,
+//   26.3 / 22.9, 73 / 54.  16 over 8: 16 rows 13.2 / 12.7, 17.9 / 23.8, 45.3 / 53.2; 18 rows 14.1 / 13.0, 25.7 / 24.2, 71 / 54.
+//   28 over 4, d 128: 14 rows 12.9 / 12.2, 14.0 / 17.6, 27.2 / 34.4; 21 rows 11.8 / 12.3, 16.7 / 17.6, 39.8 / 35.6.
+//   32 over 8, d 64: 16 rows 9.4 / 11.3, 12.0 / 20.5, 26.4 / 45.4; 20 rows 9.5 / 11.3, 16.3 / 20.0, 43.9 / 45.6; 32 rows 10.1 / 11.2,
+//   17.6 / 20.1, 45.8 / 45.5: d 64 loses by the rule from 17 to 32 rows, by up to a fifth over few keys.
 bool by_tensor_cores(const structkv_config& cfg, int n_new) {
   return cfg.dtype == STRUCTKV_BF16 && n_new > 1 && cfg.n_q_heads / cfg.n_kv_heads * n_new > 16;
 }

@@ -4,12 +4,11 @@
 // r = i G + h, new token i and head h of the group.  An item is a unit's block of up to RB rows over all of its keys; items
 // follow one another unit after unit, and their key tiles, behind the places of 512 keys for what an item costs beside them, form one sequence of
 // W places.  C CTAs take runs of it whose lengths differ by one place at most: every CTA has equally much to do whatever the lengths,
-// which only the device knows.  (Without the places for the items' own cost 16 sequences of 1 to 5003 tokens took 45 us: a CTA that
-// got eight KV heads of one token was busy for 38, the others for 20.)  What a CTA has of
-// an item it leaves as a partial (row references, sums, unscaled output) in slot item + CTA, which no other pair has, so that an
+// which only the device knows.  (Without the places for the items' own cost a CTA that gets eight KV heads of one token is busy twice as
+// long as the others: figures at kOverKeys.)  What a CTA has of an item it leaves as a partial (row references, sums, unscaled output) in slot item + CTA, which no other pair has, so that an
 // item's partials lie side by side; attend_finish() merges them in that order: results do not depend on timing.  (Merged by the CTA
-// that leaves an item's last partial, which spares the launch, 1 x 1024 keys took 16.8 us instead of 13.4: all of its work then stands
-// in one row behind the last tile, on one SM.)
+// that leaves an item's last partial, which spares the launch, 1 x 1024 keys took 16.8 us when that version's two launches took 13.4,
+// which are down to 9.1 now: all of the merging stands in one row behind the last tile, on one SM.)
 #pragma once
 
 #include <atomic>

@@ -293,7 +293,8 @@ __global__ void __launch_bounds__(64 + 128 * NG, 1) attend_mma(const __grid_cons
         for (int e = 0; e < 4; ++e) p[e] = fast_exp2(s[i][e] - (m[i][e & 1] == -INFINITY ? 0.f : m[i][e & 1]));
         l[i][0] += p[0] + p[2];
         l[i][1] += p[1] + p[3];
-        // p keeps 8 bits for the product, as V does; the sum l is of the unrounded values
+        // p keeps 8 bits for the product, as V does; the sum l is of the unrounded values.  (Outputs over 16 x 16384 keys are off by 2.0e-3,
+        // relative, against 64 bits; with p in fp32 by 1.7e-3, which is the result's own rounding.)
         pf[i][0] = transposed(bf16x2(p[0], p[1]));
         pf[i][1] = transposed(bf16x2(p[2], p[3]));
       }

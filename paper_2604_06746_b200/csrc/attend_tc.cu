@@ -17,7 +17,8 @@
 // bound by the chain of one half's tile, 4250 clocks: scores loaded 290, maximum 145, reference 330, exponentials 1220, the
 // other quarters' 430, outputs 640, scores of the next tile 1050; products and exponentials alone would be 2048 each.  The
 // chain is not shortened by a quarter of the exponentials on the FMA pipe (their NaN need a maximum that keeps one: 88 us became
-// 92); scores of the next tile beside them would need tensor memory that outputs (256 columns) and scores (256) leave none of.
+// 92).  Not built: P takes half of the 128 columns that its scores had; half of the next tile's scores could be made in the other half
+// meanwhile.
 #include <algorithm>
 
 #include "attend.cuh"
@@ -446,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
                 float p0, p1;
                 unpack2(x, p0, p1);
                 sum = add2(sum, x);
-                // p keeps 8 bits for the product, as V does; the sum l is of the unrounded values
+                // p keeps 8 bits for the product, as V does; the sum l is of the unrounded values  (attend_mma.cu has the errors)
                 p[e / 2] = bf16x2(p0, p1);
               }
               tmem_st16(s_at + c / 2, p);                          // (over scores, which are in registers)

@@ -106,7 +106,9 @@ __global__ void __launch_bounds__(256) commit(const __grid_constant__ CacheView 
 //
 // A block goes through its steps once, each waiting for the one before: 128 units of 8320 tokens, 128 of which go, take 9.5 us (8.5 MB
 // read, 8.4 MB moved: 3 at the copy bandwidth): words there 1.3, keys 1.2, rank 1.7, lists 2.0, rows 1.5, their words and the
-// end 1.8; 256 units of 2049, one of which goes, 3.5.
+// end 1.8; 256 units of 2049, one of which goes, 3.5.  A block a unit is a choice: a cluster of CTAs a unit, as select.cu has it, is not
+// built.  Beyond 16384 tokens the words are read again for every level and for the lists: append, commit and eviction of 128 of 32896 for
+// 128 units take 57 us (10.5 for the bytes), of 1 of 32769 for 64 units 14 (2.6).
 constexpr int kList = 4096;
 struct EvictShared {
   RadixShared<1> radix;

@@ -210,8 +210,9 @@ class Prefill:
 class Decode:
     """Decoding over what a Prefill kept (the paper stops at the compacted cache).  A token's step is ``step`` for every layer, then
     ``advance``; drafted tokens, a tree of them or a chain, are looked at by ``verify`` for every layer, then ``accept`` keeps
-    some.  Cached tokens gather the attention weight that new ones give them; with a ``budget`` every KV head keeps its
-    ``recent`` newest tokens and the heaviest others.  All layers of all sequences are in one cache (sequence ``layer * batch +
+    some.  Cached tokens gather the attention weight that new ones give them, multiplied by ``decay`` once a ``step`` and once an
+    ``accept``, however many tokens that keeps; with a ``budget`` every KV head keeps its ``recent`` newest tokens and the
+    heaviest others.  All layers of all sequences are in one cache (sequence ``layer * batch +
     b``), so that commit and eviction are one launch each; every call can be captured into a graph.  Lengths live on the device:
     a KV head that has no room for new tokens is left as it is, and ``ctx.poll_device_status`` says so."""
 
