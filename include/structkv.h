@@ -566,7 +566,8 @@ structkv_status structkv_attend(structkv_ctx* ctx, const structkv_cache* cache, 
  *   accepted    device, [batch] 64-bit words; bits from n_new on are ignored.
  * decay is applied once a call, however many tokens were accepted: three tokens one by one decay a weight three times, three at once
  * a single time.  A caller who wants it by the token passes its power.
- * Sums are in fp32; they are added to a weight, which rounds it, once for every 8 (fp32 storage) or 64 rows.
+ * Sums are in fp32; they are added to a weight, which rounds it, once for every 8 (fp32 storage) or 64 rows.  A probability is as exact as
+ * lse in fp32 lets it be: off by 2^-23 |lse|, relative.
  * Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
  */
 structkv_status structkv_weigh(structkv_ctx* ctx, const structkv_cache* cache, const structkv_attend_args* args,

@@ -349,6 +349,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
         const bool idle = r - lane >= a.rows;                      // no row of this warp: it only keeps step
         const RowOptions ro = row_options(a, sg.u, min(r, a.rows - 1));
         float m = -INFINITY, l = 0.f;
+        // A reference is a rounded product of a score and the scale, the products in the exponents are not rounded: 2^-24 |m| apart.  Where
+        // that is more than 1/16 they are rounded as well (`far`).
 #pragma unroll 1
         for (int k = 0; k < jobs; ++k, ++done) {
           const int t = MT == 2 ? k : 2 * k + s, j0 = (sg.t0 + t) * kTile;
@@ -410,12 +412,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
               top = fmaxf(max3(t0, t1, v[kTile - 2]), v[kTile - 1]);
             }
             const float mul = OPT ? 1.f : scale2;
+            float times = mul;
             top *= mul;
+            auto far = [&] { return !OPT && r < a.rows && fabsf(m) > 0x1p20f; };   // (rows behind the last hold anything)
             const bool grown = top > m + kSlack;
-            if (__any_sync(0xffffffffu, grown)) {
+            if (__any_sync(0xffffffffu, grown || far())) {
               const float to = grown ? top : m, f = m == -INFINITY ? 0.f : fast_exp2(m - to);
               m = to;
               l *= f;
+              if (!OPT && __any_sync(0xffffffffu, far())) {
+#pragma unroll
+                for (int e = 0; e < kTile; ++e) v[e] *= mul;
+                times = 1.f;
+              }
               if (k > 0) {
                 if (!(ok = wait(o_done(s), (done - 1) & 1))) break;
                 tc_fence_after();
@@ -436,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_tc(const __grid_constant__
             // into step, and exponentials and products wait for one another (a key tile of 256 rows 5200 clocks).
             if (MT == 2 && done >= 1 - s && !(ok = wait(turn(s), (done - 1 + s) & 1))) break;
             const float ref = m == -INFINITY ? 0.f : m;
-            const uint64_t mul2 = pack2(mul, mul), ref2 = pack2(-ref, -ref);
+            const uint64_t mul2 = pack2(times, times), ref2 = pack2(-ref, -ref);
             uint64_t sum = pack2(0.f, 0.f);
 #pragma unroll
             for (int c = 0; c < kTile; c += 32) {
