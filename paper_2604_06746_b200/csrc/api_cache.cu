@@ -92,7 +92,10 @@ bool args_of(const structkv_ctx* ctx, const structkv_cache* cache, const structk
   if (!x->q || (uintptr_t)x->q % 16 || !strides_ok(elem, x->q_stride_batch, x->q_stride_token, x->q_stride_head)) return false;
   if (!std::isfinite(x->scale) || !std::isfinite(x->softcap) || x->softcap < 0.f || !std::isfinite(x->decay)) return false;
   if ((uintptr_t)x->slopes % 4 || (uintptr_t)x->tree % 8 || (uintptr_t)x->lse % 4) return false;
-  const float inv = x->softcap > 0.f ? x->scale / x->softcap : 0.f, cap2 = x->softcap * kLog2e;
+  // A cap beyond 2^100 |scale| caps nothing: tanh(y) is y to 24 bits for products of q and k below 2^88, and scale / softcap, or y, would lose
+  // bits below the smallest normal number.
+  const float softcap = x->softcap > 0x1p100f * std::fabs(x->scale) ? 0.f : x->softcap;
+  const float inv = softcap > 0.f ? x->scale / softcap : 0.f, cap2 = softcap * kLog2e;
   if (!std::isfinite(inv) || !std::isfinite(cap2) || !std::isfinite(x->scale * kLog2e)) return false;
   a->q = (const char*)x->q;
   a->q_batch = x->q_stride_batch * elem;
