@@ -595,6 +595,157 @@ structkv_status structkv_commit(structkv_ctx* ctx, const structkv_cache* cache, 
 structkv_status structkv_evict(structkv_ctx* ctx, const structkv_cache* cache, int budget, int recent, void* stream);
 
 /*
+ * Rotary positions.  Paper: Section 3.4, Eq. 12 (K' = f_RoPE(K, P'): kept tokens keep their positions).  A head's first `dim` elements form
+ * dim / 2 pairs (a, b); at position p pair c is turned by p * step[c], counted in 2^-64 of a turn, modulo one turn, and multiplied:
+ *     a' = amplitude (a cos - b sin),  b' = amplitude (b cos + a sin);
+ * the elements from `dim` on stay.  Angles are exact products of 64 bits: far positions lose nothing.  structkv_rope_init fills the block
+ * in, on the host and in extended precision, for frequencies f[c] = base^(-2c / dim) (radians a position), which scaling changes:
+ *   PLAIN   f.
+ *   LINEAR  f / factor.
+ *   BASE    base is base * factor^(dim / (dim - 2)); dim above 2.
+ *   BANDS   with turns = original f / 2 pi over the original context and part = (turns - slow) / (fast - slow) within [0, 1]:
+ *           part f + (1 - part) f / factor.
+ *   RAMP    the same form, part by the pair's number: with pair(t) = dim ln(original / (2 pi t)) / (2 ln base), lo = max(0, floor(pair(fast)))
+ *           and hi = min(dim - 1, ceil(pair(slow))): part = 1 - (c - lo) / max(hi - lo, 0.001) within [0, 1]; amplitude = 0.1 ln(factor) + 1
+ *           where factor is above 1.
+ *   dim         even, 2 .. STRUCTKV_ROPE_MAX_DIM;  interleaved  not 0: pairs are (2c, 2c + 1), else (c, c + dim / 2);  base above 1.
+ *   factor, original, slow, fast   what the scaling uses: positive and finite; slow below fast (the others are not looked at).
+ * Errors: INVALID_ARG.
+ */
+#define STRUCTKV_ROPE_MAX_DIM 128
+typedef enum {
+  STRUCTKV_ROPE_PLAIN = 0,
+  STRUCTKV_ROPE_LINEAR = 1,
+  STRUCTKV_ROPE_BASE = 2,
+  STRUCTKV_ROPE_BANDS = 3,
+  STRUCTKV_ROPE_RAMP = 4
+} structkv_rope_scaling;
+typedef struct {
+  int dim, interleaved;
+  float amplitude;
+  unsigned long long step[STRUCTKV_ROPE_MAX_DIM / 2];
+} structkv_rope;
+structkv_status structkv_rope_init(structkv_rope* rope, int dim, int interleaved, double base, int scaling, double factor,
+                                   double original, double slow, double fast);
+
+/*
+ * Rotates heads of the context's dtype and head_dim (any number of heads; rope->dim at most head_dim).
+ *   x, out      device, element (b, i, h, c) at x + b*x_stride_batch + i*x_stride_token + h*x_stride_head + c, out alike (bases 16-byte
+ *               aligned, strides multiples of 16 bytes; x's may be 0).  out is x with the same strides (in place), or they do
+ *               not overlap.
+ *   positions   device, token (b, i) at positions + b*positions_stride + i (0: the same for every b).  Any 32-bit number.
+ *   inverse     not 0: turned the other way, amplitude as it is: the transpose of the rotation, so the gradient of x from that of out.
+ * Computed in fp32 and rounded once.  batch * tokens below 2^31; none of the sizes is negative, and nothing is done where one is 0.
+ * Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
+ */
+typedef struct {
+  const void* x;
+  long long x_stride_batch, x_stride_token, x_stride_head;
+  void* out;
+  long long out_stride_batch, out_stride_token, out_stride_head;
+  const int* positions;
+  long long positions_stride;
+  int batch, tokens, heads;
+  int inverse;
+} structkv_rotate_args;
+structkv_status structkv_rotate(structkv_ctx* ctx, const structkv_rope* rope, const structkv_rotate_args* args, void* stream);
+
+/*
+ * A paged cache in 8 bits.  A page holds page_size tokens for every KV head, K and V as e4m3 codes; STRUCTKV_SCALE_BLOCK neighbouring
+ * slots of a head share a scale, a power of two 2^e held as the byte e + 127: a value is code * 2^e.  Sequence b's slot j is slot
+ * j mod page_size of page table[b, j / page_size].
+ *   k, v        device, element (page, g, slot, c) at k + page*stride_page + g*stride_head + slot*stride_token + c (bytes; d contiguous;
+ *               bases 16-byte aligned, strides multiples of 16; pages, heads and slots do not overlap).
+ *   k_scales, v_scales   device, [pages, H_kv, page_size / STRUCTKV_SCALE_BLOCK] bytes; what the calls write lies in 87 .. 247.
+ *   table       device, row b at table + b*table_stride, table_columns entries.  An entry that is looked at and is no page records
+ *               STRUCTKV_ERR_INVALID_ARG in the device status word; its slots are neither written nor seen.
+ *   lengths     device, [batch] int32, the tokens of a sequence.  One that is negative or leaves no room for the new tokens records
+ *               STRUCTKV_ERR_INVALID_ARG in the device status word, and nothing of that sequence is read or written but its rows of
+ *               an attention's output, which become those of a row that sees nothing.
+ *   page_size   16, 32, 64, 128 or 256.
+ * Full pages may be in several sequences' tables.  Calls on one cache are ordered by the caller (one stream).  All of them can be captured into
+ * graphs.  The context's device has to be current.
+ */
+#define STRUCTKV_SCALE_BLOCK 16
+typedef struct {
+  void *k, *v;
+  unsigned char *k_scales, *v_scales;
+  long long stride_page, stride_head, stride_token;
+  const int* table;
+  long long table_stride;
+  int table_columns;
+  int* lengths;
+  int batch, pages, page_size;
+} structkv_pages;
+
+/*
+ * Quantises the rows of new tokens into slots lengths[b] .. and up; K is rotated on the way.  `lengths` stays: the tokens count once the
+ * caller adds them.  Row r of sequence b comes from source token t = index[b, r], or r without an index, and has its position.
+ * A block of STRUCTKV_SCALE_BLOCK slots gets the smallest e, at least -40, with which its largest finite magnitude stays within 448 * 2^e;
+ * where it holds tokens already, the larger of that and the e that it has, to which their codes are rounded (to nearest, ties to even)
+ * anew.  What is not finite becomes NaN.  Values are rotated in fp32 and rounded once, to their codes.
+ *   k, v        device, element (b, t, g, c) at k + b*stride_batch + t*stride_token + g*stride_head + c, dtype of the context
+ *               (bases 16-byte aligned, strides multiples of 16 bytes, any order, 0 for a dimension that is broadcast).
+ *   tokens      source tokens of a sequence.
+ *   n_new       1 .. table_columns * page_size rows of a sequence at most; without an index n_new <= tokens.
+ *   counts      device, [batch] int32 or NULL: rows of each sequence, 0 .. n_new (else as a length without room).  NULL: n_new.
+ *   index       device, row b at index + b*index_stride, n_new entries, or NULL.  One that is no source token records
+ *               STRUCTKV_ERR_INVALID_ARG in the device status word; its row becomes 0.
+ *   rope        host, or NULL: K is not rotated.
+ *   positions   device, source token t of sequence b at positions + b*positions_stride + t; NULL without rope.
+ *   q, q_out    device or NULL: n_heads query heads of the new tokens, rotated in the same launch (without an index, with a rope; all n_new
+ *               of them, whatever counts says): element (b, i, h, c) at q + b*q_stride_batch + i*q_stride_token + h*q_stride_head + c,
+ *               q_out [batch, n_new, H, d] contiguous; q_out is q where that is contiguous, or they do not overlap.
+ * Errors: INVALID_ARG, CUDA.  Asynchronous on `stream`.
+ */
+typedef struct {
+  const void *k, *v;
+  long long stride_batch, stride_token, stride_head;
+  int tokens, n_new;
+  const int* counts;
+  const int* index;
+  long long index_stride;
+  const structkv_rope* rope;
+  const int* positions;
+  long long positions_stride;
+  const void* q;
+  long long q_stride_batch, q_stride_token, q_stride_head;
+  void* q_out;
+} structkv_append_pages_args;
+structkv_status structkv_append_pages(structkv_ctx* ctx, const structkv_pages* pages, const structkv_append_pages_args* args, void* stream);
+
+/*
+ * Attention of n_new (1 .. 64) new tokens a sequence, whose rows are in the slots behind lengths (structkv_append_pages), over the pages.
+ * With n = lengths[b], new token i < counts[b] and query head h of KV head g, over the slots j <= n + i:
+ *     x[j] = scale q.k[j], then softcap tanh(x / softcap) if softcap > 0;  lse = log sum_j exp(x[j]),  out = sum_j exp(x[j] - lse) v[j]
+ * A token i >= counts[b], and one that sees nothing, gets out 0 and lse minus infinity.
+ *   q           device, element (b, i, h, c) at q + b*q_stride_batch + i*q_stride_token + h*q_stride_head + c, dtype of the context, rotated
+ *               already; 16-byte aligned, strides multiples of 16 bytes.
+ *   counts      device, [batch] int32 or NULL: n_new.  Outside 0 .. n_new: as a length without room.
+ *   out         device, [batch, n_new, H, d] contiguous, dtype of the context, 16-byte aligned.
+ *   lse         device, [batch, n_new, H] fp32 or NULL.
+ *   workspace   device, 256-byte aligned, at least structkv_attend_pages_workspace_bytes() bytes (0 for arguments that are not
+ *               valid; slots: table_columns * page_size), caller-owned; calls that share it are ordered by the caller.
+ * Codes are exact operands; sums are in fp32; probabilities keep 11 bits for their product with V (22 for fp32 storage) where probability
+ * times V's scale is at least 2^-21 (2^-10) of the largest such product of its row, and below that are off by 2^-32 of it.  A NaN in V makes its
+ * column NaN in every row that sees the token, however small its probability; rows that do not see a token are not
+ * reached by it.  Errors: INVALID_ARG, WORKSPACE, CUDA.  Asynchronous on `stream`.
+ */
+typedef struct {
+  const void* q;
+  long long q_stride_batch, q_stride_token, q_stride_head;
+  int n_new;
+  const int* counts;
+  float scale, softcap;
+  void* out;
+  float* lse;
+  void* workspace;
+  size_t workspace_bytes;
+} structkv_attend_pages_args;
+size_t structkv_attend_pages_workspace_bytes(const structkv_config* cfg, int batch, int n_new, long long slots);
+structkv_status structkv_attend_pages(structkv_ctx* ctx, const structkv_pages* pages, const structkv_attend_pages_args* args, void* stream);
+
+/*
  * Self-test of the error path every device-side wait shares (the paper has no counterpart; the
  * conventions at the top of this header define it): launches one thread that waits, with the
  * scorer's bounded-wait helper and a bound of `limit_cycles` SM clock cycles (1 .. 4e9), on a

@@ -143,6 +143,27 @@ class CacheStruct(ctypes.Structure):
 MAX_NEW = 64
 lib.structkv_attend_workspace_bytes.restype = ctypes.c_size_t
 lib.structkv_attend_workspace_bytes.argtypes = [ctypes.POINTER(Config), _i, _i, _i]
+SCALE_BLOCK = 16
+MAX_ROPE_DIM = 128
+lib.structkv_attend_pages_workspace_bytes.restype = ctypes.c_size_t
+lib.structkv_attend_pages_workspace_bytes.argtypes = [ctypes.POINTER(Config), _i, _i, _ll]
+
+
+class PagesStruct(ctypes.Structure):
+    """structkv_pages."""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scales", _vp), ("v_scales", _vp), ("stride_page", _ll), ("stride_head", _ll),
+                ("stride_token", _ll), ("table", _vp), ("table_stride", _ll), ("table_columns", _i), ("lengths", _vp), ("batch", _i),
+                ("pages", _i), ("page_size", _i)]
+
+
+class RopeStruct(ctypes.Structure):
+    """structkv_rope."""
+    _fields_ = [("dim", _i), ("interleaved", _i), ("amplitude", _f), ("step", ctypes.c_ulonglong * (MAX_ROPE_DIM // 2))]
+
+
+_d = ctypes.c_double
+lib.structkv_rope_init.restype = _i
+lib.structkv_rope_init.argtypes = [ctypes.POINTER(RopeStruct), _i, _i, _d, _i, _d, _d, _d, _d]
 lib.structkv_selftest_wait_expiry.restype = _i
 lib.structkv_selftest_wait_expiry.argtypes = [_vp, ctypes.c_ulonglong, _vp]
 lib.structkv_selftest_ctas.restype = _i
@@ -248,6 +269,71 @@ class Cache:
     positions = property(lambda self: self._tensors[2])
     weights = property(lambda self: self._tensors[3])
     lengths = property(lambda self: self._tensors[4])
+
+
+class Rope:
+    """structkv_rope: rotary positions over the first ``dim`` elements of a head, paired (c, c + dim / 2), or neighbours where ``interleaved``.
+    ``scaling``: None, "linear", "base", "bands" or "ramp" (``factor``; the last two also take ``original``, ``slow``, ``fast``)."""
+
+    SCALINGS = (None, "linear", "base", "bands", "ramp")
+
+    def __init__(self, dim: int, base: float = 10000.0, interleaved: bool = False, scaling: Optional[str] = None, factor: float = 1.0,
+                 original: float = 0.0, slow: float = 1.0, fast: float = 32.0):
+        if scaling not in self.SCALINGS:
+            raise ValueError(f"scaling: one of {self.SCALINGS}")
+        self._struct = RopeStruct()
+        _check(lib.structkv_rope_init(ctypes.byref(self._struct), dim, int(interleaved), base, self.SCALINGS.index(scaling), factor,
+                                      original, slow, fast), "structkv_rope_init")
+        self.native = ctypes.addressof(self._struct)
+
+    dim = property(lambda self: self._struct.dim)
+    interleaved = property(lambda self: bool(self._struct.interleaved))
+    amplitude = property(lambda self: self._struct.amplitude)
+
+    @property
+    def turns(self) -> list:
+        """Turns per position of every pair."""
+        return [self._struct.step[c] / 2.0 ** 64 for c in range(self._struct.dim // 2)]
+
+
+class Pages:
+    """structkv_pages over tensors of the caller, which it keeps: ``k``, ``v [pages, H_kv, page_size, d]`` float8_e4m3fn (same strides, ``d``
+    contiguous), ``k_scales``, ``v_scales [pages, H_kv, page_size / 16]`` float8_e8m0fnu, ``table [batch, columns]`` int32 (page numbers,
+    contiguous rows), ``lengths [batch]`` int32: sequence ``b`` has ``lengths[b]`` tokens in the pages ``table[b]``."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, table: torch.Tensor,
+                 lengths: torch.Tensor):
+        assert k.dim() == 4 and k.dtype == torch.float8_e4m3fn and v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride()
+        assert k.stride(3) == 1
+        pages, n_kv, page_size, d = k.shape
+        for s in (k_scales, v_scales):
+            assert s.shape == (pages, n_kv, page_size // SCALE_BLOCK) and s.dtype == torch.float8_e8m0fnu and s.is_contiguous()
+        assert page_size in (16, 32, 64, 128, 256), "page_size: 16, 32, 64, 128 or 256"
+        assert table.dim() == 2 and table.dtype == torch.int32 and (table.shape[1] <= 1 or table.stride(1) == 1) and table.shape[1] >= 1
+        assert lengths.shape == (table.shape[0],) and lengths.dtype == torch.int32 and lengths.is_contiguous()
+        assert k.is_cuda and all(t.device == k.device for t in (v, k_scales, v_scales, table, lengths))
+        self._tensors = (k, v, k_scales, v_scales, table, lengths)
+        self._struct = PagesStruct(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                                   table.data_ptr(), table.stride(0), table.shape[1], lengths.data_ptr(), table.shape[0], pages, page_size)
+        self.slots = table.shape[1] * page_size
+        self.native = (ctypes.addressof(self._struct), k.device.index, table.shape[0], n_kv, d, self.slots)
+        self.batch, self.n_kv_heads, self.head_dim, self.page_size, self.device = table.shape[0], n_kv, d, page_size, k.device
+
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_scales = property(lambda self: self._tensors[2])
+    v_scales = property(lambda self: self._tensors[3])
+    table = property(lambda self: self._tensors[4])
+    lengths = property(lambda self: self._tensors[5])
+
+    @staticmethod
+    def empty(pages: int, n_kv_heads: int, page_size: int, head_dim: int, table: torch.Tensor, lengths: torch.Tensor) -> "Pages":
+        """New storage for ``pages`` pages on the table's device; what it holds is not looked at before it is written."""
+        k, v = (torch.empty((pages, n_kv_heads, page_size, head_dim), dtype=torch.uint8, device=table.device).view(torch.float8_e4m3fn)
+                for _ in range(2))
+        scales = (torch.zeros((pages, n_kv_heads, page_size // SCALE_BLOCK), dtype=torch.uint8, device=table.device).view(torch.float8_e8m0fnu)
+                  for _ in range(2))
+        return Pages(k, v, *scales, table, lengths)
 
 
 class Context:
@@ -493,6 +579,44 @@ class Context:
         ``attend`` that wrote ``lse``."""
         _check(_native.weigh(self._h.value, self.cfg.n_q_heads, self._of(cache), q, scale, lse, accepted, tree, softcap,
                              slopes, decay, stream), "structkv_weigh")
+
+    # ---- rotary positions, a paged cache in 8 bits --------------------------------------------
+    def rotate(self, x: torch.Tensor, positions: torch.Tensor, rope: Rope, out: Optional[torch.Tensor] = None, inverse: bool = False,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+        """structkv_rotate: ``x``, ``out [batch, tokens, heads, d]`` of any strides (``out`` None: in place), ``positions [batch, tokens]``
+        or ``[tokens]`` int32.  ``inverse``: the transpose, which takes the gradient of ``out`` to that of ``x``."""
+        _check(_native.rotate(self._h.value, self.cfg.dtype, self.cfg.head_dim, self.device.index or 0, x, positions, rope.native, out,
+                              inverse, stream), "structkv_rotate")
+
+    def _pages(self, pages: Pages) -> tuple:
+        assert pages.n_kv_heads == self.cfg.n_kv_heads and pages.head_dim == self.cfg.head_dim, "the pages have another shape than the context"
+        return pages.native
+
+    def append_pages(self, pages: Pages, k_new: torch.Tensor, v_new: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                     rope: Optional[Rope] = None, counts: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None,
+                     q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> None:
+        """structkv_append_pages: rows ``[batch, tokens, H_kv, d]``, all of them or those that ``index [batch, n_new]`` (or ``[n_new]``) names,
+        ``counts [batch]`` of them for each sequence; K is rotated by ``rope`` at ``positions [batch, tokens]`` (or ``[tokens]``), and so
+        are the queries ``q [batch, tokens, H, d]`` that come along, into ``q_out`` (None: in place)."""
+        _check(_native.append_pages(self._h.value, self.cfg.n_q_heads, self.cfg.dtype, self._pages(pages), k_new, v_new, positions,
+                                    None if rope is None else rope.native, counts, index, q, q_out, stream), "structkv_append_pages")
+
+    def attend_pages_workspace(self, pages: Pages, n_new: int) -> torch.Tensor:
+        """A workspace for ``attend_pages`` with ``n_new`` new tokens a sequence over ``pages``."""
+        self._pages(pages)
+        n = lib.structkv_attend_pages_workspace_bytes(ctypes.byref(self.cfg), pages.batch, n_new, pages.slots)
+        if n == 0:
+            raise StructKVError(ERR_INVALID_ARG, "structkv_attend_pages_workspace_bytes")
+        return torch.empty(n, dtype=torch.uint8, device=pages.device)
+
+    def attend_pages(self, pages: Pages, q: torch.Tensor, scale: float, out: torch.Tensor, workspace: torch.Tensor,
+                     counts: Optional[torch.Tensor] = None, softcap: float = 0.0, lse: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None) -> None:
+        """structkv_attend_pages: ``q``, ``out [batch, n_new, H, d]`` of the tokens behind ``lengths`` (which ``append_pages`` wrote),
+        ``counts [batch]`` of them for each sequence; ``lse [batch, n_new, H]`` float32."""
+        _check(_native.attend_pages(self._h.value, self.cfg.n_q_heads, self.cfg.dtype, self._pages(pages), q, scale, out, workspace, counts,
+                                    softcap, lse, stream), "structkv_attend_pages")
 
     def commit(self, cache: Cache, n_new: int, counts: Optional[torch.Tensor] = None, path: Optional[torch.Tensor] = None,
                stream: Optional[torch.cuda.Stream] = None) -> None:

@@ -1,0 +1,460 @@
+// Attention of new tokens over a paged cache in 8 bits.
+//
+// One pass: per row a reference m, sum l and unscaled output O over the keys seen so far.  16 keys at a time, which share a scale of K
+// and one of V, give S = K Q^T, y = x + e_v (x in bits, 2^e_v the scale of V), w = 2^(y - m), l += 2^-e_v sum w, O^T += V^T w.  V's scale
+// goes with the weights, and references follow what a key weighs in O: codes are exact operands of fp16 products, whose weights keep 11
+// bits as long as they matter to O, whatever the scales.  Queries become fp16 as well, times a power of two that brings the
+// row's largest element to 2^13 .. 2^14: bf16 queries lose nothing within 2^-28 of it; fp32 ones go in two pieces, as their weights do.
+//
+// Reading K and V is the bound, so a warp's loads go straight into the operands' registers: keys are the long side of the m16n8k16
+// products, and neither the order of a row's elements within QK^T nor that of V's columns matters as long as both sides have the
+// same, so that 16 bytes of a row are four products' share of a lane.  A warp takes every NW-th 16 keys of the CTA's run, with
+// statistics of its own; nothing is waited for but loads, and a segment's end merges the warps.  References follow a row's maximum only
+// where that outgrows it by 2^kSlack.
+#include <algorithm>
+
+#include "attend_pages.cuh"
+
+namespace skv {
+namespace {
+
+constexpr float kRaise = 7.f;          // weights are up to 2^(kRaise + kSlack): fp16 keeps those down to 2^-31 of the largest
+
+__device__ __forceinline__ uint4 load16(const char* p) {
+  uint4 x;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+  return x;
+}
+__device__ __forceinline__ uint2 load8(const char* p) {
+  uint2 x;
+  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "l"(p));
+  return x;
+}
+// Codes of a word's lower and upper half as two fp16 each.
+__device__ __forceinline__ uint32_t half_lo(uint32_t w) {
+  uint32_t x;
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %1;\ncvt.rn.f16x2.e4m3x2 %0, a;\n}" : "=r"(x) : "r"(w));
+  return x;
+}
+__device__ __forceinline__ uint32_t half_hi(uint32_t w) {
+  uint32_t x;
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %1;\ncvt.rn.f16x2.e4m3x2 %0, b;\n}" : "=r"(x) : "r"(w));
+  return x;
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// What two values lose as fp16, as fp16.
+__device__ __forceinline__ uint32_t rest2(float lo, float hi, uint32_t of) {
+  float a, b;
+  asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.f32.f16 %0, x;\ncvt.f32.f16 %1, y;\n}" : "=f"(a), "=f"(b) : "r"(of));
+  return f16x2(lo - a, hi - b);
+}
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+// A word's bytes that are NaN codes, as 0x80 of each.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ float exp2i(int e) { return __int_as_float(min(max(127 + e, 1), 254) << 23); }   // within fp32's normal numbers
+
+template <int D, int NR, int NW>
+struct PagesShape {
+  static constexpr int RB = 8 * NR, kRow = D + 4;
+  static constexpr int kSmem = NW * RB * (kRow + 2) * 4;
+};
+
+// NR: blocks of 8 rows; F32: fp32 storage; CAP: capped scores; NW: warps.
+template <int D, int NR, bool F32, bool CAP, int NW, int PER>
+__global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_constant__ AttendPagesArgs a) {
+  using S = PagesShape<D, NR, NW>;
+  constexpr int RB = S::RB, KK = D / 16, KH = D / 64, PIECES = F32 ? 2 : 1, VW = D / 32;   // VW: words of V a lane has of a key
+  extern __shared__ float smem[];
+  float* const outs = smem;                                      // [warp][RB][kRow]
+  float* const refs = outs + NW * RB * S::kRow;                  // [RB][warp]
+  float* const sums = refs + RB * NW;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
+  pdl_trigger();
+  pdl_wait();
+  const PageRun run = find_run(a, blockIdx.x == 0 ? a.seq_start : nullptr);
+  PageSegment sg = first_segment(a, run);
+  const int sh4 = a.c.page_shift - kBlockShift, per_page = 1 << sh4;
+#pragma unroll 1
+  for (; sg.t1; next_segment(sg, a)) {
+    const int b = sg.b, g = quotient(sg.nth, a.by_blocks), rb = sg.nth - g * a.blocks;
+    const int n_old = a.c.lengths[b], first_row = rb * RB + 2 * t4;
+    const int s_end = min(sg.t1 * (kPageTile / 16), (sg.keys + 15) / 16);
+    int s = sg.t0 * (kPageTile / 16) + warp;
+    const int* const table = (const int*)((const char*)a.c.table + b * a.c.s_table);
+    const char *const k0 = a.c.k + g * a.c.s_head + t4 * 16, *const v0 = a.c.v + g * a.c.s_head + g8 * (VW * 4);
+    // (a page that is none: its slots are not seen; the loads go to page 0)
+    auto page_of = [&](int step) { return step < s_end ? table[step >> sh4] : 0; };
+    struct At { size_t page, scale; int slot; bool bad; };
+    auto at_of = [&](int step, int page) {
+      const bool bad = page < 0 || page >= a.c.pages;
+      const size_t p = bad ? 0 : page;
+      return At{p, ((p * a.c.n_kv + g) << sh4) + (step & (per_page - 1)), (step & (per_page - 1)) << kBlockShift, bad};
+    };
+    uint4 kb[2][KH];
+    uint32_t vb[4][VW];
+    int ke = 0, ve = 0;
+    auto load_k = [&](const At& x) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int h = 0; h < KH; ++h) kb[y][h] = load16(k0 + x.page * a.c.s_page + (x.slot + g8 + 8 * y) * a.c.s_token + h * 64);
+      ke = a.c.k_scales[x.scale];
+    };
+    auto load_v = [&](const At& x) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const char* const p = v0 + x.page * a.c.s_page + (x.slot + 2 * t4 + (e & 1) + 8 * (e >> 1)) * a.c.s_token;
+        if constexpr (VW == 4) {
+          const uint4 w = load16(p);
+          vb[e][0] = w.x; vb[e][1] = w.y; vb[e][2] = w.z; vb[e][3] = w.w;
+        } else {
+          const uint2 w = load8(p);
+          vb[e][0] = w.x; vb[e][1] = w.y;
+        }
+      }
+      ve = a.c.v_scales[x.scale];
+    };
+    At now = at_of(s, page_of(s));
+    if (s < s_end) {
+      load_k(now);
+      load_v(now);
+    }
+    int next_page = page_of(s + NW);
+
+    // the rows
+    uint32_t qf[PIECES][NR][KK][2];
+    float qs[NR][2];                                             // a row's factor: scale in bits (capped scores: 1), times 2^-the raise of its queries
+    float o[NR][KK][4], m[NR][2], l[NR][2];                      // o[.][t]: columns 16 g8 (8 g8) + 2 t and + 1 of rows 2 t4 and + 1
+    int last[NR][2];                                             // the last slot that a row sees
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int r = rb * RB + 8 * i + g8;
+      const bool is = r < a.rows;
+      const int tok = is ? quotient(r, a.by_group) : 0, h = is ? r - tok * a.group : 0;
+      const char* const q = a.q + b * a.q_batch + tok * a.q_token + (g * a.group + h) * a.q_head;
+      float x[KK][4];                                            // of the lane's 16 elements in each 64
+      float top = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const int c = kk / 4 * 64 + t4 * 16 + kk % 4 * 4;
+        if (F32) {
+          const float4 w = is ? *(const float4*)(q + c * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+          x[kk][0] = w.x; x[kk][1] = w.y; x[kk][2] = w.z; x[kk][3] = w.w;
+        } else {
+          const uint2 w = is ? *(const uint2*)(q + c * 2) : make_uint2(0u, 0u);
+          x[kk][0] = __uint_as_float(w.x << 16); x[kk][1] = __uint_as_float(w.x & 0xffff0000u);
+          x[kk][2] = __uint_as_float(w.y << 16); x[kk][3] = __uint_as_float(w.y & 0xffff0000u);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[kk][e]));
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // raise: top's exponent becomes 13  (rows of zeros, tiny or infinite ones: as far as fp32's exponents go)
+      const int raise = min(max(13 - ((int)(__float_as_uint(top) >> 23) - 127), -113), 126);
+      const float up = exp2i(raise);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const float lo = x[kk][2 * y] * up, hi = x[kk][2 * y + 1] * up;
+          qf[0][i][kk][y] = f16x2(lo, hi);
+          if (F32) qf[PIECES - 1][i][kk][y] = rest2(lo, hi, qf[0][i][kk][y]);
+        }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int down = __shfl_sync(0xffffffffu, raise, (2 * t4 + e) * 4);
+        qs[i][e] = exp2i(-down) * (CAP ? 1.f : a.scale2);
+        last[i][e] = n_old + quotient(min(first_row + 8 * i + e, a.rows - 1), a.by_group);
+        m[i][e] = -INFINITY;
+        l[i][e] = 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < KK; ++k) o[i][k][0] = o[i][k][1] = o[i][k][2] = o[i][k][3] = 0.f;
+    }
+
+#pragma unroll 1
+    while (s < s_end) {
+      const int sn = s + NW, j0 = s << kBlockShift;
+      const bool more = sn < s_end;
+      const At next = at_of(sn, next_page);
+      next_page = page_of(sn + NW);
+      // products: two chains where a warp has one block of rows
+      constexpr int CHAINS = NR == 1 ? 2 : 1;
+      float acc[CHAINS][NR][4];
+#pragma unroll
+      for (int c = 0; c < CHAINS; ++c)
+#pragma unroll
+        for (int i = 0; i < NR; ++i) acc[c][i][0] = acc[c][i][1] = acc[c][i][2] = acc[c][i][3] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const uint32_t* const w0 = (const uint32_t*)&kb[0][kk / 4];
+        const uint32_t* const w1 = (const uint32_t*)&kb[1][kk / 4];
+        const uint32_t x0 = half_lo(w0[kk % 4]), x1 = half_lo(w1[kk % 4]), x2 = half_hi(w0[kk % 4]), x3 = half_hi(w1[kk % 4]);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+          for (int i = 0; i < NR; ++i) mma(acc[kk % CHAINS][i], x0, x1, x2, x3, qf[p][i][kk][0], qf[p][i][kk][1]);
+      }
+      const float kf = exp2i(ke - 127), vl = exp2i(127 - ve), vx = (float)(ve - 127);
+      if (more) load_k(next);
+      float y[NR][4];                                            // element 2 z + x: key g8 + 8 z, row x
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[i][e] = (CHAINS == 2 ? acc[0][i][e] + acc[CHAINS - 1][i][e] : acc[0][i][e]) * (qs[i][e & 1] * kf);
+        if (CAP) {
+          capped2(y[i][0], y[i][1], pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
+          capped2(y[i][2], y[i][3], pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[i][e] += vx;
+      }
+      const bool tail = j0 + 16 > n_old + 1 || now.bad;
+      uint32_t odd[4] = {0u, 0u, 0u, 0u};                        // columns of the lane's four keys whose V is NaN, as bits
+      bool any_odd = false;
+      if (tail) {
+        if (now.bad && lane == 0) tell_invalid(a.c);
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (now.bad || j0 + g8 + 8 * (e >> 1) > last[i][e & 1]) y[i][e] = -INFINITY;
+        // What holds NaN here reaches only rows that see it (0 x NaN): it is taken out, and put to those at the end.
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int w = 0; w < VW; ++w) {
+            const uint32_t is = nan_bytes(vb[e][w]);
+            vb[e][w] &= ~((is >> 7) * 0xffu);
+            odd[e] |= ((is >> 7 & 1) | (is >> 14 & 2) | (is >> 21 & 4) | (is >> 28 & 8)) << (4 * w);
+          }
+        any_odd = __any_sync(0xffffffffu, (odd[0] | odd[1] | odd[2] | odd[3]) != 0) && !now.bad;
+      }
+      // references
+      bool grown = false;
+#pragma unroll
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) grown |= fmaxf(y[i][e], y[i][2 + e]) - kRaise > m[i][e] + kSlack;
+      if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float t = fmaxf(y[i][e], y[i][2 + e]);
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            t = fmaxf(t - kRaise, m[i][e]);
+            const float f = m[i][e] == -INFINITY ? 0.f : fast_exp2(m[i][e] - t);
+            m[i][e] = t;
+            l[i][e] *= f;
+#pragma unroll
+            for (int k = 0; k < KK; ++k) { o[i][k][e] *= f; o[i][k][2 + e] *= f; }
+          }
+      }
+      uint32_t pf[PIECES][NR][2];                                // keys 2 t4 and + 1 (+ 8), row g8
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = fast_exp2(y[i][e] - (m[i][e & 1] == -INFINITY ? 0.f : m[i][e & 1]));
+        l[i][0] = fmaf(p[0] + p[2], vl, l[i][0]);
+        l[i][1] = fmaf(p[1] + p[3], vl, l[i][1]);
+        // weights keep 11 bits for the product (22 for fp32 storage); the sum is of the unrounded ones
+        const uint32_t w0 = f16x2(p[0], p[1]), w1 = f16x2(p[2], p[3]);
+        pf[0][i][0] = transposed(w0);
+        pf[0][i][1] = transposed(w1);
+        if (F32) {
+          pf[PIECES - 1][i][0] = transposed(rest2(p[0], p[1], w0));
+          pf[PIECES - 1][i][1] = transposed(rest2(p[2], p[3], w1));
+        }
+      }
+#pragma unroll
+      for (int w = 0; w < VW; ++w) {
+        const uint32_t a0 = __byte_perm(vb[0][w], vb[1][w], 0x5140), a1 = __byte_perm(vb[0][w], vb[1][w], 0x7362);
+        const uint32_t b0 = __byte_perm(vb[2][w], vb[3][w], 0x5140), b1 = __byte_perm(vb[2][w], vb[3][w], 0x7362);
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const uint32_t x = z ? a1 : a0, x2 = z ? b1 : b0, f0 = half_lo(x), f1 = half_hi(x), f2 = half_lo(x2), f3 = half_hi(x2);
+#pragma unroll
+          for (int q = 0; q < PIECES; ++q)
+#pragma unroll
+            for (int i = 0; i < NR; ++i) mma(o[i][2 * w + z], f0, f1, f2, f3, pf[q][i][0], pf[q][i][1]);
+        }
+      }
+      if (more) load_v(next);
+      if (any_odd) {
+#pragma unroll 1
+        for (int c = 0; c < 16; ++c) {                           // lane c / 4 of the four has key 2 (c / 4) + (c & 1) + 8 (c / 2 & 1)
+          const uint32_t mine = c & 2 ? (c & 1 ? odd[3] : odd[2]) : (c & 1 ? odd[1] : odd[0]);
+          const uint32_t cols = __shfl_sync(0xffffffffu, mine, (lane & 28) | c >> 2);
+          const int j = j0 + 2 * (c >> 2) + (c & 1) + 8 * (c >> 1 & 1);
+#pragma unroll
+          for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int k = 0; k < KK; ++k)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if ((cols >> (2 * k + (e >> 1)) & 1) && j <= last[i][e & 1]) o[i][k][e] = __int_as_float(0x7fffffff);
+        }
+      }
+      s = sn;
+      now = next;
+    }
+
+    // the segment ends: its warps' outputs, each against its own reference, then their sum against a common one
+    const int sets = min(NW, s_end - sg.t0 * (kPageTile / 16));
+    if (warp < sets) {
+#pragma unroll
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+          for (int d = 4; d < 32; d *= 2) l[i][e] += __shfl_xor_sync(0xffffffffu, l[i][e], d);
+          const int row = 8 * i + 2 * t4 + e;
+          if (g8 == 0) {
+            refs[row * NW + warp] = m[i][e];
+            sums[row * NW + warp] = l[i][e];
+          }
+          float* const to = outs + (warp * RB + row) * S::kRow + g8 * (2 * KK);
+#pragma unroll
+          for (int k = 0; k < KK; k += 2) *(float4*)(to + 2 * k) = make_float4(o[i][k][e], o[i][k][2 + e], o[i][k + 1][e], o[i][k + 1][2 + e]);
+        }
+    }
+    __syncthreads();
+    const int slot = b * a.c.n_kv * a.blocks + sg.nth + blockIdx.x, rows = min(RB, a.rows - rb * RB);
+#pragma unroll 1
+    for (int i = tid; i < rows * (D / 4); i += NW * 32) {
+      const int row = i / (D / 4), c4 = i % (D / 4);
+      float top = -INFINITY, sum = 0.f;
+      for (int w = 0; w < sets; ++w) top = fmaxf(top, refs[row * NW + w]);
+      const float base = top == -INFINITY ? 0.f : top;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int w = 0; w < sets; ++w) {
+        const float f = fast_exp2(refs[row * NW + w] - base);
+        const float4 x = *(const float4*)(outs + (w * RB + row) * S::kRow + c4 * 4);
+        sum = fmaf(f, sums[row * NW + w], sum);
+        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+      }
+      *(float4*)(a.part_out + ((size_t)slot * RB + row) * D + c4 * 4) = v;
+      if (c4 == 0) a.part_stat[(size_t)slot * RB + row] = make_float2(top, sum);
+    }
+    __syncthreads();
+  }
+}
+
+// Merges an item's partials, a warp a row: M = max m_c, out = sum 2^(m_c - M) O_c / sum 2^(m_c - M) l_c, c ascending.
+constexpr int kFinishThreads = 128;
+
+template <int D, bool F32>
+__global__ void __launch_bounds__(kFinishThreads) attend_pages_finish(const __grid_constant__ AttendPagesArgs a, int rb_rows) {
+  constexpr int DL = D / 32, kAhead = 8;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long all = (long long)a.c.batch * a.c.n_kv * a.rows;
+  pdl_trigger();
+  pdl_wait();
+  const int W1 = a.seq_start[a.c.batch], items = a.c.n_kv * a.blocks;
+  const Shares sh = shares_of(W1 * items, a.ctas, a.by_ctas, a.least);
+#pragma unroll 1
+  for (long long at = (long long)blockIdx.x * (kFinishThreads / 32) + warp; at < all; at += (long long)gridDim.x * (kFinishThreads / 32)) {
+    const int u = quotient((int)at, a.by_rows), r = (int)at - u * a.rows, rb = r / rb_rows, row = r - rb * rb_rows;
+    const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, tok = quotient(r, a.by_group), h = r - tok * a.group;
+    const int before = a.seq_start[b], places = a.seq_start[b + 1] - before, count = a.counts ? a.counts[b] : a.n_new;
+    float M = -INFINITY, L = 0.f, acc[DL];
+#pragma unroll
+    for (int e = 0; e < DL; ++e) acc[e] = 0.f;
+    if (places > 0 && tok < count) {
+      const int start = before * items + (g * a.blocks + rb) * places, c0 = cta_of(sh, start + a.over), c1 = cta_of(sh, start + places - 1);
+      const int first = (b * a.c.n_kv + g) * a.blocks + rb + c0, parts = c1 - c0 + 1;
+      const float2* const stat = a.part_stat + (size_t)first * rb_rows + row;
+      const float* const from = a.part_out + ((size_t)first * rb_rows + row) * D + lane * DL;
+#pragma unroll 1
+      for (int c = 0; c < parts; c += kAhead) {
+        float2 st[kAhead];
+        float x[kAhead][DL];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          const int k = min(c + e, parts - 1);
+          st[e] = stat[(size_t)k * rb_rows];
+#pragma unroll
+          for (int d = 0; d < DL; ++d) x[e][d] = from[(size_t)k * rb_rows * D + d];
+        }
+        float top = M;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          if (c + e >= parts) st[e] = make_float2(-INFINITY, 0.f);
+          top = fmaxf(top, st[e].x);
+        }
+        const float ref = top == -INFINITY ? 0.f : top, f = fast_exp2(M - ref);
+        M = top;
+        L *= f;
+#pragma unroll
+        for (int d = 0; d < DL; ++d) acc[d] *= f;
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+          if (c + e < parts) {
+            const float w = fast_exp2(st[e].x - ref);
+            L = fmaf(w, st[e].y, L);
+#pragma unroll
+            for (int d = 0; d < DL; ++d) acc[d] = fmaf(w, x[e][d], acc[d]);
+          }
+      }
+    }
+    const bool nothing = M == -INFINITY && L == 0.f;
+    const float inv = nothing ? 0.f : 1.f / L;
+    const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
+#pragma unroll
+    for (int d = 0; d < DL; ++d) acc[d] = nothing ? 0.f : acc[d] * inv;
+    if (F32) {
+#pragma unroll
+      for (int d = 0; d < DL; ++d) ((float*)a.out)[q * D + lane * DL + d] = acc[d];
+    } else {
+#pragma unroll
+      for (int d = 0; d < DL; d += 2) ((uint32_t*)a.out)[(q * D + lane * DL + d) / 2] = bf16x2(acc[d], acc[d + 1]);
+    }
+    if (lane == 0 && a.lse) a.lse[q] = nothing ? -INFINITY : (M + log2f(L)) * kLn2;
+  }
+}
+
+template <int D, int NR, bool F32, bool CAP, int NW, int PER>
+cudaError_t launch_one(const AttendPagesArgs& a, cudaStream_t st) {
+  using S = PagesShape<D, NR, NW>;
+  const cudaError_t e = allow_smem<attend_pages<D, NR, F32, CAP, NW, PER>>(S::kSmem);
+  return e != cudaSuccess ? e : launch_pdl(attend_pages<D, NR, F32, CAP, NW, PER>, dim3(a.ctas), dim3(NW * 32), S::kSmem, st, a);
+}
+template <int D, bool CAP>
+cudaError_t launch_rows(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
+  if (ctx.cfg.dtype == STRUCTKV_FP32) return launch_one<D, 1, true, CAP, 8, 1>(a, st);
+  return p.rb == 8 ? launch_one<D, 1, false, CAP, 16, 1>(a, st) : launch_one<D, 2, false, CAP, 8, 1>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_pages(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
+  if (ctx.cfg.head_dim == 128) return a.cap2 != 0.f ? launch_rows<128, true>(ctx, a, p, st) : launch_rows<128, false>(ctx, a, p, st);
+  return a.cap2 != 0.f ? launch_rows<64, true>(ctx, a, p, st) : launch_rows<64, false>(ctx, a, p, st);
+}
+
+cudaError_t launch_attend_pages_finish(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
+  const long long rows = (long long)a.c.batch * a.c.n_kv * a.rows;
+  const dim3 grid((unsigned)std::min<long long>((rows + 3) / 4, 16ll * ctx.sm_count));
+  const bool f32 = ctx.cfg.dtype == STRUCTKV_FP32;
+  auto* const kernel = ctx.cfg.head_dim == 128 ? (f32 ? attend_pages_finish<128, true> : attend_pages_finish<128, false>)
+                                               : (f32 ? attend_pages_finish<64, true> : attend_pages_finish<64, false>);
+  return launch_pdl(kernel, grid, dim3(kFinishThreads), 0, st, a, p.rb);
+}
+
+}  // namespace skv

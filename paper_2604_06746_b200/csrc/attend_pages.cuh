@@ -1,0 +1,120 @@
+// Attention of new tokens over a paged cache in 8 bits, what its kernels share: how the work is cut and partial results.
+//
+// An item is (sequence b, KV head g, block of up to RB rows) over the sequence's keys, lengths[b] old ones and count[b] new ones; row r =
+// i G + h is new token i and head h of the group.  Items follow one another, sequence after sequence; their tiles of 64 keys, behind `over`
+// places for what an item costs beside them, form one sequence of W places, of which C CTAs take runs that differ by one place at
+// most.  What a CTA has of an item it leaves as a partial in slot item + CTA (no other pair has it), merged in that order by a second
+// launch: results do not depend on timing.
+#pragma once
+
+#include "pages.cuh"
+
+namespace skv {
+
+constexpr int kPageTile = 64, kPageTileShift = 6;                // keys of a place
+
+struct AttendPagesArgs {
+  PagesView c;
+  Div by_blocks, by_group, by_ctas, by_rows, by_kv;
+  const char* q;
+  long long q_batch, q_token, q_head;
+  const int* counts;
+  int n_new, group, rows, blocks;                               // rows = n_new group; blocks of rows
+  float scale2, cap2, inv_cap;                                  // as in AttendArgs
+  char* out;
+  float* lse;
+  int* seq_start;                                               // [batch + 1] places of one item before a sequence's
+  float2* part_stat;                                            // [slot][RB] reference (bits) and sum
+  float* part_out;                                              // [slot][RB][d]
+  int ctas, least, over;
+};
+
+// Rows of a block, CTAs that run at once.
+struct PagesPlan { int rb, ctas; };
+
+cudaError_t launch_attend_pages(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
+cudaError_t launch_attend_pages_finish(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
+
+#ifdef __CUDACC__
+
+// Keys of sequence b, old ones and new ones; 0: nothing of it is looked at.
+__device__ __forceinline__ int page_keys(const AttendPagesArgs& a, int b) {
+  int n;
+  const int count = rows_of_sequence(a.c, a.counts, b, a.n_new, n);
+  if (count < 0) tell_invalid(a.c);
+  return count <= 0 ? 0 : n + count;
+}
+__device__ __forceinline__ int page_places(int keys, int over) { return keys == 0 ? 0 : ((keys + kPageTile - 1) >> kPageTileShift) + over; }
+
+// A CTA's run of places and where it begins: sequence, its keys, places of one item before it.
+struct PageRun { int lo, hi, b, before, keys; };
+__device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a, int* save) {
+  const int lane = threadIdx.x & 31, items = a.c.n_kv * a.blocks;
+  int total = 0, keys = 0, places = 0, incl = 0;
+  auto sweep = [&](int b0) {
+    keys = b0 + lane < a.c.batch ? page_keys(a, b0 + lane) : 0;
+    places = incl = page_places(keys, a.over);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += t;
+    }
+  };
+#pragma unroll 1
+  for (int b0 = 0; b0 < a.c.batch; b0 += 32) {
+    sweep(b0);
+    if (save && threadIdx.x < 32 && b0 + lane < a.c.batch) save[b0 + lane] = total + incl - places;
+    total += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (save && threadIdx.x == 0) save[a.c.batch] = total;
+  PageRun w{};
+  const Shares all = shares_of(total * items, a.ctas, a.by_ctas, a.least);
+  w.lo = first_of(all, blockIdx.x);
+  w.hi = first_of(all, blockIdx.x + 1);
+  if (w.lo >= w.hi) return w;
+  int before = 0;
+#pragma unroll 1
+  for (int b0 = 0; b0 < a.c.batch; b0 += 32) {
+    if (a.c.batch > 32) sweep(b0);
+    const unsigned mine = __ballot_sync(0xffffffffu, (before + incl) * items > w.lo);
+    if (mine) {
+      const int from = __ffs(mine) - 1;
+      w.b = b0 + from;
+      w.before = before + __shfl_sync(0xffffffffu, incl - places, from);
+      w.keys = __shfl_sync(0xffffffffu, keys, from);
+      break;
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return w;
+}
+
+// A CTA's run item by item: tiles [t0, t1) of item `nth` of sequence b (none left: t1 = 0).
+struct PageSegment { int b, nth, t0, t1, keys, tiles, at, hi; };
+__device__ __forceinline__ void next_segment(PageSegment& s, const AttendPagesArgs& a) {
+  s.at += s.tiles + a.over;
+  s.t0 = s.t1 = 0;
+  if (s.at + a.over >= s.hi) return;
+  if (++s.nth == a.c.n_kv * a.blocks) {
+    s.nth = 0;
+    do ++s.b;
+    while ((s.keys = page_keys(a, s.b)) == 0 && s.b < a.c.batch - 1);
+    s.tiles = (s.keys + kPageTile - 1) >> kPageTileShift;
+  }
+  s.t1 = min(s.tiles, s.hi - s.at - a.over);
+}
+__device__ __forceinline__ PageSegment first_segment(const AttendPagesArgs& a, const PageRun& w) {
+  const int items = a.c.n_kv * a.blocks;
+  PageSegment s{w.b, 0, 0, 0, w.keys, (w.keys + kPageTile - 1) >> kPageTileShift, w.before * items, w.hi};
+  if (w.lo >= w.hi) return s;
+  const int each = s.tiles + a.over;
+  s.nth = (w.lo - s.at) / each;
+  s.at += s.nth * each;
+  s.t0 = max(0, w.lo - s.at - a.over);
+  s.t1 = max(0, min(s.tiles, w.hi - s.at - a.over));
+  if (s.t1 <= s.t0) next_segment(s, a);
+  return s;
+}
+
+#endif  // __CUDACC__
+}  // namespace skv

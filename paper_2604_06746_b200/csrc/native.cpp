@@ -512,11 +512,151 @@ PyObject* evict(PyObject* const* a) {
   return call_on(c, [&] { return structkv_evict(x, c.c, budget, recent, st); });
 }
 
+// ---- rotary positions and a paged cache: pages are (address of a structkv_pages, device, batch, KV heads, head dim, slots of a sequence), a
+// tuple that binding.Pages keeps with its tensors; a rope is the address of a structkv_rope -----------------------------
+const structkv_rope* rope_of(PyObject* o) {
+  if (o == Py_None) return nullptr;
+  const structkv_rope* const r = (const structkv_rope*)PyLong_AsVoidPtr(o);
+  if (PyErr_Occurred()) throw PyError{};
+  return r;
+}
+// int32 [batch, n] with contiguous rows, or [n] for every sequence.
+struct Words { const int* p; long long stride; };
+Words words_of(PyObject* o, int device, int64_t batch, int64_t n, const char* what) {
+  if (o == Py_None) return {nullptr, 0};
+  const at::Tensor& t = tensor(o);
+  const int64_t dims = t.dim();
+  require((dims == 1 || (dims == 2 && t.size(0) == batch)) && t.size(dims - 1) == n && (n <= 1 || t.stride(dims - 1) == 1) && t.scalar_type() == at::kInt &&
+              t.is_cuda() && t.get_device() == device, what);
+  return {(const int*)t.data_ptr(), dims == 2 && batch > 1 ? t.stride(0) : 0};
+}
+// ctx, dtype, head dim, device, x, positions, rope, out, inverse, stream
+PyObject* rotate(PyObject* const* a) {
+  structkv_ctx* const c = context(a[0]);
+  const at::ScalarType dt = dtype_of(a[1]);
+  const int64_t d = integer(a[2]);
+  const int device = int_of(a[3]);
+  const at::Tensor &x = tensor(a[4]), &out = tensor(a[7] == Py_None ? a[4] : a[7]);
+  require(x.dim() == 4 && x.size(3) == d && x.stride(3) == 1 && x.scalar_type() == dt && x.is_cuda() && x.get_device() == device,
+          "x: [batch, tokens, heads, d] of the context's dtype and device, contiguous vectors");
+  require(out.sizes() == x.sizes() && out.stride(3) == 1 && out.scalar_type() == dt && out.is_cuda() && out.get_device() == device, "out: as x");
+  require(x.size(0) <= INT_MAX && x.size(1) <= INT_MAX && x.size(2) <= INT_MAX, "x: sizes of 31 bits");
+  const Words p = words_of(a[5], device, x.size(0), x.size(1), "positions: int32 [batch, tokens] or [tokens], contiguous rows, on the context's device");
+  require(p.p || x.numel() == 0, "positions are needed");
+  const structkv_rope* const r = rope_of(a[6]);
+  const int inverse = PyObject_IsTrue(a[8]);
+  if (inverse < 0) throw PyError{};
+  const structkv_rotate_args args{x.data_ptr(), x.stride(0), x.stride(1), x.stride(2), out.data_ptr(), out.stride(0), out.stride(1), out.stride(2),
+                                  p.p, p.stride, (int)x.size(0), (int)x.size(1), (int)x.size(2), inverse};
+  void* const st = a[9] == Py_None ? c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream() : stream_of(a[9]);
+  const c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
+  return call([&] { return structkv_rotate(c, r, &args, st); });
+}
+struct PagesOf {
+  const structkv_pages* p;
+  CacheOf c;                                               // its sizes: capacity is a sequence's slots
+};
+PagesOf pages_of(PyObject* o, PyObject* heads, PyObject* dtype) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 6) fail(PyExc_TypeError, "pages are expected");
+  auto size = [&](int i) { return integer(PyTuple_GET_ITEM(o, i)); };
+  return {(const structkv_pages*)size(0), {nullptr, dtype_of(dtype), (int)size(1), size(2), integer(heads), size(3), size(4), size(5)}};
+}
+// ctx, heads, dtype, pages, k_new, v_new, positions, rope, counts, index, q, q_out, stream
+PyObject* append_pages(PyObject* const* a) {
+  structkv_ctx* const x = context(a[0]);
+  const PagesOf p = pages_of(a[3], a[1], a[2]);
+  const CacheOf& c = p.c;
+  const at::Tensor &k = tensor(a[4]), &v = tensor(a[5]);
+  const int64_t tokens = dim_of(k, 1);
+  vectors(c, k, tokens, c.kv, "k_new: [batch, tokens, H_kv, d] of the context's dtype, contiguous vectors");
+  vectors(c, v, tokens, c.kv, "v_new: as k_new");
+  require(k.strides() == v.strides(), "k_new and v_new: the same strides");
+  there(c, k, "k_new: on the pages' device");
+  there(c, v, "v_new: on the pages' device");
+  structkv_append_pages_args g{};
+  g.k = k.data_ptr();
+  g.v = v.data_ptr();
+  g.stride_batch = k.stride(0);
+  g.stride_token = k.stride(1);
+  g.stride_head = k.stride(2);
+  int64_t n = tokens;
+  if (a[9] != Py_None) {
+    const at::Tensor& t = tensor(a[9]);
+    require(t.dim() == 1 || t.dim() == 2, "index: [batch, n_new] or [n_new]");
+    n = t.size(t.dim() - 1);
+    const Words w = words_of(a[9], c.device, c.batch, n, "index: int32 [batch, n_new] or [n_new], contiguous rows, on the pages' device");
+    g.index = w.p;
+    g.index_stride = w.stride;
+  }
+  require(n >= 1 && tokens <= INT_MAX && n <= c.capacity, "one row at least, and no more than a sequence has slots");
+  g.tokens = (int)tokens;
+  g.n_new = (int)n;
+  g.counts = words(c, a[8], {c.batch}, "counts: contiguous int32 [batch], on the pages' device");
+  g.rope = rope_of(a[7]);
+  const Words at = words_of(a[6], c.device, c.batch, tokens, "positions: int32 [batch, tokens] or [tokens], contiguous rows, on the pages' device");
+  require(at.p || !g.rope, "positions come with a rope");
+  g.positions = at.p;
+  g.positions_stride = at.stride;
+  if (a[10] != Py_None) {
+    const at::Tensor& q = tensor(a[10]);
+    require(!g.index && g.rope, "q: with a rope and without an index");
+    vectors(c, q, n, c.heads, "q: [batch, n_new, H, d] of the context's dtype, contiguous vectors");
+    there(c, q, "q: on the pages' device");
+    const at::Tensor& out = tensor(a[11] == Py_None ? a[10] : a[11]);
+    require(fits(out, {c.batch, n, c.heads, c.d}, c.dtype), "q_out: contiguous [batch, n_new, H, d] of the context's dtype");
+    there(c, out, "q_out: on the pages' device");
+    g.q = q.data_ptr();
+    g.q_stride_batch = q.stride(0);
+    g.q_stride_token = q.stride(1);
+    g.q_stride_head = q.stride(2);
+    g.q_out = out.data_ptr();
+  } else {
+    require(a[11] == Py_None, "q_out comes with q");
+  }
+  void* const st = stream_on(c, a[12]);
+  return call_on(c, [&] { return structkv_append_pages(x, p.p, &g, st); });
+}
+// ctx, heads, dtype, pages, q, scale, out, workspace, counts, softcap, lse, stream
+PyObject* attend_pages(PyObject* const* a) {
+  structkv_ctx* const x = context(a[0]);
+  const PagesOf p = pages_of(a[3], a[1], a[2]);
+  const CacheOf& c = p.c;
+  const at::Tensor &q = tensor(a[4]), &out = tensor(a[6]), &ws = tensor(a[7]);
+  const int64_t n = dim_of(q, 1);
+  vectors(c, q, n, c.heads, "q: [batch, n_new, H, d] of the context's dtype, contiguous vectors");
+  require(n >= 1 && n <= STRUCTKV_MAX_NEW, "q: 1 to 64 new tokens");
+  require(fits(out, {c.batch, n, c.heads, c.d}, c.dtype), "out: contiguous [batch, n_new, H, d] of the context's dtype");
+  there(c, q, "q: on the pages' device");
+  there(c, out, "out: on the pages' device");
+  there(c, ws, "workspace: on the pages' device");
+  structkv_attend_pages_args g{};
+  g.q = q.data_ptr();
+  g.q_stride_batch = q.stride(0);
+  g.q_stride_token = q.stride(1);
+  g.q_stride_head = q.stride(2);
+  g.n_new = (int)n;
+  g.counts = words(c, a[8], {c.batch}, "counts: contiguous int32 [batch], on the pages' device");
+  g.scale = real(a[5]);
+  g.softcap = real(a[9]);
+  g.out = out.data_ptr();
+  if (a[10] != Py_None) {
+    const at::Tensor& lse = tensor(a[10]);
+    require(fits(lse, {c.batch, n, c.heads}, at::kFloat), "lse: contiguous float32 [batch, n_new, H]");
+    there(c, lse, "lse: on the pages' device");
+    g.lse = (float*)lse.data_ptr();
+  }
+  g.workspace = ws.data_ptr();
+  g.workspace_bytes = (size_t)(ws.is_contiguous() ? ws.numel() * ws.element_size() : 0);
+  void* const st = stream_on(c, a[11]);
+  return call_on(c, [&] { return structkv_attend_pages(x, p.p, &g, st); });
+}
+
 #define ENTRY(f, n) {#f, (PyCFunction)(void (*)())entry<f, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(score_layer, 12), ENTRY(select, 6), ENTRY(compact, 5), ENTRY(compact_per_slab, 5),
                          ENTRY(group_saliency, 6), ENTRY(block_scores, 5), ENTRY(mass_recovery, 5), ENTRY(accumulate, 6),
                          ENTRY(fill_prefill, 19), ENTRY(prefill, 3), ENTRY(append, 7), ENTRY(attend, 17),
-                         ENTRY(weigh, 12), ENTRY(commit, 7), ENTRY(evict, 6), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(weigh, 12), ENTRY(commit, 7), ENTRY(evict, 6), ENTRY(rotate, 10), ENTRY(append_pages, 13),
+                         ENTRY(attend_pages, 12), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
