@@ -167,7 +167,7 @@ structkv_status structkv_append_pages(structkv_ctx* ctx, const structkv_pages* p
   }
   const long long blocks = ((long long)x->n_new + 2 * kBlockSlots - 2) / kBlockSlots, rows = (long long)a.c.batch * x->n_new;
   // (CTAs of both kinds are counted in 31 bits)
-  if (rows * (heads + 1) > 0x3fffffffll || a.c.batch * blocks * ((2ll * a.c.n_kv + 7) / 8) > 0x3fffffffll) return STRUCTKV_ERR_INVALID_ARG;
+  if (rows * (heads + 1) > 0x3fffffffll || a.c.batch * blocks * a.c.n_kv > 0x3fffffffll) return STRUCTKV_ERR_INVALID_ARG;
   if (!on_device(ctx)) return STRUCTKV_ERR_INVALID_ARG;
   a.by_blocks = div_by((unsigned)blocks);
   a.by_new = div_by(x->n_new);
@@ -192,10 +192,9 @@ structkv_status structkv_append_pages(structkv_ctx* ctx, const structkv_pages* p
   a.q_out = (char*)x->q_out;
   a.heads = heads;
   a.q_rows = (int)rows;
-  a.head_step = heads_at_once(rows, d * elem / 32, heads, ctx->c.sm_count);
-  // a warp takes one head's K or V where there are few blocks, several of the same tokens where there are many
-  const int most = (2 * a.c.n_kv + 7) / 8;
-  a.splits = a.c.batch * blocks >= 2ll * ctx->c.sm_count ? 1 : most;
+  a.head_step = heads_at_once(rows, d / 8, heads, ctx->c.sm_count);
+  a.splits = append_splits(a.c.batch * blocks, a.c.n_kv, ctx->c.sm_count);
+  a.by_splits = div_by(a.splits);
   a.append_ctas = (int)(a.c.batch * blocks * a.splits);
   return told(launch_append_pages(ctx->c, rope_args(x->rope), a, (cudaStream_t)stream));
 }

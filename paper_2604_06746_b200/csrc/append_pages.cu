@@ -1,8 +1,9 @@
 // New tokens' rows go to pages: gathered, K rotated, quantised to e4m3 with a scale for 16 slots of a head.
 //
-// A CTA has one block of 16 slots of a sequence (or a share of its heads): cosines and sines of its tokens go to shared memory once, then
-// a warp takes K or V of one head at a time, all 16 rows in registers: the largest magnitude is known before anything is
-// written, and every element is read once.  Further CTAs rotate the queries that came along.
+// A CTA has one block of 16 slots of a sequence and K and V of one head or of four.  A lane has four pairs of one row, of all those heads: their
+// angles are worked out once, in registers, and all of a lane's loads are in flight together.  The blocks' largest magnitudes
+// meet in shared memory; then every row goes through the rotation once more and becomes codes, so that nothing but the rows as they came is
+// held meanwhile and every element is read once.  Further CTAs rotate the queries that came along.
 #include <algorithm>
 
 #include "pages.cuh"
@@ -10,7 +11,8 @@
 namespace skv {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kManyHeads = 4;                                     // of a CTA, where there are many blocks; else one
+constexpr int kPairs = 4;                                         // a lane's of a row
 
 // The smallest e with which `top` stays within 448 2^e, from the bits of the finite top = m 2^x, 1 <= m < 2 (448 = 1.75 2^8).
 __device__ __forceinline__ int exponent_of(float top) {
@@ -34,163 +36,186 @@ __device__ __forceinline__ uint32_t scaled2(uint32_t codes, uint32_t by) {
   return y;
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kWarps * 32) append_pages(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendPagesArgs a) {
-  constexpr int N = Chunk<T>::N, LANES = D / (2 * N), ROWS = 32 / LANES, IT = kBlockSlots / ROWS;
-  __shared__ float2 turns[kBlockSlots][D / 2 + 1];
-  __shared__ int source[kBlockSlots];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// The largest magnitude of eight bf16, NaN aside.
+__device__ __forceinline__ float largest(const RawPairs<__nv_bfloat16, kPairs>& r) {
+  auto max2 = [](uint32_t x, uint32_t y) {
+    asm("max.bf16x2 %0, %0, %1;" : "+r"(x) : "r"(y));
+    return x;
+  };
+  constexpr uint32_t kMagnitude = 0x7fff7fffu;
+  const uint32_t m = max2(max2(r.x[0] & kMagnitude, r.x[1] & kMagnitude), max2(r.y[0] & kMagnitude, r.y[1] & kMagnitude));
+  return fmaxf(fmaxf(0.f, __uint_as_float(m << 16)), __uint_as_float(m & 0xffff0000u));
+}
+__device__ __forceinline__ float largest(const RawPairs<float, kPairs>&) { return 0.f; }
+
+// HEADS: K and V of so many.
+template <typename T, int D, Pairing P, int HEADS>
+__global__ void __launch_bounds__(2 * D, (sizeof(T) == 2 ? 768 : 512) / (2 * D)) append_pages(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendPagesArgs a) {
+  constexpr int JOBS = 2 * HEADS, LANES = D / (2 * kPairs), THREADS = kBlockSlots * LANES, WARPS = THREADS / 32;
+  static_assert(THREADS == 2 * D, "a lane for four pairs of every slot");
+  using Place = PairPlace<T, D, P, kPairs>;
+  __shared__ float tops[JOBS][WARPS], finite_tops[JOBS][WARPS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, p0 = (tid % LANES) * kPairs;
   pdl_trigger();
   pdl_wait();
   if (blockIdx.x >= a.append_ctas) {
     // queries: a group of lanes a token
-    const int per = kWarps * 32 / LANES, groups = (a.heads + a.head_step - 1) / a.head_step;
-    const long long at = (long long)(blockIdx.x - a.append_ctas) * per + tid / LANES;
+    const int groups = (a.heads + a.head_step - 1) / a.head_step;
+    const long long at = (long long)(blockIdx.x - a.append_ctas) * kBlockSlots + tid / LANES;
     const int row = (int)(at / groups), h0 = (int)(at % groups) * a.head_step;
     if (at >= (long long)a.q_rows * groups) return;
     const int b = quotient(row, a.by_new), i = row - b * a.n_new;
-    rotate_heads<T>(r, false, (const T*)(a.q + b * a.q_batch + i * a.q_token), a.q_head / (int)sizeof(T),
-                    (T*)a.q_out + (long long)row * a.heads * D, D, a.positions[b * a.s_positions + i], (tid % LANES) * N, h0,
-                    min(h0 + a.head_step, a.heads));
+    rotate_heads<T, D, P, kPairs>(r, false, (const T*)(a.q + b * a.q_batch + i * a.q_token), a.q_head / (int)sizeof(T),
+                                  (T*)a.q_out + (long long)row * a.heads * D, D, a.positions[b * a.s_positions + i], p0, h0,
+                                  min(h0 + a.head_step, a.heads));
     return;
   }
-  const int job0 = blockIdx.x % a.splits, task = blockIdx.x / a.splits, b = quotient(task, a.by_blocks), nth = task - b * a.blocks;
+  const int task = quotient(blockIdx.x, a.by_splits), g0 = (blockIdx.x - task * a.splits) * HEADS;
+  const int b = quotient(task, a.by_blocks), nth = task - b * a.blocks, heads = min(HEADS, a.c.n_kv - g0);
   int n;
   const int count = rows_of_sequence(a.c, a.counts, b, a.n_new, n);
   if (count < 0) {
     if (nth == 0 && tid == 0) tell_invalid(a.c);
     return;
   }
-  const int slot0 = ((n >> kBlockShift) + nth) << kBlockShift, lo = max(slot0, n), hi = min(slot0 + kBlockSlots, n + count);
-  if (lo >= hi) return;
+  const int slot0 = ((n >> kBlockShift) + nth) << kBlockShift, slot = slot0 + tid / LANES;
+  if (max(slot0, n) >= min(slot0 + kBlockSlots, n + count)) return;
+  const bool mine = slot >= n && slot < n + count;
+  int t = -1;                                                     // the slot's source token
+  if (mine) t = a.index ? a.index[b * a.s_index + slot - n] : slot - n;
   const int page = *(const int*)((const char*)a.c.table + b * a.c.s_table + (long long)(slot0 >> a.c.page_shift) * 4);
-  if (page < 0 || page >= a.c.pages) {
-    if (tid == 0) tell_invalid(a.c);
-    return;
+  const bool is = t >= 0 && t < a.tokens, no_page = page < 0 || page >= a.c.pages;
+  if ((mine && !is) || no_page) tell_invalid(a.c);
+  if (no_page) return;
+  const Place at(r, p0);
+  typename Place::Raw raw[JOBS] = {};
+  if (is) {
+    const char *const k = a.k + b * a.s_batch + t * a.s_token + g0 * a.s_head, *const v = a.v + (k - a.k);
+#pragma unroll
+    for (int j = 0; j < JOBS; ++j)
+      if (j / 2 < heads) raw[j] = at.load((const T*)((j & 1 ? v : k) + (j / 2) * a.s_head));
   }
-  if (tid < kBlockSlots) {
-    const int j = slot0 + tid;
-    int t = -1;
-    if (j >= lo && j < hi) {
-      t = a.index ? a.index[b * a.s_index + j - n] : j - n;
-      if (t < 0 || t >= a.tokens) {
-        tell_invalid(a.c);
-        t = -1;
-      }
+  uint64_t cos[kPairs / 2], sin[kPairs / 2];
+  if (a.rotated) at.angles(r, is ? a.positions[b * a.s_positions + t] : 0, false, cos, sin);
+  auto row_of = [&](int j, float (&u)[kPairs], float (&v)[kPairs]) {
+    Place::pairs(raw[j], u, v);
+    if (!(j & 1) && a.rotated) at.turn(u, v, cos, sin);
+  };
+  // (positive numbers are ordered as their bits are; NaN has no part in a maximum)
+  auto across = [](float x) { return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x))); };
+  // lane j of every warp: the scale of job j, where the block holds tokens already
+  const int in_page = slot0 & ((1 << a.c.page_shift) - 1);
+  const bool job = lane < JOBS && lane / 2 < heads;
+  unsigned char* const scale = (lane & 1 ? a.c.v_scales : a.c.k_scales) +
+                               (((size_t)page * a.c.n_kv + g0 + (job ? lane / 2 : 0)) << (a.c.page_shift - kBlockShift)) + (in_page >> kBlockShift);
+  const int had = job && slot0 < n ? (int)*scale - 127 : -127;
+  bool infinite = false;
+#pragma unroll
+  for (int j = 0; j < JOBS; ++j) {
+    float top = 0.f;
+    if (sizeof(T) == 2 && (j & 1 || !a.rotated)) {
+      top = largest(raw[j]);
+    } else {
+      float u[kPairs], v[kPairs];
+      row_of(j, u, v);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) top = fmaxf(top, fmaxf(fabsf(u[i]), fabsf(v[i])));
     }
-    source[tid] = t;
+    top = across(top);
+    infinite |= top == INFINITY;
+    if (lane == 0) tops[j][warp] = top;
   }
-  __syncthreads();
-  if (a.rotated) {
-    for (int i = tid; i < kBlockSlots * (r.dim / 2); i += kWarps * 32) {
-      const int row = i / (r.dim / 2), p = i - row * (r.dim / 2), t = source[row];
-      if (t >= 0) turns[row][p] = cos_sin<T>(turn_of(r.step[p], a.positions[b * a.s_positions + t]), r.amplitude);
+  infinite = __syncthreads_or(infinite);
+  if (infinite) {
+    // infinities are stored as NaN, and the others' largest is what counts
+#pragma unroll
+    for (int j = 0; j < JOBS; ++j) {
+      float u[kPairs], v[kPairs], top = 0.f;
+      row_of(j, u, v);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        if (fabsf(u[i]) != INFINITY) top = fmaxf(top, fabsf(u[i]));
+        if (fabsf(v[i]) != INFINITY) top = fmaxf(top, fabsf(v[i]));
+      }
+      top = across(top);
+      if (lane == 0) finite_tops[j][warp] = top;
     }
     __syncthreads();
   }
-  const int in_page = slot0 & ((1 << a.c.page_shift) - 1), p0 = (lane % LANES) * N, row0 = lane / LANES;
-#pragma unroll 1
-  for (int job = job0 * kWarps + warp; job < 2 * a.c.n_kv; job += a.splits * kWarps) {
-    const int g = job >> 1;
-    const bool is_v = job & 1;
-    const PairPlace<T> at(!is_v && a.rotated ? r.dim : 0, r.interleaved, p0);
-    const char* const from = (is_v ? a.v : a.k) + b * a.s_batch + g * a.s_head;
-    float u[IT][N], v[IT][N];
-#pragma unroll
-    for (int k = 0; k < IT; ++k) {
-      const int t = source[k * ROWS + row0];
-      if (t >= 0) load_pairs<T>(at, (const T*)(from + t * a.s_token), u[k], v[k]);
-      else
-#pragma unroll
-        for (int i = 0; i < N; ++i) u[k][i] = v[k][i] = 0.f;
-    }
+  int e = 0, down = 0;                                            // how far older codes go down
+  if (job) {
     float top = 0.f;
 #pragma unroll
-    for (int k = 0; k < IT; ++k) {
-      if (!is_v && a.rotated && source[k * ROWS + row0] >= 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (at.turns(i)) turn(u[k][i], v[k][i], turns[k * ROWS + row0][p0 + i]);
-#pragma unroll
-      for (int i = 0; i < N; ++i) top = fmaxf(top, fmaxf(fabsf(u[k][i]), fabsf(v[k][i])));   // (NaN has no part in it)
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (top == INFINITY) {
-      // infinities are stored as NaN
-      top = 0.f;
-      auto no_infinity = [&](float& x) {
-        if (fabsf(x) == INFINITY) x = __int_as_float(0x7fffffff);
-        top = fmaxf(top, fabsf(x));
-      };
-#pragma unroll
-      for (int k = 0; k < IT; ++k)
-#pragma unroll
-        for (int i = 0; i < N; ++i) { no_infinity(u[k][i]); no_infinity(v[k][i]); }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    }
-    int e = exponent_of(top);
-    unsigned char* const scale = (is_v ? a.c.v_scales : a.c.k_scales) + (((size_t)page * a.c.n_kv + g) << (a.c.page_shift - kBlockShift)) + (in_page >> kBlockShift);
-    char* const to = (is_v ? a.c.v : a.c.k) + page * a.c.s_page + g * a.c.s_head + in_page * a.c.s_token;
+    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, infinite ? finite_tops[lane][w] : tops[lane][w]);
+    e = exponent_of(top);
     if (slot0 < n) {
-      // older tokens: their codes by the larger of the scales
-      const int had = (int)*scale - 127;
-      if (e > had) {
-        const int down = min(e - had, 24);
-        const uint32_t half = down > 14 ? 1u << (24 - down) : (uint32_t)(15 - down) << 10, by = half | half << 16;
-        for (int i = lane; i < (n - slot0) * (D / 4); i += 32) {
-          uint32_t* const w = (uint32_t*)(to + (i / (D / 4)) * a.c.s_token + (i % (D / 4)) * 4);
-          const uint32_t x = *w;
-          *w = scaled2(x & 0xffffu, by) | scaled2(x >> 16, by) << 16;
-        }
-      } else {
-        e = had;
-      }
-      __syncwarp();
+      down = max(0, min(e - had, 24));
+      e = max(e, had);
     }
-    if (lane == 0) *scale = (unsigned char)(e + 127);
-    const float by = __int_as_float((127 - e) << 23);
+    if (warp == 0) *scale = (unsigned char)(e + 127);
+  }
+  char *const k = a.c.k + page * a.c.s_page + g0 * a.c.s_head + (in_page + tid / LANES) * a.c.s_token, *const v = a.c.v + (k - a.c.k);
 #pragma unroll
-    for (int k = 0; k < IT; ++k) {
-      const int row = k * ROWS + row0;
-      if (slot0 + row < lo || slot0 + row >= hi) continue;
-      char* const out = to + row * a.c.s_token;
+  for (int j = 0; j < JOBS; ++j) {
+    const int ej = __shfl_sync(0xffffffffu, e, j), dj = __shfl_sync(0xffffffffu, down, j);
+    if (j / 2 >= heads) break;
+    char* const out = (j & 1 ? v : k) + (j / 2) * a.c.s_head;
+    if (mine) {
+      const float by = __int_as_float((127 - ej) << 23);
+      float x[kPairs], y[kPairs], u[kPairs], w[kPairs];
+      row_of(j, u, w);
 #pragma unroll
-      for (int i = 0; i < N; ++i) { u[k][i] *= by; v[k][i] *= by; }
-      if (at.whole) {
-        float x[N], y[N];
-        join<T>(at, u[k], v[k], x, y);
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-          *(uint32_t*)(out + at.a + i) = codes4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-          *(uint32_t*)(out + at.b + i) = codes4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int2 el = at.pair(i);
-          const uint32_t w = codes4(u[k][i], v[k][i], 0.f, 0.f);
-          out[el.x] = (char)w;
-          out[el.y] = (char)(w >> 8);
+      for (int i = 0; i < kPairs; ++i) {
+        u[i] *= by;
+        w[i] *= by;
+        if (infinite) {
+          if (fabsf(u[i]) == INFINITY) u[i] = __int_as_float(0x7fffffff);
+          if (fabsf(w[i]) == INFINITY) w[i] = __int_as_float(0x7fffffff);
         }
       }
+      Place::chunks(u, w, x, y);
+      const uint32_t cx = codes4(x[0], x[1], x[2], x[3]), cy = codes4(y[0], y[1], y[2], y[3]);
+      if constexpr (P == HALVES) {
+        *(uint32_t*)(out + at.a) = cx;
+        *(uint32_t*)(out + at.b) = cy;
+      } else if constexpr (P == NEIGHBOURS) {
+        *(uint2*)(out + at.a) = make_uint2(cx, cy);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {                        // (pairs of neighbours in cx, cy)
+          const int2 el = at.pair(i);
+          const uint32_t c = (i < kPairs / 2 ? cx : cy) >> (16 * (i % 2));
+          out[el.x] = (char)c;
+          out[el.y] = (char)(c >> 8);
+        }
+      }
+    } else if (dj > 0 && slot < n) {
+      // an older token: its codes by the larger scale
+      const uint32_t half = dj > 14 ? 1u << (24 - dj) : (uint32_t)(15 - dj) << 10, f = half | half << 16;
+      uint2* const at8 = (uint2*)(out + 2 * p0);
+      uint2 c = *at8;
+      c.x = scaled2(c.x & 0xffffu, f) | scaled2(c.x >> 16, f) << 16;
+      c.y = scaled2(c.y & 0xffffu, f) | scaled2(c.y >> 16, f) << 16;
+      *at8 = c;
     }
   }
 }
 
-template <typename T, int D>
-cudaError_t launch(const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
-  constexpr int PER = kWarps * 32 / (D / (2 * Chunk<T>::N));
-  const long long q = a.q ? (long long)a.q_rows * ((a.heads + a.head_step - 1) / a.head_step) : 0, ctas = a.append_ctas + (q + PER - 1) / PER;
-  return launch_pdl(append_pages<T, D>, dim3((unsigned)ctas), dim3(kWarps * 32), 0, st, r, a);
-}
+template <typename T, int D, Pairing P>
+struct Launch {
+  static cudaError_t run(const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
+    const long long q = a.q ? (long long)a.q_rows * ((a.heads + a.head_step - 1) / a.head_step) : 0, ctas = a.append_ctas + (q + kBlockSlots - 1) / kBlockSlots;
+    return launch_pdl(a.splits == a.c.n_kv ? append_pages<T, D, P, 1> : append_pages<T, D, P, kManyHeads>, dim3((unsigned)ctas), dim3(2 * D), 0, st, r, a);
+  }
+};
 
 }  // namespace
 
+// One head a CTA as long as that leaves the SMs' places for CTAs free.
+int append_splits(long long blocks, int n_kv, int sms) { return blocks * n_kv <= 3ll * sms || n_kv == 1 ? n_kv : (n_kv + kManyHeads - 1) / kManyHeads; }
+
 cudaError_t launch_append_pages(const Ctx& ctx, const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
-  if (ctx.cfg.dtype == STRUCTKV_BF16) return ctx.cfg.head_dim == 128 ? launch<__nv_bfloat16, 128>(r, a, st) : launch<__nv_bfloat16, 64>(r, a, st);
-  return ctx.cfg.head_dim == 128 ? launch<float, 128>(r, a, st) : launch<float, 64>(r, a, st);
+  return by_pairing<Launch>(ctx, pairing_of(r, kPairs), r, a, st);
 }
 
 }  // namespace skv

@@ -21,7 +21,7 @@ struct PagesView {
 
 struct AppendPagesArgs {
   PagesView c;
-  Div by_blocks, by_new;                                        // blocks of slots that a sequence's rows may touch; n_new
+  Div by_splits, by_blocks, by_new;                             // blocks of slots that a sequence's rows may touch; n_new
   const char *k, *v;
   long long s_batch, s_token, s_head;
   int tokens, n_new, blocks, splits;                            // splits: CTAs that share a block's heads
@@ -46,12 +46,13 @@ struct RotateArgs {
 };
 
 cudaError_t launch_rotate(const Ctx& ctx, const RopeArgs& r, const RotateArgs& a, cudaStream_t st);
+int append_splits(long long blocks, int n_kv, int sms);
 cudaError_t launch_append_pages(const Ctx& ctx, const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st);
 
-// Heads that a lane takes one after another with the same angles: as many as leave every SM eight warps of rows, up to eight.
+// Heads that a lane takes one after another with the same angles: up to eight, as long as every SM has 1024 lanes at work.
 inline int heads_at_once(long long rows, int lanes, int heads, int sms) {
   int n = 1;
-  while (n < 8 && n < heads && rows * lanes * ((heads + 2 * n - 1) / (2 * n)) >= 256ll * sms) n *= 2;
+  while (n < 8 && n < heads && rows * lanes * ((heads + 2 * n - 1) / (2 * n)) >= 1024ll * sms) n *= 2;
   return n;
 }
 

@@ -1,8 +1,6 @@
 // Rotary positions on the device: angles, and 16-byte chunks of a head as pairs.
 #pragma once
 
-#include <cuda_fp8.h>
-
 #include "attend.cuh"
 
 namespace skv {
@@ -20,148 +18,192 @@ __device__ __forceinline__ int turn_of(unsigned long long step, int position) {
   const unsigned lo = (unsigned)step, p = (unsigned)position;
   return (int)(__umulhi(lo, p) + (unsigned)(step >> 32) * p - (position < 0 ? lo : 0u));
 }
-// Cosine and sine times the amplitude.  For bf16 by the special-function unit, whose 2^-21 is far below the 2^-9 of a rounding.
-template <typename T>
+// Cosine and sine of a turn, times the amplitude.  The nearest quarter goes first, in integers, so that what is left, r within an eighth of a turn,
+// is exact to 24 bits; sin(2 pi r) = r S(r^2) and cos(2 pi r) = C(r^2) with polynomials fitted for the least largest error there (2^-28,
+// relative, and 2^-34; least squares reweighted by the error until it is level: Lawson's method).  In fp32 both are off by 2^-23 at most.
+// The special-function unit is off by 2^-21: that rounds one of some thousand bf16 queries to the other side.
 __device__ __forceinline__ float2 cos_sin(int turn, float amplitude) {
-  float s, c;
-  if constexpr (sizeof(T) == 2) __sincosf((float)turn * 1.4629180792671596e-9f, &s, &c);   // 2 pi 2^-32
-  else sincospif((float)turn * 4.656612873077393e-10f, &s, &c);                            // 2^-31
-  return make_float2(c * amplitude, s * amplitude);
+  const unsigned quarter = ((unsigned)turn + 0x20000000u) >> 30;
+  const float r = (float)(int)((unsigned)turn - (quarter << 30)) * 2.3283064365386963e-10f, z = r * r;   // 2^-32
+  float s = fmaf(fmaf(fmaf(-75.39356f, z, 81.592354f), z, -41.34166145f), z, 6.283185287f) * (r * amplitude);
+  float c = fmaf(fmaf(fmaf(fmaf(59.220406f, z, -85.44285f), z, 64.939316f), z, -19.73920865f), z, 1.f) * amplitude;
+  const float x = quarter & 1 ? s : c;
+  s = quarter & 1 ? c : s;
+  c = __uint_as_float(__float_as_uint(x) ^ (quarter + 1 & 2) << 30);
+  return make_float2(c, __uint_as_float(__float_as_uint(s) ^ (quarter & 2) << 30));
 }
 
-template <typename T>
-struct Chunk {
-  static constexpr int N = 16 / sizeof(T);                      // elements of 16 bytes, and pairs that a lane has of a row
-};
-__device__ __forceinline__ void widen(uint4 x, float (&f)[8]) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void widen(uint4 x, float (&f)[4]) {
-  f[0] = __uint_as_float(x.x); f[1] = __uint_as_float(x.y); f[2] = __uint_as_float(x.z); f[3] = __uint_as_float(x.w);
-}
-__device__ __forceinline__ uint4 narrow(const float (&f)[8]) { return make_uint4(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]), bf16x2(f[4], f[5]), bf16x2(f[6], f[7])); }
-__device__ __forceinline__ uint4 narrow(const float (&f)[4]) {
-  return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-}
-__device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ void put(__nv_bfloat16* at, float x) { *at = __float2bfloat16(x); }
 __device__ __forceinline__ void put(float* at, float x) { *at = x; }
 
-// Where a row's N pairs from pair p0 on lie: two chunks of N elements at `a` and `b`, element i of one paired with element i of the other
-// (apart), or pairs of neighbours.  Whole chunks of pairs are rotated or are not where dim is a multiple of 2 N; else element by element.
-template <typename T>
+// How a head's D elements form pairs for a lane that has N of them from pair p0 on, as two chunks of N elements at `a` and `b`:
+// HALVES: element i of one with element i of the other, the pairs (c, c + dim / 2), and behind them, not turned, (c, c + (D - dim) / 2);
+// NEIGHBOURS: pairs within a chunk; both where whole chunks are turned or are not (dim a multiple of 2 N).  SINGLE: element by element.
+enum Pairing { HALVES, NEIGHBOURS, SINGLE };
+inline __host__ __device__ Pairing pairing_of(const RopeArgs& r, int n) { return r.dim % (2 * n) ? SINGLE : r.interleaved ? NEIGHBOURS : HALVES; }
+
+// A lane's chunks as they lie in memory (SINGLE: as whole pairs of neighbours would).
+template <typename T, int N>
+struct RawPairs { uint32_t x[N * sizeof(T) / 4], y[N * sizeof(T) / 4]; };
+
+template <typename T, int D, Pairing P, int N>
 struct PairPlace {
-  static constexpr int N = Chunk<T>::N;
+  using Raw = RawPairs<T, N>;
+  static constexpr int W = N * sizeof(T) / 4;                   // words of a chunk
   int p0, a, b, half;
-  bool apart, turned, whole;
-  __device__ __forceinline__ PairPlace(int dim, bool interleaved, int p) {
+  bool apart;
+  __device__ __forceinline__ PairPlace(const RopeArgs& r, int p) {
     p0 = p;
-    half = dim / 2;
-    whole = dim % (2 * N) == 0;
-    turned = p < half;
-    apart = turned && !interleaved;
-    a = apart ? p : 2 * p;
-    b = apart ? p + half : 2 * p + N;
+    half = r.dim / 2;
+    apart = !r.interleaved;
+    a = P == HALVES ? (p < half ? p : p + half) : 2 * p;
+    b = P == HALVES ? (p < half ? p + half : p + D / 2) : 2 * p + N;
   }
-  // elements of pair p0 + i
+  // SINGLE: elements of pair p0 + i
   __device__ __forceinline__ int2 pair(int i) const {
     const int p = p0 + i;
     return apart && p < half ? make_int2(p, p + half) : make_int2(2 * p, 2 * p + 1);
   }
-  __device__ __forceinline__ bool turns(int i) const { return whole ? turned : p0 + i < half; }
+  __device__ __forceinline__ bool turns(int i) const { return P == SINGLE ? p0 + i < half : p0 < half; }
+
+  static __device__ __forceinline__ void load_chunk(const T* p, uint32_t (&w)[W]) {
+    if constexpr (W == 4) {
+      const uint4 v = *(const uint4*)p;
+      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else {
+      const uint2 v = *(const uint2*)p;
+      w[0] = v.x; w[1] = v.y;
+    }
+  }
+  __device__ __forceinline__ Raw load(const T* row) const {
+    Raw r;
+    if constexpr (P != SINGLE) {
+      load_chunk(row + a, r.x);
+      load_chunk(row + b, r.y);
+    } else {
+      T x[N], y[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int2 e = pair(i);
+        (i < N / 2 ? x : y)[(2 * i) % N] = row[e.x];
+        (i < N / 2 ? x : y)[(2 * i + 1) % N] = row[e.y];
+      }
+      memcpy(r.x, x, sizeof(r.x));
+      memcpy(r.y, y, sizeof(r.y));
+    }
+    return r;
+  }
+  static __device__ __forceinline__ float element(const uint32_t (&w)[W], int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+  static __device__ __forceinline__ void pairs(const Raw& r, float (&u)[N], float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      u[i] = P == HALVES ? element(r.x, i) : i < N / 2 ? element(r.x, 2 * i) : element(r.y, 2 * i - N);
+      v[i] = P == HALVES ? element(r.y, i) : i < N / 2 ? element(r.x, 2 * i + 1) : element(r.y, 2 * i + 1 - N);
+    }
+  }
+  // Pairs as chunks.
+  static __device__ __forceinline__ void chunks(const float (&u)[N], const float (&v)[N], float (&x)[N], float (&y)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = P == HALVES ? u[i] : i % 2 ? v[i / 2] : u[i / 2];
+      y[i] = P == HALVES ? v[i] : i % 2 ? v[N / 2 + i / 2] : u[N / 2 + i / 2];
+    }
+  }
+  static __device__ __forceinline__ void store_chunk(T* p, const float (&x)[N]) {
+    uint32_t w[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(x[i]);
+      else w[i] = bf16x2(x[2 * i], x[2 * i + 1]);
+    }
+    if constexpr (W == 4) *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+    else *(uint2*)p = make_uint2(w[0], w[1]);
+  }
+  __device__ __forceinline__ void store(T* row, const float (&u)[N], const float (&v)[N]) const {
+    if constexpr (P != SINGLE) {
+      float x[N], y[N];
+      chunks(u, v, x, y);
+      store_chunk(row + a, x);
+      store_chunk(row + b, y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int2 e = pair(i);
+        put(row + e.x, u[i]);
+        put(row + e.y, v[i]);
+      }
+    }
+  }
+  // Cosines and sines of a position, two pairs to a word pair for the packed products; (1, 0) where nothing turns.
+  __device__ __forceinline__ void angles(const RopeArgs& r, int position, bool inverse, uint64_t (&cos)[N / 2], uint64_t (&sin)[N / 2]) const {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      float2 cs[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        cs[e] = turns(i + e) ? cos_sin(turn_of(r.step[min(p0 + i + e, STRUCTKV_ROPE_MAX_DIM / 2 - 1)], position), r.amplitude) : make_float2(1.f, 0.f);
+        if (inverse) cs[e].y = -cs[e].y;
+      }
+      cos[i / 2] = pack2(cs[0].x, cs[1].x);
+      sin[i / 2] = pack2(cs[0].y, cs[1].y);
+    }
+  }
+  // Turns the pairs (those that do not turn stay as they are, infinities and NaN among them).
+  __device__ __forceinline__ void turn(float (&u)[N], float (&v)[N], const uint64_t (&cos)[N / 2], const uint64_t (&sin)[N / 2]) const {
+    if (P != SINGLE && !turns(0)) return;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const uint64_t x = pack2(u[i], u[i + 1]), y = pack2(v[i], v[i + 1]);
+      float a0, a1, b0, b1;
+      unpack2(fma2(x, cos[i / 2], mul2(y, sin[i / 2] ^ 0x8000000080000000ull)), a0, a1);
+      unpack2(fma2(y, cos[i / 2], mul2(x, sin[i / 2])), b0, b1);
+      if (turns(i)) { u[i] = a0; v[i] = b0; }
+      if (turns(i + 1)) { u[i + 1] = a1; v[i + 1] = b1; }
+    }
+  }
 };
-// x: pairs as (u[i], v[i])
-template <typename T>
-__device__ __forceinline__ void split(const PairPlace<T>& at, const float (&x)[Chunk<T>::N], const float (&y)[Chunk<T>::N], float (&u)[Chunk<T>::N],
-                                      float (&v)[Chunk<T>::N]) {
-  constexpr int N = Chunk<T>::N;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    u[i] = at.apart ? x[i] : i < N / 2 ? x[(2 * i) % N] : y[(2 * i) % N];
-    v[i] = at.apart ? y[i] : i < N / 2 ? x[(2 * i + 1) % N] : y[(2 * i + 1) % N];
-  }
-}
-template <typename T>
-__device__ __forceinline__ void join(const PairPlace<T>& at, const float (&u)[Chunk<T>::N], const float (&v)[Chunk<T>::N], float (&x)[Chunk<T>::N],
-                                     float (&y)[Chunk<T>::N]) {
-  constexpr int N = Chunk<T>::N;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    x[i] = at.apart ? u[i] : i % 2 ? v[i / 2] : u[i / 2];
-    y[i] = at.apart ? v[i] : i % 2 ? v[N / 2 + i / 2] : u[N / 2 + i / 2];
-  }
-}
-template <typename T>
-__device__ __forceinline__ void load_pairs(const PairPlace<T>& at, const T* row, float (&u)[Chunk<T>::N], float (&v)[Chunk<T>::N]) {
-  constexpr int N = Chunk<T>::N;
-  if (at.whole) {
-    float x[N], y[N];
-    widen(*(const uint4*)(row + at.a), x);
-    widen(*(const uint4*)(row + at.b), y);
-    split<T>(at, x, y, u, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int2 e = at.pair(i);
-      u[i] = value(row[e.x]);
-      v[i] = value(row[e.y]);
-    }
-  }
-}
-template <typename T>
-__device__ __forceinline__ void store_pairs(const PairPlace<T>& at, T* row, const float (&u)[Chunk<T>::N], const float (&v)[Chunk<T>::N]) {
-  constexpr int N = Chunk<T>::N;
-  if (at.whole) {
-    float x[N], y[N];
-    join<T>(at, u, v, x, y);
-    *(uint4*)(row + at.a) = narrow(x);
-    *(uint4*)(row + at.b) = narrow(y);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int2 e = at.pair(i);
-      put(row + e.x, u[i]);
-      put(row + e.y, v[i]);
-    }
-  }
-}
-__device__ __forceinline__ void turn(float& u, float& v, float2 cs) {
-  const float x = u;
-  u = fmaf(x, cs.x, -(v * cs.y));
-  v = fmaf(v, cs.x, x * cs.y);
-}
 
 // Heads [h0, h1) of one token: this lane's N pairs of each, from pair p0 on.
-template <typename T>
+template <typename T, int D, Pairing P, int N>
 __device__ __forceinline__ void rotate_heads(const RopeArgs& r, bool inverse, const T* x, long long x_head, T* y, long long y_head, int position,
                                              int p0, int h0, int h1) {
-  constexpr int N = Chunk<T>::N, U = 4;
-  const PairPlace<T> at(r.dim, r.interleaved, p0);
-  float2 cs[N];
+  constexpr int U = 2;
+  using Place = PairPlace<T, D, P, N>;
+  const Place at(r, p0);
+  typename Place::Raw raw[U];
+  auto load = [&](int h) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    cs[i] = at.turns(i) ? cos_sin<T>(turn_of(r.step[min(p0 + i, STRUCTKV_ROPE_MAX_DIM / 2 - 1)], position), r.amplitude) : make_float2(1.f, 0.f);
-    if (inverse) cs[i].y = -cs[i].y;
-  }
+    for (int e = 0; e < U; ++e) raw[e] = at.load(x + (long long)min(h + e, h1 - 1) * x_head);
+  };
+  load(h0);
+  uint64_t cos[N / 2], sin[N / 2];
+  at.angles(r, position, inverse, cos, sin);
 #pragma unroll 1
   for (int h = h0; h < h1; h += U) {
-    float u[U][N], v[U][N];
-#pragma unroll
-    for (int e = 0; e < U; ++e) load_pairs<T>(at, x + (long long)min(h + e, h1 - 1) * x_head, u[e], v[e]);
 #pragma unroll
     for (int e = 0; e < U; ++e) {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (at.turns(i)) turn(u[e][i], v[e][i], cs[i]);
-      if (h + e < h1) store_pairs<T>(at, y + (long long)(h + e) * y_head, u[e], v[e]);
+      float u[N], v[N];
+      at.pairs(raw[e], u, v);
+      at.turn(u, v, cos, sin);
+      if (h + e < h1) at.store(y + (long long)(h + e) * y_head, u, v);
     }
+    if (h + U < h1) load(h + U);
   }
+}
+
+// Runs L<storage type, elements of a head, pairing of a lane's n pairs>::run(args).
+template <template <typename, int, Pairing> class L, typename T, int D, typename... Args>
+inline cudaError_t by_dim(Pairing p, const Args&... args) {
+  return p == SINGLE ? L<T, D, SINGLE>::run(args...) : p == HALVES ? L<T, D, HALVES>::run(args...) : L<T, D, NEIGHBOURS>::run(args...);
+}
+template <template <typename, int, Pairing> class L, typename... Args>
+inline cudaError_t by_pairing(const Ctx& ctx, Pairing p, const Args&... args) {
+  const bool bf16 = ctx.cfg.dtype == STRUCTKV_BF16, wide = ctx.cfg.head_dim == 128;
+  if (bf16) return wide ? by_dim<L, __nv_bfloat16, 128>(p, args...) : by_dim<L, __nv_bfloat16, 64>(p, args...);
+  return wide ? by_dim<L, float, 128>(p, args...) : by_dim<L, float, 64>(p, args...);
 }
 
 #endif  // __CUDACC__

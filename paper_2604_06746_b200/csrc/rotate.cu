@@ -8,32 +8,33 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) rotate(const __grid_constant__ RopeArgs r, const __grid_constant__ RotateArgs a) {
-  constexpr int N = Chunk<T>::N, LANES = D / (2 * N);
+template <typename T, int D, Pairing P>
+__global__ void __launch_bounds__(kThreads, 3) rotate(const __grid_constant__ RopeArgs r, const __grid_constant__ RotateArgs a) {
+  constexpr int N = 16 / sizeof(T), LANES = D / (2 * N);
   pdl_trigger();
   pdl_wait();
   const long long row = (long long)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
   const int h0 = blockIdx.y * a.head_step;
   if (row >= a.rows) return;
   const int b = quotient((int)row, a.by_tokens), i = (int)row - b * a.tokens;
-  rotate_heads<T>(r, a.inverse, (const T*)(a.x + b * a.x_batch + i * a.x_token), a.x_head / (int)sizeof(T),
+  rotate_heads<T, D, P, N>(r, a.inverse, (const T*)(a.x + b * a.x_batch + i * a.x_token), a.x_head / (int)sizeof(T),
                   (T*)(a.out + b * a.o_batch + i * a.o_token), a.o_head / (int)sizeof(T), a.positions[b * a.s_positions + i],
                   (threadIdx.x % LANES) * N, h0, min(h0 + a.head_step, a.heads));
 }
 
-template <typename T, int D>
-cudaError_t launch(const RopeArgs& r, const RotateArgs& a, cudaStream_t st) {
-  constexpr int PER = kThreads / (D / (2 * Chunk<T>::N));
-  return launch_pdl(rotate<T, D>, dim3((unsigned)(((long long)a.rows + PER - 1) / PER), (a.heads + a.head_step - 1) / a.head_step), dim3(kThreads), 0,
-                    st, r, a);
-}
+template <typename T, int D, Pairing P>
+struct Launch {
+  static cudaError_t run(const RopeArgs& r, const RotateArgs& a, cudaStream_t st) {
+    constexpr int PER = kThreads / (D * (int)sizeof(T) / 32);
+    return launch_pdl(rotate<T, D, P>, dim3((unsigned)(((long long)a.rows + PER - 1) / PER), (a.heads + a.head_step - 1) / a.head_step), dim3(kThreads),
+                      0, st, r, a);
+  }
+};
 
 }  // namespace
 
 cudaError_t launch_rotate(const Ctx& ctx, const RopeArgs& r, const RotateArgs& a, cudaStream_t st) {
-  if (ctx.cfg.dtype == STRUCTKV_BF16) return ctx.cfg.head_dim == 128 ? launch<__nv_bfloat16, 128>(r, a, st) : launch<__nv_bfloat16, 64>(r, a, st);
-  return ctx.cfg.head_dim == 128 ? launch<float, 128>(r, a, st) : launch<float, 64>(r, a, st);
+  return by_pairing<Launch>(ctx, pairing_of(r, ctx.cfg.dtype == STRUCTKV_BF16 ? 8 : 4), r, a, st);
 }
 
 }  // namespace skv
