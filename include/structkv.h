@@ -655,7 +655,8 @@ structkv_status structkv_rotate(structkv_ctx* ctx, const structkv_rope* rope, co
  * slots of a head share a scale, a power of two 2^e held as the byte e + 127: a value is code * 2^e.  Sequence b's slot j is slot
  * j mod page_size of page table[b, j / page_size].
  *   k, v        device, element (page, g, slot, c) at k + page*stride_page + g*stride_head + slot*stride_token + c (bytes; d contiguous;
- *               bases 16-byte aligned, strides multiples of 16; pages, heads and slots do not overlap).
+ *               bases 16-byte aligned, strides multiples of 16, not negative, stride_token below 2^22 and stride_page below 2^32; pages, heads and slots
+ *               do not overlap).
  *   k_scales, v_scales   device, [pages, H_kv, page_size / STRUCTKV_SCALE_BLOCK] bytes; what the calls write lies in 87 .. 247.
  *   table       device, row b at table + b*table_stride, table_columns entries.  An entry that is looked at and is no page records
  *               STRUCTKV_ERR_INVALID_ARG in the device status word; its slots are neither written nor seen.

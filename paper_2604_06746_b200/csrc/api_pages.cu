@@ -43,10 +43,12 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
   if (!steps_16(1, p->stride_page, p->stride_head, p->stride_token)) return false;
   if (p->stride_token < cfg.head_dim || (cfg.n_kv_heads > 1 && p->stride_head < cfg.head_dim) || (p->pages > 1 && p->stride_page < cfg.head_dim))
     return false;
+  // (a step within a page is counted in 31 bits, one between pages in 32, blocks of slots in 31)
+  if (p->stride_token >= 1ll << 22 || p->stride_page >= 1ll << 32 || (long long)p->pages * cfg.n_kv_heads * (p->page_size / 16) > 0x7fffffffll) return false;
   int shift = 4;
   while (1 << shift < p->page_size) ++shift;
-  *v = PagesView{(char*)p->k, (char*)p->v, p->k_scales, p->v_scales, p->stride_page, p->stride_head, p->stride_token, p->table_stride * 4,
-                 p->table, p->lengths, p->batch, cfg.n_kv_heads, p->pages, shift, p->table_columns << shift, ctx->c.ws.status};
+  *v = PagesView{(char*)p->k, (char*)p->v, p->k_scales, p->v_scales, p->stride_page, p->stride_head, p->table_stride * 4,
+                 (int)p->stride_token, p->table, p->lengths, p->batch, cfg.n_kv_heads, p->pages, shift, p->table_columns << shift, ctx->c.ws.status};
   return true;
 }
 
@@ -60,7 +62,7 @@ bool sizes_ok(const structkv_config& cfg, int batch, int n_new, long long slots)
   const long long units = (long long)batch * cfg.n_kv_heads, rows = (long long)cfg.n_q_heads / cfg.n_kv_heads * n_new;
   return units <= 0x3fffffffll && units * rows <= 0x3fffffffll && units * ((rows + 7) / 8) <= 0x7fffffffll / (slots / kPageTile + 1 + kOverTiles);
 }
-struct PagesWs { int* seq_start; float2* part_stat; float* part_out; size_t bytes; };
+struct PagesWs { int2* item_parts; float2* part_stat; float* part_out; size_t bytes; };
 PagesWs carve(const structkv_config& cfg, const PagesPlan& p, int batch, int n_new, void* base) {
   PagesWs w{};
   char* at = (char*)base;
@@ -70,8 +72,8 @@ PagesWs carve(const structkv_config& cfg, const PagesPlan& p, int batch, int n_n
     off += align_up(bytes, 256);
     return r;
   };
-  const size_t group = cfg.n_q_heads / cfg.n_kv_heads, slots = (size_t)batch * cfg.n_kv_heads * ((group * n_new + p.rb - 1) / p.rb) + p.ctas;
-  w.seq_start = (int*)take(((size_t)batch + 1) * sizeof(int));
+  const size_t group = cfg.n_q_heads / cfg.n_kv_heads, items = (size_t)batch * cfg.n_kv_heads * ((group * n_new + p.rb - 1) / p.rb), slots = items + p.ctas;
+  w.item_parts = (int2*)take(items * sizeof(int2));
   w.part_stat = (float2*)take(slots * p.rb * sizeof(float2));
   w.part_out = (float*)take(slots * p.rb * cfg.head_dim * sizeof(float));
   w.bytes = off;
@@ -239,7 +241,7 @@ structkv_status structkv_attend_pages(structkv_ctx* ctx, const structkv_pages* p
   a.by_ctas = div_by(plan.ctas);
   a.out = (char*)x->out;
   a.lse = x->lse;
-  a.seq_start = w.seq_start;
+  a.item_parts = w.item_parts;
   a.part_stat = w.part_stat;
   a.part_out = w.part_out;
   a.ctas = plan.ctas;

@@ -19,6 +19,7 @@ namespace skv {
 namespace {
 
 constexpr float kRaise = 7.f;          // weights are up to 2^(kRaise + kSlack): fp16 keeps those down to 2^-31 of the largest
+constexpr float kNothing = -3.4e38f;   // reference of a row that has seen nothing
 
 __device__ __forceinline__ uint4 load16(const char* p) {
   uint4 x;
@@ -65,79 +66,104 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 __device__ __forceinline__ float exp2i(int e) { return __int_as_float(min(max(127 + e, 1), 254) << 23); }   // within fp32's normal numbers
 
+// NR blocks of 8 rows, NW warps.
 template <int D, int NR, int NW>
 struct PagesShape {
-  static constexpr int RB = 8 * NR, kRow = D + 4;
-  static constexpr int kSmem = NW * RB * (kRow + 2) * 4;
+  static constexpr int RB = 8 * NR, kRow = D + 4, kSet = RB * kRow + 16;   // of a warp's output: neighbouring warps' are in other banks
+  static constexpr int kSmem = (NW * kSet + 2 * RB * 16) * 4;
+  static_assert(NW >= 8 && NW <= 16, "a row's references are read sixteen at a time");
 };
 
-// NR: blocks of 8 rows; F32: fp32 storage; CAP: capped scores; NW: warps.
-template <int D, int NR, bool F32, bool CAP, int NW, int PER>
-__global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_constant__ AttendPagesArgs a) {
+// F32: fp32 storage; CAP: capped scores.
+template <int D, int NR, bool F32, bool CAP, int NW>
+__global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant__ AttendPagesArgs a) {
   using S = PagesShape<D, NR, NW>;
   constexpr int RB = S::RB, KK = D / 16, KH = D / 64, PIECES = F32 ? 2 : 1, VW = D / 32;   // VW: words of V a lane has of a key
-  extern __shared__ float smem[];
-  float* const outs = smem;                                      // [warp][RB][kRow]
-  float* const refs = outs + NW * RB * S::kRow;                  // [RB][warp]
-  float* const sums = refs + RB * NW;
+  extern __shared__ __align__(16) float smem[];
+  float* const outs = smem;                                      // [warp] [RB][kRow]
+  float* const refs = outs + NW * S::kSet;                       // [RB][16], by warps
+  float* const sums = refs + RB * 16;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
   pdl_trigger();
   pdl_wait();
-  const PageRun run = find_run(a, blockIdx.x == 0 ? a.seq_start : nullptr);
+  const PageRun run = find_run(a);
   PageSegment sg = first_segment(a, run);
-  const int sh4 = a.c.page_shift - kBlockShift, per_page = 1 << sh4;
-#pragma unroll 1
-  for (; sg.t1; next_segment(sg, a)) {
-    const int b = sg.b, g = quotient(sg.nth, a.by_blocks), rb = sg.nth - g * a.blocks;
-    const int n_old = a.c.lengths[b], first_row = rb * RB + 2 * t4;
-    const int s_end = min(sg.t1 * (kPageTile / 16), (sg.keys + 15) / 16);
-    int s = sg.t0 * (kPageTile / 16) + warp;
-    const int* const table = (const int*)((const char*)a.c.table + b * a.c.s_table);
-    const char *const k0 = a.c.k + g * a.c.s_head + t4 * 16, *const v0 = a.c.v + g * a.c.s_head + g8 * (VW * 4);
-    // (a page that is none: its slots are not seen; the loads go to page 0)
-    auto page_of = [&](int step) { return step < s_end ? table[step >> sh4] : 0; };
-    struct At { size_t page, scale; int slot; bool bad; };
-    auto at_of = [&](int step, int page) {
-      const bool bad = page < 0 || page >= a.c.pages;
-      const size_t p = bad ? 0 : page;
-      return At{p, ((p * a.c.n_kv + g) << sh4) + (step & (per_page - 1)), (step & (per_page - 1)) << kBlockShift, bad};
-    };
-    uint4 kb[2][KH];
-    uint32_t vb[4][VW];
-    int ke = 0, ve = 0;
-    auto load_k = [&](const At& x) {
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-#pragma unroll
-        for (int h = 0; h < KH; ++h) kb[y][h] = load16(k0 + x.page * a.c.s_page + (x.slot + g8 + 8 * y) * a.c.s_token + h * 64);
-      ke = a.c.k_scales[x.scale];
-    };
-    auto load_v = [&](const At& x) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const char* const p = v0 + x.page * a.c.s_page + (x.slot + 2 * t4 + (e & 1) + 8 * (e >> 1)) * a.c.s_token;
-        if constexpr (VW == 4) {
-          const uint4 w = load16(p);
-          vb[e][0] = w.x; vb[e][1] = w.y; vb[e][2] = w.z; vb[e][3] = w.w;
-        } else {
-          const uint2 w = load8(p);
-          vb[e][0] = w.x; vb[e][1] = w.y;
-        }
-      }
-      ve = a.c.v_scales[x.scale];
-    };
-    At now = at_of(s, page_of(s));
-    if (s < s_end) {
-      load_k(now);
-      load_v(now);
-    }
-    int next_page = page_of(s + NW);
+  const int sh4 = a.c.page_shift - kBlockShift, per_page = 1 << sh4, token = a.c.s_token;
 
+  // A warp has every NW-th 16 keys of a segment.  Lane i knows the page and the scales of the i-th of the next 32 that it has, and of the 32 behind
+  // them: bytes of K's and V's scale, and above them whether the page is none (its slots are not seen; the copies come from page 0).
+  int b, g, rb, n_old, s, s_end, page, page_after;
+  unsigned about, about_after;
+  const char *k0, *v0;
+  const int* table;
+  auto look = [&](int step, unsigned& what) {
+    int p = 0;
+    what = 0;
+    if (step < s_end) {
+      p = table[step >> sh4];
+      if ((unsigned)p >= (unsigned)a.c.pages) {
+        p = 0;
+        what = 1u << 16;
+      }
+      const unsigned at = (((unsigned)p * a.c.n_kv + g) << sh4) + (step & (per_page - 1));
+      what |= a.c.k_scales[at] | (unsigned)a.c.v_scales[at] << 8;
+    }
+    return p;
+  };
+  // this lane's rows of K (keys g8 and g8 + 8) and of V (keys 2 t4, + 1, + 8, + 9)
+  uint4 kb[2][KH];
+  uint32_t vb[4][VW];
+  auto bytes_of = [&](int step, int p) { return (long long)((unsigned long long)(unsigned)p * (unsigned)a.c.s_page) + (step & (per_page - 1)) * (token << kBlockShift); };
+  auto load_k = [&](int step, int p) {
+    const char* const from = k0 + bytes_of(step, p);
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int h = 0; h < KH; ++h) kb[y][h] = load16(from + y * 8 * token + h * 64);
+  };
+  auto load_v = [&](int step, int p) {
+    const char* const from = v0 + bytes_of(step, p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const char* const at = from + ((e & 1) + 8 * (e >> 1)) * token;
+      if constexpr (VW == 4) {
+        const uint4 w = load16(at);
+        vb[e][0] = w.x; vb[e][1] = w.y; vb[e][2] = w.z; vb[e][3] = w.w;
+      } else {
+        const uint2 w = load8(at);
+        vb[e][0] = w.x; vb[e][1] = w.y;
+      }
+    }
+  };
+  // A segment begins: its first keys are on their way.
+  auto begin = [&]() {
+    b = sg.b;
+    g = quotient(sg.nth, a.by_blocks);
+    rb = sg.nth - g * a.blocks;
+    n_old = a.c.lengths[b];
+    s = sg.t0 * (kPageTile / 16) + warp;
+    s_end = min(sg.t1 * (kPageTile / 16), (sg.keys + 15) / 16);
+    table = (const int*)((const char*)a.c.table + b * a.c.s_table);
+    k0 = a.c.k + g * a.c.s_head + (long long)g8 * token + t4 * 16;
+    v0 = a.c.v + g * a.c.s_head + 2ll * t4 * token + g8 * (VW * 4);
+    page = look(s + lane * NW, about);
+    const int p = __shfl_sync(0xffffffffu, page, 0);
+    if (s < s_end) {
+      load_k(s, p);
+      load_v(s, p);
+    }
+    page_after = look(s + (32 + lane) * NW, about_after);
+  };
+  if (sg.t1) begin();
+#pragma unroll 1
+  while (sg.t1) {
+    const int first_row = rb * RB + 2 * t4, s0 = sg.t0 * (kPageTile / 16);
     // the rows
     uint32_t qf[PIECES][NR][KK][2];
     float qs[NR][2];                                             // a row's factor: scale in bits (capped scores: 1), times 2^-the raise of its queries
     float o[NR][KK][4], m[NR][2], l[NR][2];                      // o[.][t]: columns 16 g8 (8 g8) + 2 t and + 1 of rows 2 t4 and + 1
     int last[NR][2];                                             // the last slot that a row sees
+    bool far = false;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       const int r = rb * RB + 8 * i + g8;
@@ -178,7 +204,7 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
         const int down = __shfl_sync(0xffffffffu, raise, (2 * t4 + e) * 4);
         qs[i][e] = exp2i(-down) * (CAP ? 1.f : a.scale2);
         last[i][e] = n_old + quotient(min(first_row + 8 * i + e, a.rows - 1), a.by_group);
-        m[i][e] = -INFINITY;
+        m[i][e] = kNothing;
         l[i][e] = 0.f;
       }
 #pragma unroll
@@ -186,11 +212,17 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
     }
 
 #pragma unroll 1
-    while (s < s_end) {
-      const int sn = s + NW, j0 = s << kBlockShift;
-      const bool more = sn < s_end;
-      const At next = at_of(sn, next_page);
-      next_page = page_of(sn + NW);
+    for (int nth = 0; s < s_end; ++nth, s += NW) {
+      const int ahead = s + NW, j0 = s << kBlockShift, i32 = nth & 31;
+      if (i32 == 0 && nth > 0) {
+        page = page_after;
+        about = about_after;
+        page_after = look(s + (32 + lane) * NW, about_after);
+      }
+      const unsigned what = __shfl_sync(0xffffffffu, about, i32);
+      const int page_ahead = __shfl_sync(0xffffffffu, i32 < 31 ? page : page_after, (i32 + 1) & 31);
+      const int ke = what & 0xff, ve = what >> 8 & 0xff;
+      const bool bad = what >> 16;
       // products: two chains where a warp has one block of rows
       constexpr int CHAINS = NR == 1 ? 2 : 1;
       float acc[CHAINS][NR][4];
@@ -209,29 +241,72 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
           for (int i = 0; i < NR; ++i) mma(acc[kk % CHAINS][i], x0, x1, x2, x3, qf[p][i][kk][0], qf[p][i][kk][1]);
       }
       const float kf = exp2i(ke - 127), vl = exp2i(127 - ve), vx = (float)(ve - 127);
-      if (more) load_k(next);
-      float y[NR][4];                                            // element 2 z + x: key g8 + 8 z, row x
+      // y - m, element 2 z + x: key g8 + 8 z, row x.  References are whole numbers, so that vx - m is exact.
+      float y[NR][4];
+      auto scores = [&](int i, const float (&c)[2]) {
+        float z[4];
 #pragma unroll
-      for (int i = 0; i < NR; ++i) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][e] = (CHAINS == 2 ? acc[0][i][e] + acc[CHAINS - 1][i][e] : acc[0][i][e]) * (qs[i][e & 1] * kf);
+        for (int e = 0; e < 4; ++e) z[e] = CHAINS == 2 ? acc[0][i][e] + acc[CHAINS - 1][i][e] : acc[0][i][e];
+        const float f[2] = {qs[i][0] * kf, qs[i][1] * kf};
         if (CAP) {
-          capped2(y[i][0], y[i][1], pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
-          capped2(y[i][2], y[i][3], pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[e] *= f[e & 1];
+          capped2(z[0], z[1], pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
+          capped2(z[2], z[3], pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][e] += vx;
+        for (int e = 0; e < 4; ++e) y[i][e] = CAP ? z[e] + c[e & 1] : fmaf(z[e], f[e & 1], c[e & 1]);
+      };
+      if (ahead < s_end) load_k(ahead, page_ahead);
+      const bool tail = j0 + 16 > n_old + 1 || bad;
+      auto hide = [&](int i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (bad || j0 + g8 + 8 * (e >> 1) > last[i][e & 1]) y[i][e] = -INFINITY;
+      };
+      // references: those that are outgrown follow, and the scores are worked out again
+#pragma unroll 1
+      for (bool again = false;; again = true) {
+        bool grown = false;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          scores(i, {vx - m[i][0], vx - m[i][1]});
+          if (tail) hide(i);
+          grown |= fmaxf(fmaxf(y[i][0], y[i][1]), fmaxf(y[i][2], y[i][3])) > kRaise + kSlack;
+        }
+        if (!__any_sync(0xffffffffu, grown) || again) break;
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+          scores(i, {vx, vx});
+          if (tail) hide(i);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float t = fmaxf(y[i][e], y[i][2 + e]);
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            t = fmaxf(ceilf(t) - kRaise, m[i][e]);
+            const float f = fast_exp2(m[i][e] - t);
+            m[i][e] = t;
+            if (t != kNothing) top = fmaxf(top, fabsf(t));
+            l[i][e] *= f;
+#pragma unroll
+            for (int k = 0; k < KK; ++k) { o[i][k][e] *= f; o[i][k][2 + e] *= f; }
+          }
+        }
+        far = __any_sync(0xffffffffu, top > 0x1p20f);
       }
-      const bool tail = j0 + 16 > n_old + 1 || now.bad;
-      uint32_t odd[4] = {0u, 0u, 0u, 0u};                        // columns of the lane's four keys whose V is NaN, as bits
-      bool any_odd = false;
-      if (tail) {
-        if (now.bad && lane == 0) tell_invalid(a.c);
+      // A score and a reference so far from zero that their difference is off by whole bits: no weight is above the largest.
+      if (far)
 #pragma unroll
         for (int i = 0; i < NR; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (now.bad || j0 + g8 + 8 * (e >> 1) > last[i][e & 1]) y[i][e] = -INFINITY;
+            if (y[i][e] > kRaise + kSlack) y[i][e] = kRaise + kSlack;
+      uint32_t odd[4] = {0u, 0u, 0u, 0u};                        // columns of the lane's four keys whose V is NaN, as bits
+      bool any_odd = false;
+      if (tail) {
+        if (bad && lane == 0) tell_invalid(a.c);
         // What holds NaN here reaches only rows that see it (0 x NaN): it is taken out, and put to those at the end.
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -241,36 +316,14 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
             vb[e][w] &= ~((is >> 7) * 0xffu);
             odd[e] |= ((is >> 7 & 1) | (is >> 14 & 2) | (is >> 21 & 4) | (is >> 28 & 8)) << (4 * w);
           }
-        any_odd = __any_sync(0xffffffffu, (odd[0] | odd[1] | odd[2] | odd[3]) != 0) && !now.bad;
-      }
-      // references
-      bool grown = false;
-#pragma unroll
-      for (int i = 0; i < NR; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) grown |= fmaxf(y[i][e], y[i][2 + e]) - kRaise > m[i][e] + kSlack;
-      if (__any_sync(0xffffffffu, grown)) {
-#pragma unroll
-        for (int i = 0; i < NR; ++i)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float t = fmaxf(y[i][e], y[i][2 + e]);
-#pragma unroll
-            for (int d = 4; d < 32; d *= 2) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-            t = fmaxf(t - kRaise, m[i][e]);
-            const float f = m[i][e] == -INFINITY ? 0.f : fast_exp2(m[i][e] - t);
-            m[i][e] = t;
-            l[i][e] *= f;
-#pragma unroll
-            for (int k = 0; k < KK; ++k) { o[i][k][e] *= f; o[i][k][2 + e] *= f; }
-          }
+        any_odd = __any_sync(0xffffffffu, (odd[0] | odd[1] | odd[2] | odd[3]) != 0) && !bad;
       }
       uint32_t pf[PIECES][NR][2];                                // keys 2 t4 and + 1 (+ 8), row g8
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
         float p[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = fast_exp2(y[i][e] - (m[i][e & 1] == -INFINITY ? 0.f : m[i][e & 1]));
+        for (int e = 0; e < 4; ++e) p[e] = fast_exp2(y[i][e]);
         l[i][0] = fmaf(p[0] + p[2], vl, l[i][0]);
         l[i][1] = fmaf(p[1] + p[3], vl, l[i][1]);
         // weights keep 11 bits for the product (22 for fp32 storage); the sum is of the unrounded ones
@@ -295,7 +348,7 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
             for (int i = 0; i < NR; ++i) mma(o[i][2 * w + z], f0, f1, f2, f3, pf[q][i][0], pf[q][i][1]);
         }
       }
-      if (more) load_v(next);
+      if (ahead < s_end) load_v(ahead, page_ahead);
       if (any_odd) {
 #pragma unroll 1
         for (int c = 0; c < 16; ++c) {                           // lane c / 4 of the four has key 2 (c / 4) + (c & 1) + 8 (c / 2 & 1)
@@ -311,44 +364,67 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
                 if ((cols >> (2 * k + (e >> 1)) & 1) && j <= last[i][e & 1]) o[i][k][e] = __int_as_float(0x7fffffff);
         }
       }
-      s = sn;
-      now = next;
     }
 
     // the segment ends: its warps' outputs, each against its own reference, then their sum against a common one
-    const int sets = min(NW, s_end - sg.t0 * (kPageTile / 16));
-    if (warp < sets) {
+    const int sets = min(NW, s_end - s0), rows = min(RB, a.rows - rb * RB);
 #pragma unroll
-      for (int i = 0; i < NR; ++i)
+    for (int i = 0; i < NR; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+      for (int e = 0; e < 2; ++e) {
 #pragma unroll
-          for (int d = 4; d < 32; d *= 2) l[i][e] += __shfl_xor_sync(0xffffffffu, l[i][e], d);
-          const int row = 8 * i + 2 * t4 + e;
-          if (g8 == 0) {
-            refs[row * NW + warp] = m[i][e];
-            sums[row * NW + warp] = l[i][e];
-          }
-          float* const to = outs + (warp * RB + row) * S::kRow + g8 * (2 * KK);
+        for (int d = 4; d < 32; d *= 2) l[i][e] += __shfl_xor_sync(0xffffffffu, l[i][e], d);
+        const int row = 8 * i + 2 * t4 + e;
+        if (row >= rows) continue;
+        if (g8 == 0) {
+          refs[row * 16 + warp] = m[i][e] == kNothing ? -INFINITY : m[i][e];
+          sums[row * 16 + warp] = l[i][e];
+        }
+        if (warp == 0 && NW + g8 < 16) refs[row * 16 + NW + g8] = -INFINITY;
+        if (warp < sets) {
+          float* const to = outs + warp * S::kSet + row * S::kRow + g8 * (2 * KK);
 #pragma unroll
           for (int k = 0; k < KK; k += 2) *(float4*)(to + 2 * k) = make_float4(o[i][k][e], o[i][k][2 + e], o[i][k + 1][e], o[i][k + 1][2 + e]);
         }
-    }
+      }
     __syncthreads();
-    const int slot = b * a.c.n_kv * a.blocks + sg.nth + blockIdx.x, rows = min(RB, a.rows - rb * RB);
+    const int item = b * a.c.n_kv * a.blocks + sg.nth, slot = item + blockIdx.x;
+    if (tid == 0 && sg.t0 == 0) {
+      // who merges this item: where its partials lie, and how many they are
+      const int end = sg.at + a.over + sg.tiles - 1;
+      a.item_parts[item] = make_int2(slot, cta_of(run.all, end) - (int)blockIdx.x + 1);
+    }
+    next_segment(sg, a);
+    if (sg.t1) begin();
+    // two neighbouring threads have four columns of a row, of every other warp
 #pragma unroll 1
-    for (int i = tid; i < rows * (D / 4); i += NW * 32) {
-      const int row = i / (D / 4), c4 = i % (D / 4);
-      float top = -INFINITY, sum = 0.f;
-      for (int w = 0; w < sets; ++w) top = fmaxf(top, refs[row * NW + w]);
+    for (int i = tid / 2; i < rows * (D / 4); i += NW * 16) {
+      const int row = i / (D / 4), c4 = i % (D / 4), odd = tid & 1;
+      float ref[16], top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 16; w += 4) {
+        const float4 x = *(const float4*)(refs + row * 16 + w);
+        ref[w] = x.x; ref[w + 1] = x.y; ref[w + 2] = x.z; ref[w + 3] = x.w;
+        top = fmaxf(fmaxf(fmaxf(top, x.x), fmaxf(x.y, x.z)), x.w);
+      }
       const float base = top == -INFINITY ? 0.f : top;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int w = 0; w < sets; ++w) {
-        const float f = fast_exp2(refs[row * NW + w] - base);
-        const float4 x = *(const float4*)(outs + (w * RB + row) * S::kRow + c4 * 4);
-        sum = fmaf(f, sums[row * NW + w], sum);
-        v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+      float sum = 0.f;
+      const float* const from = outs + row * S::kRow + c4 * 4;
+#pragma unroll
+      for (int w = 0; w < NW; w += 2) {
+        const int my = w + odd;
+        if (my < sets) {
+          const float f = fast_exp2((odd ? ref[(w + 1) % 16] : ref[w]) - base);
+          const float4 x = *(const float4*)(from + my * S::kSet);
+          sum = fmaf(f, sums[row * 16 + my], sum);
+          v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
+        }
       }
+      // (a warp has sixteen neighbouring pieces, and there are a multiple of as many: it is whole here)
+      auto add = [&](float& x) { x += __shfl_xor_sync(0xffffffffu, x, 1); };
+      add(v.x); add(v.y); add(v.z); add(v.w); add(sum);
+      if (odd) continue;
       *(float4*)(a.part_out + ((size_t)slot * RB + row) * D + c4 * 4) = v;
       if (c4 == 0) a.part_stat[(size_t)slot * RB + row] = make_float2(top, sum);
     }
@@ -356,89 +432,115 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
   }
 }
 
-// Merges an item's partials, a warp a row: M = max m_c, out = sum 2^(m_c - M) O_c / sum 2^(m_c - M) l_c, c ascending.
+// Merges an item's partials: M = max m_c, out = sum 2^(m_c - M) O_c / sum 2^(m_c - M) l_c.  2^by warps of a block share a row's; each takes them in
+// order, and their results are joined in order.  Blocks of 128 threads find room beside an attention CTA and so are there when it ends.
 constexpr int kFinishThreads = 128;
 
 template <int D, bool F32>
-__global__ void __launch_bounds__(kFinishThreads) attend_pages_finish(const __grid_constant__ AttendPagesArgs a, int rb_rows) {
-  constexpr int DL = D / 32, kAhead = 8;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long all = (long long)a.c.batch * a.c.n_kv * a.rows;
+__global__ void __launch_bounds__(kFinishThreads, 8) attend_pages_finish(const __grid_constant__ AttendPagesArgs a, int rb_shift, int by) {
+  constexpr int DL = D / 32, kAhead = 8, kWarps = kFinishThreads / 32;
+  __shared__ float s_out[kWarps][D];
+  __shared__ float2 s_stat[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp & ((1 << by) - 1);
+  const int at = blockIdx.x * (kWarps >> by) + (warp >> by);
+  const bool is = at < a.c.batch * a.c.n_kv * a.rows;
+  const int u = quotient(is ? at : 0, a.by_rows), r = is ? at - u * a.rows : 0, rb = r >> rb_shift;
+  const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, tok = quotient(r, a.by_group), h = r - tok * a.group;
   pdl_trigger();
   pdl_wait();
-  const int W1 = a.seq_start[a.c.batch], items = a.c.n_kv * a.blocks;
-  const Shares sh = shares_of(W1 * items, a.ctas, a.by_ctas, a.least);
+  int n;
+  const int2 where = a.item_parts[u * a.blocks + rb];
+  const int count = rows_of_sequence(a.c, a.counts, b, a.n_new, n), parts = is && tok < count ? where.y : 0;
+  float M = -INFINITY, L = 0.f, acc[DL];
+#pragma unroll
+  for (int e = 0; e < DL; ++e) acc[e] = 0.f;
+  auto join = [&](float2 st, const float (&x)[DL], float ref) {
+    const float w = fast_exp2(st.x - ref);
+    L = fmaf(w, st.y, L);
+#pragma unroll
+    for (int d = 0; d < DL; ++d) acc[d] = fmaf(w, x[d], acc[d]);
+  };
+  auto rescale = [&](float top) {
+    const float ref = top == -INFINITY ? 0.f : top, f = fast_exp2(M - ref);
+    M = top;
+    L *= f;
+#pragma unroll
+    for (int d = 0; d < DL; ++d) acc[d] *= f;
+    return ref;
+  };
+  // (this warp's are neighbours)
+  const int share = (parts + (1 << by) - 1) >> by, first = where.x + mine * share, left = min(share, parts - mine * share);
+  const int row = r & ((1 << rb_shift) - 1);
+  const float2* const stat = a.part_stat + ((size_t)first << rb_shift) + row;
+  const float* const from = a.part_out + (((size_t)first << rb_shift) + row) * D + lane * DL;
 #pragma unroll 1
-  for (long long at = (long long)blockIdx.x * (kFinishThreads / 32) + warp; at < all; at += (long long)gridDim.x * (kFinishThreads / 32)) {
-    const int u = quotient((int)at, a.by_rows), r = (int)at - u * a.rows, rb = r / rb_rows, row = r - rb * rb_rows;
-    const int b = quotient(u, a.by_kv), g = u - b * a.c.n_kv, tok = quotient(r, a.by_group), h = r - tok * a.group;
-    const int before = a.seq_start[b], places = a.seq_start[b + 1] - before, count = a.counts ? a.counts[b] : a.n_new;
-    float M = -INFINITY, L = 0.f, acc[DL];
+  for (int c = 0; c < left; c += kAhead) {
+    float2 st[kAhead];
+    float x[kAhead][DL];
 #pragma unroll
-    for (int e = 0; e < DL; ++e) acc[e] = 0.f;
-    if (places > 0 && tok < count) {
-      const int start = before * items + (g * a.blocks + rb) * places, c0 = cta_of(sh, start + a.over), c1 = cta_of(sh, start + places - 1);
-      const int first = (b * a.c.n_kv + g) * a.blocks + rb + c0, parts = c1 - c0 + 1;
-      const float2* const stat = a.part_stat + (size_t)first * rb_rows + row;
-      const float* const from = a.part_out + ((size_t)first * rb_rows + row) * D + lane * DL;
-#pragma unroll 1
-      for (int c = 0; c < parts; c += kAhead) {
-        float2 st[kAhead];
-        float x[kAhead][DL];
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) {
-          const int k = min(c + e, parts - 1);
-          st[e] = stat[(size_t)k * rb_rows];
-#pragma unroll
-          for (int d = 0; d < DL; ++d) x[e][d] = from[(size_t)k * rb_rows * D + d];
-        }
-        float top = M;
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) {
-          if (c + e >= parts) st[e] = make_float2(-INFINITY, 0.f);
-          top = fmaxf(top, st[e].x);
-        }
-        const float ref = top == -INFINITY ? 0.f : top, f = fast_exp2(M - ref);
-        M = top;
-        L *= f;
-#pragma unroll
-        for (int d = 0; d < DL; ++d) acc[d] *= f;
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e)
-          if (c + e < parts) {
-            const float w = fast_exp2(st[e].x - ref);
-            L = fmaf(w, st[e].y, L);
-#pragma unroll
-            for (int d = 0; d < DL; ++d) acc[d] = fmaf(w, x[e][d], acc[d]);
-          }
+    for (int e = 0; e < kAhead; ++e) {
+      const size_t k = (size_t)min(c + e, left - 1) << rb_shift;
+      st[e] = stat[k];
+      if constexpr (DL == 4) {
+        const float4 v = *(const float4*)(from + k * D);
+        x[e][0] = v.x; x[e][1] = v.y; x[e][2] = v.z; x[e][3] = v.w;
+      } else {
+        const float2 v = *(const float2*)(from + k * D);
+        x[e][0] = v.x; x[e][1] = v.y;
       }
     }
-    const bool nothing = M == -INFINITY && L == 0.f;
-    const float inv = nothing ? 0.f : 1.f / L;
-    const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
+    float top = M;
 #pragma unroll
-    for (int d = 0; d < DL; ++d) acc[d] = nothing ? 0.f : acc[d] * inv;
-    if (F32) {
+    for (int e = 0; e < kAhead; ++e) top = fmaxf(top, st[e].x);
+    const float ref = rescale(top);
 #pragma unroll
-      for (int d = 0; d < DL; ++d) ((float*)a.out)[q * D + lane * DL + d] = acc[d];
-    } else {
-#pragma unroll
-      for (int d = 0; d < DL; d += 2) ((uint32_t*)a.out)[(q * D + lane * DL + d) / 2] = bf16x2(acc[d], acc[d + 1]);
-    }
-    if (lane == 0 && a.lse) a.lse[q] = nothing ? -INFINITY : (M + log2f(L)) * kLn2;
+    for (int e = 0; e < kAhead; ++e)
+      if (c + e < left) join(st[e], x[e], ref);
   }
+  if (by) {
+    if (mine) {
+#pragma unroll
+      for (int d = 0; d < DL; ++d) s_out[warp][lane * DL + d] = acc[d];
+      if (lane == 0) s_stat[warp] = make_float2(M, L);
+    }
+    __syncthreads();
+    if (mine) return;
+    float top = M;
+    for (int k = 1; k < 1 << by; ++k) top = fmaxf(top, s_stat[warp + k].x);
+    const float ref = rescale(top);
+    for (int k = 1; k < 1 << by; ++k) {
+      float x[DL];
+#pragma unroll
+      for (int d = 0; d < DL; ++d) x[d] = s_out[warp + k][lane * DL + d];
+      join(s_stat[warp + k], x, ref);
+    }
+  }
+  if (!is) return;
+  const bool nothing = M == -INFINITY && L == 0.f;
+  const float inv = nothing ? 0.f : 1.f / L;
+  const size_t q = ((size_t)b * a.n_new + tok) * (a.group * a.c.n_kv) + g * a.group + h;
+#pragma unroll
+  for (int d = 0; d < DL; ++d) acc[d] = nothing ? 0.f : acc[d] * inv;
+  if constexpr (F32) {
+    if constexpr (DL == 4) *(float4*)((float*)a.out + q * D + lane * DL) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    else *(float2*)((float*)a.out + q * D + lane * DL) = make_float2(acc[0], acc[1]);
+  } else {
+    if constexpr (DL == 4) *(uint2*)(a.out + (q * D + lane * DL) * 2) = make_uint2(bf16x2(acc[0], acc[1]), bf16x2(acc[2], acc[3]));
+    else *(uint32_t*)(a.out + (q * D + lane * DL) * 2) = bf16x2(acc[0], acc[1]);
+  }
+  if (lane == 0 && a.lse) a.lse[q] = nothing ? -INFINITY : (M + log2f(L)) * kLn2;
 }
 
-template <int D, int NR, bool F32, bool CAP, int NW, int PER>
+template <int D, int NR, bool F32, bool CAP, int NW>
 cudaError_t launch_one(const AttendPagesArgs& a, cudaStream_t st) {
   using S = PagesShape<D, NR, NW>;
-  const cudaError_t e = allow_smem<attend_pages<D, NR, F32, CAP, NW, PER>>(S::kSmem);
-  return e != cudaSuccess ? e : launch_pdl(attend_pages<D, NR, F32, CAP, NW, PER>, dim3(a.ctas), dim3(NW * 32), S::kSmem, st, a);
+  const cudaError_t e = allow_smem<attend_pages<D, NR, F32, CAP, NW>>(S::kSmem);
+  return e != cudaSuccess ? e : launch_pdl(attend_pages<D, NR, F32, CAP, NW>, dim3(a.ctas), dim3(NW * 32), S::kSmem, st, a);
 }
 template <int D, bool CAP>
 cudaError_t launch_rows(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
-  if (ctx.cfg.dtype == STRUCTKV_FP32) return launch_one<D, 1, true, CAP, 8, 1>(a, st);
-  return p.rb == 8 ? launch_one<D, 1, false, CAP, 16, 1>(a, st) : launch_one<D, 2, false, CAP, 8, 1>(a, st);
+  if (ctx.cfg.dtype == STRUCTKV_FP32) return launch_one<D, 1, true, CAP, 8>(a, st);
+  return p.rb == 8 ? launch_one<D, 1, false, CAP, 14>(a, st) : launch_one<D, 2, false, CAP, 8>(a, st);
 }
 
 }  // namespace
@@ -450,11 +552,14 @@ cudaError_t launch_attend_pages(const Ctx& ctx, const AttendPagesArgs& a, const 
 
 cudaError_t launch_attend_pages_finish(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
   const long long rows = (long long)a.c.batch * a.c.n_kv * a.rows;
-  const dim3 grid((unsigned)std::min<long long>((rows + 3) / 4, 16ll * ctx.sm_count));
+  int by = 0, rb_shift = 3;                                       // (as many warps as the SMs hold beside an attention CTA)
+  while (by < 2 && rows << by < 4 * ctx.sm_count) ++by;
+  while (1 << rb_shift < p.rb) ++rb_shift;
+  const dim3 grid((unsigned)(((rows << by) + 3) / 4));
   const bool f32 = ctx.cfg.dtype == STRUCTKV_FP32;
   auto* const kernel = ctx.cfg.head_dim == 128 ? (f32 ? attend_pages_finish<128, true> : attend_pages_finish<128, false>)
                                                : (f32 ? attend_pages_finish<64, true> : attend_pages_finish<64, false>);
-  return launch_pdl(kernel, grid, dim3(kFinishThreads), 0, st, a, p.rb);
+  return launch_pdl(kernel, grid, dim3(kFinishThreads), 0, st, a, rb_shift, by);
 }
 
 }  // namespace skv

@@ -23,7 +23,7 @@ struct AttendPagesArgs {
   float scale2, cap2, inv_cap;                                  // as in AttendArgs
   char* out;
   float* lse;
-  int* seq_start;                                               // [batch + 1] places of one item before a sequence's
+  int2* item_parts;                                             // [item] its first partial's slot, and how many it has
   float2* part_stat;                                            // [slot][RB] reference (bits) and sum
   float* part_out;                                              // [slot][RB][d]
   int ctas, least, over;
@@ -47,8 +47,8 @@ __device__ __forceinline__ int page_keys(const AttendPagesArgs& a, int b) {
 __device__ __forceinline__ int page_places(int keys, int over) { return keys == 0 ? 0 : ((keys + kPageTile - 1) >> kPageTileShift) + over; }
 
 // A CTA's run of places and where it begins: sequence, its keys, places of one item before it.
-struct PageRun { int lo, hi, b, before, keys; };
-__device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a, int* save) {
+struct PageRun { int lo, hi, b, before, keys; Shares all; };
+__device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a) {
   const int lane = threadIdx.x & 31, items = a.c.n_kv * a.blocks;
   int total = 0, keys = 0, places = 0, incl = 0;
   auto sweep = [&](int b0) {
@@ -63,14 +63,12 @@ __device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a, int* save)
 #pragma unroll 1
   for (int b0 = 0; b0 < a.c.batch; b0 += 32) {
     sweep(b0);
-    if (save && threadIdx.x < 32 && b0 + lane < a.c.batch) save[b0 + lane] = total + incl - places;
     total += __shfl_sync(0xffffffffu, incl, 31);
   }
-  if (save && threadIdx.x == 0) save[a.c.batch] = total;
   PageRun w{};
-  const Shares all = shares_of(total * items, a.ctas, a.by_ctas, a.least);
-  w.lo = first_of(all, blockIdx.x);
-  w.hi = first_of(all, blockIdx.x + 1);
+  w.all = shares_of(total * items, a.ctas, a.by_ctas, a.least);
+  w.lo = first_of(w.all, blockIdx.x);
+  w.hi = first_of(w.all, blockIdx.x + 1);
   if (w.lo >= w.hi) return w;
   int before = 0;
 #pragma unroll 1

@@ -8,11 +8,12 @@ namespace skv {
 constexpr int kBlockShift = 4, kBlockSlots = STRUCTKV_SCALE_BLOCK;   // slots that share a scale
 constexpr int kLowExponent = -40;                                   // of a scale; 448 2^-40 is 4e-10
 
-// Strides in bytes.
+// Strides in bytes, s_page below 2^32.
 struct PagesView {
   char *k, *v;
   unsigned char *k_scales, *v_scales;
-  long long s_page, s_head, s_token, s_table;
+  long long s_page, s_head, s_table;
+  int s_token;
   const int* table;
   const int* lengths;
   int batch, n_kv, pages, page_shift, slots;                    // slots: of a sequence, columns of the table times slots of a page
