@@ -52,15 +52,17 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
   return true;
 }
 
+// More than 16 rows of a KV head go to tcgen05's tiles of 128.
 PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  return {cfg.dtype == STRUCTKV_FP32 || rows <= 8 ? 8 : 16, sms};
+  if (cfg.dtype == STRUCTKV_BF16 && rows > 16) return {128, sms, 7, 2};
+  return {cfg.dtype == STRUCTKV_FP32 || rows <= 8 ? 8 : 16, sms, 6, 1};
 }
 // Items, rows and places are counted in 31 bits.
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, long long slots) {
   if (batch < 1 || n_new < 1 || n_new > kMaxNew || slots < 1 || slots > 1 << 30) return false;
   const long long units = (long long)batch * cfg.n_kv_heads, rows = (long long)cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  return units <= 0x3fffffffll && units * rows <= 0x3fffffffll && units * ((rows + 7) / 8) <= 0x7fffffffll / (slots / kPageTile + 1 + kOverTiles);
+  return units <= 0x3fffffffll && units * rows <= 0x3fffffffll && units * ((rows + 7) / 8) <= 0x7fffffffll / (slots / 64 + 1 + kOverTiles);
 }
 struct PagesWs { int2* item_parts; float2* part_stat; float* part_out; size_t bytes; };
 PagesWs carve(const structkv_config& cfg, const PagesPlan& p, int batch, int n_new, void* base) {
@@ -72,7 +74,7 @@ PagesWs carve(const structkv_config& cfg, const PagesPlan& p, int batch, int n_n
     off += align_up(bytes, 256);
     return r;
   };
-  const size_t group = cfg.n_q_heads / cfg.n_kv_heads, items = (size_t)batch * cfg.n_kv_heads * ((group * n_new + p.rb - 1) / p.rb), slots = items + p.ctas;
+  const size_t group = cfg.n_q_heads / cfg.n_kv_heads, items = (size_t)batch * cfg.n_kv_heads * ((group * n_new + p.rb - 1) / p.rb), slots = (items + p.ctas) * p.parts;
   w.item_parts = (int2*)take(items * sizeof(int2));
   w.part_stat = (float2*)take(slots * p.rb * sizeof(float2));
   w.part_out = (float*)take(slots * p.rb * cfg.head_dim * sizeof(float));
@@ -247,7 +249,8 @@ structkv_status structkv_attend_pages(structkv_ctx* ctx, const structkv_pages* p
   a.ctas = plan.ctas;
   a.least = 0;
   a.over = kOverTiles;
-  cudaError_t e = launch_attend_pages(ctx->c, a, plan, (cudaStream_t)stream);
+  a.tile_shift = plan.tile_shift;
+  cudaError_t e = (plan.rb == 128 ? launch_attend_pages_tc : launch_attend_pages)(ctx->c, a, plan, (cudaStream_t)stream);
   if (e == cudaSuccess) e = launch_attend_pages_finish(ctx->c, a, plan, (cudaStream_t)stream);
   return told(e);
 }

@@ -18,8 +18,7 @@
 namespace skv {
 namespace {
 
-constexpr float kRaise = 7.f;          // weights are up to 2^(kRaise + kSlack): fp16 keeps those down to 2^-31 of the largest
-constexpr float kNothing = -3.4e38f;   // reference of a row that has seen nothing
+constexpr int kTileBlocks = 4;         // blocks of 16 keys of a place
 
 __device__ __forceinline__ uint4 load16(const char* p) {
   uint4 x;
@@ -30,22 +29,6 @@ __device__ __forceinline__ uint2 load8(const char* p) {
   uint2 x;
   asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "l"(p));
   return x;
-}
-// Codes of a word's lower and upper half as two fp16 each.
-__device__ __forceinline__ uint32_t half_lo(uint32_t w) {
-  uint32_t x;
-  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %1;\ncvt.rn.f16x2.e4m3x2 %0, a;\n}" : "=r"(x) : "r"(w));
-  return x;
-}
-__device__ __forceinline__ uint32_t half_hi(uint32_t w) {
-  uint32_t x;
-  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %1;\ncvt.rn.f16x2.e4m3x2 %0, b;\n}" : "=r"(x) : "r"(w));
-  return x;
-}
-__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
 }
 // What two values lose as fp16, as fp16.
 __device__ __forceinline__ uint32_t rest2(float lo, float hi, uint32_t of) {
@@ -62,10 +45,6 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-// A word's bytes that are NaN codes, as 0x80 of each.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-__device__ __forceinline__ float exp2i(int e) { return __int_as_float(min(max(127 + e, 1), 254) << 23); }   // within fp32's normal numbers
-
 // NR blocks of 8 rows, NW warps.
 template <int D, int NR, int NW>
 struct PagesShape {
@@ -141,8 +120,8 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
     g = quotient(sg.nth, a.by_blocks);
     rb = sg.nth - g * a.blocks;
     n_old = a.c.lengths[b];
-    s = sg.t0 * (kPageTile / 16) + warp;
-    s_end = min(sg.t1 * (kPageTile / 16), (sg.keys + 15) / 16);
+    s = sg.t0 * (kTileBlocks) + warp;
+    s_end = min(sg.t1 * (kTileBlocks), (sg.keys + 15) / 16);
     table = (const int*)((const char*)a.c.table + b * a.c.s_table);
     k0 = a.c.k + g * a.c.s_head + (long long)g8 * token + t4 * 16;
     v0 = a.c.v + g * a.c.s_head + 2ll * t4 * token + g8 * (VW * 4);
@@ -157,7 +136,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
   if (sg.t1) begin();
 #pragma unroll 1
   while (sg.t1) {
-    const int first_row = rb * RB + 2 * t4, s0 = sg.t0 * (kPageTile / 16);
+    const int first_row = rb * RB + 2 * t4, s0 = sg.t0 * (kTileBlocks);
     // the rows
     uint32_t qf[PIECES][NR][KK][2];
     float qs[NR][2];                                             // a row's factor: scale in bits (capped scores: 1), times 2^-the raise of its queries
@@ -455,6 +434,7 @@ __global__ void __launch_bounds__(kFinishThreads, 8) attend_pages_finish(const _
 #pragma unroll
   for (int e = 0; e < DL; ++e) acc[e] = 0.f;
   auto join = [&](float2 st, const float (&x)[DL], float ref) {
+    if (st.x == -INFINITY && st.y == 0.f) return;                  // (may not have been written)
     const float w = fast_exp2(st.x - ref);
     L = fmaf(w, st.y, L);
 #pragma unroll

@@ -1,17 +1,15 @@
 // Attention of new tokens over a paged cache in 8 bits, what its kernels share: how the work is cut and partial results.
 //
 // An item is (sequence b, KV head g, block of up to RB rows) over the sequence's keys, lengths[b] old ones and count[b] new ones; row r =
-// i G + h is new token i and head h of the group.  Items follow one another, sequence after sequence; their tiles of 64 keys, behind `over`
+// i G + h is new token i and head h of the group.  Items follow one another, sequence after sequence; their tiles (of 64 keys, or 128), behind `over`
 // places for what an item costs beside them, form one sequence of W places, of which C CTAs take runs that differ by one place at
-// most.  What a CTA has of an item it leaves as a partial in slot item + CTA (no other pair has it), merged in that order by a second
-// launch: results do not depend on timing.
+// most.  What a CTA has of an item it leaves as one partial, or two, from slot (item + CTA) times that on (no other pair has them), merged
+// in that order by a second launch: results do not depend on timing.
 #pragma once
 
 #include "pages.cuh"
 
 namespace skv {
-
-constexpr int kPageTile = 64, kPageTileShift = 6;                // keys of a place
 
 struct AttendPagesArgs {
   PagesView c;
@@ -26,16 +24,40 @@ struct AttendPagesArgs {
   int2* item_parts;                                             // [item] its first partial's slot, and how many it has
   float2* part_stat;                                            // [slot][RB] reference (bits) and sum
   float* part_out;                                              // [slot][RB][d]
-  int ctas, least, over;
+  int ctas, least, over, tile_shift;
 };
 
-// Rows of a block, CTAs that run at once.
-struct PagesPlan { int rb, ctas; };
+// Rows of a block, CTAs that run at once, log2 of a tile's keys, partials that a CTA leaves of an item.
+struct PagesPlan { int rb, ctas, tile_shift, parts; };
 
 cudaError_t launch_attend_pages(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
+cudaError_t launch_attend_pages_tc(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
 cudaError_t launch_attend_pages_finish(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
 
 #ifdef __CUDACC__
+
+constexpr float kRaise = 7.f;          // weights are up to 2^(kRaise + kSlack): fp16 keeps those down to 2^-31 of the largest
+constexpr float kNothing = -3.4e38f;   // reference of a row that has seen nothing
+
+// Codes of a word's lower and upper half as two fp16 each.
+__device__ __forceinline__ uint32_t half_lo(uint32_t w) {
+  uint32_t x;
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %1;\ncvt.rn.f16x2.e4m3x2 %0, a;\n}" : "=r"(x) : "r"(w));
+  return x;
+}
+__device__ __forceinline__ uint32_t half_hi(uint32_t w) {
+  uint32_t x;
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %1;\ncvt.rn.f16x2.e4m3x2 %0, b;\n}" : "=r"(x) : "r"(w));
+  return x;
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// A word's bytes that are NaN codes, as 0x80 of each.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ float exp2i(int e) { return __int_as_float(min(max(127 + e, 1), 254) << 23); }   // within fp32's normal numbers
 
 // Keys of sequence b, old ones and new ones; 0: nothing of it is looked at.
 __device__ __forceinline__ int page_keys(const AttendPagesArgs& a, int b) {
@@ -44,7 +66,7 @@ __device__ __forceinline__ int page_keys(const AttendPagesArgs& a, int b) {
   if (count < 0) tell_invalid(a.c);
   return count <= 0 ? 0 : n + count;
 }
-__device__ __forceinline__ int page_places(int keys, int over) { return keys == 0 ? 0 : ((keys + kPageTile - 1) >> kPageTileShift) + over; }
+__device__ __forceinline__ int page_tiles(const AttendPagesArgs& a, int keys) { return (keys + (1 << a.tile_shift) - 1) >> a.tile_shift; }
 
 // A CTA's run of places and where it begins: sequence, its keys, places of one item before it.
 struct PageRun { int lo, hi, b, before, keys; Shares all; };
@@ -53,7 +75,7 @@ __device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a) {
   int total = 0, keys = 0, places = 0, incl = 0;
   auto sweep = [&](int b0) {
     keys = b0 + lane < a.c.batch ? page_keys(a, b0 + lane) : 0;
-    places = incl = page_places(keys, a.over);
+    places = incl = keys == 0 ? 0 : page_tiles(a, keys) + a.over;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int t = __shfl_up_sync(0xffffffffu, incl, o);
@@ -97,13 +119,13 @@ __device__ __forceinline__ void next_segment(PageSegment& s, const AttendPagesAr
     s.nth = 0;
     do ++s.b;
     while ((s.keys = page_keys(a, s.b)) == 0 && s.b < a.c.batch - 1);
-    s.tiles = (s.keys + kPageTile - 1) >> kPageTileShift;
+    s.tiles = page_tiles(a, s.keys);
   }
   s.t1 = min(s.tiles, s.hi - s.at - a.over);
 }
 __device__ __forceinline__ PageSegment first_segment(const AttendPagesArgs& a, const PageRun& w) {
   const int items = a.c.n_kv * a.blocks;
-  PageSegment s{w.b, 0, 0, 0, w.keys, (w.keys + kPageTile - 1) >> kPageTileShift, w.before * items, w.hi};
+  PageSegment s{w.b, 0, 0, 0, w.keys, page_tiles(a, w.keys), w.before * items, w.hi};
   if (w.lo >= w.hi) return s;
   const int each = s.tiles + a.over;
   s.nth = (w.lo - s.at) / each;

@@ -21,76 +21,12 @@
 // meanwhile.
 #include <algorithm>
 
-#include "attend.cuh"
+#include "attend_tc.cuh"
 
 namespace skv {
 namespace {
 
-constexpr int kTile = 128, kThreads = 384;
-
-// An N-major operand of 64-element blocks of 128-byte rows (128-byte swizzle): blocks kTile rows apart, 8-row groups 1024 bytes.
-__device__ __forceinline__ uint64_t smem_desc_n(uint32_t addr) {
-  return smem_desc(addr) & ~(0x3fffull << 16) | (uint64_t)((kTile * 128) >> 4) << 16;
-}
-constexpr uint32_t kTransposeB = 1u << 16;
-// Products that a whole warp comes by and one lane (lead) issues: without a branch for it the operands can stay uniform.  Descriptors
-// by their lower words; hi: the upper word, the same for all of an operand's.
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate, uint32_t lead) {
-  asm volatile(
-      "{\n.reg .pred p, q;\n.reg .b64 da, db;\nsetp.ne.b32 q, %6, 0;\nsetp.ne.b32 p, %5, 0;\nmov.b64 da, {%1, %3};\nmov.b64 db, {%2, %3};\n"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n}"
-      ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(lead) : "memory");
-}
-// a in tensor memory
-__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate, uint32_t lead) {
-  asm volatile(
-      "{\n.reg .pred p, q;\n.reg .b64 db;\nsetp.ne.b32 q, %6, 0;\nsetp.ne.b32 p, %5, 0;\nmov.b64 db, {%2, %3};\n"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}"
-      ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(lead) : "memory");
-}
-__device__ __forceinline__ void commit_by(uint32_t lead, uint32_t bar) {
-  asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}"
-               ::"r"(bar), "r"(lead) : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
-                 "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
-}
-// The load of 32 columns and its wait apart: several loads travel together.
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-               "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
-                 "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
-                 "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]),
-                 "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]),
-                 "=f"(v[30]), "=f"(v[31])
-               : "r"(taddr) : "memory");
-}
-// (registers that a load in flight writes are operands of a wait, so that no use of them comes before it)
-__device__ __forceinline__ void tmem_landed(float* v) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
-                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
-                 "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]),
-                 "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]),
-                 "+f"(v[30]), "+f"(v[31])
-               :: "memory");
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&f)[32]) {
-  uint32_t lo[16], hi[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) { lo[i] = __float_as_uint(f[i]); hi[i] = __float_as_uint(f[16 + i]); }
-  tmem_st16(taddr, lo);
-  tmem_st16(taddr + 16, hi);
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+constexpr int kThreads = 384;
 
 // MT: halves of 128 rows in a block.
 template <int D, int MT, bool OPT>
