@@ -1,14 +1,14 @@
 // Attention of new tokens over a paged cache in 8 bits where a KV head has more than 16 rows.
 //
-// S = K Q^T's rows and O += P V on the tensor cores (tcgen05): tiles of 128 rows x 128 keys, lane = row.  Two streams, the even and the odd
-// tiles of a segment, alternate, so that one's products run beside the other's exponentials; each leaves a partial.  K and V come as codes:
-// a stream's four producing warps copy them lane by lane (cp.async, two units ahead), widen them to fp16, which is exact, and lay
-// them out as the products' operands; a code is widened once for all rows.  Scales stay out of the operands: in bits, a score is
-// s f 2^e_k and its weight in O 2^(s f 2^e_k + e_v - m), one multiply-add with two numbers for each 16 keys.  References, weights and queries
-// as in attend_pages.cu.
+// S = Q K^T and O += P V on the tensor cores (tcgen05): tiles of 128 rows x 64 keys, lane = row.  Two streams, the even and the odd
+// tiles of a segment, alternate; each has two places for scores, so that the next tile's are there when a tile's exponentials are done, and
+// leaves a partial of its own.  K and V come as codes: a stream's four producing warps copy them lane by lane (cp.async, two tiles
+// ahead), widen them to fp16, which is exact, and lay them out as the products' operands; a code is widened once for all rows.  Scales stay
+// out of the operands: in bits, a score is s f 2^e_k and its weight in O 2^(s f 2^e_k + e_v - m), one multiply-add with two numbers for each 16
+// keys.  References, weights and queries as in attend_pages.cu; a tile's weights are worked out against the reference as it is, and again
+// where that is outgrown.
 //
-// Warps: 0-3 and 4-7 bring a segment's rows (0-3) and are the streams' softmax; 8-11 and 12-15 produce; 16 and 17 issue the streams' products.
-// A tile's scores are read twice, for their maximum and for the exponentials: 18 warps have 112 registers.
+// Warps: 0-3 and 4-7 bring a segment's rows and are the streams' softmax; 8-11 and 12-15 produce; 16 and 17 issue the streams' products.
 #include <algorithm>
 
 #include "attend_pages.cuh"
@@ -17,7 +17,10 @@
 namespace skv {
 namespace {
 
-constexpr int kThreads = 576, kBlocks = kTile / kBlockSlots;     // blocks of slots of a tile
+constexpr int kThreads = 576, kRows = kTile, kKeys = 64, kBlocks = kKeys / kBlockSlots;   // of a tile: rows, keys, blocks of slots
+
+// An N-major operand of 64-element blocks of 128-byte rows (128-byte swizzle): blocks kKeys rows apart, 8-row groups 1024 bytes.
+__device__ __forceinline__ uint64_t keys_desc_n(uint32_t addr) { return smem_desc(addr) & ~(0x3fffull << 16) | (uint64_t)((kKeys * 128) >> 4) << 16; }
 
 __device__ __forceinline__ void copy16(uint32_t to, const char* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -43,43 +46,48 @@ __device__ __forceinline__ float greatest16(const float* v) {
 
 template <int D>
 struct PagesTc {
-  static constexpr int kUnit = kTile * D * 2, kRaw = kTile * D;   // K or V of a tile, as operands and as codes
-  static constexpr int kOps = kUnit, kRaws = kOps + 4 * kUnit, kInfo = kRaws + 4 * kRaw, kQs = kInfo + 4 * kBlocks * 16, kBars = kQs + kTile * 4;
-  static constexpr int kSmem = kBars + 256 + 1024;
+  static constexpr int kUnit = kKeys * D * 2, kRaw = kKeys * D;   // K or V of a tile, as operands and as codes
+  // the rows, then for each stream two tiles as operands, two as codes; a tile's numbers for every 16 keys, four tiles a stream
+  static constexpr int kOps = kRows * D * 2, kRaws = kOps + 8 * kUnit, kInfo = kRaws + 8 * kRaw, kQs = kInfo + 8 * kBlocks * 16, kBars = kQs + 2 * kRows * 4;
+  static constexpr int kSmem = kBars + 304 + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
 template <int D, bool CAP>
 __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_constant__ AttendPagesArgs a) {
   using S = PagesTc<D>;
-  constexpr int RB = kTile;
+  constexpr int RB = kRows;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
-  // (stream s, K or V: operands, codes; a job's numbers for every 16 keys: K's scale, exponent of V's, its inverse)
-  auto operand = [&](int s, int v) { return (uint32_t)(S::kOps + (2 * s + v) * S::kUnit); };
-  float4* const info = (float4*)(sm + S::kInfo);                 // [stream][job mod 2][block]
-  float* const qs = (float*)(sm + S::kQs);                       // a row's factor: scale in bits (capped scores: 1) times 2^-the raise of its queries
+  // stream s, K or V, job mod 2
+  auto operand = [&](int s, int v, int p) { return (uint32_t)(S::kOps + (4 * s + 2 * v + p) * S::kUnit); };
+  float4* const info = (float4*)(sm + S::kInfo);                 // [stream][job mod 4][block]: K's scale, exponent of V's, its inverse
+  float* const tops = (float*)(sm + S::kQs);                     // [half of a head][row]: the largest element of a row
   const uint32_t bars = base + S::kBars;
-  auto full = [&](int s, int v) { return bars + 8 * (2 * s + v); };
-  auto empty = [&](int s, int v) { return bars + 32 + 8 * (2 * s + v); };
-  auto s_full = [&](int s) { return bars + 64 + 8 * s; };
-  auto p_ready = [&](int s) { return bars + 80 + 8 * s; };
-  auto o_done = [&](int s) { return bars + 96 + 8 * s; };
-  auto o_free = [&](int s) { return bars + 112 + 8 * s; };
-  auto drained = [&](int s) { return bars + 128 + 8 * s; };
-  const uint32_t q_full = bars + 144, q_empty = bars + 152;
-  volatile int* const words = (volatile int*)(sm + S::kBars + 160);
+  auto full = [&](int s, int v, int p) { return bars + 8 * (4 * s + 2 * v + p); };
+  auto empty = [&](int s, int v, int p) { return bars + 64 + 8 * (4 * s + 2 * v + p); };
+  auto s_full = [&](int s, int p) { return bars + 128 + 8 * (2 * s + p); };
+  auto p_ready = [&](int s, int p) { return bars + 160 + 8 * (2 * s + p); };
+  auto o_done = [&](int s, int p) { return bars + 192 + 8 * (2 * s + p); };
+  auto o_free = [&](int s) { return bars + 224 + 8 * s; };
+  auto drained = [&](int s) { return bars + 240 + 8 * s; };
+  const uint32_t q_full = bars + 256, q_empty = bars + 264, top_full = bars + 272;
+  volatile int* const words = (volatile int*)(sm + S::kBars + 280);
   volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v[s]: in a tile of stream s some new token's V was NaN
   volatile uint32_t* const tmem_at = (volatile uint32_t*)words + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, token = a.c.s_token;
   pdl_trigger();
   if (tid == 0) {
     for (int s = 0; s < 2; ++s) {
-      for (int v = 0; v < 2; ++v) { mbar_init(full(s, v), 128); mbar_init(empty(s, v), 1); }
-      mbar_init(s_full(s), 1); mbar_init(p_ready(s), 4); mbar_init(o_done(s), 1); mbar_init(o_free(s), 4); mbar_init(drained(s), 1);
+      for (int p = 0; p < 2; ++p) {
+        for (int v = 0; v < 2; ++v) { mbar_init(full(s, v, p), 128); mbar_init(empty(s, v, p), 1); }
+        mbar_init(s_full(s, p), 1); mbar_init(p_ready(s, p), 4); mbar_init(o_done(s, p), 1);
+      }
+      mbar_init(o_free(s), 4); mbar_init(drained(s), 1);
     }
-    mbar_init(q_full, 128);
+    mbar_init(q_full, 256);
+    mbar_init(top_full, 256);
     mbar_init(q_empty, 10);                                        // softmax's warps, products' warps
     *abort_flag = 0;
     odd_v[0] = odd_v[1] = 0;
@@ -104,13 +112,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
   const int sh4 = a.c.page_shift - kBlockShift, per_page = 1 << sh4;
 
   if (work && warp >= 16) {
-    // Products of stream s, each job's scores made after the outputs of the job before.
+    // Products of stream s: a job's outputs, then the scores of the job after next, which take its place.
     const int s = warp - 16;
     const uint32_t lead = lane == 0;
     constexpr uint32_t kF16 = 1u << 4;                             // fp16 operands, fp32 results
-    const uint32_t idesc_s = kF16 | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24 | (a.scale2 < 0.f ? 1u << 13 : 0u);
-    constexpr uint32_t idesc_o = kF16 | (uint32_t)(D >> 3) << 17 | (uint32_t)(kTile >> 4) << 24 | kTransposeB;
-    const uint64_t q_desc = smem_desc(base), k_desc = smem_desc(base + operand(s, 0)), v_desc = smem_desc_n(base + operand(s, 1));
+    const uint32_t idesc_s = kF16 | (uint32_t)(kKeys >> 3) << 17 | (uint32_t)(kRows >> 4) << 24 | (a.scale2 < 0.f ? 1u << 13 : 0u);
+    constexpr uint32_t idesc_o = kF16 | (uint32_t)(D >> 3) << 17 | (uint32_t)(kRows >> 4) << 24 | kTransposeB;
+    const uint64_t q_desc = smem_desc(base), k_desc = smem_desc(base + operand(s, 0, 0)), v_desc = keys_desc_n(base + operand(s, 1, 0));
     const uint32_t q_lo = (uint32_t)q_desc, k_lo = (uint32_t)k_desc, v_lo = (uint32_t)v_desc, hi_k = (uint32_t)(q_desc >> 32), hi_v = (uint32_t)(v_desc >> 32);
     const uint32_t s_at = tmem + s * 128, o_at = tmem + 256 + s * 128;
     int seg = 0, done = 0, used = 0;                               // segments, jobs, segments with jobs
@@ -118,29 +126,33 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
     do {
       const int jobs = jobs_of(sg, s);
       auto scores = [&](int job) {
-        if (!(ok = wait(full(s, 0), job & 1))) return;
+        const int p = job & 1;
+        if (!(ok = wait(full(s, 0, p), job >> 1 & 1))) return;
         tc_fence_after();
+        const uint32_t kd = k_lo + (p * S::kUnit >> 4);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          mma_ss(s_at, q_lo + (((kk / 4) * RB * 128 + (kk % 4) * 32) >> 4), k_lo + (((kk / 4) * kTile * 128 + (kk % 4) * 32) >> 4), hi_k, idesc_s, kk > 0, lead);
-        commit_by(lead, s_full(s));
-        commit_by(lead, empty(s, 0));
+          mma_ss(s_at + p * 64, q_lo + (((kk / 4) * RB * 128 + (kk % 4) * 32) >> 4), kd + (((kk / 4) * kKeys * 128 + (kk % 4) * 32) >> 4), hi_k, idesc_s, kk > 0, lead);
+        commit_by(lead, s_full(s, p));
+        commit_by(lead, empty(s, 0, p));
       };
       // (a stream without a tile in the segment says as well that it came by: else its wait might be for a phase that is gone)
       if ((ok = wait(q_full, seg & 1)) && lead) mbar_arrive(q_empty);
       if (ok && jobs > 0) scores(done);
+      if (ok && jobs > 1) scores(done + 1);
 #pragma unroll 1
-      for (int k = 0; k < jobs && ok; ++k) {
-        if (!(ok = wait(full(s, 1), done & 1))) break;
+      for (int k = 0; k < jobs && ok; ++k, ++done) {
+        const int p = done & 1;
+        if (!(ok = wait(full(s, 1, p), done >> 1 & 1))) break;
         if (k == 0 && used++ > 0 && !(ok = wait(o_free(s), used & 1))) break;
-        if (!(ok = wait(p_ready(s), done & 1))) break;
+        if (!(ok = wait(p_ready(s, p), done >> 1 & 1))) break;
         tc_fence_after();
+        const uint32_t vd = v_lo + (p * S::kUnit >> 4);
 #pragma unroll
-        for (int kk = 0; kk < kTile / 16; ++kk) mma_ts(o_at, s_at + kk * 8, v_lo + ((kk * 16 * 128) >> 4), hi_v, idesc_o, k > 0 || kk > 0, lead);
-        commit_by(lead, o_done(s));
-        commit_by(lead, empty(s, 1));
-        ++done;
-        if (k + 1 < jobs) scores(done);
+        for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts(o_at, s_at + p * 64 + kk * 8, vd + ((kk * 16 * 128) >> 4), hi_v, idesc_o, k > 0 || kk > 0, lead);
+        commit_by(lead, o_done(s, p));
+        commit_by(lead, empty(s, 1, p));
+        if (k + 2 < jobs) scores(done + 2);
       }
       ++seg;
       next_segment(sg, a);
@@ -148,133 +160,122 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
     commit_by(lead, drained(s));
     if (!mbar_drain(drained(s), 0, abort_flag)) *abort_flag = 2;
   } else if (work && warp >= 8) {
-    // Producers of stream s: a warp has two blocks of 16 keys of every tile.  Lane i knows page and scales of block i mod 2 of the (i / 2)-th of
-    // the next 16 jobs, and of the 16 behind them: bytes of K's and V's scale, and above them whether there is nothing (a block behind
-    // the last key, or a page that is none).
-    constexpr int NI = D / 32;                                     // 16-byte pieces of a block that a lane has
+    // Producers of stream s: a warp has 16 keys of every tile.  Lane i knows page and scales of the i-th of 32 jobs, and in good time of
+    // the 32 behind them: page -1: nothing there (behind the last key, or a page that is none); bytes of K's and V's scale.
+    constexpr int NI = D / 32;                                     // 16-byte pieces that a lane has of 16 keys
     const int s = (warp - 8) / 4, pw = warp & 3;
     const int c = D == 128 ? (lane & 3) | (lane & 8) >> 1 : lane & 3, row = D == 128 ? (lane >> 2 & 1) | lane >> 4 << 1 : lane >> 2;   // of piece 0
-    constexpr int kRows = 16 / NI;                                 // rows from piece to piece
-    const uint32_t raw = base + S::kRaws + s * 2 * S::kRaw + pw * (2 * NI * 512) + lane * 16;
-    int j = 0, jobs = 0, page = 0, page_after = 0;
-    unsigned about = 0, about_after = 0;
+    constexpr int kStep = 16 / NI;                                 // rows from piece to piece
+    const uint32_t raw = base + S::kRaws + s * 4 * S::kRaw + pw * (NI * 512) + lane * 16;
+    int j = -1, jobs = 0, page = -1, page_after = -1, g = 0, n_old = 0;
+    unsigned scales = 0, scales_after = 0;
     const int* table = nullptr;
     const char *k0 = nullptr, *v0 = nullptr;
-    int g = 0, n_old = 0;
     auto look = [&](int job, unsigned& what) {
-      const int t = sg.t0 + s + 2 * job, step = t * kBlocks + 2 * pw + (lane & 1);
-      int p = 0;
-      what = 1u << 16;
+      const int t = sg.t0 + s + 2 * job, step = t * kBlocks + pw;
+      int p = -1;
+      what = 0;
       if (t < sg.t1 && step * 16 < sg.keys) {
         p = table[step >> sh4];
         if ((unsigned)p >= (unsigned)a.c.pages) {
-          p = 0;
+          p = -1;
           tell_invalid(a.c);
-        } else {
-          const unsigned at = (((unsigned)p * a.c.n_kv + g) << sh4) + (step & (per_page - 1));
-          what = a.c.k_scales[at] | (unsigned)a.c.v_scales[at] << 8;
         }
+        const unsigned at = (((unsigned)max(p, 0) * a.c.n_kv + g) << sh4) + (step & (per_page - 1));
+        what = a.c.k_scales[at] | (unsigned)a.c.v_scales[at] << 8;
       }
       return p;
     };
-    // A job: its tile, its sequence's keys and old ones among them, pages and scales of this warp's blocks.
-    struct Job { int t, keys, n_old, page[2]; unsigned what[2]; const char *k, *v; bool live; };
-    auto here = [&]() {
-      Job x{sg.t0 + s + 2 * j, sg.keys, n_old, {}, {}, k0, v0, sg.t1 > 0};
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        x.page[e] = __shfl_sync(0xffffffffu, page, 2 * (j & 15) + e);
-        x.what[e] = __shfl_sync(0xffffffffu, about, 2 * (j & 15) + e);
-      }
-      return x;
-    };
-    auto enter = [&]() {                                           // the first segment from here on that has a job for this stream
-      while (sg.t1 && jobs_of(sg, s) == 0) next_segment(sg, a);
-      j = 0;
-      if (sg.t1 == 0) return;
-      jobs = jobs_of(sg, s);
-      g = quotient(sg.nth, a.by_blocks);
-      n_old = a.c.lengths[sg.b];
-      table = (const int*)((const char*)a.c.table + sg.b * a.c.s_table);
-      k0 = a.c.k + g * a.c.s_head + (long long)row * token + c * 16;
-      v0 = a.c.v + g * a.c.s_head + (long long)row * token + c * 16;
-      page = look(lane >> 1, about);
-      page_after = look(16 + (lane >> 1), about_after);
-    };
+    // A job: its tile (-1: there is none), its sequence's keys and old ones among them, page and scales of this warp's part.
+    struct Job { int t, keys, n_old, page; unsigned scales; };
     auto next = [&]() {
-      if (++j == jobs) {
-        next_segment(sg, a);
-        enter();
-      } else if ((j & 15) == 0) {
-        page = page_after;
-        about = about_after;
-        page_after = look(j + 16 + (lane >> 1), about_after);
-      }
-    };
-    auto copy = [&](const Job& x, int v) {
-      if (x.live)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (x.what[e] >> 16) continue;
-          const int block = (x.t * kBlocks + 2 * pw + e) & (per_page - 1);
-          const char* const from = (v ? x.v : x.k) + (long long)((unsigned long long)(unsigned)x.page[e] * (unsigned)a.c.s_page) + block * (token << kBlockShift);
-#pragma unroll
-          for (int i = 0; i < NI; ++i) copy16(raw + v * S::kRaw + (e * NI + i) * 512, from + i * kRows * token);
+      if (sg.t1 && ++j == jobs) {
+        if (j > 0) next_segment(sg, a);
+        while (sg.t1 && jobs_of(sg, s) == 0) next_segment(sg, a);
+        if (sg.t1) {
+          j = 0;
+          jobs = jobs_of(sg, s);
+          g = quotient(sg.nth, a.by_blocks);
+          n_old = a.c.lengths[sg.b];
+          table = (const int*)((const char*)a.c.table + sg.b * a.c.s_table);
+          k0 = a.c.k + g * a.c.s_head + (long long)row * token + c * 16;
+          v0 = a.c.v + g * a.c.s_head + (long long)row * token + c * 16;
+          page = look(lane, scales);
         }
+      } else if ((j & 31) == 0) {
+        page = page_after;
+        scales = scales_after;
+      } else if ((j & 31) == 4 && jobs > (j | 31)) {
+        page_after = look((j | 31) + 1 + lane, scales_after);
+      }
+      const int p = __shfl_sync(0xffffffffu, page, j & 31);
+      const unsigned what = __shfl_sync(0xffffffffu, scales, j & 31);
+      return sg.t1 ? Job{sg.t0 + s + 2 * j, sg.keys, n_old, p, what} : Job{-1, 0, 0, -1, 0};
+    };
+    // (called while the job is the newest: k0 and v0 are its sequence's)
+    auto copy = [&](const Job& x, int place, int v) {
+      if (x.page >= 0) {
+        const char* const from = (v ? v0 : k0) + (long long)((unsigned long long)(unsigned)x.page * (unsigned)a.c.s_page) + ((x.t * kBlocks + pw) & (per_page - 1)) * (token << kBlockShift);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) copy16(raw + (2 * place + v) * S::kRaw + i * 512, from + i * kStep * token);
+      }
       copies_end();
     };
-    enter();
-    Job now = here();
-    copy(now, 0);
-    copy(now, 1);
+    Job now = next();
+    copy(now, 0, 0);
+    copy(now, 0, 1);
+    Job then = next();
+    copy(then, 1, 0);
+    copy(then, 1, 1);
     bool ok = true;
 #pragma unroll 1
-    for (int done = 0; now.live && ok; ++done) {
-      next();
-      const Job then = here();
-      const int key0 = now.t * kTile + pw * 32 + row;
-      const bool tail = (now.t + 1) * kTile > now.n_old;
+    for (int done = 0; now.t >= 0 && ok; ++done) {
+      const int p = done & 1;
+      const Job later = next();
+      const bool tail = (now.t + 1) * kKeys > now.n_old;
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
-        copies_landed<1>();
-        if (done > 0 && !(ok = wait_long(empty(s, v), (done - 1) & 1))) break;
+        copies_landed<3>();
+        if (done > 1 && !(ok = wait_long(empty(s, v, p), (done >> 1) - 1 & 1))) break;
+        uint4 w[NI];
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int i = 0; i < NI; ++i) w[i] = now.page >= 0 ? shared16(raw + (2 * p + v) * S::kRaw + i * 512) : make_uint4(0u, 0u, 0u, 0u);
+        if (v == 1 && tail) {
+          // What the slots behind the last key hold reaches nobody; NaN of a new token is added, at the end, to the rows that see it.
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
-            uint4 w = make_uint4(0u, 0u, 0u, 0u);
-            if (!(now.what[e] >> 16)) w = shared16(raw + v * S::kRaw + (e * NI + i) * 512);
-            if (v == 1 && tail) {
-              // What the slots behind the last key hold reaches nobody; NaN of a new token is added, at the end, to the rows that see it.
-              const int key = key0 + e * 16 + i * kRows;
-              if (key >= now.keys) w = make_uint4(0u, 0u, 0u, 0u);
-              if (key >= now.n_old && (nan_bytes(w.x) | nan_bytes(w.y) | nan_bytes(w.z) | nan_bytes(w.w))) {
-                odd_v[s] = 1;
-                w.x &= ~((nan_bytes(w.x) >> 7) * 0xffu); w.y &= ~((nan_bytes(w.y) >> 7) * 0xffu);
-                w.z &= ~((nan_bytes(w.z) >> 7) * 0xffu); w.w &= ~((nan_bytes(w.w) >> 7) * 0xffu);
-              }
+            const int key = now.t * kKeys + pw * 16 + row + i * kStep;
+            if (key >= now.keys) w[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (key >= now.n_old && (nan_bytes(w[i].x) | nan_bytes(w[i].y) | nan_bytes(w[i].z) | nan_bytes(w[i].w))) {
+              odd_v[s] = 1;
+              w[i].x &= ~((nan_bytes(w[i].x) >> 7) * 0xffu); w[i].y &= ~((nan_bytes(w[i].y) >> 7) * 0xffu);
+              w[i].z &= ~((nan_bytes(w[i].z) >> 7) * 0xffu); w[i].w &= ~((nan_bytes(w[i].w) >> 7) * 0xffu);
             }
-            const uint32_t to = base + operand(s, v);
-            const int r = pw * 32 + e * 16 + row + i * kRows;
-            put16(to + tile_at<kTile>(r, 2 * c), half_lo(w.x), half_hi(w.x), half_lo(w.y), half_hi(w.y));
-            put16(to + tile_at<kTile>(r, 2 * c + 1), half_lo(w.z), half_hi(w.z), half_lo(w.w), half_hi(w.w));
           }
-        if (v == 0 && lane < 2) {
-          // (this job's softmax is behind the one that had these numbers' place: its scores were made after that one's outputs)
-          const unsigned what = lane ? now.what[1] : now.what[0];
-          const int ke = what & 0xff, ve = what >> 8 & 0xff;
-          info[(s * 2 + (done & 1)) * kBlocks + 2 * pw + lane] = what >> 16 ? make_float4(1.f, -INFINITY, 0.f, 0.f) : make_float4(exp2i(ke - 127), (float)(ve - 127), exp2i(127 - ve), 0.f);
         }
-        copy(then, v);
+        const uint32_t to = base + operand(s, v, p);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int r = pw * 16 + row + i * kStep;
+          put16(to + tile_at<kKeys>(r, 2 * c), half_lo(w[i].x), half_hi(w[i].x), half_lo(w[i].y), half_hi(w[i].y));
+          put16(to + tile_at<kKeys>(r, 2 * c + 1), half_lo(w[i].z), half_hi(w[i].z), half_lo(w[i].w), half_hi(w[i].w));
+        }
+        if (v == 0 && lane == 0) {
+          // (the job four before, which had this place, is done: the scores of the one two before were made behind its outputs)
+          const int ke = now.scales & 0xff, ve = now.scales >> 8;
+          info[(s * 4 + (done & 3)) * kBlocks + pw] = now.page < 0 ? make_float4(1.f, -INFINITY, 0.f, 0.f) : make_float4(exp2i(ke - 127), (float)(ve - 127), exp2i(127 - ve), 0.f);
+        }
+        copy(later, p, v);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(full(s, v));
+        mbar_arrive(full(s, v, p));
       }
       now = then;
+      then = later;
     }
     copies_landed<0>();
   } else if (work) {
     const int s = warp / 4, quarter = warp & 3;
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at0 = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
     const uint64_t cap2 = pack2(a.cap2, a.cap2), inv2 = pack2(fabsf(a.inv_cap), fabsf(a.inv_cap));
     const int row = quarter * 32 + lane;
     int done = 0, seg = 0;
@@ -283,48 +284,59 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
       const int g = quotient(sg.nth, a.by_blocks), rb = sg.nth - g * a.blocks, n_old = a.c.lengths[sg.b];
       const int r = rb * RB + row, tok = quotient(min(r, a.rows - 1), a.by_group), h = min(r, a.rows - 1) - tok * a.group;
       const bool is = r < a.rows, idle = r - lane >= a.rows;       // idle: no row of this warp, which only keeps step
-      if (s == 0) {
-        // the segment's rows, once the products of the segment before have read theirs
-        if (seg > 0 && !(ok = wait(q_empty, (seg - 1) & 1))) break;
-        const char* const q = a.q + sg.b * a.q_batch + tok * a.q_token + (g * a.group + h) * a.q_head;
+      // The segment's rows, once the products of the segment before have read theirs; each stream's warps bring half of the heads' elements.
+      float f = 0.f;                                               // a row's factor: scale in bits (capped scores: 1) times 2^-the raise of its queries
+      {
+        const char* const q = a.q + sg.b * a.q_batch + tok * a.q_token + (g * a.group + h) * a.q_head + s * D;
+        uint4 w[D / 16];
         float top = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < D / 8; ++i) {
-          const uint4 w = is ? *(const uint4*)(q + i * 16) : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        if (!idle)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
-        }
-        const int raise = min(max(13 - ((int)(__float_as_uint(top) >> 23) - 127), -113), 126);
-        const float up = exp2i(raise);
-#pragma unroll 4
-        for (int i = 0; i < D / 8; ++i) {
-          const uint4 w = is ? *(const uint4*)(q + i * 16) : make_uint4(0u, 0u, 0u, 0u);
-          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-          uint32_t y[4];
+          for (int i = 0; i < D / 16; ++i) w[i] = *(const uint4*)(q + i * 16);
+        if (seg > 0 && !(ok = wait(q_empty, (seg - 1) & 1))) break;
+        if (!idle) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = f16x2(__uint_as_float(x[e] << 16) * up, __uint_as_float(x[e] & 0xffff0000u) * up);
-          put16(base + tile_at<RB>(row, i), y[0], y[1], y[2], y[3]);
+          for (int i = 0; i < D / 16; ++i) {
+            const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
+          }
+          tops[s * kRows + row] = top;
         }
-        qs[row] = exp2i(-raise) * (CAP ? 1.f : fabsf(a.scale2));   // (a negative scale negates the product)
+        mbar_arrive(top_full);
+        if (!(ok = wait(top_full, seg & 1))) break;
+        if (!idle) {
+          top = fmaxf(top, tops[(1 - s) * kRows + row]);
+          const int raise = min(max(13 - ((int)(__float_as_uint(top) >> 23) - 127), -113), 126);
+          const float up = exp2i(raise);
+          f = exp2i(-raise) * (CAP ? 1.f : fabsf(a.scale2));       // (a negative scale negates the product)
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+            uint32_t y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = f16x2(__uint_as_float(x[e] << 16) * up, __uint_as_float(x[e] & 0xffff0000u) * up);
+            put16(base + tile_at<RB>(row, s * (D / 16) + i), y[0], y[1], y[2], y[3]);
+          }
+        }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(q_full);
+        ++seg;
       }
-      if (!(ok = wait(q_full, seg & 1))) break;
-      ++seg;
-      const float f = qs[row];
       const int jobs = jobs_of(sg, s), last = n_old + tok;
       float m = kNothing, l = 0.f;
       bool far = false;
 #pragma unroll 1
       for (int k = 0; k < jobs; ++k, ++done) {
-        const int j0 = (sg.t0 + s + 2 * k) * kTile;
-        if (!(ok = wait(s_full(s), done & 1))) break;
+        const int j0 = (sg.t0 + s + 2 * k) * kKeys;
+        const uint32_t s_at = s_at0 + (done & 1) * 64;
+        if (!(ok = wait(s_full(s, done & 1), done >> 1 & 1))) break;
         tc_fence_after();
         if (!idle) {
-          const float4* const in = info + (s * 2 + (done & 1)) * kBlocks;
-          const bool tail = j0 + kTile > n_old + 1;
-          // y of 16 scores, in bits and with V's exponent, less c's; hidden ones minus infinity
+          const float4* const in = info + (s * 4 + (done & 3)) * kBlocks;
+          const bool tail = j0 + kKeys > n_old + 1;
+          const int sees = last - j0;                              // the last column that is seen
+          // y of 16 scores from column col on, in bits and with V's exponent, less c's; hidden ones minus infinity
           auto weigh = [&](const float* v, int col, float fk, float c, float (&y)[16]) {
             if (CAP) {
 #pragma unroll
@@ -340,44 +352,64 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
 #pragma unroll
               for (int e = 0; e < 16; e += 2) unpack2(fma2(pack2(v[e], v[e + 1]), f2, c2), y[e], y[e + 1]);
             }
-            if (tail) {
-              const int sees = last - j0 - col;                    // the columns up to this one
+            if (tail)
 #pragma unroll
-              for (int e = 0; e < 16; ++e) y[e] = e <= sees ? y[e] : -INFINITY;
-            }
+              for (int e = 0; e < 16; ++e) y[e] = col + e <= sees ? y[e] : -INFINITY;
           };
-          float v[2][32], top = -INFINITY;
-          tmem_ld32(s_at, v[0]);
+          uint32_t p[kKeys / 2];
+          float sum = 0.f;
+#pragma unroll 1
+          for (bool again = false;; again = true) {
+            float top = -INFINITY;
+            sum = 0.f;
 #pragma unroll
-          for (int c = 0; c < kTile; c += 32) {
-            float* const x = v[c / 32 & 1];
-            tmem_landed(x);
-            if (c + 32 < kTile) tmem_ld32(s_at + c + 32, v[(c / 32 + 1) & 1]);
+            for (int c = 0; c < kKeys; c += 32) {
+              float x[32];
+              tmem_ld(s_at + c, x);
 #pragma unroll
-            for (int b = 0; b < 32; b += 16) {
-              const float4 n = in[(c + b) / 16];
-              if (tail) {
+              for (int b = 0; b < 32; b += 16) {
+                const float4 n = in[(c + b) / 16];
                 float y[16];
-                weigh(x + b, c + b, f * n.x, n.y, y);
+                weigh(x + b, c + b, f * n.x, n.y - m, y);
                 top = fmaxf(top, greatest16(y));
-              } else {
-                float t = greatest16(x + b) * (f * n.x), u = t;    // (rises with the score)
-                if (CAP) capped2(t, u, cap2, inv2);
-                top = fmaxf(top, t + n.y);
+                // A score and a reference so far from zero that their difference is off by whole bits: no weight is above the largest.
+                if (far && again)
+#pragma unroll
+                  for (int e = 0; e < 16; ++e)
+                    if (y[e] > kRaise + kSlack) y[e] = kRaise + kSlack;
+                uint64_t part = pack2(0.f, 0.f);
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                  const uint64_t w = exp2_sfu2(pack2(y[e], y[e + 1]));
+                  float p0, p1;
+                  unpack2(w, p0, p1);
+                  part = add2(part, w);
+                  p[(c + b + e) / 2] = f16x2(p0, p1);
+                }
+                float s0, s1;
+                unpack2(part, s0, s1);
+                sum = fmaf(s0 + s1, n.z, sum);
               }
             }
-          }
-          // the first of the scores again, while the reference is looked at
-          tmem_ld32(s_at, v[0]);
-          const bool grown = top > m + (kRaise + kSlack);
-          if (__any_sync(0xffffffffu, grown)) {
+            const bool grown = top > kRaise + kSlack;
+            if (again || !__any_sync(0xffffffffu, grown)) break;
+            // the reference follows: the largest score, without the one as it was
+            top = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < kKeys; c += 16) {
+              float x[16], y[16];
+              tmem_ld_issue<16>(s_at + c, x);
+              tmem_ld_wait(x);
+              const float4 n = in[c / 16];
+              weigh(x, c, f * n.x, n.y, y);
+              top = fmaxf(top, greatest16(y));
+            }
             const float to = grown ? fmaxf(ceilf(top) - kRaise, m) : m, by = fast_exp2(m - to);
             m = to;
             l *= by;
             far = __any_sync(0xffffffffu, is && m != kNothing && fabsf(m) > 0x1p20f);
-            tmem_landed(v[0]);
             if (k > 0) {
-              if (!(ok = wait(o_done(s), (done - 1) & 1))) break;
+              if (!(ok = wait(o_done(s, (done - 1) & 1), (done - 1) >> 1 & 1))) break;
               tc_fence_after();
 #pragma unroll 1
               for (int c = 0; c < D; c += 16) {
@@ -392,41 +424,20 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
               tmem_st_wait();
             }
           }
+          if (!ok) break;
+          l += sum;
+          {
+            uint32_t lo[16], hi[16];
 #pragma unroll
-          for (int c = 0; c < kTile; c += 32) {
-            float* const x = v[c / 32 & 1];
-            uint32_t p[16];
-            tmem_landed(x);
-            if (c + 32 < kTile) tmem_ld32(s_at + c + 32, v[(c / 32 + 1) & 1]);
-#pragma unroll
-            for (int b = 0; b < 32; b += 16) {
-              const float4 n = in[(c + b) / 16];
-              float y[16];
-              weigh(x + b, c + b, f * n.x, n.y - m, y);
-              if (far)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                  if (y[e] > kRaise + kSlack) y[e] = kRaise + kSlack;
-              uint64_t sum = pack2(0.f, 0.f);
-#pragma unroll
-              for (int e = 0; e < 16; e += 2) {
-                const uint64_t w = exp2_sfu2(pack2(y[e], y[e + 1]));
-                float p0, p1;
-                unpack2(w, p0, p1);
-                sum = add2(sum, w);
-                p[(b + e) / 2] = f16x2(p0, p1);
-              }
-              float s0, s1;
-              unpack2(sum, s0, s1);
-              l = fmaf(s0 + s1, n.z, l);
-            }
-            tmem_st16(s_at + c / 2, p);                            // (over scores that have been read)
+            for (int e = 0; e < 16; ++e) { lo[e] = p[e]; hi[e] = p[16 + e]; }
+            tmem_st16(s_at, lo);                                   // (over the scores)
+            tmem_st16(s_at + 16, hi);
           }
           tmem_st_wait();
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready(s));
+        if (lane == 0) mbar_arrive(p_ready(s, done & 1));
       }
       if (!ok) break;
       if (lane == 0) mbar_arrive(q_empty);                         // (this stream's scores are all there)
@@ -438,10 +449,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
       const size_t at = (size_t)slot * RB + row;
       if (is) a.part_stat[at] = make_float2(m == kNothing ? -INFINITY : m, l);
       if (jobs > 0) {
-        if (!(ok = wait(o_done(s), (done - 1) & 1))) break;
+        if (!(ok = wait(o_done(s, (done - 1) & 1), (done - 1) >> 1 & 1))) break;
         tc_fence_after();
         if (!idle) {
-          const bool odd = odd_v[s] && sg.t1 * kTile > n_old;
+          const bool odd = odd_v[s] && sg.t1 * kKeys > n_old;
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
             float v[32];
@@ -449,9 +460,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
             if (odd && is) {
 #pragma unroll 1
               for (int i = n_old; i <= last && i < sg.keys; ++i) {
-                const int p = ((const int*)((const char*)a.c.table + sg.b * a.c.s_table))[i >> a.c.page_shift];
-                if ((unsigned)p >= (unsigned)a.c.pages) continue;
-                const uint32_t* const from = (const uint32_t*)(a.c.v + p * a.c.s_page + g * a.c.s_head + (long long)(i & ((1 << a.c.page_shift) - 1)) * token + c);
+                const int pg = ((const int*)((const char*)a.c.table + sg.b * a.c.s_table))[i >> a.c.page_shift];
+                if ((unsigned)pg >= (unsigned)a.c.pages) continue;
+                const uint32_t* const from = (const uint32_t*)(a.c.v + pg * a.c.s_page + g * a.c.s_head + (long long)(i & ((1 << a.c.page_shift) - 1)) * token + c);
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
                   if ((from[e / 4] >> (8 * (e % 4)) & 0x7f) == 0x7f) v[e] = __int_as_float(0x7fffffff);
