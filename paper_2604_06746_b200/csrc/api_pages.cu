@@ -52,10 +52,10 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
   return true;
 }
 
-// More than 16 rows of a KV head go to tcgen05, whose tiles have 128 rows.
+// More than 32 rows of a KV head go to tcgen05, whose tiles have 128 rows.
 PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  if (cfg.dtype == STRUCTKV_BF16 && rows > 16) return {128, sms, 6, 2};
+  if (cfg.dtype == STRUCTKV_BF16 && rows > 32) return {128, sms, 6, 2};
   return {cfg.dtype == STRUCTKV_FP32 || rows <= 8 ? 8 : 16, sms, 6, 1};
 }
 // Items, rows and places are counted in 31 bits.

@@ -48,7 +48,7 @@ template <int D>
 struct PagesTc {
   static constexpr int kUnit = kKeys * D * 2, kRaw = kKeys * D;   // K or V of a tile, as operands and as codes
   // the rows, then for each stream two tiles as operands, two as codes; a tile's numbers for every 16 keys, four tiles a stream
-  static constexpr int kOps = kRows * D * 2, kRaws = kOps + 8 * kUnit, kInfo = kRaws + 8 * kRaw, kQs = kInfo + 8 * kBlocks * 16, kBars = kQs + 2 * kRows * 4;
+  static constexpr int kOps = kRows * D * 2, kRaws = kOps + 8 * kUnit, kInfo = kRaws + 8 * kRaw, kQs = kInfo + 8 * kBlocks * 16, kBars = kQs + kRows * 4;
   static constexpr int kSmem = kBars + 304 + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
   // stream s, K or V, job mod 2
   auto operand = [&](int s, int v, int p) { return (uint32_t)(S::kOps + (4 * s + 2 * v + p) * S::kUnit); };
   float4* const info = (float4*)(sm + S::kInfo);                 // [stream][job mod 4][block]: K's scale, exponent of V's, its inverse
-  float* const tops = (float*)(sm + S::kQs);                     // [half of a head][row]: the largest element of a row
+  float* const qs = (float*)(sm + S::kQs);                       // a row's factor: scale in bits (capped scores: 1) times 2^-the raise of its queries
   const uint32_t bars = base + S::kBars;
   auto full = [&](int s, int v, int p) { return bars + 8 * (4 * s + 2 * v + p); };
   auto empty = [&](int s, int v, int p) { return bars + 64 + 8 * (4 * s + 2 * v + p); };
@@ -72,8 +72,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
   auto o_done = [&](int s, int p) { return bars + 192 + 8 * (2 * s + p); };
   auto o_free = [&](int s) { return bars + 224 + 8 * s; };
   auto drained = [&](int s) { return bars + 240 + 8 * s; };
-  const uint32_t q_full = bars + 256, q_empty = bars + 264, top_full = bars + 272;
-  volatile int* const words = (volatile int*)(sm + S::kBars + 280);
+  const uint32_t q_full = bars + 256, q_empty = bars + 264;
+  volatile int* const words = (volatile int*)(sm + S::kBars + 272);
   volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v[s]: in a tile of stream s some new token's V was NaN
   volatile uint32_t* const tmem_at = (volatile uint32_t*)words + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, token = a.c.s_token;
@@ -87,7 +87,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
       mbar_init(o_free(s), 4); mbar_init(drained(s), 1);
     }
     mbar_init(q_full, 256);
-    mbar_init(top_full, 256);
     mbar_init(q_empty, 10);                                        // softmax's warps, products' warps
     *abort_flag = 0;
     odd_v[0] = odd_v[1] = 0;
@@ -284,45 +283,48 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
       const int g = quotient(sg.nth, a.by_blocks), rb = sg.nth - g * a.blocks, n_old = a.c.lengths[sg.b];
       const int r = rb * RB + row, tok = quotient(min(r, a.rows - 1), a.by_group), h = min(r, a.rows - 1) - tok * a.group;
       const bool is = r < a.rows, idle = r - lane >= a.rows;       // idle: no row of this warp, which only keeps step
-      // The segment's rows, once the products of the segment before have read theirs; each stream's warps bring half of the heads' elements.
-      float f = 0.f;                                               // a row's factor: scale in bits (capped scores: 1) times 2^-the raise of its queries
+      // The segment's rows, once the products of the segment before have read theirs: D / 8 lanes a row.
+      if (seg > 0 && !(ok = wait(q_empty, (seg - 1) & 1))) break;
       {
-        const char* const q = a.q + sg.b * a.q_batch + tok * a.q_token + (g * a.group + h) * a.q_head + s * D;
-        uint4 w[D / 16];
-        float top = 0.f;
-        if (!idle)
+        constexpr int LANES = D / 8, ROWS = 32 / LANES;
+        const int c = lane % LANES, end = min(RB, a.rows - rb * RB);
+        const char* const q = a.q + sg.b * a.q_batch + (g * a.group) * a.q_head + c * 16;
+        constexpr int BATCH = 4, STEP = 8 * ROWS;                  // rows that are on their way together, rows of all warps
+#pragma unroll 1
+        for (int i0 = warp * ROWS + lane / LANES; i0 - lane / LANES < end; i0 += BATCH * STEP) {
+          uint4 w[BATCH];
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) w[i] = *(const uint4*)(q + i * 16);
-        if (seg > 0 && !(ok = wait(q_empty, (seg - 1) & 1))) break;
-        if (!idle) {
-#pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = max3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
+          for (int b = 0; b < BATCH; ++b) {
+            const int x = rb * RB + min(i0 + b * STEP, end - 1), t = quotient(x, a.by_group);
+            w[b] = *(const uint4*)(q + t * a.q_token + (x - t * a.group) * a.q_head);
           }
-          tops[s * kRows + row] = top;
-        }
-        mbar_arrive(top_full);
-        if (!(ok = wait(top_full, seg & 1))) break;
-        if (!idle) {
-          top = fmaxf(top, tops[(1 - s) * kRows + row]);
-          const int raise = min(max(13 - ((int)(__float_as_uint(top) >> 23) - 127), -113), 126);
-          const float up = exp2i(raise);
-          f = exp2i(-raise) * (CAP ? 1.f : fabsf(a.scale2));       // (a negative scale negates the product)
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+          for (int b = 0; b < BATCH; ++b) {
+            const int i = i0 + b * STEP;
+            const uint32_t x[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
+            uint32_t top = 0u;                                     // of two elements' magnitudes, as bf16
+#pragma unroll
+            for (int e = 0; e < 4; ++e) asm("max.bf16x2 %0, %0, %1;" : "+r"(top) : "r"(x[e] & 0x7fff7fffu));
+#pragma unroll
+            for (int o = 1; o < LANES; o *= 2) asm("max.bf16x2 %0, %0, %1;" : "+r"(top) : "r"(__shfl_xor_sync(0xffffffffu, top, o)));
+            const int exponent = (int)(max(top << 16, top & 0xffff0000u) >> 23);
+            const int raise = min(max(13 - (exponent - 127), -113), 126);
+            const float up = exp2i(raise);
             uint32_t y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = f16x2(__uint_as_float(x[e] << 16) * up, __uint_as_float(x[e] & 0xffff0000u) * up);
-            put16(base + tile_at<RB>(row, s * (D / 16) + i), y[0], y[1], y[2], y[3]);
+            if (i < RB) {
+              put16(base + tile_at<RB>(i, c), y[0], y[1], y[2], y[3]);
+              if (c == 0) qs[i] = exp2i(-raise) * (CAP ? 1.f : fabsf(a.scale2));   // (a negative scale negates the product)
+            }
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(q_full);
-        ++seg;
       }
+      if (!(ok = wait(q_full, seg & 1))) break;
+      ++seg;
+      const float f = qs[row];                                     // (rows behind the last have anything, which stays with them)
       const int jobs = jobs_of(sg, s), last = n_old + tok;
       float m = kNothing, l = 0.f;
       bool far = false;
