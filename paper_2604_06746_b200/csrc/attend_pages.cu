@@ -220,9 +220,10 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
           for (int i = 0; i < NR; ++i) mma(acc[kk % CHAINS][i], x0, x1, x2, x3, qf[p][i][kk][0], qf[p][i][kk][1]);
       }
       const float kf = exp2i(ke - 127), vl = exp2i(127 - ve), vx = (float)(ve - 127);
-      // y - m, element 2 z + x: key g8 + 8 z, row x.  References are whole numbers, so that vx - m is exact.
+      // y, element 2 z + x: key g8 + 8 z, row x; less the reference, or without.  References are whole numbers, so that vx - m is exact.  So far
+      // from zero that an unrounded product and a rounded reference are off by a part of a bit, products are rounded as references are.
       float y[NR][4];
-      auto scores = [&](int i, const float (&c)[2]) {
+      auto scores = [&](int i, bool bare) {
         float z[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[e] = CHAINS == 2 ? acc[0][i][e] + acc[CHAINS - 1][i][e] : acc[0][i][e];
@@ -233,8 +234,17 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
           capped2(z[0], z[1], pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
           capped2(z[2], z[3], pack2(a.cap2, a.cap2), pack2(a.inv_cap, a.inv_cap));
         }
+        if (bare || far) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[i][e] = CAP ? z[e] + c[e & 1] : fmaf(z[e], f[e & 1], c[e & 1]);
+          for (int e = 0; e < 4; ++e) {
+            y[i][e] = __fadd_rn(CAP ? z[e] : __fmul_rn(z[e], f[e & 1]), vx);
+            if (!bare) y[i][e] = __fadd_rn(y[i][e], -m[i][e & 1]);
+          }
+        } else {
+          const float c[2] = {vx - m[i][0], vx - m[i][1]};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[i][e] = CAP ? z[e] + c[e & 1] : fmaf(z[e], f[e & 1], c[e & 1]);
+        }
       };
       if (ahead < s_end) load_k(ahead, page_ahead);
       const bool tail = j0 + 16 > n_old + 1 || bad;
@@ -249,7 +259,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
         bool grown = false;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          scores(i, {vx - m[i][0], vx - m[i][1]});
+          scores(i, false);
           if (tail) hide(i);
           grown |= fmaxf(fmaxf(y[i][0], y[i][1]), fmaxf(y[i][2], y[i][3])) > kRaise + kSlack;
         }
@@ -257,7 +267,7 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
         float top = 0.f;
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-          scores(i, {vx, vx});
+          scores(i, true);
           if (tail) hide(i);
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
@@ -275,13 +285,6 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
         }
         far = __any_sync(0xffffffffu, top > 0x1p20f);
       }
-      // A score and a reference so far from zero that their difference is off by whole bits: no weight is above the largest.
-      if (far)
-#pragma unroll
-        for (int i = 0; i < NR; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (y[i][e] > kRaise + kSlack) y[i][e] = kRaise + kSlack;
       uint32_t odd[4] = {0u, 0u, 0u, 0u};                        // columns of the lane's four keys whose V is NaN, as bits
       bool any_odd = false;
       if (tail) {

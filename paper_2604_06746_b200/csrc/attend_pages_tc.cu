@@ -338,21 +338,27 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
           const float4* const in = info + (s * 4 + (done & 3)) * kBlocks;
           const bool tail = j0 + kKeys > n_old + 1;
           const int sees = last - j0;                              // the last column that is seen
-          // y of 16 scores from column col on, in bits and with V's exponent, less c's; hidden ones minus infinity
-          auto weigh = [&](const float* v, int col, float fk, float c, float (&y)[16]) {
+          // y of 16 scores from column col on, in bits and with V's exponent, less the reference or without; hidden ones minus infinity
+          auto weigh = [&](const float* v, int col, const float4& n, bool bare, float (&y)[16]) {
+            const float fk = f * n.x;
             if (CAP) {
 #pragma unroll
               for (int e = 0; e < 16; e += 2) {
                 y[e] = v[e] * fk;
                 y[e + 1] = v[e + 1] * fk;
                 capped2(y[e], y[e + 1], cap2, inv2);
-                y[e] += c;
-                y[e + 1] += c;
+              }
+            }
+            if (bare || far) {                                     // (as in attend_pages.cu)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                y[e] = __fadd_rn(CAP ? y[e] : __fmul_rn(v[e], fk), n.y);
+                if (!bare) y[e] = __fadd_rn(y[e], -m);
               }
             } else {
-              const uint64_t f2 = pack2(fk, fk), c2 = pack2(c, c);
+              const uint64_t f2 = pack2(fk, fk), c2 = pack2(n.y - m, n.y - m);
 #pragma unroll
-              for (int e = 0; e < 16; e += 2) unpack2(fma2(pack2(v[e], v[e + 1]), f2, c2), y[e], y[e + 1]);
+              for (int e = 0; e < 16; e += 2) unpack2(CAP ? add2(pack2(y[e], y[e + 1]), c2) : fma2(pack2(v[e], v[e + 1]), f2, c2), y[e], y[e + 1]);
             }
             if (tail)
 #pragma unroll
@@ -372,13 +378,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
               for (int b = 0; b < 32; b += 16) {
                 const float4 n = in[(c + b) / 16];
                 float y[16];
-                weigh(x + b, c + b, f * n.x, n.y - m, y);
+                weigh(x + b, c + b, n, false, y);
                 top = fmaxf(top, greatest16(y));
-                // A score and a reference so far from zero that their difference is off by whole bits: no weight is above the largest.
-                if (far && again)
-#pragma unroll
-                  for (int e = 0; e < 16; ++e)
-                    if (y[e] > kRaise + kSlack) y[e] = kRaise + kSlack;
                 uint64_t part = pack2(0.f, 0.f);
 #pragma unroll
                 for (int e = 0; e < 16; e += 2) {
@@ -403,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
               tmem_ld_issue<16>(s_at + c, x);
               tmem_ld_wait(x);
               const float4 n = in[c / 16];
-              weigh(x, c, f * n.x, n.y, y);
+              weigh(x, c, n, true, y);
               top = fmaxf(top, greatest16(y));
             }
             const float to = grown ? fmaxf(ceilf(top) - kRaise, m) : m, by = fast_exp2(m - to);

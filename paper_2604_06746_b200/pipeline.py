@@ -55,6 +55,12 @@ class Prefill:
         self._layers_ws = None
         self._plan = None
 
+    def rotate(self, q_win: torch.Tensor, k: torch.Tensor, rope: binding.Rope, positions: torch.Tensor) -> None:
+        """Eq. 12's f_RoPE, in place: a layer's keys ``[H_kv, N, d]`` at ``positions [N]`` (int32) and its window queries ``[H, w, d]`` at the
+        last of them, as the scorer takes them."""
+        self.ctx.rotate(k.transpose(0, 1)[None], positions, rope)
+        self.ctx.rotate(q_win.transpose(0, 1)[None], positions[-q_win.shape[1]:], rope)
+
     # -- Algorithm 1 lines 3-6 for one layer
     def score(self, layer: int, q_win: torch.Tensor, k: torch.Tensor, scale: float,
               head_cols_out: Optional[torch.Tensor] = None) -> None:
@@ -319,3 +325,95 @@ class Decode:
     def _evict(self) -> None:
         if self.budget:
             self.ctx.evict(self.cache, self.budget, self.recent)
+
+
+class PagedDecode:
+    """Decoding over a paged cache in 8 bits, for what a Prefill kept or for prompts whose keys come here.  Pages are shared out by
+    ``reserve`` and given back by ``release``; page numbers, table and lengths are the same for all layers, of which each has storage of its
+    own.  A step is ``step`` for every layer, with one new token a sequence or up to ``max_new``, then ``advance`` by as many as stay:
+    tokens behind ``lengths`` do not count, and the next ones take their slots.  With a ``rope`` new keys and queries come without positions
+    and are rotated on the way.  Every call but ``reserve`` and ``release`` can be captured into a graph.  A sequence without room is left
+    as it is, and ``ctx.poll_device_status`` says so."""
+
+    def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, pages: int, columns: int, dtype: torch.dtype,
+                 batch: int = 1, page_size: int = 64, max_new: int = 1, rope: Optional[binding.Rope] = None, softcap: float = 0.0,
+                 device: str = "cuda:0"):
+        if not 1 <= max_new <= binding.MAX_NEW:
+            raise ValueError(f"max_new: 1 to {binding.MAX_NEW} new tokens")
+        if pages < 1 or columns < 1 or batch < 1 or n_layers < 1:
+            raise ValueError("layers, pages, columns and sequences: one at least")
+        self.L, self.B, self.max_new, self.rope, self.softcap, self.page_size = n_layers, batch, max_new, rope, softcap, page_size
+        self.ctx = binding.Context(n_q_heads, n_kv_heads, head_dim, 8, 8, dtype, device)
+        dev = torch.device(device)
+        self.table = torch.full((batch, columns), -1, dtype=torch.int32, device=dev)
+        self.lengths = torch.zeros((batch,), dtype=torch.int32, device=dev)
+        self.layers = [binding.Pages.empty(pages, n_kv_heads, page_size, head_dim, self.table, self.lengths) for _ in range(n_layers)]
+        self._of = [[self._part(p, b) for b in range(batch)] for p in self.layers]     # a sequence by itself
+        self._q = torch.empty((batch * max_new * n_q_heads * head_dim,), dtype=dtype, device=dev) if rope is not None else None
+        self._ws = self.ctx.attend_pages_workspace(self.layers[0], 1)
+        for t in range(2, max_new + 1):                      # (not always more for more tokens)
+            ws = self.ctx.attend_pages_workspace(self.layers[0], t)
+            self._ws = ws if ws.numel() > self._ws.numel() else self._ws
+        self._free, self._have = list(range(pages)), [[] for _ in range(batch)]
+
+    def _part(self, p: binding.Pages, b: int) -> binding.Pages:
+        return binding.Pages(p.k, p.v, p.k_scales, p.v_scales, self.table[b:b + 1], self.lengths[b:b + 1])
+
+    def reserve(self, sequence: int, tokens: int) -> None:
+        """Pages for ``tokens`` tokens of a sequence in all, those that it has among them."""
+        have, need = self._have[sequence], -(-tokens // self.page_size)
+        if need > self.table.shape[1] or need - len(have) > len(self._free):
+            raise ValueError("reserve: more pages than a sequence can have, or than are free")
+        more = [self._free.pop() for _ in range(need - len(have))]
+        if more:
+            self.table[sequence, len(have):need] = torch.tensor(more, dtype=torch.int32, device=self.table.device)
+            have += more
+
+    def release(self, sequence: int) -> None:
+        """The sequence ends: its pages are free again.  (Calls that read them were made before, on the same stream.)"""
+        self._free += self._have[sequence]
+        self._have[sequence] = []
+        self.table[sequence] = -1
+        self.lengths[sequence] = 0
+
+    def take(self, prefill: Prefill, sequence: int = 0) -> None:
+        """The sequence begins with the prompt that ``prefill`` compacted: its K (rotated, as it was scored) and V.  ``reserve`` comes first."""
+        c = self.ctx.cfg
+        if not prefill.keep_kv or (prefill.L, prefill.Hkv, prefill.d, prefill.dtype) != (self.L, c.n_kv_heads, c.head_dim, self.ctx.dtype):
+            raise ValueError("take: a Prefill of these layers, heads and type that keeps K and V")
+        if prefill.kv_out.device != self.table.device:
+            raise ValueError("take: a Prefill on the pages' device")
+        if len(self._have[sequence]) * self.page_size < prefill.kv_budget:
+            raise ValueError("take: pages for the prompt's tokens are reserved first")
+        self.lengths[sequence] = 0
+        for l in range(self.L):
+            self.ctx.append_pages(self._of[l][sequence], prefill.k_out[l].transpose(0, 1)[None], prefill.v_out[l].transpose(0, 1)[None])
+        self.lengths[sequence] = prefill.kv_budget
+
+    def keep(self, layer: int, sequence: int, k: torch.Tensor, v: torch.Tensor, index: Optional[torch.Tensor] = None,
+             positions: Optional[torch.Tensor] = None) -> None:
+        """Rows of one layer's K and V ``[H_kv, N, d]`` go behind the sequence's tokens: those that ``index`` (int32, one list for all heads)
+        names, or all; with ``positions [N]`` K is rotated on the way.  ``advance`` comes after the last layer."""
+        rope = self.rope if positions is not None else None
+        self.ctx.append_pages(self._of[layer][sequence], k.transpose(0, 1)[None], v.transpose(0, 1)[None], positions=positions, rope=rope, index=index)
+
+    def step(self, layer: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, positions: Optional[torch.Tensor], scale: float,
+             out: torch.Tensor, counts: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> None:
+        """New tokens, ``q``, ``out [batch, n_new, H, d]``, ``k_new``, ``v_new [batch, n_new, H_kv, d]``, ``counts [batch]`` of them for each
+        sequence (None: all): they are rotated (with a rope), appended, and see the cache and those before them."""
+        b, n, h, d = q.shape
+        if n > self.max_new:
+            raise ValueError("step: more tokens than max_new")
+        if self.rope is not None:
+            if positions is None:
+                raise ValueError("step: positions come with a rope")
+            rotated = self._q[:b * n * h * d].view(b, n, h, d)
+            self.ctx.append_pages(self.layers[layer], k_new, v_new, positions=positions, rope=self.rope, counts=counts, q=q, q_out=rotated)
+            q = rotated
+        else:
+            self.ctx.append_pages(self.layers[layer], k_new, v_new, counts=counts)
+        self.ctx.attend_pages(self.layers[layer], q, scale, out, self._ws, counts=counts, softcap=self.softcap, lse=lse)
+
+    def advance(self, n_new) -> None:
+        """After the last layer: the first ``n_new`` of the new tokens stay (a number, or int32 ``[batch]`` on the device)."""
+        self.lengths += n_new
