@@ -56,7 +56,8 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
 PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
   if (cfg.dtype == STRUCTKV_BF16 && rows > 32) return {128, sms, 6, 2};
-  return {cfg.dtype == STRUCTKV_FP32 || rows <= 8 ? 8 : 16, sms, 6, 1};
+  // (two CTAs an SM, one of which streams while the other begins or ends a segment)
+  return cfg.dtype == STRUCTKV_FP32 ? PagesPlan{8, sms, 6, 1} : rows <= 8 ? PagesPlan{8, 2 * sms, 6, 1} : PagesPlan{16, sms, 6, 1};
 }
 // Items, rows and places are counted in 31 bits.
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, long long slots) {

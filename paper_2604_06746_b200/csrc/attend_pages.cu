@@ -49,19 +49,20 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 template <int D, int NR, int NW>
 struct PagesShape {
   static constexpr int RB = 8 * NR, kRow = D + 4, kSet = RB * kRow + 16;   // of a warp's output: neighbouring warps' are in other banks
-  static constexpr int kSmem = (NW * kSet + 2 * RB * 16) * 4;
-  static_assert(NW >= 8 && NW <= 16, "a row's references are read sixteen at a time");
+  static constexpr int kRefs = NW <= 8 ? 8 : 16;                // a row's references that are read together
+  static constexpr int kSmem = (NW * kSet + 2 * RB * kRefs) * 4;
+  static_assert(NW <= 16 && kRefs - NW <= 8, "references of warps that there are not");
 };
 
 // F32: fp32 storage; CAP: capped scores.
-template <int D, int NR, bool F32, bool CAP, int NW>
-__global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant__ AttendPagesArgs a) {
+template <int D, int NR, bool F32, bool CAP, int NW, int PER>
+__global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_constant__ AttendPagesArgs a) {
   using S = PagesShape<D, NR, NW>;
-  constexpr int RB = S::RB, KK = D / 16, KH = D / 64, PIECES = F32 ? 2 : 1, VW = D / 32;   // VW: words of V a lane has of a key
+  constexpr int RB = S::RB, KK = D / 16, KH = D / 64, PIECES = F32 ? 2 : 1, VW = D / 32, RW = S::kRefs;   // VW: words of V a lane has of a key
   extern __shared__ __align__(16) float smem[];
   float* const outs = smem;                                      // [warp] [RB][kRow]
-  float* const refs = outs + NW * S::kSet;                       // [RB][16], by warps
-  float* const sums = refs + RB * 16;
+  float* const refs = outs + NW * S::kSet;                       // [RB][kRefs], by warps
+  float* const sums = refs + RB * RW;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, t4 = lane & 3;
   pdl_trigger();
   pdl_wait();
@@ -69,23 +70,24 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
   PageSegment sg = first_segment(a, run);
   const int sh4 = a.c.page_shift - kBlockShift, per_page = 1 << sh4, token = a.c.s_token;
 
-  // A warp has every NW-th 16 keys of a segment.  Lane i knows the page and the scales of the i-th of the next 32 that it has, and of the 32 behind
-  // them: bytes of K's and V's scale, and above them whether the page is none (its slots are not seen; the copies come from page 0).
-  int b, g, rb, n_old, s, s_end, page, page_after;
-  unsigned about, about_after;
+  // A warp has every NW-th 16 keys of a segment.  Lane i knows the page and the scales of the i-th of 32 that it has, and in good time of the
+  // 32 behind them; K's scale is 256 where the page is none: its slots are not seen (and its loads go to page 0).
+  int b, g, rb, n_old, s, s_end, page, ks, vs, page_after = 0, ks_after = 0, vs_after = 0;
   const char *k0, *v0;
   const int* table;
-  auto look = [&](int step, unsigned& what) {
+  auto look = [&](int step, int& k, int& v) {                    // (nothing is made of the scales here: they may be on their way)
     int p = 0;
-    what = 0;
+    k = 256;
+    v = 127;
     if (step < s_end) {
       p = table[step >> sh4];
       if ((unsigned)p >= (unsigned)a.c.pages) {
         p = 0;
-        what = 1u << 16;
+      } else {
+        const unsigned at = (((unsigned)p * a.c.n_kv + g) << sh4) + (step & (per_page - 1));
+        k = a.c.k_scales[at];
+        v = a.c.v_scales[at];
       }
-      const unsigned at = (((unsigned)p * a.c.n_kv + g) << sh4) + (step & (per_page - 1));
-      what |= a.c.k_scales[at] | (unsigned)a.c.v_scales[at] << 8;
     }
     return p;
   };
@@ -114,24 +116,39 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
       }
     }
   };
-  // A segment begins: its first keys are on their way.
+  // A lane's elements of row g8 (+ 8) as they lie in memory: 16 of each 64.
+  constexpr int QW = F32 ? 4 : 2;                                // words of four
+  uint32_t xq[NR][KK][QW];
+  // A segment begins: its rows and its first keys are on their way.
   auto begin = [&]() {
     b = sg.b;
     g = quotient(sg.nth, a.by_blocks);
     rb = sg.nth - g * a.blocks;
-    n_old = a.c.lengths[b];
-    s = sg.t0 * (kTileBlocks) + warp;
-    s_end = min(sg.t1 * (kTileBlocks), (sg.keys + 15) / 16);
+    n_old = sg.n;
+    s = sg.t0 * kTileBlocks + warp;
+    s_end = min(sg.t1 * kTileBlocks, (sg.keys + 15) / 16);
     table = (const int*)((const char*)a.c.table + b * a.c.s_table);
     k0 = a.c.k + g * a.c.s_head + (long long)g8 * token + t4 * 16;
     v0 = a.c.v + g * a.c.s_head + 2ll * t4 * token + g8 * (VW * 4);
-    page = look(s + lane * NW, about);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int r = min(rb * RB + 8 * i + g8, a.rows - 1), tok = quotient(r, a.by_group), h = r - tok * a.group;   // (rows behind the last: it again)
+      const char* const q = a.q + b * a.q_batch + tok * a.q_token + (g * a.group + h) * a.q_head + t4 * (F32 ? 64 : 32);
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int w = 0; w < QW; w += 2) {
+          const uint2 x = *(const uint2*)(q + kk / 4 * (F32 ? 256 : 128) + kk % 4 * (QW * 4) + w * 4);
+          xq[i][kk][w] = x.x;
+          xq[i][kk][w + 1] = x.y;
+        }
+    }
+    page = look(s + lane * NW, ks, vs);
     const int p = __shfl_sync(0xffffffffu, page, 0);
     if (s < s_end) {
       load_k(s, p);
       load_v(s, p);
     }
-    page_after = look(s + (32 + lane) * NW, about_after);
   };
   if (sg.t1) begin();
 #pragma unroll 1
@@ -145,25 +162,15 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
     bool far = false;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-      const int r = rb * RB + 8 * i + g8;
-      const bool is = r < a.rows;
-      const int tok = is ? quotient(r, a.by_group) : 0, h = is ? r - tok * a.group : 0;
-      const char* const q = a.q + b * a.q_batch + tok * a.q_token + (g * a.group + h) * a.q_head;
-      float x[KK][4];                                            // of the lane's 16 elements in each 64
-      float top = 0.f;
+      float x[KK][4], top = 0.f;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        const int c = kk / 4 * 64 + t4 * 16 + kk % 4 * 4;
-        if (F32) {
-          const float4 w = is ? *(const float4*)(q + c * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-          x[kk][0] = w.x; x[kk][1] = w.y; x[kk][2] = w.z; x[kk][3] = w.w;
-        } else {
-          const uint2 w = is ? *(const uint2*)(q + c * 2) : make_uint2(0u, 0u);
-          x[kk][0] = __uint_as_float(w.x << 16); x[kk][1] = __uint_as_float(w.x & 0xffff0000u);
-          x[kk][2] = __uint_as_float(w.y << 16); x[kk][3] = __uint_as_float(w.y & 0xffff0000u);
-        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[kk][e]));
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t w = xq[i][kk][F32 ? e % QW : e / 2];
+          x[kk][e] = __uint_as_float(F32 ? w : e % 2 ? w & 0xffff0000u : w << 16);
+          top = fmaxf(top, fabsf(x[kk][e]));
+        }
       }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -195,13 +202,13 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
       const int ahead = s + NW, j0 = s << kBlockShift, i32 = nth & 31;
       if (i32 == 0 && nth > 0) {
         page = page_after;
-        about = about_after;
-        page_after = look(s + (32 + lane) * NW, about_after);
+        ks = ks_after;
+        vs = vs_after;
       }
-      const unsigned what = __shfl_sync(0xffffffffu, about, i32);
+      if (i32 == 8 && s + 24 * NW < s_end) page_after = look(s + (24 + lane) * NW, ks_after, vs_after);
+      const int ke = __shfl_sync(0xffffffffu, ks, i32), ve = __shfl_sync(0xffffffffu, vs, i32);
       const int page_ahead = __shfl_sync(0xffffffffu, i32 < 31 ? page : page_after, (i32 + 1) & 31);
-      const int ke = what & 0xff, ve = what >> 8 & 0xff;
-      const bool bad = what >> 16;
+      const bool bad = ke == 256;
       // products: two chains where a warp has one block of rows
       constexpr int CHAINS = NR == 1 ? 2 : 1;
       float acc[CHAINS][NR][4];
@@ -359,10 +366,10 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
         const int row = 8 * i + 2 * t4 + e;
         if (row >= rows) continue;
         if (g8 == 0) {
-          refs[row * 16 + warp] = m[i][e] == kNothing ? -INFINITY : m[i][e];
-          sums[row * 16 + warp] = l[i][e];
+          refs[row * RW + warp] = m[i][e] == kNothing ? -INFINITY : m[i][e];
+          sums[row * RW + warp] = l[i][e];
         }
-        if (warp == 0 && NW + g8 < 16) refs[row * 16 + NW + g8] = -INFINITY;
+        if (warp == 0 && NW + g8 < RW) refs[row * RW + NW + g8] = -INFINITY;
         if (warp < sets) {
           float* const to = outs + warp * S::kSet + row * S::kRow + g8 * (2 * KK);
 #pragma unroll
@@ -382,10 +389,10 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
 #pragma unroll 1
     for (int i = tid / 2; i < rows * (D / 4); i += NW * 16) {
       const int row = i / (D / 4), c4 = i % (D / 4), odd = tid & 1;
-      float ref[16], top = -INFINITY;
+      float ref[RW], top = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < 16; w += 4) {
-        const float4 x = *(const float4*)(refs + row * 16 + w);
+      for (int w = 0; w < RW; w += 4) {
+        const float4 x = *(const float4*)(refs + row * RW + w);
         ref[w] = x.x; ref[w + 1] = x.y; ref[w + 2] = x.z; ref[w + 3] = x.w;
         top = fmaxf(fmaxf(fmaxf(top, x.x), fmaxf(x.y, x.z)), x.w);
       }
@@ -397,9 +404,9 @@ __global__ void __launch_bounds__(NW * 32, 1) attend_pages(const __grid_constant
       for (int w = 0; w < NW; w += 2) {
         const int my = w + odd;
         if (my < sets) {
-          const float f = fast_exp2((odd ? ref[(w + 1) % 16] : ref[w]) - base);
+          const float f = fast_exp2((odd ? ref[(w + 1) % RW] : ref[w]) - base);
           const float4 x = *(const float4*)(from + my * S::kSet);
-          sum = fmaf(f, sums[row * 16 + my], sum);
+          sum = fmaf(f, sums[row * RW + my], sum);
           v.x = fmaf(f, x.x, v.x); v.y = fmaf(f, x.y, v.y); v.z = fmaf(f, x.z, v.z); v.w = fmaf(f, x.w, v.w);
         }
       }
@@ -514,16 +521,16 @@ __global__ void __launch_bounds__(kFinishThreads, 8) attend_pages_finish(const _
   if (lane == 0 && a.lse) a.lse[q] = nothing ? -INFINITY : (M + log2f(L)) * kLn2;
 }
 
-template <int D, int NR, bool F32, bool CAP, int NW>
+template <int D, int NR, bool F32, bool CAP, int NW, int PER>
 cudaError_t launch_one(const AttendPagesArgs& a, cudaStream_t st) {
   using S = PagesShape<D, NR, NW>;
-  const cudaError_t e = allow_smem<attend_pages<D, NR, F32, CAP, NW>>(S::kSmem);
-  return e != cudaSuccess ? e : launch_pdl(attend_pages<D, NR, F32, CAP, NW>, dim3(a.ctas), dim3(NW * 32), S::kSmem, st, a);
+  const cudaError_t e = allow_smem<attend_pages<D, NR, F32, CAP, NW, PER>>(S::kSmem);
+  return e != cudaSuccess ? e : launch_pdl(attend_pages<D, NR, F32, CAP, NW, PER>, dim3(a.ctas), dim3(NW * 32), S::kSmem, st, a);
 }
 template <int D, bool CAP>
 cudaError_t launch_rows(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
-  if (ctx.cfg.dtype == STRUCTKV_FP32) return launch_one<D, 1, true, CAP, 8>(a, st);
-  return p.rb == 8 ? launch_one<D, 1, false, CAP, 14>(a, st) : launch_one<D, 2, false, CAP, 8>(a, st);
+  if (ctx.cfg.dtype == STRUCTKV_FP32) return launch_one<D, 1, true, CAP, 8, 1>(a, st);
+  return p.rb == 8 ? launch_one<D, 1, false, CAP, 7, 2>(a, st) : launch_one<D, 2, false, CAP, 8, 1>(a, st);
 }
 
 }  // namespace

@@ -59,9 +59,8 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 __device__ __forceinline__ float exp2i(int e) { return __int_as_float(min(max(127 + e, 1), 254) << 23); }   // within fp32's normal numbers
 
-// Keys of sequence b, old ones and new ones; 0: nothing of it is looked at.
-__device__ __forceinline__ int page_keys(const AttendPagesArgs& a, int b) {
-  int n;
+// Keys of sequence b, old ones (n) and new ones; 0: nothing of it is looked at.
+__device__ __forceinline__ int page_keys(const AttendPagesArgs& a, int b, int& n) {
   const int count = rows_of_sequence(a.c, a.counts, b, a.n_new, n);
   if (count < 0) tell_invalid(a.c);
   return count <= 0 ? 0 : n + count;
@@ -69,12 +68,12 @@ __device__ __forceinline__ int page_keys(const AttendPagesArgs& a, int b) {
 __device__ __forceinline__ int page_tiles(const AttendPagesArgs& a, int keys) { return (keys + (1 << a.tile_shift) - 1) >> a.tile_shift; }
 
 // A CTA's run of places and where it begins: sequence, its keys, places of one item before it.
-struct PageRun { int lo, hi, b, before, keys; Shares all; };
+struct PageRun { int lo, hi, b, before, keys, n; Shares all; };
 __device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a) {
   const int lane = threadIdx.x & 31, items = a.c.n_kv * a.blocks;
-  int total = 0, keys = 0, places = 0, incl = 0;
+  int total = 0, keys = 0, n = 0, places = 0, incl = 0;
   auto sweep = [&](int b0) {
-    keys = b0 + lane < a.c.batch ? page_keys(a, b0 + lane) : 0;
+    keys = b0 + lane < a.c.batch ? page_keys(a, b0 + lane, n) : 0;
     places = incl = keys == 0 ? 0 : page_tiles(a, keys) + a.over;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -102,6 +101,7 @@ __device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a) {
       w.b = b0 + from;
       w.before = before + __shfl_sync(0xffffffffu, incl - places, from);
       w.keys = __shfl_sync(0xffffffffu, keys, from);
+      w.n = __shfl_sync(0xffffffffu, n, from);
       break;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);
@@ -110,7 +110,7 @@ __device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a) {
 }
 
 // A CTA's run item by item: tiles [t0, t1) of item `nth` of sequence b (none left: t1 = 0).
-struct PageSegment { int b, nth, t0, t1, keys, tiles, at, hi; };
+struct PageSegment { int b, nth, t0, t1, keys, n, tiles, at, hi; };
 __device__ __forceinline__ void next_segment(PageSegment& s, const AttendPagesArgs& a) {
   s.at += s.tiles + a.over;
   s.t0 = s.t1 = 0;
@@ -118,14 +118,14 @@ __device__ __forceinline__ void next_segment(PageSegment& s, const AttendPagesAr
   if (++s.nth == a.c.n_kv * a.blocks) {
     s.nth = 0;
     do ++s.b;
-    while ((s.keys = page_keys(a, s.b)) == 0 && s.b < a.c.batch - 1);
+    while ((s.keys = page_keys(a, s.b, s.n)) == 0 && s.b < a.c.batch - 1);
     s.tiles = page_tiles(a, s.keys);
   }
   s.t1 = min(s.tiles, s.hi - s.at - a.over);
 }
 __device__ __forceinline__ PageSegment first_segment(const AttendPagesArgs& a, const PageRun& w) {
   const int items = a.c.n_kv * a.blocks;
-  PageSegment s{w.b, 0, 0, 0, w.keys, page_tiles(a, w.keys), w.before * items, w.hi};
+  PageSegment s{w.b, 0, 0, 0, w.keys, w.n, page_tiles(a, w.keys), w.before * items, w.hi};
   if (w.lo >= w.hi) return s;
   const int each = s.tiles + a.over;
   s.nth = (w.lo - s.at) / each;

@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
           j = 0;
           jobs = jobs_of(sg, s);
           g = quotient(sg.nth, a.by_blocks);
-          n_old = a.c.lengths[sg.b];
+          n_old = sg.n;
           table = (const int*)((const char*)a.c.table + sg.b * a.c.s_table);
           k0 = a.c.k + g * a.c.s_head + (long long)row * token + c * 16;
           v0 = a.c.v + g * a.c.s_head + (long long)row * token + c * 16;
@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
     int done = 0, seg = 0;
     bool ok = true;
     do {
-      const int g = quotient(sg.nth, a.by_blocks), rb = sg.nth - g * a.blocks, n_old = a.c.lengths[sg.b];
+      const int g = quotient(sg.nth, a.by_blocks), rb = sg.nth - g * a.blocks, n_old = sg.n;
       const int r = rb * RB + row, tok = quotient(min(r, a.rows - 1), a.by_group), h = min(r, a.rows - 1) - tok * a.group;
       const bool is = r < a.rows, idle = r - lane >= a.rows;       // idle: no row of this warp, which only keeps step
       // The segment's rows, once the products of the segment before have read theirs: D / 8 lanes a row.
