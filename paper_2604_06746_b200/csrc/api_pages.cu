@@ -11,7 +11,7 @@ using namespace skv;
 namespace skv {
 namespace {
 
-constexpr int kOverTiles = 8;          // places of an item's own cost
+constexpr int kOver = 4, kOverTc = 8;  // places of an item's own cost
 
 structkv_status told(cudaError_t e) { return e == cudaSuccess ? STRUCTKV_OK : STRUCTKV_ERR_CUDA; }
 int elem_of(const structkv_ctx* ctx) { return ctx->c.cfg.dtype == STRUCTKV_BF16 ? 2 : 4; }
@@ -55,15 +55,15 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
 // More than 32 rows of a KV head go to tcgen05, whose tiles have 128 rows.
 PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  if (cfg.dtype == STRUCTKV_BF16 && rows > 32) return {128, sms, 6, 2};
-  // (two CTAs an SM, one of which streams while the other begins or ends a segment)
-  return cfg.dtype == STRUCTKV_FP32 ? PagesPlan{8, sms, 6, 1} : rows <= 8 ? PagesPlan{8, 2 * sms, 6, 1} : PagesPlan{16, sms, 6, 1};
+  if (cfg.dtype == STRUCTKV_BF16 && rows > 32) return {128, sms, 2, kOverTc};
+  // (several CTAs an SM: one begins or ends a segment while others stream)
+  return cfg.dtype == STRUCTKV_FP32 ? PagesPlan{8, 2 * sms, 1, kOver} : rows <= 8 ? PagesPlan{8, 4 * sms, 1, kOver} : PagesPlan{16, 2 * sms, 1, kOver};
 }
 // Items, rows and places are counted in 31 bits.
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, long long slots) {
   if (batch < 1 || n_new < 1 || n_new > kMaxNew || slots < 1 || slots > 1 << 30) return false;
   const long long units = (long long)batch * cfg.n_kv_heads, rows = (long long)cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  return units <= 0x3fffffffll && units * rows <= 0x3fffffffll && units * ((rows + 7) / 8) <= 0x7fffffffll / (slots / 64 + 1 + kOverTiles);
+  return units <= 0x3fffffffll && units * rows <= 0x3fffffffll && units * ((rows + 7) / 8) <= 0x7fffffffll / (slots / 64 + 1 + kOverTc);
 }
 struct PagesWs { int2* item_parts; float2* part_stat; float* part_out; size_t bytes; };
 PagesWs carve(const structkv_config& cfg, const PagesPlan& p, int batch, int n_new, void* base) {
@@ -248,9 +248,7 @@ structkv_status structkv_attend_pages(structkv_ctx* ctx, const structkv_pages* p
   a.part_stat = w.part_stat;
   a.part_out = w.part_out;
   a.ctas = plan.ctas;
-  a.least = 0;
-  a.over = kOverTiles;
-  a.tile_shift = plan.tile_shift;
+  a.over = plan.over;
   cudaError_t e = (plan.rb == 128 ? launch_attend_pages_tc : launch_attend_pages)(ctx->c, a, plan, (cudaStream_t)stream);
   if (e == cudaSuccess) e = launch_attend_pages_finish(ctx->c, a, plan, (cudaStream_t)stream);
   return told(e);

@@ -95,15 +95,15 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
   uint4 kb[2][KH];
   uint32_t vb[4][VW];
   auto bytes_of = [&](int step, int p) { return (long long)((unsigned long long)(unsigned)p * (unsigned)a.c.s_page) + (step & (per_page - 1)) * (token << kBlockShift); };
-  auto load_k = [&](int step, int p) {
-    const char* const from = k0 + bytes_of(step, p);
+  auto load_k = [&](long long at) {
+    const char* const from = k0 + at;
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
       for (int h = 0; h < KH; ++h) kb[y][h] = load16(from + y * 8 * token + h * 64);
   };
-  auto load_v = [&](int step, int p) {
-    const char* const from = v0 + bytes_of(step, p);
+  auto load_v = [&](long long at) {
+    const char* const from = v0 + at;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const char* const at = from + ((e & 1) + 8 * (e >> 1)) * token;
@@ -144,10 +144,10 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
         }
     }
     page = look(s + lane * NW, ks, vs);
-    const int p = __shfl_sync(0xffffffffu, page, 0);
+    const long long at = bytes_of(s, __shfl_sync(0xffffffffu, page, 0));
     if (s < s_end) {
-      load_k(s, p);
-      load_v(s, p);
+      load_k(at);
+      load_v(at);
     }
   };
   if (sg.t1) begin();
@@ -209,6 +209,7 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
       const int ke = __shfl_sync(0xffffffffu, ks, i32), ve = __shfl_sync(0xffffffffu, vs, i32);
       const int page_ahead = __shfl_sync(0xffffffffu, i32 < 31 ? page : page_after, (i32 + 1) & 31);
       const bool bad = ke == 256;
+      const long long at_ahead = bytes_of(ahead, page_ahead);
       // products: two chains where a warp has one block of rows
       constexpr int CHAINS = NR == 1 ? 2 : 1;
       float acc[CHAINS][NR][4];
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
 #pragma unroll
           for (int i = 0; i < NR; ++i) mma(acc[kk % CHAINS][i], x0, x1, x2, x3, qf[p][i][kk][0], qf[p][i][kk][1]);
       }
-      const float kf = exp2i(ke - 127), vl = exp2i(127 - ve), vx = (float)(ve - 127);
+      const float kf = __int_as_float(ke << 23), vl = __int_as_float((254 - ve) << 23), vx = __int_as_float(0x4b000000 | ve) - (0x1p23f + 127.f);
       // y, element 2 z + x: key g8 + 8 z, row x; less the reference, or without.  References are whole numbers, so that vx - m is exact.  So far
       // from zero that an unrounded product and a rounded reference are off by a part of a bit, products are rounded as references are.
       float y[NR][4];
@@ -253,7 +254,7 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
           for (int e = 0; e < 4; ++e) y[i][e] = CAP ? z[e] + c[e & 1] : fmaf(z[e], f[e & 1], c[e & 1]);
         }
       };
-      if (ahead < s_end) load_k(ahead, page_ahead);
+      if (ahead < s_end) load_k(at_ahead);
       const bool tail = j0 + 16 > n_old + 1 || bad;
       auto hide = [&](int i) {
 #pragma unroll
@@ -337,7 +338,7 @@ __global__ void __launch_bounds__(NW * 32, PER) attend_pages(const __grid_consta
             for (int i = 0; i < NR; ++i) mma(o[i][2 * w + z], f0, f1, f2, f3, pf[q][i][0], pf[q][i][1]);
         }
       }
-      if (ahead < s_end) load_v(ahead, page_ahead);
+      if (ahead < s_end) load_v(at_ahead);
       if (any_odd) {
 #pragma unroll 1
         for (int c = 0; c < 16; ++c) {                           // lane c / 4 of the four has key 2 (c / 4) + (c & 1) + 8 (c / 2 & 1)
@@ -529,8 +530,8 @@ cudaError_t launch_one(const AttendPagesArgs& a, cudaStream_t st) {
 }
 template <int D, bool CAP>
 cudaError_t launch_rows(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
-  if (ctx.cfg.dtype == STRUCTKV_FP32) return launch_one<D, 1, true, CAP, 8, 1>(a, st);
-  return p.rb == 8 ? launch_one<D, 1, false, CAP, 7, 2>(a, st) : launch_one<D, 2, false, CAP, 8, 1>(a, st);
+  if (ctx.cfg.dtype == STRUCTKV_FP32) return launch_one<D, 1, true, CAP, 4, 2>(a, st);
+  return p.rb == 8 ? launch_one<D, 1, false, CAP, 4, 4>(a, st) : launch_one<D, 2, false, CAP, 4, 2>(a, st);
 }
 
 }  // namespace

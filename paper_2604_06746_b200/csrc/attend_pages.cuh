@@ -1,7 +1,7 @@
 // Attention of new tokens over a paged cache in 8 bits, what its kernels share: how the work is cut and partial results.
 //
 // An item is (sequence b, KV head g, block of up to RB rows) over the sequence's keys, lengths[b] old ones and count[b] new ones; row r =
-// i G + h is new token i and head h of the group.  Items follow one another, sequence after sequence; their tiles (of 64 keys, or 128), behind `over`
+// i G + h is new token i and head h of the group.  Items follow one another, sequence after sequence; their tiles of 64 keys, behind `over`
 // places for what an item costs beside them, form one sequence of W places, of which C CTAs take runs that differ by one place at
 // most.  What a CTA has of an item it leaves as one partial, or two, from slot (item + CTA) times that on (no other pair has them), merged
 // in that order by a second launch: results do not depend on timing.
@@ -24,11 +24,11 @@ struct AttendPagesArgs {
   int2* item_parts;                                             // [item] its first partial's slot, and how many it has
   float2* part_stat;                                            // [slot][RB] reference (bits) and sum
   float* part_out;                                              // [slot][RB][d]
-  int ctas, least, over, tile_shift;
+  int ctas, over;
 };
 
-// Rows of a block, CTAs that run at once, log2 of a tile's keys, partials that a CTA leaves of an item.
-struct PagesPlan { int rb, ctas, tile_shift, parts; };
+// Rows of a block, CTAs that run at once, partials that a CTA leaves of an item, places of an item's own cost.
+struct PagesPlan { int rb, ctas, parts, over; };
 
 cudaError_t launch_attend_pages(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
 cudaError_t launch_attend_pages_tc(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
@@ -65,7 +65,7 @@ __device__ __forceinline__ int page_keys(const AttendPagesArgs& a, int b, int& n
   if (count < 0) tell_invalid(a.c);
   return count <= 0 ? 0 : n + count;
 }
-__device__ __forceinline__ int page_tiles(const AttendPagesArgs& a, int keys) { return (keys + (1 << a.tile_shift) - 1) >> a.tile_shift; }
+__device__ __forceinline__ int page_tiles(int keys) { return (keys + 63) >> 6; }
 
 // A CTA's run of places and where it begins: sequence, its keys, places of one item before it.
 struct PageRun { int lo, hi, b, before, keys, n; Shares all; };
@@ -74,7 +74,7 @@ __device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a) {
   int total = 0, keys = 0, n = 0, places = 0, incl = 0;
   auto sweep = [&](int b0) {
     keys = b0 + lane < a.c.batch ? page_keys(a, b0 + lane, n) : 0;
-    places = incl = keys == 0 ? 0 : page_tiles(a, keys) + a.over;
+    places = incl = keys == 0 ? 0 : page_tiles(keys) + a.over;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int t = __shfl_up_sync(0xffffffffu, incl, o);
@@ -87,7 +87,7 @@ __device__ __forceinline__ PageRun find_run(const AttendPagesArgs& a) {
     total += __shfl_sync(0xffffffffu, incl, 31);
   }
   PageRun w{};
-  w.all = shares_of(total * items, a.ctas, a.by_ctas, a.least);
+  w.all = shares_of(total * items, a.ctas, a.by_ctas, 0);
   w.lo = first_of(w.all, blockIdx.x);
   w.hi = first_of(w.all, blockIdx.x + 1);
   if (w.lo >= w.hi) return w;
@@ -119,13 +119,13 @@ __device__ __forceinline__ void next_segment(PageSegment& s, const AttendPagesAr
     s.nth = 0;
     do ++s.b;
     while ((s.keys = page_keys(a, s.b, s.n)) == 0 && s.b < a.c.batch - 1);
-    s.tiles = page_tiles(a, s.keys);
+    s.tiles = page_tiles(s.keys);
   }
   s.t1 = min(s.tiles, s.hi - s.at - a.over);
 }
 __device__ __forceinline__ PageSegment first_segment(const AttendPagesArgs& a, const PageRun& w) {
   const int items = a.c.n_kv * a.blocks;
-  PageSegment s{w.b, 0, 0, 0, w.keys, w.n, page_tiles(a, w.keys), w.before * items, w.hi};
+  PageSegment s{w.b, 0, 0, 0, w.keys, w.n, page_tiles(w.keys), w.before * items, w.hi};
   if (w.lo >= w.hi) return s;
   const int each = s.tiles + a.over;
   s.nth = (w.lo - s.at) / each;

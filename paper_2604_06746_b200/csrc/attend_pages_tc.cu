@@ -124,35 +124,36 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
     bool ok = true;
     do {
       const int jobs = jobs_of(sg, s);
-      auto scores = [&](int job) {
-        const int p = job & 1;
-        if (!(ok = wait(full(s, 0, p), job >> 1 & 1))) return;
-        tc_fence_after();
-        const uint32_t kd = k_lo + (p * S::kUnit >> 4);
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-          mma_ss(s_at + p * 64, q_lo + (((kk / 4) * RB * 128 + (kk % 4) * 32) >> 4), kd + (((kk / 4) * kKeys * 128 + (kk % 4) * 32) >> 4), hi_k, idesc_s, kk > 0, lead);
-        commit_by(lead, s_full(s, p));
-        commit_by(lead, empty(s, 0, p));
-      };
       // (a stream without a tile in the segment says as well that it came by: else its wait might be for a phase that is gone)
       if ((ok = wait(q_full, seg & 1)) && lead) mbar_arrive(q_empty);
-      if (ok && jobs > 0) scores(done);
-      if (ok && jobs > 1) scores(done + 1);
+      // (from two jobs before the first on, so that this code is there once: what a launch fetches of it is most of its way to the first tile)
 #pragma unroll 1
-      for (int k = 0; k < jobs && ok; ++k, ++done) {
-        const int p = done & 1;
-        if (!(ok = wait(full(s, 1, p), done >> 1 & 1))) break;
-        if (k == 0 && used++ > 0 && !(ok = wait(o_free(s), used & 1))) break;
-        if (!(ok = wait(p_ready(s, p), done >> 1 & 1))) break;
-        tc_fence_after();
-        const uint32_t vd = v_lo + (p * S::kUnit >> 4);
+      for (int k = -2; k < jobs && ok; ++k) {
+        const int job = done + k, p = job & 1;
+        if (k >= 0) {
+          if (!(ok = wait(full(s, 1, p), job >> 1 & 1))) break;
+          if (k == 0 && used++ > 0 && !(ok = wait(o_free(s), used & 1))) break;
+          if (!(ok = wait(p_ready(s, p), job >> 1 & 1))) break;
+          tc_fence_after();
+          const uint32_t vd = v_lo + (p * S::kUnit >> 4);
 #pragma unroll
-        for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts(o_at, s_at + p * 64 + kk * 8, vd + ((kk * 16 * 128) >> 4), hi_v, idesc_o, k > 0 || kk > 0, lead);
-        commit_by(lead, o_done(s, p));
-        commit_by(lead, empty(s, 1, p));
-        if (k + 2 < jobs) scores(done + 2);
+          for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts(o_at, s_at + p * 64 + kk * 8, vd + ((kk * 16 * 128) >> 4), hi_v, idesc_o, k > 0 || kk > 0, lead);
+          commit_by(lead, o_done(s, p));
+          commit_by(lead, empty(s, 1, p));
+        }
+        if (k + 2 < jobs) {
+          // the scores of the job after next
+          if (!(ok = wait(full(s, 0, p), (job + 2) >> 1 & 1))) break;
+          tc_fence_after();
+          const uint32_t kd = k_lo + (p * S::kUnit >> 4);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            mma_ss(s_at + p * 64, q_lo + (((kk / 4) * RB * 128 + (kk % 4) * 32) >> 4), kd + (((kk / 4) * kKeys * 128 + (kk % 4) * 32) >> 4), hi_k, idesc_s, kk > 0, lead);
+          commit_by(lead, s_full(s, p));
+          commit_by(lead, empty(s, 0, p));
+        }
       }
+      done += max(jobs, 0);
       ++seg;
       next_segment(sg, a);
     } while (ok && sg.t1);
@@ -211,62 +212,61 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
       const unsigned what = __shfl_sync(0xffffffffu, scales, j & 31);
       return sg.t1 ? Job{sg.t0 + s + 2 * j, sg.keys, n_old, p, what} : Job{-1, 0, 0, -1, 0};
     };
-    // (called while the job is the newest: k0 and v0 are its sequence's)
-    auto copy = [&](const Job& x, int place, int v) {
-      if (x.page >= 0) {
-        const char* const from = (v ? v0 : k0) + (long long)((unsigned long long)(unsigned)x.page * (unsigned)a.c.s_page) + ((x.t * kBlocks + pw) & (per_page - 1)) * (token << kBlockShift);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) copy16(raw + (2 * place + v) * S::kRaw + i * 512, from + i * kStep * token);
-      }
-      copies_end();
-    };
-    Job now = next();
-    copy(now, 0, 0);
-    copy(now, 0, 1);
-    Job then = next();
-    copy(then, 1, 0);
-    copy(then, 1, 1);
+    // (from two jobs before the first on, so that this code is there once)
+    Job now{-1, 0, 0, -1, 0}, then = now;
     bool ok = true;
 #pragma unroll 1
-    for (int done = 0; now.t >= 0 && ok; ++done) {
+    for (int done = -2; ok; ++done) {
       const int p = done & 1;
       const Job later = next();
+      if (done >= 0 && now.t < 0) break;
       const bool tail = (now.t + 1) * kKeys > now.n_old;
-#pragma unroll
+#pragma unroll 1
       for (int v = 0; v < 2; ++v) {
-        copies_landed<3>();
-        if (done > 1 && !(ok = wait_long(empty(s, v, p), (done >> 1) - 1 & 1))) break;
-        uint4 w[NI];
+        const uint32_t codes = raw + (2 * p + v) * S::kRaw;
+        if (done >= 0) {
+          copies_landed<3>();
+          if (done > 1 && !(ok = wait_long(empty(s, v, p), (done >> 1) - 1 & 1))) break;
+          uint4 w[NI];
 #pragma unroll
-        for (int i = 0; i < NI; ++i) w[i] = now.page >= 0 ? shared16(raw + (2 * p + v) * S::kRaw + i * 512) : make_uint4(0u, 0u, 0u, 0u);
-        if (v == 1 && tail) {
-          // What the slots behind the last key hold reaches nobody; NaN of a new token is added, at the end, to the rows that see it.
+          for (int i = 0; i < NI; ++i) w[i] = now.page >= 0 ? shared16(codes + i * 512) : make_uint4(0u, 0u, 0u, 0u);
+          if (v == 1 && tail) {
+            // What the slots behind the last key hold reaches nobody; NaN of a new token is added, at the end, to the rows that see it.
 #pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            const int key = now.t * kKeys + pw * 16 + row + i * kStep;
-            if (key >= now.keys) w[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (key >= now.n_old && (nan_bytes(w[i].x) | nan_bytes(w[i].y) | nan_bytes(w[i].z) | nan_bytes(w[i].w))) {
-              odd_v[s] = 1;
-              w[i].x &= ~((nan_bytes(w[i].x) >> 7) * 0xffu); w[i].y &= ~((nan_bytes(w[i].y) >> 7) * 0xffu);
-              w[i].z &= ~((nan_bytes(w[i].z) >> 7) * 0xffu); w[i].w &= ~((nan_bytes(w[i].w) >> 7) * 0xffu);
+            for (int i = 0; i < NI; ++i) {
+              const int key = now.t * kKeys + pw * 16 + row + i * kStep;
+              if (key >= now.keys) w[i] = make_uint4(0u, 0u, 0u, 0u);
+              if (key >= now.n_old && (nan_bytes(w[i].x) | nan_bytes(w[i].y) | nan_bytes(w[i].z) | nan_bytes(w[i].w))) {
+                odd_v[s] = 1;
+                w[i].x &= ~((nan_bytes(w[i].x) >> 7) * 0xffu); w[i].y &= ~((nan_bytes(w[i].y) >> 7) * 0xffu);
+                w[i].z &= ~((nan_bytes(w[i].z) >> 7) * 0xffu); w[i].w &= ~((nan_bytes(w[i].w) >> 7) * 0xffu);
+              }
             }
           }
-        }
-        const uint32_t to = base + operand(s, v, p);
+          const uint32_t to = base + operand(s, v, p);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const int r = pw * 16 + row + i * kStep;
-          put16(to + tile_at<kKeys>(r, 2 * c), half_lo(w[i].x), half_hi(w[i].x), half_lo(w[i].y), half_hi(w[i].y));
-          put16(to + tile_at<kKeys>(r, 2 * c + 1), half_lo(w[i].z), half_hi(w[i].z), half_lo(w[i].w), half_hi(w[i].w));
+          for (int i = 0; i < NI; ++i) {
+            const int r = pw * 16 + row + i * kStep;
+            put16(to + tile_at<kKeys>(r, 2 * c), half_lo(w[i].x), half_hi(w[i].x), half_lo(w[i].y), half_hi(w[i].y));
+            put16(to + tile_at<kKeys>(r, 2 * c + 1), half_lo(w[i].z), half_hi(w[i].z), half_lo(w[i].w), half_hi(w[i].w));
+          }
+          if (v == 0 && lane == 0) {
+            // (the job four before, which had this place, is done: the scores of the one two before were made behind its outputs)
+            const int ke = now.scales & 0xff, ve = now.scales >> 8;
+            info[(s * 4 + (done & 3)) * kBlocks + pw] = now.page < 0 ? make_float4(1.f, -INFINITY, 0.f, 0.f) : make_float4(exp2i(ke - 127), (float)(ve - 127), exp2i(127 - ve), 0.f);
+          }
         }
-        if (v == 0 && lane == 0) {
-          // (the job four before, which had this place, is done: the scores of the one two before were made behind its outputs)
-          const int ke = now.scales & 0xff, ve = now.scales >> 8;
-          info[(s * 4 + (done & 3)) * kBlocks + pw] = now.page < 0 ? make_float4(1.f, -INFINITY, 0.f, 0.f) : make_float4(exp2i(ke - 127), (float)(ve - 127), exp2i(127 - ve), 0.f);
+        if (later.page >= 0) {
+          // (k0 and v0 are the newest job's)
+          const char* const from = (v ? v0 : k0) + (long long)((unsigned long long)(unsigned)later.page * (unsigned)a.c.s_page) + ((later.t * kBlocks + pw) & (per_page - 1)) * (token << kBlockShift);
+#pragma unroll
+          for (int i = 0; i < NI; ++i) copy16(codes + i * 512, from + i * kStep * token);
         }
-        copy(later, p, v);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(full(s, v, p));
+        copies_end();
+        if (done >= 0) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_arrive(full(s, v, p));
+        }
       }
       now = then;
       then = later;
