@@ -11,6 +11,7 @@ using namespace skv;
 namespace skv {
 namespace {
 
+constexpr int kRowsTc = 16;
 constexpr int kOver = 4, kOverTc = 8;  // places of an item's own cost
 
 structkv_status told(cudaError_t e) { return e == cudaSuccess ? STRUCTKV_OK : STRUCTKV_ERR_CUDA; }
@@ -55,7 +56,10 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
 // More than 32 rows of a KV head go to tcgen05, whose tiles have 128 rows.
 PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  if (cfg.dtype == STRUCTKV_BF16 && rows > 32) return {128, sms, 2, kOverTc};
+  if (cfg.dtype == STRUCTKV_BF16 && rows > kRowsTc) {
+    const int rb = rows <= 64 ? 64 : 128;
+    return {rb, sms, 1, kOverTc};
+  }
   // (several CTAs an SM: one begins or ends a segment while others stream)
   return cfg.dtype == STRUCTKV_FP32 ? PagesPlan{8, 2 * sms, 1, kOver} : rows <= 8 ? PagesPlan{8, 4 * sms, 1, kOver} : PagesPlan{16, 2 * sms, 1, kOver};
 }
@@ -249,7 +253,7 @@ structkv_status structkv_attend_pages(structkv_ctx* ctx, const structkv_pages* p
   a.part_out = w.part_out;
   a.ctas = plan.ctas;
   a.over = plan.over;
-  cudaError_t e = (plan.rb == 128 ? launch_attend_pages_tc : launch_attend_pages)(ctx->c, a, plan, (cudaStream_t)stream);
+  cudaError_t e = (plan.rb > 16 ? launch_attend_pages_tc : launch_attend_pages)(ctx->c, a, plan, (cudaStream_t)stream);
   if (e == cudaSuccess) e = launch_attend_pages_finish(ctx->c, a, plan, (cudaStream_t)stream);
   return told(e);
 }

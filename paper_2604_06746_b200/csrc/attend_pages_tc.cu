@@ -44,19 +44,27 @@ __device__ __forceinline__ float greatest16(const float* v) {
   return fmaxf(max3(a, v[14], v[15]), b);
 }
 
+// Two words of a row.
+__device__ __forceinline__ void tmem_st2(uint32_t at, float a, float b) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\ntcgen05.wait::st.sync.aligned;" ::"r"(at), "f"(a), "f"(b) : "memory");
+}
+__device__ __forceinline__ void tmem_ld2(uint32_t at, float& a, float& b) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];\ntcgen05.wait::ld.sync.aligned;" : "=f"(a), "=f"(b) : "r"(at) : "memory");
+}
+
 template <int D>
 struct PagesTc {
   static constexpr int kUnit = kKeys * D * 2, kRaw = kKeys * D;   // K or V of a tile, as operands and as codes
   // the rows, then for each stream two tiles as operands, two as codes; a tile's numbers for every 16 keys, four tiles a stream
-  static constexpr int kOps = kRows * D * 2, kRaws = kOps + 8 * kUnit, kInfo = kRaws + 8 * kRaw, kQs = kInfo + 8 * kBlocks * 16, kBars = kQs + kRows * 4;
+  static constexpr int kOps = kRows * D * 2, kRaws = kOps + 8 * kUnit, kInfo = kRaws + 8 * kRaw, kQs = kInfo + 8 * kBlocks * 16, kBars = kQs + kRows * 8;
   static constexpr int kSmem = kBars + 304 + 1024;
   static_assert(kSmem <= 227 * 1024, "shared memory");
 };
 
-template <int D, bool CAP>
+template <int D, int COPIES, bool CAP>
 __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_constant__ AttendPagesArgs a) {
   using S = PagesTc<D>;
-  constexpr int RB = kRows;
+  constexpr int RB = kRows, NR = RB / COPIES, W = kKeys / COPIES;   // rows of a block, columns of a tile that a copy of them sees
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   unsigned char* const sm = smem_raw + (base - smem_u32(smem_raw));
@@ -64,17 +72,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
   auto operand = [&](int s, int v, int p) { return (uint32_t)(S::kOps + (4 * s + 2 * v + p) * S::kUnit); };
   float4* const info = (float4*)(sm + S::kInfo);                 // [stream][job mod 4][block]: K's scale, exponent of V's, its inverse
   float* const qs = (float*)(sm + S::kQs);                       // a row's factor: scale in bits (capped scores: 1) times 2^-the raise of its queries
+  float2* const stats = (float2*)qs;                             // at a segment's end: a row's reference and sum
   const uint32_t bars = base + S::kBars;
   auto full = [&](int s, int v, int p) { return bars + 8 * (4 * s + 2 * v + p); };
   auto empty = [&](int s, int v, int p) { return bars + 64 + 8 * (4 * s + 2 * v + p); };
   auto s_full = [&](int s, int p) { return bars + 128 + 8 * (2 * s + p); };
   auto p_ready = [&](int s, int p) { return bars + 160 + 8 * (2 * s + p); };
   auto o_done = [&](int s, int p) { return bars + 192 + 8 * (2 * s + p); };
-  auto o_free = [&](int s) { return bars + 224 + 8 * s; };
-  auto drained = [&](int s) { return bars + 240 + 8 * s; };
-  const uint32_t q_full = bars + 256, q_empty = bars + 264;
+  auto drained = [&](int s) { return bars + 224 + 8 * s; };
+  const uint32_t q_full = bars + 240, q_empty = bars + 248, met = bars + 256, sent = bars + 264;
   volatile int* const words = (volatile int*)(sm + S::kBars + 272);
-  volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v[s]: in a tile of stream s some new token's V was NaN
+  volatile int *const abort_flag = words, *const odd_v = words + 2;   // odd_v: some new token's V was NaN
   volatile uint32_t* const tmem_at = (volatile uint32_t*)words + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, token = a.c.s_token;
   pdl_trigger();
@@ -84,12 +92,13 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
         for (int v = 0; v < 2; ++v) { mbar_init(full(s, v, p), 128); mbar_init(empty(s, v, p), 1); }
         mbar_init(s_full(s, p), 1); mbar_init(p_ready(s, p), 4); mbar_init(o_done(s, p), 1);
       }
-      mbar_init(o_free(s), 4); mbar_init(drained(s), 1);
+      mbar_init(drained(s), 1);
     }
     mbar_init(q_full, 256);
     mbar_init(q_empty, 10);                                        // softmax's warps, products' warps
+    mbar_init(met, 8); mbar_init(sent, 8);
     *abort_flag = 0;
-    odd_v[0] = odd_v[1] = 0;
+    *odd_v = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 16) {
@@ -120,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
     const uint64_t q_desc = smem_desc(base), k_desc = smem_desc(base + operand(s, 0, 0)), v_desc = keys_desc_n(base + operand(s, 1, 0));
     const uint32_t q_lo = (uint32_t)q_desc, k_lo = (uint32_t)k_desc, v_lo = (uint32_t)v_desc, hi_k = (uint32_t)(q_desc >> 32), hi_v = (uint32_t)(v_desc >> 32);
     const uint32_t s_at = tmem + s * 128, o_at = tmem + 256 + s * 128;
-    int seg = 0, done = 0, used = 0;                               // segments, jobs, segments with jobs
+    int seg = 0, done = 0;                                         // segments, jobs
     bool ok = true;
     do {
       const int jobs = jobs_of(sg, s);
@@ -132,7 +141,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
         const int job = done + k, p = job & 1;
         if (k >= 0) {
           if (!(ok = wait(full(s, 1, p), job >> 1 & 1))) break;
-          if (k == 0 && used++ > 0 && !(ok = wait(o_free(s), used & 1))) break;
           if (!(ok = wait(p_ready(s, p), job >> 1 & 1))) break;
           tc_fence_after();
           const uint32_t vd = v_lo + (p * S::kUnit >> 4);
@@ -186,9 +194,11 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
       }
       return p;
     };
-    // A job: its tile (-1: there is none), its sequence's keys and old ones among them, page and scales of this warp's part.
+    // A job: its tile (-1: there is none), its sequence's keys and old ones among them, page and scales of this warp's part (the scales one
+    // call later: copies need not wait for them).
     struct Job { int t, keys, n_old, page; unsigned scales; };
-    auto next = [&]() {
+    auto next = [&](Job& last) {
+      last.scales = __shfl_sync(0xffffffffu, scales, j & 31);
       if (sg.t1 && ++j == jobs) {
         if (j > 0) next_segment(sg, a);
         while (sg.t1 && jobs_of(sg, s) == 0) next_segment(sg, a);
@@ -209,64 +219,71 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
         page_after = look((j | 31) + 1 + lane, scales_after);
       }
       const int p = __shfl_sync(0xffffffffu, page, j & 31);
-      const unsigned what = __shfl_sync(0xffffffffu, scales, j & 31);
-      return sg.t1 ? Job{sg.t0 + s + 2 * j, sg.keys, n_old, p, what} : Job{-1, 0, 0, -1, 0};
+      return sg.t1 ? Job{sg.t0 + s + 2 * j, sg.keys, n_old, p, 0u} : Job{-1, 0, 0, -1, 0u};
+    };
+    auto widen = [&](uint32_t to, const uint4 (&w)[NI]) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int r = pw * 16 + row + i * kStep;
+        put16(to + tile_at<kKeys>(r, 2 * c), half_lo(w[i].x), half_hi(w[i].x), half_lo(w[i].y), half_hi(w[i].y));
+        put16(to + tile_at<kKeys>(r, 2 * c + 1), half_lo(w[i].z), half_hi(w[i].z), half_lo(w[i].w), half_hi(w[i].w));
+      }
     };
     // (from two jobs before the first on, so that this code is there once)
-    Job now{-1, 0, 0, -1, 0}, then = now;
-    bool ok = true;
+    Job now{-1, 0, 0, -1, 0u}, then = now;
 #pragma unroll 1
-    for (int done = -2; ok; ++done) {
+    for (int done = -2;; ++done) {
       const int p = done & 1;
-      const Job later = next();
-      if (done >= 0 && now.t < 0) break;
-      const bool tail = (now.t + 1) * kKeys > now.n_old;
-#pragma unroll 1
-      for (int v = 0; v < 2; ++v) {
-        const uint32_t codes = raw + (2 * p + v) * S::kRaw;
-        if (done >= 0) {
-          copies_landed<3>();
-          if (done > 1 && !(ok = wait_long(empty(s, v, p), (done >> 1) - 1 & 1))) break;
-          uint4 w[NI];
+      const Job later = next(then);
+      const uint32_t codes = raw + 2 * p * S::kRaw;
+      uint4 kw[NI], vw[NI];
+      if (done >= 0) {
+        if (now.t < 0) break;
+        copies_landed<1>();
+        const bool is = now.page >= 0;
 #pragma unroll
-          for (int i = 0; i < NI; ++i) w[i] = now.page >= 0 ? shared16(codes + i * 512) : make_uint4(0u, 0u, 0u, 0u);
-          if (v == 1 && tail) {
-            // What the slots behind the last key hold reaches nobody; NaN of a new token is added, at the end, to the rows that see it.
+        for (int i = 0; i < NI; ++i) vw[i] = is ? shared16(codes + S::kRaw + i * 512) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-              const int key = now.t * kKeys + pw * 16 + row + i * kStep;
-              if (key >= now.keys) w[i] = make_uint4(0u, 0u, 0u, 0u);
-              if (key >= now.n_old && (nan_bytes(w[i].x) | nan_bytes(w[i].y) | nan_bytes(w[i].z) | nan_bytes(w[i].w))) {
-                odd_v[s] = 1;
-                w[i].x &= ~((nan_bytes(w[i].x) >> 7) * 0xffu); w[i].y &= ~((nan_bytes(w[i].y) >> 7) * 0xffu);
-                w[i].z &= ~((nan_bytes(w[i].z) >> 7) * 0xffu); w[i].w &= ~((nan_bytes(w[i].w) >> 7) * 0xffu);
-              }
-            }
-          }
-          const uint32_t to = base + operand(s, v, p);
+        for (int i = 0; i < NI; ++i) kw[i] = is ? shared16(codes + i * 512) : make_uint4(0u, 0u, 0u, 0u);
+        if (done > 1 && !wait_long(empty(s, 0, p), (done >> 1) - 1 & 1)) break;
+        widen(base + operand(s, 0, p), kw);
+        if (lane == 0) {
+          // (the job four before, which had this place, is done: the scores of the one two before were made behind its outputs)
+          const int ke = now.scales & 0xff, ve = now.scales >> 8;
+          info[(s * 4 + (done & 3)) * kBlocks + pw] = is ? make_float4(exp2i(ke - 127), (float)(ve - 127), exp2i(127 - ve), 0.f) : make_float4(1.f, -INFINITY, 0.f, 0.f);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(full(s, 0, p));
+      }
+      if (later.page >= 0) {
+        // (k0 and v0 are the newest job's; the codes that were here are in registers: K's, read last, have been used)
+        const long long off = (long long)((unsigned long long)(unsigned)later.page * (unsigned)a.c.s_page) + ((later.t * kBlocks + pw) & (per_page - 1)) * (token << kBlockShift);
+        const char *const k = k0 + off, *const v = v0 + off;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) copy16(codes + i * 512, k + i * kStep * token);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) copy16(codes + S::kRaw + i * 512, v + i * kStep * token);
+      }
+      copies_end();
+      if (done >= 0) {
+        if ((now.t + 1) * kKeys > now.n_old) {
+          // What the slots behind the last key hold reaches nobody; NaN of a new token is added, at the end, to the rows that see it.
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
-            const int r = pw * 16 + row + i * kStep;
-            put16(to + tile_at<kKeys>(r, 2 * c), half_lo(w[i].x), half_hi(w[i].x), half_lo(w[i].y), half_hi(w[i].y));
-            put16(to + tile_at<kKeys>(r, 2 * c + 1), half_lo(w[i].z), half_hi(w[i].z), half_lo(w[i].w), half_hi(w[i].w));
+            const int key = now.t * kKeys + pw * 16 + row + i * kStep;
+            uint4& w = vw[i];
+            if (key >= now.keys) w = make_uint4(0u, 0u, 0u, 0u);
+            if (key >= now.n_old && (nan_bytes(w.x) | nan_bytes(w.y) | nan_bytes(w.z) | nan_bytes(w.w))) {
+              *odd_v = 1;
+              w.x &= ~((nan_bytes(w.x) >> 7) * 0xffu); w.y &= ~((nan_bytes(w.y) >> 7) * 0xffu);
+              w.z &= ~((nan_bytes(w.z) >> 7) * 0xffu); w.w &= ~((nan_bytes(w.w) >> 7) * 0xffu);
+            }
           }
-          if (v == 0 && lane == 0) {
-            // (the job four before, which had this place, is done: the scores of the one two before were made behind its outputs)
-            const int ke = now.scales & 0xff, ve = now.scales >> 8;
-            info[(s * 4 + (done & 3)) * kBlocks + pw] = now.page < 0 ? make_float4(1.f, -INFINITY, 0.f, 0.f) : make_float4(exp2i(ke - 127), (float)(ve - 127), exp2i(127 - ve), 0.f);
-          }
         }
-        if (later.page >= 0) {
-          // (k0 and v0 are the newest job's)
-          const char* const from = (v ? v0 : k0) + (long long)((unsigned long long)(unsigned)later.page * (unsigned)a.c.s_page) + ((later.t * kBlocks + pw) & (per_page - 1)) * (token << kBlockShift);
-#pragma unroll
-          for (int i = 0; i < NI; ++i) copy16(codes + i * 512, from + i * kStep * token);
-        }
-        copies_end();
-        if (done >= 0) {
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          mbar_arrive(full(s, v, p));
-        }
+        if (done > 1 && !wait_long(empty(s, 1, p), (done >> 1) - 1 & 1)) break;
+        widen(base + operand(s, 1, p), vw);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(full(s, 1, p));
       }
       now = then;
       then = later;
@@ -276,18 +293,18 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
     const int s = warp / 4, quarter = warp & 3;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_at0 = tmem + s * 128 + lanes, o_at = tmem + 256 + s * 128 + lanes;
     const uint64_t cap2 = pack2(a.cap2, a.cap2), inv2 = pack2(fabsf(a.inv_cap), fabsf(a.inv_cap));
-    const int row = quarter * 32 + lane;
+    const int row = quarter * 32 + lane, copy = row / NR, c_from = copy * W;
     int done = 0, seg = 0;
     bool ok = true;
     do {
       const int g = quotient(sg.nth, a.by_blocks), rb = sg.nth - g * a.blocks, n_old = sg.n;
-      const int r = rb * RB + row, tok = quotient(min(r, a.rows - 1), a.by_group), h = min(r, a.rows - 1) - tok * a.group;
+      const int r = rb * NR + row % NR, tok = quotient(min(r, a.rows - 1), a.by_group), h = min(r, a.rows - 1) - tok * a.group;
       const bool is = r < a.rows, idle = r - lane >= a.rows;       // idle: no row of this warp, which only keeps step
       // The segment's rows, once the products of the segment before have read theirs: D / 8 lanes a row.
       if (seg > 0 && !(ok = wait(q_empty, (seg - 1) & 1))) break;
       {
         constexpr int LANES = D / 8, ROWS = 32 / LANES;
-        const int c = lane % LANES, end = min(RB, a.rows - rb * RB);
+        const int c = lane % LANES, end = min(NR, a.rows - rb * NR);
         const char* const q = a.q + sg.b * a.q_batch + (g * a.group) * a.q_head + c * 16;
         constexpr int BATCH = 4, STEP = 8 * ROWS;                  // rows that are on their way together, rows of all warps
 #pragma unroll 1
@@ -295,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
           uint4 w[BATCH];
 #pragma unroll
           for (int b = 0; b < BATCH; ++b) {
-            const int x = rb * RB + min(i0 + b * STEP, end - 1), t = quotient(x, a.by_group);
+            const int x = rb * NR + min(i0 + b * STEP, end - 1), t = quotient(x, a.by_group);
             w[b] = *(const uint4*)(q + t * a.q_token + (x - t * a.group) * a.q_head);
           }
 #pragma unroll
@@ -313,8 +330,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
             uint32_t y[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = f16x2(__uint_as_float(x[e] << 16) * up, __uint_as_float(x[e] & 0xffff0000u) * up);
-            if (i < RB) {
-              put16(base + tile_at<RB>(i, c), y[0], y[1], y[2], y[3]);
+            if (i < NR) {
+#pragma unroll
+              for (int k = 0; k < COPIES; ++k) put16(base + tile_at<RB>(k * NR + i, c), y[0], y[1], y[2], y[3]);
               if (c == 0) qs[i] = exp2i(-raise) * (CAP ? 1.f : fabsf(a.scale2));   // (a negative scale negates the product)
             }
           }
@@ -324,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
       }
       if (!(ok = wait(q_full, seg & 1))) break;
       ++seg;
-      const float f = qs[row];                                     // (rows behind the last have anything, which stays with them)
+      const float f = qs[row % NR];                                     // (rows behind the last have anything, which stays with them)
       const int jobs = jobs_of(sg, s), last = n_old + tok;
       float m = kNothing, l = 0.f;
       bool far = false;
@@ -364,21 +382,60 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
 #pragma unroll
               for (int e = 0; e < 16; ++e) y[e] = col + e <= sees ? y[e] : -INFINITY;
           };
-          uint32_t p[kKeys / 2];
+          uint32_t p[W / 2];
           float sum = 0.f;
+          bool grown = true, settle = k == 0;                      // (a segment's first tile finds its reference before it is weighed)
 #pragma unroll 1
-          for (bool again = false;; again = true) {
+          for (;;) {
+            if (settle) {
+              // the reference follows: the largest score, without the one as it was
+              float top = -INFINITY;
+#pragma unroll 1
+              for (int c = c_from; c < c_from + W; c += 16) {
+                float x[16], y[16];
+                tmem_ld_issue<16>(s_at + c, x);
+                tmem_ld_wait(x);
+                const float4 n = in[c / 16];
+                weigh(x, c, n, true, y);
+                top = fmaxf(top, greatest16(y));
+              }
+              const float to = grown ? fmaxf(ceilf(top) - kRaise, m) : m, by = fast_exp2(m - to);
+              m = to;
+              l *= by;
+              far = __any_sync(0xffffffffu, is && m != kNothing && fabsf(m) > 0x1p20f);
+              if (k > 0) {
+                if (!(ok = wait(o_done(s, (done - 1) & 1), (done - 1) >> 1 & 1))) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < D; c += 16) {
+                  float x[16];
+                  uint32_t y[16];
+                  tmem_ld_issue<16>(o_at + c, x);
+                  tmem_ld_wait(x);
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(x[e] * by);
+                  tmem_st16(o_at + c, y);
+                }
+                tmem_st_wait();
+              }
+            }
             float top = -INFINITY;
             sum = 0.f;
+            constexpr int PART = W < 32 ? W : 32;
 #pragma unroll
-            for (int c = 0; c < kKeys; c += 32) {
-              float x[32];
-              tmem_ld(s_at + c, x);
+            for (int c = 0; c < W; c += PART) {
+              float x[PART];
+              if constexpr (PART == 32) {
+                tmem_ld(s_at + c_from + c, x);
+              } else {
+                tmem_ld_issue<16>(s_at + c_from + c, x);
+                tmem_ld_wait(x);
+              }
 #pragma unroll
-              for (int b = 0; b < 32; b += 16) {
-                const float4 n = in[(c + b) / 16];
+              for (int b = 0; b < PART; b += 16) {
+                const float4 n = in[(c_from + c + b) / 16];
                 float y[16];
-                weigh(x + b, c + b, n, false, y);
+                weigh(x + b, c_from + c + b, n, false, y);
                 top = fmaxf(top, greatest16(y));
                 uint64_t part = pack2(0.f, 0.f);
 #pragma unroll
@@ -394,47 +451,19 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
                 sum = fmaf(s0 + s1, n.z, sum);
               }
             }
-            const bool grown = top > kRaise + kSlack;
-            if (again || !__any_sync(0xffffffffu, grown)) break;
-            // the reference follows: the largest score, without the one as it was
-            top = -INFINITY;
-#pragma unroll 1
-            for (int c = 0; c < kKeys; c += 16) {
-              float x[16], y[16];
-              tmem_ld_issue<16>(s_at + c, x);
-              tmem_ld_wait(x);
-              const float4 n = in[c / 16];
-              weigh(x, c, n, true, y);
-              top = fmaxf(top, greatest16(y));
-            }
-            const float to = grown ? fmaxf(ceilf(top) - kRaise, m) : m, by = fast_exp2(m - to);
-            m = to;
-            l *= by;
-            far = __any_sync(0xffffffffu, is && m != kNothing && fabsf(m) > 0x1p20f);
-            if (k > 0) {
-              if (!(ok = wait(o_done(s, (done - 1) & 1), (done - 1) >> 1 & 1))) break;
-              tc_fence_after();
-#pragma unroll 1
-              for (int c = 0; c < D; c += 16) {
-                float x[16];
-                uint32_t y[16];
-                tmem_ld_issue<16>(o_at + c, x);
-                tmem_ld_wait(x);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(x[e] * by);
-                tmem_st16(o_at + c, y);
-              }
-              tmem_st_wait();
-            }
+            grown = top > kRaise + kSlack;
+            if (settle || !__any_sync(0xffffffffu, grown)) break;
+            settle = true;
           }
           if (!ok) break;
           l += sum;
-          {
-            uint32_t lo[16], hi[16];
+          // (over the scores; a copy's weights of other columns are zero)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) { lo[e] = p[e]; hi[e] = p[16 + e]; }
-            tmem_st16(s_at, lo);                                   // (over the scores)
-            tmem_st16(s_at + 16, hi);
+          for (int h = 0; h < 2; ++h) {
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = COPIES == 1 || (16 * h + e) / (W / 2) == copy ? p[(16 * h + e) % (W / 2)] : 0u;
+            tmem_st16(s_at + 16 * h, w);
           }
           tmem_st_wait();
         }
@@ -443,45 +472,114 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
         if (lane == 0) mbar_arrive(p_ready(s, done & 1));
       }
       if (!ok) break;
-      if (lane == 0) mbar_arrive(q_empty);                         // (this stream's scores are all there)
-      const int item = sg.b * a.c.n_kv * a.blocks + sg.nth, slot = 2 * (item + blockIdx.x) + s;
+      // The segment ends: its streams' results become one, and its copies'.  Rows' operands are read no more: their place takes what a copy
+      // hands to the other.
+      if (jobs > 0 && !(ok = wait(o_done(s, (done - 1) & 1), (done - 1) >> 1 & 1))) break;
+      tc_fence_after();
+      if (!idle) tmem_st2(s_at0, m, l);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(met);
+      if (!(ok = wait(met, (seg - 1) & 1))) break;
+      tc_fence_after();
+      const int item = sg.b * a.c.n_kv * a.blocks + sg.nth, slot = item + blockIdx.x;
       if (tid == 0 && sg.t0 == 0) {
         const int end = sg.at + a.over + sg.tiles - 1;
-        a.item_parts[item] = make_int2(slot, 2 * (cta_of(run.all, end) - (int)blockIdx.x + 1));
+        a.item_parts[item] = make_int2(slot, cta_of(run.all, end) - (int)blockIdx.x + 1);
       }
-      const size_t at = (size_t)slot * RB + row;
-      if (is) a.part_stat[at] = make_float2(m == kNothing ? -INFINITY : m, l);
-      if (jobs > 0) {
-        if (!(ok = wait(o_done(s, (done - 1) & 1), (done - 1) >> 1 & 1))) break;
-        tc_fence_after();
+      constexpr int COLS = D / (2 * COPIES);                       // that a warp finishes
+      const int c_mine = copy * (D / COPIES) + s * COLS;
+      float w0 = 0.f, w1 = 0.f;
+      // 16 columns of a row's two streams, from column c on
+      auto joined = [&](int c, float (&x)[16]) {
+        float y[16];
+        tmem_ld_issue<16>(tmem + 256 + lanes + c, x);
+        tmem_ld_issue<16>(tmem + 384 + lanes + c, y);
+        tmem_ld_wait(x);
+        tmem_ld_wait(y);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = (w0 < 0.f ? 0.f : x[e] * w0) + (w1 < 0.f ? 0.f : y[e] * w1);
+      };
+      // weights of two results of a row, -1: it has seen nothing, whatever its outputs are; and what they are together
+      auto meet = [](float ma, float la, float mb, float lb, float& wa, float& wb) {
+        const float top = fmaxf(ma, mb);
+        wa = ma == kNothing && la == 0.f ? -1.f : fast_exp2(ma - top);
+        wb = mb == kNothing && lb == 0.f ? -1.f : fast_exp2(mb - top);
+        return make_float2(top, (wa < 0.f ? 0.f : wa * la) + (wb < 0.f ? 0.f : wb * lb));
+      };
+      float2 all;
+      if (!idle) {
+        float m2, l2;
+        tmem_ld2(tmem + (1 - s) * 128 + lanes, m2, l2);
+        all = s ? meet(m2, l2, m, l, w0, w1) : meet(m, l, m2, l2, w0, w1);
+      }
+      const int rr = row % NR;
+      // (pieces of 16 bytes of a row, in an order that differs from row to row: lanes meet no bank twice)
+      auto handed = [&](int c) { return base + rr * (D * 4) + (((c >> 2) ^ (rr & 7)) << 4); };
+      float w_mine = 1.f, w_other = -1.f;
+      if constexpr (COPIES == 2) {
         if (!idle) {
-          const bool odd = odd_v[s] && sg.t1 * kKeys > n_old;
+          const int c_other = (1 - copy) * (D / 2) + s * COLS;
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            float v[32];
-            tmem_ld(o_at + c, v);
-            if (odd && is) {
-#pragma unroll 1
-              for (int i = n_old; i <= last && i < sg.keys; ++i) {
-                const int pg = ((const int*)((const char*)a.c.table + sg.b * a.c.s_table))[i >> a.c.page_shift];
-                if ((unsigned)pg >= (unsigned)a.c.pages) continue;
-                const uint32_t* const from = (const uint32_t*)(a.c.v + pg * a.c.s_page + g * a.c.s_head + (long long)(i & ((1 << a.c.page_shift) - 1)) * token + c);
+          for (int c = c_other; c < c_other + COLS; c += 16) {
+            float x[16];
+            joined(c, x);
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                  if ((from[e / 4] >> (8 * (e % 4)) & 0x7f) == 0x7f) v[e] = __int_as_float(0x7fffffff);
+            for (int e = 0; e < 16; e += 4)
+              put16(handed(c + e), __float_as_uint(x[e]), __float_as_uint(x[e + 1]), __float_as_uint(x[e + 2]), __float_as_uint(x[e + 3]));
+          }
+          if (s == 0) stats[row] = all;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sent);
+        if (!(ok = wait(sent, (seg - 1) & 1))) break;
+        if (!idle) {
+          const float2 other = stats[(1 - copy) * NR + rr];
+          all = meet(all.x, all.y, other.x, other.y, w_mine, w_other);
+        }
+      }
+      if (!idle) {
+        w0 = w0 < 0.f || w_mine < 0.f ? -1.f : w0 * w_mine;
+        w1 = w1 < 0.f || w_mine < 0.f ? -1.f : w1 * w_mine;
+        const bool odd = *odd_v && sg.t1 * kKeys > n_old;
+        const size_t at = (size_t)slot * NR + rr;
+        if (is && s == 0 && copy == 0) a.part_stat[at] = make_float2(all.x == kNothing ? -INFINITY : all.x, all.y);
+#pragma unroll 1
+        for (int c = c_mine; c < c_mine + COLS; c += 16) {
+          float v[16];
+          joined(c, v);
+          if constexpr (COPIES == 2) {
+            if (!(w_other < 0.f))
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                const uint4 x = shared16(handed(c + e));
+                v[e] = fmaf(__uint_as_float(x.x), w_other, v[e]);
+                v[e + 1] = fmaf(__uint_as_float(x.y), w_other, v[e + 1]);
+                v[e + 2] = fmaf(__uint_as_float(x.z), w_other, v[e + 2]);
+                v[e + 3] = fmaf(__uint_as_float(x.w), w_other, v[e + 3]);
               }
-            }
-            if (is) {
-              float4* const to = (float4*)(a.part_out + at * D + c);
+          }
+          if (odd && is) {
+#pragma unroll 1
+            for (int i = n_old; i <= last && i < sg.keys; ++i) {
+              const int pg = ((const int*)((const char*)a.c.table + sg.b * a.c.s_table))[i >> a.c.page_shift];
+              if ((unsigned)pg >= (unsigned)a.c.pages) continue;
+              const uint32_t* const from = (const uint32_t*)(a.c.v + pg * a.c.s_page + g * a.c.s_head + (long long)(i & ((1 << a.c.page_shift) - 1)) * token + c);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) to[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+              for (int e = 0; e < 16; ++e)
+                if ((from[e / 4] >> (8 * (e % 4)) & 0x7f) == 0x7f) v[e] = __int_as_float(0x7fffffff);
             }
           }
+          if (is) {
+            float4* const to = (float4*)(a.part_out + at * D + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+          }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(o_free(s));
       }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty);
       next_segment(sg, a);
     } while (sg.t1);
   }
@@ -495,17 +593,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
   if (tid == 0 && *abort_flag) atomicCAS(a.c.status, 0, (int)STRUCTKV_ERR_TIMEOUT);
 }
 
-template <int D, bool CAP>
+template <int D, int COPIES, bool CAP>
 cudaError_t launch_one(const AttendPagesArgs& a, cudaStream_t st) {
-  const cudaError_t e = allow_smem<attend_pages_tc<D, CAP>>(PagesTc<D>::kSmem);
-  return e != cudaSuccess ? e : launch_pdl(attend_pages_tc<D, CAP>, dim3(a.ctas), dim3(kThreads), PagesTc<D>::kSmem, st, a);
+  const cudaError_t e = allow_smem<attend_pages_tc<D, COPIES, CAP>>(PagesTc<D>::kSmem);
+  return e != cudaSuccess ? e : launch_pdl(attend_pages_tc<D, COPIES, CAP>, dim3(a.ctas), dim3(kThreads), PagesTc<D>::kSmem, st, a);
+}
+template <int D, bool CAP>
+cudaError_t launch_rows(const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
+  return p.rb == 64 ? launch_one<D, 2, CAP>(a, st) : launch_one<D, 1, CAP>(a, st);
 }
 
 }  // namespace
 
-cudaError_t launch_attend_pages_tc(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan&, cudaStream_t st) {
-  if (ctx.cfg.head_dim == 128) return a.cap2 != 0.f ? launch_one<128, true>(a, st) : launch_one<128, false>(a, st);
-  return a.cap2 != 0.f ? launch_one<64, true>(a, st) : launch_one<64, false>(a, st);
+cudaError_t launch_attend_pages_tc(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st) {
+  if (ctx.cfg.head_dim == 128) return a.cap2 != 0.f ? launch_rows<128, true>(a, p, st) : launch_rows<128, false>(a, p, st);
+  return a.cap2 != 0.f ? launch_rows<64, true>(a, p, st) : launch_rows<64, false>(a, p, st);
 }
 
 }  // namespace skv
