@@ -176,13 +176,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
     constexpr int kStep = 16 / NI;                                 // rows from piece to piece
     const uint32_t raw = base + S::kRaws + s * 4 * S::kRaw + pw * (NI * 512) + lane * 16;
     int j = -1, jobs = 0, page = -1, page_after = -1, g = 0, n_old = 0;
-    unsigned scales = 0, scales_after = 0;
+    uint8_t ks = 0, vs = 0, ks_after = 0, vs_after = 0;
     const int* table = nullptr;
     const char *k0 = nullptr, *v0 = nullptr;
-    auto look = [&](int job, unsigned& what) {
+    auto look = [&](int job, uint8_t& ks, uint8_t& vs) {
       const int t = sg.t0 + s + 2 * job, step = t * kBlocks + pw;
       int p = -1;
-      what = 0;
       if (t < sg.t1 && step * 16 < sg.keys) {
         p = table[step >> sh4];
         if ((unsigned)p >= (unsigned)a.c.pages) {
@@ -190,15 +189,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
           tell_invalid(a.c);
         }
         const unsigned at = (((unsigned)max(p, 0) * a.c.n_kv + g) << sh4) + (step & (per_page - 1));
-        what = a.c.k_scales[at] | (unsigned)a.c.v_scales[at] << 8;
+        ks = a.c.k_scales[at];
+        vs = a.c.v_scales[at];
       }
       return p;
     };
     // A job: its tile (-1: there is none), its sequence's keys and old ones among them, page and scales of this warp's part (the scales one
     // call later: copies need not wait for them).
-    struct Job { int t, keys, n_old, page; unsigned scales; };
+    struct Job { int t, keys, n_old, page, scales; };
     auto next = [&](Job& last) {
-      last.scales = __shfl_sync(0xffffffffu, scales, j & 31);
+      last.scales = __shfl_sync(0xffffffffu, ks | vs << 8, j & 31);
       if (sg.t1 && ++j == jobs) {
         if (j > 0) next_segment(sg, a);
         while (sg.t1 && jobs_of(sg, s) == 0) next_segment(sg, a);
@@ -210,16 +210,17 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
           table = (const int*)((const char*)a.c.table + sg.b * a.c.s_table);
           k0 = a.c.k + g * a.c.s_head + (long long)row * token + c * 16;
           v0 = a.c.v + g * a.c.s_head + (long long)row * token + c * 16;
-          page = look(lane, scales);
+          page = look(lane, ks, vs);
         }
       } else if ((j & 31) == 0) {
         page = page_after;
-        scales = scales_after;
+        ks = ks_after;
+        vs = vs_after;
       } else if ((j & 31) == 4 && jobs > (j | 31)) {
-        page_after = look((j | 31) + 1 + lane, scales_after);
+        page_after = look((j | 31) + 1 + lane, ks_after, vs_after);
       }
       const int p = __shfl_sync(0xffffffffu, page, j & 31);
-      return sg.t1 ? Job{sg.t0 + s + 2 * j, sg.keys, n_old, p, 0u} : Job{-1, 0, 0, -1, 0u};
+      return sg.t1 ? Job{sg.t0 + s + 2 * j, sg.keys, n_old, p, 0} : Job{-1, 0, 0, -1, 0};
     };
     auto widen = [&](uint32_t to, const uint4 (&w)[NI]) {
 #pragma unroll
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
       }
     };
     // (from two jobs before the first on, so that this code is there once)
-    Job now{-1, 0, 0, -1, 0u}, then = now;
+    Job now{-1, 0, 0, -1, 0}, then = now;
 #pragma unroll 1
     for (int done = -2;; ++done) {
       const int p = done & 1;
@@ -514,8 +515,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
         all = s ? meet(m2, l2, m, l, w0, w1) : meet(m, l, m2, l2, w0, w1);
       }
       const int rr = row % NR;
-      // (pieces of 16 bytes of a row, in an order that differs from row to row: lanes meet no bank twice)
-      auto handed = [&](int c) { return base + rr * (D * 4) + (((c >> 2) ^ (rr & 7)) << 4); };
+      // Where 4 columns from c on of lane i's row pass through the rows' place: of all rows and columns for what a copy hands to the other, of
+      // the warp's 32 rows and PIECE columns otherwise; 16 bytes each, in an order that differs from row to row, so that lanes meet no bank twice.
+      constexpr int PIECE = D / 4;
+      auto passing = [&](int i, int c) {
+        if (COPIES == 2) return base + (quarter * 32 + i) % NR * (D * 4) + ((c >> 2 ^ i & 7) << 4);
+        return base + (warp * 32 + i) * (PIECE * 4) + (((c & PIECE - 1) >> 2 ^ (D == 128 ? i & 7 : i >> 1 & 3)) << 4);
+      };
+      static_assert(8 * 32 * PIECE * 4 <= S::kOps && kRows / 2 * D * 4 <= S::kOps && COLS % PIECE == 0, "within the rows' place");
       float w_mine = 1.f, w_other = -1.f;
       if constexpr (COPIES == 2) {
         if (!idle) {
@@ -526,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
             joined(c, x);
 #pragma unroll
             for (int e = 0; e < 16; e += 4)
-              put16(handed(c + e), __float_as_uint(x[e]), __float_as_uint(x[e + 1]), __float_as_uint(x[e + 2]), __float_as_uint(x[e + 3]));
+              put16(passing(lane, c + e), __float_as_uint(x[e]), __float_as_uint(x[e + 1]), __float_as_uint(x[e + 2]), __float_as_uint(x[e + 3]));
           }
           if (s == 0) stats[row] = all;
         }
@@ -552,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
             if (!(w_other < 0.f))
 #pragma unroll
               for (int e = 0; e < 16; e += 4) {
-                const uint4 x = shared16(handed(c + e));
+                const uint4 x = shared16(passing(lane, c + e));
                 v[e] = fmaf(__uint_as_float(x.x), w_other, v[e]);
                 v[e + 1] = fmaf(__uint_as_float(x.y), w_other, v[e + 1]);
                 v[e + 2] = fmaf(__uint_as_float(x.z), w_other, v[e + 2]);
@@ -570,10 +577,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_pages_tc(const __grid_cons
                 if ((from[e / 4] >> (8 * (e % 4)) & 0x7f) == 0x7f) v[e] = __int_as_float(0x7fffffff);
             }
           }
-          if (is) {
-            float4* const to = (float4*)(a.part_out + at * D + c);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) to[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+          for (int e = 0; e < 16; e += 4)
+            put16(passing(lane, c + e), __float_as_uint(v[e]), __float_as_uint(v[e + 1]), __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3]));
+          // (lane by lane a row would be a line of its own each time; side by side, LANES lanes write one)
+          constexpr int LANES = PIECE / 4;
+          const int from = c + 16 - PIECE;
+          if (from % PIECE == 0) {
+            __syncwarp();
+#pragma unroll
+            for (int i0 = 0; i0 < 32; i0 += 32 / LANES) {
+              const int i = i0 + lane / LANES, col = from + lane % LANES * 4;
+              const uint4 x = shared16(passing(i, col));
+              if (r - lane + i < min(a.rows, (rb + 1) * NR)) *(uint4*)(a.part_out + ((size_t)slot * NR + rr - lane + i) * D + col) = x;
+            }
+            __syncwarp();
           }
         }
       }
