@@ -11,7 +11,6 @@ using namespace skv;
 namespace skv {
 namespace {
 
-constexpr int kRowsTc = 16;
 constexpr int kOver = 4, kOverTc = 8;  // places of an item's own cost
 
 structkv_status told(cudaError_t e) { return e == cudaSuccess ? STRUCTKV_OK : STRUCTKV_ERR_CUDA; }
@@ -53,15 +52,13 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
   return true;
 }
 
-// More than 32 rows of a KV head go to tcgen05, whose tiles have 128 rows.
-PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms) {
+// More than 16 rows of a KV head go to tcgen05, with caps more than 32 (each score's hyperbolic tangent is worked out by 8 warps an SM there, by
+// 16 here).  Up to 16 rows mma.sync has one pass over the codes, from 17 on two or more.
+PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms, bool capped) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
-  if (cfg.dtype == STRUCTKV_BF16 && rows > kRowsTc) {
-    const int rb = rows <= 64 ? 64 : 128;
-    return {rb, sms, 1, kOverTc};
-  }
+  if (cfg.dtype == STRUCTKV_BF16 && rows > (capped ? 32 : 16)) return {rows <= 64 ? 64 : 128, sms, kOverTc};
   // (several CTAs an SM: one begins or ends a segment while others stream)
-  return cfg.dtype == STRUCTKV_FP32 ? PagesPlan{8, 2 * sms, 1, kOver} : rows <= 8 ? PagesPlan{8, 4 * sms, 1, kOver} : PagesPlan{16, 2 * sms, 1, kOver};
+  return cfg.dtype == STRUCTKV_FP32 ? PagesPlan{8, 2 * sms, kOver} : rows <= 8 ? PagesPlan{8, 4 * sms, kOver} : PagesPlan{16, 2 * sms, kOver};
 }
 // Items, rows and places are counted in 31 bits.
 bool sizes_ok(const structkv_config& cfg, int batch, int n_new, long long slots) {
@@ -79,7 +76,7 @@ PagesWs carve(const structkv_config& cfg, const PagesPlan& p, int batch, int n_n
     off += align_up(bytes, 256);
     return r;
   };
-  const size_t group = cfg.n_q_heads / cfg.n_kv_heads, items = (size_t)batch * cfg.n_kv_heads * ((group * n_new + p.rb - 1) / p.rb), slots = (items + p.ctas) * p.parts;
+  const size_t group = cfg.n_q_heads / cfg.n_kv_heads, items = (size_t)batch * cfg.n_kv_heads * ((group * n_new + p.rb - 1) / p.rb), slots = items + p.ctas;
   w.item_parts = (int2*)take(items * sizeof(int2));
   w.part_stat = (float2*)take(slots * p.rb * sizeof(float2));
   w.part_out = (float*)take(slots * p.rb * cfg.head_dim * sizeof(float));
@@ -210,7 +207,7 @@ structkv_status structkv_append_pages(structkv_ctx* ctx, const structkv_pages* p
 
 size_t structkv_attend_pages_workspace_bytes(const structkv_config* cfg, int batch, int n_new, long long slots) {
   if (structkv_workspace_bytes(cfg) == 0 || !sizes_ok(*cfg, batch, n_new, slots)) return 0;
-  return carve(*cfg, plan_of(*cfg, n_new, kMaxSms), batch, n_new, nullptr).bytes;
+  return std::max(carve(*cfg, plan_of(*cfg, n_new, kMaxSms, false), batch, n_new, nullptr).bytes, carve(*cfg, plan_of(*cfg, n_new, kMaxSms, true), batch, n_new, nullptr).bytes);
 }
 
 structkv_status structkv_attend_pages(structkv_ctx* ctx, const structkv_pages* pages, const structkv_attend_pages_args* x, void* stream) {
@@ -229,7 +226,7 @@ structkv_status structkv_attend_pages(structkv_ctx* ctx, const structkv_pages* p
   a.inv_cap = softcap > 0.f ? x->scale / softcap : 0.f;
   if (!std::isfinite(a.scale2) || !std::isfinite(a.cap2) || !std::isfinite(a.inv_cap)) return STRUCTKV_ERR_INVALID_ARG;
   if (!on_device(ctx)) return STRUCTKV_ERR_INVALID_ARG;
-  const PagesPlan plan = plan_of(cfg, x->n_new, std::min(ctx->c.sm_count, kMaxSms));
+  const PagesPlan plan = plan_of(cfg, x->n_new, std::min(ctx->c.sm_count, kMaxSms), a.cap2 != 0.f);
   const PagesWs w = carve(cfg, plan, a.c.batch, x->n_new, x->workspace);
   if (!x->workspace || x->workspace_bytes < w.bytes || (uintptr_t)x->workspace % 256) return STRUCTKV_ERR_WORKSPACE;
   a.q = (const char*)x->q;

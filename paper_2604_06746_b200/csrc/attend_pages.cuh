@@ -3,8 +3,8 @@
 // An item is (sequence b, KV head g, block of up to RB rows) over the sequence's keys, lengths[b] old ones and count[b] new ones; row r =
 // i G + h is new token i and head h of the group.  Items follow one another, sequence after sequence; their tiles of 64 keys, behind `over`
 // places for what an item costs beside them, form one sequence of W places, of which C CTAs take runs that differ by one place at
-// most.  What a CTA has of an item it leaves as one partial, or two, from slot (item + CTA) times that on (no other pair has them), merged
-// in that order by a second launch: results do not depend on timing.
+// most.  What a CTA has of an item it leaves as a partial, in slot item + CTA (no other pair has it); a second launch merges an
+// item's in order: results do not depend on timing.
 #pragma once
 
 #include "pages.cuh"
@@ -27,8 +27,8 @@ struct AttendPagesArgs {
   int ctas, over;
 };
 
-// Rows of a block, CTAs that run at once, partials that a CTA leaves of an item, places of an item's own cost.
-struct PagesPlan { int rb, ctas, parts, over; };
+// Rows of a block, CTAs that run at once, places of an item's own cost.
+struct PagesPlan { int rb, ctas, over; };
 
 cudaError_t launch_attend_pages(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
 cudaError_t launch_attend_pages_tc(const Ctx& ctx, const AttendPagesArgs& a, const PagesPlan& p, cudaStream_t st);
