@@ -33,7 +33,7 @@ def build(seed, segments, copies):
     s_full, p_ready, o_done = ({(s, p): Barrier(n) for s in range(2) for p in range(2)} for n in (1, WARPS, 1))
     drained = [Barrier(1), Barrier(1)]
     q_full, q_empty, met, sent = Barrier(2 * WARPS), Barrier(2 * WARPS + 2), Barrier(2 * WARPS), Barrier(2 * WARPS)
-    rows, scores = Place(), {k: Place() for k in s_full}
+    rows, handed, scores = Place(), Place(), {k: Place() for k in s_full}
     operand = {k: [Place() for _ in range(WARPS)] for k in full}    # each producing warp's part
     info = {(s, i): [Place() for _ in range(WARPS)] for s in range(2) for i in range(4)}
     outputs = [Place(), Place()]
@@ -105,6 +105,7 @@ def build(seed, segments, copies):
             if n > 0:
                 yield q_empty, n - 1
             rows.write(n)
+            handed.write(n)
             q_full.arrive()
             yield q_full, n
             jobs = jobs_of(seg, s)
@@ -135,6 +136,9 @@ def build(seed, segments, copies):
             if copies == 2:
                 sent.arrive()
                 yield sent, n
+            handed.readers += 1                                     # (partial results pass through the rows' place)
+            yield met, n
+            handed.readers -= 1
             for x in range(2):
                 if jobs_of(seg, x):
                     outputs[x].readers -= 1
