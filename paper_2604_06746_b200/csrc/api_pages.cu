@@ -198,7 +198,7 @@ structkv_status structkv_append_pages(structkv_ctx* ctx, const structkv_pages* p
   a.q_out = (char*)x->q_out;
   a.heads = heads;
   a.q_rows = (int)rows;
-  a.head_step = heads_at_once(rows, d / 8, heads, ctx->c.sm_count);
+  a.head_step = heads_at_once(rows, d * elem / 32, heads, ctx->c.sm_count);
   a.splits = append_splits(a.c.batch * blocks, a.c.n_kv, ctx->c.sm_count);
   a.by_splits = div_by(a.splits);
   a.append_ctas = (int)(a.c.batch * blocks * a.splits);

@@ -12,7 +12,8 @@ namespace skv {
 namespace {
 
 constexpr int kManyHeads = 4;                                     // of a CTA, where there are many blocks; else one
-constexpr int kPairs = 4;                                         // a lane's of a row
+template <typename T>
+constexpr int kPairs = 16 / sizeof(T);                            // a lane's of a row: two chunks of 16 bytes
 
 // The smallest e with which `top` stays within 448 2^e, from the bits of the finite top = m 2^x, 1 <= m < 2 (448 = 1.75 2^8).
 __device__ __forceinline__ int exponent_of(float top) {
@@ -36,26 +37,32 @@ __device__ __forceinline__ uint32_t scaled2(uint32_t codes, uint32_t by) {
   return y;
 }
 
-// The largest magnitude of eight bf16, NaN aside.
-__device__ __forceinline__ float largest(const RawPairs<__nv_bfloat16, kPairs>& r) {
-  auto max2 = [](uint32_t x, uint32_t y) {
-    asm("max.bf16x2 %0, %0, %1;" : "+r"(x) : "r"(y));
-    return x;
-  };
-  constexpr uint32_t kMagnitude = 0x7fff7fffu;
-  const uint32_t m = max2(max2(r.x[0] & kMagnitude, r.x[1] & kMagnitude), max2(r.y[0] & kMagnitude, r.y[1] & kMagnitude));
-  return fmaxf(fmaxf(0.f, __uint_as_float(m << 16)), __uint_as_float(m & 0xffff0000u));
+// The largest magnitude of a lane's bf16, NaN aside.
+template <int N>
+__device__ __forceinline__ float largest(const RawPairs<__nv_bfloat16, N>& r) {
+  uint32_t m = 0u;
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(r.x[i] & 0x7fff7fffu));
+    asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(r.y[i] & 0x7fff7fffu));
+  }
+  return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
 }
-__device__ __forceinline__ float largest(const RawPairs<float, kPairs>&) { return 0.f; }
+template <int N>
+__device__ __forceinline__ float largest(const RawPairs<float, N>&) { return 0.f; }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 
 // HEADS: K and V of so many.
 template <typename T, int D, Pairing P, int HEADS>
-__global__ void __launch_bounds__(2 * D, (sizeof(T) == 2 ? 768 : 512) / (2 * D)) append_pages(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendPagesArgs a) {
-  constexpr int JOBS = 2 * HEADS, LANES = D / (2 * kPairs), THREADS = kBlockSlots * LANES, WARPS = THREADS / 32;
-  static_assert(THREADS == 2 * D, "a lane for four pairs of every slot");
-  using Place = PairPlace<T, D, P, kPairs>;
+__global__ void __launch_bounds__(kBlockSlots * D / (2 * kPairs<T>), 512 / (kBlockSlots * D / (2 * kPairs<T>))) append_pages(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendPagesArgs a) {
+  constexpr int N = kPairs<T>, JOBS = 2 * HEADS, LANES = D / (2 * N), THREADS = kBlockSlots * LANES, WARPS = THREADS / 32;
+  using Place = PairPlace<T, D, P, N>;
   __shared__ float tops[JOBS][WARPS], finite_tops[JOBS][WARPS];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, p0 = (tid % LANES) * kPairs;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, p0 = (tid % LANES) * N;
   pdl_trigger();
   pdl_wait();
   if (blockIdx.x >= a.append_ctas) {
@@ -65,7 +72,7 @@ __global__ void __launch_bounds__(2 * D, (sizeof(T) == 2 ? 768 : 512) / (2 * D))
     const int row = (int)(at / groups), h0 = (int)(at % groups) * a.head_step;
     if (at >= (long long)a.q_rows * groups) return;
     const int b = quotient(row, a.by_new), i = row - b * a.n_new;
-    rotate_heads<T, D, P, kPairs>(r, false, (const T*)(a.q + b * a.q_batch + i * a.q_token), a.q_head / (int)sizeof(T),
+    rotate_heads<T, D, P, N>(r, false, (const T*)(a.q + b * a.q_batch + i * a.q_token), a.q_head / (int)sizeof(T),
                                   (T*)a.q_out + (long long)row * a.heads * D, D, a.positions[b * a.s_positions + i], p0, h0,
                                   min(h0 + a.head_step, a.heads));
     return;
@@ -95,9 +102,9 @@ __global__ void __launch_bounds__(2 * D, (sizeof(T) == 2 ? 768 : 512) / (2 * D))
     for (int j = 0; j < JOBS; ++j)
       if (j / 2 < heads) raw[j] = at.load((const T*)((j & 1 ? v : k) + (j / 2) * a.s_head));
   }
-  uint64_t cos[kPairs / 2], sin[kPairs / 2];
+  uint64_t cos[N / 2], sin[N / 2];
   if (a.rotated) at.angles(r, is ? a.positions[b * a.s_positions + t] : 0, false, cos, sin);
-  auto row_of = [&](int j, float (&u)[kPairs], float (&v)[kPairs]) {
+  auto row_of = [&](int j, float (&u)[N], float (&v)[N]) {
     Place::pairs(raw[j], u, v);
     if (!(j & 1) && a.rotated) at.turn(u, v, cos, sin);
   };
@@ -116,10 +123,10 @@ __global__ void __launch_bounds__(2 * D, (sizeof(T) == 2 ? 768 : 512) / (2 * D))
     if (sizeof(T) == 2 && (j & 1 || !a.rotated)) {
       top = largest(raw[j]);
     } else {
-      float u[kPairs], v[kPairs];
+      float u[N], v[N];
       row_of(j, u, v);
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) top = fmaxf(top, fmaxf(fabsf(u[i]), fabsf(v[i])));
+      for (int i = 0; i < N; ++i) top = max3(top, fabsf(u[i]), fabsf(v[i]));
     }
     top = across(top);
     infinite |= top == INFINITY;
@@ -130,10 +137,10 @@ __global__ void __launch_bounds__(2 * D, (sizeof(T) == 2 ? 768 : 512) / (2 * D))
     // infinities are stored as NaN, and the others' largest is what counts
 #pragma unroll
     for (int j = 0; j < JOBS; ++j) {
-      float u[kPairs], v[kPairs], top = 0.f;
+      float u[N], v[N], top = 0.f;
       row_of(j, u, v);
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
+      for (int i = 0; i < N; ++i) {
         if (fabsf(u[i]) != INFINITY) top = fmaxf(top, fabsf(u[i]));
         if (fabsf(v[i]) != INFINITY) top = fmaxf(top, fabsf(v[i]));
       }
@@ -162,41 +169,54 @@ __global__ void __launch_bounds__(2 * D, (sizeof(T) == 2 ? 768 : 512) / (2 * D))
     char* const out = (j & 1 ? v : k) + (j / 2) * a.c.s_head;
     if (mine) {
       const float by = __int_as_float((127 - ej) << 23);
-      float x[kPairs], y[kPairs], u[kPairs], w[kPairs];
+      const uint64_t by2 = pack2(by, by);
+      float x[N], y[N], u[N], w[N];
       row_of(j, u, w);
+      if (infinite) {
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
-        u[i] *= by;
-        w[i] *= by;
-        if (infinite) {
+        for (int i = 0; i < N; ++i) {
           if (fabsf(u[i]) == INFINITY) u[i] = __int_as_float(0x7fffffff);
           if (fabsf(w[i]) == INFINITY) w[i] = __int_as_float(0x7fffffff);
         }
       }
-      Place::chunks(u, w, x, y);
-      const uint32_t cx = codes4(x[0], x[1], x[2], x[3]), cy = codes4(y[0], y[1], y[2], y[3]);
-      if constexpr (P == HALVES) {
-        *(uint32_t*)(out + at.a) = cx;
-        *(uint32_t*)(out + at.b) = cy;
-      } else if constexpr (P == NEIGHBOURS) {
-        *(uint2*)(out + at.a) = make_uint2(cx, cy);
-      } else {
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) {                        // (pairs of neighbours in cx, cy)
+      for (int i = 0; i < N; i += 2) {
+        unpack2(mul2(pack2(u[i], u[i + 1]), by2), u[i], u[i + 1]);
+        unpack2(mul2(pack2(w[i], w[i + 1]), by2), w[i], w[i + 1]);
+      }
+      Place::chunks(u, w, x, y);
+      uint32_t cx[N / 4], cy[N / 4];
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        cx[i] = codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        cy[i] = codes4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+      }
+      if constexpr (P == SINGLE) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {                             // (pairs of neighbours in cx, cy)
           const int2 el = at.pair(i);
-          const uint32_t c = (i < kPairs / 2 ? cx : cy) >> (16 * (i % 2));
+          const uint32_t c = (i < N / 2 ? cx[i / 2 % (N / 4)] : cy[i / 2 % (N / 4)]) >> (16 * (i % 2));
           out[el.x] = (char)c;
           out[el.y] = (char)(c >> 8);
         }
+      } else if constexpr (N == 8) {
+        *(uint2*)(out + at.a) = make_uint2(cx[0], cx[1]);
+        *(uint2*)(out + at.b) = make_uint2(cy[0], cy[1]);
+      } else {
+        *(uint32_t*)(out + at.a) = cx[0];
+        *(uint32_t*)(out + at.b) = cy[0];
       }
     } else if (dj > 0 && slot < n) {
       // an older token: its codes by the larger scale
       const uint32_t half = dj > 14 ? 1u << (24 - dj) : (uint32_t)(15 - dj) << 10, f = half | half << 16;
       uint2* const at8 = (uint2*)(out + 2 * p0);
-      uint2 c = *at8;
-      c.x = scaled2(c.x & 0xffffu, f) | scaled2(c.x >> 16, f) << 16;
-      c.y = scaled2(c.y & 0xffffu, f) | scaled2(c.y >> 16, f) << 16;
-      *at8 = c;
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        uint2 c = at8[i];
+        c.x = scaled2(c.x & 0xffffu, f) | scaled2(c.x >> 16, f) << 16;
+        c.y = scaled2(c.y & 0xffffu, f) | scaled2(c.y >> 16, f) << 16;
+        at8[i] = c;
+      }
     }
   }
 }
@@ -205,7 +225,8 @@ template <typename T, int D, Pairing P>
 struct Launch {
   static cudaError_t run(const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
     const long long q = a.q ? (long long)a.q_rows * ((a.heads + a.head_step - 1) / a.head_step) : 0, ctas = a.append_ctas + (q + kBlockSlots - 1) / kBlockSlots;
-    return launch_pdl(a.splits == a.c.n_kv ? append_pages<T, D, P, 1> : append_pages<T, D, P, kManyHeads>, dim3((unsigned)ctas), dim3(2 * D), 0, st, r, a);
+    return launch_pdl(a.splits == a.c.n_kv ? append_pages<T, D, P, 1> : append_pages<T, D, P, kManyHeads>, dim3((unsigned)ctas),
+                      dim3(kBlockSlots * D / (2 * kPairs<T>)), 0, st, r, a);
   }
 };
 
@@ -215,7 +236,7 @@ struct Launch {
 int append_splits(long long blocks, int n_kv, int sms) { return blocks * n_kv <= 3ll * sms || n_kv == 1 ? n_kv : (n_kv + kManyHeads - 1) / kManyHeads; }
 
 cudaError_t launch_append_pages(const Ctx& ctx, const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
-  return by_pairing<Launch>(ctx, pairing_of(r, kPairs), r, a, st);
+  return by_pairing<Launch>(ctx, pairing_of(r, ctx.cfg.dtype == STRUCTKV_BF16 ? kPairs<__nv_bfloat16> : kPairs<float>), r, a, st);
 }
 
 }  // namespace skv
