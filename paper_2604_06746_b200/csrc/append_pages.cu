@@ -62,8 +62,11 @@ __global__ void __launch_bounds__(kBlockSlots * D / (2 * kPairs<T>), 512 / (kBlo
   constexpr int N = kPairs<T>, JOBS = 2 * HEADS, LANES = D / (2 * N), THREADS = kBlockSlots * LANES, WARPS = THREADS / 32;
   using Place = PairPlace<T, D, P, N>;
   __shared__ float tops[JOBS][WARPS], finite_tops[JOBS][WARPS];
+  __shared__ __align__(16) unsigned long long steps[D / 2];       // (lanes read different ones: from the arguments one after another)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, p0 = (tid % LANES) * N;
   pdl_trigger();
+  if (a.rotated && tid < D / 2) steps[tid] = r.step[tid];
+  __syncthreads();
   pdl_wait();
   if (blockIdx.x >= a.append_ctas) {
     // queries: a group of lanes a token
@@ -103,7 +106,7 @@ __global__ void __launch_bounds__(kBlockSlots * D / (2 * kPairs<T>), 512 / (kBlo
       if (j / 2 < heads) raw[j] = at.load((const T*)((j & 1 ? v : k) + (j / 2) * a.s_head));
   }
   uint64_t cos[N / 2], sin[N / 2];
-  if (a.rotated) at.angles(r, is ? a.positions[b * a.s_positions + t] : 0, false, cos, sin);
+  if (a.rotated) at.angles(r, steps, is ? a.positions[b * a.s_positions + t] : 0, false, cos, sin);
   auto row_of = [&](int j, float (&u)[N], float (&v)[N]) {
     Place::pairs(raw[j], u, v);
     if (!(j & 1) && a.rotated) at.turn(u, v, cos, sin);

@@ -137,14 +137,14 @@ struct PairPlace {
       }
     }
   }
-  // Cosines and sines of a position, two pairs to a word pair for the packed products; (1, 0) where nothing turns.
-  __device__ __forceinline__ void angles(const RopeArgs& r, int position, bool inverse, uint64_t (&cos)[N / 2], uint64_t (&sin)[N / 2]) const {
+  // Cosines and sines of a position, two pairs to a word pair for the packed products; (1, 0) where nothing turns.  `step`: the rope's.
+  __device__ __forceinline__ void angles(const RopeArgs& r, const unsigned long long* step, int position, bool inverse, uint64_t (&cos)[N / 2], uint64_t (&sin)[N / 2]) const {
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
       float2 cs[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        cs[e] = turns(i + e) ? cos_sin(turn_of(r.step[min(p0 + i + e, STRUCTKV_ROPE_MAX_DIM / 2 - 1)], position), r.amplitude) : make_float2(1.f, 0.f);
+        cs[e] = turns(i + e) ? cos_sin(turn_of(step[min(p0 + i + e, D / 2 - 1)], position), r.amplitude) : make_float2(1.f, 0.f);
         if (inverse) cs[e].y = -cs[e].y;
       }
       cos[i / 2] = pack2(cs[0].x, cs[1].x);
@@ -180,7 +180,7 @@ __device__ __forceinline__ void rotate_heads(const RopeArgs& r, bool inverse, co
   };
   load(h0);
   uint64_t cos[N / 2], sin[N / 2];
-  at.angles(r, position, inverse, cos, sin);
+  at.angles(r, r.step, position, inverse, cos, sin);
 #pragma unroll 1
   for (int h = h0; h < h1; h += U) {
 #pragma unroll
