@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kBlockSlots * D / (2 * kPairs<T>), 512 / (kBlo
     const int row = (int)(at / groups), h0 = (int)(at % groups) * a.head_step;
     if (at >= (long long)a.q_rows * groups) return;
     const int b = quotient(row, a.by_new), i = row - b * a.n_new;
-    rotate_heads<T, D, P, N>(r, false, (const T*)(a.q + b * a.q_batch + i * a.q_token), a.q_head / (int)sizeof(T),
+    rotate_heads<T, D, P, N>(r, steps, false, (const T*)(a.q + b * a.q_batch + i * a.q_token), a.q_head / (int)sizeof(T),
                                   (T*)a.q_out + (long long)row * a.heads * D, D, a.positions[b * a.s_positions + i], p0, h0,
                                   min(h0 + a.head_step, a.heads));
     return;

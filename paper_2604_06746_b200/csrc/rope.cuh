@@ -166,9 +166,9 @@ struct PairPlace {
   }
 };
 
-// Heads [h0, h1) of one token: this lane's N pairs of each, from pair p0 on.
+// Heads [h0, h1) of one token: this lane's N pairs of each, from pair p0 on.  `step`: the rope's.
 template <typename T, int D, Pairing P, int N>
-__device__ __forceinline__ void rotate_heads(const RopeArgs& r, bool inverse, const T* x, long long x_head, T* y, long long y_head, int position,
+__device__ __forceinline__ void rotate_heads(const RopeArgs& r, const unsigned long long* step, bool inverse, const T* x, long long x_head, T* y, long long y_head, int position,
                                              int p0, int h0, int h1) {
   constexpr int U = 2;
   using Place = PairPlace<T, D, P, N>;
@@ -180,7 +180,7 @@ __device__ __forceinline__ void rotate_heads(const RopeArgs& r, bool inverse, co
   };
   load(h0);
   uint64_t cos[N / 2], sin[N / 2];
-  at.angles(r, r.step, position, inverse, cos, sin);
+  at.angles(r, step, position, inverse, cos, sin);
 #pragma unroll 1
   for (int h = h0; h < h1; h += U) {
 #pragma unroll

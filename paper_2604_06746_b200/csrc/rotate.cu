@@ -11,13 +11,16 @@ constexpr int kThreads = 256;
 template <typename T, int D, Pairing P>
 __global__ void __launch_bounds__(kThreads, 3) rotate(const __grid_constant__ RopeArgs r, const __grid_constant__ RotateArgs a) {
   constexpr int N = 16 / sizeof(T), LANES = D / (2 * N);
+  __shared__ __align__(16) unsigned long long steps[D / 2];       // (lanes read different ones: from the arguments one after another)
   pdl_trigger();
+  if (threadIdx.x < D / 2) steps[threadIdx.x] = r.step[threadIdx.x];
+  __syncthreads();
   pdl_wait();
   const long long row = (long long)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES;
   const int h0 = blockIdx.y * a.head_step;
   if (row >= a.rows) return;
   const int b = quotient((int)row, a.by_tokens), i = (int)row - b * a.tokens;
-  rotate_heads<T, D, P, N>(r, a.inverse, (const T*)(a.x + b * a.x_batch + i * a.x_token), a.x_head / (int)sizeof(T),
+  rotate_heads<T, D, P, N>(r, steps, a.inverse, (const T*)(a.x + b * a.x_batch + i * a.x_token), a.x_head / (int)sizeof(T),
                   (T*)(a.out + b * a.o_batch + i * a.o_token), a.o_head / (int)sizeof(T), a.positions[b * a.s_positions + i],
                   (threadIdx.x % LANES) * N, h0, min(h0 + a.head_step, a.heads));
 }
