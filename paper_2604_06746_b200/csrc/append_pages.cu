@@ -50,16 +50,30 @@ __device__ __forceinline__ float largest(const RawPairs<__nv_bfloat16, N>& r) {
 }
 template <int N>
 __device__ __forceinline__ float largest(const RawPairs<float, N>&) { return 0.f; }
+// (nothing there: zeros, and nothing is read)
+__device__ __forceinline__ void copy16(uint4* to, const void* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
-// HEADS: K and V of so many.
+// A CTA for K and V of HEADS heads.  Of many heads a lane's rows wait in shared memory, in places of its own, and registers are left for more CTAs.
 template <typename T, int D, Pairing P, int HEADS>
-__global__ void __launch_bounds__(kBlockSlots * D / (2 * kPairs<T>), 512 / (kBlockSlots * D / (2 * kPairs<T>))) append_pages(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendPagesArgs a) {
-  constexpr int N = kPairs<T>, JOBS = 2 * HEADS, LANES = D / (2 * N), THREADS = kBlockSlots * LANES, WARPS = THREADS / 32;
+struct AppendShape {
+  static constexpr int N = kPairs<T>, kJobs = 2 * HEADS, kLanes = D / (2 * N), kThreads = kBlockSlots * kLanes;
+  static constexpr bool kStaged = HEADS > 1 && P != SINGLE;
+  static constexpr int kSmem = kStaged ? kJobs * 2 * kThreads * 16 : 0, kPer = (kStaged ? sizeof(T) == 2 ? 896 : 768 : 512) / kThreads;
+};
+
+template <typename T, int D, Pairing P, int HEADS>
+__global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendShape<T, D, P, HEADS>::kPer) append_pages(const __grid_constant__ RopeArgs r, const __grid_constant__ AppendPagesArgs a) {
+  using S = AppendShape<T, D, P, HEADS>;
+  constexpr int N = S::N, JOBS = S::kJobs, LANES = S::kLanes, WARPS = S::kThreads / 32;
+  extern __shared__ __align__(16) uint4 staged[];                 // [job][chunk][lane]
   using Place = PairPlace<T, D, P, N>;
   __shared__ float tops[JOBS][WARPS], finite_tops[JOBS][WARPS];
   __shared__ __align__(16) unsigned long long steps[D / 2];       // (lanes read different ones: from the arguments one after another)
@@ -98,17 +112,29 @@ __global__ void __launch_bounds__(kBlockSlots * D / (2 * kPairs<T>), 512 / (kBlo
   if ((mine && !is) || no_page) tell_invalid(a.c);
   if (no_page) return;
   const Place at(r, p0);
-  typename Place::Raw raw[JOBS] = {};
-  if (is) {
-    const char *const k = a.k + b * a.s_batch + t * a.s_token + g0 * a.s_head, *const v = a.v + (k - a.k);
+  typename Place::Raw raw[S::kStaged ? 1 : JOBS] = {};
+  const char *const k_from = a.k + b * a.s_batch + t * a.s_token + g0 * a.s_head, *const v_from = a.v + (k_from - a.k);
+  auto place = [&](int j, int chunk) { return staged + (2 * j + chunk) * S::kThreads + tid; };
 #pragma unroll
-    for (int j = 0; j < JOBS; ++j)
-      if (j / 2 < heads) raw[j] = at.load((const T*)((j & 1 ? v : k) + (j / 2) * a.s_head));
+  for (int j = 0; j < JOBS; ++j) {
+    const bool there = is && j / 2 < heads;
+    const T* const from = (const T*)((j & 1 ? v_from : k_from) + (j / 2) * a.s_head);
+    if constexpr (!S::kStaged) {
+      if (there) raw[j] = at.load(from);
+    } else {
+      copy16(place(j, 0), there ? from + at.a : (const T*)a.k, there);
+      copy16(place(j, 1), there ? from + at.b : (const T*)a.k, there);
+    }
   }
   uint64_t cos[N / 2], sin[N / 2];
   if (a.rotated) at.angles(r, steps, is ? a.positions[b * a.s_positions + t] : 0, false, cos, sin);
+  if constexpr (S::kStaged) copies_landed();
+  auto raw_of = [&](int j) {
+    if constexpr (S::kStaged) return typename Place::Raw{*place(j, 0), *place(j, 1)};
+    else return raw[j];
+  };
   auto row_of = [&](int j, float (&u)[N], float (&v)[N]) {
-    Place::pairs(raw[j], u, v);
+    Place::pairs(raw_of(j), u, v);
     if (!(j & 1) && a.rotated) at.turn(u, v, cos, sin);
   };
   // (positive numbers are ordered as their bits are; NaN has no part in a maximum)
@@ -124,7 +150,7 @@ __global__ void __launch_bounds__(kBlockSlots * D / (2 * kPairs<T>), 512 / (kBlo
   for (int j = 0; j < JOBS; ++j) {
     float top = 0.f;
     if (sizeof(T) == 2 && (j & 1 || !a.rotated)) {
-      top = largest(raw[j]);
+      top = largest(raw_of(j));
     } else {
       float u[N], v[N];
       row_of(j, u, v);
@@ -224,19 +250,24 @@ __global__ void __launch_bounds__(kBlockSlots * D / (2 * kPairs<T>), 512 / (kBlo
   }
 }
 
+template <typename T, int D, Pairing P, int HEADS>
+cudaError_t launch_one(const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
+  using S = AppendShape<T, D, P, HEADS>;
+  const long long q = a.q ? (long long)a.q_rows * ((a.heads + a.head_step - 1) / a.head_step) : 0, ctas = a.append_ctas + (q + kBlockSlots - 1) / kBlockSlots;
+  const cudaError_t e = allow_smem<append_pages<T, D, P, HEADS>>(S::kSmem);
+  return e != cudaSuccess ? e : launch_pdl(append_pages<T, D, P, HEADS>, dim3((unsigned)ctas), dim3(S::kThreads), S::kSmem, st, r, a);
+}
 template <typename T, int D, Pairing P>
 struct Launch {
   static cudaError_t run(const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
-    const long long q = a.q ? (long long)a.q_rows * ((a.heads + a.head_step - 1) / a.head_step) : 0, ctas = a.append_ctas + (q + kBlockSlots - 1) / kBlockSlots;
-    return launch_pdl(a.splits == a.c.n_kv ? append_pages<T, D, P, 1> : append_pages<T, D, P, kManyHeads>, dim3((unsigned)ctas),
-                      dim3(kBlockSlots * D / (2 * kPairs<T>)), 0, st, r, a);
+    return a.splits == a.c.n_kv ? launch_one<T, D, P, 1>(r, a, st) : launch_one<T, D, P, kManyHeads>(r, a, st);
   }
 };
 
 }  // namespace
 
 // One head a CTA as long as that leaves the SMs' places for CTAs free.
-int append_splits(long long blocks, int n_kv, int sms) { return blocks * n_kv <= 3ll * sms || n_kv == 1 ? n_kv : (n_kv + kManyHeads - 1) / kManyHeads; }
+int append_splits(long long blocks, int n_kv, int sms) { return blocks * n_kv <= 8ll * sms || n_kv == 1 ? n_kv : (n_kv + kManyHeads - 1) / kManyHeads; }
 
 cudaError_t launch_append_pages(const Ctx& ctx, const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
   return by_pairing<Launch>(ctx, pairing_of(r, ctx.cfg.dtype == STRUCTKV_BF16 ? kPairs<__nv_bfloat16> : kPairs<float>), r, a, st);

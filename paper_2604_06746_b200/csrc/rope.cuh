@@ -44,7 +44,11 @@ inline __host__ __device__ Pairing pairing_of(const RopeArgs& r, int n) { return
 
 // A lane's chunks as they lie in memory (SINGLE: as whole pairs of neighbours would).
 template <typename T, int N>
-struct RawPairs { uint32_t x[N * sizeof(T) / 4], y[N * sizeof(T) / 4]; };
+struct RawPairs {
+  uint32_t x[N * sizeof(T) / 4], y[N * sizeof(T) / 4];
+  RawPairs() = default;
+  __device__ __forceinline__ RawPairs(const uint4& a, const uint4& b) : x{a.x, a.y, a.z, a.w}, y{b.x, b.y, b.z, b.w} {}
+};
 
 template <typename T, int D, Pairing P, int N>
 struct PairPlace {
