@@ -115,6 +115,8 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
   typename Place::Raw raw[S::kStaged ? 1 : JOBS] = {};
   const char *const k_from = a.k + b * a.s_batch + t * a.s_token + g0 * a.s_head, *const v_from = a.v + (k_from - a.k);
   auto place = [&](int j, int chunk) { return staged + (2 * j + chunk) * S::kThreads + tid; };
+  const bool any = __any_sync(0xffffffffu, mine);                 // (a decoding step's blocks have one new row)
+  if (any)
 #pragma unroll
   for (int j = 0; j < JOBS; ++j) {
     const bool there = is && j / 2 < heads;
@@ -127,7 +129,7 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
     }
   }
   uint64_t cos[N / 2], sin[N / 2];
-  if (a.rotated) at.angles(r, steps, is ? a.positions[b * a.s_positions + t] : 0, false, cos, sin);
+  if (any && a.rotated) at.angles(r, steps, is ? a.positions[b * a.s_positions + t] : 0, false, cos, sin);
   if constexpr (S::kStaged) copies_landed();
   auto raw_of = [&](int j) {
     if constexpr (S::kStaged) return typename Place::Raw{*place(j, 0), *place(j, 1)};
@@ -146,6 +148,8 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
                                (((size_t)page * a.c.n_kv + g0 + (job ? lane / 2 : 0)) << (a.c.page_shift - kBlockShift)) + (in_page >> kBlockShift);
   const int had = job && slot0 < n ? (int)*scale - 127 : -127;
   bool infinite = false;
+  if (!any && lane < JOBS) tops[lane][warp] = finite_tops[lane][warp] = 0.f;
+  if (any)
 #pragma unroll
   for (int j = 0; j < JOBS; ++j) {
     float top = 0.f;
@@ -164,6 +168,7 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
   infinite = __syncthreads_or(infinite);
   if (infinite) {
     // infinities are stored as NaN, and the others' largest is what counts
+    if (any)
 #pragma unroll
     for (int j = 0; j < JOBS; ++j) {
       float u[N], v[N], top = 0.f;
