@@ -11,7 +11,9 @@ using namespace skv;
 namespace skv {
 namespace {
 
-constexpr int kOver = 4, kOverTc = 8;  // places of an item's own cost
+// Places of an item's own cost, in tiles of 64 keys.  16 sequences of 1 to 5003 keys 20.8 us; 1 place 23.0, 12 places 22.0.  On tcgen05 16 tokens over
+// 4 x 8192 keys 35.3 us; 2 places 37.0, 24 places 37.6.
+constexpr int kOver = 4, kOverTc = 8;
 
 structkv_status told(cudaError_t e) { return e == cudaSuccess ? STRUCTKV_OK : STRUCTKV_ERR_CUDA; }
 int elem_of(const structkv_ctx* ctx) { return ctx->c.cfg.dtype == STRUCTKV_BF16 ? 2 : 4; }
@@ -53,7 +55,8 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
 }
 
 // More than 16 rows of a KV head go to tcgen05, with caps more than 32 (each score's hyperbolic tangent is worked out by 8 warps an SM there, by
-// 16 here).  Up to 16 rows mma.sync has one pass over the codes, from 17 on two or more.
+// 8 or 16 here).  Up to 16 rows mma.sync has one pass over the codes, from 17 on two or more.  20 rows over 32 x 4096 keys: 129 us on mma.sync, 100 on
+// tcgen05; over 4 x 8192 39.6, 34.0; over 1 x 4096 14.5, 15.2.  With caps 20 rows over 4 x 8192 43 us and 47, 40 rows 58 and 48.
 PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms, bool capped) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
   if (cfg.dtype == STRUCTKV_BF16 && rows > (capped ? 32 : 16)) return {rows <= 64 ? 64 : 128, sms, kOverTc};

@@ -1,14 +1,24 @@
-// Attention of new tokens over a paged cache in 8 bits where a KV head has more than 16 rows.
+// Attention of new tokens over a paged cache in 8 bits where a KV head has more than 16 rows (with caps 32).
 //
 // S = Q K^T and O += P V on the tensor cores (tcgen05): tiles of 128 rows x 64 keys, lane = row.  Two streams, the even and the odd
-// tiles of a segment, alternate; each has two places for scores, so that the next tile's are there when a tile's exponentials are done, and
-// leaves a partial of its own.  K and V come as codes: a stream's four producing warps copy them lane by lane (cp.async, two tiles
-// ahead), widen them to fp16, which is exact, and lay them out as the products' operands; a code is widened once for all rows.  Scales stay
+// tiles of a segment, alternate; each has two places for scores, so that the next tile's are there when a tile's exponentials are done.
+// K and V come as codes: a stream's four producing warps copy them lane by lane (cp.async, two tiles ahead: pages and strides as they
+// come), widen them to fp16, which is exact, and lay them out as the products' operands; a code is widened once for all rows.  Scales stay
 // out of the operands: in bits, a score is s f 2^e_k and its weight in O 2^(s f 2^e_k + e_v - m), one multiply-add with two numbers for each 16
-// keys.  References, weights and queries as in attend_pages.cu; a tile's weights are worked out against the reference as it is, and again
-// where that is outgrown.
+// keys.  References, weights and queries as in attend_pages.cu; a segment's first tile finds its reference first, later tiles are weighed against
+// the reference as it is, and again where that is outgrown.
+//
+// Up to 64 rows stand twice in a tile, and each copy weighs half of its keys (its weights of the others are zero): all eight softmax warps
+// have work and a tile's exponentials take half as long, where half of the tensor cores' rows would be idle anyway.  At a segment's end streams and
+// copies become one partial, through the rows' place in shared memory, which writes whole lines.
 //
 // Warps: 0-3 and 4-7 bring a segment's rows and are the streams' softmax; 8-11 and 12-15 produce; 16 and 17 issue the streams' products.
+//
+// 16 tokens over 4 x 8192 keys (64 rows, 67 MB of codes): 34.7 us, 1.9 TB/s and 250 TFLOP/s.  A steady tile takes 1150 clocks of an SM, for
+// which the chain is the bound, not a unit: scores (1000) -> weights (1700) -> outputs (700) -> the next scores in that place, of four in
+// flight, and the producers' steps (2200 for a tile, two streams); tensor pipe 25 %, issue slots 45 %.  The rest is the first tile (5 us: lengths,
+// table, codes, cold instructions), the segment's end (2 us) and the second launch (3 us).  Without the copies 44 us; one partial for each stream and
+// copy 45; tiles of 128 keys have no room for two places; one fence for K and V 36; e4m3 operands would need e4m3 weights.
 #include <algorithm>
 
 #include "attend_pages.cuh"
