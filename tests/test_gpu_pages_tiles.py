@@ -39,3 +39,27 @@ def test_scales_far_apart(cuda_device, shape, t, spread):
     codes, exps = filled(p, t)
     q, dq = p.noise(p.b, t, p.h, p.d, spread=3.0)
     check_attend(p, q, *attend(p, dq), None, p.d ** -0.5, codes=codes, exps=exps)
+
+
+def test_calls_at_once_on_two_streams(cuda_device):
+    """Caches of their own, workspaces of their own: what they give is what they give one after another, every time."""
+    calls = []
+    for seed, (shape, t) in enumerate([("llama", 16), ("llama", 1), ("small", 40), ("qwen", 5)]):
+        p = Paged(cuda_device, shape, [2000, 70, 900], seed=seed)
+        filled(p, t)
+        dq = p.noise(p.b, t, p.h, p.d)[1]
+        calls.append((p, dq, p.ctx.attend_pages_workspace(p.pages, t), attend(p, dq)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(cuda_device) for _ in calls]
+    for _ in range(10):
+        outs = []
+        for (p, dq, ws, _), stream in zip(calls, streams):
+            out, lse = torch.empty_like(dq), torch.empty(dq.shape[:3], device=p.device)
+            stream.wait_stream(torch.cuda.current_stream())
+            for _ in range(3):
+                p.ctx.attend_pages(p.pages, dq, p.d ** -0.5, out, ws, lse=lse, stream=stream)
+            outs.append((out, lse))
+        torch.cuda.synchronize()
+        for (p, _, _, want), got in zip(calls, outs):
+            assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert all(p.ctx.poll_device_status() == 0 for p, *_ in calls)
