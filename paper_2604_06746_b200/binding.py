@@ -158,7 +158,7 @@ class PagesStruct(ctypes.Structure):
 
 class RopeStruct(ctypes.Structure):
     """structkv_rope."""
-    _fields_ = [("dim", _i), ("interleaved", _i), ("amplitude", _f), ("step", ctypes.c_ulonglong * (MAX_ROPE_DIM // 2))]
+    _fields_ = [("dim", _i), ("interleaved", _i), ("amplitude", ctypes.c_double), ("step", ctypes.c_ulonglong * (MAX_ROPE_DIM // 2))]
 
 
 _d = ctypes.c_double

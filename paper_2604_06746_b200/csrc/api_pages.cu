@@ -23,14 +23,15 @@ bool on_device(const structkv_ctx* ctx) {
 }
 bool steps_16(int elem, long long a, long long b, long long c) { return (a * elem) % 16 == 0 && (b * elem) % 16 == 0 && (c * elem) % 16 == 0; }
 bool rope_ok(const structkv_ctx* ctx, const structkv_rope* r) {
-  return r && r->dim >= 2 && r->dim % 2 == 0 && r->dim <= ctx->c.cfg.head_dim && std::isfinite(r->amplitude);
+  return r && r->dim >= 2 && r->dim % 2 == 0 && r->dim <= ctx->c.cfg.head_dim && std::isfinite((float)r->amplitude);
 }
 RopeArgs rope_args(const structkv_rope* r) {
   RopeArgs a{};
   if (!r) return a;
   a.dim = r->dim;
   a.interleaved = r->interleaved != 0;
-  a.amplitude = r->amplitude;
+  a.amplitude = (float)r->amplitude;
+  a.amplitude64 = r->amplitude;
   std::memcpy(a.step, r->step, sizeof(a.step));
   return a;
 }
@@ -114,7 +115,7 @@ structkv_status structkv_rope_init(structkv_rope* rope, int dim, int interleaved
   structkv_rope r{};
   r.dim = dim;
   r.interleaved = interleaved != 0;
-  r.amplitude = scaling == STRUCTKV_ROPE_RAMP && factor > 1.0 ? (float)(0.1L * logl(by) + 1.0L) : 1.0f;
+  r.amplitude = scaling == STRUCTKV_ROPE_RAMP && factor > 1.0 ? (double)(0.1L * logl(by) + 1.0L) : 1.0;
   for (int c = 0; c < dim / 2; ++c) {
     long double f = powl(b, -2.0L * c / dim);
     if (scaling == STRUCTKV_ROPE_LINEAR) f /= by;

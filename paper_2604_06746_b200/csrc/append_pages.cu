@@ -2,13 +2,17 @@
 //
 // A CTA has one block of 16 slots of a sequence and K and V of one head or of four.  A lane has two chunks of 16 bytes of one row, of all those
 // heads: their angles are worked out once, and all of a lane's loads are in flight together (of four heads to places of its own in shared
-// memory, which leaves registers for seven CTAs an SM: 16384 rows 26.7 to 23.4 us).  The blocks' largest magnitudes meet in shared memory; then
+// memory, which leaves registers for six CTAs an SM: 16384 rows 26.7 to 23.4 us).  The blocks' largest magnitudes meet in shared memory; then
 // every row goes through the rotation once more and becomes codes, so that nothing but the rows as they came is held meanwhile and every
 // element is read once.  Further CTAs rotate the queries that came along.
 //
-// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 23.4 us, 4.3 TB/s, 66 % of a measured copy; issue slots are the next bound (12
-// instructions an element: angles 2, rotation twice, maximum, scale, code), then the chain counts -> index -> rows -> scale -> codes, which seven CTAs
-// an SM hide.  One token of 16 sequences with its queries: 3.7 us, a launch's latency.
+// Codes of K are those nearest to the rotated values, which fp32 cannot always tell: values a little larger and a little smaller are coded, and where
+// these codes differ (one lane of some thousand), the lane's pairs are rotated in fp64.  That takes 2 us of the 25.6 below; at the end of the CTA instead of
+// where it is found it took 5.
+//
+// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 25.6 us, 3.9 TB/s, 60 % of a measured copy; issue slots are the next bound (13
+// instructions an element: angles 2, rotation twice, maximum, scale, codes), then the chain counts -> index -> rows -> scale -> codes, which six CTAs
+// an SM hide.  One token of 16 sequences with its queries: 3.8 us, a launch's latency.
 #include <algorithm>
 
 #include "pages.cuh"
@@ -30,6 +34,11 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
   return (uint32_t)lo | (uint32_t)hi << 16;
+}
+// The code nearest to y: a number of 24 bits that lies on the same side of every border (its last bit says that more follows).
+__device__ __forceinline__ float sticky(double y) {
+  const float f = __double2float_rz(y);
+  return (double)f == y || y != y ? f : __uint_as_float(__float_as_uint(f) | 1u);
 }
 // Two codes times a power of two (as two fp16), rounded anew.  (In fp16 the product is exact down to 2^-24, far below half of e4m3's
 // smallest number, 2^-10.)
@@ -71,7 +80,8 @@ template <typename T, int D, Pairing P, int HEADS>
 struct AppendShape {
   static constexpr int N = kPairs<T>, kJobs = 2 * HEADS, kLanes = D / (2 * N), kThreads = kBlockSlots * kLanes;
   static constexpr bool kStaged = HEADS > 1 && P != SINGLE;
-  static constexpr int kSmem = kStaged ? kJobs * 2 * kThreads * 16 : 0, kPer = (kStaged ? sizeof(T) == 2 ? 896 : 768 : 512) / kThreads;
+  static constexpr int kUnroll = kStaged ? 1 : 2 * HEADS;         // (of heads; registers have no index)
+  static constexpr int kSmem = kStaged ? kJobs * 2 * kThreads * 16 : 0, kPer = (kStaged ? 768 : 512) / kThreads;
 };
 
 template <typename T, int D, Pairing P, int HEADS>
@@ -134,7 +144,8 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
     }
   }
   uint64_t cos[N / 2], sin[N / 2];
-  if (any && a.rotated) at.angles(r, steps, is ? a.positions[b * a.s_positions + t] : 0, false, cos, sin);
+  const int position = a.rotated && is ? a.positions[b * a.s_positions + t] : 0;
+  if (any && a.rotated) at.angles(r, steps, position, false, cos, sin);
   if constexpr (S::kStaged) copies_landed();
   auto raw_of = [&](int j) {
     if constexpr (S::kStaged) return typename Place::Raw{*place(j, 0), *place(j, 1)};
@@ -155,10 +166,13 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
   bool infinite = false;
   if (!any && lane < JOBS) tops[lane][warp] = finite_tops[lane][warp] = 0.f;
   if (any)
+#pragma unroll (S::kUnroll)
+  for (int h = 0; h < HEADS; ++h)
 #pragma unroll
-  for (int j = 0; j < JOBS; ++j) {
+  for (int s = 0; s < 2; ++s) {
+    const int j = 2 * h + s;
     float top = 0.f;
-    if (sizeof(T) == 2 && (j & 1 || !a.rotated)) {
+    if (sizeof(T) == 2 && (s || !a.rotated)) {
       top = largest(raw_of(j));
     } else {
       float u[N], v[N];
@@ -174,7 +188,7 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
   if (infinite) {
     // infinities are stored as NaN, and the others' largest is what counts
     if (any)
-#pragma unroll
+#pragma unroll (S::kUnroll)
     for (int j = 0; j < JOBS; ++j) {
       float u[N], v[N], top = 0.f;
       row_of(j, u, v);
@@ -201,14 +215,17 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
     if (warp == 0) *scale = (unsigned char)(e + 127);
   }
   char *const k = a.c.k + page * a.c.s_page + g0 * a.c.s_head + (in_page + tid / LANES) * a.c.s_token, *const v = a.c.v + (k - a.c.k);
+#pragma unroll (S::kUnroll)
+  for (int h = 0; h < HEADS; ++h)
 #pragma unroll
-  for (int j = 0; j < JOBS; ++j) {
+  for (int s = 0; s < 2; ++s) {
+    const int j = 2 * h + s;
     const int ej = __shfl_sync(0xffffffffu, e, j), dj = __shfl_sync(0xffffffffu, down, j);
-    if (j / 2 >= heads) break;
-    char* const out = (j & 1 ? v : k) + (j / 2) * a.c.s_head;
+    if (h >= heads) break;
+    char* const out = (s ? v : k) + h * a.c.s_head;
+    uint32_t differ = 0u;
     if (mine) {
       const float by = __int_as_float((127 - ej) << 23);
-      const uint64_t by2 = pack2(by, by);
       float x[N], y[N], u[N], w[N];
       row_of(j, u, w);
       if (infinite) {
@@ -218,17 +235,32 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
           if (fabsf(w[i]) == INFINITY) w[i] = __int_as_float(0x7fffffff);
         }
       }
-#pragma unroll
-      for (int i = 0; i < N; i += 2) {
-        unpack2(mul2(pack2(u[i], u[i + 1]), by2), u[i], u[i + 1]);
-        unpack2(mul2(pack2(w[i], w[i + 1]), by2), w[i], w[i + 1]);
-      }
       Place::chunks(u, w, x, y);
       uint32_t cx[N / 4], cy[N / 4];
+      auto codes_of = [&](float f, uint32_t (&cx)[N / 4], uint32_t (&cy)[N / 4]) {
+        const uint64_t f2 = pack2(f, f);
+        float p[N], q[N];
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        cx[i] = codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-        cy[i] = codes4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+        for (int i = 0; i < N; i += 2) {
+          unpack2(mul2(pack2(x[i], x[i + 1]), f2), p[i], p[i + 1]);
+          unpack2(mul2(pack2(y[i], y[i + 1]), f2), q[i], q[i + 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+          cx[i] = codes4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
+          cy[i] = codes4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+        }
+      };
+      if (!s && a.rotated) {
+        // What is off by 2^-21 (fp32 is by 2^-23 where a pair's parts do not cancel) has the same code, or 64 bits decide.
+        const float d = P == SINGLE || at.turns(0) ? 0x1p-21f : 0.f;
+        uint32_t lx[N / 4], ly[N / 4];
+        codes_of(fmaf(by, d, by), cx, cy);
+        codes_of(fmaf(by, -d, by), lx, ly);
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) differ |= (cx[i] ^ lx[i]) | (cy[i] ^ ly[i]);
+      } else {
+        codes_of(by, cx, cy);
       }
       if constexpr (P == SINGLE) {
 #pragma unroll
@@ -255,6 +287,32 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
         c.x = scaled2(c.x & 0xffffu, f) | scaled2(c.x >> 16, f) << 16;
         c.y = scaled2(c.y & 0xffffu, f) | scaled2(c.y >> 16, f) << 16;
         at8[i] = c;
+      }
+    }
+    if (!s && a.rotated) {
+      // a lane with a value too close to a border to tell: all that it has of this head, a pair a lane
+#pragma unroll 1
+      for (unsigned left = __ballot_sync(0xffffffffu, differ != 0u); left; left &= left - 1) {
+        const int who = __ffs(left) - 1, its = warp * 32 + who;
+        const int source = __shfl_sync(0xffffffffu, t, who), where = __shfl_sync(0xffffffffu, position, who);
+        __syncwarp();                                             // (its codes are written)
+        if (lane >= N) continue;
+        const Place there(r, its % LANES * N);
+        const int2 el = there.pair(lane);
+        const T* const from = (const T*)(a.k + b * a.s_batch + source * a.s_token + (g0 + h) * a.s_head);
+        double u = (double)(float)from[el.x], w = (double)(float)from[el.y];
+        if (there.turns(lane)) {
+          const double2 cs = cos_sin64(steps[there.p0 + lane], where);
+          const double c = cs.x * r.amplitude64, d = cs.y * r.amplitude64, y = fma(u, c, w * -d);
+          w = fma(w, c, u * d);
+          u = y;
+        }
+        const double by = __longlong_as_double((long long)(1023 - ej) << 52);
+        auto scaled = [&](double y) { return fabs(y) <= 3.4028234663852886e38 ? sticky(y * by) : __int_as_float(0x7fffffff); };
+        const uint32_t codes = codes4(scaled(u), scaled(w), 0.f, 0.f);
+        char* const to = out + (its / LANES - tid / LANES) * a.c.s_token;
+        to[el.x] = (char)codes;
+        to[el.y] = (char)(codes >> 8);
       }
     }
   }

@@ -8,6 +8,7 @@ namespace skv {
 struct RopeArgs {
   int dim, interleaved;
   float amplitude;
+  double amplitude64;
   unsigned long long step[STRUCTKV_ROPE_MAX_DIM / 2];
 };
 
@@ -35,6 +36,20 @@ __device__ __forceinline__ float2 cos_sin(int turn, float amplitude) {
 
 __device__ __forceinline__ void put(__nv_bfloat16* at, float x) { *at = __float2bfloat16(x); }
 __device__ __forceinline__ void put(float* at, float x) { *at = x; }
+
+// The same in 64 bits (Taylor's polynomials within an eighth of a turn, 2^-41).
+__device__ __forceinline__ double2 cos_sin64(unsigned long long step, int position) {
+  const double turn = (double)(long long)(step * (unsigned long long)(long long)position) * 0x1p-64, quarter = rint(4.0 * turn);
+  const double x = fma(quarter, -0.25, turn) * 6.283185307179586, z = x * x;
+  double s = 1.0 / 6227020800.0, c = 1.0 / 479001600.0;
+  s = fma(s, z, -1.0 / 39916800.0); s = fma(s, z, 1.0 / 362880.0); s = fma(s, z, -1.0 / 5040.0); s = fma(s, z, 1.0 / 120.0); s = fma(s, z, -1.0 / 6.0);
+  c = fma(c, z, -1.0 / 3628800.0); c = fma(c, z, 1.0 / 40320.0); c = fma(c, z, -1.0 / 720.0); c = fma(c, z, 1.0 / 24.0); c = fma(c, z, -0.5);
+  s = fma(s * z, x, x);
+  c = fma(c, z, 1.0);
+  const int k = (int)quarter & 3;
+  const double a = k & 1 ? s : c, b = k & 1 ? c : s;
+  return make_double2(k + 1 & 2 ? -a : a, k & 2 ? -b : b);
+}
 
 // How a head's D elements form pairs for a lane that has N of them from pair p0 on, as two chunks of N elements at `a` and `b`:
 // HALVES: element i of one with element i of the other, the pairs (c, c + dim / 2), and behind them, not turned, (c, c + (D - dim) / 2);
