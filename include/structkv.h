@@ -684,8 +684,8 @@ typedef struct {
  * caller adds them.  Row r of sequence b comes from source token t = index[b, r], or r without an index, and has its position.
  * A block of STRUCTKV_SCALE_BLOCK slots gets the smallest e, at least -40, with which its largest finite magnitude stays within 448 * 2^e;
  * where it holds tokens already, the larger of that and the e that it has, to which their codes are rounded (to nearest, ties to even)
- * anew.  What is not finite in fp32 becomes NaN.  A code is the nearest one to the rotated value, to about 2^-40 of it
- * (rotated in fp32, and anew in fp64 where that is too close to a border between two codes to tell).
+ * anew.  What is not finite in fp32 becomes NaN.  Codes are those of the rotated values rounded to fp32 (which are worked
+ * out in fp32, and in fp64 where that is too close to a border between two codes to tell).
  *   k, v        device, element (b, t, g, c) at k + b*stride_batch + t*stride_token + g*stride_head + c, dtype of the context
  *               (bases 16-byte aligned, strides multiples of 16 bytes, any order, 0 for a dimension that is broadcast).
  *   tokens      source tokens of a sequence.

@@ -6,7 +6,7 @@
 // every row goes through the rotation once more and becomes codes, so that nothing but the rows as they came is held meanwhile and every
 // element is read once.  Further CTAs rotate the queries that came along.
 //
-// Codes of K are those nearest to the rotated values, which fp32 cannot always tell: values a little larger and a little smaller are coded, and where
+// Codes of K are those of the rotated values rounded once to fp32, which work in fp32 cannot always tell: values a little larger and a little smaller are coded, and where
 // these codes differ (one lane of some thousand), the lane's pairs are rotated in fp64.  That takes 2 us of the 25.6 below; at the end of the CTA instead of
 // where it is found it took 5.
 //
@@ -34,11 +34,6 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
   return (uint32_t)lo | (uint32_t)hi << 16;
-}
-// The code nearest to y: a number of 24 bits that lies on the same side of every border (its last bit says that more follows).
-__device__ __forceinline__ float sticky(double y) {
-  const float f = __double2float_rz(y);
-  return (double)f == y || y != y ? f : __uint_as_float(__float_as_uint(f) | 1u);
 }
 // Two codes times a power of two (as two fp16), rounded anew.  (In fp16 the product is exact down to 2^-24, far below half of e4m3's
 // smallest number, 2^-10.)
@@ -252,8 +247,8 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
         }
       };
       if (!s && a.rotated) {
-        // What is off by 2^-21 (fp32 is by 2^-23 where a pair's parts do not cancel) has the same code, or 64 bits decide.
-        const float d = P == SINGLE || at.turns(0) ? 0x1p-21f : 0.f;
+        // What is off by 2^-20 (fp32 is by 2^-23 where a pair's parts do not cancel) has the same code, or 64 bits decide.
+        const float d = P == SINGLE || at.turns(0) ? 0x1p-20f : 0.f;
         uint32_t lx[N / 4], ly[N / 4];
         codes_of(fmaf(by, d, by), cx, cy);
         codes_of(fmaf(by, -d, by), lx, ly);
@@ -307,9 +302,9 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
           w = fma(w, c, u * d);
           u = y;
         }
-        const double by = __longlong_as_double((long long)(1023 - ej) << 52);
-        auto scaled = [&](double y) { return fabs(y) <= 3.4028234663852886e38 ? sticky(y * by) : __int_as_float(0x7fffffff); };
-        const uint32_t codes = codes4(scaled(u), scaled(w), 0.f, 0.f);
+        const float by = __int_as_float((127 - ej) << 23), y = (float)u, z = (float)w;
+        auto finite = [](float f) { return fabsf(f) == INFINITY ? __int_as_float(0x7fffffff) : f; };
+        const uint32_t codes = codes4(finite(y) * by, finite(z) * by, 0.f, 0.f);
         char* const to = out + (its / LANES - tid / LANES) * a.c.s_token;
         to[el.x] = (char)codes;
         to[el.y] = (char)(codes >> 8);
