@@ -61,3 +61,32 @@ def test_the_same_as_sequence_after_sequence(cuda_device, shape, dtype, more):
         for which in "kv":
             assert np.array_equal(got[which], want[which])
     assert p.ctx.poll_device_status() == 0 and o.ctx.poll_device_status() == 0
+
+
+@pytest.mark.parametrize("more", [dict(scaling="ramp", factor=32.0, original=32768, slow=1.0, fast=32.0), dict(interleaved=True)])
+def test_codes_of_rotated_rows_to_the_last_bit(cuda_device, more):
+    """17 million values of K: each has the code of the value in 64 bits, rounded to fp32 (those of which much cancels, where fp32 is off by more of
+    what is left, are not compared)."""
+    from oracle import pages_oracle as P
+    from paper_2604_06746_b200 import binding
+    n = 16384
+    p = Paged(cuda_device, "llama", [0], 256, spare=n, seed=20)
+    k, v = (torch.randn((1, n, p.g, p.d), generator=torch.Generator().manual_seed(i)).to(BF).to(p.device) for i in (21, 22))
+    positions = torch.arange(n, dtype=torch.int32, device=p.device) * 61 + 5
+    p.ctx.append_pages(p.pages, k, v, positions=positions, rope=binding.Rope(p.d, **more))
+    inter = more.get("interleaved", False)
+    f, amp = P.frequencies(p.d, 10000.0, **{x: y for x, y in more.items() if x != "interleaved"})
+    angle = positions.double()[:, None, None] * torch.tensor(f, device=p.device, dtype=torch.float64)
+    first, second = P.pairs(p.d, inter)
+    a, b = k[0].double()[..., first], k[0].double()[..., second]
+    y, size = torch.empty(n, p.g, p.d, dtype=torch.float64, device=p.device), torch.empty(n, p.g, p.d, dtype=torch.float64, device=p.device)
+    y[..., first], y[..., second] = amp * (a * angle.cos() - b * angle.sin()), amp * (b * angle.cos() + a * angle.sin())
+    size[..., first] = size[..., second] = amp * (a.abs() + b.abs())
+    table = p.dtable[0, :n // 256].long()
+    codes = p.pages.k[table].view(torch.uint8).transpose(1, 2).reshape(n, p.g, p.d)
+    e = (p.pages.k_scales[table].view(torch.uint8).int() - 127).transpose(1, 2).reshape(n // 16, p.g).repeat_interleave(16, 0)[..., None]
+    scaled = y.float() * torch.exp2(-e.float())
+    want = scaled.to(torch.float8_e4m3fn).view(torch.uint8)
+    # fp32 is off by 2^-23 of the parts' size at most, and what is off by 2^-20 of the value is looked at again; below 2^-6 codes are steps of one size
+    compared = (y.abs() > size / 8) & (scaled.abs() > 2.0 ** -6)
+    assert compared.float().mean() > 0.8 and (codes[compared] == want[compared]).all()
