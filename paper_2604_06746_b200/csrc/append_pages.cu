@@ -20,7 +20,7 @@
 namespace skv {
 namespace {
 
-constexpr int kManyHeads = 4;                                     // of a CTA, where there are many blocks; else one  (two: 27.9 us for 26.9)
+constexpr int kManyHeads = 4;                                     // of a CTA, where there are many blocks; else one  (16384 rows by two heads: 6 % more)
 template <typename T>
 constexpr int kPairs = 16 / sizeof(T);                            // a lane's of a row: two chunks of 16 bytes
 
@@ -329,7 +329,8 @@ struct Launch {
 
 }  // namespace
 
-// One head a CTA as long as there are few: 2 x 1000 tokens (1008 CTAs) 6.3 us, four heads a CTA 8.2; 4 x 1000 (2016 CTAs) 10.2, four heads 9.1.
+// One head a CTA as long as there are few: 2 x 1000 tokens (1008 CTAs) 6.6 us, four heads a CTA 7.9; 4 x 1000 (2016 CTAs) 10.8, four heads 10.4;
+// 64 x 64 (2560) 13.1 and 10.4.
 int append_splits(long long blocks, int n_kv, int sms) { return blocks * n_kv <= 8ll * sms || n_kv == 1 ? n_kv : (n_kv + kManyHeads - 1) / kManyHeads; }
 
 cudaError_t launch_append_pages(const Ctx& ctx, const RopeArgs& r, const AppendPagesArgs& a, cudaStream_t st) {
