@@ -331,7 +331,8 @@ class PagedDecode:
     """Decoding over a paged cache in 8 bits, for what a Prefill kept or for prompts whose keys come here.  Pages are shared out by
     ``reserve`` and given back by ``release``; page numbers, table and lengths are the same for all layers, of which each has storage of its
     own.  A step is ``step`` for every layer, with one new token a sequence or up to ``max_new``, then ``advance`` by as many as stay:
-    tokens behind ``lengths`` do not count, and the next ones take their slots.  With a ``rope`` new keys and queries come without positions
+    tokens behind ``lengths`` do not count, and the next ones take their slots.  Only ``take`` and ``advance`` move ``lengths``, the latter within
+    the pages that a sequence has.  With a ``rope`` new keys and queries come without positions
     and are rotated on the way.  Every call but ``reserve`` and ``release`` can be captured into a graph.  A sequence without room is left
     as it is, and ``ctx.poll_device_status`` says so."""
 
@@ -355,6 +356,10 @@ class PagedDecode:
             ws = self.ctx.attend_pages_workspace(self.layers[0], t)
             self._ws = ws if ws.numel() > self._ws.numel() else self._ws
         self._free, self._have = list(range(pages)), [[] for _ in range(batch)]
+        self._room = torch.zeros((batch,), dtype=torch.int32, device=dev)             # slots of the pages that a sequence has
+        one = (batch, n_kv_heads, 1)                            # (by which advance() tells the status word; never a token in it)
+        self._asked = binding.Cache(*(torch.zeros(one + (head_dim,), dtype=dtype, device=dev) for _ in range(2)),
+                                    torch.zeros(one, dtype=torch.int32, device=dev), None, torch.zeros(one[:2], dtype=torch.int32, device=dev))
 
     def _part(self, p: binding.Pages, b: int) -> binding.Pages:
         return binding.Pages(p.k, p.v, p.k_scales, p.v_scales, self.table[b:b + 1], self.lengths[b:b + 1])
@@ -368,6 +373,7 @@ class PagedDecode:
         if more:
             self.table[sequence, len(have):need] = torch.tensor(more, dtype=torch.int32, device=self.table.device)
             have += more
+            self._room[sequence] = need * self.page_size
 
     def release(self, sequence: int) -> None:
         """The sequence ends: its pages are free again.  (Calls that read them were made before, on the same stream.)"""
@@ -375,6 +381,7 @@ class PagedDecode:
         self._have[sequence] = []
         self.table[sequence] = -1
         self.lengths[sequence] = 0
+        self._room[sequence] = 0
 
     def take(self, prefill: Prefill, sequence: int = 0) -> None:
         """The sequence begins with the prompt that ``prefill`` compacted: its K (rotated, as it was scored) and V.  ``reserve`` comes first."""
@@ -415,5 +422,11 @@ class PagedDecode:
         self.ctx.attend_pages(self.layers[layer], q, scale, out, self._ws, counts=counts, softcap=self.softcap, lse=lse)
 
     def advance(self, n_new) -> None:
-        """After the last layer: the first ``n_new`` of the new tokens stay (a number, or int32 ``[batch]`` on the device)."""
-        self.lengths += n_new
+        """After the last layer: the first ``n_new`` of the new tokens stay: a number, for every sequence that has pages, or int32 ``[batch]``
+        on the device.  A sequence whose pages do not hold as many is left as it is, and ``ctx.poll_device_status`` says so."""
+        # (int64 where a number is multiplied: what 32 bits do not hold is refused too)
+        n = n_new if isinstance(n_new, torch.Tensor) and n_new.dim() else (self._room > 0) * n_new
+        grown = self.lengths + n
+        fits = (grown >= 0) & (grown <= self._room)
+        self.lengths += fits * n
+        self.ctx.commit(self._asked, 1, counts=fits.to(torch.int32) - 1)       # (commit refuses a count of -1, and does nothing for 0)
