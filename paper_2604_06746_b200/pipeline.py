@@ -357,6 +357,8 @@ class PagedDecode:
             self._ws = ws if ws.numel() > self._ws.numel() else self._ws
         self._free, self._have = list(range(pages)), [[] for _ in range(batch)]
         self._room = torch.zeros((batch,), dtype=torch.int32, device=dev)             # slots of the pages that a sequence has
+        self._nth = torch.arange(1, max_new + 1, dtype=torch.int32, device=dev)
+        self._counts = torch.zeros((max_new, batch), dtype=torch.int32, device=dev)   # row n - 1: n where a sequence has pages, else 0
         one = (batch, n_kv_heads, 1)                            # (by which advance() tells the status word; never a token in it)
         self._asked = binding.Cache(*(torch.zeros(one + (head_dim,), dtype=dtype, device=dev) for _ in range(2)),
                                     torch.zeros(one, dtype=torch.int32, device=dev), None, torch.zeros(one[:2], dtype=torch.int32, device=dev))
@@ -374,6 +376,7 @@ class PagedDecode:
             self.table[sequence, len(have):need] = torch.tensor(more, dtype=torch.int32, device=self.table.device)
             have += more
             self._room[sequence] = need * self.page_size
+            self._counts[:, sequence] = self._nth
 
     def release(self, sequence: int) -> None:
         """The sequence ends: its pages are free again.  (Calls that read them were made before, on the same stream.)"""
@@ -382,6 +385,7 @@ class PagedDecode:
         self.table[sequence] = -1
         self.lengths[sequence] = 0
         self._room[sequence] = 0
+        self._counts[:, sequence] = 0
 
     def take(self, prefill: Prefill, sequence: int = 0) -> None:
         """The sequence begins with the prompt that ``prefill`` compacted: its K (rotated, as it was scored) and V.  ``reserve`` comes first."""
@@ -407,10 +411,13 @@ class PagedDecode:
     def step(self, layer: int, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, positions: Optional[torch.Tensor], scale: float,
              out: torch.Tensor, counts: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> None:
         """New tokens, ``q``, ``out [batch, n_new, H, d]``, ``k_new``, ``v_new [batch, n_new, H_kv, d]``, ``counts [batch]`` of them for each
-        sequence (None: all): they are rotated (with a rope), appended, and see the cache and those before them."""
+        sequence (None: all, of the sequences that have pages): they are rotated (with a rope), appended, and see the cache and those before
+        them."""
         b, n, h, d = q.shape
         if n > self.max_new:
             raise ValueError("step: more tokens than max_new")
+        if counts is None and n:
+            counts = self._counts[n - 1]
         if self.rope is not None:
             if positions is None:
                 raise ValueError("step: positions come with a rope")

@@ -110,3 +110,31 @@ def test_no_room_in_a_captured_step(cuda_device):
     torch.cuda.synchronize()
     assert dec.lengths.tolist() == [64, 33, 0] and out[1].abs().sum() > 0 and (out[2] == 0).all()
     assert dec.ctx.poll_device_status() == binding.ERR_INVALID_ARG              # (the first is full)
+
+
+@pytest.mark.parametrize("n", [1, 3])
+def test_a_batch_that_is_not_full_is_no_mistake(cuda_device, n):
+    """Steps without counts: the sequence that there is has its results, the other places nothing, and the status word stays clear; in a graph too,
+    whose places are filled and emptied between replays."""
+    from paper_2604_06746_b200 import binding
+    dec, own = decode(cuda_device, 16), decode(cuda_device, 1)
+    dec.reserve(5, 40)
+    own.reserve(0, 40)
+    keep(dec, 5, 30, 1)
+    keep(own, 0, 30, 1)
+    for i in range(2):
+        got, want = step(dec, n, 40 + i), step(own, n, 40 + i)
+        dec.advance(1)
+        own.advance(1)
+        assert near(got[:, 5], want[:, 0]) and (got[:, :5] == 0).all() and (got[:, 6:] == 0).all()
+    assert dec.ctx.poll_device_status() == binding.OK and dec.lengths.tolist() == [0] * 5 + [32] + [0] * 10
+    rows = [noise(i, cuda_device, 16, n, h, D) for i, h in enumerate((H, G, G))]
+    out, graph = torch.empty((16, n, H, D), dtype=BF, device=cuda_device), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        dec.step(0, *rows, None, D ** -0.5, out)
+    dec.reserve(9, 16)
+    dec.release(5)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert out[9].abs().sum() > 0 and (out[:9] == 0).all() and (out[10:] == 0).all() and dec.ctx.poll_device_status() == binding.OK

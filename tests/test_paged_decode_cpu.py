@@ -76,3 +76,24 @@ def test_counts_that_cannot_be(monkeypatch):
     dec.release(2)
     dec.advance(2)
     assert dec.lengths.tolist() == [13, 12, 0, 0] and dec.ctx.poll_device_status() == OK
+
+
+def test_a_batch_that_is_not_full_is_no_mistake(monkeypatch):
+    """Places without a sequence have no new tokens: nothing is reported for them, step after step, and a real mistake can be told."""
+    dec = decode(monkeypatch, pages=12, columns=4, batch=5)
+    dec.reserve(1, 40)
+    keep(dec, 1, 30)
+    for n in (1, 4, 2):
+        seen = step(dec, n)
+        assert [len(x) for x in seen] == [0, int(dec.lengths[1]) + n, 0, 0, 0] and dec.ctx.poll_device_status() == OK
+        dec.advance(1)
+    dec.reserve(4, 16)
+    assert [len(x) for x in step(dec, 3)] == [0, 36, 0, 0, 3] and dec.ctx.poll_device_status() == OK
+    # ends, and begins anew
+    dec.release(1)
+    assert [len(x) for x in step(dec, 3)] == [0, 0, 0, 0, 3] and dec.ctx.poll_device_status() == OK
+    dec.reserve(1, 2)
+    assert [len(x) for x in step(dec, 3)] == [0, 3, 0, 0, 3] and dec.ctx.poll_device_status() == OK
+    # counts of the caller's are taken as they are
+    step(dec, 3, counts=torch.tensor([1, 1, 0, 0, 1], dtype=torch.int32))
+    assert dec.ctx.poll_device_status() == INVALID
