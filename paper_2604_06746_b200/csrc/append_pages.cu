@@ -6,11 +6,13 @@
 // every row goes through the rotation once more and becomes codes, so that nothing but the rows as they came is held meanwhile and every
 // element is read once.  Further CTAs rotate the queries that came along.
 //
-// Codes of K are those of the rotated values rounded once to fp32, which work in fp32 cannot always tell: values a little larger and a little smaller are coded, and where
-// these codes differ (one lane of some thousand), the lane's pairs are rotated in fp64.  That takes 2 us of the 25.6 below; at the end of the CTA instead of
-// where it is found it took 5.
+// Codes of K are those of the rotated values rounded once to fp32, which work in fp32 cannot always tell: what a pair may be off by goes with |a| + |b|, not with what is
+// left of them.  The largest and the smallest value that there may be are coded, and where these codes differ (of normal numbers one in 24 thousand, a
+// lane of 1500, a warp's head of 46), the lane's pairs are rotated in fp64.  That takes 1.5 us of the 26.5 below: 0.8 for the two additions to every
+// value, 0.4 for what they add, 0.3 for fp64, whose pairs come from the rows' place in shared memory (from global memory 0.4 more; at the end of the CTA
+// instead of where it is found 3 more).  A part of the value itself instead of its pair's takes 1 us less and gives some ten of 17 million values a neighbour's code.
 //
-// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 25.6 us, 3.9 TB/s, 60 % of a measured copy; issue slots are the next bound (13
+// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 26.5 us, 3.8 TB/s, 58 % of a measured copy; issue slots are the next bound (13
 // instructions an element: angles 2, rotation twice, maximum, scale, codes), then the chain counts -> index -> rows -> scale -> codes, which six CTAs
 // an SM hide.  One token of 16 sequences with its queries: 3.8 us, a launch's latency.
 #include <algorithm>
@@ -221,24 +223,35 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
     uint32_t differ = 0u;
     if (mine) {
       const float by = __int_as_float((127 - ej) << 23);
-      float x[N], y[N], u[N], w[N];
-      row_of(j, u, w);
+      float x[N], y[N], u[N], w[N], off[N];                       // off: what a pair may be off by in fp32 before sums are rounded, in codes' units: below a quarter of the smallest code
+      const bool turns = !s && a.rotated && (P == SINGLE || at.turns(0));
+      Place::pairs(raw_of(j), u, w);
+      if (turns) {
+        const float part = r.off * by;
+#pragma unroll
+        for (int i = 0; i < N; ++i) off[i] = P != SINGLE || at.turns(i) ? fmaf(fabsf(u[i]), part, fabsf(w[i]) * part) : 0.f;
+        at.turn(u, w, cos, sin);
+      }
       if (infinite) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           if (fabsf(u[i]) == INFINITY) u[i] = __int_as_float(0x7fffffff);
           if (fabsf(w[i]) == INFINITY) w[i] = __int_as_float(0x7fffffff);
+          if (turns && !(off[i] < INFINITY)) off[i] = 0.f;
         }
       }
       Place::chunks(u, w, x, y);
       uint32_t cx[N / 4], cy[N / 4];
-      auto codes_of = [&](float f, uint32_t (&cx)[N / 4], uint32_t (&cy)[N / 4]) {
+      // codes of the row times f, of K with what it may be off by added
+      auto codes_of = [&](float f, bool near, uint32_t (&cx)[N / 4], uint32_t (&cy)[N / 4]) {
         const uint64_t f2 = pack2(f, f);
-        float p[N], q[N];
+        float p[N], q[N], ox[N], oy[N];
+        if (near) Place::chunks(off, off, ox, oy);
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-          unpack2(mul2(pack2(x[i], x[i + 1]), f2), p[i], p[i + 1]);
-          unpack2(mul2(pack2(y[i], y[i + 1]), f2), q[i], q[i + 1]);
+          const uint64_t px = pack2(x[i], x[i + 1]), py = pack2(y[i], y[i + 1]);
+          unpack2(near ? fma2(px, f2, pack2(ox[i], ox[i + 1])) : mul2(px, f2), p[i], p[i + 1]);
+          unpack2(near ? fma2(py, f2, pack2(oy[i], oy[i + 1])) : mul2(py, f2), q[i], q[i + 1]);
         }
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
@@ -246,16 +259,16 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
           cy[i] = codes4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
         }
       };
-      if (!s && a.rotated) {
-        // What is off by 2^-20 (fp32 is by 2^-23 where a pair's parts do not cancel) has the same code, or 64 bits decide.
-        const float d = P == SINGLE || at.turns(0) ? 0x1p-20f : 0.f;
+      if (turns) {
+        // The largest value that there may be and, with its sign turned, the smallest (the sum's rounding goes into the factor) have the same code, or
+        // 64 bits decide.  (Their signs differ where both are zeros.)
         uint32_t lx[N / 4], ly[N / 4];
-        codes_of(fmaf(by, d, by), cx, cy);
-        codes_of(fmaf(by, -d, by), lx, ly);
+        codes_of(by * (1.f + 0x1p-23f), true, cx, cy);
+        codes_of(-by * (1.f - 0x1p-23f), true, lx, ly);
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) differ |= (cx[i] ^ lx[i]) | (cy[i] ^ ly[i]);
+        for (int i = 0; i < N / 4; ++i) differ |= ((cx[i] ^ lx[i]) | (cy[i] ^ ly[i])) & 0x7f7f7f7fu;
       } else {
-        codes_of(by, cx, cy);
+        codes_of(by, false, cx, cy);
       }
       if constexpr (P == SINGLE) {
 #pragma unroll
@@ -294,8 +307,16 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
         if (lane >= N) continue;
         const Place there(r, its % LANES * N);
         const int2 el = there.pair(lane);
-        const T* const from = (const T*)(a.k + b * a.s_batch + source * a.s_token + (g0 + h) * a.s_head);
-        double u = (double)(float)from[el.x], w = (double)(float)from[el.y];
+        double u, w;
+        if constexpr (S::kStaged) {
+          const T* const from = (const T*)(staged + (2 * j + (P == NEIGHBOURS && lane >= N / 2)) * S::kThreads + its);
+          u = (double)(float)from[P == HALVES ? lane : 2 * lane % N];
+          w = (double)(float)from[P == HALVES ? S::kThreads * N + lane : 2 * lane % N + 1];
+        } else {
+          const T* const from = (const T*)(a.k + b * a.s_batch + source * a.s_token + (g0 + h) * a.s_head);
+          u = (double)(float)from[el.x];
+          w = (double)(float)from[el.y];
+        }
         if (there.turns(lane)) {
           const double2 cs = cos_sin64(steps[there.p0 + lane], where);
           const double c = cs.x * r.amplitude64, d = cs.y * r.amplitude64, y = fma(u, c, w * -d);
