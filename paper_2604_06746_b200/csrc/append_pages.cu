@@ -8,11 +8,12 @@
 //
 // Codes of K are those of the rotated values rounded once to fp32, which work in fp32 cannot always tell: what a pair may be off by goes with |a| + |b|, not with what is
 // left of them.  The largest and the smallest value that there may be are coded, and where these codes differ (of normal numbers one in 24 thousand, a
-// lane of 1500, a warp's head of 46), the lane's pairs are rotated in fp64.  That takes 1.5 us of the 26.5 below: 0.8 for the two additions to every
+// lane of 1500, a warp's head of 46), the lane's pairs are rotated in fp64.  That takes 1.5 us of the 26.8 below: 0.8 for the two additions to every
 // value, 0.4 for what they add, 0.3 for fp64, whose pairs come from the rows' place in shared memory (from global memory 0.4 more; at the end of the CTA
 // instead of where it is found 3 more).  A part of the value itself instead of its pair's takes 1 us less and gives some ten of 17 million values a neighbour's code.
+// The scale of a block of K whose largest value is as close to a border is decided in fp64 as well.
 //
-// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 26.5 us, 3.8 TB/s, 58 % of a measured copy; issue slots are the next bound (13
+// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 26.8 us, 3.8 TB/s, 57 % of a measured copy; issue slots are the next bound (13
 // instructions an element: angles 2, rotation twice, maximum, scale, codes), then the chain counts -> index -> rows -> scale -> codes, which six CTAs
 // an SM hide.  One token of 16 sequences with its queries: 3.8 us, a launch's latency.
 #include <algorithm>
@@ -31,6 +32,8 @@ __device__ __forceinline__ int exponent_of(float top) {
   const uint32_t w = __float_as_uint(top);
   return max((int)(w >> 23) - 127 - 8 + ((w & 0x7fffffu) > 0x600000u), kLowExponent);
 }
+// Whether `top` lies within 2^-19.8 of a 448 2^e, where that changes.
+__device__ __forceinline__ bool border_near(float top) { return (__float_as_uint(top) & 0x7fffffu) - (0x600000u - 16u) <= 32u; }
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   uint16_t lo, hi;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
@@ -72,6 +75,18 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// A pair turned in 64 bits and rounded to fp32 (`turns` not: as it is); what is not finite then is NaN.
+__device__ __forceinline__ float2 exact_pair(double u, double v, bool turns, unsigned long long step, int position, double amplitude) {
+  if (turns) {
+    const double2 cs = cos_sin64(step, position);
+    const double c = cs.x * amplitude, s = cs.y * amplitude, y = fma(u, c, v * -s);
+    v = fma(v, c, u * s);
+    u = y;
+  }
+  const float x = (float)u, y = (float)v;
+  return make_float2(fabsf(x) == INFINITY ? __int_as_float(0x7fffffff) : x, fabsf(y) == INFINITY ? __int_as_float(0x7fffffff) : y);
+}
+
 // A CTA for K and V of HEADS heads.  Of many heads a lane's rows wait in shared memory, in places of its own, and registers are left for more CTAs.
 template <typename T, int D, Pairing P, int HEADS>
 struct AppendShape {
@@ -87,7 +102,7 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
   constexpr int N = S::N, JOBS = S::kJobs, LANES = S::kLanes, WARPS = S::kThreads / 32;
   extern __shared__ __align__(16) uint4 staged[];                 // [job][chunk][lane]
   using Place = PairPlace<T, D, P, N>;
-  __shared__ float tops[JOBS][WARPS], finite_tops[JOBS][WARPS];
+  __shared__ float tops[JOBS][WARPS], exact_tops[JOBS][WARPS];
   __shared__ __align__(16) unsigned long long steps[D / 2];       // (lanes read different ones: from the arguments one after another)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, p0 = (tid % LANES) * N;
   pdl_trigger();
@@ -161,7 +176,7 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
                                (((size_t)page * a.c.n_kv + g0 + (job ? lane / 2 : 0)) << (a.c.page_shift - kBlockShift)) + (in_page >> kBlockShift);
   const int had = job && slot0 < n ? (int)*scale - 127 : -127;
   bool infinite = false;
-  if (!any && lane < JOBS) tops[lane][warp] = finite_tops[lane][warp] = 0.f;
+  if (!any && lane < JOBS) tops[lane][warp] = exact_tops[lane][warp] = 0.f;
   if (any)
 #pragma unroll (S::kUnroll)
   for (int h = 0; h < HEADS; ++h)
@@ -182,28 +197,38 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
     if (lane == 0) tops[j][warp] = top;
   }
   infinite = __syncthreads_or(infinite);
-  if (infinite) {
-    // infinities are stored as NaN, and the others' largest is what counts
-    if (any)
-#pragma unroll (S::kUnroll)
-    for (int j = 0; j < JOBS; ++j) {
-      float u[N], v[N], top = 0.f;
-      row_of(j, u, v);
+  auto of_warps = [&](const float (&x)[JOBS][WARPS]) {
+    float top = 0.f;
 #pragma unroll
+    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, x[lane][w]);
+    return top;
+  };
+  float top = job ? of_warps(tops) : 0.f;
+  // A pair's |a| + |b| is at most twice its larger result, so that the largest of K is off by a part of 2^-21.4 of it, with an amplitude 2^-20.6: where that is
+  // too close to a border between two scales to tell, 64 bits decide.  Infinities are stored as NaN, and the others' largest is what counts.
+  const bool unsure = a.rotated && job && !(lane & 1) && border_near(top);
+  if (infinite || __any_sync(0xffffffffu, unsure)) {              // (all warps have the same answer)
+    if (any)
+#pragma unroll 1
+    for (int j = 0; j < 2 * heads; ++j) {
+      const T* const from = (const T*)((j & 1 ? v_from : k_from) + (j / 2) * a.s_head);
+      float largest = 0.f;
+      if (is)
+#pragma unroll 1
       for (int i = 0; i < N; ++i) {
-        if (fabsf(u[i]) != INFINITY) top = fmaxf(top, fabsf(u[i]));
-        if (fabsf(v[i]) != INFINITY) top = fmaxf(top, fabsf(v[i]));
+        const int2 el = at.pair(i);
+        const float2 x = exact_pair((double)(float)from[el.x], (double)(float)from[el.y], !(j & 1) && a.rotated && at.turns(i),
+                                    steps[min(p0 + i, D / 2 - 1)], position, r.amplitude64);
+        largest = fmaxf(largest, fmaxf(fabsf(x.x), fabsf(x.y)));
       }
-      top = across(top);
-      if (lane == 0) finite_tops[j][warp] = top;
+      largest = across(largest);
+      if (lane == 0) exact_tops[j][warp] = largest;
     }
     __syncthreads();
+    if (job) top = of_warps(exact_tops);
   }
   int e = 0, down = 0;                                            // how far older codes go down
   if (job) {
-    float top = 0.f;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, infinite ? finite_tops[lane][w] : tops[lane][w]);
     e = exponent_of(top);
     if (slot0 < n) {
       down = max(0, min(e - had, 24));
@@ -317,15 +342,9 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
           u = (double)(float)from[el.x];
           w = (double)(float)from[el.y];
         }
-        if (there.turns(lane)) {
-          const double2 cs = cos_sin64(steps[there.p0 + lane], where);
-          const double c = cs.x * r.amplitude64, d = cs.y * r.amplitude64, y = fma(u, c, w * -d);
-          w = fma(w, c, u * d);
-          u = y;
-        }
-        const float by = __int_as_float((127 - ej) << 23), y = (float)u, z = (float)w;
-        auto finite = [](float f) { return fabsf(f) == INFINITY ? __int_as_float(0x7fffffff) : f; };
-        const uint32_t codes = codes4(finite(y) * by, finite(z) * by, 0.f, 0.f);
+        const float by = __int_as_float((127 - ej) << 23);
+        const float2 z = exact_pair(u, w, there.turns(lane), steps[min(there.p0 + lane, D / 2 - 1)], where, r.amplitude64);
+        const uint32_t codes = codes4(z.x * by, z.y * by, 0.f, 0.f);
         char* const to = out + (its / LANES - tid / LANES) * a.c.s_token;
         to[el.x] = (char)codes;
         to[el.y] = (char)(codes >> 8);

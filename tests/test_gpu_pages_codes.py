@@ -89,3 +89,31 @@ def test_pairs_of_which_little_is_left(cuda_device, more, tokens):
     a, b = P.pairs(rope.dim, rope.interleaved)
     x[..., a], x[..., b] = r * np.sin(angle + left), r * np.cos(angle + left)
     check(torch.from_numpy(x), positions, F32, rope)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("more", [dict(), RAMP])
+@pytest.mark.parametrize("heads", ["small", "llama"])              # (one head a thread block, four)
+def test_the_largest_value_beside_a_border_of_scales(cuda_device, dtype, more, heads):
+    """One pair a block, turned to a position where one of its values is 448 2^e within some steps of fp32."""
+    from paper_2604_06746_b200 import binding
+    d = 128 if heads == "llama" else 64
+    rope = binding.Rope(d, **more)
+    rng, step = np.random.default_rng(5), np.uint64(rope._struct.step[0])
+    positions = np.arange(1 << 22, dtype=np.uint64)
+    cos, sin = (rope.amplitude * f((positions * step).astype(np.int64) * (2 * np.pi * 2.0 ** -64)) for f in (np.cos, np.sin))
+    rows, at = [], []
+    for _ in range(12):                                            # (a pair reaches 448 at angles of its own)
+        pair = torch.from_numpy(rng.uniform(300, 500, 2) / rope.amplitude).to(dtype).double().numpy() * rng.choice([-1, 1], 2)
+        y = pair[0] * cos - pair[1] * sin
+        close = np.abs(np.abs(y) - 448.0) < 448 * 2.0 ** -21
+        close &= np.abs(pair[1] * cos + pair[0] * sin) < 440       # (the other value is smaller)
+        rows += [pair * 2.0 ** rng.integers(-20, 20)] * int(close.sum())
+        at += positions[close].tolist()
+    assert len(at) > 20, len(at)
+    least = max(len(at), 600 if heads == "llama" else 1)           # (so many blocks that a thread block has four heads)
+    k, where = torch.zeros((16 * least, 8 if heads == "llama" else 2, d)), np.zeros(16 * least, dtype=np.int64)
+    for i in range(least):
+        k[16 * i + i % 16, :, 0], k[16 * i + i % 16, :, d // 2] = (float(x) for x in rows[i % len(at)])
+        where[16 * i + i % 16] = at[i % len(at)]
+    check(k, where, dtype, rope, heads)
