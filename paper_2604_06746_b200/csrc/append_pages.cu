@@ -8,12 +8,12 @@
 //
 // Codes of K are those of the rotated values rounded once to fp32, which work in fp32 cannot always tell: what a pair may be off by goes with |a| + |b|, not with what is
 // left of them.  The largest and the smallest value that there may be are coded, and where these codes differ (of normal numbers one in 24 thousand, a
-// lane of 1500, a warp's head of 46), the lane's pairs are rotated in fp64.  That takes 1.5 us of the 26.8 below: 0.8 for the two additions to every
+// lane of 1500, a warp's head of 46), the lane's pairs are rotated in fp64.  That takes 1.5 us of the 26.9 below: 0.8 for the two additions to every
 // value, 0.4 for what they add, 0.3 for fp64, whose pairs come from the rows' place in shared memory (from global memory 0.4 more; at the end of the CTA
 // instead of where it is found 3 more).  A part of the value itself instead of its pair's takes 1 us less and gives some ten of 17 million values a neighbour's code.
 // The scale of a block of K whose largest value is as close to a border is decided in fp64 as well.
 //
-// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 26.8 us, 3.8 TB/s, 57 % of a measured copy; issue slots are the next bound (13
+// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 26.9 us, 3.7 TB/s, 57 % of a measured copy; issue slots are the next bound (13
 // instructions an element: angles 2, rotation twice, maximum, scale, codes), then the chain counts -> index -> rows -> scale -> codes, which six CTAs
 // an SM hide.  One token of 16 sequences with its queries: 3.8 us, a launch's latency.
 #include <algorithm>
@@ -24,6 +24,7 @@ namespace skv {
 namespace {
 
 constexpr int kManyHeads = 4;                                     // of a CTA, where there are many blocks; else one  (16384 rows by two heads: 6 % more)
+constexpr float kEnd = 0x1.fffp127f;                              // from here on work in fp32 does not tell numbers from infinities
 template <typename T>
 constexpr int kPairs = 16 / sizeof(T);                            // a lane's of a row: two chunks of 16 bytes
 
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
   unsigned char* const scale = (lane & 1 ? a.c.v_scales : a.c.k_scales) +
                                (((size_t)page * a.c.n_kv + g0 + (job ? lane / 2 : 0)) << (a.c.page_shift - kBlockShift)) + (in_page >> kBlockShift);
   const int had = job && slot0 < n ? (int)*scale - 127 : -127;
-  bool infinite = false;
+  bool end = false;                                               // infinities, and numbers that in fp32 may become such or not
   if (!any && lane < JOBS) tops[lane][warp] = exact_tops[lane][warp] = 0.f;
   if (any)
 #pragma unroll (S::kUnroll)
@@ -193,10 +194,10 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
       for (int i = 0; i < N; ++i) top = max3(top, fabsf(u[i]), fabsf(v[i]));
     }
     top = across(top);
-    infinite |= top == INFINITY;
+    end |= top >= kEnd;
     if (lane == 0) tops[j][warp] = top;
   }
-  infinite = __syncthreads_or(infinite);
+  end = __syncthreads_or(end);
   auto of_warps = [&](const float (&x)[JOBS][WARPS]) {
     float top = 0.f;
 #pragma unroll
@@ -207,7 +208,7 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
   // A pair's |a| + |b| is at most twice its larger result, so that the largest of K is off by a part of 2^-21.4 of it, with an amplitude 2^-20.6: where that is
   // too close to a border between two scales to tell, 64 bits decide.  Infinities are stored as NaN, and the others' largest is what counts.
   const bool unsure = a.rotated && job && !(lane & 1) && border_near(top);
-  if (infinite || __any_sync(0xffffffffu, unsure)) {              // (all warps have the same answer)
+  if (end || __any_sync(0xffffffffu, unsure)) {                   // (all warps have the same answer)
     if (any)
 #pragma unroll 1
     for (int j = 0; j < 2 * heads; ++j) {
@@ -257,13 +258,15 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
         for (int i = 0; i < N; ++i) off[i] = P != SINGLE || at.turns(i) ? fmaf(fabsf(u[i]), part, fabsf(w[i]) * part) : 0.f;
         at.turn(u, w, cos, sin);
       }
-      if (infinite) {
+      if (end) {
+        float largest = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
+          largest = max3(largest, fabsf(u[i]), fabsf(w[i]));
           if (fabsf(u[i]) == INFINITY) u[i] = __int_as_float(0x7fffffff);
           if (fabsf(w[i]) == INFINITY) w[i] = __int_as_float(0x7fffffff);
-          if (turns && !(off[i] < INFINITY)) off[i] = 0.f;
         }
+        if (turns && largest >= kEnd) differ = 1u;                // (what overflowed on the way may be a number)
       }
       Place::chunks(u, w, x, y);
       uint32_t cx[N / 4], cy[N / 4];

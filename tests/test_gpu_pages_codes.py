@@ -117,3 +117,23 @@ def test_the_largest_value_beside_a_border_of_scales(cuda_device, dtype, more, h
         k[16 * i + i % 16, :, 0], k[16 * i + i % 16, :, d // 2] = (float(x) for x in rows[i % len(at)])
         where[16 * i + i % 16] = at[i % len(at)]
     check(k, where, dtype, rope, heads)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("more", [RAMP, dict(), RAMP | dict(dim=44)])
+@pytest.mark.parametrize("tokens", [48, 9600])
+def test_values_at_the_end_of_the_range(cuda_device, dtype, more, tokens):
+    """Pairs of some 2^127: parts that fp32 does not hold while what is left of them is a number, and numbers beside its largest."""
+    from paper_2604_06746_b200 import binding
+    rope = binding.Rope(**({"dim": 128} | more))
+    rng, positions = np.random.default_rng(8), np.arange(tokens) * 5 + 3
+    x = rng.uniform(0.3, 1.99, (tokens, 8, 128)) * rng.choice([-1, 1], (tokens, 8, 128)) * 2.0 ** 127
+    x[::7] = rng.standard_normal(x[::7].shape)
+    x[16:32] = rng.standard_normal((16, 8, 128))                   # (a block without any)
+    # results within 2^-20 of the end
+    steps = np.array(rope._struct.step[:rope.dim // 2], dtype=np.uint64)
+    angle = (positions.astype(np.uint64)[:, None] * steps).astype(np.int64) * (2 * np.pi * 2.0 ** -64)
+    a, b = P.pairs(rope.dim, rope.interleaved)
+    end = (2.0 ** 128 - 2.0 ** 103) / rope.amplitude * (1 + rng.uniform(-1, 1, angle.shape) * 2.0 ** -20)
+    x[::3, 5, a], x[::3, 5, b] = (end * np.cos(angle))[::3], (-end * np.sin(angle))[::3]
+    check(torch.from_numpy(x), positions, dtype, rope, least=0.9)
