@@ -170,7 +170,7 @@ structkv_status structkv_append_pages(structkv_ctx* ctx, const structkv_pages* p
   if (!steps_16(elem, x->stride_batch, x->stride_token, x->stride_head)) return STRUCTKV_ERR_INVALID_ARG;
   if (x->n_new < 1 || x->n_new > a.c.slots || x->tokens < 1 || (!x->index && x->n_new > x->tokens)) return STRUCTKV_ERR_INVALID_ARG;
   if (((uintptr_t)x->counts | (uintptr_t)x->index | (uintptr_t)x->positions) % 4 || x->index_stride < 0 || x->positions_stride < 0) return STRUCTKV_ERR_INVALID_ARG;
-  if (x->rope && (!rope_ok(ctx, x->rope) || !x->positions)) return STRUCTKV_ERR_INVALID_ARG;
+  if ((x->rope && !rope_ok(ctx, x->rope)) || (x->rope != nullptr) != (x->positions != nullptr)) return STRUCTKV_ERR_INVALID_ARG;
   if ((x->q != nullptr) != (x->q_out != nullptr) || (x->q && (x->index || !x->rope))) return STRUCTKV_ERR_INVALID_ARG;
   const int heads = ctx->c.cfg.n_q_heads;
   if (x->q) {

@@ -594,7 +594,7 @@ PyObject* append_pages(PyObject* const* a) {
   g.counts = words(c, a[8], {c.batch}, "counts: contiguous int32 [batch], on the pages' device");
   g.rope = rope_of(a[7]);
   const Words at = words_of(a[6], c.device, c.batch, tokens, "positions: int32 [batch, tokens] or [tokens], contiguous rows, on the pages' device");
-  require(at.p || !g.rope, "positions come with a rope");
+  require((at.p != nullptr) == (g.rope != nullptr), "positions and a rope come together");
   g.positions = at.p;
   g.positions_stride = at.stride;
   if (a[10] != Py_None) {

@@ -404,7 +404,9 @@ class PagedDecode:
     def keep(self, layer: int, sequence: int, k: torch.Tensor, v: torch.Tensor, index: Optional[torch.Tensor] = None,
              positions: Optional[torch.Tensor] = None) -> None:
         """Rows of one layer's K and V ``[H_kv, N, d]`` go behind the sequence's tokens: those that ``index`` (int32, one list for all heads)
-        names, or all; with ``positions [N]`` K is rotated on the way.  ``advance`` comes after the last layer."""
+        names, or all; with ``positions [N]`` (and a rope) K is rotated on the way.  ``advance`` comes after the last layer."""
+        if positions is not None and self.rope is None:
+            raise ValueError("keep: positions come with a rope")
         rope = self.rope if positions is not None else None
         self.ctx.append_pages(self._of[layer][sequence], k.transpose(0, 1)[None], v.transpose(0, 1)[None], positions=positions, rope=rope, index=index)
 

@@ -138,3 +138,30 @@ def test_a_batch_that_is_not_full_is_no_mistake(cuda_device, n):
     graph.replay()
     torch.cuda.synchronize()
     assert out[9].abs().sum() > 0 and (out[:9] == 0).all() and (out[10:] == 0).all() and dec.ctx.poll_device_status() == binding.OK
+
+
+def test_positions_without_a_rope_are_refused(cuda_device):
+    """Also where rows are appended by the context, or by the library."""
+    import ctypes
+
+    from paper_2604_06746_b200 import binding
+    dec = decode(cuda_device, 1)
+    dec.reserve(0, 40)
+    p, (k, v) = dec.layers[0], (noise(i, cuda_device, 1, 4, G, D) for i in range(2))
+    positions = torch.arange(4, dtype=torch.int32, device=cuda_device)
+    before = p.k.view(torch.uint8).clone()
+    with pytest.raises(AssertionError):
+        dec.ctx.append_pages(p, k, v, positions=positions)
+    # structkv_append_pages_args, field by field
+    words = [k.data_ptr(), v.data_ptr(), *k.stride()[:3], 4 | 4 << 32, 0, 0, 0, 0, positions.data_ptr(), 0, 0, 0, 0, 0, 0]
+    args = (ctypes.c_longlong * len(words))(*words)
+    call = binding.lib.structkv_append_pages
+    call.restype, call.argtypes = ctypes.c_int, [ctypes.c_void_p] * 4
+    stream = torch.cuda.current_stream().cuda_stream
+    assert call(dec.ctx._h, p.native[0], ctypes.addressof(args), stream) == binding.ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert torch.equal(before, p.k.view(torch.uint8))
+    args[10] = 0
+    assert call(dec.ctx._h, p.native[0], ctypes.addressof(args), stream) == binding.OK
+    torch.cuda.synchronize()
+    assert not torch.equal(before, p.k.view(torch.uint8)) and dec.ctx.poll_device_status() == binding.OK

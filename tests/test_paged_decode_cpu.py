@@ -1,5 +1,6 @@
 """CPU: how pipeline.PagedDecode counts tokens: what is not there, has no room or no pages does not grow, and a token sees its own sequence's
 slots and nothing else."""
+import pytest
 import torch
 
 from tests.paged_fakes import INVALID, OK, decode, keep, step
@@ -97,3 +98,13 @@ def test_a_batch_that_is_not_full_is_no_mistake(monkeypatch):
     # counts of the caller's are taken as they are
     step(dec, 3, counts=torch.tensor([1, 1, 0, 0, 1], dtype=torch.int32))
     assert dec.ctx.poll_device_status() == INVALID
+
+
+def test_positions_without_a_rope_are_refused(monkeypatch):
+    """keep() would store K as it is where its caller expects it to be rotated."""
+    dec = decode(monkeypatch, pages=4, columns=2, batch=1)
+    dec.reserve(0, 20)
+    k, v = (torch.zeros((2, 10, 64), dtype=torch.bfloat16) for _ in range(2))
+    with pytest.raises(ValueError):
+        dec.keep(0, 0, k, v, positions=torch.arange(10, dtype=torch.int32))
+    dec.keep(0, 0, k, v)
