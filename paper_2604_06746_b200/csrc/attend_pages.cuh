@@ -36,7 +36,7 @@ cudaError_t launch_attend_pages_finish(const Ctx& ctx, const AttendPagesArgs& a,
 
 #ifdef __CUDACC__
 
-constexpr float kRaise = 7.f;          // weights are up to 2^(kRaise + kSlack): fp16 keeps those down to 2^-31 of the largest
+constexpr float kRaise = 7.f;          // weights are up to 2^(kRaise + kSlack), the largest above 2^(kRaise - 1): fp16 keeps 11 bits of those down to 2^-20 of it, some down to 2^-30
 constexpr float kNothing = -3.4e38f;   // reference of a row that has seen nothing
 
 // Codes of a word's lower and upper half as two fp16 each.
