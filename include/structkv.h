@@ -684,8 +684,10 @@ typedef struct {
  * caller adds them.  Row r of sequence b comes from source token t = index[b, r], or r without an index, and has its position.
  * A block of STRUCTKV_SCALE_BLOCK slots gets the smallest e, at least -40, with which its largest finite magnitude stays within 448 * 2^e;
  * where it holds tokens already, the larger of that and the e that it has, to which their codes are rounded (to nearest, ties to even)
- * anew.  What is not finite in fp32 becomes NaN.  Codes are those of the rotated values rounded to fp32 (which are worked
- * out in fp32, and in fp64 where that is too close to a border between two codes to tell).
+ * anew.  All rows that are written count, whether they stay or not: where a caller drops some of them (its lengths grow by fewer), the e that
+ * they raised and the older codes that were rounded to it remain.  What is not finite in fp32 becomes NaN.  Scales and codes are those of the
+ * rotated values rounded to fp32 (which are worked out in fp32, and in fp64 where that is too close to a border between two codes or two
+ * scales, or to fp32's end, to tell); a code of zero has either sign.
  *   k, v        device, element (b, t, g, c) at k + b*stride_batch + t*stride_token + g*stride_head + c, dtype of the context
  *               (bases 16-byte aligned, strides multiples of 16 bytes, any order, 0 for a dimension that is broadcast).
  *   tokens      source tokens of a sequence.

@@ -32,11 +32,12 @@ RopeArgs rope_args(const structkv_rope* r) {
   a.interleaved = r->interleaved != 0;
   a.amplitude = (float)r->amplitude;
   a.amplitude64 = r->amplitude;
-  // In units of 2^-24 of the amplitude: cosine or sine and its product's rounding are off by 2.53 at most (all angles were tried), by 1 more where an
-  // amplitude is multiplied in, which rounds, and by what that is off itself.
+  // In units of 2^-24 of amplitude (|a| + |b|): cosine or sine and its product's rounding are off by 2.53 at most (all angles were tried), by 1 more
+  // where an amplitude is multiplied in, which rounds, and by what that is off itself.  amplitude (|a| + |b|) is at most sqrt(2) (|a'| + |b'|), and the
+  // sum is rounded.
   int exponent;
   const double size = std::fabs(r->amplitude), itself = size > 0.0 ? std::fabs(a.amplitude - r->amplitude) / size * 0x1p24 : 0.0;
-  a.off = (float)(size * (2.54 + (std::frexp(size, &exponent) == 0.5 ? 0.0 : 1.0 + itself)) * 0x1p-24);
+  a.off = (float)((std::sqrt(2.0) * (2.54 + (std::frexp(size, &exponent) == 0.5 ? 0.0 : 1.0 + itself)) + 1.0) * 0x1p-24);
   std::memcpy(a.step, r->step, sizeof(a.step));
   return a;
 }

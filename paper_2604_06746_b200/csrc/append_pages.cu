@@ -6,16 +6,17 @@
 // every row goes through the rotation once more and becomes codes, so that nothing but the rows as they came is held meanwhile and every
 // element is read once.  Further CTAs rotate the queries that came along.
 //
-// Codes of K are those of the rotated values rounded once to fp32, which work in fp32 cannot always tell: what a pair may be off by goes with |a| + |b|, not with what is
-// left of them.  The largest and the smallest value that there may be are coded, and where these codes differ (of normal numbers one in 24 thousand, a
-// lane of 1500, a warp's head of 46), the lane's pairs are rotated in fp64.  That takes 1.5 us of the 26.9 below: 0.8 for the two additions to every
-// value, 0.4 for what they add, 0.3 for fp64, whose pairs come from the rows' place in shared memory (from global memory 0.4 more; at the end of the CTA
-// instead of where it is found 3 more).  A part of the value itself instead of its pair's takes 1 us less and gives some ten of 17 million values a neighbour's code.
-// The scale of a block of K whose largest value is as close to a border is decided in fp64 as well.
+// Codes of K are those of the rotated values rounded once to fp32, which work in fp32 cannot always tell: what a pair may be off by goes with |a| + |b|, not
+// with what is left of them.  The largest and the smallest value that there may be are coded, and where these codes differ (of normal numbers one in 17
+// thousand, a lane of 1100, a warp's head of 35), the lane's pairs are rotated in fp64, as they are for the scale of a block whose largest value is as
+// close to a border between two scales.  All that takes 0.8 us of the 25.9 below: where pairs come to fp64 from global memory, not from the rows'
+// place in shared memory, 0.4 more; with |a| + |b| of the pair as it came, which would send a third fewer there, 1.0 more; at the end of the CTA, not where
+// a value is found, 3 more.
 //
-// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 26.9 us, 3.7 TB/s, 57 % of a measured copy; issue slots are the next bound (13
+// 16384 rows of 131072 (8 heads, d 128, bf16, gathered): 25.9 us, 3.9 TB/s, 59 % of a measured copy; issue slots are the next bound (13
 // instructions an element: angles 2, rotation twice, maximum, scale, codes), then the chain counts -> index -> rows -> scale -> codes, which six CTAs
-// an SM hide.  One token of 16 sequences with its queries: 3.8 us, a launch's latency.
+// an SM hide.  One token of 16 sequences with its queries: 3.7 to 4.4 us, a launch's latency.
+// A part of the head that is no whole number of chunks goes element by element; bf16 then spills 40 bytes of 128 registers.
 #include <algorithm>
 
 #include "pages.cuh"
@@ -249,15 +250,9 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
     uint32_t differ = 0u;
     if (mine) {
       const float by = __int_as_float((127 - ej) << 23);
-      float x[N], y[N], u[N], w[N], off[N];                       // off: what a pair may be off by in fp32 before sums are rounded, in codes' units: below a quarter of the smallest code
+      float u[N], w[N];
       const bool turns = !s && a.rotated && (P == SINGLE || at.turns(0));
-      Place::pairs(raw_of(j), u, w);
-      if (turns) {
-        const float part = r.off * by;
-#pragma unroll
-        for (int i = 0; i < N; ++i) off[i] = P != SINGLE || at.turns(i) ? fmaf(fabsf(u[i]), part, fabsf(w[i]) * part) : 0.f;
-        at.turn(u, w, cos, sin);
-      }
+      row_of(j, u, w);
       if (end) {
         float largest = 0.f;
 #pragma unroll
@@ -268,31 +263,37 @@ __global__ void __launch_bounds__(AppendShape<T, D, P, HEADS>::kThreads, AppendS
         }
         if (turns && largest >= kEnd) differ = 1u;                // (what overflowed on the way may be a number)
       }
-      Place::chunks(u, w, x, y);
       uint32_t cx[N / 4], cy[N / 4];
-      // codes of the row times f, of K with what it may be off by added
+      uint64_t off[N / 2];                                        // what pairs may be off by in fp32, in codes' units: below a quarter of the smallest code
+      if (turns) {
+        const float part = r.off * by;
+        auto of = [&](int i) { return P != SINGLE || at.turns(i) ? fmaf(fabsf(u[i]), part, fabsf(w[i]) * part) : 0.f; };
+#pragma unroll
+        for (int i = 0; i < N; i += 2) off[i / 2] = pack2(of(i), of(i + 1));
+      }
+      // codes of the row times f; near: with what it may be off by added
       auto codes_of = [&](float f, bool near, uint32_t (&cx)[N / 4], uint32_t (&cy)[N / 4]) {
         const uint64_t f2 = pack2(f, f);
-        float p[N], q[N], ox[N], oy[N];
-        if (near) Place::chunks(off, off, ox, oy);
+        float p[N], q[N], x[N], y[N];
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-          const uint64_t px = pack2(x[i], x[i + 1]), py = pack2(y[i], y[i + 1]);
-          unpack2(near ? fma2(px, f2, pack2(ox[i], ox[i + 1])) : mul2(px, f2), p[i], p[i + 1]);
-          unpack2(near ? fma2(py, f2, pack2(oy[i], oy[i + 1])) : mul2(py, f2), q[i], q[i + 1]);
+          const uint64_t pu = pack2(u[i], u[i + 1]), pw = pack2(w[i], w[i + 1]);
+          unpack2(near ? fma2(pu, f2, off[i / 2]) : mul2(pu, f2), p[i], p[i + 1]);
+          unpack2(near ? fma2(pw, f2, off[i / 2]) : mul2(pw, f2), q[i], q[i + 1]);
         }
+        Place::chunks(p, q, x, y);
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-          cx[i] = codes4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
-          cy[i] = codes4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+          cx[i] = codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+          cy[i] = codes4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
         }
       };
       if (turns) {
-        // The largest value that there may be and, with its sign turned, the smallest (the sum's rounding goes into the factor) have the same code, or
-        // 64 bits decide.  (Their signs differ where both are zeros.)
+        // The largest value that there may be and, with its sign turned, the smallest have the same code, or 64 bits decide.  (Their signs differ
+        // where both are zeros.)
         uint32_t lx[N / 4], ly[N / 4];
-        codes_of(by * (1.f + 0x1p-23f), true, cx, cy);
-        codes_of(-by * (1.f - 0x1p-23f), true, lx, ly);
+        codes_of(by, true, cx, cy);
+        codes_of(-by, true, lx, ly);
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) differ |= ((cx[i] ^ lx[i]) | (cy[i] ^ ly[i])) & 0x7f7f7f7fu;
       } else {

@@ -8,7 +8,7 @@ namespace skv {
 struct RopeArgs {
   int dim, interleaved;
   float amplitude;
-  float off;                                                    // what work in fp32 is off by at most before the sum is rounded, of |a| + |b| of a pair
+  float off;                                                    // what a turned pair (a', b') is off by in fp32 at most, of |a'| + |b'|
   double amplitude64;
   unsigned long long step[STRUCTKV_ROPE_MAX_DIM / 2];
 };

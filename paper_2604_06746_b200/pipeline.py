@@ -334,7 +334,8 @@ class PagedDecode:
     tokens behind ``lengths`` do not count, and the next ones take their slots.  Only ``take`` and ``advance`` move ``lengths``, the latter within
     the pages that a sequence has.  With a ``rope`` new keys and queries come without positions
     and are rotated on the way.  Every call but ``reserve`` and ``release`` can be captured into a graph.  A sequence without room is left
-    as it is, and ``ctx.poll_device_status`` says so."""
+    as it is, and ``ctx.poll_device_status`` says so.  Rows that are dropped leave something: where one raised the scale of the 16 slots that
+    kept tokens share with it, those keep the raised scale and the codes that were rounded to it."""
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, pages: int, columns: int, dtype: torch.dtype,
                  batch: int = 1, page_size: int = 64, max_new: int = 1, rope: Optional[binding.Rope] = None, softcap: float = 0.0,

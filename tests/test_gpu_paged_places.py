@@ -165,3 +165,26 @@ def test_positions_without_a_rope_are_refused(cuda_device):
     assert call(dec.ctx._h, p.native[0], ctypes.addressof(args), stream) == binding.OK
     torch.cuda.synchronize()
     assert not torch.equal(before, p.k.view(torch.uint8)) and dec.ctx.poll_device_status() == binding.OK
+
+
+def test_dropped_rows_stay_in_the_scale(cuda_device):
+    """A drafted token far larger than the others is not kept: the block's scale stays raised, its older codes as they were rounded, and they are the
+    statement's of all rows that were written."""
+    import numpy as np
+
+    from oracle import pages_oracle as P
+    dec = decode(cuda_device, 1)
+    dec.reserve(0, 16)
+    kept, draft, after = (noise(i, cuda_device, 1, n, G, D) for i, n in enumerate((5, 3, 1)))
+    draft[0, 2] *= 64.0
+    page, host = dec.layers[0], lambda x: x[0, :, 0].double().cpu().numpy()
+    codes, exps = np.zeros((16, D), dtype=np.uint8), [P.LOW]
+    for x, n in ((kept, 0), (draft, 5), (after, 5)):
+        dec.lengths[0] = n
+        dec.ctx.append_pages(page, x, x)
+        had = exps[0]
+        codes, exps = P.append(codes, exps, n, host(x))
+    torch.cuda.synchronize()
+    at = int(dec.table[0, 0])
+    assert page.v_scales[at, 0, 0].view(torch.uint8).item() - 127 == exps[0] == had > P.append(codes, exps, 0, host(kept))[1][0]
+    assert np.array_equal(page.v[at, 0, :6].view(torch.uint8).cpu().numpy(), codes[:6])
