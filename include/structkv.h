@@ -731,7 +731,8 @@ structkv_status structkv_append_pages(structkv_ctx* ctx, const structkv_pages* p
  *   workspace   device, 256-byte aligned, at least structkv_attend_pages_workspace_bytes() bytes (0 for arguments that are not
  *               valid; slots: table_columns * page_size), caller-owned; calls that share it are ordered by the caller.
  * Codes are exact operands; sums are in fp32; probabilities keep 11 bits for their product with V (22 for fp32 storage) where probability
- * times V's scale is at least 2^-20 (2^-9) of the largest such product of its row, and below that are off by 2^-31 of it.  A NaN in V makes its
+ * times V's scale is at least 2^-20 (2^-9) of the largest such product of its row, and below that are off by 2^-31 of it; a key whose product is below
+ * 2^-118 of the largest counts neither in out nor in lse (V's scales would have to be as far apart for it to matter).  A NaN in V makes its
  * column NaN in every row that sees the token, however small its probability; rows that do not see a token are not
  * reached by it.  Errors: INVALID_ARG, WORKSPACE, CUDA.  Asynchronous on `stream`.
  */

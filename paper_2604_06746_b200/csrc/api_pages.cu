@@ -63,7 +63,8 @@ bool view_of(const structkv_ctx* ctx, const structkv_pages* p, PagesView* v) {
 
 // More than 16 rows of a KV head go to tcgen05, with caps more than 32 (each score's hyperbolic tangent is worked out by 8 warps an SM there, by
 // 8 or 16 here).  Up to 16 rows mma.sync has one pass over the codes, from 17 on two or more.  20 rows over 32 x 4096 keys: 129 us on mma.sync, 100 on
-// tcgen05; over 4 x 8192 39.6, 34.0; over 1 x 4096 14.5, 15.2.  With caps 20 rows over 4 x 8192 43 us and 47, 40 rows 58 and 48.
+// tcgen05; over 4 x 8192 39.6, 34.0; over 1 x 4096 14.5, 15.2 (how many keys there are is known on the device only).  With caps 20 rows over
+// 4 x 8192 43 us and 47, 40 rows 58 and 48.
 PagesPlan plan_of(const structkv_config& cfg, int n_new, int sms, bool capped) {
   const int rows = cfg.n_q_heads / cfg.n_kv_heads * n_new;
   if (cfg.dtype == STRUCTKV_BF16 && rows > (capped ? 32 : 16)) return {rows <= 64 ? 64 : 128, sms, kOverTc};

@@ -12,10 +12,14 @@
 // statistics of its own; nothing is waited for but loads, and a segment's end merges the warps.  References follow a row's maximum only
 // where that outgrows it by 2^kSlack.
 //
-// Single tokens, 32 heads over 8, d 128: 16 x 16384 keys 91 us, 5.9 TB/s, 90 % of a measured copy; 16 sequences of 1 to 5003 keys 20.6 us,
-// 3 TB/s; 1 x 1024 keys 8.9 us, which is two launches and their chains of loads (lengths, table, codes; partials).
-// Four CTAs of four warps an SM (two with 16 rows or fp32): one begins or ends a segment while others stream.  16 x 16384 / 16 ragged: one of 14
-// warps 103 / 25 us, one of 16 98 / 25, two of 7 100 / 22.5, two of 8 92 / 21.6, three of 5 94 / 21.9, four of 4 92 / 21.3.
+// Single tokens, 32 heads over 8, d 128: 16 x 16384 keys 91 to 97 us, 5.6 to 5.9 TB/s, 85 to 90 % of a measured copy; 16 sequences of 1 to 5003 keys
+// 20.6 us, 3 TB/s; 1 x 1024 keys 8.9 to 9.1 us, which is two launches and their chains of loads (lengths, table, codes; partials).
+// Four CTAs of four warps an SM (two with 16 rows or fp32): one begins or ends a segment while others stream.  16 x 16384 / 16 ragged, in one sitting:
+// one of 14 warps 103 / 25 us, one of 16 98 / 25, two of 7 100 / 22.5, two of 8 92 / 21.6, three of 5 94 / 21.9, four of 4 92 / 21.3.  That leaves 128
+// registers, of which d 128 spills 172 bytes (180 with caps; the merging launch 16 of 64).
+// Weights of bf16 storage in one piece of 11 bits: a second piece, as fp32 storage has, takes 102.4 us where one takes 95.8 (16 ragged 21.5, 20.6; four
+// capped tokens of eight sequences 22.1, 20.1; a step of 32 x 2048 38.4, 36.6).  The results, bf16 themselves, are off by 1.655e-3 to 1.707e-3 of their norm
+// with two, which is their own rounding, and by 1.668e-3 to 1.715e-3 with one: 8 % of them are rounded to the other side.
 // Codes through shared memory (cp.async, a ring for each warp) took 116 us where loads to registers took 101; e4m3 products (m16n8k32) for
 // the scores, whose queries then need three pieces, 115 against 104.
 #include <algorithm>

@@ -19,6 +19,7 @@
 // flight, and the producers' steps (2200 for a tile, two streams); tensor pipe 25 %, issue slots 45 %.  The rest is the first tile (5 us: lengths,
 // table, codes, cold instructions), the segment's end (2 us) and the second launch (3 us).  Without the copies 44 us; one partial for each stream and
 // copy 45; tiles of 128 keys have no room for two places; one fence for K and V 36; e4m3 operands would need e4m3 weights.
+// 576 threads have 96 registers: blocks of 128 rows at d 128 spill 80 bytes of them, with caps 116.
 #include <algorithm>
 
 #include "attend_pages.cuh"

@@ -1,8 +1,8 @@
 // Rotary positions applied to heads that stay in memory.
 //
 // A lane has the pairs of 16-byte chunks of a token's heads: their angles are worked out once for all heads that it takes, up to eight where there
-// are enough lanes.  Reading and writing is the bound: 131072 tokens of 8 heads (537 MB both ways) 83.8 us, 6.4 TB/s, 98 % of a measured copy; 64 tokens
-// of 32 heads 3.3 us, a launch's latency.
+// are enough lanes.  Reading and writing is the bound: 131072 tokens of 8 heads (537 MB both ways) 84 to 86 us, 6.3 TB/s, 96 to 98 % of a measured copy; 64
+// tokens of 32 heads 3.1 to 3.6 us, a launch's latency.
 #include "pages.cuh"
 
 namespace skv {
