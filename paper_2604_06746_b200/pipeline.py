@@ -331,7 +331,7 @@ class PagedDecode:
     """Decoding over a paged cache in 8 bits, for what a Prefill kept or for prompts whose keys come here.  Pages are shared out by
     ``reserve`` and given back by ``release``; page numbers, table and lengths are the same for all layers, of which each has storage of its
     own.  A step is ``step`` for every layer, with one new token a sequence or up to ``max_new``, then ``advance`` by as many as stay:
-    tokens behind ``lengths`` do not count, and the next ones take their slots.  Only ``take`` and ``advance`` move ``lengths``, the latter within
+    tokens behind ``lengths`` do not count, and the next ones take their slots.  Only ``take``, ``advance`` and ``release`` move ``lengths``, ``advance`` within
     the pages that a sequence has.  With a ``rope`` new keys and queries come without positions
     and are rotated on the way.  Every call but ``reserve`` and ``release`` can be captured into a graph.  A sequence without room is left
     as it is, and ``ctx.poll_device_status`` says so.  Rows that are dropped leave something: where one raised the scale of the 16 slots that
